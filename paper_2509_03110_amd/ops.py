@@ -1,0 +1,143 @@
+"""ctypes binding of the operators in include/lsam_ops.h: argument marshalling only.
+
+Tensors are checked for what the C boundary cannot see (device, type, shape, contiguous last index) and handed over
+as they lie, strides included.  Outputs that are not given are allocated on the stream that the call runs on: the
+current stream of x's device, or `stream` (a torch.cuda.Stream).  As with any torch operation, inputs that were made
+on another stream have to be ready on this one, and tensors that are dropped while another stream still reads them
+need record_stream.  Gradients are entry points of their own; nothing here records for autograd.
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+from . import lsam
+from .lsam import EINVAL, LsamError
+
+DTYPE_FP32, DTYPE_BF16 = 0, 1
+
+EXPORTS = ["lsam_dropout"]
+
+
+class lsam_dropout_desc(C.Structure):
+    _fields_ = [
+        ("replicas", C.c_int32), ("dtype", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64),
+        ("x_stride", C.c_int64), ("x_replica", C.c_int64),
+        ("residual_stride", C.c_int64), ("residual_replica", C.c_int64),
+        ("y_stride", C.c_int64), ("y_replica", C.c_int64),
+        ("p", C.c_double), ("seed", C.c_uint64), ("step", C.c_uint32), ("site", C.c_uint32),
+        ("first_replica", C.c_uint32),
+    ]
+
+
+_ready = None
+
+
+def _lib():
+    global _ready
+    if _ready is None:
+        L = lsam.lib()
+        vp = C.c_void_p
+        L.lsam_dropout.restype = C.c_int
+        L.lsam_dropout.argtypes = [C.POINTER(lsam_dropout_desc), vp, vp, vp, vp]
+        _ready = L
+    return _ready
+
+
+def _check(rc):
+    if rc < 0:
+        raise LsamError(rc, lsam.last_error())
+    return rc
+
+
+def _refuse(msg):
+    raise LsamError(EINVAL, msg)
+
+
+_types = None
+
+
+def _dtype(t, what):
+    global _types
+    if _types is None:
+        import torch
+        _types = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
+    code = _types.get(t.dtype)
+    if code is None:
+        _refuse("%s is %s: float32 or bfloat16 is wanted" % (what, t.dtype))
+    return code
+
+
+def _expect(t, what, like=None, shape=None, dtype=None, dense=False):
+    """Whether `t` is a tensor of that device, shape and type with a contiguous last index (dense: all of it)."""
+    if like is not None and t.device != like.device:
+        _refuse("%s is on %s, not on %s" % (what, t.device, like.device))
+    if not t.is_cuda:
+        _refuse("%s is not on a GPU" % what)
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        _refuse("%s has shape %s: %s is wanted" % (what, tuple(t.shape), tuple(shape)))
+    if dtype is not None and t.dtype != dtype:
+        _refuse("%s is %s: %s is wanted" % (what, t.dtype, dtype))
+    if dense:
+        if not t.is_contiguous():
+            _refuse("%s must be contiguous" % what)
+    elif t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        _refuse("the last index of %s must be contiguous" % what)
+
+
+class _On:
+    """The device and stream that a call runs on, current while it lasts; `.raw` is the stream's handle."""
+
+    def __init__(self, t, stream):
+        import torch
+        self.device, self.context = t.device, None
+        if stream is not None:
+            if stream.device != t.device:
+                _refuse("the stream belongs to %s, the tensors to %s" % (stream.device, t.device))
+            self.context = torch.cuda.stream(stream)
+        elif torch.cuda.current_device() != t.device.index:
+            self.context = torch.cuda.device(t.device)
+
+    def __enter__(self):
+        import torch
+        if self.context is not None:
+            self.context.__enter__()
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def __exit__(self, *err):
+        if self.context is not None:
+            self.context.__exit__(*err)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def dropout(x, p, seed, step, site=0, first_replica=0, residual=None, out=None, stream=None):
+    """residual + m x / (1 - p) with the mask m of (seed, step, site, place); see lsam_dropout.  x: [K, rows, cols]
+    of K replicas, [rows, cols] or [cols] of one.  The gradient of x is the same call on the gradient of the result,
+    with no residual.  `out` may be x or the residual."""
+    import torch
+    if not 1 <= x.dim() <= 3:
+        _refuse("x has %d indices: 1 to 3 are wanted" % x.dim())
+    _expect(x, "x")
+    for t, what in ((residual, "the residual"), (out, "out")):
+        if t is not None:
+            _expect(t, what, like=x, shape=x.shape, dtype=x.dtype)
+    d = lsam_dropout_desc()
+    d.dtype = _dtype(x, "x")
+    shape = (1,) * (3 - x.dim()) + tuple(x.shape)
+    d.replicas, d.rows, d.cols = shape
+    if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 32 and 0 <= site < 1 << 16 and 0 <= first_replica < 1 << 16):
+        _refuse("the seed has 64 bits, the step 32, the site and the replica 16")
+    d.p, d.seed, d.step, d.site, d.first_replica = p, seed, step, site, first_replica
+
+    def strides(t):
+        return (0,) * (2 - t.dim() + 1) + tuple(t.stride()) if t.dim() < 3 else t.stride()
+    with _On(x, stream) as raw:
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+        d.x_replica, d.x_stride = strides(x)[:2]
+        d.y_replica, d.y_stride = strides(y)[:2]
+        if residual is not None:
+            d.residual_replica, d.residual_stride = strides(residual)[:2]
+        _check(_lib().lsam_dropout(C.byref(d), x.data_ptr(), _ptr(residual), y.data_ptr(), raw))
+    return y

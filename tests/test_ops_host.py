@@ -1,0 +1,50 @@
+"""CPU-only checks of the operators' boundary: declared symbols are exported and bad arguments are refused on the
+host, before anything reaches a GPU."""
+import ctypes as C
+import os
+import re
+
+from paper_2509_03110_amd import lsam, ops
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+FAKE = 1 << 20           # never dereferenced: the checks fail first, or nothing is to be done
+
+
+def test_library_exports_every_declared_operator():
+    header = open(os.path.join(ROOT, "include", "lsam_ops.h")).read()
+    declared = set(re.findall(r"^(?:int|size_t|int64_t) (lsam_[a-z_]+)\s*\(", header, re.M))
+    assert declared == set(ops.EXPORTS)
+    L = lsam.lib()
+    for name in declared:
+        assert hasattr(L, name), name
+
+
+def _dropout(**over):
+    d = ops.lsam_dropout_desc()
+    d.replicas, d.dtype, d.rows, d.cols, d.p = 2, ops.DTYPE_FP32, 4, 16, 0.5
+    d.x_stride = d.y_stride = d.residual_stride = 16
+    d.x_replica = d.y_replica = d.residual_replica = 64
+    for k, v in over.items():
+        setattr(d, k, v)
+    return d
+
+
+def test_dropout_checks_its_arguments_before_touching_the_gpu():
+    call = ops._lib().lsam_dropout
+    for over, msg in ((dict(dtype=2), "dtype"), (dict(replicas=-1), "replicas"), (dict(replicas=65536), "replicas"),
+                      (dict(rows=-1), "rows"), (dict(cols=1 << 31), "cols"), (dict(p=2.0), "p outside"),
+                      (dict(p=float("nan")), "p outside"), (dict(site=65536), "site"), (dict(first_replica=65535), "replicas"),
+                      (dict(x_stride=15), "stride"), (dict(y_replica=63), "lie over each other"), (dict(x_replica=-1), "stride"),
+                      (dict(rows=(1 << 31) - 1, x_stride=1 << 62), "too large")):
+        d = _dropout(**over)
+        assert call(C.byref(d), FAKE, None, 4 * FAKE, None) == lsam.EINVAL, over
+        assert msg in lsam.last_error(), (over, lsam.last_error())
+    d = _dropout()
+    assert call(None, FAKE, None, FAKE, None) == lsam.EINVAL
+    assert call(C.byref(d), None, None, FAKE, None) == lsam.EINVAL
+    assert call(C.byref(d), FAKE, None, None, None) == lsam.EINVAL
+    assert call(C.byref(d), FAKE, None, FAKE + 4, None) == lsam.EINVAL and "lies over x" in lsam.last_error()
+    assert call(C.byref(d), FAKE, 4 * FAKE + 64, 4 * FAKE, None) == lsam.EINVAL and "residual" in lsam.last_error()
+    assert call(C.byref(d), FAKE + 2, None, 4 * FAKE, None) == lsam.EINVAL and "aligned" in lsam.last_error()
+    for over in (dict(rows=0), dict(cols=0), dict(replicas=0)):
+        assert call(C.byref(_dropout(**over)), None, None, None, None) == 0
