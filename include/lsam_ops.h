@@ -55,6 +55,40 @@ typedef struct {
 } lsam_dropout_desc;
 int lsam_dropout(const lsam_dropout_desc* d, const void* x, const void* residual, void* y, void* stream);
 
+/* ---- log probabilities of given tokens --------------------------------------------------------
+ * For each of `rows` rows of logits z [vocab] (dtype), with sums in fp32:
+ *   lse     [device] [rows, 2] floats: the largest logit m, and ln sum_j e^{z_j - m}.  The log normaliser is their sum;
+ *           ln p_j = (z_j - m) - ln sum e^{z - m} keeps its digits however large the logits are
+ *   entropy [device] [rows] floats: H = -sum_j p_j ln p_j, p = e^{z - lse}
+ *   logp    [device] [rows] floats: ln p of tokens[row]; 0 for a token outside 0..vocab-1, which does not count.
+ *           tokens [device] [rows] int32, or NULL: logp is not written
+ *   top_ids, top_logp [device] [rows, top]: the `top` largest logits' indices and log probabilities, the largest first, the
+ *           lowest index first among equals.  May be NULL where top = 0
+ * A logit of -inf is barred: probability 0, gradient 0, never an alternative; where fewer than `top` are left the
+ * rest is index -1, log probability -inf.  A row with every logit barred has lse (-inf, 0), entropy 0, logp -inf and
+ * no gradient.  NaN or +inf in a row makes its lse, entropy and log probabilities NaN.
+ * workspace [device, 16-byte aligned], lsam_logprobs_workspace_bytes(d) bytes (0 where rows fill the chip; also 0, with a
+ * message, for a descriptor that is refused); nothing in it has to survive the call. */
+#define LSAM_TOP_MAX 32
+typedef struct {
+  int64_t rows;
+  int64_t vocab;                             /* 1..2^31-1                                    */
+  int64_t stride;                            /* of the logits, from row to row               */
+  int32_t dtype;                             /* LSAM_DTYPE_*                                 */
+  int32_t top;                               /* 0..LSAM_TOP_MAX, at most vocab               */
+} lsam_logprobs_desc;
+size_t lsam_logprobs_workspace_bytes(const lsam_logprobs_desc* d);
+int lsam_logprobs(const lsam_logprobs_desc* d, const void* logits, const int32_t* tokens, float* logp, float* lse,
+                  float* entropy, int32_t* top_ids, float* top_logp, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradient of sum_rows g_logp logp + g_entropy entropy with respect to the logits:
+ *   dlogits_j = g_logp (1[j = token] - p_j) - g_entropy p_j (ln p_j + H)
+ * g_logp, g_entropy [device] [rows] floats, either may be NULL (0); lse and entropy as the forward call left them.
+ * dlogits has the logits' type and may be the logits themselves. `top` is not looked at beyond its range. */
+int lsam_logprobs_backward(const lsam_logprobs_desc* d, const void* logits, const int32_t* tokens, const float* lse,
+                           const float* entropy, const float* g_logp, const float* g_entropy, void* dlogits,
+                           int64_t dlogits_stride, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -9,13 +9,16 @@ need record_stream.  Gradients are entry points of their own; nothing here recor
 from __future__ import annotations
 
 import ctypes as C
+from collections import namedtuple
 
 from . import lsam
 from .lsam import EINVAL, LsamError
 
 DTYPE_FP32, DTYPE_BF16 = 0, 1
 
-EXPORTS = ["lsam_dropout"]
+TOP_MAX = 32
+
+EXPORTS = ["lsam_dropout", "lsam_logprobs_workspace_bytes", "lsam_logprobs", "lsam_logprobs_backward"]
 
 
 class lsam_dropout_desc(C.Structure):
@@ -29,6 +32,10 @@ class lsam_dropout_desc(C.Structure):
     ]
 
 
+class lsam_logprobs_desc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("vocab", C.c_int64), ("stride", C.c_int64), ("dtype", C.c_int32), ("top", C.c_int32)]
+
+
 _ready = None
 
 
@@ -39,6 +46,12 @@ def _lib():
         vp = C.c_void_p
         L.lsam_dropout.restype = C.c_int
         L.lsam_dropout.argtypes = [C.POINTER(lsam_dropout_desc), vp, vp, vp, vp]
+        L.lsam_logprobs_workspace_bytes.restype = C.c_size_t
+        L.lsam_logprobs_workspace_bytes.argtypes = [C.POINTER(lsam_logprobs_desc)]
+        L.lsam_logprobs.restype = C.c_int
+        L.lsam_logprobs.argtypes = [C.POINTER(lsam_logprobs_desc)] + [vp] * 8 + [C.c_size_t, vp]
+        L.lsam_logprobs_backward.restype = C.c_int
+        L.lsam_logprobs_backward.argtypes = [C.POINTER(lsam_logprobs_desc)] + [vp] * 7 + [C.c_int64, vp]
         _ready = L
     return _ready
 
@@ -141,3 +154,56 @@ def dropout(x, p, seed, step, site=0, first_replica=0, residual=None, out=None, 
             d.residual_replica, d.residual_stride = strides(residual)[:2]
         _check(_lib().lsam_dropout(C.byref(d), x.data_ptr(), _ptr(residual), y.data_ptr(), raw))
     return y
+
+
+LogProbs = namedtuple("LogProbs", "logp lse entropy top_ids top_logp")
+
+
+def _logprobs_desc(logits, top):
+    if logits.dim() != 2:
+        _refuse("the logits have %d indices: [rows, vocab] is wanted" % logits.dim())
+    _expect(logits, "logits")
+    d = lsam_logprobs_desc()
+    d.rows, d.vocab = logits.shape
+    d.stride, d.dtype, d.top = logits.stride(0), _dtype(logits, "logits"), top
+    return d
+
+
+def logprobs(logits, tokens=None, top=0, stream=None):
+    """Log probabilities of tokens [rows] (int32; one outside the vocabulary does not count: 0) under logits
+    [rows, vocab], with the log normaliser in two parts lse [rows, 2] (the largest logit m, and ln sum e^{z - m}), the
+    entropy [rows], and the `top` largest logits' indices and log probabilities [rows, top]; see lsam_logprobs.  Fields that were not asked for
+    are None."""
+    import torch
+    d = _logprobs_desc(logits, top)
+    if tokens is not None:
+        _expect(tokens, "tokens", like=logits, shape=(d.rows,), dtype=torch.int32, dense=True)
+    with _On(logits, stream) as raw:
+        new = lambda *shape, t=torch.float32: torch.empty(shape, dtype=t, device=logits.device)  # noqa: E731
+        need = _lib().lsam_logprobs_workspace_bytes(C.byref(d))
+        ws = new(need, t=torch.uint8) if need else None
+        r = LogProbs(None if tokens is None else new(d.rows), new(d.rows, 2), new(d.rows),
+                     new(d.rows, top, t=torch.int32) if top > 0 else None, new(d.rows, top) if top > 0 else None)
+        _check(_lib().lsam_logprobs(C.byref(d), logits.data_ptr(), _ptr(tokens), _ptr(r.logp), r.lse.data_ptr(),
+                                    r.entropy.data_ptr(), _ptr(r.top_ids), _ptr(r.top_logp), _ptr(ws), need, raw))
+    return r
+
+
+def logprobs_backward(logits, tokens, lse, entropy, g_logp=None, g_entropy=None, out=None, stream=None):
+    """Gradient of sum g_logp logp + g_entropy entropy with respect to the logits, in their type; `out` may be the logits.
+    lse and entropy are those of `logprobs`; see lsam_logprobs_backward."""
+    import torch
+    d = _logprobs_desc(logits, 0)
+    if tokens is not None:
+        _expect(tokens, "tokens", like=logits, shape=(d.rows,), dtype=torch.int32, dense=True)
+    _expect(lse, "lse", like=logits, shape=(d.rows, 2), dtype=torch.float32, dense=True)
+    for t, what in ((entropy, "the entropy"), (g_logp, "g_logp"), (g_entropy, "g_entropy")):
+        if t is not None:
+            _expect(t, what, like=logits, shape=(d.rows,), dtype=torch.float32, dense=True)
+    if out is not None:
+        _expect(out, "out", like=logits, shape=logits.shape, dtype=logits.dtype)
+    with _On(logits, stream) as raw:
+        dz = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device) if out is None else out
+        _check(_lib().lsam_logprobs_backward(C.byref(d), logits.data_ptr(), _ptr(tokens), lse.data_ptr(), _ptr(entropy),
+                                             _ptr(g_logp), _ptr(g_entropy), dz.data_ptr(), dz.stride(0), raw))
+    return dz

@@ -48,3 +48,36 @@ def test_dropout_checks_its_arguments_before_touching_the_gpu():
     assert call(C.byref(d), FAKE + 2, None, 4 * FAKE, None) == lsam.EINVAL and "aligned" in lsam.last_error()
     for over in (dict(rows=0), dict(cols=0), dict(replicas=0)):
         assert call(C.byref(_dropout(**over)), None, None, None, None) == 0
+
+
+def test_logprobs_checks_its_arguments_before_touching_the_gpu():
+    L = ops._lib()
+
+    def desc(**over):
+        d = ops.lsam_logprobs_desc()
+        d.rows, d.vocab, d.stride, d.dtype, d.top = 4, 1000, 1000, ops.DTYPE_BF16, 5
+        for k, v in over.items():
+            setattr(d, k, v)
+        return C.byref(d)
+    for over, msg in ((dict(dtype=5), "dtype"), (dict(rows=-1), "rows"), (dict(vocab=0), "vocab"), (dict(vocab=1 << 31), "vocab"),
+                      (dict(top=33), "top"), (dict(top=-1), "top"), (dict(vocab=4, top=5), "top"), (dict(stride=999), "stride"),
+                      (dict(rows=1 << 40, stride=1 << 40), "too large")):
+        assert L.lsam_logprobs(desc(**over), FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, None, 0, None) == lsam.EINVAL, over
+        assert msg in lsam.last_error(), (over, lsam.last_error())
+        assert L.lsam_logprobs_workspace_bytes(desc(**over)) == 0
+        assert L.lsam_logprobs_backward(desc(**over), FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 8 * FAKE, 1000, None) == lsam.EINVAL, over
+    need = L.lsam_logprobs_workspace_bytes(desc(vocab=100_000, stride=100_000))
+    assert need > 0 and L.lsam_logprobs_workspace_bytes(desc()) == 0 and L.lsam_logprobs_workspace_bytes(desc(rows=5000)) == 0
+    big = desc(vocab=100_000, stride=100_000)
+    assert L.lsam_logprobs(big, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, need - 1, None) == lsam.ENOMEM
+    assert L.lsam_logprobs(big, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, None, need, None) == lsam.ENOMEM
+    assert L.lsam_logprobs(big, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE + 8, need, None) == lsam.EINVAL
+    assert L.lsam_logprobs(desc(), None, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, None, 0, None) == lsam.EINVAL
+    assert L.lsam_logprobs(desc(), FAKE, FAKE, None, FAKE, FAKE, FAKE, FAKE, None, 0, None) == lsam.EINVAL
+    assert L.lsam_logprobs(desc(), FAKE, FAKE, FAKE, FAKE, FAKE, None, FAKE, None, 0, None) == lsam.EINVAL
+    assert L.lsam_logprobs(desc(), FAKE + 1, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, None, 0, None) == lsam.EINVAL
+    assert L.lsam_logprobs_backward(desc(), FAKE, None, FAKE, FAKE, FAKE, FAKE, 8 * FAKE, 1000, None) == lsam.EINVAL
+    assert L.lsam_logprobs_backward(desc(), FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE + 16, 1000, None) == lsam.EINVAL
+    assert L.lsam_logprobs_backward(desc(), FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 8 * FAKE, 999, None) == lsam.EINVAL
+    assert L.lsam_logprobs(desc(rows=0), None, None, None, None, None, None, None, None, 0, None) == 0
+    assert L.lsam_logprobs_backward(desc(rows=0), None, None, None, None, None, None, None, 1000, None) == 0
