@@ -89,6 +89,47 @@ int lsam_logprobs_backward(const lsam_logprobs_desc* d, const void* logits, cons
                            const float* entropy, const float* g_logp, const float* g_entropy, void* dlogits,
                            int64_t dlogits_stride, void* stream);
 
+/* ---- gated linear recurrence -------------------------------------------------------------------
+ * For every sequence and channel:  h_t = a_t h_{t-1} + (1 - a_t) x_t,  a_t = 1 / (1 + e^{-f_t}),  t = 0, 1, ...,
+ * from h_{-1} = h0.  States and sums are fp32; h, df and dx are rounded once, where they are stored.
+ *
+ * Sequences of equal length (packed = 0): f, x, h are `seqs` matrices [rows, dim]; rows = 1 is a step of generation.
+ * Packed sequences of any lengths (packed = 1): f, x, h are one matrix [rows, dim], and sequence i is rows offsets[i] to
+ * offsets[i + 1] - 1 of it (offsets [device] [seqs + 1] int64, not decreasing, within 0..rows: values outside are
+ * taken as the nearest inside).  Rows of no sequence are neither read nor written.  A sequence of no rows leaves its
+ * state as it is.
+ *   h0     [device] [seqs, dim] floats, or NULL: 0
+ *   last   [device] [seqs, dim] floats that receive the states after the last row, or NULL
+ *   states [device] [lsam_recurrence_states(d), dim] floats that receive what the backward pass needs, or NULL
+ * workspace [device, 16-byte aligned], lsam_recurrence_workspace_bytes(d) bytes (0 where sequences and channels fill the
+ * chip; also 0, with a message, for a descriptor that is refused); nothing in it has to survive a call. */
+typedef struct {
+  int64_t stride;                            /* from row to row, at least dim                */
+  int64_t seq;                               /* from sequence to sequence; packed: not used  */
+} lsam_rows;
+typedef struct {
+  int64_t seqs;
+  int64_t rows;                              /* of each sequence; packed: of all             */
+  int64_t dim;
+  int32_t dtype;                             /* LSAM_DTYPE_* of f, x, h, dh, df, dx          */
+  int32_t packed;
+  lsam_rows f, x, h;                         /* h: not looked at by the backward pass        */
+  lsam_rows dh, df, dx;                      /* not looked at by the forward pass            */
+} lsam_recurrence_desc;
+size_t lsam_recurrence_workspace_bytes(const lsam_recurrence_desc* d);
+int64_t lsam_recurrence_states(const lsam_recurrence_desc* d);
+int lsam_recurrence(const lsam_recurrence_desc* d, const int64_t* offsets, const void* f, const void* x, const float* h0,
+                    void* h, float* last, float* states, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients of sum dh h + dlast last with respect to f, x and h0:
+ *   e_t = a_t (dh_t + e_{t+1}) from e = dlast behind the last row,  d_t = dh_t + e_{t+1},
+ *   dx_t = (1 - a_t) d_t,  df_t = a_t (1 - a_t) d_t (h_{t-1} - x_t),  dh0 = e_0.
+ * seqs, rows, dim, dtype, packed, offsets, h0 and states are those of the forward call; dlast [device] [seqs, dim] floats or
+ * NULL (0); dh0 [device] [seqs, dim] floats or NULL (not wanted). */
+int lsam_recurrence_backward(const lsam_recurrence_desc* d, const int64_t* offsets, const void* f, const void* x,
+                             const float* h0, const float* states, const void* dh, const float* dlast, void* df, void* dx,
+                             float* dh0, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -39,6 +39,12 @@ inline int64_t extent(int64_t mats, int64_t mat_stride, int64_t rows, int64_t st
   const __int128 n = ((__int128)(mats - 1) * (mats > 1 ? mat_stride : 0) + (__int128)(rows - 1) * (rows > 1 ? stride : 0) + cols) * bytes;
   return n < ((__int128)1 << 46) ? (int64_t)n : -1;
 }
+// Whether the matrices of an output lie apart: one behind the other, or row by row side by side.
+inline bool apart(int64_t mats, int64_t mat_stride, int64_t rows, int64_t stride, int64_t cols) {
+  if (mats <= 1 || rows <= 0 || cols <= 0) return true;
+  const __int128 matrix = (__int128)(rows - 1) * (rows > 1 ? stride : 0) + cols, row = (__int128)(mats - 1) * mat_stride + cols;
+  return mat_stride >= cols && ((__int128)mat_stride >= matrix || rows == 1 || (__int128)stride >= row);
+}
 inline bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return na > 0 && nb > 0 && x < y + (uintptr_t)nb && y < x + (uintptr_t)na;

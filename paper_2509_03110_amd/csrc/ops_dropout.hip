@@ -81,7 +81,7 @@ extern "C" int lsam_dropout(const lsam_dropout_desc* d, const void* x, const voi
   const int64_t ny = extent(d->replicas, d->y_replica, d->rows, d->y_stride, d->cols, bytes);
   const bool many = d->replicas > 1, tall = d->rows > 1;
   if (nx < 0 || nr < 0 || ny < 0) return refuse(LSAM_EINVAL, "dropout: a row stride is below cols, or an array is too large");
-  if (many && d->y_replica < (d->rows - 1) * (tall ? d->y_stride : 0) + d->cols)
+  if (!apart(d->replicas, d->y_replica, d->rows, d->y_stride, d->cols))
     return refuse(LSAM_EINVAL, "dropout: the replicas of y lie over each other");
   if (overlap(x, nx, y, ny) && !(x == y && (!tall || d->x_stride == d->y_stride) && (!many || d->x_replica == d->y_replica)))
     return refuse(LSAM_EINVAL, "dropout: y lies over x without being x");

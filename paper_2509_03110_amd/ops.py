@@ -18,7 +18,8 @@ DTYPE_FP32, DTYPE_BF16 = 0, 1
 
 TOP_MAX = 32
 
-EXPORTS = ["lsam_dropout", "lsam_logprobs_workspace_bytes", "lsam_logprobs", "lsam_logprobs_backward"]
+EXPORTS = ["lsam_dropout", "lsam_logprobs_workspace_bytes", "lsam_logprobs", "lsam_logprobs_backward",
+           "lsam_recurrence_workspace_bytes", "lsam_recurrence_states", "lsam_recurrence", "lsam_recurrence_backward"]
 
 
 class lsam_dropout_desc(C.Structure):
@@ -34,6 +35,15 @@ class lsam_dropout_desc(C.Structure):
 
 class lsam_logprobs_desc(C.Structure):
     _fields_ = [("rows", C.c_int64), ("vocab", C.c_int64), ("stride", C.c_int64), ("dtype", C.c_int32), ("top", C.c_int32)]
+
+
+class lsam_rows(C.Structure):
+    _fields_ = [("stride", C.c_int64), ("seq", C.c_int64)]
+
+
+class lsam_recurrence_desc(C.Structure):
+    _fields_ = [("seqs", C.c_int64), ("rows", C.c_int64), ("dim", C.c_int64), ("dtype", C.c_int32), ("packed", C.c_int32),
+                ("f", lsam_rows), ("x", lsam_rows), ("h", lsam_rows), ("dh", lsam_rows), ("df", lsam_rows), ("dx", lsam_rows)]
 
 
 _ready = None
@@ -52,6 +62,15 @@ def _lib():
         L.lsam_logprobs.argtypes = [C.POINTER(lsam_logprobs_desc)] + [vp] * 8 + [C.c_size_t, vp]
         L.lsam_logprobs_backward.restype = C.c_int
         L.lsam_logprobs_backward.argtypes = [C.POINTER(lsam_logprobs_desc)] + [vp] * 7 + [C.c_int64, vp]
+        rec = C.POINTER(lsam_recurrence_desc)
+        L.lsam_recurrence_workspace_bytes.restype = C.c_size_t
+        L.lsam_recurrence_workspace_bytes.argtypes = [rec]
+        L.lsam_recurrence_states.restype = C.c_int64
+        L.lsam_recurrence_states.argtypes = [rec]
+        L.lsam_recurrence.restype = C.c_int
+        L.lsam_recurrence.argtypes = [rec] + [vp] * 8 + [C.c_size_t, vp]
+        L.lsam_recurrence_backward.restype = C.c_int
+        L.lsam_recurrence_backward.argtypes = [rec] + [vp] * 11 + [C.c_size_t, vp]
         _ready = L
     return _ready
 
@@ -207,3 +226,83 @@ def logprobs_backward(logits, tokens, lse, entropy, g_logp=None, g_entropy=None,
         _check(_lib().lsam_logprobs_backward(C.byref(d), logits.data_ptr(), _ptr(tokens), lse.data_ptr(), _ptr(entropy),
                                              _ptr(g_logp), _ptr(g_entropy), dz.data_ptr(), dz.stride(0), raw))
     return dz
+
+
+Recurrence = namedtuple("Recurrence", "h last states")
+
+
+def _recurrence_desc(f, x, h0, offsets):
+    import torch
+    if f.dim() != (3 if offsets is None else 2):
+        _refuse("f has %d indices: [seqs, rows, dim] is wanted, or [rows, dim] with offsets" % f.dim())
+    _expect(f, "f")
+    _expect(x, "x", like=f, shape=f.shape, dtype=f.dtype)
+    d = lsam_recurrence_desc()
+    d.dtype = _dtype(f, "f")
+    if offsets is None:
+        d.seqs, d.rows, d.dim = f.shape
+    else:
+        if offsets.dim() != 1 or offsets.shape[0] < 1:
+            _refuse("the offsets must be [seqs + 1]")
+        _expect(offsets, "the offsets", like=f, dtype=torch.int64, dense=True)
+        d.packed, d.seqs, (d.rows, d.dim) = 1, offsets.shape[0] - 1, f.shape
+    if h0 is not None:
+        _expect(h0, "h0", like=f, shape=(d.seqs, d.dim), dtype=torch.float32, dense=True)
+    _rows(d.f, f)
+    _rows(d.x, x)
+    return d
+
+
+def _rows(at, t):
+    at.seq, at.stride = (0, t.stride(0)) if t.dim() == 2 else t.stride()[:2]
+
+
+def recurrence(f, x, h0=None, offsets=None, save=False, out=None, stream=None):
+    """h_t = a_t h_{t-1} + (1 - a_t) x_t with a = sigmoid(f), along sequences of equal length (f, x: [seqs, rows, dim]) or
+    packed ones (f, x: [rows, dim], offsets: int64 [seqs + 1]); see lsam_recurrence.  Returns h in x's type, the last
+    states [seqs, dim] in fp32, and with `save` the states that `recurrence_backward` takes (else None).  Rows of no
+    sequence are not written."""
+    import torch
+    d = _recurrence_desc(f, x, h0, offsets)
+    if out is not None:
+        _expect(out, "out", like=f, shape=f.shape, dtype=f.dtype)
+    with _On(f, stream) as raw:
+        new = lambda *shape, t=torch.float32: torch.empty(shape, dtype=t, device=f.device)  # noqa: E731
+        h = new(*f.shape, t=f.dtype) if out is None else out
+        _rows(d.h, h)
+        last = new(d.seqs, d.dim)
+        states = new(_check(_lib().lsam_recurrence_states(C.byref(d))), d.dim) if save else None
+        need = _lib().lsam_recurrence_workspace_bytes(C.byref(d))
+        ws = new(need, t=torch.uint8) if need else None
+        _check(_lib().lsam_recurrence(C.byref(d), _ptr(offsets), f.data_ptr(), x.data_ptr(), _ptr(h0), h.data_ptr(),
+                                      last.data_ptr(), _ptr(states), _ptr(ws), need, raw))
+    return Recurrence(h, last, states)
+
+
+def recurrence_backward(f, x, dh, states, h0=None, dlast=None, offsets=None, df=None, dx=None, stream=None):
+    """Gradients (df, dx, dh0) of sum dh h + dlast last; `states` are those that `recurrence` saved for the same f, x, h0 and
+    offsets.  df and dx have x's type, dh0 is fp32.  Rows of no sequence are not written."""
+    import torch
+    d = _recurrence_desc(f, x, h0, offsets)
+    _expect(dh, "dh", like=f, shape=f.shape, dtype=f.dtype)
+    if dlast is not None:
+        _expect(dlast, "dlast", like=f, shape=(d.seqs, d.dim), dtype=torch.float32, dense=True)
+    for t, what in ((df, "df"), (dx, "dx")):
+        if t is not None:
+            _expect(t, what, like=f, shape=f.shape, dtype=f.dtype)
+    _expect(states, "the states", like=f, shape=(_check(_lib().lsam_recurrence_states(C.byref(d))), d.dim), dtype=torch.float32,
+            dense=True)
+    with _On(f, stream) as raw:
+        new = lambda *shape, t=torch.float32: torch.empty(shape, dtype=t, device=f.device)  # noqa: E731
+        df = new(*f.shape, t=f.dtype) if df is None else df
+        dx = new(*f.shape, t=f.dtype) if dx is None else dx
+        dh0 = new(d.seqs, d.dim)
+        _rows(d.dh, dh)
+        _rows(d.df, df)
+        _rows(d.dx, dx)
+        need = _lib().lsam_recurrence_workspace_bytes(C.byref(d))
+        ws = new(need, t=torch.uint8) if need else None
+        _check(_lib().lsam_recurrence_backward(C.byref(d), _ptr(offsets), f.data_ptr(), x.data_ptr(), _ptr(h0), states.data_ptr(),
+                                               dh.data_ptr(), _ptr(dlast), df.data_ptr(), dx.data_ptr(), dh0.data_ptr(), _ptr(ws),
+                                               need, raw))
+    return df, dx, dh0

@@ -81,3 +81,47 @@ def test_logprobs_checks_its_arguments_before_touching_the_gpu():
     assert L.lsam_logprobs_backward(desc(), FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 8 * FAKE, 999, None) == lsam.EINVAL
     assert L.lsam_logprobs(desc(rows=0), None, None, None, None, None, None, None, None, 0, None) == 0
     assert L.lsam_logprobs_backward(desc(rows=0), None, None, None, None, None, None, None, 1000, None) == 0
+
+
+def test_recurrence_checks_its_arguments_before_touching_the_gpu():
+    L = ops._lib()
+
+    def desc(**over):
+        d = ops.lsam_recurrence_desc()
+        d.seqs, d.rows, d.dim, d.dtype, d.packed = 2, 30, 10, ops.DTYPE_FP32, 0
+        for t in ("f", "x", "h", "dh", "df", "dx"):
+            getattr(d, t).stride, getattr(d, t).seq = 10, 300
+        for k, v in over.items():
+            if k.endswith("_seq") or k.endswith("_stride"):
+                setattr(getattr(d, k.split("_")[0]), k.split("_")[1], v)
+            else:
+                setattr(d, k, v)
+        return C.byref(d)
+    P = [FAKE * k for k in range(1, 13)]
+
+    def forward(d, off=None, f=P[0], x=P[1], h0=None, h=P[2], last=P[3], states=P[4], ws=None, n=0):
+        return L.lsam_recurrence(d, off, f, x, h0, h, last, states, ws, n, None)
+
+    def backward(d, off=None, f=P[0], x=P[1], h0=None, states=P[4], dh=P[5], dlast=None, df=P[6], dx=P[7], dh0=P[8], ws=None, n=0):
+        return L.lsam_recurrence_backward(d, off, f, x, h0, states, dh, dlast, df, dx, dh0, ws, n, None)
+    for over, msg in ((dict(dtype=-1), "dtype"), (dict(packed=2), "packed"), (dict(seqs=-1), "seqs"), (dict(rows=-1), "rows"),
+                      (dict(dim=0), "dim"), (dict(rows=1 << 39, seqs=1 << 30), "too large"), (dict(seqs=1 << 30, dim=1 << 20), "too large"),
+                      (dict(f_stride=9), "stride of f"), (dict(x_seq=-1), "stride of x")):
+        assert forward(desc(**over)) == lsam.EINVAL and msg in lsam.last_error(), (over, lsam.last_error())
+        assert backward(desc(**over)) == lsam.EINVAL and msg in lsam.last_error(), (over, lsam.last_error())
+    assert forward(desc(h_seq=299)) == lsam.EINVAL and "stride of h" in lsam.last_error()
+    assert backward(desc(df_seq=5)) == lsam.EINVAL and "stride of df" in lsam.last_error()
+    assert forward(desc(packed=1)) == lsam.EINVAL and "offsets" in lsam.last_error()
+    assert forward(desc(), h=P[1]) == lsam.EINVAL and "lies over" in lsam.last_error()
+    assert forward(desc(), last=P[4] + 40) == lsam.EINVAL and "lies over" in lsam.last_error()
+    assert forward(desc(), f=None) == lsam.EINVAL and forward(desc(), h=None) == lsam.EINVAL
+    assert forward(desc(), h0=FAKE + 2) == lsam.EINVAL and "aligned" in lsam.last_error()
+    assert backward(desc(), states=None) == lsam.EINVAL and backward(desc(), dx=P[6]) == lsam.EINVAL
+    long = desc(rows=100_000, f_seq=1 << 20, x_seq=1 << 20, h_seq=1 << 20, dh_seq=1 << 20, df_seq=1 << 20, dx_seq=1 << 20)
+    need = L.lsam_recurrence_workspace_bytes(long)
+    far = dict(f=1 << 30, x=2 << 30, h=3 << 30, last=4 << 30, states=5 << 30)
+    assert need > 0 and L.lsam_recurrence_workspace_bytes(desc()) == 0
+    assert forward(long, **far) == lsam.ENOMEM and forward(long, ws=6 << 30, n=need - 1, **far) == lsam.ENOMEM
+    assert forward(long, ws=(6 << 30) + 4, n=need, **far) == lsam.EINVAL
+    assert L.lsam_recurrence_states(desc()) == 2 and L.lsam_recurrence_states(desc(dim=0)) == lsam.EINVAL
+    assert forward(desc(seqs=0), f=None, x=None, h=None) == 0 and backward(desc(seqs=0), f=None) == 0
