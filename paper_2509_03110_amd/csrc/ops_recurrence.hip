@@ -2,8 +2,8 @@
 // every sequence, and its gradient.
 //
 // A run of steps maps the state that enters it to A h + H, A the product of its a_t and H what it makes of 0; runs
-// are joined by (A, H) then (A', H') = (A A', A' H + H').  A workgroup owns 128 neighbouring channels of a sequence and
-// goes along time in tiles: each wavefront takes a few rows of the tile into registers (two channels a lane), finds
+// are joined by (A, H) then (A', H') = (A A', A' H + H').  A workgroup owns 64 neighbouring channels of a sequence and
+// goes along time in tiles: each wavefront takes a few rows of the tile into registers (a channel a lane), finds
 // its own (A, H), and from those of the wavefronts before it, exchanged through LDS, the state that enters its rows.
 // So every value is read once and written once.  Where sequences and channels are too few to fill the chip, the
 // tiles of a sequence are cut into runs for several workgroups: a first launch leaves (A, H) of every run.
@@ -16,10 +16,11 @@
 namespace lsam {
 namespace {
 
-constexpr int kRows = 8;             // rows of a tile that one wavefront takes
-constexpr int kChannels = 128;       // of a workgroup: two for each lane
+constexpr int kRows = 16;            // rows of a tile that one wavefront takes
+constexpr int kChannels = 64;        // of a workgroup: one for each lane
 constexpr int kWaves = 8;            // of a workgroup; one where sequences are no longer than its rows
 constexpr int kMaxSplits = 64;
+constexpr int kTogether = 8;         // workgroups of neighbouring channels that share an XCD
 
 struct Tensor { const void* p; int64_t stride, seq; };
 
@@ -27,37 +28,13 @@ struct RecurrenceParams {
   Tensor f, x, h, dh, df, dx;
   const int64_t* offsets;            // packed sequences: seqs + 1 row numbers, else null
   int64_t seq0, rows, D;             // rows of each sequence, or of all
+  unsigned seqs;                     // of this launch
   int64_t tiles_of_each;             // saved states of a sequence (not packed)
   int splits, slabs;
+  int64_t run_tiles;                 // tiles of a run
   const float* h0; float* last; float* states;
   const float* dlast; float* dh0;
   float* runs;                       // [seqs][splits][2][D]: A and H (or E) of every run
-};
-
-template <int DTYPE> struct Pair;
-template <> struct Pair<LSAM_DTYPE_FP32> {
-  typedef f32x2 raw;
-  static __device__ __forceinline__ raw load(const float* p, int n) {
-    if (n == 2) return *reinterpret_cast<const f32x2_any*>(p);
-    return raw{n == 1 ? *p : 0.f, 0.f};
-  }
-  static __device__ __forceinline__ f32x2 wide(raw v) { return v; }
-  static __device__ __forceinline__ void store(float* p, int n, f32x2 v) {
-    if (n == 2) *reinterpret_cast<f32x2_any*>(p) = v;
-    else if (n == 1) *p = v[0];
-  }
-};
-template <> struct Pair<LSAM_DTYPE_BF16> {
-  typedef u16x2 raw;
-  static __device__ __forceinline__ raw load(const unsigned short* p, int n) {
-    if (n == 2) return *reinterpret_cast<const u16x2_any*>(p);
-    return raw{n == 1 ? *p : (unsigned short)0, 0};
-  }
-  static __device__ __forceinline__ f32x2 wide(raw v) { return f32x2{widen(v[0]), widen(v[1])}; }
-  static __device__ __forceinline__ void store(unsigned short* p, int n, f32x2 v) {
-    if (n == 2) *reinterpret_cast<u16x2_any*>(p) = u16x2{narrow(v[0]), narrow(v[1])};
-    else if (n == 1) *p = narrow(v[0]);
-  }
 };
 
 // a = sigmoid(f) and 1 - a, neither from the other: both keep their digits where they are small.
@@ -65,16 +42,49 @@ __device__ __forceinline__ void gates(float f, float& a, float& b) {
   const float e = __expf(-__builtin_fabsf(f)), r = __builtin_amdgcn_rcpf(1.f + e), small = e * r;
   a = f >= 0.f ? r : small;
   b = f >= 0.f ? small : r;
-  if (f != f) a = b = f;
 }
+
+// kRows rows of a tensor from row t0 on, zeros for rows that are not there.  The usual case, all rows there, is a run of
+// loads that nothing waits between.
+template <typename T>
+__device__ __forceinline__ void load_rows(T (&r)[kRows], const T* p, int64_t stride, int64_t t0, int64_t len) {
+  if (t0 >= 0 && t0 + kRows <= len) {
+    const T* q = p + t0 * stride;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) r[i] = q[i * stride];
+  } else {
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      r[i] = 0;
+      if (t0 + i >= 0 && t0 + i < len) r[i] = p[(t0 + i) * stride];
+    }
+  }
+}
+template <int DTYPE>
+__device__ __forceinline__ void store_rows(const float (&v)[kRows], typename Value<DTYPE>::T* p, int64_t stride, int64_t t0,
+                                           int64_t len, bool mine) {
+  if (!mine) return;
+  if (t0 >= 0 && t0 + kRows <= len) {
+    typename Value<DTYPE>::T* q = p + t0 * stride;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) Value<DTYPE>::put(q + i * stride, v[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kRows; ++i)
+      if (t0 + i >= 0 && t0 + i < len) Value<DTYPE>::put(p + (t0 + i) * stride, v[i]);
+  }
+}
+__device__ __forceinline__ float wide(float v) { return v; }
+__device__ __forceinline__ float wide(unsigned short v) { return widen(v); }
 
 // Where a workgroup's sequence lies and which of its tiles are the workgroup's.
 struct Place {
   int64_t seq, begin, len;      // begin: row number in packed tensors
   int64_t phase, state0;        // tile j: rows j R - phase ..; its saved state: states[state0 + j], j > 0
-  int64_t tiles, first, end;
-  int split;
-  int64_t ch; int n;            // this lane's channels
+  int64_t first, end;           // tiles of this workgroup's run
+  int split, last;              // number of the run, and of the sequence's last one
+  bool here;                    // there is such a workgroup
+  int64_t ch; bool mine;        // this lane's channel; a lane without one reads the last and keeps nothing
   template <typename T>
   __device__ __forceinline__ T* at(const Tensor& t) const {
     return static_cast<T*>(const_cast<void*>(t.p)) + seq * t.seq + begin * t.stride + ch;
@@ -84,9 +94,16 @@ struct Place {
 template <int R>
 __device__ __forceinline__ Place place(const RecurrenceParams& p) {
   Place w;
-  const unsigned slab = blockIdx.x % (unsigned)p.slabs, rest = blockIdx.x / (unsigned)p.slabs;
+  // Workgroups go round the eight XCDs in turn.  kTogether neighbours of a run meet in one XCD, whose L2 then serves the
+  // lines that two of them read where rows do not begin on lines.
+  const unsigned per_run = ((unsigned)p.slabs + kTogether - 1) / kTogether, local = blockIdx.x / 8;
+  const unsigned unit = local / kTogether * 8 + blockIdx.x % 8, rest = unit / per_run;
+  const unsigned slab = unit % per_run * kTogether + local % kTogether;
   w.split = (int)(rest % (unsigned)p.splits);
-  w.seq = p.seq0 + rest / (unsigned)p.splits;
+  const unsigned seq = rest / (unsigned)p.splits;
+  w.seq = p.seq0 + seq;
+  w.here = seq < p.seqs && slab < (unsigned)p.slabs;
+  if (!w.here) return w;
   w.begin = 0;
   w.len = p.rows;
   w.phase = 0;
@@ -101,83 +118,76 @@ __device__ __forceinline__ Place place(const RecurrenceParams& p) {
     w.phase = b % R;
     w.state0 = b / R;
   }
-  w.tiles = w.len > 0 ? (w.phase + w.len + R - 1) / R : 0;
-  w.first = w.tiles * w.split / p.splits;
-  w.end = w.tiles * (w.split + 1) / p.splits;
-  const int64_t ch = (int64_t)slab * kChannels + (threadIdx.x & 63) * 2;
-  w.n = p.D - ch >= 2 ? 2 : p.D - ch == 1 ? 1 : 0;
-  w.ch = w.n ? ch : 0;
+  const int64_t tiles = w.len > 0 ? (w.phase + w.len + R - 1) / R : 0;
+  w.last = tiles > 0 ? (int)((tiles - 1) / p.run_tiles) : 0;
+  w.first = w.split * p.run_tiles;
+  w.end = w.first + p.run_tiles < tiles ? w.first + p.run_tiles : tiles;
+  const int64_t ch = (int64_t)slab * kChannels + (threadIdx.x & 63);
+  w.mine = ch < p.D;
+  w.ch = w.mine ? ch : p.D - 1;
   return w;
 }
-
-typedef Pair<LSAM_DTYPE_FP32> State;
 
 // RUNS: only (A, H) of the workgroup's run, for a launch that follows.
 template <int DTYPE, int NW, bool RUNS>
 __global__ __launch_bounds__(NW * 64) void recurrence_kernel(RecurrenceParams p) {
-  typedef Pair<DTYPE> V;
   typedef typename Value<DTYPE>::T T;
   constexpr int R = NW * kRows;
-  __shared__ f32x2 shA[2][NW][64], shH[2][NW][64];
+  __shared__ float shA[2][NW][64], shH[2][NW][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Place w = place<R>(p);
+  if (!w.here || w.split > w.last) return;
   const T* f = w.at<const T>(p.f);
   const T* x = w.at<const T>(p.x);
   T* h = RUNS ? nullptr : w.at<T>(p.h);
-  f32x2 carry{0.f, 0.f}, whole{1.f, 1.f};
+  float carry = 0.f, whole = 1.f;
   if constexpr (!RUNS) {
-    if (p.h0) carry = State::load(p.h0 + w.seq * p.D + w.ch, w.n);
+    if (p.h0) carry = p.h0[w.seq * p.D + w.ch];
     for (int q = 0; q < w.split; ++q) {
       const float* run = p.runs + (w.seq * p.splits + q) * 2 * p.D + w.ch;
-      carry = State::load(run, w.n) * carry + State::load(run + p.D, w.n);
+      carry = run[0] * carry + run[p.D];
     }
   }
-  typename V::raw rf[kRows], rx[kRows];
+  T rf[kRows], rx[kRows];
   auto fetch = [&](int64_t j) {
-    const int64_t t0 = j * R - w.phase + wave * kRows;
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      const int64_t t = t0 + i;
-      const int n = j < w.end && t >= 0 && t < w.len ? w.n : 0;
-      rf[i] = V::load(f + (n ? t * p.f.stride : 0), n);
-      rx[i] = V::load(x + (n ? t * p.x.stride : 0), n);
-    }
+    const int64_t t0 = j * R - w.phase + wave * kRows, len = j < w.end ? w.len : 0;
+    load_rows(rf, f, p.f.stride, t0, len);
+    load_rows(rx, x, p.x.stride, t0, len);
   };
   fetch(w.first);
   int b = 0;
   for (int64_t j = w.first; j < w.end; ++j) {
     const int64_t t0 = j * R - w.phase + wave * kRows;
-    f32x2 a[kRows], v[kRows], A{1.f, 1.f}, H{0.f, 0.f};
+    float a[kRows], v[kRows], A = 1.f, H = 0.f;
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
-      const bool in = t0 + i >= 0 && t0 + i < w.len;
-      const f32x2 wf = V::wide(rf[i]), wx = V::wide(rx[i]);
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        float g, k;
-        gates(wf[c], g, k);
-        a[i][c] = in ? g : 1.f;               // rows outside the sequence leave the state as it is
-        v[i][c] = in ? k * wx[c] : 0.f;
-      }
+      float k;
+      gates(wide(rf[i]), a[i], k);
+      v[i] = k * wide(rx[i]);
     }
     fetch(j + 1);
+    if (t0 < 0 || t0 + kRows > w.len) {
+#pragma unroll
+      for (int i = 0; i < kRows; ++i)
+        if (t0 + i < 0 || t0 + i >= w.len) { a[i] = 1.f; v[i] = 0.f; }      // outside the sequence the state stays
+    }
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
       A *= a[i];
       H = a[i] * H + v[i];
     }
     if constexpr (!RUNS)
-      if (wave == 0 && p.states && j > 0) State::store(p.states + (w.state0 + j) * p.D + w.ch, w.n, carry);
-    f32x2 s = carry;
+      if (wave == 0 && p.states && j > 0 && w.mine) p.states[(w.state0 + j) * p.D + w.ch] = carry;
+    float s = carry;
     if constexpr (NW > 1) {
       shA[b][wave][lane] = A;
       shH[b][wave][lane] = H;
       __syncthreads();
 #pragma unroll
       for (int q = 0; q < NW; ++q) {
-        const f32x2 qa = shA[b][q][lane], qh = shH[b][q][lane];
+        const float qa = shA[b][q][lane];
         if (q == wave) s = carry;
-        carry = qa * carry + qh;
+        carry = qa * carry + shH[b][q][lane];
         if constexpr (RUNS) whole *= qa;
       }
       b ^= 1;
@@ -187,83 +197,72 @@ __global__ __launch_bounds__(NW * 64) void recurrence_kernel(RecurrenceParams p)
     }
     if constexpr (!RUNS) {
 #pragma unroll
-      for (int i = 0; i < kRows; ++i) {
-        s = a[i] * s + v[i];
-        const int64_t t = t0 + i;
-        if (t >= 0 && t < w.len) V::store(h + t * p.h.stride, w.n, s);
-      }
+      for (int i = 0; i < kRows; ++i) v[i] = s = a[i] * s + v[i];
+      store_rows<DTYPE>(v, h, p.h.stride, t0, w.len, w.mine);
     }
   }
-  if (wave != 0) return;
+  if (wave != 0 || !w.mine) return;
   if constexpr (RUNS) {
     float* run = p.runs + (w.seq * p.splits + w.split) * 2 * p.D + w.ch;
-    State::store(run, w.n, whole);
-    State::store(run + p.D, w.n, carry);
-  } else if (w.split == p.splits - 1 && p.last) {
-    State::store(p.last + w.seq * p.D + w.ch, w.n, carry);
+    run[0] = whole;
+    run[p.D] = carry;
+  } else if (w.split == w.last && p.last) {
+    p.last[w.seq * p.D + w.ch] = carry;
   }
 }
 
 // RUNS: only (A, E) of the workgroup's run.
 template <int DTYPE, int NW, bool RUNS>
 __global__ __launch_bounds__(NW * 64) void recurrence_grad_kernel(RecurrenceParams p) {
-  typedef Pair<DTYPE> V;
   typedef typename Value<DTYPE>::T T;
   constexpr int R = NW * kRows;
-  __shared__ f32x2 shA[2][NW][64], shE[2][NW][64], shH[2][NW][64];
+  __shared__ float shA[2][NW][64], shE[2][NW][64], shH[2][NW][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Place w = place<R>(p);
+  if (!w.here || w.split > w.last) return;
   const T* f = w.at<const T>(p.f);
   const T* x = RUNS ? nullptr : w.at<const T>(p.x);
   const T* dh = w.at<const T>(p.dh);
   T* df = RUNS ? nullptr : w.at<T>(p.df);
   T* dx = RUNS ? nullptr : w.at<T>(p.dx);
-  f32x2 carry{0.f, 0.f}, whole{1.f, 1.f};
+  float carry = 0.f, whole = 1.f;
   if constexpr (!RUNS) {
-    if (p.dlast) carry = State::load(p.dlast + w.seq * p.D + w.ch, w.n);
-    for (int q = p.splits - 1; q > w.split; --q) {
+    if (p.dlast) carry = p.dlast[w.seq * p.D + w.ch];
+    for (int q = w.last; q > w.split; --q) {
       const float* run = p.runs + (w.seq * p.splits + q) * 2 * p.D + w.ch;
-      carry = State::load(run, w.n) * carry + State::load(run + p.D, w.n);
+      carry = run[0] * carry + run[p.D];
     }
   }
-  typename V::raw rf[kRows], rx[kRows], rd[kRows];
-  f32x2 entry{0.f, 0.f};
+  T rf[kRows], rx[kRows], rd[kRows];
+  float entry = 0.f;
   auto fetch = [&](int64_t j) {
-    const int64_t t0 = j * R - w.phase + wave * kRows;
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      const int64_t t = t0 + i;
-      const int n = j >= w.first && t >= 0 && t < w.len ? w.n : 0;
-      rf[i] = V::load(f + (n ? t * p.f.stride : 0), n);
-      if constexpr (!RUNS) rx[i] = V::load(x + (n ? t * p.x.stride : 0), n);
-      rd[i] = V::load(dh + (n ? t * p.dh.stride : 0), n);
-    }
+    const int64_t t0 = j * R - w.phase + wave * kRows, len = j >= w.first ? w.len : 0;
+    load_rows(rf, f, p.f.stride, t0, len);
+    if constexpr (!RUNS) load_rows(rx, x, p.x.stride, t0, len);
+    load_rows(rd, dh, p.dh.stride, t0, len);
     if constexpr (!RUNS) {
-      entry = f32x2{0.f, 0.f};
-      if (j > 0) entry = State::load(p.states + (w.state0 + j) * p.D + w.ch, j >= w.first ? w.n : 0);
-      else if (j == 0 && p.h0) entry = State::load(p.h0 + w.seq * p.D + w.ch, w.first == 0 ? w.n : 0);
+      entry = 0.f;
+      if (len > 0 && j > 0) entry = p.states[(w.state0 + j) * p.D + w.ch];
+      else if (len > 0 && p.h0) entry = p.h0[w.seq * p.D + w.ch];
     }
   };
   if (w.end > w.first) fetch(w.end - 1);
   int b = 0;
   for (int64_t j = w.end - 1; j >= w.first; --j) {
     const int64_t t0 = j * R - w.phase + wave * kRows;
-    f32x2 a[kRows], k[kRows], xv[kRows], d[kRows], A{1.f, 1.f}, E{0.f, 0.f}, H{0.f, 0.f}, s = entry;
+    float a[kRows], k[kRows], xv[kRows], d[kRows], A = 1.f, E = 0.f, H = 0.f, s = entry;
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
-      const bool in = t0 + i >= 0 && t0 + i < w.len;
-      const f32x2 wf = V::wide(rf[i]);
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        float g, m;
-        gates(wf[c], g, m);
-        a[i][c] = in ? g : 1.f;
-        k[i][c] = in ? m : 0.f;
-      }
-      if constexpr (!RUNS) xv[i] = V::wide(rx[i]);
-      d[i] = V::wide(rd[i]);
+      gates(wide(rf[i]), a[i], k[i]);
+      if constexpr (!RUNS) xv[i] = wide(rx[i]);
+      d[i] = wide(rd[i]);
     }
     fetch(j - 1);
+    if (t0 < 0 || t0 + kRows > w.len) {
+#pragma unroll
+      for (int i = 0; i < kRows; ++i)
+        if (t0 + i < 0 || t0 + i >= w.len) { a[i] = 1.f; k[i] = 0.f; }
+    }
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
       A *= a[i];
@@ -271,7 +270,7 @@ __global__ __launch_bounds__(NW * 64) void recurrence_grad_kernel(RecurrencePara
     }
 #pragma unroll
     for (int i = kRows - 1; i >= 0; --i) E = a[i] * (d[i] + E);
-    f32x2 e = carry;
+    float e = carry;
     if constexpr (NW > 1) {
       shA[b][wave][lane] = A;
       shE[b][wave][lane] = E;
@@ -279,7 +278,7 @@ __global__ __launch_bounds__(NW * 64) void recurrence_grad_kernel(RecurrencePara
       __syncthreads();
 #pragma unroll
       for (int q = NW - 1; q >= 0; --q) {
-        const f32x2 qa = shA[b][q][lane];
+        const float qa = shA[b][q][lane];
         if (q == wave) e = carry;
         carry = qa * carry + shE[b][q][lane];
         if constexpr (RUNS) whole *= qa;
@@ -295,36 +294,38 @@ __global__ __launch_bounds__(NW * 64) void recurrence_grad_kernel(RecurrencePara
       if constexpr (RUNS) whole *= A;
     }
     if constexpr (!RUNS) {
-      f32x2 before[kRows];
+      float g[kRows];
 #pragma unroll
       for (int i = 0; i < kRows; ++i) {
-        before[i] = s;
+        g[i] = s - xv[i];
         s = a[i] * s + k[i] * xv[i];
       }
 #pragma unroll
       for (int i = kRows - 1; i >= 0; --i) {
-        const f32x2 t_d = d[i] + e, kd = k[i] * t_d;
-        const int64_t t = t0 + i;
-        if (t >= 0 && t < w.len) {
-          V::store(dx + t * p.dx.stride, w.n, kd);
-          V::store(df + t * p.df.stride, w.n, a[i] * kd * (before[i] - xv[i]));
-        }
-        e = a[i] * t_d;
+        const float whole_d = d[i] + e, kd = k[i] * whole_d;
+        g[i] *= a[i] * kd;
+        d[i] = kd;
+        e = a[i] * whole_d;
       }
+      store_rows<DTYPE>(d, dx, p.dx.stride, t0, w.len, w.mine);
+      store_rows<DTYPE>(g, df, p.df.stride, t0, w.len, w.mine);
     }
   }
-  if (wave != 0) return;
+  if (wave != 0 || !w.mine) return;
   if constexpr (RUNS) {
     float* run = p.runs + (w.seq * p.splits + w.split) * 2 * p.D + w.ch;
-    State::store(run, w.n, whole);
-    State::store(run + p.D, w.n, carry);
+    run[0] = whole;
+    run[p.D] = carry;
   } else if (w.split == 0 && p.dh0) {
-    State::store(p.dh0 + w.seq * p.D + w.ch, w.n, carry);
+    p.dh0[w.seq * p.D + w.ch] = carry;
   }
 }
 
-// How a call is cut.  One wavefront where sequences are no longer than its rows (a step of generation).
-struct Plan { int waves, splits, slabs; int64_t tiles_of_each, states; };
+// How a call is cut.  One wavefront where sequences are no longer than its rows (a step of generation).  Runs where
+// sequences times channels give fewer workgroups than there are units: all of one length, so that sequences of any lengths
+// fill the chip evenly, as many as give it kRunGroups workgroups, of at least four tiles each.
+constexpr int kRunGroups = 1024;
+struct Plan { int waves, splits, slabs; int64_t run_tiles, tiles_of_each, states; };
 Plan plan(const lsam_recurrence_desc* d) {
   Plan c;
   const int64_t mean = d->packed ? (d->seqs ? (d->rows + d->seqs - 1) / d->seqs : 0) : d->rows;
@@ -333,12 +334,16 @@ Plan plan(const lsam_recurrence_desc* d) {
   c.slabs = (int)((d->dim + kChannels - 1) / kChannels);
   c.tiles_of_each = d->packed ? 0 : (d->rows + R - 1) / R;
   c.states = d->packed ? d->rows / R + 1 : d->seqs * c.tiles_of_each;
-  // Runs: as many as give every unit two workgroups, of at least four tiles each.
-  const int64_t groups = d->seqs * c.slabs, tiles = (d->rows + R - 1) / R;
-  int64_t splits = groups > 0 && groups < 128 ? 512 / groups : 1;
-  if (splits > tiles / 4) splits = tiles / 4;
-  if (splits > kMaxSplits) splits = kMaxSplits;
-  c.splits = splits < 1 ? 1 : (int)splits;
+  // the most tiles a sequence can have (a packed one may begin and end inside a tile), and those of all together
+  const int64_t most = d->packed ? d->rows / R + 2 : c.tiles_of_each, all = d->packed ? most : d->seqs * most;
+  c.run_tiles = most > 0 ? most : 1;
+  c.splits = 1;
+  if (d->seqs * c.slabs < 256 && most > 4) {
+    int64_t tiles = (all * c.slabs + kRunGroups - 1) / kRunGroups;
+    if (tiles < (most + kMaxSplits - 1) / kMaxSplits) tiles = (most + kMaxSplits - 1) / kMaxSplits;
+    c.run_tiles = tiles < 4 ? 4 : tiles;
+    c.splits = (int)((most + c.run_tiles - 1) / c.run_tiles);
+  }
   return c;
 }
 
@@ -379,11 +384,13 @@ Tensor tensor(const void* p, const lsam_rows& r, bool packed) { return Tensor{p,
 template <int DTYPE, int NW, bool GRAD>
 void launch(RecurrenceParams p, int64_t seqs, hipStream_t s) {
   // a launch has less than 2^32 lanes: more sequences take further launches
-  const int64_t most = ((1ll << 31) / (NW * 64)) / ((int64_t)p.splits * p.slabs);
+  const int64_t per_run = (p.slabs + kTogether - 1) / kTogether;
+  const int64_t most = ((1ll << 31) / (NW * 64)) / (p.splits * per_run * kTogether) - 8;
   const int64_t step = most < 1 ? 1 : most;
   for (int64_t s0 = 0; s0 < seqs; s0 += step) {
     p.seq0 = s0;
-    const unsigned grid = (unsigned)((seqs - s0 < step ? seqs - s0 : step) * p.splits * p.slabs);
+    p.seqs = (unsigned)(seqs - s0 < step ? seqs - s0 : step);
+    const unsigned grid = (unsigned)((p.seqs * p.splits * per_run + 7) / 8 * 8 * kTogether);
     if constexpr (GRAD) {
       if (p.splits > 1) recurrence_grad_kernel<DTYPE, NW, true><<<grid, NW * 64, 0, s>>>(p);
       recurrence_grad_kernel<DTYPE, NW, false><<<grid, NW * 64, 0, s>>>(p);
@@ -415,7 +422,7 @@ RecurrenceParams params(const lsam_recurrence_desc* d, const Plan& c, const int6
   p.offsets = d->packed ? offsets : nullptr;
   p.rows = d->rows; p.D = d->dim;
   p.tiles_of_each = c.tiles_of_each;
-  p.splits = c.splits; p.slabs = c.slabs;
+  p.splits = c.splits; p.slabs = c.slabs; p.run_tiles = c.run_tiles;
   p.runs = static_cast<float*>(workspace);
   return p;
 }
