@@ -130,6 +130,50 @@ int lsam_recurrence_backward(const lsam_recurrence_desc* d, const int64_t* offse
                              const float* h0, const float* states, const void* dh, const float* dlast, void* df, void* dx,
                              float* dh0, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- low-rank adapters beside a shared projection ------------------------------------------------
+ * For `rows` rows x [in]:  y = x W^T + bias + scale (x A_a^T) B_a^T, with W [out, in] and bias shared by all rows and a the adapter
+ * of the row.  The rows of a request, or of a replica, are one segment: segment s is rows seg_begin[s] .. seg_begin[s + 1] - 1
+ * (seg_begin [device] [segs + 1] int32, not decreasing; values outside 0..rows are taken as the nearest inside) with adapter
+ * seg_adapter[s] ([device] [segs] int32).  Rows of no segment, and of segments whose adapter is outside 0..adapters-1 (-1, say),
+ * have none: y = x W^T + bias.  Several segments may share an adapter; segments may be empty.
+ *   x, W, y    [device] of dtype; bias [device] [out] floats, or NULL
+ *   A, B       [device] of adapter_dtype: adapters matrices [rank, in] and [out, rank], as far apart as a_adapter and b_adapter
+ *              say (for replicas whose parameters are rows of a [K, d] array: d)
+ *   u          [device] [rows, rank] floats that receive x A_a^T (0 without an adapter), for the backward pass
+ * Products are summed in fp32; operands in fp32 are not rounded to fewer bits.  A row's result depends on its own values, W and
+ * its own adapter only; where an element of B_a is infinite or NaN, the results it takes part in are infinite or NaN.
+ * workspace [device, 256-byte aligned], lsam_adapter_workspace_bytes(d, 0) bytes for this call, (d, 1) for the backward one (0, with
+ * a message, for a descriptor that is refused); nothing in it has to survive a call.  Parts of it are used only where rows are
+ * not aligned to 16 bytes, or fp32. */
+#define LSAM_ADAPTER_MAX_RANK 64
+typedef struct {
+  int64_t rows;                              /* below 2^28                                   */
+  int32_t in, out;                           /* 1..2^21; rows in, rows out, in out <= 2^35   */
+  int32_t rank;                              /* 1..LSAM_ADAPTER_MAX_RANK                     */
+  int32_t adapters, segs;                    /* adapters up to 65535                         */
+  int32_t dtype, adapter_dtype;              /* LSAM_DTYPE_*                                 */
+  float scale;
+  int64_t x_stride, w_stride, y_stride;      /* from row to row                              */
+  int64_t a_adapter, a_stride;               /* from adapter to adapter, from rank to rank   */
+  int64_t b_adapter, b_stride;               /* from adapter to adapter, from output to output */
+  int64_t dy_stride, dx_stride;              /* backward pass only, as what follows          */
+  int64_t da_adapter, da_stride, db_adapter, db_stride;
+} lsam_adapter_desc;
+size_t lsam_adapter_workspace_bytes(const lsam_adapter_desc* d, int32_t backward);
+int lsam_adapter(const lsam_adapter_desc* d, const void* x, const void* W, const float* bias, const void* A, const void* B,
+                 const int32_t* seg_begin, const int32_t* seg_adapter, float* u, void* y, void* workspace,
+                 size_t workspace_bytes, void* stream);
+
+/* Gradients with respect to x, A and B (W and bias are frozen), for the dy of y:
+ *   du = scale dy B_a,  dx = dy W + du A_a,  dA_a = sum du^T x,  dB_a = scale sum dy^T u over the rows of adapter a.
+ *   u      as the forward call left it
+ *   dx     [device] of dtype, or NULL: not wanted
+ *   dA, dB [device] floats laid out as A and B are, strides of their own, or both NULL.  Written whole (0 for an adapter
+ *          of no row), not added to.  They may be parts of one [adapters, d] array */
+int lsam_adapter_backward(const lsam_adapter_desc* d, const void* x, const void* W, const void* A, const void* B,
+                          const int32_t* seg_begin, const int32_t* seg_adapter, const float* u, const void* dy, void* dx,
+                          float* dA, float* dB, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,1105 @@
+// lsam_adapter, lsam_adapter_backward: y = x W^T + bias + scale (x A_a^T) B_a^T, W shared by all rows and a the adapter of
+// the row's segment, and the gradients of x, A and B.
+//
+// The products run on the bf16 matrix units with fp32 sums.  bf16 operands are multiplied as they are; an fp32 number is
+// split into three bfloat16 pieces h + m + l (24 bits: exact), of whose nine products the six that reach fp32's last bit are
+// formed.  The rank-sized results u = x A^T and du = scale dy B stay in fp32 between the kernels.
+//
+//   shrink_kernel   u or du: [rows, rank], 64 rows of one segment a workgroup, the long contraction cut over its wavefronts
+//   product_kernel  y or dx: tiles of W's product; then, for every segment that the tile's rows belong to, a few more steps
+//                   of the same loop over the pieces of u and B (or du and A), rows of other segments being zero
+//   few_rows_kernel y or dx where there are at most 64 rows: reads W once, 16 outputs a workgroup, no tile of x
+//   grads_kernel    dA = sum du^T x and dB = scale sum dy^T u over the rows of an adapter, no sum split over workgroups
+//   planes_kernel   pieces, aligned copies and the transposed W of the backward pass
+#include "ops.h"
+#include "planes.h"
+
+namespace lsam {
+namespace {
+
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+
+constexpr int kMaxRank = LSAM_ADAPTER_MAX_RANK;
+
+// ---- segments ---------------------------------------------------------------------------------------
+// Segment s is rows begin[s] .. begin[s + 1] - 1 with adapter which[s]; rows of no segment, and of one whose adapter does not
+// exist, have none.  Whatever the arrays hold, no row outside the matrix and no adapter that is not there is touched.
+struct Segments {
+  const int32_t* begin; const int32_t* which;
+  int n, adapters;
+};
+__device__ __forceinline__ int64_t seg_row(const Segments& g, int s, int64_t rows) {
+  const int64_t b = g.begin[s];
+  return b < 0 ? 0 : b > rows ? rows : b;
+}
+// The last segment that begins at or before `row`, or -1.
+__device__ __forceinline__ int seg_at(const Segments& g, int64_t row) {
+  int lo = 0, hi = g.n;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (g.begin[mid] <= row) lo = mid + 1; else hi = mid;
+  }
+  return lo - 1;
+}
+__device__ __forceinline__ int seg_adapter(const Segments& g, int s) {
+  const int a = g.which[s];
+  return a >= 0 && a < g.adapters ? a : -1;
+}
+__device__ __forceinline__ int row_adapter(const Segments& g, int64_t row, int64_t rows) {
+  const int s = seg_at(g, row);
+  return s >= 0 && row < seg_row(g, s + 1, rows) ? seg_adapter(g, s) : -1;
+}
+
+template <int N> struct Count { static constexpr int value = N; };
+
+// ---- operands of the matrix units -------------------------------------------------------------------
+// Eight numbers as NP words of eight bfloat16 pieces.
+template <int NP> struct Pieces { bf16x8 p[NP]; };
+
+__device__ __forceinline__ void split8(const float (&v)[8], Pieces<3>& o) {
+  unsigned w[3][4];
+  float most = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) most = largest_of(most, v[e]);
+  if (past_rounding(most)) split_words_any<3, 8>(v, w);
+  else split_words<3, 8>(v, w);
+#pragma unroll
+  for (int q = 0; q < 3; ++q) o.p[q] = __builtin_bit_cast(bf16x8, u32x4{w[q][0], w[q][1], w[q][2], w[q][3]});
+}
+
+// Pieces of a stored type: numbers that are bfloat16 already are their own.
+template <int DTYPE> constexpr int kPieces = DTYPE == LSAM_DTYPE_BF16 ? 1 : 3;
+
+// Eight numbers from p on, `step` apart (UNIT: neighbours).  A run of such loads waits for nothing in between.
+template <int DTYPE, bool UNIT>
+__device__ __forceinline__ void load8(const typename Value<DTYPE>::T* p, int64_t step, Pieces<kPieces<DTYPE>>& o) {
+  if constexpr (DTYPE == LSAM_DTYPE_BF16) {
+    u16x8 w;
+    if constexpr (UNIT) {
+      w = *reinterpret_cast<const u16x8_any*>(p);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = p[e * step];
+    }
+    o.p[0] = __builtin_bit_cast(bf16x8, w);
+  } else {
+    float v[8];
+    if constexpr (UNIT) {
+      Value<DTYPE>::load8(p, v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = p[e * step];
+    }
+    split8(v, o);
+  }
+}
+// The same where only the first n are there (n may be negative); the others count as 0.
+template <int DTYPE>
+__device__ __forceinline__ void load8_some(const typename Value<DTYPE>::T* p, int64_t step, int n, Pieces<kPieces<DTYPE>>& o) {
+  if constexpr (DTYPE == LSAM_DTYPE_BF16) {
+    u16x8 w;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = e < n ? p[e * step] : (unsigned short)0;
+    o.p[0] = __builtin_bit_cast(bf16x8, w);
+  } else {
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < n ? p[e * step] : 0.f;
+    split8(v, o);
+  }
+}
+
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+__device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// c += a b^T over 32 numbers of each row, from their pieces; small products first.
+template <int NA, int NB>
+__device__ __forceinline__ f32x4 multiply(const Pieces<NA>& a, const Pieces<NB>& b, f32x4 c) {
+  constexpr int most = NA > NB ? NA : NB;
+#pragma unroll
+  for (int sum = most - 1; sum >= 0; --sum)
+#pragma unroll
+    for (int i = 0; i <= sum; ++i)
+      if (i < NA && sum - i < NB) c = mfma16(a.p[i], b.p[sum - i], c);
+  return c;
+}
+
+// ---- u = x A^T, du = scale dy B ---------------------------------------------------------------------
+constexpr int kShrinkWaves = 8;
+
+struct ShrinkParams {
+  const void* x; int64_t x_stride;
+  const void* A; int64_t a_adapter, a_rank, a_k;      // strides from adapter to adapter, and along rank and contraction
+  float* u;
+  int64_t rows; int K, rank;
+  float scale;
+  Segments g;
+};
+
+// Workgroup (tile, j): the j-th, j + gridDim.y-th, ... segment of the tile's 16 RT rows.  The wavefronts take 32 numbers of the
+// contraction in turn.  Bound by reading x where segments are long, by reading A where each row has its own.
+// UNIT: the contraction is contiguous in A.
+template <int DTYPE, int ATYPE, bool UNIT, int NR, int RT>
+__global__ __launch_bounds__(kShrinkWaves * 64) void shrink_kernel(ShrinkParams p) {
+  typedef typename Value<DTYPE>::T T;
+  typedef typename Value<ATYPE>::T TA;
+  constexpr int ROWS = RT * 16;
+  constexpr int PITCH = NR * 16 + 1;
+  __shared__ float part[kShrinkWaves][16][PITCH];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, quarter = lane >> 4;
+  const int64_t row0 = (int64_t)blockIdx.x * ROWS, row1 = row0 + ROWS < p.rows ? row0 + ROWS : p.rows;
+  if (blockIdx.y == 0) {
+    // rows without an adapter
+    for (int i = tid; i < ROWS * p.rank; i += kShrinkWaves * 64) {
+      const int64_t row = row0 + i / p.rank;
+      if (row < row1 && row_adapter(p.g, row, p.rows) < 0) p.u[row * p.rank + i % p.rank] = 0.f;
+    }
+  }
+  const int found = seg_at(p.g, row0);
+  for (int s = (found < 0 ? 0 : found) + (int)blockIdx.y; s < p.g.n; s += gridDim.y) {
+    int64_t lo = seg_row(p.g, s, p.rows), hi = seg_row(p.g, s + 1, p.rows);
+    if (lo >= row1) break;
+    lo = lo > row0 ? lo : row0;
+    hi = hi < row1 ? hi : row1;
+    const int a = seg_adapter(p.g, s);
+    if (a < 0 || lo >= hi) continue;
+    // rows and ranks past the last one read the last one again, and their results are dropped
+    const T* x[RT];
+    const TA* A[NR];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const int64_t row = lo + t * 16 + l16 < hi ? lo + t * 16 + l16 : hi - 1;
+      x[t] = static_cast<const T*>(p.x) + row * p.x_stride + quarter * 8;
+    }
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      const int rr = r * 16 + l16 < p.rank ? r * 16 + l16 : p.rank - 1;
+      A[r] = static_cast<const TA*>(p.A) + a * p.a_adapter + rr * p.a_rank + quarter * 8 * p.a_k;
+    }
+    f32x4 acc[RT][NR];
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int r = 0; r < NR; ++r) acc[t][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+    int k = wave * 32;
+    constexpr int STEP = kShrinkWaves * 32;
+    auto steps = [&](auto count) {
+      constexpr int N = decltype(count)::value;
+      Pieces<kPieces<ATYPE>> fa[N][NR];
+      Pieces<kPieces<DTYPE>> fx[N][RT];
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) load8<DTYPE, true>(x[t] + k + i * STEP, 1, fx[i][t]);
+#pragma unroll
+        for (int r = 0; r < NR; ++r) load8<ATYPE, UNIT>(A[r] + (k + i * STEP) * p.a_k, p.a_k, fa[i][r]);
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+          for (int r = 0; r < NR; ++r) acc[t][r] = multiply(fa[i][r], fx[i][t], acc[t][r]);
+      k += N * STEP;
+    };
+    constexpr int AHEAD = RT == 1 ? 4 : 2;             // steps whose loads are in flight together
+    while (k + (AHEAD - 1) * STEP + 32 <= p.K) steps(Count<AHEAD>{});
+    while (k + 32 <= p.K) steps(Count<1>{});
+    if (k < p.K) {
+      const int n = p.K - k - quarter * 8;
+      Pieces<kPieces<ATYPE>> fa[NR];
+#pragma unroll
+      for (int r = 0; r < NR; ++r) load8_some<ATYPE>(A[r] + k * p.a_k, p.a_k, n, fa[r]);
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        Pieces<kPieces<DTYPE>> fx;
+        load8_some<DTYPE>(x[t] + k, 1, n, fx);
+#pragma unroll
+        for (int r = 0; r < NR; ++r) acc[t][r] = multiply(fa[r], fx, acc[t][r]);
+      }
+    }
+    // lane: row l16 of a tile, ranks 4 quarter .. + 3
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      if (lo + t * 16 < hi) {              // the same for all
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) part[wave][l16][r * 16 + quarter * 4 + i] = acc[t][r][i];
+        __syncthreads();
+        for (int i = tid; i < 16 * NR * 16; i += kShrinkWaves * 64) {
+          const int row = i / (NR * 16), r = i % (NR * 16);
+          if (r < p.rank && lo + t * 16 + row < hi) {
+            float sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < kShrinkWaves; ++w) sum += part[w][row][r];
+            p.u[(lo + t * 16 + row) * p.rank + r] = p.scale * sum;
+          }
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// ---- y or dx, many rows -----------------------------------------------------------------------------
+struct ProductParams {
+  const unsigned short* X; int64_t ldx, plane_x;      // [planes][M][ldx], K of each row
+  const unsigned short* W; int64_t ldw, plane_w;      // [planes][N][ldw]
+  int products;                                       // 1, or the 6 of three planes
+  int64_t M; int N, K;                                // K a multiple of 8, rows 16-byte aligned
+  void* Y; int64_t ldy;
+  const float* bias;
+  const float* u; float scale;                        // [M][rank]
+  const void* Q; int64_t q_adapter, q_n, q_r;         // strides along adapter, output and rank
+  int rank;
+  int pairs; unsigned pair_u, pair_q;                 // products of pieces of u and Q: four bits for the piece of each
+  int tilesM, tilesN;
+  Segments g;
+};
+
+// The six products of three pieces each that fp32 can tell from 0, the smallest first, four bits for a piece: l h, m m, h l,
+// m h, h m, h h.
+constexpr unsigned kSixLeft = 0x001012u, kSixRight = 0x010210u;
+
+constexpr int kBK = 64;                               // numbers of a row in a step: 128 bytes
+constexpr int waitcnt(int vm, int lgkm) { return (vm & 0xF) | ((vm >> 4) << 14) | (0x7 << 4) | ((lgkm & 0xF) << 8); }
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* base, unsigned bytes) {
+  const unsigned long long a = reinterpret_cast<unsigned long long>(base);
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)a);
+  const unsigned hi = __builtin_amdgcn_readfirstlane((unsigned)(a >> 32));
+  void* ptr = reinterpret_cast<void*>(((unsigned long long)hi << 32) | lo);
+  return __builtin_amdgcn_make_buffer_rsrc(ptr, 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+}
+
+// Waits for the wavefront's own loads, those to LDS among them, and then for the workgroup.
+__device__ __forceinline__ void arrived() {
+  __builtin_amdgcn_s_waitcnt(waitcnt(0, 0));
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// One operand's tile of R rows by kBK numbers in LDS: row r is 128 bytes = 8 units of 16, unit q at position q ^ (r % 8), so
+// that neighbouring rows' units lie in different banks.  Global memory goes to LDS directly, eight whole rows an instruction;
+// the lane order of that copy is fixed, so a lane asks for the unit that belongs at its position.
+template <int R, int NW>
+struct RowTile {
+  static constexpr int BYTES = R * kBK * 2;
+  static constexpr int NLOAD = R / 8 / NW;
+  unsigned goff[NLOAD];        // of this lane's unit, at step 0
+  int k[NLOAD];                // the first number of the unit
+  __device__ __forceinline__ void init(int64_t ld, int lane, int wave) {
+#pragma unroll
+    for (int j = 0; j < NLOAD; ++j) {
+      const int row = (wave * NLOAD + j) * 8 + (lane >> 3), unit = (lane & 7) ^ (row & 7);
+      k[j] = unit * 8;
+      goff[j] = (unsigned)(row * ld * 2) + (unsigned)unit * 16u;
+    }
+  }
+  // Numbers k0 .. k0 + 63 of every row; units past K, and rows past the resource's end, arrive as zeros.
+  __device__ __forceinline__ void issue(__amdgpu_buffer_rsrc_t rsrc, lds_byte* tile, int k0, int K, int wave) const {
+#pragma unroll
+    for (int j = 0; j < NLOAD; ++j)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(tile + (wave * NLOAD + j) * 1024), 16,
+                                               k0 + k[j] < K ? goff[j] + (unsigned)k0 * 2u : 0x7FFFFFF0u, 0, 0, 0);
+  }
+};
+// The 16 bytes that a lane feeds to the matrix unit: row `row`, numbers 16 kc + 8 half ..
+__device__ __forceinline__ u32x4 fragment(const lds_byte* tile, int row, int kc, int half) {
+  return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(tile + row * 128 + (((kc * 2 + half) ^ (row & 7)) << 4));
+}
+__device__ __forceinline__ void put_unit(lds_byte* tile, int row, int unit, u32x4 v) {
+  *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(tile + row * 128 + ((unit ^ (row & 7)) << 4)) = v;
+}
+
+// Piece `which` of eight numbers, as split_planes makes them, with few registers.
+__device__ __forceinline__ unsigned short leading_piece(float x) {
+  const unsigned u = __builtin_bit_cast(unsigned, x), mag = u & 0x7FFFFFFFu;
+  return mag >= 0x7F7F8000u && mag <= 0x7F800000u ? (unsigned short)(u >> 16) : narrow(x);
+}
+__device__ __forceinline__ u32x4 piece8(const float (&v)[8], unsigned which) {
+  u16x8 o;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float r = v[e];
+#pragma unroll
+    for (unsigned q = 0; q < 2; ++q) {
+      const float rest = __builtin_fabsf(r) < __builtin_inff() ? r - widen(leading_piece(r)) : 0.f;
+      r = which > q ? rest : r;
+    }
+    o[e] = leading_piece(r);
+  }
+  return __builtin_bit_cast(u32x4, o);
+}
+
+// BM x BN outputs by WM x WN wavefronts, each a block of 32 x 32 results TM x TN times.
+template <int OTYPE, int QTYPE, int BM, int BN, int WM, int WN>
+__device__ __forceinline__ void product_tile(const ProductParams& p) {
+  constexpr int NW = WM * WN, NT = NW * 64;
+  constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
+  typedef RowTile<BM, NW> OX;
+  typedef RowTile<BN, NW> OW;
+  __shared__ __attribute__((aligned(1024))) unsigned char st0[OX::BYTES + OW::BYTES];
+  __shared__ __attribute__((aligned(1024))) unsigned char st1[OX::BYTES + OW::BYTES];
+  __shared__ int not_finite[BN];
+  __shared__ int any_not_finite;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, half = lane >> 5;
+  const int wm = (wave / WN) * (TM * 32), wn = (wave % WN) * (TN * 32);
+
+  // Workgroups go round the eight XCDs; an XCD takes a run of tiles, eight rows of tiles at a time, so that what runs there
+  // together shares the rows of x and W that its L2 holds.
+  const unsigned total = (unsigned)p.tilesM * (unsigned)p.tilesN, xcd = blockIdx.x % 8, each = total / 8, more = total % 8;
+  const unsigned id = xcd * each + (xcd < more ? xcd : more) + blockIdx.x / 8;
+  constexpr unsigned kBand = 8;
+  const unsigned band = id / (kBand * p.tilesN), in_band = id % (kBand * p.tilesN);
+  const unsigned rows_of_band = p.tilesM - band * kBand < kBand ? p.tilesM - band * kBand : kBand;
+  const int64_t m0 = (int64_t)(band * kBand + in_band % rows_of_band) * BM;
+  const int n0 = (int)(in_band / rows_of_band) * BN;
+  const int64_t m_here = p.M - m0 < BM ? p.M - m0 : BM;
+  const int n_here = p.N - n0 < BN ? p.N - n0 : BN;
+
+  OX ox;
+  OW ow;
+  ox.init(p.ldx, lane, wave);
+  ow.init(p.ldw, lane, wave);
+  const unsigned bytes_x = (unsigned)(((m_here - 1) * p.ldx + p.K) * 2), bytes_w = (unsigned)(((n_here - 1) * p.ldw + p.K) * 2);
+  const unsigned short* X = p.X + m0 * p.ldx;
+  const unsigned short* W = p.W + (int64_t)n0 * p.ldw;
+  lds_byte* const a0 = (lds_byte*)st0;
+  lds_byte* const a1 = (lds_byte*)st1;
+
+  f32x16 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+  u32x4 fx[2][TM], fw[2][TN];
+  auto read = [&](const lds_byte* tile, int kc, int buf) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i) fx[buf][i] = fragment(tile, wm + i * 32 + l32, kc, half);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) fw[buf][j] = fragment(tile + OX::BYTES, wn + j * 32 + l32, kc, half);
+  };
+  auto multiply_chunk = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = mfma32(fw[buf][j], fx[buf][i], acc[i][j]);
+  };
+
+  // Steps: the products of planes one after the other, each over all of K.  Step s + 1 is on its way while s is multiplied.
+  const int per_product = (p.K + kBK - 1) / kBK, steps = p.products * per_product;
+  int next_k = 0, next_q = 0;
+  auto request = [&](lds_byte* tile, int step) {
+    if (step >= steps) return;
+    const unsigned px = p.products == 1 ? 0u : (kSixLeft >> (4 * next_q)) & 15u;
+    const unsigned pw = p.products == 1 ? 0u : (kSixRight >> (4 * next_q)) & 15u;
+    ox.issue(make_rsrc(X + px * p.plane_x, bytes_x), tile, next_k, p.K, wave);
+    ow.issue(make_rsrc(W + pw * p.plane_w, bytes_w), tile + OX::BYTES, next_k, p.K, wave);
+    next_k += kBK;
+    if (next_k >= per_product * kBK) { next_k = 0; ++next_q; }
+  };
+  request(a0, 0);
+  request(a1, 1);
+  arrived();
+  read(a0, 0, 0);
+  auto step = [&](lds_byte* now, lds_byte* then, int s) {
+    read(now, 1, 1);
+    multiply_chunk(0);
+    read(now, 2, 0);
+    multiply_chunk(1);
+    read(now, 3, 1);
+    multiply_chunk(0);
+    // Every wavefront has taken its last fragment of this step and the next one has arrived, requested a step ago.
+    arrived();
+    request(now, s + 2);
+    read(then, 0, 0);                    // past the last step: never multiplied
+    multiply_chunk(1);
+  };
+  for (int s = 0; s < steps; s += 2) {
+    step(a0, a1, s);
+    if (s + 1 < steps) step(a1, a0, s + 1);
+  }
+  __syncthreads();
+
+  // The adapters of the tile's rows.
+  const int rp = (p.rank + 7) & ~7, low_k = p.pairs * rp;
+  const int found = seg_at(p.g, m0);
+  for (int s = found < 0 ? 0 : found; s < p.g.n; ++s) {
+    int64_t lo = seg_row(p.g, s, p.M) - m0, hi = seg_row(p.g, s + 1, p.M) - m0;
+    if (lo >= m_here) break;
+    lo = lo > 0 ? lo : 0;
+    hi = hi < m_here ? hi : m_here;
+    const int a = seg_adapter(p.g, s);
+    if (a < 0 || lo >= hi) continue;
+    typedef typename Value<QTYPE>::T TQ;
+    const TQ* Q = static_cast<const TQ*>(p.Q) + a * p.q_adapter + n0 * p.q_n;
+    if (tid < BN) not_finite[tid] = 0;
+    if (tid == 0) any_not_finite = 0;
+    __syncthreads();
+    for (int k0 = 0; k0 < low_k; k0 += kBK) {
+      for (int i = tid; i < BM * 8; i += NT) {
+        const int row = i >> 3, k = k0 + (i & 7) * 8;
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (row >= lo && row < hi && k < low_k) {
+          const float* u = p.u + (m0 + row) * p.rank + k % rp;
+          const int n = p.rank - k % rp;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = e < n ? p.scale * u[e] : 0.f;
+        }
+        put_unit(a0, row, i & 7, piece8(v, k < low_k ? (p.pair_u >> (4 * (k / rp))) & 15u : 0u));
+      }
+      for (int i = tid; i < BN * 8; i += NT) {
+        // lanes along whatever is contiguous in Q
+        const int col = p.q_r == 1 ? i >> 3 : i % BN, unit = p.q_r == 1 ? i & 7 : i / BN, k = k0 + unit * 8;
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (col < n_here && k < low_k) {
+          const TQ* q = Q + col * p.q_n + (k % rp) * p.q_r;
+          const int n = p.rank - k % rp;
+          bool odd = false;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            v[e] = e < n ? Value<QTYPE>::get(q + e * p.q_r) : 0.f;
+            // An infinity or NaN here would reach the rows of other segments, whose 0 it is multiplied with.
+            if (!(__builtin_fabsf(v[e]) < __builtin_inff())) { v[e] = 0.f; odd = true; }
+          }
+          if (odd) { not_finite[col] = 1; any_not_finite = 1; }
+        }
+        put_unit(a0 + OX::BYTES, col, unit, piece8(v, k < low_k ? (p.pair_q >> (4 * (k / rp))) & 15u : 0u));
+      }
+      __syncthreads();
+#pragma unroll
+      for (int kc = 0; kc < 4; ++kc) {
+        if (k0 + kc * 16 < low_k) {
+          read(a0, kc, 0);
+          multiply_chunk(0);
+        }
+      }
+      __syncthreads();
+    }
+    if (any_not_finite) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        const int row = wm + i * 32 + l32;
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (row >= lo && row < hi && not_finite[wn + j * 32 + (e >> 2) * 8 + half * 4 + (e & 3)]) acc[i][j][e] = __builtin_nanf("");
+      }
+    }
+    __syncthreads();
+  }
+
+  typedef Value<OTYPE> VO;
+  typedef typename VO::T TO;
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int row = wm + i * 32 + l32;
+    if (row < m_here) {
+      TO* y = static_cast<TO*>(p.Y) + (m0 + row) * p.ldy + n0;
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int col = wn + j * 32 + q * 8 + half * 4;
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = acc[i][j][q * 4 + e] + (p.bias && col + e < n_here ? p.bias[n0 + col + e] : 0.f);
+          if (col + 4 <= n_here) {
+            if constexpr (OTYPE == LSAM_DTYPE_BF16) {
+              *reinterpret_cast<u16x4_any*>(y + col) = u16x4{narrow(v[0]), narrow(v[1]), narrow(v[2]), narrow(v[3])};
+            } else {
+              *reinterpret_cast<f32x4_any*>(y + col) = f32x4{v[0], v[1], v[2], v[3]};
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (col + e < n_here) VO::put(y + col + e, v[e]);
+          }
+        }
+    }
+  }
+}
+
+template <int OTYPE, int QTYPE, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * 64) void product_kernel(ProductParams p) {
+  product_tile<OTYPE, QTYPE, BM, BN, WM, WN>(p);
+}
+
+// ---- y or dx, at most 64 rows -----------------------------------------------------------------------
+struct FewRowsParams {
+  const void* X; int64_t ldx;
+  const void* W; int64_t ldw;
+  int M, N, K;
+  void* Y; int64_t ldy;
+  const float* bias;
+  const float* u; float scale;
+  const void* Q; int64_t q_adapter, q_n, q_r;
+  int rank;
+  Segments g;
+};
+constexpr int kFewRows = 64;
+constexpr int kFewWaves = 8;
+
+// A workgroup's 16 outputs: eight wavefronts go along the rows of W 512 bytes (bf16) at a time, so that W streams from
+// memory once; x comes from L2.  Bound by reading W.
+template <int DTYPE, int QTYPE, int RT>
+__global__ __launch_bounds__(kFewWaves * 64) void few_rows_kernel(FewRowsParams p) {
+  typedef typename Value<DTYPE>::T T;
+  typedef typename Value<QTYPE>::T TQ;
+  __shared__ float part[kFewWaves][RT * 16][17];
+  __shared__ int adapter[RT * 16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, quarter = lane >> 4;
+  const int n0 = blockIdx.x * 16;
+  const T* w = static_cast<const T*>(p.W) + (int64_t)(n0 + l16 < p.N ? n0 + l16 : p.N - 1) * p.ldw + quarter * 8;
+  const T* x[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
+    x[t] = static_cast<const T*>(p.X) + (int64_t)(t * 16 + l16 < p.M ? t * 16 + l16 : p.M - 1) * p.ldx + quarter * 8;
+  if (tid < RT * 16) adapter[tid] = tid < p.M ? row_adapter(p.g, tid, p.M) : -1;
+  f32x4 acc[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  int k = wave * 32;
+  constexpr int STEP = kFewWaves * 32;
+  auto steps = [&](auto count) {
+    constexpr int N = decltype(count)::value;
+    Pieces<kPieces<DTYPE>> fw[N], fx[N][RT];
+#pragma unroll
+    for (int i = 0; i < N; ++i) load8<DTYPE, true>(w + k + i * STEP, 1, fw[i]);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int t = 0; t < RT; ++t) load8<DTYPE, true>(x[t] + k + i * STEP, 1, fx[i][t]);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int t = 0; t < RT; ++t) acc[t] = multiply(fw[i], fx[i][t], acc[t]);
+    k += N * STEP;
+  };
+  constexpr int AHEAD = RT == 1 ? 8 : RT == 2 ? 4 : 2;
+  while (k + (AHEAD - 1) * STEP + 32 <= p.K) steps(Count<AHEAD>{});
+  while (k + 32 <= p.K) steps(Count<1>{});
+  if (k < p.K) {
+    const int n = p.K - k - quarter * 8;
+    Pieces<kPieces<DTYPE>> fw, fx;
+    load8_some<DTYPE>(w + k, 1, n, fw);
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      load8_some<DTYPE>(x[t] + k, 1, n, fx);
+      acc[t] = multiply(fw, fx, acc[t]);
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) part[wave][t * 16 + l16][quarter * 4 + i] = acc[t][i];
+  __syncthreads();
+  for (int i = tid; i < RT * 256; i += kFewWaves * 64) {
+    const int row = i >> 4, col = n0 + (i & 15);
+    if (row >= p.M || col >= p.N) continue;
+    float sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < kFewWaves; ++v) sum += part[v][row][i & 15];
+    const int a = adapter[row];
+    if (a >= 0) {
+      const TQ* q = static_cast<const TQ*>(p.Q) + a * p.q_adapter + col * p.q_n;
+      const float* u = p.u + (int64_t)row * p.rank;
+      float low = 0.f;
+      for (int r = 0; r < p.rank; ++r) low = __builtin_fmaf(u[r], Value<QTYPE>::get(q + r * p.q_r), low);
+      sum = __builtin_fmaf(p.scale, low, sum);
+    }
+    if (p.bias) sum += p.bias[col];
+    Value<DTYPE>::put(static_cast<T*>(p.Y) + row * p.ldy + col, sum);
+  }
+}
+
+// ---- dA, dB -----------------------------------------------------------------------------------------
+struct GradsParams {
+  struct Side {
+    const void* V; int64_t stride; int cols;           // x or dy
+    const float* S;                                    // du or u: [rows][rank]
+    float* G; int64_t adapter, col, rank;              // strides of dA or dB
+    float scale;
+  } side[2];
+  int tiles0;                                          // tiles of 64 columns of side 0
+  int64_t rows; int rank;
+  Segments g;
+};
+constexpr int kGradWaves = 8;
+
+// G[c][r] = scale sum_t V[t][c] S[t][r] over the rows t of an adapter's segments: 64 columns of one adapter a workgroup, whose
+// wavefronts take 32 rows each in turn.  Bound by reading V.  The matrix unit wants eight successive t of a column in a
+// lane: a lane loads four neighbouring columns of eight rows and deals them out.
+template <int DTYPE, int NR>
+__global__ __launch_bounds__(kGradWaves * 64) void grads_kernel(GradsParams p) {
+  typedef typename Value<DTYPE>::T T;
+  constexpr int PITCH = NR * 16 + 1;
+  __shared__ float part[kGradWaves / 2][64][PITCH];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, quarter = lane >> 4;
+  const bool second = (int)blockIdx.x >= p.tiles0;
+  const GradsParams::Side& d = p.side[second ? 1 : 0];
+  const int c0 = ((int)blockIdx.x - (second ? p.tiles0 : 0)) * 64, a = blockIdx.y;
+  const int c = c0 + l16 * 4, nc = d.cols - c;         // this lane's columns
+  f32x4 acc[4][NR];
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+#pragma unroll
+    for (int r = 0; r < NR; ++r) acc[q][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const T* V = static_cast<const T*>(d.V) + (nc > 0 ? c : 0);
+  int rank[NR];                                        // past the last: the last again, and dropped
+#pragma unroll
+  for (int r = 0; r < NR; ++r) rank[r] = r * 16 + l16 < p.rank ? r * 16 + l16 : p.rank - 1;
+  for (int s = 0; s < p.g.n; ++s) {
+    if (p.g.which[s] != a) continue;
+    const int64_t lo = seg_row(p.g, s, p.rows), hi = seg_row(p.g, s + 1, p.rows);
+    for (int64_t t0 = lo + wave * 32; t0 < hi; t0 += kGradWaves * 32) {
+      const int64_t t = t0 + quarter * 8;
+      const int nt = hi - t < 8 ? (int)(hi - t) : 8;   // rows that are the segment's: others' may hold anything
+      typedef T T4 __attribute__((ext_vector_type(4)));
+      typedef T4 T4_any __attribute__((aligned(sizeof(T))));
+      T4 w[8];
+      Pieces<3> fs[NR];
+      if (t0 + 32 <= hi && c0 + 64 <= d.cols) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = *reinterpret_cast<const T4_any*>(V + (t + j) * d.stride);
+#pragma unroll
+        for (int r = 0; r < NR; ++r) load8<LSAM_DTYPE_FP32, false>(d.S + t * p.rank + rank[r], p.rank, fs[r]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) w[j][q] = j < nt && q < nc ? V[(t + j) * d.stride + q] : (T)0;
+#pragma unroll
+        for (int r = 0; r < NR; ++r) load8_some<LSAM_DTYPE_FP32>(d.S + t * p.rank + rank[r], p.rank, nt, fs[r]);
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        Pieces<kPieces<DTYPE>> fv;
+        if constexpr (DTYPE == LSAM_DTYPE_BF16) {
+          u16x8 o;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) o[j] = w[j][q];
+          fv.p[0] = __builtin_bit_cast(bf16x8, o);
+        } else {
+          float o[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) o[j] = w[j][q];
+          split8(o, fv);
+        }
+#pragma unroll
+        for (int r = 0; r < NR; ++r) acc[q][r] = multiply(fv, fs[r], acc[q][r]);
+      }
+    }
+  }
+  // lane: rank r 16 + l16, column 4 (4 quarter + i) + q.  The upper half of the wavefronts hand over to the lower, twice.
+  constexpr int H = kGradWaves / 2;
+  if (wave >= H) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part[wave - H][(quarter * 4 + i) * 4 + q][r * 16 + l16] = acc[q][r][i];
+  }
+  __syncthreads();
+  if (wave < H) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part[wave][(quarter * 4 + i) * 4 + q][r * 16 + l16] += acc[q][r][i];
+  }
+  __syncthreads();
+  // lanes along what is contiguous in G
+  for (int i = tid; i < 64 * p.rank; i += kGradWaves * 64) {
+    const int col = d.col == 1 ? i % 64 : i / p.rank, r = d.col == 1 ? i / 64 : i % p.rank;
+    if (c0 + col >= d.cols) continue;
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < H; ++w) sum += part[w][col][r];
+    d.G[a * d.adapter + (c0 + col) * d.col + r * d.rank] = d.scale * sum;
+  }
+}
+
+// ---- pieces, aligned and transposed copies ----------------------------------------------------------
+struct PlanesParams {
+  const void* src; int64_t stride; int64_t rows; int cols;
+  unsigned short* dst; int64_t ld, plane;              // [pieces][rows][ld], or transposed [pieces][cols][ld]; ld a multiple of 8
+};
+template <int DTYPE, bool TRANSPOSE>
+__global__ __launch_bounds__(256) void planes_kernel(PlanesParams p) {
+  typedef typename Value<DTYPE>::T T;
+  constexpr int NP = kPieces<DTYPE>;
+  const int tid = threadIdx.x;
+  if constexpr (!TRANSPOSE) {
+    const unsigned units = (unsigned)(p.ld / 8);
+    const int64_t at = (int64_t)blockIdx.x * 256 + tid, row = at / units;
+    const int c = (int)(at - row * units) * 8;
+    if (row >= p.rows) return;
+    Pieces<NP> o;
+    load8_some<DTYPE>(static_cast<const T*>(p.src) + row * p.stride + c, 1, p.cols - c, o);
+#pragma unroll
+    for (int q = 0; q < NP; ++q) *reinterpret_cast<bf16x8*>(p.dst + q * p.plane + row * p.ld + c) = o.p[q];
+  } else {
+    __shared__ T tile[64][65];
+    const unsigned across = (unsigned)((p.cols + 63) / 64);
+    const int64_t r0 = (int64_t)(blockIdx.x / across) * 64;
+    const int c0 = (int)(blockIdx.x % across) * 64;
+    for (int i = tid; i < 64 * 64; i += 256) {
+      const int64_t r = r0 + i / 64;
+      const int c = c0 + i % 64;
+      tile[i / 64][i % 64] = r < p.rows && c < p.cols ? static_cast<const T*>(p.src)[r * p.stride + c] : (T)0;
+    }
+    __syncthreads();
+    for (int i = tid; i < 64 * 8; i += 256) {
+      const int c = i / 8, r = (i % 8) * 8;
+      if (c0 + c >= p.cols || r0 + r >= p.ld) continue;
+      Pieces<NP> o;
+      if constexpr (DTYPE == LSAM_DTYPE_BF16) {
+        u16x8 w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = tile[r + e][c];
+        o.p[0] = __builtin_bit_cast(bf16x8, w);
+      } else {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = tile[r + e][c];
+        split8(v, o);
+      }
+#pragma unroll
+      for (int q = 0; q < NP; ++q) *reinterpret_cast<bf16x8*>(p.dst + q * p.plane + (int64_t)(c0 + c) * p.ld + r0 + r) = o.p[q];
+    }
+  }
+}
+
+// ---- host -------------------------------------------------------------------------------------------
+int64_t up8(int64_t n) { return (n + 7) & ~7ll; }
+size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// Whether the tiles can be read straight from the caller's rows: bf16, whole aligned units, tiles within 31 bits.
+bool straight(const void* p, int64_t stride, int cols, int dtype) {
+  return dtype == LSAM_DTYPE_BF16 && !misaligned(p, 16) && stride % 8 == 0 && cols % 8 == 0 && stride <= 1 << 21;
+}
+// The same from the descriptor alone: what a workspace must be large enough for.
+size_t planes_bytes(int64_t rows, int cols, int dtype) { return up256((size_t)(dtype == LSAM_DTYPE_BF16 ? 1 : 3) * rows * up8(cols) * 2); }
+
+struct Layout { size_t x, w, u, total; };
+Layout layout(const lsam_adapter_desc* d, bool backward) {
+  Layout l;
+  const bool tiles = backward || d->rows > kFewRows;
+  l.x = 0;
+  l.w = l.x + (tiles ? planes_bytes(d->rows, backward ? d->out : d->in, d->dtype) : 0);
+  // the backward pass reads W transposed
+  l.u = l.w + (backward ? planes_bytes(d->in, d->out, d->dtype) : tiles ? planes_bytes(d->out, d->in, d->dtype) : 0);
+  l.total = l.u + (backward ? up256((size_t)d->rows * d->rank * 4) : 0);
+  return l;
+}
+
+int check(const lsam_adapter_desc* d, const char* who) {
+  if (!d) return refuse(LSAM_EINVAL, "%s: the descriptor is NULL", who);
+  if (!known_dtype(d->dtype) || !known_dtype(d->adapter_dtype)) return refuse(LSAM_EINVAL, "%s: a dtype is none of LSAM_DTYPE_*", who);
+  if (d->rows < 0 || d->rows >= 1ll << 28) return refuse(LSAM_EINVAL, "%s: rows outside 0..2^28-1", who);
+  if (d->in < 1 || d->in > 1 << 21 || d->out < 1 || d->out > 1 << 21) return refuse(LSAM_EINVAL, "%s: in and out must be in 1..2^21", who);
+  if (d->rank < 1 || d->rank > kMaxRank) return refuse(LSAM_EINVAL, "%s: rank outside 1..LSAM_ADAPTER_MAX_RANK", who);
+  if (d->adapters < 0 || d->adapters > 65535 || d->segs < 0) return refuse(LSAM_EINVAL, "%s: adapters outside 0..65535, or segs below 0", who);
+  const int64_t wide = d->in > d->out ? d->in : d->out;
+  if ((int64_t)d->in * d->out > 1ll << 35 || d->rows * wide > 1ll << 35) return refuse(LSAM_EINVAL, "%s: the matrices are too large", who);
+  return LSAM_OK;
+}
+
+// An argument: `bytes` from the first to behind the last value; where it is blocks of `one` bytes each `step` bytes apart, as the
+// adapters of one vector per replica are, those too.
+struct Arg { const char* name; const void* p; int64_t bytes; int align; bool output; int64_t one, step; };
+bool meet(const Arg& a, const Arg& b) {
+  if (!a.p || !b.p || !overlap(a.p, a.bytes, b.p, b.bytes)) return false;
+  if (a.step > 0 && a.step == b.step) {
+    // blocks of both, in turn
+    const int64_t off = (int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p)) % a.step;
+    const int64_t at = off < 0 ? off + a.step : off;
+    return !(at >= a.one && at + b.one <= a.step);
+  }
+  return true;
+}
+int check_args(const Arg* args, int n, const char* who) {
+  for (int i = 0; i < n; ++i) {
+    if (args[i].bytes < 0) return refuse(LSAM_EINVAL, "%s: a stride of %s is too small, or the array is too large", who, args[i].name);
+    if (args[i].bytes && !args[i].p) return refuse(LSAM_EINVAL, "%s: %s is NULL", who, args[i].name);
+    if (misaligned(args[i].p, args[i].align)) return refuse(LSAM_EINVAL, "%s: %s is not aligned to its values", who, args[i].name);
+  }
+  for (int i = 0; i < n; ++i)
+    for (int j = 0; j < n; ++j)
+      if (i != j && args[i].output && meet(args[i], args[j]))
+        return refuse(LSAM_EINVAL, "%s: %s lies over %s", who, args[i].name, args[j].name);
+  return LSAM_OK;
+}
+
+template <int DTYPE, int ATYPE, bool UNIT, int NR>
+void launch_shrink_rank(const ShrinkParams& p, hipStream_t s) {
+  // tiles of 16 rows where segments are no longer than that, of 64 otherwise
+  const bool narrow_tiles = p.rows <= 16ll * p.g.n;
+  const int64_t rows = narrow_tiles ? 16 : 64, tiles = (p.rows + rows - 1) / rows;
+  int64_t y = p.g.n / tiles + 1;
+  y = y > 64 ? 64 : y;
+  const dim3 grid((unsigned)tiles, (unsigned)y);
+  if (narrow_tiles) shrink_kernel<DTYPE, ATYPE, UNIT, NR, 1><<<grid, kShrinkWaves * 64, 0, s>>>(p);
+  else shrink_kernel<DTYPE, ATYPE, UNIT, NR, 4><<<grid, kShrinkWaves * 64, 0, s>>>(p);
+}
+template <int DTYPE, int ATYPE>
+void launch_shrink(const ShrinkParams& p, hipStream_t s) {
+  if (p.a_k == 1) {
+    if (p.rank <= 16) launch_shrink_rank<DTYPE, ATYPE, true, 1>(p, s);
+    else if (p.rank <= 32) launch_shrink_rank<DTYPE, ATYPE, true, 2>(p, s);
+    else launch_shrink_rank<DTYPE, ATYPE, true, 4>(p, s);
+  } else {
+    if (p.rank <= 16) launch_shrink_rank<DTYPE, ATYPE, false, 1>(p, s);
+    else if (p.rank <= 32) launch_shrink_rank<DTYPE, ATYPE, false, 2>(p, s);
+    else launch_shrink_rank<DTYPE, ATYPE, false, 4>(p, s);
+  }
+}
+void launch_shrink_any(const ShrinkParams& p, int dtype, int atype, hipStream_t s) {
+  if (dtype == LSAM_DTYPE_BF16) {
+    if (atype == LSAM_DTYPE_BF16) launch_shrink<LSAM_DTYPE_BF16, LSAM_DTYPE_BF16>(p, s);
+    else launch_shrink<LSAM_DTYPE_BF16, LSAM_DTYPE_FP32>(p, s);
+  } else {
+    if (atype == LSAM_DTYPE_BF16) launch_shrink<LSAM_DTYPE_FP32, LSAM_DTYPE_BF16>(p, s);
+    else launch_shrink<LSAM_DTYPE_FP32, LSAM_DTYPE_FP32>(p, s);
+  }
+}
+
+template <int DTYPE>
+void launch_planes(const void* src, int64_t stride, int64_t rows, int cols, bool transpose, unsigned short* dst, hipStream_t s) {
+  PlanesParams p;
+  p.src = src; p.stride = stride; p.rows = rows; p.cols = cols; p.dst = dst;
+  p.ld = up8(transpose ? rows : cols);
+  p.plane = (transpose ? cols : rows) * p.ld;
+  if (transpose) {
+    const int64_t groups = ((rows + 63) / 64) * ((cols + 63) / 64);
+    planes_kernel<DTYPE, true><<<(unsigned)groups, 256, 0, s>>>(p);
+  } else {
+    const int64_t groups = (rows * (p.ld / 8) + 255) / 256;
+    planes_kernel<DTYPE, false><<<(unsigned)groups, 256, 0, s>>>(p);
+  }
+}
+void launch_planes_any(const void* src, int64_t stride, int64_t rows, int cols, int dtype, bool transpose, unsigned short* dst, hipStream_t s) {
+  if (dtype == LSAM_DTYPE_BF16) launch_planes<LSAM_DTYPE_BF16>(src, stride, rows, cols, transpose, dst, s);
+  else launch_planes<LSAM_DTYPE_FP32>(src, stride, rows, cols, transpose, dst, s);
+}
+
+template <int OTYPE, int QTYPE, int BM, int BN, int WM, int WN>
+void launch_product_tile(ProductParams p, hipStream_t s) {
+  p.tilesM = (int)((p.M + BM - 1) / BM);
+  p.tilesN = (p.N + BN - 1) / BN;
+  product_kernel<OTYPE, QTYPE, BM, BN, WM, WN><<<(unsigned)p.tilesM * (unsigned)p.tilesN, WM * WN * 64, 0, s>>>(p);
+}
+// Large tiles reuse what they read most; smaller ones where large ones would leave units idle.
+template <int OTYPE, int QTYPE>
+void launch_product(const ProductParams& p, hipStream_t s) {
+  auto tiles = [&](int64_t b) { return ((p.M + b - 1) / b) * ((p.N + b - 1) / b); };
+  if (tiles(256) >= 224) launch_product_tile<OTYPE, QTYPE, 256, 256, 2, 2>(p, s);
+  else if (tiles(128) >= 160) launch_product_tile<OTYPE, QTYPE, 128, 128, 2, 2>(p, s);
+  else launch_product_tile<OTYPE, QTYPE, 64, 64, 2, 2>(p, s);
+}
+void launch_product_any(const ProductParams& p, int otype, int qtype, hipStream_t s) {
+  if (otype == LSAM_DTYPE_BF16) {
+    if (qtype == LSAM_DTYPE_BF16) launch_product<LSAM_DTYPE_BF16, LSAM_DTYPE_BF16>(p, s);
+    else launch_product<LSAM_DTYPE_BF16, LSAM_DTYPE_FP32>(p, s);
+  } else {
+    if (qtype == LSAM_DTYPE_BF16) launch_product<LSAM_DTYPE_FP32, LSAM_DTYPE_BF16>(p, s);
+    else launch_product<LSAM_DTYPE_FP32, LSAM_DTYPE_FP32>(p, s);
+  }
+}
+
+template <int DTYPE, int QTYPE>
+void launch_few_rows(const FewRowsParams& p, hipStream_t s) {
+  const unsigned grid = (unsigned)((p.N + 15) / 16);
+  if (p.M <= 16) few_rows_kernel<DTYPE, QTYPE, 1><<<grid, kFewWaves * 64, 0, s>>>(p);
+  else if (p.M <= 32) few_rows_kernel<DTYPE, QTYPE, 2><<<grid, kFewWaves * 64, 0, s>>>(p);
+  else few_rows_kernel<DTYPE, QTYPE, 4><<<grid, kFewWaves * 64, 0, s>>>(p);
+}
+void launch_few_rows_any(const FewRowsParams& p, int dtype, int qtype, hipStream_t s) {
+  if (dtype == LSAM_DTYPE_BF16) {
+    if (qtype == LSAM_DTYPE_BF16) launch_few_rows<LSAM_DTYPE_BF16, LSAM_DTYPE_BF16>(p, s);
+    else launch_few_rows<LSAM_DTYPE_BF16, LSAM_DTYPE_FP32>(p, s);
+  } else {
+    if (qtype == LSAM_DTYPE_BF16) launch_few_rows<LSAM_DTYPE_FP32, LSAM_DTYPE_BF16>(p, s);
+    else launch_few_rows<LSAM_DTYPE_FP32, LSAM_DTYPE_FP32>(p, s);
+  }
+}
+
+template <int DTYPE>
+void launch_grads(const GradsParams& p, int adapters, hipStream_t s) {
+  const dim3 grid((unsigned)(p.tiles0 + (p.side[1].cols + 63) / 64), (unsigned)adapters);
+  if (p.rank <= 16) grads_kernel<DTYPE, 1><<<grid, kGradWaves * 64, 0, s>>>(p);
+  else if (p.rank <= 32) grads_kernel<DTYPE, 2><<<grid, kGradWaves * 64, 0, s>>>(p);
+  else grads_kernel<DTYPE, 4><<<grid, kGradWaves * 64, 0, s>>>(p);
+}
+
+// y = X W'^T + bias + scale u Q: W' is [N][K], or for the backward pass the transposed copy of [K][N].
+struct Product {
+  const lsam_adapter_desc* d;
+  const void* X; int64_t x_stride; int K;
+  const void* W; bool transposed; int N;
+  void* Y; int64_t y_stride;
+  const float* bias; const float* u; float scale;
+  const void* Q; int64_t q_adapter, q_n, q_r;
+  char* ws; Layout l;
+  Segments g;
+};
+void run_product(const Product& o, hipStream_t s) {
+  const lsam_adapter_desc* d = o.d;
+  unsigned short* const ws_x = reinterpret_cast<unsigned short*>(o.ws + o.l.x);
+  unsigned short* const ws_w = reinterpret_cast<unsigned short*>(o.ws + o.l.w);
+  const int64_t ld = up8(o.K);
+  if (d->rows <= kFewRows && !o.transposed) {
+    FewRowsParams p;
+    p.X = o.X; p.ldx = o.x_stride; p.W = o.W; p.ldw = d->w_stride;
+    p.M = (int)d->rows; p.N = o.N; p.K = o.K; p.Y = o.Y; p.ldy = o.y_stride; p.bias = o.bias; p.u = o.u; p.scale = o.scale;
+    p.Q = o.Q; p.q_adapter = o.q_adapter; p.q_n = o.q_n; p.q_r = o.q_r; p.rank = d->rank; p.g = o.g;
+    launch_few_rows_any(p, d->dtype, d->adapter_dtype, s);
+    return;
+  }
+  ProductParams p;
+  p.M = d->rows; p.N = o.N;
+  if (straight(o.X, o.x_stride, o.K, d->dtype)) {
+    p.X = static_cast<const unsigned short*>(o.X); p.ldx = o.x_stride; p.plane_x = 0;
+  } else {
+    launch_planes_any(o.X, o.x_stride, d->rows, o.K, d->dtype, false, ws_x, s);
+    p.X = ws_x; p.ldx = ld; p.plane_x = d->rows * ld;
+  }
+  if (!o.transposed && straight(o.W, d->w_stride, o.K, d->dtype)) {
+    p.W = static_cast<const unsigned short*>(o.W); p.ldw = d->w_stride; p.plane_w = 0;
+  } else {
+    launch_planes_any(o.W, d->w_stride, d->out, d->in, d->dtype, o.transposed, ws_w, s);
+    p.W = ws_w; p.ldw = ld; p.plane_w = o.N * ld;
+  }
+  p.K = (int)ld;                                      // where that is more than K, both are copies, padded with zeros
+  p.products = d->dtype == LSAM_DTYPE_BF16 ? 1 : 6;
+  p.Y = o.Y; p.ldy = o.y_stride; p.bias = o.bias; p.u = o.u; p.scale = o.scale;
+  p.Q = o.Q; p.q_adapter = o.q_adapter; p.q_n = o.q_n; p.q_r = o.q_r; p.rank = d->rank; p.g = o.g;
+  // Pieces of u and of the adapter, enough for the result's type: what is left out is 2^-16 of a product before it is rounded to
+  // bfloat16, 2^-24 otherwise.
+  const bool whole = d->dtype == LSAM_DTYPE_FP32, fine = d->adapter_dtype == LSAM_DTYPE_FP32;
+  if (whole && fine) { p.pairs = 6; p.pair_u = kSixLeft; p.pair_q = kSixRight; }
+  else if (whole) { p.pairs = 3; p.pair_u = 0x012u; p.pair_q = 0x000u; }
+  else if (fine) { p.pairs = 3; p.pair_u = 0x001u; p.pair_q = 0x010u; }
+  else { p.pairs = 2; p.pair_u = 0x01u; p.pair_q = 0x00u; }
+  launch_product_any(p, d->dtype, d->adapter_dtype, s);
+}
+
+Segments segments(const lsam_adapter_desc* d, const int32_t* begin, const int32_t* which) {
+  Segments g;
+  g.begin = begin; g.which = which; g.n = d->adapters > 0 ? d->segs : 0; g.adapters = d->adapters;
+  return g;
+}
+
+int check_workspace(size_t need, const void* workspace, size_t bytes, const char* who) {
+  if (need && (!workspace || bytes < need))
+    return refuse(LSAM_ENOMEM, "%s: the workspace has %zu bytes, %zu are needed", who, workspace ? bytes : 0, need);
+  if (need && misaligned(workspace, 256)) return refuse(LSAM_EINVAL, "%s: the workspace must be 256-byte aligned", who);
+  return LSAM_OK;
+}
+
+}  // namespace
+}  // namespace lsam
+
+using namespace lsam;
+
+extern "C" size_t lsam_adapter_workspace_bytes(const lsam_adapter_desc* d, int32_t backward) {
+  return check(d, "adapter") == LSAM_OK ? layout(d, backward != 0).total : 0;
+}
+
+extern "C" int lsam_adapter(const lsam_adapter_desc* d, const void* x, const void* W, const float* bias, const void* A, const void* B,
+                            const int32_t* seg_begin, const int32_t* seg_adapter, float* u, void* y, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+  int rc = check(d, "adapter");
+  if (rc != LSAM_OK) return rc;
+  if (d->rows == 0) return LSAM_OK;
+  const int b = dtype_bytes(d->dtype), ba = dtype_bytes(d->adapter_dtype);
+  const Arg args[] = {
+      {"x", x, extent(1, 0, d->rows, d->x_stride, d->in, b), b, false, 0, 0},
+      {"W", W, extent(1, 0, d->out, d->w_stride, d->in, b), b, false, 0, 0},
+      {"bias", bias, bias ? d->out * 4ll : 0, 4, false, 0, 0},
+      {"A", A, extent(d->adapters, d->a_adapter, d->rank, d->a_stride, d->in, ba), ba, false, 0, 0},
+      {"B", B, extent(d->adapters, d->b_adapter, d->out, d->b_stride, d->rank, ba), ba, false, 0, 0},
+      {"seg_begin", seg_begin, d->segs ? (d->segs + 1) * 4ll : 0, 4, false, 0, 0},
+      {"seg_adapter", seg_adapter, d->segs * 4ll, 4, false, 0, 0},
+      {"u", u, d->rows * d->rank * 4, 4, true, 0, 0},
+      {"y", y, extent(1, 0, d->rows, d->y_stride, d->out, b), b, true, 0, 0}};
+  rc = check_args(args, sizeof args / sizeof args[0], "adapter");
+  if (rc != LSAM_OK) return rc;
+  const Layout l = layout(d, false);
+  rc = check_workspace(l.total, workspace, workspace_bytes, "adapter");
+  if (rc != LSAM_OK) return rc;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const Segments g = segments(d, seg_begin, seg_adapter);
+  launch_shrink_any(ShrinkParams{x, d->x_stride, A, d->a_adapter, d->a_stride, 1, u, d->rows, d->in, d->rank, 1.f, g}, d->dtype,
+                    d->adapter_dtype, s);
+  run_product(Product{d, x, d->x_stride, d->in, W, false, d->out, y, d->y_stride, bias, u, d->scale, B, d->b_adapter, d->b_stride, 1,
+                      static_cast<char*>(workspace), l, g}, s);
+  return launched();
+}
+
+extern "C" int lsam_adapter_backward(const lsam_adapter_desc* d, const void* x, const void* W, const void* A, const void* B,
+                                     const int32_t* seg_begin, const int32_t* seg_adapter, const float* u, const void* dy, void* dx,
+                                     float* dA, float* dB, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check(d, "adapter_backward");
+  if (rc != LSAM_OK) return rc;
+  if ((dA == nullptr) != (dB == nullptr)) return refuse(LSAM_EINVAL, "adapter_backward: dA and dB are wanted together");
+  const int b = dtype_bytes(d->dtype), ba = dtype_bytes(d->adapter_dtype);
+  const int64_t na = dA ? extent(d->adapters, d->da_adapter, d->rank, d->da_stride, d->in, 4) : 0;
+  const int64_t nb = dB ? extent(d->adapters, d->db_adapter, d->out, d->db_stride, d->rank, 4) : 0;
+  const Arg args[] = {
+      {"x", x, dA ? extent(1, 0, d->rows, d->x_stride, d->in, b) : 0, b, false, 0, 0},
+      {"W", W, dx && d->rows ? extent(1, 0, d->out, d->w_stride, d->in, b) : 0, b, false, 0, 0},
+      {"A", A, d->rows ? extent(d->adapters, d->a_adapter, d->rank, d->a_stride, d->in, ba) : 0, ba, false, 0, 0},
+      {"B", B, d->rows ? extent(d->adapters, d->b_adapter, d->out, d->b_stride, d->rank, ba) : 0, ba, false, 0, 0},
+      {"seg_begin", seg_begin, d->segs ? (d->segs + 1) * 4ll : 0, 4, false, 0, 0},
+      {"seg_adapter", seg_adapter, d->segs * 4ll, 4, false, 0, 0},
+      {"u", u, dA ? d->rows * d->rank * 4 : 0, 4, false, 0, 0},
+      {"dy", dy, extent(1, 0, d->rows, d->dy_stride, d->out, b), b, false, 0, 0},
+      {"dx", dx, dx ? extent(1, 0, d->rows, d->dx_stride, d->in, b) : 0, b, true, 0, 0},
+      {"dA", dA, dA && !apart(d->adapters, d->da_adapter, d->rank, d->da_stride, d->in) ? -1 : na, 4, true,
+       extent(1, 0, d->rank, d->da_stride, d->in, 4), d->adapters > 1 ? d->da_adapter * 4 : 0},
+      {"dB", dB, dB && !apart(d->adapters, d->db_adapter, d->out, d->db_stride, d->rank) ? -1 : nb, 4, true,
+       extent(1, 0, d->out, d->db_stride, d->rank, 4), d->adapters > 1 ? d->db_adapter * 4 : 0}};
+  rc = check_args(args, sizeof args / sizeof args[0], "adapter_backward");
+  if (rc != LSAM_OK) return rc;
+  const Layout l = layout(d, true);
+  rc = check_workspace(l.total, workspace, workspace_bytes, "adapter_backward");
+  if (rc != LSAM_OK) return rc;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const Segments g = segments(d, seg_begin, seg_adapter);
+  float* const du = reinterpret_cast<float*>(static_cast<char*>(workspace) + l.u);
+  if (d->rows > 0)
+    launch_shrink_any(ShrinkParams{dy, d->dy_stride, B, d->b_adapter, 1, d->b_stride, du, d->rows, d->out, d->rank, d->scale, g}, d->dtype,
+                      d->adapter_dtype, s);
+  if (dx && d->rows > 0)
+    run_product(Product{d, dy, d->dy_stride, d->out, W, true, d->in, dx, d->dx_stride, nullptr, du, 1.f, A, d->a_adapter, 1, d->a_stride,
+                        static_cast<char*>(workspace), l, g}, s);
+  if (dA && d->adapters > 0) {
+    GradsParams p;
+    p.side[0] = {x, d->x_stride, d->in, du, dA, d->da_adapter, 1, d->da_stride, 1.f};
+    p.side[1] = {dy, d->dy_stride, d->out, u, dB, d->db_adapter, d->db_stride, 1, d->scale};
+    p.tiles0 = (d->in + 63) / 64;
+    p.rows = d->rows; p.rank = d->rank; p.g = g;
+    if (d->dtype == LSAM_DTYPE_BF16) launch_grads<LSAM_DTYPE_BF16>(p, d->adapters, s);
+    else launch_grads<LSAM_DTYPE_FP32>(p, d->adapters, s);
+  }
+  return launched();
+}

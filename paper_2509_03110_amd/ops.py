@@ -17,9 +17,11 @@ from .lsam import EINVAL, LsamError
 DTYPE_FP32, DTYPE_BF16 = 0, 1
 
 TOP_MAX = 32
+ADAPTER_MAX_RANK = 64
 
 EXPORTS = ["lsam_dropout", "lsam_logprobs_workspace_bytes", "lsam_logprobs", "lsam_logprobs_backward",
-           "lsam_recurrence_workspace_bytes", "lsam_recurrence_states", "lsam_recurrence", "lsam_recurrence_backward"]
+           "lsam_recurrence_workspace_bytes", "lsam_recurrence_states", "lsam_recurrence", "lsam_recurrence_backward",
+           "lsam_adapter_workspace_bytes", "lsam_adapter", "lsam_adapter_backward"]
 
 
 class lsam_dropout_desc(C.Structure):
@@ -44,6 +46,13 @@ class lsam_rows(C.Structure):
 class lsam_recurrence_desc(C.Structure):
     _fields_ = [("seqs", C.c_int64), ("rows", C.c_int64), ("dim", C.c_int64), ("dtype", C.c_int32), ("packed", C.c_int32),
                 ("f", lsam_rows), ("x", lsam_rows), ("h", lsam_rows), ("dh", lsam_rows), ("df", lsam_rows), ("dx", lsam_rows)]
+
+
+class lsam_adapter_desc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("in_", C.c_int32), ("out", C.c_int32), ("rank", C.c_int32), ("adapters", C.c_int32),
+                ("segs", C.c_int32), ("dtype", C.c_int32), ("adapter_dtype", C.c_int32), ("scale", C.c_float)] + [
+                    (n, C.c_int64) for n in ("x_stride", "w_stride", "y_stride", "a_adapter", "a_stride", "b_adapter", "b_stride",
+                                             "dy_stride", "dx_stride", "da_adapter", "da_stride", "db_adapter", "db_stride")]
 
 
 _ready = None
@@ -71,6 +80,12 @@ def _lib():
         L.lsam_recurrence.argtypes = [rec] + [vp] * 8 + [C.c_size_t, vp]
         L.lsam_recurrence_backward.restype = C.c_int
         L.lsam_recurrence_backward.argtypes = [rec] + [vp] * 11 + [C.c_size_t, vp]
+        L.lsam_adapter_workspace_bytes.restype = C.c_size_t
+        L.lsam_adapter_workspace_bytes.argtypes = [C.POINTER(lsam_adapter_desc), C.c_int32]
+        L.lsam_adapter.restype = C.c_int
+        L.lsam_adapter.argtypes = [C.POINTER(lsam_adapter_desc)] + [vp] * 10 + [C.c_size_t, vp]
+        L.lsam_adapter_backward.restype = C.c_int
+        L.lsam_adapter_backward.argtypes = [C.POINTER(lsam_adapter_desc)] + [vp] * 12 + [C.c_size_t, vp]
         _ready = L
     return _ready
 
@@ -306,3 +321,77 @@ def recurrence_backward(f, x, dh, states, h0=None, dlast=None, offsets=None, df=
                                                dh.data_ptr(), _ptr(dlast), df.data_ptr(), dx.data_ptr(), dh0.data_ptr(), _ptr(ws),
                                                need, raw))
     return df, dx, dh0
+
+
+def _adapter_desc(x, W, A, B, seg_begin, seg_adapter, scale):
+    import torch
+    for t, what, n in ((x, "x", 2), (W, "W", 2), (A, "A", 3), (B, "B", 3)):
+        if t.dim() != n:
+            _refuse("%s has %d indices: %d are wanted" % (what, t.dim(), n))
+    _expect(x, "x")
+    d = lsam_adapter_desc()
+    d.rows, d.in_ = x.shape
+    d.out, (d.adapters, d.rank) = W.shape[0], A.shape[:2]
+    _expect(W, "W", like=x, shape=(d.out, d.in_), dtype=x.dtype)
+    _expect(A, "A", like=x, shape=(d.adapters, d.rank, d.in_))
+    _expect(B, "B", like=x, shape=(d.adapters, d.out, d.rank), dtype=A.dtype)
+    _expect(seg_adapter, "seg_adapter", like=x, dtype=torch.int32, dense=True)
+    d.segs = seg_adapter.numel()
+    _expect(seg_begin, "seg_begin", like=x, shape=(d.segs + 1,), dtype=torch.int32, dense=True)
+    d.dtype, d.adapter_dtype, d.scale = _dtype(x, "x"), _dtype(A, "A"), scale
+    d.x_stride, d.w_stride = x.stride(0), W.stride(0)
+    d.a_adapter, d.a_stride = A.stride()[:2]
+    d.b_adapter, d.b_stride = B.stride()[:2]
+    return d
+
+
+def adapter(x, W, A, B, seg_begin, seg_adapter, scale, bias=None, out=None, stream=None):
+    """x W^T + bias + scale (x A_a^T) B_a^T for x [rows, in], W [out, in], A [adapters, rank, in], B [adapters, out, rank], a the adapter of
+    the row's segment (seg_begin: int32 [segs + 1], seg_adapter: int32 [segs]; -1: none); see lsam_adapter.  Returns the
+    result in x's type and u = x A_a^T [rows, rank] in fp32, which `adapter_backward` takes.  A and B may be parts of one
+    [adapters, d] array."""
+    import torch
+    d = _adapter_desc(x, W, A, B, seg_begin, seg_adapter, scale)
+    if bias is not None:
+        _expect(bias, "the bias", like=x, shape=(d.out,), dtype=torch.float32, dense=True)
+    if out is not None:
+        _expect(out, "out", like=x, shape=(d.rows, d.out), dtype=x.dtype)
+    with _On(x, stream) as raw:
+        y = torch.empty((d.rows, d.out), dtype=x.dtype, device=x.device) if out is None else out
+        u = torch.empty((d.rows, d.rank), dtype=torch.float32, device=x.device)
+        d.y_stride = y.stride(0)
+        need = _lib().lsam_adapter_workspace_bytes(C.byref(d), 0)
+        ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+        _check(_lib().lsam_adapter(C.byref(d), x.data_ptr(), W.data_ptr(), _ptr(bias), A.data_ptr(), B.data_ptr(), seg_begin.data_ptr(),
+                                   seg_adapter.data_ptr(), u.data_ptr(), y.data_ptr(), _ptr(ws), need, raw))
+    return y, u
+
+
+def adapter_backward(x, W, A, B, u, dy, seg_begin, seg_adapter, scale, dx=None, dA=None, dB=None, want_dx=True, want_adapters=True,
+                     stream=None):
+    """Gradients (dx, dA, dB) of `adapter` for dy [rows, out]: dx in x's type, dA and dB in fp32, written whole.  dA and dB may be
+    parts of one [adapters, d] array, as gradients that go to lsam_step_grads are.  What is not wanted is None."""
+    import torch
+    d = _adapter_desc(x, W, A, B, seg_begin, seg_adapter, scale)
+    _expect(dy, "dy", like=x, shape=(d.rows, d.out), dtype=x.dtype)
+    _expect(u, "u", like=x, shape=(d.rows, d.rank), dtype=torch.float32, dense=True)
+    for t, what, shape, dtype in ((dx, "dx", x.shape, x.dtype), (dA, "dA", A.shape, torch.float32), (dB, "dB", B.shape, torch.float32)):
+        if t is not None:
+            _expect(t, what, like=x, shape=shape, dtype=dtype)
+    with _On(x, stream) as raw:
+        new = lambda like, dtype: torch.empty(like.shape, dtype=dtype, device=x.device)  # noqa: E731
+        dx = (new(x, x.dtype) if dx is None else dx) if want_dx else None
+        dA = (new(A, torch.float32) if dA is None else dA) if want_adapters else None
+        dB = (new(B, torch.float32) if dB is None else dB) if want_adapters else None
+        d.dy_stride = dy.stride(0)
+        if want_dx:
+            d.dx_stride = dx.stride(0)
+        if want_adapters:
+            d.da_adapter, d.da_stride = dA.stride()[:2]
+            d.db_adapter, d.db_stride = dB.stride()[:2]
+        need = _lib().lsam_adapter_workspace_bytes(C.byref(d), 1)
+        ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+        _check(_lib().lsam_adapter_backward(C.byref(d), x.data_ptr(), W.data_ptr(), A.data_ptr(), B.data_ptr(), seg_begin.data_ptr(),
+                                            seg_adapter.data_ptr(), u.data_ptr(), dy.data_ptr(), _ptr(dx), _ptr(dA), _ptr(dB), _ptr(ws),
+                                            need, raw))
+    return dx, dA, dB

@@ -125,3 +125,57 @@ def test_recurrence_checks_its_arguments_before_touching_the_gpu():
     assert forward(long, ws=(6 << 30) + 4, n=need, **far) == lsam.EINVAL
     assert L.lsam_recurrence_states(desc()) == 2 and L.lsam_recurrence_states(desc(dim=0)) == lsam.EINVAL
     assert forward(desc(seqs=0), f=None, x=None, h=None) == 0 and backward(desc(seqs=0), f=None) == 0
+
+
+def test_adapter_checks_its_arguments_before_touching_the_gpu():
+    L = ops._lib()
+
+    def desc(**over):
+        d = ops.lsam_adapter_desc()
+        d.rows, d.in_, d.out, d.rank, d.adapters, d.segs, d.dtype, d.adapter_dtype, d.scale = 100, 32, 48, 8, 3, 4, 1, 0, 1.0
+        d.x_stride = d.w_stride = d.a_stride = d.dx_stride = d.da_stride = 32
+        d.y_stride = d.dy_stride = 48
+        d.b_stride = d.db_stride = 8
+        d.a_adapter = d.da_adapter = 8 * 32
+        d.b_adapter = d.db_adapter = 8 * 48
+        for k, v in over.items():
+            setattr(d, k, v)
+        return C.byref(d)
+    P = {n: FAKE * (i + 1) for i, n in enumerate(("x", "W", "bias", "A", "B", "begin", "which", "u", "y", "dy", "dx", "dA", "dB", "ws"))}
+
+    def forward(d, n=1 << 20, **over):
+        a = dict(P, **over)
+        return L.lsam_adapter(d, *(a[k] for k in ("x", "W", "bias", "A", "B", "begin", "which", "u", "y", "ws")), n, None)
+
+    def backward(d, n=1 << 20, **over):
+        a = dict(P, **over)
+        return L.lsam_adapter_backward(d, *(a[k] for k in ("x", "W", "A", "B", "begin", "which", "u", "dy", "dx", "dA", "dB", "ws")), n, None)
+    for over, msg in ((dict(dtype=2), "dtype"), (dict(adapter_dtype=-1), "dtype"), (dict(rows=-1), "rows"), (dict(rows=1 << 28), "rows"),
+                      (dict(in_=0), "in and out"), (dict(out=(1 << 21) + 1), "in and out"), (dict(rank=0), "rank"), (dict(rank=65), "rank"),
+                      (dict(adapters=-1), "adapters"), (dict(adapters=65536), "adapters"), (dict(segs=-1), "segs"),
+                      (dict(in_=1 << 20, out=1 << 20), "too large"), (dict(rows=1 << 27, in_=1 << 20), "too large"),
+                      (dict(x_stride=31), "stride of x"), (dict(w_stride=-32), "stride of W"), (dict(a_stride=31), "stride of A"),
+                      (dict(b_adapter=-1), "stride of B")):
+        assert forward(desc(**over)) == lsam.EINVAL and msg in lsam.last_error(), (over, lsam.last_error())
+        assert backward(desc(**over)) == lsam.EINVAL and msg in lsam.last_error(), (over, lsam.last_error())
+    assert forward(desc(y_stride=47)) == lsam.EINVAL and backward(desc(dy_stride=47)) == lsam.EINVAL
+    assert backward(desc(dx_stride=31)) == lsam.EINVAL and backward(desc(da_adapter=255)) == lsam.EINVAL
+    assert backward(desc(db_stride=7)) == lsam.EINVAL
+    for name in ("x", "W", "A", "B", "begin", "which", "u", "y"):
+        assert forward(desc(), **{name: None}) == lsam.EINVAL and name in lsam.last_error(), (name, lsam.last_error())
+    for name in ("x", "W", "A", "B", "begin", "which", "u", "dy"):
+        assert backward(desc(), **{name: None}) == lsam.EINVAL and name in lsam.last_error(), (name, lsam.last_error())
+    assert backward(desc(), dA=None) == lsam.EINVAL and "together" in lsam.last_error()
+    assert forward(desc(), y=P["x"]) == lsam.EINVAL and "lies over" in lsam.last_error()
+    assert backward(desc(), dx=P["dy"] + 2) == lsam.EINVAL and "lies over" in lsam.last_error()
+    assert backward(desc(), dB=P["dA"] + 64) == lsam.EINVAL and "lies over" in lsam.last_error()
+    # blocks of one array per adapter, in turn: dB may not reach into dA's blocks
+    apart = desc(da_adapter=1000, db_adapter=1000)
+    assert backward(apart, dB=P["dA"] + 4 * 255) == lsam.EINVAL and "lies over" in lsam.last_error()
+    assert backward(apart, dB=P["dA"] + 4 * 617) == lsam.EINVAL and "lies over" in lsam.last_error()
+    assert backward(apart, dB=P["dA"] + 4 * 616, n=0) == lsam.ENOMEM
+    assert forward(desc(), x=P["x"] + 1) == lsam.EINVAL and "aligned" in lsam.last_error()
+    assert forward(desc(), ws=None) == lsam.ENOMEM and forward(desc(), ws=P["ws"] + 16) == lsam.EINVAL
+    assert L.lsam_adapter_workspace_bytes(desc(rank=0), 0) == 0 and L.lsam_adapter_workspace_bytes(desc(rows=64), 0) == 0
+    assert L.lsam_adapter_workspace_bytes(desc(), 1) > 100 * 8 * 4
+    assert forward(desc(rows=0), x=None, y=None, u=None) == 0
