@@ -162,9 +162,9 @@ def test_adapter_checks_its_arguments_before_touching_the_gpu():
     assert backward(desc(dx_stride=31)) == lsam.EINVAL and backward(desc(da_adapter=255)) == lsam.EINVAL
     assert backward(desc(db_stride=7)) == lsam.EINVAL
     for name in ("x", "W", "A", "B", "begin", "which", "u", "y"):
-        assert forward(desc(), **{name: None}) == lsam.EINVAL and name in lsam.last_error(), (name, lsam.last_error())
+        assert forward(desc(), **{name: None}) == lsam.EINVAL and "NULL" in lsam.last_error(), (name, lsam.last_error())
     for name in ("x", "W", "A", "B", "begin", "which", "u", "dy"):
-        assert backward(desc(), **{name: None}) == lsam.EINVAL and name in lsam.last_error(), (name, lsam.last_error())
+        assert backward(desc(), **{name: None}) == lsam.EINVAL and "NULL" in lsam.last_error(), (name, lsam.last_error())
     assert backward(desc(), dA=None) == lsam.EINVAL and "together" in lsam.last_error()
     assert forward(desc(), y=P["x"]) == lsam.EINVAL and "lies over" in lsam.last_error()
     assert backward(desc(), dx=P["dy"] + 2) == lsam.EINVAL and "lies over" in lsam.last_error()
