@@ -127,6 +127,29 @@ __device__ __forceinline__ f32x4 multiply(const Pieces<NA>& a, const Pieces<NB>&
   return c;
 }
 
+// The six products of three pieces each that fp32 can tell from 0, the smallest first, four bits for a piece: l h, m m, h l,
+// m h, h m, h h.
+constexpr unsigned kSixLeft = 0x001012u, kSixRight = 0x010210u;
+
+// A number's leading bfloat16 piece, as split_planes makes it, and its piece `which`.
+__device__ __forceinline__ unsigned short leading_piece(float x) {
+  const unsigned u = __builtin_bit_cast(unsigned, x), mag = u & 0x7FFFFFFFu;
+  return mag >= 0x7F7F8000u && mag <= 0x7F800000u ? (unsigned short)(u >> 16) : narrow(x);
+}
+__device__ __forceinline__ unsigned short piece(float x, unsigned which) {
+  float r = x;
+  for (unsigned q = 0; q < which; ++q) r = __builtin_fabsf(r) < __builtin_inff() ? r - widen(leading_piece(r)) : 0.f;
+  return leading_piece(r);
+}
+
+// The low-rank part of a product as more steps of its contraction: for each pair of pieces a copy of u and of the adapter, rank
+// padded to 8 (`padded`), side by side.
+struct LowRank {
+  int rank, padded, pairs;
+  unsigned left, right;                               // the pieces of each pair, four bits each
+  int k() const { return pairs * padded; }
+};
+
 // ---- u = x A^T, du = scale dy B ---------------------------------------------------------------------
 constexpr int kShrinkWaves = 8;
 
@@ -136,6 +159,7 @@ struct ShrinkParams {
   float* u;
   int64_t rows; int K, rank;
   float scale;
+  unsigned short* copy; float copy_scale; LowRank low; int low_k;      // pieces of copy_scale u for product_kernel, or null
   Segments g;
 };
 
@@ -234,17 +258,55 @@ __global__ __launch_bounds__(kShrinkWaves * 64) void shrink_kernel(ShrinkParams 
         __syncthreads();
         for (int i = tid; i < 16 * NR * 16; i += kShrinkWaves * 64) {
           const int row = i / (NR * 16), r = i % (NR * 16);
-          if (r < p.rank && lo + t * 16 + row < hi) {
+          if (r < p.low.padded && lo + t * 16 + row < hi) {
             float sum = 0.f;
 #pragma unroll
             for (int w = 0; w < kShrinkWaves; ++w) sum += part[w][row][r];
-            p.u[(lo + t * 16 + row) * p.rank + r] = p.scale * sum;
+            sum = r < p.rank ? p.scale * sum : 0.f;
+            if (r < p.rank) p.u[(lo + t * 16 + row) * p.rank + r] = sum;
+            if (p.copy)
+              for (int q = 0; q < p.low.pairs; ++q)
+                p.copy[(lo + t * 16 + row) * p.low_k + q * p.low.padded + r] = piece(p.copy_scale * sum, (p.low.left >> (4 * q)) & 15u);
           }
         }
       }
     }
     __syncthreads();
   }
+}
+
+// ---- the adapters' pieces for product_kernel --------------------------------------------------------
+struct CopiesParams {
+  const void* Q; int64_t q_adapter, q_n, q_r;         // strides along adapter, output and rank
+  unsigned short* copy; unsigned char* odd;           // [adapters][N][low_k], [adapters][N]
+  int adapters, N, low_k;
+  LowRank low;
+};
+// An infinity or NaN in an adapter would reach the rows of other segments in its tile, whose 0 it is multiplied with: it is left
+// out here, and the outputs it belongs to are marked.
+template <int QTYPE>
+__global__ __launch_bounds__(256) void copies_kernel(CopiesParams p) {
+  typedef typename Value<QTYPE>::T TQ;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int a = (int)(at / p.N), n = (int)(at - (int64_t)a * p.N);
+  if (a >= p.adapters) return;
+  const TQ* q = static_cast<const TQ*>(p.Q) + a * p.q_adapter + n * p.q_n;
+  bool odd = false;
+  for (int r0 = 0; r0 < p.low.padded; r0 += 8) {
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] = r0 + e < p.low.rank ? Value<QTYPE>::get(q + (r0 + e) * p.q_r) : 0.f;
+      if (!(__builtin_fabsf(v[e]) < __builtin_inff())) { v[e] = 0.f; odd = true; }
+    }
+    for (int i = 0; i < p.low.pairs; ++i) {
+      u16x8 o;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = piece(v[e], (p.low.right >> (4 * i)) & 15u);
+      *reinterpret_cast<u16x8*>(p.copy + at * p.low_k + i * p.low.padded + r0) = o;
+    }
+  }
+  p.odd[at] = odd;
 }
 
 // ---- y or dx, many rows -----------------------------------------------------------------------------
@@ -255,17 +317,12 @@ struct ProductParams {
   int64_t M; int N, K;                                // K a multiple of 8, rows 16-byte aligned
   void* Y; int64_t ldy;
   const float* bias;
-  const float* u; float scale;                        // [M][rank]
-  const void* Q; int64_t q_adapter, q_n, q_r;         // strides along adapter, output and rank
-  int rank;
-  int pairs; unsigned pair_u, pair_q;                 // products of pieces of u and Q: four bits for the piece of each
+  const unsigned short* u; const unsigned short* Q;   // copies: [M][low_k], [adapters][N][low_k]
+  const unsigned char* odd;                           // [adapters][N]
+  int low_k;
   int tilesM, tilesN;
   Segments g;
 };
-
-// The six products of three pieces each that fp32 can tell from 0, the smallest first, four bits for a piece: l h, m m, h l,
-// m h, h m, h h.
-constexpr unsigned kSixLeft = 0x001012u, kSixRight = 0x010210u;
 
 constexpr int kBK = 64;                               // numbers of a row in a step: 128 bytes
 constexpr int waitcnt(int vm, int lgkm) { return (vm & 0xF) | ((vm >> 4) << 14) | (0x7 << 4) | ((lgkm & 0xF) << 8); }
@@ -311,45 +368,32 @@ struct RowTile {
                                                k0 + k[j] < K ? goff[j] + (unsigned)k0 * 2u : 0x7FFFFFF0u, 0, 0, 0);
   }
 };
+// The same for numbers k0 .. k0 + 63 of the first `rows` rows of [rows][ld], K = ld, as zeros the rows outside lo .. hi - 1.
+template <int R, int NW>
+__device__ __forceinline__ void issue_rows(const unsigned short* base, int ld, int rows, int lo, int hi, lds_byte* tile, int k0,
+                                           int lane, int wave) {
+  const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(base, (unsigned)(rows * ld * 2));
+  constexpr int NLOAD = R / 8 / NW;
+#pragma unroll
+  for (int j = 0; j < NLOAD; ++j) {
+    const int row = (wave * NLOAD + j) * 8 + (lane >> 3), k = k0 + ((lane & 7) ^ (row & 7)) * 8;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(tile + (wave * NLOAD + j) * 1024), 16,
+                                             row >= lo && row < hi && k < ld ? (unsigned)(row * ld + k) * 2u : 0x7FFFFFF0u, 0, 0, 0);
+  }
+}
 // The 16 bytes that a lane feeds to the matrix unit: row `row`, numbers 16 kc + 8 half ..
 __device__ __forceinline__ u32x4 fragment(const lds_byte* tile, int row, int kc, int half) {
   return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(tile + row * 128 + (((kc * 2 + half) ^ (row & 7)) << 4));
 }
-__device__ __forceinline__ void put_unit(lds_byte* tile, int row, int unit, u32x4 v) {
-  *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(tile + row * 128 + ((unit ^ (row & 7)) << 4)) = v;
-}
-
-// Piece `which` of eight numbers, as split_planes makes them, with few registers.
-__device__ __forceinline__ unsigned short leading_piece(float x) {
-  const unsigned u = __builtin_bit_cast(unsigned, x), mag = u & 0x7FFFFFFFu;
-  return mag >= 0x7F7F8000u && mag <= 0x7F800000u ? (unsigned short)(u >> 16) : narrow(x);
-}
-__device__ __forceinline__ u32x4 piece8(const float (&v)[8], unsigned which) {
-  u16x8 o;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    float r = v[e];
-#pragma unroll
-    for (unsigned q = 0; q < 2; ++q) {
-      const float rest = __builtin_fabsf(r) < __builtin_inff() ? r - widen(leading_piece(r)) : 0.f;
-      r = which > q ? rest : r;
-    }
-    o[e] = leading_piece(r);
-  }
-  return __builtin_bit_cast(u32x4, o);
-}
-
 // BM x BN outputs by WM x WN wavefronts, each a block of 32 x 32 results TM x TN times.
-template <int OTYPE, int QTYPE, int BM, int BN, int WM, int WN>
+template <int OTYPE, int BM, int BN, int WM, int WN>
 __device__ __forceinline__ void product_tile(const ProductParams& p) {
-  constexpr int NW = WM * WN, NT = NW * 64;
+  constexpr int NW = WM * WN;
   constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
   typedef RowTile<BM, NW> OX;
   typedef RowTile<BN, NW> OW;
   __shared__ __attribute__((aligned(1024))) unsigned char st0[OX::BYTES + OW::BYTES];
   __shared__ __attribute__((aligned(1024))) unsigned char st1[OX::BYTES + OW::BYTES];
-  __shared__ int not_finite[BN];
-  __shared__ int any_not_finite;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, half = lane >> 5;
   const int wm = (wave / WN) * (TM * 32), wn = (wave % WN) * (TN * 32);
@@ -398,108 +442,64 @@ __device__ __forceinline__ void product_tile(const ProductParams& p) {
       for (int j = 0; j < TN; ++j) acc[i][j] = mfma32(fw[buf][j], fx[buf][i], acc[i][j]);
   };
 
-  // Steps: the products of planes one after the other, each over all of K.  Step s + 1 is on its way while s is multiplied.
-  const int per_product = (p.K + kBK - 1) / kBK, steps = p.products * per_product;
+  // Steps: the products of planes one after the other, each over all of K.  A step is requested while the one before it is
+  // multiplied; behind the last one zeros are, which add nothing, so that the loop has no exit between its two halves.
+  const int steps = p.products * ((p.K + kBK - 1) / kBK);
   int next_k = 0, next_q = 0;
-  auto request = [&](lds_byte* tile, int step) {
-    if (step >= steps) return;
-    const unsigned px = p.products == 1 ? 0u : (kSixLeft >> (4 * next_q)) & 15u;
-    const unsigned pw = p.products == 1 ? 0u : (kSixRight >> (4 * next_q)) & 15u;
-    ox.issue(make_rsrc(X + px * p.plane_x, bytes_x), tile, next_k, p.K, wave);
-    ow.issue(make_rsrc(W + pw * p.plane_w, bytes_w), tile + OX::BYTES, next_k, p.K, wave);
+  auto request = [&](lds_byte* tile) {
+    const bool some = next_q < p.products;
+    const unsigned px = p.products > 1 && some ? (kSixLeft >> (4 * next_q)) & 15u : 0u;
+    const unsigned pw = p.products > 1 && some ? (kSixRight >> (4 * next_q)) & 15u : 0u;
+    const int k0 = some ? next_k : p.K;
+    ox.issue(make_rsrc(X + px * p.plane_x, bytes_x), tile, k0, p.K, wave);
+    ow.issue(make_rsrc(W + pw * p.plane_w, bytes_w), tile + OX::BYTES, k0, p.K, wave);
     next_k += kBK;
-    if (next_k >= per_product * kBK) { next_k = 0; ++next_q; }
+    if (next_k >= p.K) { next_k = 0; ++next_q; }
   };
-  request(a0, 0);
-  request(a1, 1);
+  request(a0);
+  request(a1);
   arrived();
   read(a0, 0, 0);
-  auto step = [&](lds_byte* now, lds_byte* then, int s) {
+  auto step = [&](lds_byte* now, lds_byte* then) {
     read(now, 1, 1);
     multiply_chunk(0);
     read(now, 2, 0);
     multiply_chunk(1);
     read(now, 3, 1);
     multiply_chunk(0);
-    // Every wavefront has taken its last fragment of this step and the next one has arrived, requested a step ago.
+    // Every wavefront has taken its last fragment of this step, and the next one, requested a step ago, has arrived.
     arrived();
-    request(now, s + 2);
-    read(then, 0, 0);                    // past the last step: never multiplied
+    request(now);
+    read(then, 0, 0);                    // behind the last step: never multiplied
     multiply_chunk(1);
   };
   for (int s = 0; s < steps; s += 2) {
-    step(a0, a1, s);
-    if (s + 1 < steps) step(a1, a0, s + 1);
+    step(a0, a1);
+    step(a1, a0);
   }
-  __syncthreads();
+  arrived();                             // nothing may still be on its way to LDS
 
-  // The adapters of the tile's rows.
-  const int rp = (p.rank + 7) & ~7, low_k = p.pairs * rp;
+  // Every segment that rows of the tile belong to: the copies of u and of its adapter, rows of other segments being zeros.
   const int found = seg_at(p.g, m0);
-  for (int s = found < 0 ? 0 : found; s < p.g.n; ++s) {
-    int64_t lo = seg_row(p.g, s, p.M) - m0, hi = seg_row(p.g, s + 1, p.M) - m0;
-    if (lo >= m_here) break;
-    lo = lo > 0 ? lo : 0;
-    hi = hi < m_here ? hi : m_here;
-    const int a = seg_adapter(p.g, s);
+  const int seg0 = found < 0 ? 0 : found;
+  for (int s = seg0; s < p.g.n; ++s) {
+    const int64_t l = seg_row(p.g, s, p.M) - m0, h = seg_row(p.g, s + 1, p.M) - m0;
+    if (l >= m_here) break;
+    const int lo = (int)(l > 0 ? l : 0), hi = (int)(h < m_here ? h : m_here), a = seg_adapter(p.g, s);
     if (a < 0 || lo >= hi) continue;
-    typedef typename Value<QTYPE>::T TQ;
-    const TQ* Q = static_cast<const TQ*>(p.Q) + a * p.q_adapter + n0 * p.q_n;
-    if (tid < BN) not_finite[tid] = 0;
-    if (tid == 0) any_not_finite = 0;
-    __syncthreads();
-    for (int k0 = 0; k0 < low_k; k0 += kBK) {
-      for (int i = tid; i < BM * 8; i += NT) {
-        const int row = i >> 3, k = k0 + (i & 7) * 8;
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (row >= lo && row < hi && k < low_k) {
-          const float* u = p.u + (m0 + row) * p.rank + k % rp;
-          const int n = p.rank - k % rp;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = e < n ? p.scale * u[e] : 0.f;
-        }
-        put_unit(a0, row, i & 7, piece8(v, k < low_k ? (p.pair_u >> (4 * (k / rp))) & 15u : 0u));
-      }
-      for (int i = tid; i < BN * 8; i += NT) {
-        // lanes along whatever is contiguous in Q
-        const int col = p.q_r == 1 ? i >> 3 : i % BN, unit = p.q_r == 1 ? i & 7 : i / BN, k = k0 + unit * 8;
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (col < n_here && k < low_k) {
-          const TQ* q = Q + col * p.q_n + (k % rp) * p.q_r;
-          const int n = p.rank - k % rp;
-          bool odd = false;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            v[e] = e < n ? Value<QTYPE>::get(q + e * p.q_r) : 0.f;
-            // An infinity or NaN here would reach the rows of other segments, whose 0 it is multiplied with.
-            if (!(__builtin_fabsf(v[e]) < __builtin_inff())) { v[e] = 0.f; odd = true; }
-          }
-          if (odd) { not_finite[col] = 1; any_not_finite = 1; }
-        }
-        put_unit(a0 + OX::BYTES, col, unit, piece8(v, k < low_k ? (p.pair_q >> (4 * (k / rp))) & 15u : 0u));
-      }
-      __syncthreads();
+    for (int k0 = 0; k0 < p.low_k; k0 += kBK) {
+      issue_rows<BM, NW>(p.u + m0 * p.low_k, p.low_k, (int)m_here, lo, hi, a0, k0, lane, wave);
+      issue_rows<BN, NW>(p.Q + ((int64_t)a * p.N + n0) * p.low_k, p.low_k, n_here, 0, n_here, a0 + OX::BYTES, k0, lane, wave);
+      arrived();
 #pragma unroll
       for (int kc = 0; kc < 4; ++kc) {
-        if (k0 + kc * 16 < low_k) {
+        if (k0 + kc * 16 < p.low_k) {
           read(a0, kc, 0);
           multiply_chunk(0);
         }
       }
-      __syncthreads();
+      arrived();
     }
-    if (any_not_finite) {
-#pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        const int row = wm + i * 32 + l32;
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (row >= lo && row < hi && not_finite[wn + j * 32 + (e >> 2) * 8 + half * 4 + (e & 3)]) acc[i][j][e] = __builtin_nanf("");
-      }
-    }
-    __syncthreads();
   }
 
   typedef Value<OTYPE> VO;
@@ -531,11 +531,32 @@ __device__ __forceinline__ void product_tile(const ProductParams& p) {
         }
     }
   }
+
+  // Outputs that a number of their adapter's belongs to which is not finite: the lane that stored them says so.
+  for (int s = seg0; s < p.g.n; ++s) {
+    const int64_t l = seg_row(p.g, s, p.M) - m0, h = seg_row(p.g, s + 1, p.M) - m0;
+    if (l >= m_here) break;
+    const int a = seg_adapter(p.g, s);
+    if (a < 0 || l >= h) continue;
+    const unsigned char* odd = p.odd + (int64_t)a * p.N + n0;
+    bool some = false;
+    for (int n = lane; n < n_here; n += 64) some |= odd[n] != 0;
+    if (__ballot(some) == 0) continue;
+    for (int i = 0; i < TM; ++i) {
+      const int row = wm + i * 32 + l32;
+      if (row < l || row >= h || row >= m_here) continue;
+      TO* y = static_cast<TO*>(p.Y) + (m0 + row) * p.ldy + n0;
+      for (int c = 0; c < TN * 16; ++c) {
+        const int col = wn + (c >> 4) * 32 + ((c >> 2) & 3) * 8 + half * 4 + (c & 3);
+        if (col < n_here && odd[col]) VO::put(y + col, __builtin_nanf(""));
+      }
+    }
+  }
 }
 
-template <int OTYPE, int QTYPE, int BM, int BN, int WM, int WN>
+template <int OTYPE, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM * WN * 64) void product_kernel(ProductParams p) {
-  product_tile<OTYPE, QTYPE, BM, BN, WM, WN>(p);
+  product_tile<OTYPE, BM, BN, WM, WN>(p);
 }
 
 // ---- y or dx, at most 64 rows -----------------------------------------------------------------------
@@ -799,15 +820,35 @@ bool straight(const void* p, int64_t stride, int cols, int dtype) {
 // The same from the descriptor alone: what a workspace must be large enough for.
 size_t planes_bytes(int64_t rows, int cols, int dtype) { return up256((size_t)(dtype == LSAM_DTYPE_BF16 ? 1 : 3) * rows * up8(cols) * 2); }
 
-struct Layout { size_t x, w, u, total; };
+// Pieces of u and of the adapter, enough for the result's type: what is left out is 2^-16 of a product before it is rounded to
+// bfloat16, 2^-24 otherwise.
+LowRank low_rank(const lsam_adapter_desc* d) {
+  LowRank l;
+  l.rank = d->rank;
+  l.padded = (d->rank + 7) & ~7;
+  const bool whole = d->dtype == LSAM_DTYPE_FP32, fine = d->adapter_dtype == LSAM_DTYPE_FP32;
+  if (whole && fine) { l.pairs = 6; l.left = kSixLeft; l.right = kSixRight; }
+  else if (whole) { l.pairs = 3; l.left = 0x012u; l.right = 0x000u; }
+  else if (fine) { l.pairs = 3; l.left = 0x001u; l.right = 0x010u; }
+  else { l.pairs = 2; l.left = 0x01u; l.right = 0x00u; }
+  return l;
+}
+
+// Offsets in the workspace: copies of x or dy and of W, of u and of the adapters, marks, du.
+struct Layout { size_t x, w, u, q, odd, du, total; bool tiles; };
 Layout layout(const lsam_adapter_desc* d, bool backward) {
   Layout l;
-  const bool tiles = backward || d->rows > kFewRows;
+  const int N = backward ? d->in : d->out;
+  l.tiles = backward || d->rows > kFewRows;
   l.x = 0;
-  l.w = l.x + (tiles ? planes_bytes(d->rows, backward ? d->out : d->in, d->dtype) : 0);
+  l.w = l.x + (l.tiles ? planes_bytes(d->rows, backward ? d->out : d->in, d->dtype) : 0);
   // the backward pass reads W transposed
-  l.u = l.w + (backward ? planes_bytes(d->in, d->out, d->dtype) : tiles ? planes_bytes(d->out, d->in, d->dtype) : 0);
-  l.total = l.u + (backward ? up256((size_t)d->rows * d->rank * 4) : 0);
+  l.u = l.w + (backward ? planes_bytes(d->in, d->out, d->dtype) : l.tiles ? planes_bytes(d->out, d->in, d->dtype) : 0);
+  const size_t low_k = (size_t)low_rank(d).k();
+  l.q = l.u + (l.tiles ? up256((size_t)d->rows * low_k * 2) : 0);
+  l.odd = l.q + (l.tiles ? up256((size_t)d->adapters * N * low_k * 2) : 0);
+  l.du = l.odd + (l.tiles ? up256((size_t)d->adapters * N) : 0);
+  l.total = l.du + (backward ? up256((size_t)d->rows * d->rank * 4) : 0);
   return l;
 }
 
@@ -901,28 +942,19 @@ void launch_planes_any(const void* src, int64_t stride, int64_t rows, int cols, 
   else launch_planes<LSAM_DTYPE_FP32>(src, stride, rows, cols, transpose, dst, s);
 }
 
-template <int OTYPE, int QTYPE, int BM, int BN, int WM, int WN>
+template <int OTYPE, int BM, int BN, int WM, int WN>
 void launch_product_tile(ProductParams p, hipStream_t s) {
   p.tilesM = (int)((p.M + BM - 1) / BM);
   p.tilesN = (p.N + BN - 1) / BN;
-  product_kernel<OTYPE, QTYPE, BM, BN, WM, WN><<<(unsigned)p.tilesM * (unsigned)p.tilesN, WM * WN * 64, 0, s>>>(p);
+  product_kernel<OTYPE, BM, BN, WM, WN><<<(unsigned)p.tilesM * (unsigned)p.tilesN, WM * WN * 64, 0, s>>>(p);
 }
 // Large tiles reuse what they read most; smaller ones where large ones would leave units idle.
-template <int OTYPE, int QTYPE>
+template <int OTYPE>
 void launch_product(const ProductParams& p, hipStream_t s) {
   auto tiles = [&](int64_t b) { return ((p.M + b - 1) / b) * ((p.N + b - 1) / b); };
-  if (tiles(256) >= 224) launch_product_tile<OTYPE, QTYPE, 256, 256, 2, 2>(p, s);
-  else if (tiles(128) >= 160) launch_product_tile<OTYPE, QTYPE, 128, 128, 2, 2>(p, s);
-  else launch_product_tile<OTYPE, QTYPE, 64, 64, 2, 2>(p, s);
-}
-void launch_product_any(const ProductParams& p, int otype, int qtype, hipStream_t s) {
-  if (otype == LSAM_DTYPE_BF16) {
-    if (qtype == LSAM_DTYPE_BF16) launch_product<LSAM_DTYPE_BF16, LSAM_DTYPE_BF16>(p, s);
-    else launch_product<LSAM_DTYPE_BF16, LSAM_DTYPE_FP32>(p, s);
-  } else {
-    if (qtype == LSAM_DTYPE_BF16) launch_product<LSAM_DTYPE_FP32, LSAM_DTYPE_BF16>(p, s);
-    else launch_product<LSAM_DTYPE_FP32, LSAM_DTYPE_FP32>(p, s);
-  }
+  if (tiles(256) >= 224) launch_product_tile<OTYPE, 256, 256, 2, 2>(p, s);
+  else if (tiles(128) >= 160) launch_product_tile<OTYPE, 128, 128, 2, 2>(p, s);
+  else launch_product_tile<OTYPE, 64, 64, 2, 2>(p, s);
 }
 
 template <int DTYPE, int QTYPE>
@@ -990,16 +1022,21 @@ void run_product(const Product& o, hipStream_t s) {
   }
   p.K = (int)ld;                                      // where that is more than K, both are copies, padded with zeros
   p.products = d->dtype == LSAM_DTYPE_BF16 ? 1 : 6;
-  p.Y = o.Y; p.ldy = o.y_stride; p.bias = o.bias; p.u = o.u; p.scale = o.scale;
-  p.Q = o.Q; p.q_adapter = o.q_adapter; p.q_n = o.q_n; p.q_r = o.q_r; p.rank = d->rank; p.g = o.g;
-  // Pieces of u and of the adapter, enough for the result's type: what is left out is 2^-16 of a product before it is rounded to
-  // bfloat16, 2^-24 otherwise.
-  const bool whole = d->dtype == LSAM_DTYPE_FP32, fine = d->adapter_dtype == LSAM_DTYPE_FP32;
-  if (whole && fine) { p.pairs = 6; p.pair_u = kSixLeft; p.pair_q = kSixRight; }
-  else if (whole) { p.pairs = 3; p.pair_u = 0x012u; p.pair_q = 0x000u; }
-  else if (fine) { p.pairs = 3; p.pair_u = 0x001u; p.pair_q = 0x010u; }
-  else { p.pairs = 2; p.pair_u = 0x01u; p.pair_q = 0x00u; }
-  launch_product_any(p, d->dtype, d->adapter_dtype, s);
+  p.Y = o.Y; p.ldy = o.y_stride; p.bias = o.bias; p.g = o.g;
+  const LowRank low = low_rank(d);
+  p.low_k = low.k();
+  p.u = reinterpret_cast<const unsigned short*>(o.ws + o.l.u);          // written by shrink_kernel
+  unsigned short* const q = reinterpret_cast<unsigned short*>(o.ws + o.l.q);
+  unsigned char* const odd = reinterpret_cast<unsigned char*>(o.ws + o.l.odd);
+  p.Q = q; p.odd = odd;
+  if (o.g.n > 0) {
+    const CopiesParams c{o.Q, o.q_adapter, o.q_n, o.q_r, q, odd, d->adapters, o.N, p.low_k, low};
+    const unsigned grid = (unsigned)(((int64_t)d->adapters * o.N + 255) / 256);
+    if (d->adapter_dtype == LSAM_DTYPE_BF16) copies_kernel<LSAM_DTYPE_BF16><<<grid, 256, 0, s>>>(c);
+    else copies_kernel<LSAM_DTYPE_FP32><<<grid, 256, 0, s>>>(c);
+  }
+  if (d->dtype == LSAM_DTYPE_BF16) launch_product<LSAM_DTYPE_BF16>(p, s);
+  else launch_product<LSAM_DTYPE_FP32>(p, s);
 }
 
 Segments segments(const lsam_adapter_desc* d, const int32_t* begin, const int32_t* which) {
@@ -1048,8 +1085,10 @@ extern "C" int lsam_adapter(const lsam_adapter_desc* d, const void* x, const voi
   if (rc != LSAM_OK) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const Segments g = segments(d, seg_begin, seg_adapter);
-  launch_shrink_any(ShrinkParams{x, d->x_stride, A, d->a_adapter, d->a_stride, 1, u, d->rows, d->in, d->rank, 1.f, g}, d->dtype,
-                    d->adapter_dtype, s);
+  const LowRank low = low_rank(d);
+  unsigned short* const copy = l.tiles ? reinterpret_cast<unsigned short*>(static_cast<char*>(workspace) + l.u) : nullptr;
+  launch_shrink_any(ShrinkParams{x, d->x_stride, A, d->a_adapter, d->a_stride, 1, u, d->rows, d->in, d->rank, 1.f, copy, d->scale, low,
+                                 low.k(), g}, d->dtype, d->adapter_dtype, s);
   run_product(Product{d, x, d->x_stride, d->in, W, false, d->out, y, d->y_stride, bias, u, d->scale, B, d->b_adapter, d->b_stride, 1,
                       static_cast<char*>(workspace), l, g}, s);
   return launched();
@@ -1085,10 +1124,12 @@ extern "C" int lsam_adapter_backward(const lsam_adapter_desc* d, const void* x, 
   if (rc != LSAM_OK) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const Segments g = segments(d, seg_begin, seg_adapter);
-  float* const du = reinterpret_cast<float*>(static_cast<char*>(workspace) + l.u);
+  const LowRank low = low_rank(d);
+  float* const du = reinterpret_cast<float*>(static_cast<char*>(workspace) + l.du);
+  unsigned short* const copy = dx ? reinterpret_cast<unsigned short*>(static_cast<char*>(workspace) + l.u) : nullptr;
   if (d->rows > 0)
-    launch_shrink_any(ShrinkParams{dy, d->dy_stride, B, d->b_adapter, 1, d->b_stride, du, d->rows, d->out, d->rank, d->scale, g}, d->dtype,
-                      d->adapter_dtype, s);
+    launch_shrink_any(ShrinkParams{dy, d->dy_stride, B, d->b_adapter, 1, d->b_stride, du, d->rows, d->out, d->rank, d->scale, copy, 1.f, low,
+                                   low.k(), g}, d->dtype, d->adapter_dtype, s);
   if (dx && d->rows > 0)
     run_product(Product{d, dy, d->dy_stride, d->out, W, true, d->in, dx, d->dx_stride, nullptr, du, 1.f, A, d->a_adapter, 1, d->a_stride,
                         static_cast<char*>(workspace), l, g}, s);
