@@ -32,25 +32,35 @@ __device__ __forceinline__ int64_t seg_row(const Segments& g, int s, int64_t row
   const int64_t b = g.begin[s];
   return b < 0 ? 0 : b > rows ? rows : b;
 }
-// The last segment that begins at or before `row`, or -1.
+// The last segment that begins at or before `row`, or -1; the same row in all lanes.  The last 64 candidates are looked at
+// together: one load to wait for instead of six.
 __device__ __forceinline__ int seg_at(const Segments& g, int64_t row) {
   int lo = 0, hi = g.n;
-  while (lo < hi) {
+  while (hi - lo > 64) {
     const int mid = (lo + hi) >> 1;
     if (g.begin[mid] <= row) lo = mid + 1; else hi = mid;
   }
-  return lo - 1;
+  const int i = lo + (int)(threadIdx.x & 63);
+  return lo + __popcll(__ballot(i < hi && g.begin[i < hi ? i : 0] <= row)) - 1;
 }
 __device__ __forceinline__ int seg_adapter(const Segments& g, int s) {
   const int a = g.which[s];
   return a >= 0 && a < g.adapters ? a : -1;
 }
-__device__ __forceinline__ int row_adapter(const Segments& g, int64_t row, int64_t rows) {
-  const int s = seg_at(g, row);
-  return s >= 0 && row < seg_row(g, s + 1, rows) ? seg_adapter(g, s) : -1;
+// The adapter of a row, another row in every lane; `begin` may be a copy of the segments'.
+__device__ __forceinline__ int row_adapter(const Segments& g, const int* begin, int64_t row, int64_t rows) {
+  int lo = 0, hi = g.n;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (begin[mid] <= row) lo = mid + 1; else hi = mid;
+  }
+  const int64_t end = lo > 0 ? begin[lo] : 0;
+  return lo > 0 && row < (end > rows ? rows : end) ? seg_adapter(g, lo - 1) : -1;
 }
 
 template <int N> struct Count { static constexpr int value = N; };
+// What is written above stays above: a run of loads goes out before the first of them is waited for.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
 
 // ---- operands of the matrix units -------------------------------------------------------------------
 // Eight numbers as NP words of eight bfloat16 pieces.
@@ -160,10 +170,11 @@ struct ShrinkParams {
   int64_t rows; int K, rank;
   float scale;
   unsigned short* copy; float copy_scale; LowRank low; int low_k;      // pieces of copy_scale u for product_kernel, or null
+  int* adapter;                                       // receives the adapter of every row, or null
   Segments g;
 };
 
-// Workgroup (tile, j): the j-th, j + gridDim.y-th, ... segment of the tile's 16 RT rows.  The wavefronts take 32 numbers of the
+// Workgroup (tile, j): the j-th, j + gridDim.y-th, ... segment of the tile's 16 RT rows.  The wavefronts take 64 numbers of the
 // contraction in turn.  Bound by reading x where segments are long, by reading A where each row has its own.
 // UNIT: the contraction is contiguous in A.
 template <int DTYPE, int ATYPE, bool UNIT, int NR, int RT>
@@ -178,9 +189,12 @@ __global__ __launch_bounds__(kShrinkWaves * 64) void shrink_kernel(ShrinkParams 
   const int64_t row0 = (int64_t)blockIdx.x * ROWS, row1 = row0 + ROWS < p.rows ? row0 + ROWS : p.rows;
   if (blockIdx.y == 0) {
     // rows without an adapter
-    for (int i = tid; i < ROWS * p.rank; i += kShrinkWaves * 64) {
-      const int64_t row = row0 + i / p.rank;
-      if (row < row1 && row_adapter(p.g, row, p.rows) < 0) p.u[row * p.rank + i % p.rank] = 0.f;
+    for (int i = tid; i < ROWS; i += kShrinkWaves * 64) {
+      if (row0 + i >= row1) break;
+      const int a = row_adapter(p.g, p.g.begin, row0 + i, p.rows);
+      if (p.adapter) p.adapter[row0 + i] = a;
+      if (a < 0)
+        for (int r = 0; r < p.rank; ++r) p.u[(row0 + i) * p.rank + r] = 0.f;
     }
   }
   const int found = seg_at(p.g, row0);
@@ -197,53 +211,68 @@ __global__ __launch_bounds__(kShrinkWaves * 64) void shrink_kernel(ShrinkParams 
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       const int64_t row = lo + t * 16 + l16 < hi ? lo + t * 16 + l16 : hi - 1;
-      x[t] = static_cast<const T*>(p.x) + row * p.x_stride + quarter * 8;
+      x[t] = static_cast<const T*>(p.x) + row * p.x_stride;
     }
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
       const int rr = r * 16 + l16 < p.rank ? r * 16 + l16 : p.rank - 1;
-      A[r] = static_cast<const TA*>(p.A) + a * p.a_adapter + rr * p.a_rank + quarter * 8 * p.a_k;
+      A[r] = static_cast<const TA*>(p.A) + a * p.a_adapter + rr * p.a_rank;
     }
     f32x4 acc[RT][NR];
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
       for (int r = 0; r < NR; ++r) acc[t][r] = f32x4{0.f, 0.f, 0.f, 0.f};
-    int k = wave * 32;
-    constexpr int STEP = kShrinkWaves * 32;
+    // A step is 64 numbers of every row, 16 of them for each quarter of the lanes: two loads that share a line of 128 bytes.
+    int k = wave * 64;
+    constexpr int STEP = kShrinkWaves * 64;
+    const int k_lane = quarter * 16;
     auto steps = [&](auto count) {
       constexpr int N = decltype(count)::value;
-      Pieces<kPieces<ATYPE>> fa[N][NR];
-      Pieces<kPieces<DTYPE>> fx[N][RT];
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-#pragma unroll
-        for (int t = 0; t < RT; ++t) load8<DTYPE, true>(x[t] + k + i * STEP, 1, fx[i][t]);
-#pragma unroll
-        for (int r = 0; r < NR; ++r) load8<ATYPE, UNIT>(A[r] + (k + i * STEP) * p.a_k, p.a_k, fa[i][r]);
-      }
+      Pieces<kPieces<ATYPE>> fa[N][2][NR];
+      Pieces<kPieces<DTYPE>> fx[N][2][RT];
 #pragma unroll
       for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int t = 0; t < RT; ++t)
+        for (int j = 0; j < 2; ++j) {
+          const int at = k + k_lane + i * STEP + j * 8;
 #pragma unroll
-          for (int r = 0; r < NR; ++r) acc[t][r] = multiply(fa[i][r], fx[i][t], acc[t][r]);
+          for (int t = 0; t < RT; ++t) load8<DTYPE, true>(x[t] + at, 1, fx[i][j][t]);
+#pragma unroll
+          for (int r = 0; r < NR; ++r) load8<ATYPE, UNIT>(A[r] + at * p.a_k, p.a_k, fa[i][j][r]);
+        }
+      in_order();
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int r = 0; r < NR; ++r) acc[t][r] = multiply(fa[i][j][r], fx[i][j][t], acc[t][r]);
       k += N * STEP;
     };
-    constexpr int AHEAD = RT == 1 ? 4 : 2;             // steps whose loads are in flight together
-    while (k + (AHEAD - 1) * STEP + 32 <= p.K) steps(Count<AHEAD>{});
-    while (k + 32 <= p.K) steps(Count<1>{});
+    // steps whose loads are in flight together, as registers allow
+    constexpr int REGS = (RT * kPieces<DTYPE> + NR * kPieces<ATYPE>) * 8;
+    constexpr int AHEAD = REGS * 8 <= 128 ? 8 : REGS * 4 <= 128 ? 4 : REGS * 2 <= 128 ? 2 : 1;
+    while (k + (AHEAD - 1) * STEP + 64 <= p.K) steps(Count<AHEAD>{});
+    if constexpr (AHEAD > 2)
+      while (k + STEP + 64 <= p.K) steps(Count<2>{});
+    while (k + 64 <= p.K) steps(Count<1>{});
     if (k < p.K) {
-      const int n = p.K - k - quarter * 8;
-      Pieces<kPieces<ATYPE>> fa[NR];
 #pragma unroll
-      for (int r = 0; r < NR; ++r) load8_some<ATYPE>(A[r] + k * p.a_k, p.a_k, n, fa[r]);
+      for (int j = 0; j < 2; ++j) {
+        const int at = k + k_lane + j * 8, n = p.K - at;
+        Pieces<kPieces<ATYPE>> fa[NR];
 #pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        Pieces<kPieces<DTYPE>> fx;
-        load8_some<DTYPE>(x[t] + k, 1, n, fx);
+        for (int r = 0; r < NR; ++r) load8_some<ATYPE>(A[r] + at * p.a_k, p.a_k, n, fa[r]);
 #pragma unroll
-        for (int r = 0; r < NR; ++r) acc[t][r] = multiply(fa[r], fx, acc[t][r]);
+        for (int t = 0; t < RT; ++t) {
+          Pieces<kPieces<DTYPE>> fx;
+          load8_some<DTYPE>(x[t] + at, 1, n, fx);
+#pragma unroll
+          for (int r = 0; r < NR; ++r) acc[t][r] = multiply(fa[r], fx, acc[t][r]);
+        }
       }
     }
     // lane: row l16 of a tile, ranks 4 quarter .. + 3
@@ -296,14 +325,19 @@ __global__ __launch_bounds__(256) void copies_kernel(CopiesParams p) {
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      v[e] = r0 + e < p.low.rank ? Value<QTYPE>::get(q + (r0 + e) * p.q_r) : 0.f;
+      const int r = r0 + e < p.low.rank ? r0 + e : p.low.rank - 1;
+      v[e] = Value<QTYPE>::get(q + r * p.q_r);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (r0 + e >= p.low.rank) v[e] = 0.f;
       if (!(__builtin_fabsf(v[e]) < __builtin_inff())) { v[e] = 0.f; odd = true; }
     }
+    Pieces<3> o;
+    split8(v, o);
     for (int i = 0; i < p.low.pairs; ++i) {
-      u16x8 o;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = piece(v[e], (p.low.right >> (4 * i)) & 15u);
-      *reinterpret_cast<u16x8*>(p.copy + at * p.low_k + i * p.low.padded + r0) = o;
+      const unsigned w = (p.low.right >> (4 * i)) & 15u;
+      *reinterpret_cast<bf16x8*>(p.copy + at * p.low_k + i * p.low.padded + r0) = w == 0 ? o.p[0] : w == 1 ? o.p[1] : o.p[2];
     }
   }
   p.odd[at] = odd;
@@ -335,17 +369,19 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* base, un
   return __builtin_amdgcn_make_buffer_rsrc(ptr, 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
 }
 
-// Waits for the wavefront's own loads, those to LDS among them, and then for the workgroup.
+// Waits until at most LEFT of the wavefront's own loads, those to LDS among them, are on their way, and then for the workgroup.
+template <int LEFT>
 __device__ __forceinline__ void arrived() {
-  __builtin_amdgcn_s_waitcnt(waitcnt(0, 0));
+  __builtin_amdgcn_s_waitcnt(waitcnt(LEFT, 0));
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
 
-// One operand's tile of R rows by kBK numbers in LDS: row r is 128 bytes = 8 units of 16, unit q at position q ^ (r % 8), so
-// that neighbouring rows' units lie in different banks.  Global memory goes to LDS directly, eight whole rows an instruction;
-// the lane order of that copy is fixed, so a lane asks for the unit that belongs at its position.
+// One operand's tile of R rows by kBK numbers in LDS: row r is 128 bytes = 8 units of 16, unit q at position q ^ (r / 2 % 8): the
+// sixteen lanes whose fragments LDS serves together (0-3, 12-15, 20-23, 24-27 and so on) then read from different banks (no
+// conflict counted).  Global memory goes to LDS directly, eight whole rows an instruction; the lane order of that copy is fixed,
+// so a lane asks for the unit that belongs at its position.
 template <int R, int NW>
 struct RowTile {
   static constexpr int BYTES = R * kBK * 2;
@@ -355,7 +391,7 @@ struct RowTile {
   __device__ __forceinline__ void init(int64_t ld, int lane, int wave) {
 #pragma unroll
     for (int j = 0; j < NLOAD; ++j) {
-      const int row = (wave * NLOAD + j) * 8 + (lane >> 3), unit = (lane & 7) ^ (row & 7);
+      const int row = (wave * NLOAD + j) * 8 + (lane >> 3), unit = (lane & 7) ^ ((row >> 1) & 7);
       k[j] = unit * 8;
       goff[j] = (unsigned)(row * ld * 2) + (unsigned)unit * 16u;
     }
@@ -376,24 +412,44 @@ __device__ __forceinline__ void issue_rows(const unsigned short* base, int ld, i
   constexpr int NLOAD = R / 8 / NW;
 #pragma unroll
   for (int j = 0; j < NLOAD; ++j) {
-    const int row = (wave * NLOAD + j) * 8 + (lane >> 3), k = k0 + ((lane & 7) ^ (row & 7)) * 8;
+    const int row = (wave * NLOAD + j) * 8 + (lane >> 3), k = k0 + ((lane & 7) ^ ((row >> 1) & 7)) * 8;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(tile + (wave * NLOAD + j) * 1024), 16,
                                              row >= lo && row < hi && k < ld ? (unsigned)(row * ld + k) * 2u : 0x7FFFFFF0u, 0, 0, 0);
   }
 }
 // The 16 bytes that a lane feeds to the matrix unit: row `row`, numbers 16 kc + 8 half ..
 __device__ __forceinline__ u32x4 fragment(const lds_byte* tile, int row, int kc, int half) {
-  return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(tile + row * 128 + (((kc * 2 + half) ^ (row & 7)) << 4));
+  return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(tile + row * 128 + (((kc * 2 + half) ^ ((row >> 1) & 7)) << 4));
 }
+// Lays N instructions of the kinds in MASK (0x100 LDS reads, 0x20 loads) evenly among M of the matrix unit, instead of the
+// compiler's order, which reads fragments just before they are multiplied and waits for them.
+template <int MASK, int N, int M, int I = 0>
+__device__ __forceinline__ void interleave() {
+  constexpr int now = N * (I + 1) / M - N * I / M;
+  if constexpr (now > 0) __builtin_amdgcn_sched_group_barrier(MASK, now, 0);
+  __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+  if constexpr (I + 1 < M) interleave<MASK, N, M, I + 1>();
+}
+
 // BM x BN outputs by WM x WN wavefronts, each a block of 32 x 32 results TM x TN times.
-template <int OTYPE, int BM, int BN, int WM, int WN>
+// S steps of the operands are in LDS: one is multiplied, the others are on their way.
+template <int OTYPE, int BM, int BN, int WM, int WN, int S>
 __device__ __forceinline__ void product_tile(const ProductParams& p) {
   constexpr int NW = WM * WN;
   constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
   typedef RowTile<BM, NW> OX;
   typedef RowTile<BN, NW> OW;
-  __shared__ __attribute__((aligned(1024))) unsigned char st0[OX::BYTES + OW::BYTES];
-  __shared__ __attribute__((aligned(1024))) unsigned char st1[OX::BYTES + OW::BYTES];
+  // an array each, so that the compiler knows the stage that is read from those that are on their way
+  static_assert(S == 2 || S == 4 || S == 8, "stages");
+  constexpr int STAGE = OX::BYTES + OW::BYTES, NL = OX::NLOAD + OW::NLOAD;
+  __shared__ __attribute__((aligned(1024))) unsigned char st0[STAGE];
+  __shared__ __attribute__((aligned(1024))) unsigned char st1[STAGE];
+  __shared__ __attribute__((aligned(1024))) unsigned char st2[S > 2 ? STAGE : 16];
+  __shared__ __attribute__((aligned(1024))) unsigned char st3[S > 2 ? STAGE : 16];
+  __shared__ __attribute__((aligned(1024))) unsigned char st4[S > 4 ? STAGE : 16];
+  __shared__ __attribute__((aligned(1024))) unsigned char st5[S > 4 ? STAGE : 16];
+  __shared__ __attribute__((aligned(1024))) unsigned char st6[S > 4 ? STAGE : 16];
+  __shared__ __attribute__((aligned(1024))) unsigned char st7[S > 4 ? STAGE : 16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, half = lane >> 5;
   const int wm = (wave / WN) * (TM * 32), wn = (wave % WN) * (TN * 32);
@@ -417,8 +473,8 @@ __device__ __forceinline__ void product_tile(const ProductParams& p) {
   const unsigned bytes_x = (unsigned)(((m_here - 1) * p.ldx + p.K) * 2), bytes_w = (unsigned)(((n_here - 1) * p.ldw + p.K) * 2);
   const unsigned short* X = p.X + m0 * p.ldx;
   const unsigned short* W = p.W + (int64_t)n0 * p.ldw;
-  lds_byte* const a0 = (lds_byte*)st0;
-  lds_byte* const a1 = (lds_byte*)st1;
+  lds_byte *const a0 = (lds_byte*)st0, *const a1 = (lds_byte*)st1, *const a2 = (lds_byte*)st2, *const a3 = (lds_byte*)st3;
+  lds_byte *const a4 = (lds_byte*)st4, *const a5 = (lds_byte*)st5, *const a6 = (lds_byte*)st6, *const a7 = (lds_byte*)st7;
 
   f32x16 acc[TM][TN];
 #pragma unroll
@@ -442,8 +498,9 @@ __device__ __forceinline__ void product_tile(const ProductParams& p) {
       for (int j = 0; j < TN; ++j) acc[i][j] = mfma32(fw[buf][j], fx[buf][i], acc[i][j]);
   };
 
-  // Steps: the products of planes one after the other, each over all of K.  A step is requested while the one before it is
-  // multiplied; behind the last one zeros are, which add nothing, so that the loop has no exit between its two halves.
+  // Steps: the products of planes one after the other, each over all of K.  S - 1 steps are on their way while one is
+  // multiplied; behind the last one zeros are, which add nothing, so that the loop runs in whole rounds of the stages and the
+  // loads to wait for are as many in every step.
   const int steps = p.products * ((p.K + kBK - 1) / kBK);
   int next_k = 0, next_q = 0;
   auto request = [&](lds_byte* tile) {
@@ -458,26 +515,46 @@ __device__ __forceinline__ void product_tile(const ProductParams& p) {
   };
   request(a0);
   request(a1);
-  arrived();
+  if constexpr (S > 2) { request(a2); request(a3); }
+  if constexpr (S > 4) { request(a4); request(a5); request(a6); request(a7); }
+  arrived<(S - 1) * NL>();
   read(a0, 0, 0);
   auto step = [&](lds_byte* now, lds_byte* then) {
     read(now, 1, 1);
     multiply_chunk(0);
+    interleave<0x100, TM + TN, TM * TN>();
     read(now, 2, 0);
     multiply_chunk(1);
+    interleave<0x100, TM + TN, TM * TN>();
     read(now, 3, 1);
     multiply_chunk(0);
-    // Every wavefront has taken its last fragment of this step, and the next one, requested a step ago, has arrived.
-    arrived();
+    interleave<0x100, TM + TN, TM * TN>();
+    // Every wavefront has taken its last fragment of this step, and the next one has arrived.
+    arrived<(S - 2) * NL>();
     request(now);
     read(then, 0, 0);                    // behind the last step: never multiplied
     multiply_chunk(1);
+    interleave<0x120, TM + TN + NL, TM * TN>();
   };
-  for (int s = 0; s < steps; s += 2) {
+  for (int s = 0; s < steps; s += S) {
     step(a0, a1);
-    step(a1, a0);
+    if constexpr (S == 2) {
+      step(a1, a0);
+    } else {
+      step(a1, a2);
+      step(a2, a3);
+      if constexpr (S == 4) {
+        step(a3, a0);
+      } else {
+        step(a3, a4);
+        step(a4, a5);
+        step(a5, a6);
+        step(a6, a7);
+        step(a7, a0);
+      }
+    }
   }
-  arrived();                             // nothing may still be on its way to LDS
+  arrived<0>();                          // nothing may still be on its way to LDS
 
   // Every segment that rows of the tile belong to: the copies of u and of its adapter, rows of other segments being zeros.
   const int found = seg_at(p.g, m0);
@@ -487,18 +564,29 @@ __device__ __forceinline__ void product_tile(const ProductParams& p) {
     if (l >= m_here) break;
     const int lo = (int)(l > 0 ? l : 0), hi = (int)(h < m_here ? h : m_here), a = seg_adapter(p.g, s);
     if (a < 0 || lo >= hi) continue;
-    for (int k0 = 0; k0 < p.low_k; k0 += kBK) {
-      issue_rows<BM, NW>(p.u + m0 * p.low_k, p.low_k, (int)m_here, lo, hi, a0, k0, lane, wave);
-      issue_rows<BN, NW>(p.Q + ((int64_t)a * p.N + n0) * p.low_k, p.low_k, n_here, 0, n_here, a0 + OX::BYTES, k0, lane, wave);
-      arrived();
+    const unsigned short* const u = p.u + m0 * p.low_k;
+    const unsigned short* const q = p.Q + ((int64_t)a * p.N + n0) * p.low_k;
+    auto request_low = [&](lds_byte* tile, int k0) {
+      if (k0 >= p.low_k) return;
+      issue_rows<BM, NW>(u, p.low_k, (int)m_here, lo, hi, tile, k0, lane, wave);
+      issue_rows<BN, NW>(q, p.low_k, n_here, 0, n_here, tile + OX::BYTES, k0, lane, wave);
+    };
+    auto multiply_low = [&](const lds_byte* tile, int k0) {
 #pragma unroll
       for (int kc = 0; kc < 4; ++kc) {
         if (k0 + kc * 16 < p.low_k) {
-          read(a0, kc, 0);
+          read(tile, kc, 0);
           multiply_chunk(0);
         }
       }
-      arrived();
+    };
+    for (int k0 = 0; k0 < p.low_k; k0 += 2 * kBK) {
+      request_low(a0, k0);
+      request_low(a1, k0 + kBK);
+      arrived<0>();
+      multiply_low(a0, k0);
+      multiply_low(a1, k0 + kBK);
+      arrived<0>();
     }
   }
 
@@ -554,9 +642,9 @@ __device__ __forceinline__ void product_tile(const ProductParams& p) {
   }
 }
 
-template <int OTYPE, int BM, int BN, int WM, int WN>
+template <int OTYPE, int BM, int BN, int WM, int WN, int S>
 __global__ __launch_bounds__(WM * WN * 64) void product_kernel(ProductParams p) {
-  product_tile<OTYPE, BM, BN, WM, WN>(p);
+  product_tile<OTYPE, BM, BN, WM, WN, S>(p);
 }
 
 // ---- y or dx, at most 64 rows -----------------------------------------------------------------------
@@ -569,10 +657,11 @@ struct FewRowsParams {
   const float* u; float scale;
   const void* Q; int64_t q_adapter, q_n, q_r;
   int rank;
-  Segments g;
+  const int* adapter;                                 // of every row
 };
 constexpr int kFewRows = 64;
 constexpr int kFewWaves = 8;
+constexpr int kHead = 16;                             // ranks that are read ahead
 
 // A workgroup's 16 outputs: eight wavefronts go along the rows of W 512 bytes (bf16) at a time, so that W streams from
 // memory once; x comes from L2.  Bound by reading W.
@@ -581,47 +670,76 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_rows_kernel(FewRowsParams 
   typedef typename Value<DTYPE>::T T;
   typedef typename Value<QTYPE>::T TQ;
   __shared__ float part[kFewWaves][RT * 16][17];
-  __shared__ int adapter[RT * 16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, quarter = lane >> 4;
   const int n0 = blockIdx.x * 16;
-  const T* w = static_cast<const T*>(p.W) + (int64_t)(n0 + l16 < p.N ? n0 + l16 : p.N - 1) * p.ldw + quarter * 8;
+  // This lane's outputs, rows row0 + 32 o of column `col`, and what their low-rank part needs: asked for before W is.
+  constexpr int OUT = RT > 1 ? RT / 2 : 1;
+  const int row0 = tid >> 4, col = n0 + (tid & 15);
+  int adapter[OUT];
+  float u[OUT][kHead], q[OUT][kHead];
+#pragma unroll
+  for (int o = 0; o < OUT; ++o) adapter[o] = row0 + o * 32 < p.M ? p.adapter[row0 + o * 32] : -1;
+#pragma unroll
+  for (int o = 0; o < OUT; ++o)
+#pragma unroll
+    for (int e = 0; e < kHead; ++e) {
+      const int r = e < p.rank ? e : p.rank - 1;
+      u[o][e] = adapter[o] >= 0 && col < p.N ? p.u[(int64_t)(row0 + o * 32) * p.rank + r] : 0.f;
+      q[o][e] = adapter[o] >= 0 && col < p.N
+                    ? Value<QTYPE>::get(static_cast<const TQ*>(p.Q) + adapter[o] * p.q_adapter + col * p.q_n + r * p.q_r) : 0.f;
+    }
+  in_order();
+  const T* w = static_cast<const T*>(p.W) + (int64_t)(n0 + l16 < p.N ? n0 + l16 : p.N - 1) * p.ldw;
   const T* x[RT];
 #pragma unroll
-  for (int t = 0; t < RT; ++t)
-    x[t] = static_cast<const T*>(p.X) + (int64_t)(t * 16 + l16 < p.M ? t * 16 + l16 : p.M - 1) * p.ldx + quarter * 8;
-  if (tid < RT * 16) adapter[tid] = tid < p.M ? row_adapter(p.g, tid, p.M) : -1;
+  for (int t = 0; t < RT; ++t) x[t] = static_cast<const T*>(p.X) + (int64_t)(t * 16 + l16 < p.M ? t * 16 + l16 : p.M - 1) * p.ldx;
   f32x4 acc[RT];
 #pragma unroll
   for (int t = 0; t < RT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  int k = wave * 32;
-  constexpr int STEP = kFewWaves * 32;
+  // A step is 64 numbers of every row, 16 of them for each quarter of the lanes: two loads that share a line of 128 bytes.
+  int k = wave * 64;
+  constexpr int STEP = kFewWaves * 64;
+  const int k_lane = quarter * 16;
   auto steps = [&](auto count) {
     constexpr int N = decltype(count)::value;
-    Pieces<kPieces<DTYPE>> fw[N], fx[N][RT];
-#pragma unroll
-    for (int i = 0; i < N; ++i) load8<DTYPE, true>(w + k + i * STEP, 1, fw[i]);
+    Pieces<kPieces<DTYPE>> fw[N][2], fx[N][2][RT];
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
-      for (int t = 0; t < RT; ++t) load8<DTYPE, true>(x[t] + k + i * STEP, 1, fx[i][t]);
+      for (int j = 0; j < 2; ++j) load8<DTYPE, true>(w + k + k_lane + i * STEP + j * 8, 1, fw[i][j]);
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
-      for (int t = 0; t < RT; ++t) acc[t] = multiply(fw[i], fx[i][t], acc[t]);
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) load8<DTYPE, true>(x[t] + k + k_lane + i * STEP + j * 8, 1, fx[i][j][t]);
+    in_order();
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) acc[t] = multiply(fw[i][j], fx[i][j][t], acc[t]);
     k += N * STEP;
   };
-  constexpr int AHEAD = RT == 1 ? 8 : RT == 2 ? 4 : 2;
-  while (k + (AHEAD - 1) * STEP + 32 <= p.K) steps(Count<AHEAD>{});
-  while (k + 32 <= p.K) steps(Count<1>{});
+  // steps whose loads are in flight together, as registers allow
+  constexpr int AHEAD = DTYPE == LSAM_DTYPE_BF16 ? 8 / RT : RT == 1 ? 2 : 1;
+  while (k + (AHEAD - 1) * STEP + 64 <= p.K) steps(Count<AHEAD>{});
+  if constexpr (AHEAD > 2)
+    while (k + STEP + 64 <= p.K) steps(Count<2>{});
+  while (k + 64 <= p.K) steps(Count<1>{});
   if (k < p.K) {
-    const int n = p.K - k - quarter * 8;
-    Pieces<kPieces<DTYPE>> fw, fx;
-    load8_some<DTYPE>(w + k, 1, n, fw);
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      load8_some<DTYPE>(x[t] + k, 1, n, fx);
-      acc[t] = multiply(fw, fx, acc[t]);
+    for (int j = 0; j < 2; ++j) {
+      const int at = k + k_lane + j * 8, n = p.K - at;
+      Pieces<kPieces<DTYPE>> fw, fx;
+      load8_some<DTYPE>(w + at, 1, n, fw);
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        load8_some<DTYPE>(x[t] + at, 1, n, fx);
+        acc[t] = multiply(fw, fx, acc[t]);
+      }
     }
   }
 #pragma unroll
@@ -629,18 +747,20 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_rows_kernel(FewRowsParams 
 #pragma unroll
     for (int i = 0; i < 4; ++i) part[wave][t * 16 + l16][quarter * 4 + i] = acc[t][i];
   __syncthreads();
-  for (int i = tid; i < RT * 256; i += kFewWaves * 64) {
-    const int row = i >> 4, col = n0 + (i & 15);
-    if (row >= p.M || col >= p.N) continue;
+#pragma unroll
+  for (int o = 0; o < OUT; ++o) {
+    const int row = row0 + o * 32;
+    if (row >= p.M || row >= RT * 16 || col >= p.N) continue;
     float sum = 0.f;
 #pragma unroll
-    for (int v = 0; v < kFewWaves; ++v) sum += part[v][row][i & 15];
-    const int a = adapter[row];
-    if (a >= 0) {
-      const TQ* q = static_cast<const TQ*>(p.Q) + a * p.q_adapter + col * p.q_n;
-      const float* u = p.u + (int64_t)row * p.rank;
+    for (int v = 0; v < kFewWaves; ++v) sum += part[v][row][tid & 15];
+    if (adapter[o] >= 0) {
       float low = 0.f;
-      for (int r = 0; r < p.rank; ++r) low = __builtin_fmaf(u[r], Value<QTYPE>::get(q + r * p.q_r), low);
+#pragma unroll
+      for (int e = 0; e < kHead; ++e)
+        if (e < p.rank) low = __builtin_fmaf(u[o][e], q[o][e], low);
+      const TQ* const more = static_cast<const TQ*>(p.Q) + adapter[o] * p.q_adapter + col * p.q_n;
+      for (int r = kHead; r < p.rank; ++r) low = __builtin_fmaf(p.u[(int64_t)row * p.rank + r], Value<QTYPE>::get(more + r * p.q_r), low);
       sum = __builtin_fmaf(p.scale, low, sum);
     }
     if (p.bias) sum += p.bias[col];
@@ -778,15 +898,29 @@ __global__ __launch_bounds__(256) void planes_kernel(PlanesParams p) {
 #pragma unroll
     for (int q = 0; q < NP; ++q) *reinterpret_cast<bf16x8*>(p.dst + q * p.plane + row * p.ld + c) = o.p[q];
   } else {
-    __shared__ T tile[64][65];
+    __shared__ T tile[64][66];
     const unsigned across = (unsigned)((p.cols + 63) / 64);
     const int64_t r0 = (int64_t)(blockIdx.x / across) * 64;
     const int c0 = (int)(blockIdx.x % across) * 64;
-    for (int i = tid; i < 64 * 64; i += 256) {
-      const int64_t r = r0 + i / 64;
-      const int c = c0 + i % 64;
-      tile[i / 64][i % 64] = r < p.rows && c < p.cols ? static_cast<const T*>(p.src)[r * p.stride + c] : (T)0;
+    typedef T T8 __attribute__((ext_vector_type(8)));
+    typedef T8 T8_any __attribute__((aligned(sizeof(T))));
+    T8 w[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int64_t r = r0 + j * 32 + tid / 8;
+      const int c = c0 + (tid % 8) * 8;
+      const T* src = static_cast<const T*>(p.src) + r * p.stride + c;
+      if (r < p.rows && c + 8 <= p.cols) {
+        w[j] = *reinterpret_cast<const T8_any*>(src);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[j][e] = r < p.rows && c + e < p.cols ? src[e] : (T)0;
+      }
     }
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) tile[j * 32 + tid / 8][(tid % 8) * 8 + e] = w[j][e];
     __syncthreads();
     for (int i = tid; i < 64 * 8; i += 256) {
       const int c = i / 8, r = (i % 8) * 8;
@@ -834,8 +968,8 @@ LowRank low_rank(const lsam_adapter_desc* d) {
   return l;
 }
 
-// Offsets in the workspace: copies of x or dy and of W, of u and of the adapters, marks, du.
-struct Layout { size_t x, w, u, q, odd, du, total; bool tiles; };
+// Offsets in the workspace: copies of x or dy and of W, of u and of the adapters, marks, adapters of rows, du.
+struct Layout { size_t x, w, u, q, odd, adapter, du, total; bool tiles; };
 Layout layout(const lsam_adapter_desc* d, bool backward) {
   Layout l;
   const int N = backward ? d->in : d->out;
@@ -847,7 +981,8 @@ Layout layout(const lsam_adapter_desc* d, bool backward) {
   const size_t low_k = (size_t)low_rank(d).k();
   l.q = l.u + (l.tiles ? up256((size_t)d->rows * low_k * 2) : 0);
   l.odd = l.q + (l.tiles ? up256((size_t)d->adapters * N * low_k * 2) : 0);
-  l.du = l.odd + (l.tiles ? up256((size_t)d->adapters * N) : 0);
+  l.adapter = l.odd + (l.tiles ? up256((size_t)d->adapters * N) : 0);
+  l.du = l.adapter + (l.tiles ? 0 : up256((size_t)d->rows * 4));
   l.total = l.du + (backward ? up256((size_t)d->rows * d->rank * 4) : 0);
   return l;
 }
@@ -892,14 +1027,16 @@ int check_args(const Arg* args, int n, const char* who) {
 
 template <int DTYPE, int ATYPE, bool UNIT, int NR>
 void launch_shrink_rank(const ShrinkParams& p, hipStream_t s) {
-  // tiles of 16 rows where segments are no longer than that, of 64 otherwise
-  const bool narrow_tiles = p.rows <= 16ll * p.g.n;
-  const int64_t rows = narrow_tiles ? 16 : 64, tiles = (p.rows + rows - 1) / rows;
+  // Tiles of 64 rows read the adapter least often; of 32 or 16 rows where those leave units idle or segments are short.
+  const bool brief = p.rows <= 16ll * p.g.n;
+  const int64_t rows = !brief && p.rows >= 64 * 256 ? 64 : !brief && p.rows >= 32 * 192 ? 32 : 16;
+  const int64_t tiles = (p.rows + rows - 1) / rows;
   int64_t y = p.g.n / tiles + 1;
   y = y > 64 ? 64 : y;
   const dim3 grid((unsigned)tiles, (unsigned)y);
-  if (narrow_tiles) shrink_kernel<DTYPE, ATYPE, UNIT, NR, 1><<<grid, kShrinkWaves * 64, 0, s>>>(p);
-  else shrink_kernel<DTYPE, ATYPE, UNIT, NR, 4><<<grid, kShrinkWaves * 64, 0, s>>>(p);
+  if (rows == 64) shrink_kernel<DTYPE, ATYPE, UNIT, NR, 4><<<grid, kShrinkWaves * 64, 0, s>>>(p);
+  else if (rows == 32) shrink_kernel<DTYPE, ATYPE, UNIT, NR, 2><<<grid, kShrinkWaves * 64, 0, s>>>(p);
+  else shrink_kernel<DTYPE, ATYPE, UNIT, NR, 1><<<grid, kShrinkWaves * 64, 0, s>>>(p);
 }
 template <int DTYPE, int ATYPE>
 void launch_shrink(const ShrinkParams& p, hipStream_t s) {
@@ -942,19 +1079,19 @@ void launch_planes_any(const void* src, int64_t stride, int64_t rows, int cols, 
   else launch_planes<LSAM_DTYPE_FP32>(src, stride, rows, cols, transpose, dst, s);
 }
 
-template <int OTYPE, int BM, int BN, int WM, int WN>
+template <int OTYPE, int BM, int BN, int WM, int WN, int S>
 void launch_product_tile(ProductParams p, hipStream_t s) {
   p.tilesM = (int)((p.M + BM - 1) / BM);
   p.tilesN = (p.N + BN - 1) / BN;
-  product_kernel<OTYPE, BM, BN, WM, WN><<<(unsigned)p.tilesM * (unsigned)p.tilesN, WM * WN * 64, 0, s>>>(p);
+  product_kernel<OTYPE, BM, BN, WM, WN, S><<<(unsigned)p.tilesM * (unsigned)p.tilesN, WM * WN * 64, 0, s>>>(p);
 }
 // Large tiles reuse what they read most; smaller ones where large ones would leave units idle.
 template <int OTYPE>
 void launch_product(const ProductParams& p, hipStream_t s) {
   auto tiles = [&](int64_t b) { return ((p.M + b - 1) / b) * ((p.N + b - 1) / b); };
-  if (tiles(256) >= 224) launch_product_tile<OTYPE, 256, 256, 2, 2>(p, s);
-  else if (tiles(128) >= 160) launch_product_tile<OTYPE, 128, 128, 2, 2>(p, s);
-  else launch_product_tile<OTYPE, 64, 64, 2, 2>(p, s);
+  if (tiles(256) >= 224) launch_product_tile<OTYPE, 256, 256, 2, 2, 2>(p, s);
+  else if (tiles(128) >= 160) launch_product_tile<OTYPE, 128, 128, 2, 2, 4>(p, s);
+  else launch_product_tile<OTYPE, 64, 64, 2, 2, 8>(p, s);
 }
 
 template <int DTYPE, int QTYPE>
@@ -1002,7 +1139,8 @@ void run_product(const Product& o, hipStream_t s) {
     FewRowsParams p;
     p.X = o.X; p.ldx = o.x_stride; p.W = o.W; p.ldw = d->w_stride;
     p.M = (int)d->rows; p.N = o.N; p.K = o.K; p.Y = o.Y; p.ldy = o.y_stride; p.bias = o.bias; p.u = o.u; p.scale = o.scale;
-    p.Q = o.Q; p.q_adapter = o.q_adapter; p.q_n = o.q_n; p.q_r = o.q_r; p.rank = d->rank; p.g = o.g;
+    p.Q = o.Q; p.q_adapter = o.q_adapter; p.q_n = o.q_n; p.q_r = o.q_r; p.rank = d->rank;
+    p.adapter = reinterpret_cast<const int*>(o.ws + o.l.adapter);
     launch_few_rows_any(p, d->dtype, d->adapter_dtype, s);
     return;
   }
@@ -1088,7 +1226,7 @@ extern "C" int lsam_adapter(const lsam_adapter_desc* d, const void* x, const voi
   const LowRank low = low_rank(d);
   unsigned short* const copy = l.tiles ? reinterpret_cast<unsigned short*>(static_cast<char*>(workspace) + l.u) : nullptr;
   launch_shrink_any(ShrinkParams{x, d->x_stride, A, d->a_adapter, d->a_stride, 1, u, d->rows, d->in, d->rank, 1.f, copy, d->scale, low,
-                                 low.k(), g}, d->dtype, d->adapter_dtype, s);
+                                 low.k(), l.tiles ? nullptr : reinterpret_cast<int*>(static_cast<char*>(workspace) + l.adapter), g}, d->dtype, d->adapter_dtype, s);
   run_product(Product{d, x, d->x_stride, d->in, W, false, d->out, y, d->y_stride, bias, u, d->scale, B, d->b_adapter, d->b_stride, 1,
                       static_cast<char*>(workspace), l, g}, s);
   return launched();
@@ -1129,7 +1267,7 @@ extern "C" int lsam_adapter_backward(const lsam_adapter_desc* d, const void* x, 
   unsigned short* const copy = dx ? reinterpret_cast<unsigned short*>(static_cast<char*>(workspace) + l.u) : nullptr;
   if (d->rows > 0)
     launch_shrink_any(ShrinkParams{dy, d->dy_stride, B, d->b_adapter, 1, d->b_stride, du, d->rows, d->out, d->rank, d->scale, copy, 1.f, low,
-                                   low.k(), g}, d->dtype, d->adapter_dtype, s);
+                                   low.k(), nullptr, g}, d->dtype, d->adapter_dtype, s);
   if (dx && d->rows > 0)
     run_product(Product{d, dy, d->dy_stride, d->out, W, true, d->in, dx, d->dx_stride, nullptr, du, 1.f, A, d->a_adapter, 1, d->a_stride,
                         static_cast<char*>(workspace), l, g}, s);
