@@ -160,9 +160,229 @@ struct LowRank {
   int k() const { return pairs * padded; }
 };
 
-// ---- u = x A^T, du = scale dy B ---------------------------------------------------------------------
-constexpr int kShrinkWaves = 8;
+constexpr int waitcnt(int vm, int lgkm) { return (vm & 0xF) | ((vm >> 4) << 14) | (0x7 << 4) | ((lgkm & 0xF) << 8); }
 
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* base, unsigned bytes) {
+  const unsigned long long a = reinterpret_cast<unsigned long long>(base);
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)a);
+  const unsigned hi = __builtin_amdgcn_readfirstlane((unsigned)(a >> 32));
+  void* ptr = reinterpret_cast<void*>(((unsigned long long)hi << 32) | lo);
+  return __builtin_amdgcn_make_buffer_rsrc(ptr, 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+}
+
+// The wavefront's own loads, those to LDS among them: at most LEFT are still on their way.
+template <int LEFT>
+__device__ __forceinline__ void wait_loads() {
+  __builtin_amdgcn_s_waitcnt(waitcnt(LEFT, 15));
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void wait_lds() {
+  __builtin_amdgcn_s_waitcnt(waitcnt(63, 0));
+  asm volatile("" ::: "memory");
+}
+// Waits until at most LEFT of the wavefront's own loads, those to LDS among them, are on their way, and then for the workgroup.
+template <int LEFT>
+__device__ __forceinline__ void arrived() {
+  __builtin_amdgcn_s_waitcnt(waitcnt(LEFT, 0));
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// ---- a few rows of two matrices against each other ---------------------------------------------------
+// Sums acc[x tile][left tile] of 16 x 16 results over all of K, each wavefront for its own steps of 64 numbers (wave, wave + WAVES,
+// ...).  The matrix unit wants neighbouring lanes in different rows, which the address unit takes one line at a time: 64 cycles
+// a load instead of 16, 18 us for 32 rows against 4096 x 4096.  So the rows go to LDS directly, whole lines of 128 bytes in
+// neighbouring lanes, into a ring of S steps that belongs to the wavefront alone.  Rows that are not aligned for that are read
+// straight into the matrix unit's layout.
+//
+// ROWS rows of 64 numbers of a step: bf16 in a line, fp32 in two.  Unit q (16 bytes) of a line of row r is at position
+// q ^ (r / 2 % 8).
+template <int DTYPE, int ROWS>
+struct Lines {
+  static constexpr int EACH = DTYPE == LSAM_DTYPE_BF16 ? 1 : 2;       // lines of a row in a step
+  static constexpr int BYTES = ROWS * 128 * EACH, NLOAD = ROWS / 8 * EACH;
+  static constexpr int B = DTYPE == LSAM_DTYPE_BF16 ? 2 : 4;
+  unsigned goff[ROWS / 8];
+  int k;
+  __device__ __forceinline__ void init(int64_t stride, int lane) {
+#pragma unroll
+    for (int j = 0; j < ROWS / 8; ++j) goff[j] = (unsigned)((j * 8 + (lane >> 3)) * stride * B);
+    k = 0;
+  }
+  // Rows past the resource's end and units past K arrive as zeros.
+  __device__ __forceinline__ void issue(__amdgpu_buffer_rsrc_t rsrc, lds_byte* tile, int k0, int K, int lane) const {
+#pragma unroll
+    for (int l = 0; l < EACH; ++l)
+#pragma unroll
+      for (int j = 0; j < ROWS / 8; ++j) {
+        const int row = j * 8 + (lane >> 3), at = k0 + l * 32 + ((lane & 7) ^ ((row >> 1) & 7)) * (16 / B);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(tile + (l * ROWS / 8 + j) * 1024), 16,
+                                                 at < K ? goff[j] + (unsigned)(at * B) : 0x7FFFFFF0u, 0, 0, 0);
+      }
+  }
+  // Eight numbers of row `row`: 32 kc + 8 quarter ..
+  __device__ __forceinline__ void read(const lds_byte* tile, int row, int kc, int quarter, Pieces<kPieces<DTYPE>>& o) const {
+    typedef const __attribute__((address_space(3))) u32x4* lds_unit;
+    const int turn = (row >> 1) & 7;
+    if constexpr (DTYPE == LSAM_DTYPE_BF16) {
+      o.p[0] = __builtin_bit_cast(bf16x8, *reinterpret_cast<lds_unit>(tile + row * 128 + (((kc * 4 + quarter) ^ turn) << 4)));
+    } else {
+      const lds_byte* line = tile + kc * ROWS * 128 + row * 128;
+      const f32x4 a = __builtin_bit_cast(f32x4, *reinterpret_cast<lds_unit>(line + (((quarter * 2) ^ turn) << 4)));
+      const f32x4 b = __builtin_bit_cast(f32x4, *reinterpret_cast<lds_unit>(line + (((quarter * 2 + 1) ^ turn) << 4)));
+      const float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+      split8(v, o);
+    }
+  }
+};
+
+// The left rows are contiguous along K (UNIT) or along the rows; `some`: how many there are.
+template <int TYPE> struct Rows {
+  const typename Value<TYPE>::T* p;
+  int64_t stride, step;                               // from row to row, along K
+  int some;
+};
+template <int DTYPE>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const Rows<DTYPE>& r, int K) {
+  return make_rsrc(r.p, (unsigned)(((r.some - 1) * r.stride + K) * (DTYPE == LSAM_DTYPE_BF16 ? 2 : 4)));
+}
+
+constexpr int kRing = 3;
+// Bytes of a wavefront's part of a stage.
+template <int LTYPE, int XTYPE, bool UNIT, int NL, int NX>
+constexpr int kStageBytes = Lines<XTYPE, NX * 16>::BYTES + (UNIT ? Lines<LTYPE, NL * 16>::BYTES : 0);
+
+// A wavefront's way along K.
+template <int LTYPE, int XTYPE, bool UNIT, int NL, int NX, int WAVES>
+struct Staged {
+  typedef Lines<XTYPE, NX * 16> LX;
+  typedef Lines<LTYPE, NL * 16> LL;
+  static constexpr int LOADS = LX::NLOAD + (UNIT ? LL::NLOAD : 0);
+  Rows<LTYPE> left;
+  Rows<XTYPE> x;
+  LX lx;
+  LL ll;
+  int K, lane, k, k_next;
+
+  __device__ __forceinline__ void request(lds_byte* stage) {
+    lx.issue(resource(x, K), stage, k_next, K, lane);
+    if constexpr (UNIT) ll.issue(resource(left, K), stage + LX::BYTES, k_next, K, lane);
+    k_next += WAVES * 64;
+  }
+  // Multiplies a stage and asks for the step after next but one in its place.
+  __device__ __forceinline__ void step(lds_byte* stage, f32x4 (&acc)[NX][NL]) {
+    const int l16 = lane & 15, quarter = lane >> 4;
+    Pieces<kPieces<LTYPE>> fl[2][NL];
+    if constexpr (!UNIT) {
+      // not staged: neighbouring lanes are neighbours in memory
+#pragma unroll
+      for (int kc = 0; kc < 2; ++kc)
+#pragma unroll
+        for (int r = 0; r < NL; ++r) {
+          const int at = k + kc * 32 + quarter * 8;
+          const typename Value<LTYPE>::T* p = left.p + (r * 16 + l16 < left.some ? r * 16 + l16 : left.some - 1) * left.stride + at * left.step;
+          if (k + 64 <= K) load8<LTYPE, false>(p, left.step, fl[kc][r]);
+          else load8_some<LTYPE>(p, left.step, K - at, fl[kc][r]);
+        }
+    }
+    wait_loads<(kRing - 1) * LOADS>();
+    Pieces<kPieces<XTYPE>> fx[2][NX];
+#pragma unroll
+    for (int kc = 0; kc < 2; ++kc) {
+#pragma unroll
+      for (int t = 0; t < NX; ++t) lx.read(stage, t * 16 + l16, kc, quarter, fx[kc][t]);
+      if constexpr (UNIT) {
+#pragma unroll
+        for (int r = 0; r < NL; ++r) ll.read(stage + LX::BYTES, r * 16 + l16, kc, quarter, fl[kc][r]);
+      }
+    }
+    wait_lds();                                       // the fragments are here: the stage may be filled again
+    request(stage);
+#pragma unroll
+    for (int kc = 0; kc < 2; ++kc)
+#pragma unroll
+      for (int t = 0; t < NX; ++t)
+#pragma unroll
+        for (int r = 0; r < NL; ++r) acc[t][r] = multiply(fl[kc][r], fx[kc][t], acc[t][r]);
+    k += WAVES * 64;
+  }
+};
+
+template <int LTYPE, int XTYPE, bool UNIT, int NL, int NX, int WAVES>
+__device__ __forceinline__ void contract_staged(const Rows<LTYPE>& left, const Rows<XTYPE>& x, int K, int wave, int lane, lds_byte* s0,
+                                                lds_byte* s1, lds_byte* s2, f32x4 (&acc)[NX][NL]) {
+  Staged<LTYPE, XTYPE, UNIT, NL, NX, WAVES> o;
+  o.left = left;
+  o.x = x;
+  o.K = K;
+  o.lane = lane;
+  o.k = o.k_next = wave * 64;
+  o.lx.init(x.stride, lane);
+  if constexpr (UNIT) o.ll.init(left.stride, lane);
+  o.request(s0);
+  o.request(s1);
+  o.request(s2);                                      // past K: zeros
+  while (o.k < K) {
+    o.step(s0, acc);
+    o.step(s1, acc);
+    o.step(s2, acc);
+  }
+  wait_loads<0>();                                    // nothing may still be on its way to LDS
+}
+
+template <int LTYPE, int XTYPE, bool UNIT, int NL, int NX, int WAVES>
+__device__ __forceinline__ void contract_straight(const Rows<LTYPE>& left, const Rows<XTYPE>& rows, int K, int wave, int lane,
+                                                  f32x4 (&acc)[NX][NL]) {
+  const int l16 = lane & 15, quarter = lane >> 4;
+  // rows past the last one read the last one again, and their results are dropped
+  const typename Value<XTYPE>::T* x[NX];
+  const typename Value<LTYPE>::T* A[NL];
+#pragma unroll
+  for (int t = 0; t < NX; ++t) x[t] = rows.p + (t * 16 + l16 < rows.some ? t * 16 + l16 : rows.some - 1) * rows.stride;
+#pragma unroll
+  for (int r = 0; r < NL; ++r) A[r] = left.p + (r * 16 + l16 < left.some ? r * 16 + l16 : left.some - 1) * left.stride;
+  // 16 numbers for each quarter of the lanes: two loads that share a line of 128 bytes
+  const int k_lane = quarter * 16;
+  int k = wave * 64;
+  for (; k + 64 <= K; k += WAVES * 64) {
+    Pieces<kPieces<LTYPE>> fa[2][NL];
+    Pieces<kPieces<XTYPE>> fx[2][NX];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int at = k + k_lane + j * 8;
+#pragma unroll
+      for (int t = 0; t < NX; ++t) load8<XTYPE, true>(x[t] + at, 1, fx[j][t]);
+#pragma unroll
+      for (int r = 0; r < NL; ++r) load8<LTYPE, UNIT>(A[r] + at * left.step, left.step, fa[j][r]);
+    }
+    in_order();
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int t = 0; t < NX; ++t)
+#pragma unroll
+        for (int r = 0; r < NL; ++r) acc[t][r] = multiply(fa[j][r], fx[j][t], acc[t][r]);
+  }
+  if (k < K) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int at = k + k_lane + j * 8, n = K - at;
+      Pieces<kPieces<LTYPE>> fa[NL];
+#pragma unroll
+      for (int r = 0; r < NL; ++r) load8_some<LTYPE>(A[r] + at * left.step, left.step, n, fa[r]);
+#pragma unroll
+      for (int t = 0; t < NX; ++t) {
+        Pieces<kPieces<XTYPE>> fx;
+        load8_some<XTYPE>(x[t] + at, 1, n, fx);
+#pragma unroll
+        for (int r = 0; r < NL; ++r) acc[t][r] = multiply(fa[r], fx, acc[t][r]);
+      }
+    }
+  }
+}
+
+// ---- u = x A^T, du = scale dy B ---------------------------------------------------------------------
 struct ShrinkParams {
   const void* x; int64_t x_stride;
   const void* A; int64_t a_adapter, a_rank, a_k;      // strides from adapter to adapter, and along rank and contraction
@@ -174,22 +394,32 @@ struct ShrinkParams {
   Segments g;
 };
 
-// Workgroup (tile, j): the j-th, j + gridDim.y-th, ... segment of the tile's 16 RT rows.  The wavefronts take 64 numbers of the
-// contraction in turn.  Bound by reading x where segments are long, by reading A where each row has its own.
-// UNIT: the contraction is contiguous in A.
+// Wavefronts of a workgroup: as many as the LDS of a compute unit has room for.
 template <int DTYPE, int ATYPE, bool UNIT, int NR, int RT>
-__global__ __launch_bounds__(kShrinkWaves * 64) void shrink_kernel(ShrinkParams p) {
+constexpr int kShrinkWaves = kStageBytes<ATYPE, DTYPE, UNIT, NR, RT> <= 6144 ? 8 : kStageBytes<ATYPE, DTYPE, UNIT, NR, RT> <= 12288 ? 4 : 2;
+
+// Workgroup (tile, j): the j-th, j + gridDim.y-th, ... segment of the tile's 16 RT rows, the contraction cut over its wavefronts.
+// Bound by reading x where segments are long, by reading A where each row has its own.  UNIT: the contraction is contiguous in A.
+template <int DTYPE, int ATYPE, bool UNIT, int NR, int RT, int WAVES, bool STAGED>
+__global__ __launch_bounds__(WAVES * 64) void shrink_kernel(ShrinkParams p) {
   typedef typename Value<DTYPE>::T T;
   typedef typename Value<ATYPE>::T TA;
   constexpr int ROWS = RT * 16;
   constexpr int PITCH = NR * 16 + 1;
-  __shared__ float part[kShrinkWaves][16][PITCH];
+  constexpr int STAGE = kStageBytes<ATYPE, DTYPE, UNIT, NR, RT>;
+  constexpr int PART = WAVES * 16 * PITCH * 4;
+  constexpr int FIRST = STAGED && WAVES * STAGE > PART ? WAVES * STAGE : PART;      // the sums go where a stage was
+  // an array for each stage, so that the compiler knows the one that is read from those that are on their way
+  __shared__ __attribute__((aligned(1024))) unsigned char st0[FIRST];
+  __shared__ __attribute__((aligned(1024))) unsigned char st1[STAGED ? WAVES * STAGE : 16];
+  __shared__ __attribute__((aligned(1024))) unsigned char st2[STAGED ? WAVES * STAGE : 16];
+  float (*part)[16][PITCH] = reinterpret_cast<float (*)[16][PITCH]>(st0);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, quarter = lane >> 4;
   const int64_t row0 = (int64_t)blockIdx.x * ROWS, row1 = row0 + ROWS < p.rows ? row0 + ROWS : p.rows;
   if (blockIdx.y == 0) {
     // rows without an adapter
-    for (int i = tid; i < ROWS; i += kShrinkWaves * 64) {
+    for (int i = tid; i < ROWS; i += WAVES * 64) {
       if (row0 + i >= row1) break;
       const int a = row_adapter(p.g, p.g.begin, row0 + i, p.rows);
       if (p.adapter) p.adapter[row0 + i] = a;
@@ -205,76 +435,18 @@ __global__ __launch_bounds__(kShrinkWaves * 64) void shrink_kernel(ShrinkParams 
     hi = hi < row1 ? hi : row1;
     const int a = seg_adapter(p.g, s);
     if (a < 0 || lo >= hi) continue;
-    // rows and ranks past the last one read the last one again, and their results are dropped
-    const T* x[RT];
-    const TA* A[NR];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      const int64_t row = lo + t * 16 + l16 < hi ? lo + t * 16 + l16 : hi - 1;
-      x[t] = static_cast<const T*>(p.x) + row * p.x_stride;
-    }
-#pragma unroll
-    for (int r = 0; r < NR; ++r) {
-      const int rr = r * 16 + l16 < p.rank ? r * 16 + l16 : p.rank - 1;
-      A[r] = static_cast<const TA*>(p.A) + a * p.a_adapter + rr * p.a_rank;
-    }
     f32x4 acc[RT][NR];
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
       for (int r = 0; r < NR; ++r) acc[t][r] = f32x4{0.f, 0.f, 0.f, 0.f};
-    // A step is 64 numbers of every row, 16 of them for each quarter of the lanes: two loads that share a line of 128 bytes.
-    int k = wave * 64;
-    constexpr int STEP = kShrinkWaves * 64;
-    const int k_lane = quarter * 16;
-    auto steps = [&](auto count) {
-      constexpr int N = decltype(count)::value;
-      Pieces<kPieces<ATYPE>> fa[N][2][NR];
-      Pieces<kPieces<DTYPE>> fx[N][2][RT];
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int at = k + k_lane + i * STEP + j * 8;
-#pragma unroll
-          for (int t = 0; t < RT; ++t) load8<DTYPE, true>(x[t] + at, 1, fx[i][j][t]);
-#pragma unroll
-          for (int r = 0; r < NR; ++r) load8<ATYPE, UNIT>(A[r] + at * p.a_k, p.a_k, fa[i][j][r]);
-        }
-      in_order();
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int t = 0; t < RT; ++t)
-#pragma unroll
-            for (int r = 0; r < NR; ++r) acc[t][r] = multiply(fa[i][j][r], fx[i][j][t], acc[t][r]);
-      k += N * STEP;
-    };
-    // steps whose loads are in flight together, as registers allow
-    constexpr int REGS = (RT * kPieces<DTYPE> + NR * kPieces<ATYPE>) * 8;
-    constexpr int AHEAD = REGS * 8 <= 128 ? 8 : REGS * 4 <= 128 ? 4 : REGS * 2 <= 128 ? 2 : 1;
-    while (k + (AHEAD - 1) * STEP + 64 <= p.K) steps(Count<AHEAD>{});
-    if constexpr (AHEAD > 2)
-      while (k + STEP + 64 <= p.K) steps(Count<2>{});
-    while (k + 64 <= p.K) steps(Count<1>{});
-    if (k < p.K) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int at = k + k_lane + j * 8, n = p.K - at;
-        Pieces<kPieces<ATYPE>> fa[NR];
-#pragma unroll
-        for (int r = 0; r < NR; ++r) load8_some<ATYPE>(A[r] + at * p.a_k, p.a_k, n, fa[r]);
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-          Pieces<kPieces<DTYPE>> fx;
-          load8_some<DTYPE>(x[t] + at, 1, n, fx);
-#pragma unroll
-          for (int r = 0; r < NR; ++r) acc[t][r] = multiply(fa[r], fx, acc[t][r]);
-        }
-      }
-    }
+    const Rows<ATYPE> left{static_cast<const TA*>(p.A) + a * p.a_adapter, p.a_rank, p.a_k, p.rank};
+    const Rows<DTYPE> x{static_cast<const T*>(p.x) + lo * p.x_stride, p.x_stride, 1, (int)(hi - lo)};
+    if constexpr (STAGED)
+      contract_staged<ATYPE, DTYPE, UNIT, NR, RT, WAVES>(left, x, p.K, wave, lane, (lds_byte*)st0 + wave * STAGE, (lds_byte*)st1 + wave * STAGE,
+                                                         (lds_byte*)st2 + wave * STAGE, acc);
+    else
+      contract_straight<ATYPE, DTYPE, UNIT, NR, RT, WAVES>(left, x, p.K, wave, lane, acc);
     // lane: row l16 of a tile, ranks 4 quarter .. + 3
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
@@ -285,12 +457,12 @@ __global__ __launch_bounds__(kShrinkWaves * 64) void shrink_kernel(ShrinkParams 
 #pragma unroll
           for (int i = 0; i < 4; ++i) part[wave][l16][r * 16 + quarter * 4 + i] = acc[t][r][i];
         __syncthreads();
-        for (int i = tid; i < 16 * NR * 16; i += kShrinkWaves * 64) {
+        for (int i = tid; i < 16 * NR * 16; i += WAVES * 64) {
           const int row = i / (NR * 16), r = i % (NR * 16);
           if (r < p.low.padded && lo + t * 16 + row < hi) {
             float sum = 0.f;
 #pragma unroll
-            for (int w = 0; w < kShrinkWaves; ++w) sum += part[w][row][r];
+            for (int w = 0; w < WAVES; ++w) sum += part[w][row][r];
             sum = r < p.rank ? p.scale * sum : 0.f;
             if (r < p.rank) p.u[(lo + t * 16 + row) * p.rank + r] = sum;
             if (p.copy)
@@ -359,25 +531,6 @@ struct ProductParams {
 };
 
 constexpr int kBK = 64;                               // numbers of a row in a step: 128 bytes
-constexpr int waitcnt(int vm, int lgkm) { return (vm & 0xF) | ((vm >> 4) << 14) | (0x7 << 4) | ((lgkm & 0xF) << 8); }
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* base, unsigned bytes) {
-  const unsigned long long a = reinterpret_cast<unsigned long long>(base);
-  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)a);
-  const unsigned hi = __builtin_amdgcn_readfirstlane((unsigned)(a >> 32));
-  void* ptr = reinterpret_cast<void*>(((unsigned long long)hi << 32) | lo);
-  return __builtin_amdgcn_make_buffer_rsrc(ptr, 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
-}
-
-// Waits until at most LEFT of the wavefront's own loads, those to LDS among them, are on their way, and then for the workgroup.
-template <int LEFT>
-__device__ __forceinline__ void arrived() {
-  __builtin_amdgcn_s_waitcnt(waitcnt(LEFT, 0));
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-
 // One operand's tile of R rows by kBK numbers in LDS: row r is 128 bytes = 8 units of 16, unit q at position q ^ (r / 2 % 8): the
 // sixteen lanes whose fragments LDS serves together (0-3, 12-15, 20-23, 24-27 and so on) then read from different banks (no
 // conflict counted).  Global memory goes to LDS directly, eight whole rows an instruction; the lane order of that copy is fixed,
@@ -660,100 +813,66 @@ struct FewRowsParams {
   const int* adapter;                                 // of every row
 };
 constexpr int kFewRows = 64;
-constexpr int kFewWaves = 8;
 constexpr int kHead = 16;                             // ranks that are read ahead
 
-// A workgroup's 16 outputs: eight wavefronts go along the rows of W 512 bytes (bf16) at a time, so that W streams from
-// memory once; x comes from L2.  Bound by reading W.
-template <int DTYPE, int QTYPE, int RT>
-__global__ __launch_bounds__(kFewWaves * 64) void few_rows_kernel(FewRowsParams p) {
+// A workgroup's 16 outputs, the contraction cut over its wavefronts.  Bound by reading W.
+template <int DTYPE, int RT>
+constexpr int kFewWaves = kStageBytes<DTYPE, DTYPE, true, 1, RT> <= 6144 ? 8 : kStageBytes<DTYPE, DTYPE, true, 1, RT> <= 12288 ? 4 : 2;
+
+template <int DTYPE, int QTYPE, int RT, int WAVES, bool STAGED>
+__global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(FewRowsParams p) {
   typedef typename Value<DTYPE>::T T;
   typedef typename Value<QTYPE>::T TQ;
-  __shared__ float part[kFewWaves][RT * 16][17];
+  constexpr int STAGE = kStageBytes<DTYPE, DTYPE, true, 1, RT>;
+  constexpr int PART = WAVES * RT * 16 * 17 * 4;
+  constexpr int FIRST = STAGED && WAVES * STAGE > PART ? WAVES * STAGE : PART;      // the sums go where a stage was
+  __shared__ __attribute__((aligned(1024))) unsigned char st0[FIRST];
+  __shared__ __attribute__((aligned(1024))) unsigned char st1[STAGED ? WAVES * STAGE : 16];
+  __shared__ __attribute__((aligned(1024))) unsigned char st2[STAGED ? WAVES * STAGE : 16];
+  float (*part)[RT * 16][17] = reinterpret_cast<float (*)[RT * 16][17]>(st0);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, quarter = lane >> 4;
   const int n0 = blockIdx.x * 16;
-  // This lane's outputs, rows row0 + 32 o of column `col`, and what their low-rank part needs: asked for before W is.
-  constexpr int OUT = RT > 1 ? RT / 2 : 1;
+  // This lane's outputs, rows row0 + EACH o of column `col`, and what their low-rank part needs: asked for before W is.
+  constexpr int EACH = WAVES * 4, OUT = RT * 16 > EACH ? RT * 16 / EACH : 1;
   const int row0 = tid >> 4, col = n0 + (tid & 15);
   int adapter[OUT];
   float u[OUT][kHead], q[OUT][kHead];
 #pragma unroll
-  for (int o = 0; o < OUT; ++o) adapter[o] = row0 + o * 32 < p.M ? p.adapter[row0 + o * 32] : -1;
+  for (int o = 0; o < OUT; ++o) adapter[o] = row0 + o * EACH < p.M ? p.adapter[row0 + o * EACH] : -1;
 #pragma unroll
   for (int o = 0; o < OUT; ++o)
 #pragma unroll
     for (int e = 0; e < kHead; ++e) {
       const int r = e < p.rank ? e : p.rank - 1;
-      u[o][e] = adapter[o] >= 0 && col < p.N ? p.u[(int64_t)(row0 + o * 32) * p.rank + r] : 0.f;
+      u[o][e] = adapter[o] >= 0 && col < p.N ? p.u[(int64_t)(row0 + o * EACH) * p.rank + r] : 0.f;
       q[o][e] = adapter[o] >= 0 && col < p.N
                     ? Value<QTYPE>::get(static_cast<const TQ*>(p.Q) + adapter[o] * p.q_adapter + col * p.q_n + r * p.q_r) : 0.f;
     }
   in_order();
-  const T* w = static_cast<const T*>(p.W) + (int64_t)(n0 + l16 < p.N ? n0 + l16 : p.N - 1) * p.ldw;
-  const T* x[RT];
+  f32x4 acc[RT][1];
 #pragma unroll
-  for (int t = 0; t < RT; ++t) x[t] = static_cast<const T*>(p.X) + (int64_t)(t * 16 + l16 < p.M ? t * 16 + l16 : p.M - 1) * p.ldx;
-  f32x4 acc[RT];
-#pragma unroll
-  for (int t = 0; t < RT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  // A step is 64 numbers of every row, 16 of them for each quarter of the lanes: two loads that share a line of 128 bytes.
-  int k = wave * 64;
-  constexpr int STEP = kFewWaves * 64;
-  const int k_lane = quarter * 16;
-  auto steps = [&](auto count) {
-    constexpr int N = decltype(count)::value;
-    Pieces<kPieces<DTYPE>> fw[N][2], fx[N][2][RT];
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) load8<DTYPE, true>(w + k + k_lane + i * STEP + j * 8, 1, fw[i][j]);
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int t = 0; t < RT; ++t) load8<DTYPE, true>(x[t] + k + k_lane + i * STEP + j * 8, 1, fx[i][j][t]);
-    in_order();
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int t = 0; t < RT; ++t) acc[t] = multiply(fw[i][j], fx[i][j][t], acc[t]);
-    k += N * STEP;
-  };
-  // steps whose loads are in flight together, as registers allow
-  constexpr int AHEAD = DTYPE == LSAM_DTYPE_BF16 ? 8 / RT : RT == 1 ? 2 : 1;
-  while (k + (AHEAD - 1) * STEP + 64 <= p.K) steps(Count<AHEAD>{});
-  if constexpr (AHEAD > 2)
-    while (k + STEP + 64 <= p.K) steps(Count<2>{});
-  while (k + 64 <= p.K) steps(Count<1>{});
-  if (k < p.K) {
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int at = k + k_lane + j * 8, n = p.K - at;
-      Pieces<kPieces<DTYPE>> fw, fx;
-      load8_some<DTYPE>(w + at, 1, n, fw);
-#pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        load8_some<DTYPE>(x[t] + at, 1, n, fx);
-        acc[t] = multiply(fw, fx, acc[t]);
-      }
-    }
-  }
+  for (int t = 0; t < RT; ++t) acc[t][0] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const Rows<DTYPE> left{static_cast<const T*>(p.W) + (int64_t)n0 * p.ldw, p.ldw, 1, p.N - n0 < 16 ? p.N - n0 : 16};
+  const Rows<DTYPE> x{static_cast<const T*>(p.X), p.ldx, 1, p.M};
+  if constexpr (STAGED)
+    contract_staged<DTYPE, DTYPE, true, 1, RT, WAVES>(left, x, p.K, wave, lane, (lds_byte*)st0 + wave * STAGE, (lds_byte*)st1 + wave * STAGE,
+                                                      (lds_byte*)st2 + wave * STAGE, acc);
+  else
+    contract_straight<DTYPE, DTYPE, true, 1, RT, WAVES>(left, x, p.K, wave, lane, acc);
+  __syncthreads();
 #pragma unroll
   for (int t = 0; t < RT; ++t)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) part[wave][t * 16 + l16][quarter * 4 + i] = acc[t][i];
+    for (int i = 0; i < 4; ++i) part[wave][t * 16 + l16][quarter * 4 + i] = acc[t][0][i];
   __syncthreads();
 #pragma unroll
   for (int o = 0; o < OUT; ++o) {
-    const int row = row0 + o * 32;
+    const int row = row0 + o * EACH;
     if (row >= p.M || row >= RT * 16 || col >= p.N) continue;
     float sum = 0.f;
 #pragma unroll
-    for (int v = 0; v < kFewWaves; ++v) sum += part[v][row][tid & 15];
+    for (int v = 0; v < WAVES; ++v) sum += part[v][row][tid & 15];
     if (adapter[o] >= 0) {
       float low = 0.f;
 #pragma unroll
@@ -947,10 +1066,13 @@ __global__ __launch_bounds__(256) void planes_kernel(PlanesParams p) {
 int64_t up8(int64_t n) { return (n + 7) & ~7ll; }
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Whether the tiles can be read straight from the caller's rows: bf16, whole aligned units, tiles within 31 bits.
-bool straight(const void* p, int64_t stride, int cols, int dtype) {
-  return dtype == LSAM_DTYPE_BF16 && !misaligned(p, 16) && stride % 8 == 0 && cols % 8 == 0 && stride <= 1 << 21;
+// Whether rows can go to LDS as they lie: whole aligned units of 16 bytes, tiles within 31 bits.
+bool whole_units(const void* p, int64_t stride, int cols, int dtype) {
+  const int n = 16 / dtype_bytes(dtype);
+  return !misaligned(p, 16) && stride % n == 0 && cols % n == 0 && stride <= 1 << 21;
 }
+// The same for the tiles of product_kernel, which are bf16.
+bool straight(const void* p, int64_t stride, int cols, int dtype) { return dtype == LSAM_DTYPE_BF16 && whole_units(p, stride, cols, dtype); }
 // The same from the descriptor alone: what a workspace must be large enough for.
 size_t planes_bytes(int64_t rows, int cols, int dtype) { return up256((size_t)(dtype == LSAM_DTYPE_BF16 ? 1 : 3) * rows * up8(cols) * 2); }
 
@@ -1025,18 +1147,28 @@ int check_args(const Arg* args, int n, const char* who) {
   return LSAM_OK;
 }
 
+template <int DTYPE, int ATYPE, bool UNIT, int NR, int RT>
+void launch_shrink_tile(const ShrinkParams& p, dim3 grid, bool staged, hipStream_t s) {
+  constexpr int waves = kShrinkWaves<DTYPE, ATYPE, UNIT, NR, RT>;
+  if (staged) shrink_kernel<DTYPE, ATYPE, UNIT, NR, RT, waves, true><<<grid, waves * 64, 0, s>>>(p);
+  else shrink_kernel<DTYPE, ATYPE, UNIT, NR, RT, waves, false><<<grid, waves * 64, 0, s>>>(p);
+}
 template <int DTYPE, int ATYPE, bool UNIT, int NR>
 void launch_shrink_rank(const ShrinkParams& p, hipStream_t s) {
   // Tiles of 64 rows read the adapter least often; of 32 or 16 rows where those leave units idle or segments are short.
   const bool brief = p.rows <= 16ll * p.g.n;
-  const int64_t rows = !brief && p.rows >= 64 * 256 ? 64 : !brief && p.rows >= 32 * 192 ? 32 : 16;
+  constexpr bool ROOM = kStageBytes<ATYPE, DTYPE, UNIT, NR, 4> <= 24576;          // for three stages of two wavefronts
+  const int64_t rows = ROOM && !brief && p.rows >= 64 * 256 ? 64 : !brief && p.rows >= 32 * 192 ? 32 : 16;
   const int64_t tiles = (p.rows + rows - 1) / rows;
   int64_t y = p.g.n / tiles + 1;
   y = y > 64 ? 64 : y;
   const dim3 grid((unsigned)tiles, (unsigned)y);
-  if (rows == 64) shrink_kernel<DTYPE, ATYPE, UNIT, NR, 4><<<grid, kShrinkWaves * 64, 0, s>>>(p);
-  else if (rows == 32) shrink_kernel<DTYPE, ATYPE, UNIT, NR, 2><<<grid, kShrinkWaves * 64, 0, s>>>(p);
-  else shrink_kernel<DTYPE, ATYPE, UNIT, NR, 1><<<grid, kShrinkWaves * 64, 0, s>>>(p);
+  const bool staged = whole_units(p.x, p.x_stride, p.K, DTYPE) &&
+                      (!UNIT || (whole_units(p.A, p.a_rank, p.K, ATYPE) && p.a_adapter % (16 / dtype_bytes(ATYPE)) == 0));
+  if constexpr (ROOM)
+    if (rows == 64) return launch_shrink_tile<DTYPE, ATYPE, UNIT, NR, 4>(p, grid, staged, s);
+  if (rows == 32) launch_shrink_tile<DTYPE, ATYPE, UNIT, NR, 2>(p, grid, staged, s);
+  else launch_shrink_tile<DTYPE, ATYPE, UNIT, NR, 1>(p, grid, staged, s);
 }
 template <int DTYPE, int ATYPE>
 void launch_shrink(const ShrinkParams& p, hipStream_t s) {
@@ -1094,12 +1226,18 @@ void launch_product(const ProductParams& p, hipStream_t s) {
   else launch_product_tile<OTYPE, 64, 64, 2, 2, 8>(p, s);
 }
 
+template <int DTYPE, int QTYPE, int RT>
+void launch_few_rows_tile(const FewRowsParams& p, hipStream_t s) {
+  const unsigned grid = (unsigned)((p.N + 15) / 16);
+  constexpr int waves = kFewWaves<DTYPE, RT>;
+  if (whole_units(p.X, p.ldx, p.K, DTYPE) && whole_units(p.W, p.ldw, p.K, DTYPE)) few_rows_kernel<DTYPE, QTYPE, RT, waves, true><<<grid, waves * 64, 0, s>>>(p);
+  else few_rows_kernel<DTYPE, QTYPE, RT, waves, false><<<grid, waves * 64, 0, s>>>(p);
+}
 template <int DTYPE, int QTYPE>
 void launch_few_rows(const FewRowsParams& p, hipStream_t s) {
-  const unsigned grid = (unsigned)((p.N + 15) / 16);
-  if (p.M <= 16) few_rows_kernel<DTYPE, QTYPE, 1><<<grid, kFewWaves * 64, 0, s>>>(p);
-  else if (p.M <= 32) few_rows_kernel<DTYPE, QTYPE, 2><<<grid, kFewWaves * 64, 0, s>>>(p);
-  else few_rows_kernel<DTYPE, QTYPE, 4><<<grid, kFewWaves * 64, 0, s>>>(p);
+  if (p.M <= 16) launch_few_rows_tile<DTYPE, QTYPE, 1>(p, s);
+  else if (p.M <= 32) launch_few_rows_tile<DTYPE, QTYPE, 2>(p, s);
+  else launch_few_rows_tile<DTYPE, QTYPE, 4>(p, s);
 }
 void launch_few_rows_any(const FewRowsParams& p, int dtype, int qtype, hipStream_t s) {
   if (dtype == LSAM_DTYPE_BF16) {
