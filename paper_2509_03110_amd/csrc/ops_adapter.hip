@@ -248,14 +248,18 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const Rows<DTYPE>& r,
   return make_rsrc(r.p, (unsigned)(((r.some - 1) * r.stride + K) * (DTYPE == LSAM_DTYPE_BF16 ? 2 : 4)));
 }
 
-constexpr int kRing = 3;
-// Bytes of a wavefront's part of a stage.
+// Bytes of a wavefront's part of a stage; wavefronts of a workgroup and stages, as many as the LDS of a compute unit has room for
+// (more wavefronts rather than more stages: fp32's pieces are cut by the vector units, one wavefront at a time).
 template <int LTYPE, int XTYPE, bool UNIT, int NL, int NX>
 constexpr int kStageBytes = Lines<XTYPE, NX * 16>::BYTES + (UNIT ? Lines<LTYPE, NL * 16>::BYTES : 0);
+constexpr int kRoom = 156 << 10;
+constexpr int waves_for(int bytes) { return 8 * 2 * bytes <= kRoom ? 8 : 4 * 2 * bytes <= kRoom ? 4 : 2; }
+constexpr int ring_for(int bytes) { return waves_for(bytes) * 3 * bytes <= kRoom ? 3 : 2; }
 
 // A wavefront's way along K.
 template <int LTYPE, int XTYPE, bool UNIT, int NL, int NX, int WAVES>
 struct Staged {
+  static constexpr int RING = ring_for(kStageBytes<LTYPE, XTYPE, UNIT, NL, NX>);
   typedef Lines<XTYPE, NX * 16> LX;
   typedef Lines<LTYPE, NL * 16> LL;
   static constexpr int LOADS = LX::NLOAD + (UNIT ? LL::NLOAD : 0);
@@ -270,7 +274,7 @@ struct Staged {
     if constexpr (UNIT) ll.issue(resource(left, K), stage + LX::BYTES, k_next, K, lane);
     k_next += WAVES * 64;
   }
-  // Multiplies a stage and asks for the step after next but one in its place.
+  // Multiplies a stage and asks for the step RING steps later in its place.
   __device__ __forceinline__ void step(lds_byte* stage, f32x4 (&acc)[NX][NL]) {
     const int l16 = lane & 15, quarter = lane >> 4;
     Pieces<kPieces<LTYPE>> fl[2][NL];
@@ -286,7 +290,7 @@ struct Staged {
           else load8_some<LTYPE>(p, left.step, K - at, fl[kc][r]);
         }
     }
-    wait_loads<(kRing - 1) * LOADS>();
+    wait_loads<(RING - 1) * LOADS>();
     Pieces<kPieces<XTYPE>> fx[2][NX];
 #pragma unroll
     for (int kc = 0; kc < 2; ++kc) {
@@ -322,11 +326,11 @@ __device__ __forceinline__ void contract_staged(const Rows<LTYPE>& left, const R
   if constexpr (UNIT) o.ll.init(left.stride, lane);
   o.request(s0);
   o.request(s1);
-  o.request(s2);                                      // past K: zeros
+  if constexpr (o.RING > 2) o.request(s2);            // past K: zeros
   while (o.k < K) {
     o.step(s0, acc);
     o.step(s1, acc);
-    o.step(s2, acc);
+    if constexpr (o.RING > 2) o.step(s2, acc);
   }
   wait_loads<0>();                                    // nothing may still be on its way to LDS
 }
@@ -394,9 +398,8 @@ struct ShrinkParams {
   Segments g;
 };
 
-// Wavefronts of a workgroup: as many as the LDS of a compute unit has room for.
 template <int DTYPE, int ATYPE, bool UNIT, int NR, int RT>
-constexpr int kShrinkWaves = kStageBytes<ATYPE, DTYPE, UNIT, NR, RT> <= 6144 ? 8 : kStageBytes<ATYPE, DTYPE, UNIT, NR, RT> <= 12288 ? 4 : 2;
+constexpr int kShrinkWaves = waves_for(kStageBytes<ATYPE, DTYPE, UNIT, NR, RT>);
 
 // Workgroup (tile, j): the j-th, j + gridDim.y-th, ... segment of the tile's 16 RT rows, the contraction cut over its wavefronts.
 // Bound by reading x where segments are long, by reading A where each row has its own.  UNIT: the contraction is contiguous in A.
@@ -412,7 +415,7 @@ __global__ __launch_bounds__(WAVES * 64) void shrink_kernel(ShrinkParams p) {
   // an array for each stage, so that the compiler knows the one that is read from those that are on their way
   __shared__ __attribute__((aligned(1024))) unsigned char st0[FIRST];
   __shared__ __attribute__((aligned(1024))) unsigned char st1[STAGED ? WAVES * STAGE : 16];
-  __shared__ __attribute__((aligned(1024))) unsigned char st2[STAGED ? WAVES * STAGE : 16];
+  __shared__ __attribute__((aligned(1024))) unsigned char st2[STAGED && ring_for(STAGE) > 2 ? WAVES * STAGE : 16];
   float (*part)[16][PITCH] = reinterpret_cast<float (*)[16][PITCH]>(st0);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, quarter = lane >> 4;
@@ -444,7 +447,7 @@ __global__ __launch_bounds__(WAVES * 64) void shrink_kernel(ShrinkParams p) {
     const Rows<DTYPE> x{static_cast<const T*>(p.x) + lo * p.x_stride, p.x_stride, 1, (int)(hi - lo)};
     if constexpr (STAGED)
       contract_staged<ATYPE, DTYPE, UNIT, NR, RT, WAVES>(left, x, p.K, wave, lane, (lds_byte*)st0 + wave * STAGE, (lds_byte*)st1 + wave * STAGE,
-                                                         (lds_byte*)st2 + wave * STAGE, acc);
+                                                         (lds_byte*)st2 + (ring_for(STAGE) > 2 ? wave * STAGE : 0), acc);
     else
       contract_straight<ATYPE, DTYPE, UNIT, NR, RT, WAVES>(left, x, p.K, wave, lane, acc);
     // lane: row l16 of a tile, ranks 4 quarter .. + 3
@@ -817,7 +820,7 @@ constexpr int kHead = 16;                             // ranks that are read ahe
 
 // A workgroup's 16 outputs, the contraction cut over its wavefronts.  Bound by reading W.
 template <int DTYPE, int RT>
-constexpr int kFewWaves = kStageBytes<DTYPE, DTYPE, true, 1, RT> <= 6144 ? 8 : kStageBytes<DTYPE, DTYPE, true, 1, RT> <= 12288 ? 4 : 2;
+constexpr int kFewWaves = waves_for(kStageBytes<DTYPE, DTYPE, true, 1, RT>);
 
 template <int DTYPE, int QTYPE, int RT, int WAVES, bool STAGED>
 __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(FewRowsParams p) {
@@ -828,7 +831,7 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(FewRowsParams p) {
   constexpr int FIRST = STAGED && WAVES * STAGE > PART ? WAVES * STAGE : PART;      // the sums go where a stage was
   __shared__ __attribute__((aligned(1024))) unsigned char st0[FIRST];
   __shared__ __attribute__((aligned(1024))) unsigned char st1[STAGED ? WAVES * STAGE : 16];
-  __shared__ __attribute__((aligned(1024))) unsigned char st2[STAGED ? WAVES * STAGE : 16];
+  __shared__ __attribute__((aligned(1024))) unsigned char st2[STAGED && ring_for(STAGE) > 2 ? WAVES * STAGE : 16];
   float (*part)[RT * 16][17] = reinterpret_cast<float (*)[RT * 16][17]>(st0);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, quarter = lane >> 4;
@@ -857,7 +860,7 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(FewRowsParams p) {
   const Rows<DTYPE> x{static_cast<const T*>(p.X), p.ldx, 1, p.M};
   if constexpr (STAGED)
     contract_staged<DTYPE, DTYPE, true, 1, RT, WAVES>(left, x, p.K, wave, lane, (lds_byte*)st0 + wave * STAGE, (lds_byte*)st1 + wave * STAGE,
-                                                      (lds_byte*)st2 + wave * STAGE, acc);
+                                                      (lds_byte*)st2 + (ring_for(STAGE) > 2 ? wave * STAGE : 0), acc);
   else
     contract_straight<DTYPE, DTYPE, true, 1, RT, WAVES>(left, x, p.K, wave, lane, acc);
   __syncthreads();
@@ -1157,11 +1160,11 @@ template <int DTYPE, int ATYPE, bool UNIT, int NR>
 void launch_shrink_rank(const ShrinkParams& p, hipStream_t s) {
   // Tiles of 64 rows read the adapter least often; of 32 or 16 rows where those leave units idle or segments are short.
   const bool brief = p.rows <= 16ll * p.g.n;
-  constexpr bool ROOM = kStageBytes<ATYPE, DTYPE, UNIT, NR, 4> <= 24576;          // for three stages of two wavefronts
+  constexpr bool ROOM = 2 * 2 * kStageBytes<ATYPE, DTYPE, UNIT, NR, 4> <= kRoom;      // for two stages of two wavefronts
   const int64_t rows = ROOM && !brief && p.rows >= 64 * 256 ? 64 : !brief && p.rows >= 32 * 192 ? 32 : 16;
   const int64_t tiles = (p.rows + rows - 1) / rows;
-  int64_t y = p.g.n / tiles + 1;
-  y = y > 64 ? 64 : y;
+  int64_t y = p.g.n / tiles + 2;                      // two segments meet in many a tile: a workgroup for each
+  y = y > 64 ? 64 : y > p.g.n ? (p.g.n > 0 ? p.g.n : 1) : y;
   const dim3 grid((unsigned)tiles, (unsigned)y);
   const bool staged = whole_units(p.x, p.x_stride, p.K, DTYPE) &&
                       (!UNIT || (whole_units(p.A, p.a_rank, p.K, ATYPE) && p.a_adapter % (16 / dtype_bytes(ATYPE)) == 0));
