@@ -596,7 +596,7 @@ __device__ __forceinline__ void product_tile(const ProductParams& p) {
   typedef RowTile<BM, NW> OX;
   typedef RowTile<BN, NW> OW;
   // an array each, so that the compiler knows the stage that is read from those that are on their way
-  static_assert(S == 2 || S == 4 || S == 8, "stages");
+  static_assert(TM * TN == 1 ? S == 8 : S == 2 || S == 4, "small tiles have eight stages, others two or four");
   constexpr int STAGE = OX::BYTES + OW::BYTES, NL = OX::NLOAD + OW::NLOAD;
   __shared__ __attribute__((aligned(1024))) unsigned char st0[STAGE];
   __shared__ __attribute__((aligned(1024))) unsigned char st1[STAGE];
@@ -674,39 +674,70 @@ __device__ __forceinline__ void product_tile(const ProductParams& p) {
   if constexpr (S > 2) { request(a2); request(a3); }
   if constexpr (S > 4) { request(a4); request(a5); request(a6); request(a7); }
   arrived<(S - 1) * NL>();
-  read(a0, 0, 0);
-  auto step = [&](lds_byte* now, lds_byte* then) {
-    read(now, 1, 1);
-    multiply_chunk(0);
-    interleave<0x100, TM + TN, TM * TN>();
-    read(now, 2, 0);
-    multiply_chunk(1);
-    interleave<0x100, TM + TN, TM * TN>();
-    read(now, 3, 1);
-    multiply_chunk(0);
-    interleave<0x100, TM + TN, TM * TN>();
-    // Every wavefront has taken its last fragment of this step, and the next one has arrived.
-    arrived<(S - 2) * NL>();
-    request(now);
-    read(then, 0, 0);                    // behind the last step: never multiplied
-    multiply_chunk(1);
-    interleave<0x120, TM + TN + NL, TM * TN>();
-  };
-  for (int s = 0; s < steps; s += S) {
-    step(a0, a1);
-    if constexpr (S == 2) {
-      step(a1, a0);
-    } else {
-      step(a1, a2);
-      step(a2, a3);
-      if constexpr (S == 4) {
-        step(a3, a0);
+  if constexpr (TM * TN == 1) {
+    // One block of results a wavefront: too little to multiply while a fragment comes from LDS.  All of the next step's
+    // fragments are read while this one's are multiplied, into two sums, so that they do not wait for each other.
+    u32x4 gx[2][4], gw[2][4];
+    f32x16 other;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) other[e] = 0.f;
+    auto read_all = [&](const lds_byte* tile, int buf) {
+#pragma unroll
+      for (int kc = 0; kc < 4; ++kc) {
+        gx[buf][kc] = fragment(tile, wm + l32, kc, half);
+        gw[buf][kc] = fragment(tile + OX::BYTES, wn + l32, kc, half);
+      }
+    };
+    read_all(a0, 0);
+    auto step = [&](lds_byte* now, lds_byte* then, int buf) {
+      arrived<(S - 2) * NL>();
+      request(now);
+      read_all(then, buf ^ 1);
+#pragma unroll
+      for (int kc = 0; kc < 4; kc += 2) {
+        acc[0][0] = mfma32(gw[buf][kc], gx[buf][kc], acc[0][0]);
+        other = mfma32(gw[buf][kc + 1], gx[buf][kc + 1], other);
+      }
+    };
+    for (int s = 0; s < steps; s += S) {
+      step(a0, a1, 0);
+      step(a1, a2, 1);
+      step(a2, a3, 0);
+      step(a3, a4, 1);
+      step(a4, a5, 0);
+      step(a5, a6, 1);
+      step(a6, a7, 0);
+      step(a7, a0, 1);
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[0][0][e] += other[e];
+  } else {
+    read(a0, 0, 0);
+    auto step = [&](lds_byte* now, lds_byte* then) {
+      read(now, 1, 1);
+      multiply_chunk(0);
+      interleave<0x100, TM + TN, TM * TN>();
+      read(now, 2, 0);
+      multiply_chunk(1);
+      interleave<0x100, TM + TN, TM * TN>();
+      read(now, 3, 1);
+      multiply_chunk(0);
+      interleave<0x100, TM + TN, TM * TN>();
+      // Every wavefront has taken its last fragment of this step, and the next one has arrived.
+      arrived<(S - 2) * NL>();
+      request(now);
+      read(then, 0, 0);                    // behind the last step: never multiplied
+      multiply_chunk(1);
+      interleave<0x120, TM + TN + NL, TM * TN>();
+    };
+    for (int s = 0; s < steps; s += S) {
+      step(a0, a1);
+      if constexpr (S == 2) {
+        step(a1, a0);
       } else {
-        step(a3, a4);
-        step(a4, a5);
-        step(a5, a6);
-        step(a6, a7);
-        step(a7, a0);
+        step(a1, a2);
+        step(a2, a3);
+        step(a3, a0);
       }
     }
   }
