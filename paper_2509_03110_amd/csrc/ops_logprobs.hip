@@ -47,7 +47,7 @@ __device__ __forceinline__ u64 ranked(unsigned key, unsigned index) { return (u6
 
 struct TopShared {
   u64 list[2][LSAM_TOP_MAX];           // the best so far, best first, and the next such list
-  u64 cand[kCandidates];
+  u64 cand[kCandidates + 8];
   u64 wave_max[kWaves];
   unsigned bound[kWaves];
   int count, hits;
@@ -59,7 +59,7 @@ struct TopShared {
 //
 // A wavefront's top-th largest of its 64 lane maxima is no larger than the block's top-th largest logit: what lies
 // below that bound (found bit by bit, with ballots) cannot be among the best.  Little more than `top` candidates are
-// left as a rule; each counts the candidates above it, which is its rank.  Where many equals leave too many of them,
+// left as a rule, the list among them; each counts the candidates above it, which is its rank.  Where many equals leave too many of them,
 // the best are found one after the other instead.
 template <int N>
 __device__ __forceinline__ int join_top(TopShared& sh, int cur, int have, int top, const unsigned (&key)[N],
@@ -71,11 +71,14 @@ __device__ __forceinline__ int join_top(TopShared& sh, int cur, int have, int to
   unsigned most = 0;
 #pragma unroll
   for (int i = 0; i < N; ++i) most = key[i] > most ? key[i] : most;
-  if (tid == 0) { sh.count = 0; sh.hits = 0; }
+  if (tid == 0) { sh.count = have; sh.hits = 0; }
+  if (tid < have) sh.cand[tid] = list[tid];
   __syncthreads();
   if (__ballot(most > last) != 0 && lane == 0) sh.hits = 1;
+  // 18 bits tell bfloat16 logits apart and fp32 ones to 2^-9: a bound that is a little low lets a few more candidates through
   unsigned bound = 0;
-  for (int bit = 31; bit >= 0; --bit) {
+#pragma unroll
+  for (int bit = 31; bit >= 14; --bit) {
     const unsigned trial = bound | 1u << bit;
     if (__popcll(__ballot(most >= trial)) >= top) bound = trial;
   }
@@ -98,13 +101,21 @@ __device__ __forceinline__ int join_top(TopShared& sh, int cur, int have, int to
   }
   __syncthreads();
   const int n = sh.count;
-  int got = have + n < top ? have + n : top;
+  int got = n < top ? n : top;
   if (n <= kCandidates) {
-    for (int j = tid; j < have + n; j += kThreads) {
-      const u64 mine = j < have ? list[j] : sh.cand[j - have];
+    // nothing behind the last candidate is above any, so that they can be read eight at a time
+    if (tid < 8) sh.cand[n + tid] = 0;
+    __syncthreads();
+    for (int j = tid; j < n; j += kThreads) {
+      const u64 mine = sh.cand[j];
       int above = 0;
-      for (int i = 0; i < have; ++i) above += list[i] > mine;
-      for (int i = 0; i < n; ++i) above += sh.cand[i] > mine;
+      for (int i = 0; i < n; i += 8) {
+        u64 c[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) c[e] = sh.cand[i + e];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) above += c[e] > mine;
+      }
       if (above < top) next[above] = mine;
     }
   } else {
@@ -166,27 +177,29 @@ __device__ __forceinline__ Sums join_wave(Sums v) {
   return v;
 }
 
-// The row's results from its sums; one lane.
+// The row's token and its logit, asked for before the row is read.
+struct Wanted { int64_t token; float z; };
 template <int DTYPE>
-__device__ __forceinline__ void finish_row(const LogprobParams& p, int64_t row, const Sums& v, float (&lse)[2]) {
+__device__ __forceinline__ Wanted wanted(const LogprobParams& p, int64_t row) {
   typedef typename Value<DTYPE>::T T;
+  Wanted w{-1, 0.f};
+  if (p.tokens) w.token = p.tokens[row];
+  if (w.token >= p.V) w.token = -1;
+  if (w.token >= 0) w.z = Value<DTYPE>::get(static_cast<const T*>(p.z) + row * p.stride + w.token);
+  return w;
+}
+
+// The row's results from its sums; one lane.
+__device__ __forceinline__ void finish_row(const LogprobParams& p, int64_t row, const Sums& v, const Wanted& w, float (&lse)[2]) {
   const float inf = __builtin_inff();
   const bool empty = v.m == -inf && v.s == 0.f;                       // every logit is -inf
-  const double ln_s = empty ? 0.0 : log((double)v.s);
+  const float ln_s = empty ? 0.f : logf(v.s);
   lse[0] = v.s != v.s ? v.s : v.m;                                    // NaN or +inf in the row: NaN
-  lse[1] = (float)ln_s;
-  p.entropy[row] = empty ? 0.f : (float)(ln_s - (double)v.t / (double)v.s);
+  lse[1] = ln_s;
+  p.entropy[row] = empty ? 0.f : ln_s - v.t / v.s;
   p.lse[2 * row] = lse[0];
   p.lse[2 * row + 1] = lse[1];
-  if (p.tokens) {
-    const int64_t tok = p.tokens[row];
-    float lp = 0.f;
-    if (tok >= 0 && tok < p.V) {
-      const float z = Value<DTYPE>::get(static_cast<const T*>(p.z) + row * p.stride + tok);
-      lp = empty ? -inf : (float)((double)z - (double)lse[0] - ln_s);
-    }
-    p.logp[row] = lp;
-  }
+  if (p.tokens) p.logp[row] = w.token < 0 ? 0.f : empty ? -inf : w.z - lse[0] - ln_s;
 }
 
 __device__ __forceinline__ void write_top(const LogprobParams& p, int64_t row, const u64* list, int have, const float* lse) {
@@ -215,20 +228,22 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobParams p) {
   const float inf = __builtin_inff();
   Sums v{-inf, 0.f, 0.f};
   int have = 0, cur = 0;
+  Wanted w{-1, 0.f};
+  if (p.splits == 1 && tid == 0) w = wanted<DTYPE>(p, row);
   for (int64_t at = begin; at < end; at += kStep) {
     float x[N];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int64_t c = at + (j * kThreads + tid) * 8;
-      float w[8];
+      float eight[8];
       if (c + 8 <= end) {
-        V::load8(z + c, w);
+        V::load8(z + c, eight);
       } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = c + e < end ? V::get(z + c + e) : -inf;
+        for (int e = 0; e < 8; ++e) eight[e] = c + e < end ? V::get(z + c + e) : -inf;
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[8 * j + e] = w[e];
+      for (int e = 0; e < 8; ++e) x[8 * j + e] = eight[e];
     }
     float m = v.m;
 #pragma unroll
@@ -269,7 +284,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobParams p) {
   if (p.splits == 1) {
     if (tid == 0) {
       float lse[2];
-      finish_row<DTYPE>(p, row, v, lse);
+      finish_row(p, row, v, w, lse);
       row_lse[0] = lse[0];
       row_lse[1] = lse[1];
     }
@@ -295,6 +310,8 @@ __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(LogprobParams p
   const int64_t row = p.row0 + blockIdx.x;
   if (tid < 64) {
     Sums v{-__builtin_inff(), 0.f, 0.f};
+    Wanted w{-1, 0.f};
+    if (tid == 0) w = wanted<DTYPE>(p, row);
     if (tid < p.splits) {
       const f32x4 q = *reinterpret_cast<const f32x4*>(p.part + 4 * (row * p.splits + tid));
       v = Sums{q[0], q[1], q[2]};
@@ -302,7 +319,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(LogprobParams p
     v = join_wave(v);
     if (tid == 0) {
       float lse[2];
-      finish_row<DTYPE>(p, row, v, lse);
+      finish_row(p, row, v, w, lse);
       row_lse[0] = lse[0];
       row_lse[1] = lse[1];
     }
