@@ -520,9 +520,8 @@ __global__ __launch_bounds__(256) void copies_kernel(CopiesParams p) {
 
 // ---- y or dx, many rows -----------------------------------------------------------------------------
 struct ProductParams {
-  const unsigned short* X; int64_t ldx, plane_x;      // [planes][M][ldx], K of each row
-  const unsigned short* W; int64_t ldw, plane_w;      // [planes][N][ldw]
-  int products;                                       // 1, or the 6 of three planes
+  const unsigned short* X; int64_t ldx, plane_x;      // [pieces][M][ldx], K of each row
+  const unsigned short* W; int64_t ldw, plane_w;      // [pieces][N][ldw]
   int64_t M; int N, K;                                // K a multiple of 8, rows 16-byte aligned
   void* Y; int64_t ldy;
   const float* bias;
@@ -533,50 +532,56 @@ struct ProductParams {
   Segments g;
 };
 
-constexpr int kBK = 64;                               // numbers of a row in a step: 128 bytes
-// One operand's tile of R rows by kBK numbers in LDS: row r is 128 bytes = 8 units of 16, unit q at position q ^ (r / 2 % 8): the
-// sixteen lanes whose fragments LDS serves together (0-3, 12-15, 20-23, 24-27 and so on) then read from different banks (no
-// conflict counted).  Global memory goes to LDS directly, eight whole rows an instruction; the lane order of that copy is fixed,
-// so a lane asks for the unit that belongs at its position.
-template <int R, int NW>
+// One operand's tile of R rows by BK numbers in LDS.  BK = 64: row r is a line of 128 bytes, 8 units of 16, unit q at position
+// q ^ (r / 2 % 8); BK = 32: 64 bytes, 4 units, unit q at q ^ (r / 4 % 4).  The sixteen lanes whose fragments LDS serves together
+// (0-3, 12-15, 20-23, 24-27 and so on) then read from different banks (no conflict counted).  Global memory goes to LDS
+// directly, whole rows in neighbouring lanes; the lane order of that copy is fixed, so a lane asks for the unit that belongs at
+// its position.
+template <int BK>
+__device__ __forceinline__ int turned(int row, int unit) { return BK == 64 ? unit ^ ((row >> 1) & 7) : unit ^ ((row >> 2) & 3); }
+
+template <int R, int NW, int BK>
 struct RowTile {
-  static constexpr int BYTES = R * kBK * 2;
-  static constexpr int NLOAD = R / 8 / NW;
+  static constexpr int BYTES = R * BK * 2;
+  static constexpr int EACH = 512 / BK;              // rows of an instruction
+  static constexpr int NLOAD = R / EACH / NW;
+  static_assert(R % (EACH * NW) == 0, "whole instructions for every wavefront");
   unsigned goff[NLOAD];        // of this lane's unit, at step 0
   int k[NLOAD];                // the first number of the unit
+  static __device__ __forceinline__ int row(int j, int lane, int wave) { return (wave * NLOAD + j) * EACH + lane / (BK / 8); }
+  static __device__ __forceinline__ int first(int j, int lane, int wave) { return turned<BK>(row(j, lane, wave), lane % (BK / 8)) * 8; }
   __device__ __forceinline__ void init(int64_t ld, int lane, int wave) {
 #pragma unroll
     for (int j = 0; j < NLOAD; ++j) {
-      const int row = (wave * NLOAD + j) * 8 + (lane >> 3), unit = (lane & 7) ^ ((row >> 1) & 7);
-      k[j] = unit * 8;
-      goff[j] = (unsigned)(row * ld * 2) + (unsigned)unit * 16u;
+      k[j] = first(j, lane, wave);
+      goff[j] = (unsigned)((row(j, lane, wave) * ld + k[j]) * 2);
     }
   }
-  // Numbers k0 .. k0 + 63 of every row; units past K, and rows past the resource's end, arrive as zeros.
+  // Numbers k0 .. k0 + BK - 1 of every row; units past K, and rows past the resource's end, arrive as zeros.
   __device__ __forceinline__ void issue(__amdgpu_buffer_rsrc_t rsrc, lds_byte* tile, int k0, int K, int wave) const {
 #pragma unroll
     for (int j = 0; j < NLOAD; ++j)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(tile + (wave * NLOAD + j) * 1024), 16,
                                                k0 + k[j] < K ? goff[j] + (unsigned)k0 * 2u : 0x7FFFFFF0u, 0, 0, 0);
   }
-};
-// The same for numbers k0 .. k0 + 63 of the first `rows` rows of [rows][ld], K = ld, as zeros the rows outside lo .. hi - 1.
-template <int R, int NW>
-__device__ __forceinline__ void issue_rows(const unsigned short* base, int ld, int rows, int lo, int hi, lds_byte* tile, int k0,
-                                           int lane, int wave) {
-  const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(base, (unsigned)(rows * ld * 2));
-  constexpr int NLOAD = R / 8 / NW;
+  // The same of the first `rows` rows of [rows][ld], K = ld, as zeros the rows outside lo .. hi - 1.
+  static __device__ __forceinline__ void issue_some(const unsigned short* base, int ld, int rows, int lo, int hi, lds_byte* tile, int k0,
+                                                    int lane, int wave) {
+    const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(base, (unsigned)(rows * ld * 2));
 #pragma unroll
-  for (int j = 0; j < NLOAD; ++j) {
-    const int row = (wave * NLOAD + j) * 8 + (lane >> 3), k = k0 + ((lane & 7) ^ ((row >> 1) & 7)) * 8;
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(tile + (wave * NLOAD + j) * 1024), 16,
-                                             row >= lo && row < hi && k < ld ? (unsigned)(row * ld + k) * 2u : 0x7FFFFFF0u, 0, 0, 0);
+    for (int j = 0; j < NLOAD; ++j) {
+      const int r = row(j, lane, wave), at = k0 + first(j, lane, wave);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(tile + (wave * NLOAD + j) * 1024), 16,
+                                               r >= lo && r < hi && at < ld ? (unsigned)(r * ld + at) * 2u : 0x7FFFFFF0u, 0, 0, 0);
+    }
   }
-}
+};
 // The 16 bytes that a lane feeds to the matrix unit: row `row`, numbers 16 kc + 8 half ..
+template <int BK>
 __device__ __forceinline__ u32x4 fragment(const lds_byte* tile, int row, int kc, int half) {
-  return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(tile + row * 128 + (((kc * 2 + half) ^ ((row >> 1) & 7)) << 4));
+  return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(tile + row * BK * 2 + (turned<BK>(row, kc * 2 + half) << 4));
 }
+
 // Lays N instructions of the kinds in MASK (0x100 LDS reads, 0x20 loads) evenly among M of the matrix unit, instead of the
 // compiler's order, which reads fragments just before they are multiplied and waits for them.
 template <int MASK, int N, int M, int I = 0>
@@ -587,21 +592,24 @@ __device__ __forceinline__ void interleave() {
   if constexpr (I + 1 < M) interleave<MASK, N, M, I + 1>();
 }
 
-// BM x BN outputs by WM x WN wavefronts, each a block of 32 x 32 results TM x TN times.
-// S steps of the operands are in LDS: one is multiplied, the others are on their way.
-template <int OTYPE, int BM, int BN, int WM, int WN, int S>
+// BM x BN outputs by four wavefronts, each a block of 32 x 32 results TM x TN times.  S steps of BK numbers of the operands are in
+// LDS: one is multiplied, the others are on their way.  fp32 results: all three pieces of both operands are there together, and
+// their six products are formed from the same fragments (one product after the other, each with tiles of its own, read
+// twice as much: the whole call 777 x 1000 -> 1501 96 us, 71 so).
+template <int OTYPE, int BM, int BN, int BK, int S>
 __device__ __forceinline__ void product_tile(const ProductParams& p) {
-  constexpr int NW = WM * WN;
-  constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
-  typedef RowTile<BM, NW> OX;
-  typedef RowTile<BN, NW> OW;
-  // an array each, so that the compiler knows the stage that is read from those that are on their way
-  static_assert(TM * TN == 1 ? S == 8 : S == 2 || S == 4, "small tiles have eight stages, others two or four");
-  constexpr int STAGE = OX::BYTES + OW::BYTES, NL = OX::NLOAD + OW::NLOAD;
+  constexpr int NW = 4, WN = 2;
+  constexpr int TM = BM / 64, TN = BN / 64, NP = OTYPE == LSAM_DTYPE_FP32 ? 3 : 1, NC = BK / 16;
+  typedef RowTile<BM, NW, BK> OX;
+  typedef RowTile<BN, NW, BK> OW;
+  constexpr bool SMALL = NP == 1 && TM * TN == 1;
+  static_assert(SMALL ? S == 8 && NC == 4 : S >= 2 && S <= 4, "small tiles have eight stages, others two to four");
+  // an array for each stage, so that the compiler knows the one that is read from those that are on their way
+  constexpr int PART_W = NP * OX::BYTES, STAGE = NP * (OX::BYTES + OW::BYTES), NL = NP * (OX::NLOAD + OW::NLOAD);
   __shared__ __attribute__((aligned(1024))) unsigned char st0[STAGE];
   __shared__ __attribute__((aligned(1024))) unsigned char st1[STAGE];
   __shared__ __attribute__((aligned(1024))) unsigned char st2[S > 2 ? STAGE : 16];
-  __shared__ __attribute__((aligned(1024))) unsigned char st3[S > 2 ? STAGE : 16];
+  __shared__ __attribute__((aligned(1024))) unsigned char st3[S > 3 ? STAGE : 16];
   __shared__ __attribute__((aligned(1024))) unsigned char st4[S > 4 ? STAGE : 16];
   __shared__ __attribute__((aligned(1024))) unsigned char st5[S > 4 ? STAGE : 16];
   __shared__ __attribute__((aligned(1024))) unsigned char st6[S > 4 ? STAGE : 16];
@@ -640,41 +648,48 @@ __device__ __forceinline__ void product_tile(const ProductParams& p) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-  u32x4 fx[2][TM], fw[2][TN];
+  // A chunk is 16 numbers of the contraction.
+  u32x4 fx[2][NP][TM], fw[2][NP][TN];
   auto read = [&](const lds_byte* tile, int kc, int buf) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) fx[buf][i] = fragment(tile, wm + i * 32 + l32, kc, half);
+    for (int q = 0; q < NP; ++q) {
 #pragma unroll
-    for (int j = 0; j < TN; ++j) fw[buf][j] = fragment(tile + OX::BYTES, wn + j * 32 + l32, kc, half);
+      for (int i = 0; i < TM; ++i) fx[buf][q][i] = fragment<BK>(tile + q * OX::BYTES, wm + i * 32 + l32, kc, half);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) fw[buf][q][j] = fragment<BK>(tile + PART_W + q * OW::BYTES, wn + j * 32 + l32, kc, half);
+    }
   };
+  constexpr int PAIRS = NP == 3 ? 6 : 1;
   auto multiply_chunk = [&](int buf) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
+    for (int q = 0; q < PAIRS; ++q) {
+      const unsigned px = NP == 3 ? (kSixLeft >> (4 * q)) & 15u : 0u, pw = NP == 3 ? (kSixRight >> (4 * q)) & 15u : 0u;
 #pragma unroll
-      for (int j = 0; j < TN; ++j) acc[i][j] = mfma32(fw[buf][j], fx[buf][i], acc[i][j]);
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = mfma32(fw[buf][pw][j], fx[buf][px][i], acc[i][j]);
+    }
   };
 
-  // Steps: the products of planes one after the other, each over all of K.  S - 1 steps are on their way while one is
-  // multiplied; behind the last one zeros are, which add nothing, so that the loop runs in whole rounds of the stages and the
-  // loads to wait for are as many in every step.
-  const int steps = p.products * ((p.K + kBK - 1) / kBK);
-  int next_k = 0, next_q = 0;
+  // S - 1 steps are on their way while one is multiplied; behind the last one zeros are, which add nothing, so that the loop
+  // runs in whole rounds of the stages and the loads to wait for are as many in every step.
+  const int steps = (p.K + BK - 1) / BK;
+  int next_k = 0;
   auto request = [&](lds_byte* tile) {
-    const bool some = next_q < p.products;
-    const unsigned px = p.products > 1 && some ? (kSixLeft >> (4 * next_q)) & 15u : 0u;
-    const unsigned pw = p.products > 1 && some ? (kSixRight >> (4 * next_q)) & 15u : 0u;
-    const int k0 = some ? next_k : p.K;
-    ox.issue(make_rsrc(X + px * p.plane_x, bytes_x), tile, k0, p.K, wave);
-    ow.issue(make_rsrc(W + pw * p.plane_w, bytes_w), tile + OX::BYTES, k0, p.K, wave);
-    next_k += kBK;
-    if (next_k >= p.K) { next_k = 0; ++next_q; }
+#pragma unroll
+    for (int q = 0; q < NP; ++q) {
+      ox.issue(make_rsrc(X + q * p.plane_x, bytes_x), tile + q * OX::BYTES, next_k, p.K, wave);
+      ow.issue(make_rsrc(W + q * p.plane_w, bytes_w), tile + PART_W + q * OW::BYTES, next_k, p.K, wave);
+    }
+    next_k = next_k < p.K ? next_k + BK : p.K;
   };
   request(a0);
   request(a1);
-  if constexpr (S > 2) { request(a2); request(a3); }
+  if constexpr (S > 2) request(a2);
+  if constexpr (S > 3) request(a3);
   if constexpr (S > 4) { request(a4); request(a5); request(a6); request(a7); }
   arrived<(S - 1) * NL>();
-  if constexpr (TM * TN == 1) {
+  if constexpr (SMALL) {
     // One block of results a wavefront: too little to multiply while a fragment comes from LDS.  All of the next step's
     // fragments are read while this one's are multiplied, into two sums, so that they do not wait for each other.
     u32x4 gx[2][4], gw[2][4];
@@ -684,8 +699,8 @@ __device__ __forceinline__ void product_tile(const ProductParams& p) {
     auto read_all = [&](const lds_byte* tile, int buf) {
 #pragma unroll
       for (int kc = 0; kc < 4; ++kc) {
-        gx[buf][kc] = fragment(tile, wm + l32, kc, half);
-        gw[buf][kc] = fragment(tile + OX::BYTES, wn + l32, kc, half);
+        gx[buf][kc] = fragment<BK>(tile, wm + l32, kc, half);
+        gw[buf][kc] = fragment<BK>(tile + PART_W, wn + l32, kc, half);
       }
     };
     read_all(a0, 0);
@@ -714,21 +729,18 @@ __device__ __forceinline__ void product_tile(const ProductParams& p) {
   } else {
     read(a0, 0, 0);
     auto step = [&](lds_byte* now, lds_byte* then) {
-      read(now, 1, 1);
-      multiply_chunk(0);
-      interleave<0x100, TM + TN, TM * TN>();
-      read(now, 2, 0);
-      multiply_chunk(1);
-      interleave<0x100, TM + TN, TM * TN>();
-      read(now, 3, 1);
-      multiply_chunk(0);
-      interleave<0x100, TM + TN, TM * TN>();
+#pragma unroll
+      for (int c = 0; c + 1 < NC; ++c) {
+        read(now, c + 1, (c + 1) & 1);
+        multiply_chunk(c & 1);
+        interleave<0x100, NP * (TM + TN), PAIRS * TM * TN>();
+      }
       // Every wavefront has taken its last fragment of this step, and the next one has arrived.
       arrived<(S - 2) * NL>();
       request(now);
       read(then, 0, 0);                    // behind the last step: never multiplied
-      multiply_chunk(1);
-      interleave<0x120, TM + TN + NL, TM * TN>();
+      multiply_chunk((NC - 1) & 1);
+      interleave<0x120, NP * (TM + TN) + NL, PAIRS * TM * TN>();
     };
     for (int s = 0; s < steps; s += S) {
       step(a0, a1);
@@ -736,8 +748,12 @@ __device__ __forceinline__ void product_tile(const ProductParams& p) {
         step(a1, a0);
       } else {
         step(a1, a2);
-        step(a2, a3);
-        step(a3, a0);
+        if constexpr (S == 3) {
+          step(a2, a0);
+        } else {
+          step(a2, a3);
+          step(a3, a0);
+        }
       }
     }
   }
@@ -755,24 +771,30 @@ __device__ __forceinline__ void product_tile(const ProductParams& p) {
     const unsigned short* const q = p.Q + ((int64_t)a * p.N + n0) * p.low_k;
     auto request_low = [&](lds_byte* tile, int k0) {
       if (k0 >= p.low_k) return;
-      issue_rows<BM, NW>(u, p.low_k, (int)m_here, lo, hi, tile, k0, lane, wave);
-      issue_rows<BN, NW>(q, p.low_k, n_here, 0, n_here, tile + OX::BYTES, k0, lane, wave);
+      OX::issue_some(u, p.low_k, (int)m_here, lo, hi, tile, k0, lane, wave);
+      OW::issue_some(q, p.low_k, n_here, 0, n_here, tile + PART_W, k0, lane, wave);
     };
     auto multiply_low = [&](const lds_byte* tile, int k0) {
 #pragma unroll
-      for (int kc = 0; kc < 4; ++kc) {
+      for (int kc = 0; kc < NC; ++kc) {
         if (k0 + kc * 16 < p.low_k) {
-          read(tile, kc, 0);
-          multiply_chunk(0);
+#pragma unroll
+          for (int i = 0; i < TM; ++i) fx[0][0][i] = fragment<BK>(tile, wm + i * 32 + l32, kc, half);
+#pragma unroll
+          for (int j = 0; j < TN; ++j) fw[0][0][j] = fragment<BK>(tile + PART_W, wn + j * 32 + l32, kc, half);
+#pragma unroll
+          for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = mfma32(fw[0][0][j], fx[0][0][i], acc[i][j]);
         }
       }
     };
-    for (int k0 = 0; k0 < p.low_k; k0 += 2 * kBK) {
+    for (int k0 = 0; k0 < p.low_k; k0 += 2 * BK) {
       request_low(a0, k0);
-      request_low(a1, k0 + kBK);
+      request_low(a1, k0 + BK);
       arrived<0>();
       multiply_low(a0, k0);
-      multiply_low(a1, k0 + kBK);
+      multiply_low(a1, k0 + BK);
       arrived<0>();
     }
   }
@@ -829,9 +851,9 @@ __device__ __forceinline__ void product_tile(const ProductParams& p) {
   }
 }
 
-template <int OTYPE, int BM, int BN, int WM, int WN, int S>
-__global__ __launch_bounds__(WM * WN * 64) void product_kernel(ProductParams p) {
-  product_tile<OTYPE, BM, BN, WM, WN, S>(p);
+template <int OTYPE, int BM, int BN, int BK, int S>
+__global__ __launch_bounds__(256) void product_kernel(ProductParams p) {
+  product_tile<OTYPE, BM, BN, BK, S>(p);
 }
 
 // ---- y or dx, at most 64 rows -----------------------------------------------------------------------
@@ -1125,20 +1147,27 @@ LowRank low_rank(const lsam_adapter_desc* d) {
 }
 
 // Offsets in the workspace: copies of x or dy and of W, of u and of the adapters, marks, adapters of rows, du.
-struct Layout { size_t x, w, u, q, odd, adapter, du, total; bool tiles; };
+//
+// Few rows of one forward call go to few_rows_kernel, whose workgroups each read all of x from L2 for 16 outputs, or, where that
+// costs more than the further launch for the adapters' copies, to product_kernel in tiles of 64 x 64: bf16, 4096 -> 4096,
+// 20 us against 28 for 16 rows and 27 against 30 for 64; 4096 -> 14336 40 against 35 and 82 against 36; 14336 -> 4096 51 against
+// 64 for 64 rows.  Only if x and W go to LDS as they lie: a copy of W would cost more than it brings (fp32, 4096 -> 4096: 58
+// against 113 us for 16 rows, 115 against 127 for 64).
+struct Layout { size_t x, w, u, q, odd, adapter, du, total; bool tiles, copies; };
 Layout layout(const lsam_adapter_desc* d, bool backward) {
   Layout l;
   const int N = backward ? d->in : d->out;
-  l.tiles = backward || d->rows > kFewRows;
+  l.copies = backward || d->rows > kFewRows;
+  l.tiles = l.copies || (d->dtype == LSAM_DTYPE_BF16 && (int64_t)N * (d->rows > 32 ? (d->rows + 15) / 16 : 2) > 16384);
   l.x = 0;
-  l.w = l.x + (l.tiles ? planes_bytes(d->rows, backward ? d->out : d->in, d->dtype) : 0);
+  l.w = l.x + (l.copies ? planes_bytes(d->rows, backward ? d->out : d->in, d->dtype) : 0);
   // the backward pass reads W transposed
-  l.u = l.w + (backward ? planes_bytes(d->in, d->out, d->dtype) : l.tiles ? planes_bytes(d->out, d->in, d->dtype) : 0);
+  l.u = l.w + (backward ? planes_bytes(d->in, d->out, d->dtype) : l.copies ? planes_bytes(d->out, d->in, d->dtype) : 0);
   const size_t low_k = (size_t)low_rank(d).k();
   l.q = l.u + (l.tiles ? up256((size_t)d->rows * low_k * 2) : 0);
   l.odd = l.q + (l.tiles ? up256((size_t)d->adapters * N * low_k * 2) : 0);
   l.adapter = l.odd + (l.tiles ? up256((size_t)d->adapters * N) : 0);
-  l.du = l.adapter + (l.tiles ? 0 : up256((size_t)d->rows * 4));
+  l.du = l.adapter + (l.copies ? 0 : up256((size_t)d->rows * 4));
   l.total = l.du + (backward ? up256((size_t)d->rows * d->rank * 4) : 0);
   return l;
 }
@@ -1245,19 +1274,31 @@ void launch_planes_any(const void* src, int64_t stride, int64_t rows, int cols, 
   else launch_planes<LSAM_DTYPE_FP32>(src, stride, rows, cols, transpose, dst, s);
 }
 
-template <int OTYPE, int BM, int BN, int WM, int WN, int S>
+template <int OTYPE, int BM, int BN, int BK, int S>
 void launch_product_tile(ProductParams p, hipStream_t s) {
   p.tilesM = (int)((p.M + BM - 1) / BM);
   p.tilesN = (p.N + BN - 1) / BN;
-  product_kernel<OTYPE, BM, BN, WM, WN, S><<<(unsigned)p.tilesM * (unsigned)p.tilesN, WM * WN * 64, 0, s>>>(p);
+  product_kernel<OTYPE, BM, BN, BK, S><<<(unsigned)p.tilesM * (unsigned)p.tilesN, 256, 0, s>>>(p);
 }
-// Large tiles reuse what they read most; smaller ones where large ones would leave units idle.
-template <int OTYPE>
-void launch_product(const ProductParams& p, hipStream_t s) {
-  auto tiles = [&](int64_t b) { return ((p.M + b - 1) / b) * ((p.N + b - 1) / b); };
-  if (tiles(256) >= 224) launch_product_tile<OTYPE, 256, 256, 2, 2, 2>(p, s);
-  else if (tiles(128) >= 160) launch_product_tile<OTYPE, 128, 128, 2, 2, 4>(p, s);
-  else launch_product_tile<OTYPE, 64, 64, 2, 2, 8>(p, s);
+// Large tiles reuse what they read most, and are taken where they still fill the 256 units; the smaller ones where the next
+// larger would leave units idle.  Whole calls, us, in tiles of 256 / 128 / 64 a side, bf16: 16384 x 4096 -> 4096 505 / 647 / 1042,
+// 4096 x 2048 -> 3584 (224 tiles of 256) 81 / 107 / 152, 2048 x 2048 -> 3584 (112 of 256, 448 of 128) 73 / 57 / 83,
+// 1024 x 2048 -> 1024 (64 of 128) 67 / 33 / 23, and 64 x 4096 -> 65536, whose tiles of 256 are mostly empty, 170 in those and
+// 156 in tiles of 64.  fp32: 4096 x 4096 -> 4096 819 in tiles of 256 x 128, 868 of 128 x 128; 2048 x 2048 -> 2048 141 of
+// 128 x 128, 164 of 128 x 64, 184 of 64 x 64; 777 x 1000 -> 1501 85 of 128 x 128, 71 of 128 x 64, 81 of 64 x 64 (312 tiles: a
+// second round for 56 of them); 1024 x 1024 -> 1024 60 of 128 x 64, 53 of 64 x 64.
+void launch_product(const ProductParams& p, int dtype, hipStream_t s) {
+  auto tiles = [&](int64_t m, int64_t n) { return ((p.M + m - 1) / m) * ((p.N + n - 1) / n); };
+  if (dtype == LSAM_DTYPE_BF16) {
+    if (p.M > 128 && tiles(256, 256) >= 224) launch_product_tile<LSAM_DTYPE_BF16, 256, 256, 64, 2>(p, s);
+    else if (tiles(128, 128) >= 160) launch_product_tile<LSAM_DTYPE_BF16, 128, 128, 64, 4>(p, s);
+    else launch_product_tile<LSAM_DTYPE_BF16, 64, 64, 64, 8>(p, s);
+  } else {
+    if (tiles(64, 64) <= 256) launch_product_tile<LSAM_DTYPE_FP32, 64, 64, 32, 3>(p, s);
+    else if (tiles(128, 64) <= 256) launch_product_tile<LSAM_DTYPE_FP32, 128, 64, 32, 3>(p, s);
+    else if (p.M <= 128 || tiles(256, 128) < 448) launch_product_tile<LSAM_DTYPE_FP32, 128, 128, 32, 3>(p, s);
+    else launch_product_tile<LSAM_DTYPE_FP32, 256, 128, 32, 2>(p, s);
+  }
 }
 
 template <int DTYPE, int QTYPE, int RT>
@@ -1307,7 +1348,7 @@ void run_product(const Product& o, hipStream_t s) {
   unsigned short* const ws_x = reinterpret_cast<unsigned short*>(o.ws + o.l.x);
   unsigned short* const ws_w = reinterpret_cast<unsigned short*>(o.ws + o.l.w);
   const int64_t ld = up8(o.K);
-  if (d->rows <= kFewRows && !o.transposed) {
+  if (!o.l.tiles) {
     FewRowsParams p;
     p.X = o.X; p.ldx = o.x_stride; p.W = o.W; p.ldw = d->w_stride;
     p.M = (int)d->rows; p.N = o.N; p.K = o.K; p.Y = o.Y; p.ldy = o.y_stride; p.bias = o.bias; p.u = o.u; p.scale = o.scale;
@@ -1331,7 +1372,6 @@ void run_product(const Product& o, hipStream_t s) {
     p.W = ws_w; p.ldw = ld; p.plane_w = o.N * ld;
   }
   p.K = (int)ld;                                      // where that is more than K, both are copies, padded with zeros
-  p.products = d->dtype == LSAM_DTYPE_BF16 ? 1 : 6;
   p.Y = o.Y; p.ldy = o.y_stride; p.bias = o.bias; p.g = o.g;
   const LowRank low = low_rank(d);
   p.low_k = low.k();
@@ -1345,8 +1385,7 @@ void run_product(const Product& o, hipStream_t s) {
     if (d->adapter_dtype == LSAM_DTYPE_BF16) copies_kernel<LSAM_DTYPE_BF16><<<grid, 256, 0, s>>>(c);
     else copies_kernel<LSAM_DTYPE_FP32><<<grid, 256, 0, s>>>(c);
   }
-  if (d->dtype == LSAM_DTYPE_BF16) launch_product<LSAM_DTYPE_BF16>(p, s);
-  else launch_product<LSAM_DTYPE_FP32>(p, s);
+  launch_product(p, d->dtype, s);
 }
 
 Segments segments(const lsam_adapter_desc* d, const int32_t* begin, const int32_t* which) {
@@ -1390,9 +1429,10 @@ extern "C" int lsam_adapter(const lsam_adapter_desc* d, const void* x, const voi
       {"y", y, extent(1, 0, d->rows, d->y_stride, d->out, b), b, true, 0, 0}};
   rc = check_args(args, sizeof args / sizeof args[0], "adapter");
   if (rc != LSAM_OK) return rc;
-  const Layout l = layout(d, false);
+  Layout l = layout(d, false);
   rc = check_workspace(l.total, workspace, workspace_bytes, "adapter");
   if (rc != LSAM_OK) return rc;
+  if (!l.copies && !(straight(x, d->x_stride, d->in, d->dtype) && straight(W, d->w_stride, d->in, d->dtype))) l.tiles = false;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const Segments g = segments(d, seg_begin, seg_adapter);
   const LowRank low = low_rank(d);

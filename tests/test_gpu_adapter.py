@@ -122,6 +122,17 @@ def test_every_size_of_tile(dtype, atype):
         check(x, W, A, B, bias, dy, [0, rows // 3, rows // 2 + 1, rows], [2, 0, 1])
 
 
+@pytest.mark.parametrize("rows,inp,out", [(1, 40, 8400), (33, 72, 9001), (64, 64, 4112), (17, 41, 8400), (5, 48, 60000)])
+def test_few_rows_of_many_outputs(rows, inp, out):
+    x, W, A, B, bias, dy = make(rows, inp, out, 12, 3, B16, F32, seed=rows, bias=True)
+    check(x, W, A, B, bias, dy, [0, rows // 2, rows], [2, 0])
+
+
+def test_tiles_that_are_not_square():
+    x, W, A, B, bias, dy = make(1100, 100, 1200, 16, 3, F32, F32, seed=1100, bias=True)
+    check(x, W, A, B, bias, dy, [0, 400, 777, 1100], [2, 0, 1])
+
+
 @pytest.mark.parametrize("dtype", [F32, B16])
 def test_long_contractions_and_many_rows_of_one_adapter(dtype):
     check(*make(1, 9000, 24, 8, 1, dtype, F32, seed=1), [0, 1], [0])
