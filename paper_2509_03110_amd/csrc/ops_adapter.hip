@@ -402,7 +402,9 @@ template <int DTYPE, int ATYPE, bool UNIT, int NR, int RT>
 constexpr int kShrinkWaves = waves_for(kStageBytes<ATYPE, DTYPE, UNIT, NR, RT>);
 
 // Workgroup (tile, j): the j-th, j + gridDim.y-th, ... segment of the tile's 16 RT rows, the contraction cut over its wavefronts.
-// Bound by reading x where segments are long, by reading A where each row has its own.  UNIT: the contraction is contiguous in A.
+// Bound by reading x where segments are long (16384 x 4096 bf16, 134 MB, rank 16 with fp32 adapters, whose pieces the vector
+// units cut: 42 us, 3.2 TB/s), by reading A where each row has its own (32 rows of 32 adapters, 4096 -> rank 16: 7 us, half of it
+// the wait for the segments and then the first rows).  UNIT: the contraction is contiguous in A.
 template <int DTYPE, int ATYPE, bool UNIT, int NR, int RT, int WAVES, bool STAGED>
 __global__ __launch_bounds__(WAVES * 64) void shrink_kernel(ShrinkParams p) {
   typedef typename Value<DTYPE>::T T;
@@ -487,7 +489,7 @@ struct CopiesParams {
   LowRank low;
 };
 // An infinity or NaN in an adapter would reach the rows of other segments in its tile, whose 0 it is multiplied with: it is left
-// out here, and the outputs it belongs to are marked.
+// out here, and the outputs it belongs to are marked.  16 adapters of 8192 x 32 in bf16 15 us.
 template <int QTYPE>
 __global__ __launch_bounds__(256) void copies_kernel(CopiesParams p) {
   typedef typename Value<QTYPE>::T TQ;
@@ -596,6 +598,9 @@ __device__ __forceinline__ void interleave() {
 // LDS: one is multiplied, the others are on their way.  fp32 results: all three pieces of both operands are there together, and
 // their six products are formed from the same fragments (one product after the other, each with tiles of its own, read
 // twice as much: the whole call 777 x 1000 -> 1501 96 us, 71 so).
+// 16384 x 4096 -> 4096 bf16 500-535 us (1.03-1.1 PFLOP/s; a library's product of 8192 a side reaches 1.33, the matrix units alone
+// 2.08): bound by the power that products of random numbers draw -- rings of smaller steps, other orders of the loads and
+// of the fragments all measured the same, and zeros run at 1.5.  fp32 4096 x 4096 -> 4096: 0.98 PFLOP/s of its pieces.
 template <int OTYPE, int BM, int BN, int BK, int S>
 __device__ __forceinline__ void product_tile(const ProductParams& p) {
   constexpr int NW = 4, WN = 2;
@@ -871,7 +876,8 @@ struct FewRowsParams {
 constexpr int kFewRows = 64;
 constexpr int kHead = 16;                             // ranks that are read ahead
 
-// A workgroup's 16 outputs, the contraction cut over its wavefronts.  Bound by reading W.
+// A workgroup's 16 outputs, the contraction cut over its wavefronts.  Bound by reading W, each workgroup's share of it in one go, and
+// by x, which every workgroup reads from L2: 32 rows, 4096 -> 4096 bf16, 34 MB, 13-14 us (2.5 TB/s).
 template <int DTYPE, int RT>
 constexpr int kFewWaves = waves_for(kStageBytes<DTYPE, DTYPE, true, 1, RT>);
 
@@ -958,7 +964,8 @@ struct GradsParams {
 constexpr int kGradWaves = 8;
 
 // G[c][r] = scale sum_t V[t][c] S[t][r] over the rows t of an adapter's segments: 64 columns of one adapter a workgroup, whose
-// wavefronts take 32 rows each in turn.  Bound by reading V.  The matrix unit wants eight successive t of a column in a
+// wavefronts take 32 rows each in turn.  Bound by reading V: 16384 rows of 4096 + 4096 columns bf16, 268 MB, 57-59 us (4.6 TB/s;
+// the whole call 75 us with 8 wavefronts, 90 with 4, 100 with 16).  The matrix unit wants eight successive t of a column in a
 // lane: a lane loads four neighbouring columns of eight rows and deals them out.
 template <int DTYPE, int NR>
 __global__ __launch_bounds__(kGradWaves * 64) void grads_kernel(GradsParams p) {
@@ -1058,6 +1065,8 @@ struct PlanesParams {
   const void* src; int64_t stride; int64_t rows; int cols;
   unsigned short* dst; int64_t ld, plane;              // [pieces][rows][ld], or transposed [pieces][cols][ld]; ld a multiple of 8
 };
+// The matrix unit wants numbers along the contraction side by side; W of the backward pass has them a row apart: 64 x 64 numbers
+// turn in LDS, whole lines in and out.  Bound by memory: 4096 x 4096 bf16, 67 MB, 15 us (4.5 TB/s).
 template <int DTYPE, bool TRANSPOSE>
 __global__ __launch_bounds__(256) void planes_kernel(PlanesParams p) {
   typedef typename Value<DTYPE>::T T;
@@ -1218,10 +1227,12 @@ void launch_shrink_tile(const ShrinkParams& p, dim3 grid, bool staged, hipStream
 }
 template <int DTYPE, int ATYPE, bool UNIT, int NR>
 void launch_shrink_rank(const ShrinkParams& p, hipStream_t s) {
-  // Tiles of 64 rows read the adapter least often; of 32 or 16 rows where those leave units idle or segments are short.
+  // Tiles of 64 rows read the adapter least often; of 32 or 16 rows where those leave units idle or segments are short.  Calls
+  // with 8 outputs, 4096 -> rank 16 in fp32 adapters, us in tiles of 64 / 32 / 16 rows: 16384 rows 59 / 72 / 99, 8191 47 / 57 / 73,
+  // 6144 44 / 41 / 55, 4096 44 / 39 / 40, 1024 42 / 36 / 36; 1024 rows of 512 segments 77 / 73 / 70.
   const bool brief = p.rows <= 16ll * p.g.n;
   constexpr bool ROOM = 2 * 2 * kStageBytes<ATYPE, DTYPE, UNIT, NR, 4> <= kRoom;      // for two stages of two wavefronts
-  const int64_t rows = ROOM && !brief && p.rows >= 64 * 256 ? 64 : !brief && p.rows >= 32 * 192 ? 32 : 16;
+  const int64_t rows = ROOM && !brief && p.rows >= 64 * 112 ? 64 : !brief && p.rows >= 32 * 192 ? 32 : 16;
   const int64_t tiles = (p.rows + rows - 1) / rows;
   int64_t y = p.g.n / tiles + 2;                      // two segments meet in many a tile: a workgroup for each
   y = y > 64 ? 64 : y > p.g.n ? (p.g.n > 0 ? p.g.n : 1) : y;

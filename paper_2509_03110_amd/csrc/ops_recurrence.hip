@@ -16,11 +16,16 @@
 namespace lsam {
 namespace {
 
-constexpr int kRows = 16;            // rows of a tile that one wavefront takes
+// Rows of a tile that one wavefront takes, and wavefronts of a workgroup (one where sequences are no longer than its rows).
+// 8 x 4096 x 2048 bf16 forward and backward take 252 us with 16 rows and 8 wavefronts, 318 with 8 rows, 289 with 8 rows and 16
+// wavefronts, 456 with 16 and 16 (too few registers); a tile more on its way 250, at twice the registers.
+constexpr int kRows = 16;
+constexpr int kWaves = 8;
 constexpr int kChannels = 64;        // of a workgroup: one for each lane
-constexpr int kWaves = 8;            // of a workgroup; one where sequences are no longer than its rows
 constexpr int kMaxSplits = 64;
-constexpr int kTogether = 8;         // workgroups of neighbouring channels that share an XCD
+// Workgroups of neighbouring channels that share an XCD.  4 x 2000 x 1001 fp32 36 us against 44 where each is on its own,
+// 8 x 4096 x 1001 bf16 70 against 100; no difference where rows begin on lines; 4 and 16 as 8.
+constexpr int kTogether = 8;
 
 struct Tensor { const void* p; int64_t stride, seq; };
 
@@ -129,6 +134,9 @@ __device__ __forceinline__ Place place(const RecurrenceParams& p) {
 }
 
 // RUNS: only (A, H) of the workgroup's run, for a launch that follows.
+// Bound by memory and, with one workgroup on a unit, by how much of it is on its way: 8 x 4096 x 2048 bf16, 403 MB, 101-105 us
+// (3.9 TB/s, the vector units half busy); 131073 x 1000 fp32 in runs, 1.05 GB read for the runs in 220 us and 1.57 GB in 340 us
+// (4.7 TB/s), rows of 4000 bytes that do not begin on lines.
 template <int DTYPE, int NW, bool RUNS>
 __global__ __launch_bounds__(NW * 64) void recurrence_kernel(RecurrenceParams p) {
   typedef typename Value<DTYPE>::T T;
@@ -212,6 +220,8 @@ __global__ __launch_bounds__(NW * 64) void recurrence_kernel(RecurrenceParams p)
 }
 
 // RUNS: only (A, E) of the workgroup's run.
+// 8 x 4096 x 2048 bf16, 671 MB, 153 us (4.4 TB/s); 131073 x 1000 fp32, 1.05 GB for the runs in 230 us and 2.62 GB in 545 us
+// (4.8 TB/s).
 template <int DTYPE, int NW, bool RUNS>
 __global__ __launch_bounds__(NW * 64) void recurrence_grad_kernel(RecurrenceParams p) {
   typedef typename Value<DTYPE>::T T;
@@ -321,7 +331,7 @@ __global__ __launch_bounds__(NW * 64) void recurrence_grad_kernel(RecurrencePara
   }
 }
 
-// One step of every sequence (generation): eight channels a lane.  Bound by the launch: 64 x 4096 take 4 us, 9.7 where
+// One step of every sequence (generation): eight channels a lane.  Bound by the launch: 64 x 4096 take 3.2 us, 9.7 where
 // workgroups of one wavefront walk tiles of which one row is there.
 template <int DTYPE>
 __global__ __launch_bounds__(256) void recurrence_step_kernel(RecurrenceParams p) {
@@ -369,7 +379,8 @@ __global__ __launch_bounds__(256) void recurrence_step_kernel(RecurrenceParams p
 
 // How a call is cut.  One wavefront where sequences are no longer than its rows (a step of generation).  Runs where
 // sequences times channels give fewer workgroups than there are units: all of one length, so that sequences of any lengths
-// fill the chip evenly, as many as give it kRunGroups workgroups, of at least four tiles each.
+// fill the chip evenly, as many as give it kRunGroups workgroups, of at least four tiles each (131073 x 1000 fp32, both directions:
+// 1340 us with 1024, 1350 with 2048; 1 x 32768 x 4096 bf16 forward 306, 309 with 512).
 constexpr int kRunGroups = 1024;
 struct Plan { int waves, splits, slabs; int64_t run_tiles, tiles_of_each, states; };
 Plan plan(const lsam_recurrence_desc* d) {
