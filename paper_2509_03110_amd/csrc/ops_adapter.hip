@@ -386,6 +386,52 @@ __device__ __forceinline__ void contract_straight(const Rows<LTYPE>& left, const
   }
 }
 
+// The segments of a tile's rows, `step` numbers of the low-rank part at a time.  The next 64 segments are held a lane each.
+struct SegmentsOf {
+  const Segments& g;
+  int m0, m_here, low_k, step;
+  int64_t rows;
+  int window, i, begins, adapters;
+  int lo, hi, a, k0;                                   // rows of the tile, adapter, first number
+  bool done;
+  __device__ __forceinline__ SegmentsOf(const Segments& g_, int64_t m0_, int m_here_, int64_t rows_, int low_k_, int step_)
+      : g(g_), m0((int)m0_), m_here(m_here_), low_k(low_k_), step(step_), rows(rows_), i(0), k0(low_k_), done(g_.n == 0) {
+    const int found = done ? 0 : seg_at(g, m0_);
+    window = found < 0 ? 0 : found;
+    if (!done) load();
+  }
+  __device__ __forceinline__ void load() {
+    const int s = window + (int)(threadIdx.x & 63);
+    begins = (int)seg_row(g, s < g.n ? s : g.n, rows);
+    adapters = s < g.n ? seg_adapter(g, s) : -1;
+  }
+  __device__ __forceinline__ bool next() {
+    if (done) return false;
+    k0 += step;
+    if (k0 < low_k) return true;
+    while (true) {
+      if (i == 63) {
+        window += 63;
+        i = 0;
+        load();
+      }
+      const int l = __builtin_amdgcn_readlane(begins, i) - m0, h = __builtin_amdgcn_readlane(begins, i + 1) - m0;
+      if (window + i >= g.n || l >= m_here) {
+        done = true;
+        return false;
+      }
+      a = __builtin_amdgcn_readlane(adapters, i);
+      ++i;
+      lo = l > 0 ? l : 0;
+      hi = h < m_here ? h : m_here;
+      if (a >= 0 && lo < hi) {
+        k0 = 0;
+        return true;
+      }
+    }
+  }
+};
+
 // ---- u = x A^T, du = scale dy B ---------------------------------------------------------------------
 struct ShrinkParams {
   const void* x; int64_t x_stride;
@@ -401,10 +447,10 @@ struct ShrinkParams {
 template <int DTYPE, int ATYPE, bool UNIT, int NR, int RT>
 constexpr int kShrinkWaves = waves_for(kStageBytes<ATYPE, DTYPE, UNIT, NR, RT>);
 
-// Workgroup (tile, j): the j-th, j + gridDim.y-th, ... segment of the tile's 16 RT rows, the contraction cut over its wavefronts.
-// Bound by reading x where segments are long (16384 x 4096 bf16, 134 MB, rank 16 with fp32 adapters, whose pieces the vector
-// units cut: 42 us, 3.2 TB/s), by reading A where each row has its own (32 rows of 32 adapters, 4096 -> rank 16: 7 us, half of it
-// the wait for the segments and then the first rows).  UNIT: the contraction is contiguous in A.
+// Workgroup (tile, j, r): ranks 16 NR r and on of the j-th, j + groups-th, ... segment of the tile's 16 RT rows, the contraction
+// cut over its wavefronts.  Bound by reading x where segments are long (16384 x 4096 bf16, 134 MB, rank 16 with fp32 adapters,
+// whose pieces the vector units cut: 42 us, 3.2 TB/s), by reading A where each row has its own (32 rows of 32 adapters,
+// 4096 -> rank 16: 7 us, half of it the wait for the segments and then the first rows).  UNIT: the contraction is contiguous in A.
 template <int DTYPE, int ATYPE, bool UNIT, int NR, int RT, int WAVES, bool STAGED>
 __global__ __launch_bounds__(WAVES * 64) void shrink_kernel(ShrinkParams p) {
   typedef typename Value<DTYPE>::T T;
@@ -422,8 +468,10 @@ __global__ __launch_bounds__(WAVES * 64) void shrink_kernel(ShrinkParams p) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, quarter = lane >> 4;
   const int64_t row0 = (int64_t)blockIdx.x * ROWS, row1 = row0 + ROWS < p.rows ? row0 + ROWS : p.rows;
-  if (blockIdx.y == 0) {
-    // rows without an adapter
+  const int groups = (int)gridDim.y - 1, rank0 = (int)blockIdx.z * (NR * 16);
+  if ((int)blockIdx.y == groups) {
+    if (rank0 > 0) return;
+    // the last one: adapters of rows, and the rows without one (a search that the others need not wait for)
     for (int i = tid; i < ROWS; i += WAVES * 64) {
       if (row0 + i >= row1) break;
       const int a = row_adapter(p.g, p.g.begin, row0 + i, p.rows);
@@ -431,9 +479,10 @@ __global__ __launch_bounds__(WAVES * 64) void shrink_kernel(ShrinkParams p) {
       if (a < 0)
         for (int r = 0; r < p.rank; ++r) p.u[(row0 + i) * p.rank + r] = 0.f;
     }
+    return;
   }
   const int found = seg_at(p.g, row0);
-  for (int s = (found < 0 ? 0 : found) + (int)blockIdx.y; s < p.g.n; s += gridDim.y) {
+  for (int s = (found < 0 ? 0 : found) + (int)blockIdx.y; s < p.g.n; s += groups) {
     int64_t lo = seg_row(p.g, s, p.rows), hi = seg_row(p.g, s + 1, p.rows);
     if (lo >= row1) break;
     lo = lo > row0 ? lo : row0;
@@ -445,7 +494,8 @@ __global__ __launch_bounds__(WAVES * 64) void shrink_kernel(ShrinkParams p) {
     for (int t = 0; t < RT; ++t)
 #pragma unroll
       for (int r = 0; r < NR; ++r) acc[t][r] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const Rows<ATYPE> left{static_cast<const TA*>(p.A) + a * p.a_adapter, p.a_rank, p.a_k, p.rank};
+    const int ranks = p.rank - rank0 < NR * 16 ? p.rank - rank0 : NR * 16;
+    const Rows<ATYPE> left{static_cast<const TA*>(p.A) + a * p.a_adapter + rank0 * p.a_rank, p.a_rank, p.a_k, ranks};
     const Rows<DTYPE> x{static_cast<const T*>(p.x) + lo * p.x_stride, p.x_stride, 1, (int)(hi - lo)};
     if constexpr (STAGED)
       contract_staged<ATYPE, DTYPE, UNIT, NR, RT, WAVES>(left, x, p.K, wave, lane, (lds_byte*)st0 + wave * STAGE, (lds_byte*)st1 + wave * STAGE,
@@ -463,11 +513,11 @@ __global__ __launch_bounds__(WAVES * 64) void shrink_kernel(ShrinkParams p) {
           for (int i = 0; i < 4; ++i) part[wave][l16][r * 16 + quarter * 4 + i] = acc[t][r][i];
         __syncthreads();
         for (int i = tid; i < 16 * NR * 16; i += WAVES * 64) {
-          const int row = i / (NR * 16), r = i % (NR * 16);
+          const int row = i / (NR * 16), r = rank0 + i % (NR * 16);
           if (r < p.low.padded && lo + t * 16 + row < hi) {
             float sum = 0.f;
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) sum += part[w][row][r];
+            for (int w = 0; w < WAVES; ++w) sum += part[w][row][r - rank0];
             sum = r < p.rank ? p.scale * sum : 0.f;
             if (r < p.rank) p.u[(lo + t * 16 + row) * p.rank + r] = sum;
             if (p.copy)
@@ -764,44 +814,55 @@ __device__ __forceinline__ void product_tile(const ProductParams& p) {
   }
   arrived<0>();                          // nothing may still be on its way to LDS
 
-  // Every segment that rows of the tile belong to: the copies of u and of its adapter, rows of other segments being zeros.
-  const int found = seg_at(p.g, m0);
-  const int seg0 = found < 0 ? 0 : found;
-  for (int s = seg0; s < p.g.n; ++s) {
-    const int64_t l = seg_row(p.g, s, p.M) - m0, h = seg_row(p.g, s + 1, p.M) - m0;
-    if (l >= m_here) break;
-    const int lo = (int)(l > 0 ? l : 0), hi = (int)(h < m_here ? h : m_here), a = seg_adapter(p.g, s);
-    if (a < 0 || lo >= hi) continue;
-    const unsigned short* const u = p.u + m0 * p.low_k;
-    const unsigned short* const q = p.Q + ((int64_t)a * p.N + n0) * p.low_k;
-    auto request_low = [&](lds_byte* tile, int k0) {
-      if (k0 >= p.low_k) return;
-      OX::issue_some(u, p.low_k, (int)m_here, lo, hi, tile, k0, lane, wave);
-      OW::issue_some(q, p.low_k, n_here, 0, n_here, tile + PART_W, k0, lane, wave);
-    };
-    auto multiply_low = [&](const lds_byte* tile, int k0) {
+  // Every segment that rows of the tile belong to: the copies of u and of its adapter, rows of other segments being zeros.  BK
+  // numbers of them in each stage, then all stages are multiplied: many segments of few rows would wait one by one.
+  const unsigned short* const u = p.u + m0 * p.low_k;
+  auto multiply_low = [&](const lds_byte* tile, int k0) {
 #pragma unroll
-      for (int kc = 0; kc < NC; ++kc) {
-        if (k0 + kc * 16 < p.low_k) {
+    for (int kc = 0; kc < NC; ++kc) {
+      if (k0 + kc * 16 < p.low_k) {
 #pragma unroll
-          for (int i = 0; i < TM; ++i) fx[0][0][i] = fragment<BK>(tile, wm + i * 32 + l32, kc, half);
+        for (int i = 0; i < TM; ++i) fx[0][0][i] = fragment<BK>(tile, wm + i * 32 + l32, kc, half);
 #pragma unroll
-          for (int j = 0; j < TN; ++j) fw[0][0][j] = fragment<BK>(tile + PART_W, wn + j * 32 + l32, kc, half);
+        for (int j = 0; j < TN; ++j) fw[0][0][j] = fragment<BK>(tile + PART_W, wn + j * 32 + l32, kc, half);
 #pragma unroll
-          for (int i = 0; i < TM; ++i)
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = mfma32(fw[0][0][j], fx[0][0][i], acc[i][j]);
-        }
+          for (int j = 0; j < TN; ++j) acc[i][j] = mfma32(fw[0][0][j], fx[0][0][i], acc[i][j]);
       }
-    };
-    for (int k0 = 0; k0 < p.low_k; k0 += 2 * BK) {
-      request_low(a0, k0);
-      request_low(a1, k0 + BK);
-      arrived<0>();
-      multiply_low(a0, k0);
-      multiply_low(a1, k0 + BK);
-      arrived<0>();
     }
+  };
+  SegmentsOf walk(p.g, m0, (int)m_here, p.M, p.low_k, BK);
+  unsigned marks = 0;                    // whether any of their adapters has a number that is not finite
+  while (true) {
+    int k[S];
+    unsigned mark[S][BN / 64];
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      k[i] = -1;
+#pragma unroll
+      for (int j = 0; j < BN / 64; ++j) mark[i][j] = 0;
+      if (!walk.next()) continue;
+      lds_byte* const tile = i == 0 ? a0 : i == 1 ? a1 : i == 2 ? a2 : i == 3 ? a3 : i == 4 ? a4 : i == 5 ? a5 : i == 6 ? a6 : a7;
+      k[i] = walk.k0;
+      OX::issue_some(u, p.low_k, (int)m_here, walk.lo, walk.hi, tile, walk.k0, lane, wave);
+      OW::issue_some(p.Q + ((int64_t)walk.a * p.N + n0) * p.low_k, p.low_k, n_here, 0, n_here, tile + PART_W, walk.k0, lane, wave);
+      const unsigned char* const odd = p.odd + (int64_t)walk.a * p.N + n0;
+#pragma unroll
+      for (int j = 0; j < BN / 64; ++j) mark[i][j] = odd[j * 64 + lane < n_here ? j * 64 + lane : 0];
+    }
+    if (k[0] < 0) break;
+    arrived<0>();
+#pragma unroll
+    for (int i = 0; i < S; ++i)
+#pragma unroll
+      for (int j = 0; j < BN / 64; ++j) marks |= mark[i][j];
+#pragma unroll
+    for (int i = 0; i < S; ++i)
+      if (k[i] >= 0)
+        multiply_low(i == 0 ? a0 : i == 1 ? a1 : i == 2 ? a2 : i == 3 ? a3 : i == 4 ? a4 : i == 5 ? a5 : i == 6 ? a6 : a7, k[i]);
+    if (walk.done) break;
+    arrived<0>();
   }
 
   typedef Value<OTYPE> VO;
@@ -835,15 +896,14 @@ __device__ __forceinline__ void product_tile(const ProductParams& p) {
   }
 
   // Outputs that a number of their adapter's belongs to which is not finite: the lane that stored them says so.
-  for (int s = seg0; s < p.g.n; ++s) {
+  if (__ballot(marks != 0) == 0) return;
+  const int found = seg_at(p.g, m0);
+  for (int s = found < 0 ? 0 : found; s < p.g.n; ++s) {
     const int64_t l = seg_row(p.g, s, p.M) - m0, h = seg_row(p.g, s + 1, p.M) - m0;
     if (l >= m_here) break;
     const int a = seg_adapter(p.g, s);
     if (a < 0 || l >= h) continue;
     const unsigned char* odd = p.odd + (int64_t)a * p.N + n0;
-    bool some = false;
-    for (int n = lane; n < n_here; n += 64) some |= odd[n] != 0;
-    if (__ballot(some) == 0) continue;
     for (int i = 0; i < TM; ++i) {
       const int row = wm + i * 32 + l32;
       if (row < l || row >= h || row >= m_here) continue;
@@ -1236,7 +1296,7 @@ void launch_shrink_rank(const ShrinkParams& p, hipStream_t s) {
   const int64_t tiles = (p.rows + rows - 1) / rows;
   int64_t y = p.g.n / tiles + 2;                      // two segments meet in many a tile: a workgroup for each
   y = y > 64 ? 64 : y > p.g.n ? (p.g.n > 0 ? p.g.n : 1) : y;
-  const dim3 grid((unsigned)tiles, (unsigned)y);
+  const dim3 grid((unsigned)tiles, (unsigned)y + 1, (unsigned)(p.rank + NR * 16 - 1) / (NR * 16));
   const bool staged = whole_units(p.x, p.x_stride, p.K, DTYPE) &&
                       (!UNIT || (whole_units(p.A, p.a_rank, p.K, ATYPE) && p.a_adapter % (16 / dtype_bytes(ATYPE)) == 0));
   if constexpr (ROOM)
@@ -1244,17 +1304,21 @@ void launch_shrink_rank(const ShrinkParams& p, hipStream_t s) {
   if (rows == 32) launch_shrink_tile<DTYPE, ATYPE, UNIT, NR, 2>(p, grid, staged, s);
   else launch_shrink_tile<DTYPE, ATYPE, UNIT, NR, 1>(p, grid, staged, s);
 }
+// A workgroup has at most 32 ranks, which leaves LDS for more wavefronts to cut fp32's pieces; all 64 where there is nothing to
+// cut and many rows would be read twice.  Rank 64, 4096 numbers, calls with 8 outputs, us with 64 / 32 ranks a workgroup: 30 rows
+// fp32 121 / 72, bf16 24 / 22; 1024 rows fp32 154 / 99, bf16 34 / 31; 16384 rows fp32 441 / 499, bf16 with fp32 adapters 122 / 91,
+// bf16 63 / 88.
+template <int DTYPE, int ATYPE, bool UNIT>
+void launch_shrink_along(const ShrinkParams& p, hipStream_t s) {
+  if (p.rank <= 16) return launch_shrink_rank<DTYPE, ATYPE, UNIT, 1>(p, s);
+  if constexpr (DTYPE == LSAM_DTYPE_BF16 && ATYPE == LSAM_DTYPE_BF16)
+    if (p.rank > 32 && p.rows >= 64 * 112) return launch_shrink_rank<DTYPE, ATYPE, UNIT, 4>(p, s);
+  launch_shrink_rank<DTYPE, ATYPE, UNIT, 2>(p, s);
+}
 template <int DTYPE, int ATYPE>
 void launch_shrink(const ShrinkParams& p, hipStream_t s) {
-  if (p.a_k == 1) {
-    if (p.rank <= 16) launch_shrink_rank<DTYPE, ATYPE, true, 1>(p, s);
-    else if (p.rank <= 32) launch_shrink_rank<DTYPE, ATYPE, true, 2>(p, s);
-    else launch_shrink_rank<DTYPE, ATYPE, true, 4>(p, s);
-  } else {
-    if (p.rank <= 16) launch_shrink_rank<DTYPE, ATYPE, false, 1>(p, s);
-    else if (p.rank <= 32) launch_shrink_rank<DTYPE, ATYPE, false, 2>(p, s);
-    else launch_shrink_rank<DTYPE, ATYPE, false, 4>(p, s);
-  }
+  if (p.a_k == 1) launch_shrink_along<DTYPE, ATYPE, true>(p, s);
+  else launch_shrink_along<DTYPE, ATYPE, false>(p, s);
 }
 void launch_shrink_any(const ShrinkParams& p, int dtype, int atype, hipStream_t s) {
   if (dtype == LSAM_DTYPE_BF16) {

@@ -304,3 +304,18 @@ def test_refusals():
     assert none[0].shape == (0, 24)
     z = ops.adapter_backward(torch.zeros(0, 16, device=DEV), W, A, B, none[1], torch.zeros(0, 24, device=DEV), *segs([0], []), 1.0)
     assert bool((z[1] == 0).all()) and bool((z[2] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, B16])
+@pytest.mark.parametrize("rank", [33, 64])
+def test_large_ranks_of_many_rows(dtype, rank):
+    x, W, A, B, bias, dy = make(7300, 136, 72, rank, 2, dtype, dtype, seed=rank, bias=True)
+    check(x, W, A, B, bias, dy, [0, 3000, 3001, 7290], [1, 0, 1])
+
+
+@pytest.mark.parametrize("dtype", [F32, B16])
+def test_more_segments_than_lanes(dtype):
+    rows, n = 300, 620                                       # every second one empty: 128 in a tile of 64 rows
+    begin = [min(rows, i // 2) for i in range(n + 1)]
+    x, W, A, B, bias, dy = make(rows, 72, 104, 8, 7, dtype, F32, seed=n, bias=True)
+    check(x, W, A, B, bias, dy, begin, [i % 8 - 1 for i in range(n)])
