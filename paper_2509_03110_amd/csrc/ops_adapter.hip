@@ -8,7 +8,7 @@
 //   shrink_kernel   u or du: [rows, rank], 64 rows of one segment a workgroup, the long contraction cut over its wavefronts
 //   product_kernel  y or dx: tiles of W's product; then, for every segment that the tile's rows belong to, a few more steps
 //                   of the same loop over the pieces of u and B (or du and A), rows of other segments being zero
-//   few_rows_kernel y or dx where there are at most 64 rows: reads W once, 16 outputs a workgroup, no tile of x
+//   few_rows_kernel y or dx where there are at most 64 rows: reads W once, 16 outputs a workgroup, no tile of x, no copy of W
 //   grads_kernel    dA = sum du^T x and dB = scale sum dy^T u over the rows of an adapter, no sum split over workgroups
 //   planes_kernel   pieces, aligned copies and the transposed W of the backward pass
 #include "ops.h"
@@ -937,15 +937,18 @@ constexpr int kFewRows = 64;
 constexpr int kHead = 16;                             // ranks that are read ahead
 
 // A workgroup's 16 outputs, the contraction cut over its wavefronts.  Bound by reading W, each workgroup's share of it in one go, and
-// by x, which every workgroup reads from L2: 32 rows, 4096 -> 4096 bf16, 34 MB, 13-14 us (2.5 TB/s).
-template <int DTYPE, int RT>
-constexpr int kFewWaves = waves_for(kStageBytes<DTYPE, DTYPE, true, 1, RT>);
+// by x, which every workgroup reads from L2: 32 rows, 4096 -> 4096 bf16, 34 MB, 13-14 us (2.5 TB/s).  Backward (not UNIT) W's rows
+// lie along the outputs and go to the matrix unit as they are: no transposed copy, no copies of the adapters (dx of 8 rows,
+// 4096 -> 4096, with du before it: bf16 25 us against 45 in tiles, fp32 53 against 100; 64 rows 31 against 46, 76 against 115).
+template <int DTYPE, int RT, bool UNIT>
+constexpr int kFewWaves = waves_for(kStageBytes<DTYPE, DTYPE, UNIT, 1, RT>);
+constexpr int kNeighbours = 4;                        // workgroups that share the lines of W's rows, in one XCD (not UNIT)
 
-template <int DTYPE, int QTYPE, int RT, int WAVES, bool STAGED>
+template <int DTYPE, int QTYPE, int RT, int WAVES, bool STAGED, bool UNIT>
 __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(FewRowsParams p) {
   typedef typename Value<DTYPE>::T T;
   typedef typename Value<QTYPE>::T TQ;
-  constexpr int STAGE = kStageBytes<DTYPE, DTYPE, true, 1, RT>;
+  constexpr int STAGE = kStageBytes<DTYPE, DTYPE, UNIT, 1, RT>;
   constexpr int PART = WAVES * RT * 16 * 17 * 4;
   constexpr int FIRST = STAGED && WAVES * STAGE > PART ? WAVES * STAGE : PART;      // the sums go where a stage was
   __shared__ __attribute__((aligned(1024))) unsigned char st0[FIRST];
@@ -954,7 +957,10 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(FewRowsParams p) {
   float (*part)[RT * 16][17] = reinterpret_cast<float (*)[RT * 16][17]>(st0);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, quarter = lane >> 4;
-  const int n0 = blockIdx.x * 16;
+  const unsigned local = blockIdx.x / 8;
+  const unsigned tile = UNIT ? blockIdx.x : (local / kNeighbours * 8 + blockIdx.x % 8) * kNeighbours + local % kNeighbours;
+  if (tile >= ((unsigned)p.N + 15) / 16) return;
+  const int n0 = (int)tile * 16;
   // This lane's outputs, rows row0 + EACH o of column `col`, and what their low-rank part needs: asked for before W is.
   constexpr int EACH = WAVES * 4, OUT = RT * 16 > EACH ? RT * 16 / EACH : 1;
   const int row0 = tid >> 4, col = n0 + (tid & 15);
@@ -975,13 +981,13 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(FewRowsParams p) {
   f32x4 acc[RT][1];
 #pragma unroll
   for (int t = 0; t < RT; ++t) acc[t][0] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const Rows<DTYPE> left{static_cast<const T*>(p.W) + (int64_t)n0 * p.ldw, p.ldw, 1, p.N - n0 < 16 ? p.N - n0 : 16};
+  const Rows<DTYPE> left{static_cast<const T*>(p.W) + n0 * (UNIT ? p.ldw : 1), UNIT ? p.ldw : 1, UNIT ? 1 : p.ldw, p.N - n0 < 16 ? p.N - n0 : 16};
   const Rows<DTYPE> x{static_cast<const T*>(p.X), p.ldx, 1, p.M};
   if constexpr (STAGED)
-    contract_staged<DTYPE, DTYPE, true, 1, RT, WAVES>(left, x, p.K, wave, lane, (lds_byte*)st0 + wave * STAGE, (lds_byte*)st1 + wave * STAGE,
+    contract_staged<DTYPE, DTYPE, UNIT, 1, RT, WAVES>(left, x, p.K, wave, lane, (lds_byte*)st0 + wave * STAGE, (lds_byte*)st1 + wave * STAGE,
                                                       (lds_byte*)st2 + (ring_for(STAGE) > 2 ? wave * STAGE : 0), acc);
   else
-    contract_straight<DTYPE, DTYPE, true, 1, RT, WAVES>(left, x, p.K, wave, lane, acc);
+    contract_straight<DTYPE, DTYPE, UNIT, 1, RT, WAVES>(left, x, p.K, wave, lane, acc);
   __syncthreads();
 #pragma unroll
   for (int t = 0; t < RT; ++t)
@@ -1226,12 +1232,12 @@ struct Layout { size_t x, w, u, q, odd, adapter, du, total; bool tiles, copies; 
 Layout layout(const lsam_adapter_desc* d, bool backward) {
   Layout l;
   const int N = backward ? d->in : d->out;
-  l.copies = backward || d->rows > kFewRows;
-  l.tiles = l.copies || (d->dtype == LSAM_DTYPE_BF16 && (int64_t)N * (d->rows > 32 ? (d->rows + 15) / 16 : 2) > 16384);
+  l.copies = d->rows > kFewRows;
+  l.tiles = l.copies || (!backward && d->dtype == LSAM_DTYPE_BF16 && (int64_t)N * (d->rows > 32 ? (d->rows + 15) / 16 : 2) > 16384);
   l.x = 0;
   l.w = l.x + (l.copies ? planes_bytes(d->rows, backward ? d->out : d->in, d->dtype) : 0);
   // the backward pass reads W transposed
-  l.u = l.w + (backward ? planes_bytes(d->in, d->out, d->dtype) : l.copies ? planes_bytes(d->out, d->in, d->dtype) : 0);
+  l.u = l.w + (!l.copies ? 0 : backward ? planes_bytes(d->in, d->out, d->dtype) : planes_bytes(d->out, d->in, d->dtype));
   const size_t low_k = (size_t)low_rank(d).k();
   l.q = l.u + (l.tiles ? up256((size_t)d->rows * low_k * 2) : 0);
   l.odd = l.q + (l.tiles ? up256((size_t)d->adapters * N * low_k * 2) : 0);
@@ -1376,26 +1382,32 @@ void launch_product(const ProductParams& p, int dtype, hipStream_t s) {
   }
 }
 
-template <int DTYPE, int QTYPE, int RT>
+template <int DTYPE, int QTYPE, int RT, bool UNIT>
 void launch_few_rows_tile(const FewRowsParams& p, hipStream_t s) {
-  const unsigned grid = (unsigned)((p.N + 15) / 16);
-  constexpr int waves = kFewWaves<DTYPE, RT>;
-  if (whole_units(p.X, p.ldx, p.K, DTYPE) && whole_units(p.W, p.ldw, p.K, DTYPE)) few_rows_kernel<DTYPE, QTYPE, RT, waves, true><<<grid, waves * 64, 0, s>>>(p);
-  else few_rows_kernel<DTYPE, QTYPE, RT, waves, false><<<grid, waves * 64, 0, s>>>(p);
+  const unsigned tiles = (unsigned)((p.N + 15) / 16), all = 8 * kNeighbours, grid = UNIT ? tiles : (tiles + all - 1) / all * all;
+  constexpr int waves = kFewWaves<DTYPE, RT, UNIT>;
+  const bool staged = whole_units(p.X, p.ldx, p.K, DTYPE) && (!UNIT || whole_units(p.W, p.ldw, p.K, DTYPE));
+  if (staged) few_rows_kernel<DTYPE, QTYPE, RT, waves, true, UNIT><<<grid, waves * 64, 0, s>>>(p);
+  else few_rows_kernel<DTYPE, QTYPE, RT, waves, false, UNIT><<<grid, waves * 64, 0, s>>>(p);
+}
+template <int DTYPE, int QTYPE, int RT>
+void launch_few_rows_along(const FewRowsParams& p, bool transposed, hipStream_t s) {
+  if (transposed) launch_few_rows_tile<DTYPE, QTYPE, RT, false>(p, s);
+  else launch_few_rows_tile<DTYPE, QTYPE, RT, true>(p, s);
 }
 template <int DTYPE, int QTYPE>
-void launch_few_rows(const FewRowsParams& p, hipStream_t s) {
-  if (p.M <= 16) launch_few_rows_tile<DTYPE, QTYPE, 1>(p, s);
-  else if (p.M <= 32) launch_few_rows_tile<DTYPE, QTYPE, 2>(p, s);
-  else launch_few_rows_tile<DTYPE, QTYPE, 4>(p, s);
+void launch_few_rows(const FewRowsParams& p, bool transposed, hipStream_t s) {
+  if (p.M <= 16) launch_few_rows_along<DTYPE, QTYPE, 1>(p, transposed, s);
+  else if (p.M <= 32) launch_few_rows_along<DTYPE, QTYPE, 2>(p, transposed, s);
+  else launch_few_rows_along<DTYPE, QTYPE, 4>(p, transposed, s);
 }
-void launch_few_rows_any(const FewRowsParams& p, int dtype, int qtype, hipStream_t s) {
+void launch_few_rows_any(const FewRowsParams& p, bool transposed, int dtype, int qtype, hipStream_t s) {
   if (dtype == LSAM_DTYPE_BF16) {
-    if (qtype == LSAM_DTYPE_BF16) launch_few_rows<LSAM_DTYPE_BF16, LSAM_DTYPE_BF16>(p, s);
-    else launch_few_rows<LSAM_DTYPE_BF16, LSAM_DTYPE_FP32>(p, s);
+    if (qtype == LSAM_DTYPE_BF16) launch_few_rows<LSAM_DTYPE_BF16, LSAM_DTYPE_BF16>(p, transposed, s);
+    else launch_few_rows<LSAM_DTYPE_BF16, LSAM_DTYPE_FP32>(p, transposed, s);
   } else {
-    if (qtype == LSAM_DTYPE_BF16) launch_few_rows<LSAM_DTYPE_FP32, LSAM_DTYPE_BF16>(p, s);
-    else launch_few_rows<LSAM_DTYPE_FP32, LSAM_DTYPE_FP32>(p, s);
+    if (qtype == LSAM_DTYPE_BF16) launch_few_rows<LSAM_DTYPE_FP32, LSAM_DTYPE_BF16>(p, transposed, s);
+    else launch_few_rows<LSAM_DTYPE_FP32, LSAM_DTYPE_FP32>(p, transposed, s);
   }
 }
 
@@ -1429,7 +1441,7 @@ void run_product(const Product& o, hipStream_t s) {
     p.M = (int)d->rows; p.N = o.N; p.K = o.K; p.Y = o.Y; p.ldy = o.y_stride; p.bias = o.bias; p.u = o.u; p.scale = o.scale;
     p.Q = o.Q; p.q_adapter = o.q_adapter; p.q_n = o.q_n; p.q_r = o.q_r; p.rank = d->rank;
     p.adapter = reinterpret_cast<const int*>(o.ws + o.l.adapter);
-    launch_few_rows_any(p, d->dtype, d->adapter_dtype, s);
+    launch_few_rows_any(p, o.transposed, d->dtype, d->adapter_dtype, s);
     return;
   }
   ProductParams p;
@@ -1551,10 +1563,11 @@ extern "C" int lsam_adapter_backward(const lsam_adapter_desc* d, const void* x, 
   const Segments g = segments(d, seg_begin, seg_adapter);
   const LowRank low = low_rank(d);
   float* const du = reinterpret_cast<float*>(static_cast<char*>(workspace) + l.du);
-  unsigned short* const copy = dx ? reinterpret_cast<unsigned short*>(static_cast<char*>(workspace) + l.u) : nullptr;
+  unsigned short* const copy = dx && l.tiles ? reinterpret_cast<unsigned short*>(static_cast<char*>(workspace) + l.u) : nullptr;
+  int* const adapter = dx && !l.tiles ? reinterpret_cast<int*>(static_cast<char*>(workspace) + l.adapter) : nullptr;
   if (d->rows > 0)
     launch_shrink_any(ShrinkParams{dy, d->dy_stride, B, d->b_adapter, 1, d->b_stride, du, d->rows, d->out, d->rank, d->scale, copy, 1.f, low,
-                                   low.k(), nullptr, g}, d->dtype, d->adapter_dtype, s);
+                                   low.k(), adapter, g}, d->dtype, d->adapter_dtype, s);
   if (dx && d->rows > 0)
     run_product(Product{d, dy, d->dy_stride, d->out, W, true, d->in, dx, d->dx_stride, nullptr, du, 1.f, A, d->a_adapter, 1, d->a_stride,
                         static_cast<char*>(workspace), l, g}, s);
