@@ -1053,47 +1053,83 @@ __global__ __launch_bounds__(kGradWaves * 64) void grads_kernel(GradsParams p) {
   int rank[NR];                                        // past the last: the last again, and dropped
 #pragma unroll
   for (int r = 0; r < NR; ++r) rank[r] = r * 16 + l16 < p.rank ? r * 16 + l16 : p.rank - 1;
-  for (int s = 0; s < p.g.n; ++s) {
-    if (p.g.which[s] != a) continue;
-    const int64_t lo = seg_row(p.g, s, p.rows), hi = seg_row(p.g, s + 1, p.rows);
-    for (int64_t t0 = lo + wave * 32; t0 < hi; t0 += kGradWaves * 32) {
-      const int64_t t = t0 + quarter * 8;
-      const int nt = hi - t < 8 ? (int)(hi - t) : 8;   // rows that are the segment's: others' may hold anything
-      typedef T T4 __attribute__((ext_vector_type(4)));
-      typedef T4 T4_any __attribute__((aligned(sizeof(T))));
-      T4 w[8];
-      Pieces<3> fs[NR];
-      if (t0 + 32 <= hi && c0 + 64 <= d.cols) {
+  bool any = false;
+  int turn = 0;                                        // pieces of 32 rows go round the wavefronts, from segment to segment
+  for (int s0 = 0; s0 < p.g.n; s0 += 64) {
+    // 64 segments at a time, a lane each
+    const int s = s0 + lane;
+    const int begin = s < p.g.n ? (int)seg_row(p.g, s, p.rows) : 0, end = s < p.g.n ? (int)seg_row(p.g, s + 1, p.rows) : 0;
+    unsigned long long mine = __ballot(begin < end && p.g.which[s < p.g.n ? s : 0] == a);
+    while (mine) {
+      const int at = __builtin_ctzll(mine);
+      mine &= mine - 1;
+      any = true;
+      const int64_t lo = __builtin_amdgcn_readlane(begin, at), hi = __builtin_amdgcn_readlane(end, at);
+      const int64_t first = lo + ((wave - turn) & (kGradWaves - 1)) * 32;
+      turn += (int)((hi - lo + 31) / 32) & (kGradWaves - 1);
+      for (int64_t t0 = first; t0 < hi; t0 += kGradWaves * 32) {
+        const int64_t t = t0 + quarter * 8;
+        const int nt = hi - t < 8 ? (int)(hi - t) : 8;   // rows that are the segment's: others' may hold anything
+        typedef T T4 __attribute__((ext_vector_type(4)));
+        typedef T4 T4_any __attribute__((aligned(sizeof(T))));
+        T4 w[8];
+        Pieces<3> fs[NR];
+        if (t0 + 32 <= hi && c0 + 64 <= d.cols) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = *reinterpret_cast<const T4_any*>(V + (t + j) * d.stride);
+          for (int j = 0; j < 8; ++j) w[j] = *reinterpret_cast<const T4_any*>(V + (t + j) * d.stride);
 #pragma unroll
-        for (int r = 0; r < NR; ++r) load8<LSAM_DTYPE_FP32, false>(d.S + t * p.rank + rank[r], p.rank, fs[r]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) w[j][q] = j < nt && q < nc ? V[(t + j) * d.stride + q] : (T)0;
-#pragma unroll
-        for (int r = 0; r < NR; ++r) load8_some<LSAM_DTYPE_FP32>(d.S + t * p.rank + rank[r], p.rank, nt, fs[r]);
-      }
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        Pieces<kPieces<DTYPE>> fv;
-        if constexpr (DTYPE == LSAM_DTYPE_BF16) {
-          u16x8 o;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) o[j] = w[j][q];
-          fv.p[0] = __builtin_bit_cast(bf16x8, o);
+          for (int r = 0; r < NR; ++r) load8<LSAM_DTYPE_FP32, false>(d.S + t * p.rank + rank[r], p.rank, fs[r]);
         } else {
-          float o[8];
+          // places that are not there: the nearest that is, so that no load depends on a condition, and 0 afterwards
 #pragma unroll
-          for (int j = 0; j < 8; ++j) o[j] = w[j][q];
-          split8(o, fv);
+          for (int j = 0; j < 8; ++j) {
+            const int64_t row = t + j < hi ? t + j : hi - 1;
+            if (c0 + 64 <= d.cols) {
+              w[j] = *reinterpret_cast<const T4_any*>(V + row * d.stride);
+            } else {
+#pragma unroll
+              for (int q = 0; q < 4; ++q) w[j][q] = V[row * d.stride + (q < nc ? q : nc > 0 ? nc - 1 : 0)];
+            }
+          }
+#pragma unroll
+          for (int r = 0; r < NR; ++r) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = d.S[(t + j < hi ? t + j : hi - 1) * p.rank + rank[r]];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = j < nt ? v[j] : 0.f;
+            split8(v, fs[r]);
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (j >= nt) w[j] = T4{0, 0, 0, 0};
         }
 #pragma unroll
-        for (int r = 0; r < NR; ++r) acc[q][r] = multiply(fv, fs[r], acc[q][r]);
+        for (int q = 0; q < 4; ++q) {
+          Pieces<kPieces<DTYPE>> fv;
+          if constexpr (DTYPE == LSAM_DTYPE_BF16) {
+            u16x8 o;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] = w[j][q];
+            fv.p[0] = __builtin_bit_cast(bf16x8, o);
+          } else {
+            float o[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] = w[j][q];
+            split8(o, fv);
+          }
+#pragma unroll
+          for (int r = 0; r < NR; ++r) acc[q][r] = multiply(fv, fs[r], acc[q][r]);
+        }
       }
     }
+  }
+  if (!any) {                                          // the same for the whole workgroup
+    for (int i = tid; i < 64 * p.rank; i += kGradWaves * 64) {
+      const int col = d.col == 1 ? i % 64 : i / p.rank, r = d.col == 1 ? i / 64 : i % p.rank;
+      if (c0 + col < d.cols) d.G[a * d.adapter + (c0 + col) * d.col + r * d.rank] = 0.f;
+    }
+    return;
   }
   // lane: rank r 16 + l16, column 4 (4 quarter + i) + q.  The upper half of the wavefronts hand over to the lower, twice.
   constexpr int H = kGradWaves / 2;
