@@ -648,9 +648,9 @@ __device__ __forceinline__ void interleave() {
 // LDS: one is multiplied, the others are on their way.  fp32 results: all three pieces of both operands are there together, and
 // their six products are formed from the same fragments (one product after the other, each with tiles of its own, read
 // twice as much: the whole call 777 x 1000 -> 1501 96 us, 71 so).
-// 16384 x 4096 -> 4096 bf16 485-560 us (0.98-1.13 PFLOP/s, from card to card; a library's product of 8192 a side reaches 1.33, the matrix units alone
-// 2.08): bound by the power that products of random numbers draw -- rings of smaller steps, other orders of the loads and
-// of the fragments all measured the same, and zeros run at 1.5.  fp32 4096 x 4096 -> 4096: 0.98 PFLOP/s of its pieces.
+// 16384 x 4096 -> 4096 bf16 485-560 us (0.98-1.13 PFLOP/s, from card to card; a library's product of 8192 a side reaches 1.33,
+// the matrix units alone 2.08): bound by the power that products of random numbers draw -- rings of smaller steps, other orders of
+// the loads and of the fragments all measured the same, and zeros run at 1.5.  fp32 4096 x 4096 -> 4096: 0.98 PFLOP/s of its pieces.
 template <int OTYPE, int BM, int BN, int BK, int S>
 __device__ __forceinline__ void product_tile(const ProductParams& p) {
   constexpr int NW = 4, WN = 2;
