@@ -140,8 +140,9 @@ int lsam_recurrence_backward(const lsam_recurrence_desc* d, const int64_t* offse
  *   A, B       [device] of adapter_dtype: adapters matrices [rank, in] and [out, rank], as far apart as a_adapter and b_adapter
  *              say (for replicas whose parameters are rows of a [K, d] array: d)
  *   u          [device] [rows, rank] floats that receive x A_a^T (0 without an adapter), for the backward pass
- * Products are summed in fp32; operands in fp32 are not rounded to fewer bits.  A row's result depends on its own values, W and
- * its own adapter only; where an element of B_a is infinite or NaN, the results it takes part in are infinite or NaN.
+ * Products are summed in fp32; operands in fp32, u among them, are not rounded to fewer bits.  No value of another row, and none
+ * of another adapter, takes part in a row's result; the order in which its sums are added goes by the sizes of the call.
+ * What is not finite in x, W, A_a or B_a makes the results it takes part in infinite or NaN.
  * workspace [device, 256-byte aligned], lsam_adapter_workspace_bytes(d, 0) bytes for this call, (d, 1) for the backward one (0, with
  * a message, for a descriptor that is refused); nothing in it has to survive a call.  Parts of it are used only where rows are
  * not aligned to 16 bytes, or fp32. */

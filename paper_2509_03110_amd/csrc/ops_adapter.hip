@@ -1243,17 +1243,14 @@ bool straight(const void* p, int64_t stride, int cols, int dtype) { return dtype
 // The same from the descriptor alone: what a workspace must be large enough for.
 size_t planes_bytes(int64_t rows, int cols, int dtype) { return up256((size_t)(dtype == LSAM_DTYPE_BF16 ? 1 : 3) * rows * up8(cols) * 2); }
 
-// Pieces of u and of the adapter, enough for the result's type: what is left out is 2^-16 of a product before it is rounded to
-// bfloat16, 2^-24 otherwise.
+// Pieces of u and of the adapter that lose none of their digits: u, or du, is fp32 whatever the result's type is, and so may the
+// adapter be; a bfloat16 is its own piece.
 LowRank low_rank(const lsam_adapter_desc* d) {
   LowRank l;
   l.rank = d->rank;
   l.padded = (d->rank + 7) & ~7;
-  const bool whole = d->dtype == LSAM_DTYPE_FP32, fine = d->adapter_dtype == LSAM_DTYPE_FP32;
-  if (whole && fine) { l.pairs = 6; l.left = kSixLeft; l.right = kSixRight; }
-  else if (whole) { l.pairs = 3; l.left = 0x012u; l.right = 0x000u; }
-  else if (fine) { l.pairs = 3; l.left = 0x001u; l.right = 0x010u; }
-  else { l.pairs = 2; l.left = 0x01u; l.right = 0x00u; }
+  if (d->adapter_dtype == LSAM_DTYPE_FP32) { l.pairs = 6; l.left = kSixLeft; l.right = kSixRight; }
+  else { l.pairs = 3; l.left = 0x012u; l.right = 0x000u; }
   return l;
 }
 
