@@ -91,7 +91,8 @@ int lsam_logprobs_backward(const lsam_logprobs_desc* d, const void* logits, cons
 
 /* ---- gated linear recurrence -------------------------------------------------------------------
  * For every sequence and channel:  h_t = a_t h_{t-1} + (1 - a_t) x_t,  a_t = 1 / (1 + e^{-f_t}),  t = 0, 1, ...,
- * from h_{-1} = h0.  States and sums are fp32; h, df and dx are rounded once, where they are stored.
+ * from h_{-1} = h0.  States and sums are fp32; h, df and dx are rounded once, where they are stored.  A gate below 2^-126 is 0.  An
+ * infinite state stays infinite while the gates are positive, and is NaN behind a gate of 0, as step by step.
  *
  * Sequences of equal length (packed = 0): f, x, h are `seqs` matrices [rows, dim]; rows = 1 is a step of generation.
  * Packed sequences of any lengths (packed = 1): f, x, h are one matrix [rows, dim], and sequence i is rows offsets[i] to

@@ -49,6 +49,26 @@ __device__ __forceinline__ void gates(float f, float& a, float& b) {
   b = f >= 0.f ? small : r;
 }
 
+// A = the product of gates: where it underflows although all of them are positive, the smallest number above 0 stands for it, so
+// that an infinite state passes a run as it passes its steps (0 x inf would be NaN).
+constexpr float kLeast = 0x1p-149f;
+__device__ __forceinline__ float product_of(const float (&a)[kRows]) {
+  float A = 1.f;
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) A *= a[i];
+  if (A == 0.f) {
+    float least = a[0];
+#pragma unroll
+    for (int i = 1; i < kRows; ++i) least = __builtin_fminf(least, a[i]);
+    A = least > 0.f ? kLeast : 0.f;
+  }
+  return A;
+}
+__device__ __forceinline__ float product_of(float A, float B) {
+  const float AB = A * B;
+  return AB == 0.f && A > 0.f && B > 0.f ? kLeast : AB;
+}
+
 // kRows rows of a tensor from row t0 on, zeros for rows that are not there.  The usual case, all rows there, is a run of
 // loads that nothing waits between.
 template <typename T>
@@ -166,7 +186,7 @@ __global__ __launch_bounds__(NW * 64) void recurrence_kernel(RecurrenceParams p)
   int b = 0;
   for (int64_t j = w.first; j < w.end; ++j) {
     const int64_t t0 = j * R - w.phase + wave * kRows;
-    float a[kRows], v[kRows], A = 1.f, H = 0.f;
+    float a[kRows], v[kRows], H = 0.f;
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
       float k;
@@ -179,11 +199,9 @@ __global__ __launch_bounds__(NW * 64) void recurrence_kernel(RecurrenceParams p)
       for (int i = 0; i < kRows; ++i)
         if (t0 + i < 0 || t0 + i >= w.len) { a[i] = 1.f; v[i] = 0.f; }      // outside the sequence the state stays
     }
+    const float A = product_of(a);
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      A *= a[i];
-      H = a[i] * H + v[i];
-    }
+    for (int i = 0; i < kRows; ++i) H = a[i] * H + v[i];
     if constexpr (!RUNS)
       if (wave == 0 && p.states && j > 0 && w.mine) p.states[(w.state0 + j) * p.D + w.ch] = carry;
     float s = carry;
@@ -196,12 +214,12 @@ __global__ __launch_bounds__(NW * 64) void recurrence_kernel(RecurrenceParams p)
         const float qa = shA[b][q][lane];
         if (q == wave) s = carry;
         carry = qa * carry + shH[b][q][lane];
-        if constexpr (RUNS) whole *= qa;
+        if constexpr (RUNS) whole = product_of(whole, qa);
       }
       b ^= 1;
     } else {
       carry = A * carry + H;
-      if constexpr (RUNS) whole *= A;
+      if constexpr (RUNS) whole = product_of(whole, A);
     }
     if constexpr (!RUNS) {
 #pragma unroll
@@ -260,7 +278,7 @@ __global__ __launch_bounds__(NW * 64) void recurrence_grad_kernel(RecurrencePara
   int b = 0;
   for (int64_t j = w.end - 1; j >= w.first; --j) {
     const int64_t t0 = j * R - w.phase + wave * kRows;
-    float a[kRows], k[kRows], xv[kRows], d[kRows], A = 1.f, E = 0.f, H = 0.f, s = entry;
+    float a[kRows], k[kRows], xv[kRows], d[kRows], E = 0.f, H = 0.f, s = entry;
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
       gates(wide(rf[i]), a[i], k[i]);
@@ -273,10 +291,10 @@ __global__ __launch_bounds__(NW * 64) void recurrence_grad_kernel(RecurrencePara
       for (int i = 0; i < kRows; ++i)
         if (t0 + i < 0 || t0 + i >= w.len) { a[i] = 1.f; k[i] = 0.f; }
     }
+    const float A = product_of(a);
+    if constexpr (!RUNS) {
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      A *= a[i];
-      if constexpr (!RUNS) H = a[i] * H + k[i] * xv[i];
+      for (int i = 0; i < kRows; ++i) H = a[i] * H + k[i] * xv[i];
     }
 #pragma unroll
     for (int i = kRows - 1; i >= 0; --i) E = a[i] * (d[i] + E);
@@ -291,7 +309,7 @@ __global__ __launch_bounds__(NW * 64) void recurrence_grad_kernel(RecurrencePara
         const float qa = shA[b][q][lane];
         if (q == wave) e = carry;
         carry = qa * carry + shE[b][q][lane];
-        if constexpr (RUNS) whole *= qa;
+        if constexpr (RUNS) whole = product_of(whole, qa);
       }
       if constexpr (!RUNS) {
 #pragma unroll
@@ -301,7 +319,7 @@ __global__ __launch_bounds__(NW * 64) void recurrence_grad_kernel(RecurrencePara
       b ^= 1;
     } else {
       carry = A * carry + E;
-      if constexpr (RUNS) whole *= A;
+      if constexpr (RUNS) whole = product_of(whole, A);
     }
     if constexpr (!RUNS) {
       float g[kRows];
