@@ -27,6 +27,7 @@ constexpr int kMaxRank = LSAM_ADAPTER_MAX_RANK;
 struct Segments {
   const int32_t* begin; const int32_t* which;
   int n, adapters;
+  bool each;                                          // copies for product_kernel: one for each segment, else for each adapter
 };
 __device__ __forceinline__ int64_t seg_row(const Segments& g, int s, int64_t rows) {
   const int64_t b = g.begin[s];
@@ -46,6 +47,11 @@ __device__ __forceinline__ int seg_at(const Segments& g, int64_t row) {
 __device__ __forceinline__ int seg_adapter(const Segments& g, int s) {
   const int a = g.which[s];
   return a >= 0 && a < g.adapters ? a : -1;
+}
+// The copy of the adapter of segment s for product_kernel, or -1.
+__device__ __forceinline__ int seg_copy(const Segments& g, int s) {
+  const int a = seg_adapter(g, s);
+  return a >= 0 && g.each ? s : a;
 }
 // The adapter of a row, another row in every lane; `begin` may be a copy of the segments'.
 __device__ __forceinline__ int row_adapter(const Segments& g, const int* begin, int64_t row, int64_t rows) {
@@ -391,8 +397,8 @@ struct SegmentsOf {
   const Segments& g;
   int m0, m_here, low_k, step;
   int64_t rows;
-  int window, i, begins, adapters;
-  int lo, hi, a, k0;                                   // rows of the tile, adapter, first number
+  int window, i, begins, copies;
+  int lo, hi, copy, k0;                                // rows of the tile, copy of the adapter, first number
   bool done;
   __device__ __forceinline__ SegmentsOf(const Segments& g_, int64_t m0_, int m_here_, int64_t rows_, int low_k_, int step_)
       : g(g_), m0((int)m0_), m_here(m_here_), low_k(low_k_), step(step_), rows(rows_), i(0), k0(low_k_), done(g_.n == 0) {
@@ -403,7 +409,7 @@ struct SegmentsOf {
   __device__ __forceinline__ void load() {
     const int s = window + (int)(threadIdx.x & 63);
     begins = (int)seg_row(g, s < g.n ? s : g.n, rows);
-    adapters = s < g.n ? seg_adapter(g, s) : -1;
+    copies = s < g.n ? seg_copy(g, s) : -1;
   }
   __device__ __forceinline__ bool next() {
     if (done) return false;
@@ -420,11 +426,11 @@ struct SegmentsOf {
         done = true;
         return false;
       }
-      a = __builtin_amdgcn_readlane(adapters, i);
+      copy = __builtin_amdgcn_readlane(copies, i);
       ++i;
       lo = l > 0 ? l : 0;
       hi = h < m_here ? h : m_here;
-      if (a >= 0 && lo < hi) {
+      if (copy >= 0 && lo < hi) {
         k0 = 0;
         return true;
       }
@@ -534,18 +540,21 @@ __global__ __launch_bounds__(WAVES * 64) void shrink_kernel(ShrinkParams p) {
 // ---- the adapters' pieces for product_kernel --------------------------------------------------------
 struct CopiesParams {
   const void* Q; int64_t q_adapter, q_n, q_r;         // strides along adapter, output and rank
-  unsigned short* copy; unsigned char* odd;           // [adapters][N][low_k], [adapters][N]
-  int adapters, N, low_k;
+  unsigned short* copy; unsigned char* odd;           // [copies][N][low_k], [copies][N]
+  int N, low_k;
   LowRank low;
+  Segments g; int64_t rows;
 };
 // An infinity or NaN in an adapter would reach the rows of other segments in its tile, whose 0 it is multiplied with: it is left
-// out here, and the outputs it belongs to are marked.  16 adapters of 8192 x 32 in bf16 15 us.
+// out here, and the outputs it belongs to are marked.  There is a copy for each segment or for each adapter, whichever are fewer: what
+// a call costs does not go by adapters that it does not use.  16 adapters of 8192 x 32 in bf16 15 us.
 template <int QTYPE>
 __global__ __launch_bounds__(256) void copies_kernel(CopiesParams p) {
   typedef typename Value<QTYPE>::T TQ;
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int a = (int)(at / p.N), n = (int)(at - (int64_t)a * p.N);
-  if (a >= p.adapters) return;
+  const int n = (int)(blockIdx.x * 256 + threadIdx.x), c = (int)blockIdx.y;
+  const int a = !p.g.each ? c : seg_row(p.g, c, p.rows) < seg_row(p.g, c + 1, p.rows) ? seg_adapter(p.g, c) : -1;
+  if (a < 0 || n >= p.N) return;
+  const int64_t at = (int64_t)c * p.N + n;
   const TQ* q = static_cast<const TQ*>(p.Q) + a * p.q_adapter + n * p.q_n;
   bool odd = false;
   for (int r0 = 0; r0 < p.low.padded; r0 += 8) {
@@ -577,8 +586,8 @@ struct ProductParams {
   int64_t M; int N, K;                                // K a multiple of 8, rows 16-byte aligned
   void* Y; int64_t ldy;
   const float* bias;
-  const unsigned short* u; const unsigned short* Q;   // copies: [M][low_k], [adapters][N][low_k]
-  const unsigned char* odd;                           // [adapters][N]
+  const unsigned short* u; const unsigned short* Q;   // copies: [M][low_k], [copies][N][low_k]
+  const unsigned char* odd;                           // [copies][N]
   int low_k;
   int tilesM, tilesN;
   Segments g;
@@ -846,8 +855,8 @@ __device__ __forceinline__ void product_tile(const ProductParams& p) {
       lds_byte* const tile = i == 0 ? a0 : i == 1 ? a1 : i == 2 ? a2 : i == 3 ? a3 : i == 4 ? a4 : i == 5 ? a5 : i == 6 ? a6 : a7;
       k[i] = walk.k0;
       OX::issue_some(u, p.low_k, (int)m_here, walk.lo, walk.hi, tile, walk.k0, lane, wave);
-      OW::issue_some(p.Q + ((int64_t)walk.a * p.N + n0) * p.low_k, p.low_k, n_here, 0, n_here, tile + PART_W, walk.k0, lane, wave);
-      const unsigned char* const odd = p.odd + (int64_t)walk.a * p.N + n0;
+      OW::issue_some(p.Q + ((int64_t)walk.copy * p.N + n0) * p.low_k, p.low_k, n_here, 0, n_here, tile + PART_W, walk.k0, lane, wave);
+      const unsigned char* const odd = p.odd + (int64_t)walk.copy * p.N + n0;
 #pragma unroll
       for (int j = 0; j < BN / 64; ++j) mark[i][j] = odd[j * 64 + lane < n_here ? j * 64 + lane : 0];
     }
@@ -901,9 +910,9 @@ __device__ __forceinline__ void product_tile(const ProductParams& p) {
   for (int s = found < 0 ? 0 : found; s < p.g.n; ++s) {
     const int64_t l = seg_row(p.g, s, p.M) - m0, h = seg_row(p.g, s + 1, p.M) - m0;
     if (l >= m_here) break;
-    const int a = seg_adapter(p.g, s);
-    if (a < 0 || l >= h) continue;
-    const unsigned char* odd = p.odd + (int64_t)a * p.N + n0;
+    const int copy = seg_copy(p.g, s);
+    if (copy < 0 || l >= h) continue;
+    const unsigned char* odd = p.odd + (int64_t)copy * p.N + n0;
     for (int i = 0; i < TM; ++i) {
       const int row = wm + i * 32 + l32;
       if (row < l || row >= h || row >= m_here) continue;
@@ -1257,24 +1266,28 @@ LowRank low_rank(const lsam_adapter_desc* d) {
 // Offsets in the workspace: copies of x or dy and of W, of u and of the adapters, marks, adapters of rows, du.
 //
 // Few rows of one forward call go to few_rows_kernel, whose workgroups each read all of x from L2 for 16 outputs, or, where that
-// costs more than the further launch for the adapters' copies, to product_kernel in tiles of 64 x 64: bf16, 4096 -> 4096,
-// 20 us against 28 for 16 rows and 27 against 30 for 64; 4096 -> 14336 40 against 35 and 82 against 36; 14336 -> 4096 51 against
-// 64 for 64 rows.  Only if x and W go to LDS as they lie: a copy of W would cost more than it brings (fp32, 4096 -> 4096: 58
-// against 113 us for 16 rows, 115 against 127 for 64).
+// costs more than the further launch for the adapters' copies, to product_kernel in tiles of 64 x 64.  us, bf16, one segment of
+// rank 16: 4096 -> 4096 19 against 27 for 16 rows and 27 against 28 for 64; 4096 -> 14336 40 against 33 and 82 against 34.  A copy
+// has to serve four rows (of the 16, 32, 48 or 64 that the workgroups take): 4096 -> 14336, 16 rows with 4 copies 40 against 36, with 16 40
+// against 52; 64 rows with 16 copies 82 against 53, with 64 83 against 104, of rank 64 175 against 144 and 222 against 541.
+// Only if x and W go to LDS as they lie: a copy of W would cost more than it brings (fp32, 4096 -> 4096: 58 against 113 us for
+// 16 rows, 115 against 127 for 64).
+int copies_of(const lsam_adapter_desc* d) { return d->segs < d->adapters ? d->segs : d->adapters; }
 struct Layout { size_t x, w, u, q, odd, adapter, du, total; bool tiles, copies; };
 Layout layout(const lsam_adapter_desc* d, bool backward) {
   Layout l;
   const int N = backward ? d->in : d->out;
   l.copies = d->rows > kFewRows;
-  l.tiles = l.copies || (!backward && d->dtype == LSAM_DTYPE_BF16 && (int64_t)N * (d->rows > 32 ? (d->rows + 15) / 16 : 2) > 16384);
+  const int64_t tall = (d->rows + 15) / 16;            // tiles of 16 rows
+  l.tiles = l.copies || (!backward && d->dtype == LSAM_DTYPE_BF16 && copies_of(d) <= 4 * tall && (int64_t)N * (tall > 2 ? tall : 2) > 16384);
   l.x = 0;
   l.w = l.x + (l.copies ? planes_bytes(d->rows, backward ? d->out : d->in, d->dtype) : 0);
   // the backward pass reads W transposed
   l.u = l.w + (!l.copies ? 0 : backward ? planes_bytes(d->in, d->out, d->dtype) : planes_bytes(d->out, d->in, d->dtype));
   const size_t low_k = (size_t)low_rank(d).k();
   l.q = l.u + (l.tiles ? up256((size_t)d->rows * low_k * 2) : 0);
-  l.odd = l.q + (l.tiles ? up256((size_t)d->adapters * N * low_k * 2) : 0);
-  l.adapter = l.odd + (l.tiles ? up256((size_t)d->adapters * N) : 0);
+  l.odd = l.q + (l.tiles ? up256((size_t)copies_of(d) * N * low_k * 2) : 0);
+  l.adapter = l.odd + (l.tiles ? up256((size_t)copies_of(d) * N) : 0);
   l.du = l.adapter + (l.copies ? 0 : up256((size_t)d->rows * 4));
   l.total = l.du + (backward ? up256((size_t)d->rows * d->rank * 4) : 0);
   return l;
@@ -1500,8 +1513,8 @@ void run_product(const Product& o, hipStream_t s) {
   unsigned char* const odd = reinterpret_cast<unsigned char*>(o.ws + o.l.odd);
   p.Q = q; p.odd = odd;
   if (o.g.n > 0) {
-    const CopiesParams c{o.Q, o.q_adapter, o.q_n, o.q_r, q, odd, d->adapters, o.N, p.low_k, low};
-    const unsigned grid = (unsigned)(((int64_t)d->adapters * o.N + 255) / 256);
+    const CopiesParams c{o.Q, o.q_adapter, o.q_n, o.q_r, q, odd, o.N, p.low_k, low, o.g, d->rows};
+    const dim3 grid((unsigned)(o.N + 255) / 256, (unsigned)copies_of(d));
     if (d->adapter_dtype == LSAM_DTYPE_BF16) copies_kernel<LSAM_DTYPE_BF16><<<grid, 256, 0, s>>>(c);
     else copies_kernel<LSAM_DTYPE_FP32><<<grid, 256, 0, s>>>(c);
   }
@@ -1511,6 +1524,7 @@ void run_product(const Product& o, hipStream_t s) {
 Segments segments(const lsam_adapter_desc* d, const int32_t* begin, const int32_t* which) {
   Segments g;
   g.begin = begin; g.which = which; g.n = d->adapters > 0 ? d->segs : 0; g.adapters = d->adapters;
+  g.each = d->segs < d->adapters;
   return g;
 }
 
