@@ -1342,18 +1342,17 @@ void launch_shrink_rank(const ShrinkParams& p, hipStream_t s) {
   // Tiles of 64 rows read the adapter least often; of 32 or 16 rows where those leave units idle or segments are short.  Calls
   // with 8 outputs, 4096 -> rank 16 in fp32 adapters, us in tiles of 64 / 32 / 16 rows: 16384 rows 59 / 72 / 99, 8191 47 / 57 / 73,
   // 6144 44 / 41 / 55, 4096 44 / 39 / 40, 1024 42 / 36 / 36; 1024 rows of 512 segments 77 / 73 / 70.
-  const bool brief = p.rows <= 16ll * p.g.n;
-  constexpr bool ROOM = 2 * 2 * kStageBytes<ATYPE, DTYPE, UNIT, NR, 4> <= kRoom;      // for two stages of two wavefronts
-  const int64_t rows = ROOM && !brief && p.rows >= 64 * 112 ? 64 : !brief && p.rows >= 32 * 192 ? 32 : 16;
+  // A launch has less than 2^32 lanes (more wrap, without an error): from 2^26 rows on tiles have 64 whatever the segments are.
+  const bool brief = p.rows <= 16ll * p.g.n && p.rows < 1ll << 26;
+  const int64_t rows = !brief && p.rows >= 64 * 112 ? 64 : !brief && p.rows >= 32 * 192 ? 32 : 16;
   const int64_t tiles = (p.rows + rows - 1) / rows;
   int64_t y = p.g.n / tiles + 2;                      // two segments meet in many a tile: a workgroup for each
   y = y > 64 ? 64 : y > p.g.n ? (p.g.n > 0 ? p.g.n : 1) : y;
   const dim3 grid((unsigned)tiles, (unsigned)y + 1, (unsigned)(p.rank + NR * 16 - 1) / (NR * 16));
   const bool staged = whole_units(p.x, p.x_stride, p.K, DTYPE) &&
                       (!UNIT || (whole_units(p.A, p.a_rank, p.K, ATYPE) && p.a_adapter % (16 / dtype_bytes(ATYPE)) == 0));
-  if constexpr (ROOM)
-    if (rows == 64) return launch_shrink_tile<DTYPE, ATYPE, UNIT, NR, 4>(p, grid, staged, s);
-  if (rows == 32) launch_shrink_tile<DTYPE, ATYPE, UNIT, NR, 2>(p, grid, staged, s);
+  if (rows == 64) launch_shrink_tile<DTYPE, ATYPE, UNIT, NR, 4>(p, grid, staged, s);
+  else if (rows == 32) launch_shrink_tile<DTYPE, ATYPE, UNIT, NR, 2>(p, grid, staged, s);
   else launch_shrink_tile<DTYPE, ATYPE, UNIT, NR, 1>(p, grid, staged, s);
 }
 // A workgroup has at most 32 ranks, which leaves LDS for more wavefronts to cut fp32's pieces; all 64 where there is nothing to

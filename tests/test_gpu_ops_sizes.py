@@ -1,4 +1,5 @@
-"""The operators at sizes where a call becomes several launches, or a launch nears the most lanes that it can have."""
+"""The operators at sizes where a call becomes several launches, or a launch nears the most lanes that it can have.  Cases that need
+more memory than is free are skipped."""
 import pytest
 import torch
 
@@ -17,6 +18,11 @@ def room():
     torch.cuda.empty_cache()
 
 
+def need(gib):
+    if torch.cuda.mem_get_info()[0] < gib * 2 ** 30:
+        pytest.skip("%d GiB of free memory are needed" % gib)
+
+
 def test_more_adapters_times_outputs_than_a_launch_has_lanes():
     # 65535 x 65552 > 2^32; all adapters but two are the same memory
     rows, inp, out, m = 65, 8, 65552, 65535
@@ -31,3 +37,24 @@ def test_more_adapters_times_outputs_than_a_launch_has_lanes():
     dy = torch.randn(rows, out, device=DEV, generator=g).to(B16)
     dx = ops.adapter_backward(x, W, A.expand(m, 2, inp), B.expand(m, out, 2), u, dy, sb, which, 0.5, want_adapters=False)[0]
     assert torch.equal(dx, ops.adapter_backward(x, W, A, B, u, dy, sb, torch.zeros_like(which), 0.5, want_adapters=False)[0])
+
+
+def test_short_segments_of_very_many_rows():
+    # segments of 16 rows: tiles of 16 rows would be 2^23 workgroups of 512 lanes
+    need(24)
+    rows, inp, out, n = (1 << 27) + 40, 8, 8, (1 << 23) + 4
+    g = torch.Generator(device=DEV).manual_seed(2)
+    x = torch.randint(-4, 5, (rows, inp), device=DEV, generator=g, dtype=torch.int8).to(B16)      # whole numbers: sums are exact
+    W = torch.randint(-4, 5, (out, inp), device=DEV, generator=g).to(B16)
+    A, B = (torch.randint(-2, 3, s, device=DEV, generator=g).to(B16) for s in ((3, 1, inp), (3, out, 1)))
+    sb = (torch.arange(n + 1, device=DEV, dtype=torch.int64) * 16).clamp(max=rows).int()
+    which = (torch.arange(n, device=DEV) % 4 - 1).int()
+    y, u = ops.adapter(x, W, A, B, sb, which, 1.0)
+    for lo in (0, (1 << 26) - 100, (1 << 27) - 300, rows - 300):
+        r = torch.arange(lo, lo + 300, device=DEV)
+        a = which[r // 16].long()
+        xs = x[lo:lo + 300].float()
+        v = (xs[:, None, :] * A.float()[a.clamp(min=0), 0][:, None, :]).sum(2) * (a >= 0)[:, None]
+        assert torch.equal(u[lo:lo + 300], v)
+        want = (xs[:, None, :] * W.float()).sum(2) + v * B.float()[a.clamp(min=0), :, 0]
+        assert torch.equal(y[lo:lo + 300], want.to(B16))
