@@ -1391,8 +1391,15 @@ void launch_planes(const void* src, int64_t stride, int64_t rows, int cols, bool
     const int64_t groups = ((rows + 63) / 64) * ((cols + 63) / 64);
     planes_kernel<DTYPE, true><<<(unsigned)groups, 256, 0, s>>>(p);
   } else {
-    const int64_t groups = (rows * (p.ld / 8) + 255) / 256;
-    planes_kernel<DTYPE, false><<<(unsigned)groups, 256, 0, s>>>(p);
+    // a launch has less than 2^32 lanes: more rows take further launches
+    const int64_t most = (1ll << 31) / (p.ld / 8);
+    for (int64_t r0 = 0; r0 < rows; r0 += most) {
+      p.rows = rows - r0 < most ? rows - r0 : most;
+      p.src = static_cast<const char*>(src) + r0 * stride * dtype_bytes(DTYPE);
+      p.dst = dst + r0 * p.ld;
+      const int64_t groups = (p.rows * (p.ld / 8) + 255) / 256;
+      planes_kernel<DTYPE, false><<<(unsigned)groups, 256, 0, s>>>(p);
+    }
   }
 }
 void launch_planes_any(const void* src, int64_t stride, int64_t rows, int cols, int dtype, bool transpose, unsigned short* dst, hipStream_t s) {

@@ -58,3 +58,18 @@ def test_short_segments_of_very_many_rows():
         assert torch.equal(u[lo:lo + 300], v)
         want = (xs[:, None, :] * W.float()).sum(2) + v * B.float()[a.clamp(min=0), :, 0]
         assert torch.equal(y[lo:lo + 300], want.to(B16))
+
+
+def test_copies_of_more_numbers_than_a_launch_has_lanes_for():
+    # rows of 129 numbers are copied to rows of 136: 2^32 lanes of eight numbers at these rows
+    need(160)
+    rows, inp = 254_000_000, 129
+    x = torch.zeros(rows, inp, device=DEV, dtype=B16)
+    marked = torch.tensor([0, 5, 126_000_000, rows - 900_000, rows - 1], device=DEV)
+    x[marked] = 1
+    W = torch.ones(1, inp, device=DEV, dtype=B16)
+    A, B = torch.ones(1, 1, inp, device=DEV, dtype=B16), torch.ones(1, 1, 1, device=DEV, dtype=B16)
+    sb, which = torch.tensor([rows - 10, rows], dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    y, u = ops.adapter(x, W, A, B, sb, which, 1.0)
+    assert torch.equal(y[marked, 0].float(), torch.tensor([129.0, 129, 129, 129, 258], device=DEV).to(B16).float())
+    assert int((y != 0).sum()) == 5 and int((u != 0).sum()) == 1
