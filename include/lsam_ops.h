@@ -11,8 +11,8 @@
  * nothing allocated, the host never blocked, every call valid under HIP graph capture.  Strides are
  * counted in elements; the last index of every array is contiguous, and arrays need the
  * alignment of one element only (16-byte aligned rows are faster).  Sizes of zero are valid and
- * launch nothing that has nothing to write.  Outputs must not lie over inputs, except where that
- * is said to be allowed.  Results do not depend on the stream, on timing or on other calls: sums are
+ * launch nothing that has nothing to write.  Outputs and workspaces must not lie over inputs or each
+ * other, except where that is said to be allowed: such calls are refused.  Results do not depend on the stream, on timing or on other calls: sums are
  * added in a fixed order.
  */
 #ifndef LSAM_OPS_H

@@ -51,6 +51,48 @@ inline bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
 }
 inline bool misaligned(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
 
+// An argument: `bytes` from the first to behind the last value; where it is blocks of `one` bytes each `step` bytes apart, as the
+// adapters of one vector per replica are, those too.
+struct Arg { const char* name; const void* p; int64_t bytes; int align; bool output; int64_t one, step; };
+inline bool meet(const Arg& a, const Arg& b) {
+  if (!a.p || !b.p || !overlap(a.p, a.bytes, b.p, b.bytes)) return false;
+  if (a.step > 0 && a.step == b.step) {
+    // blocks of both, in turn
+    const int64_t off = (int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p)) % a.step;
+    const int64_t at = off < 0 ? off + a.step : off;
+    return !(at >= a.one && at + b.one <= a.step);
+  }
+  return true;
+}
+// That arguments are there, aligned and not too large.
+inline int check_values(const Arg* args, int n, const char* who) {
+  for (int i = 0; i < n; ++i) {
+    if (args[i].bytes < 0) return refuse(LSAM_EINVAL, "%s: a stride of %s is too small, or the array is too large", who, args[i].name);
+    if (args[i].bytes && !args[i].p) return refuse(LSAM_EINVAL, "%s: %s is NULL", who, args[i].name);
+    if (misaligned(args[i].p, args[i].align)) return refuse(LSAM_EINVAL, "%s: %s is not aligned to its values", who, args[i].name);
+  }
+  return LSAM_OK;
+}
+// That no output lies over another argument.
+inline int check_apart(const Arg* args, int n, const char* who) {
+  for (int i = 0; i < n; ++i)
+    for (int j = 0; j < n; ++j)
+      if (i != j && args[i].output && meet(args[i], args[j]))
+        return refuse(LSAM_EINVAL, "%s: %s lies over %s", who, args[i].name, args[j].name);
+  return LSAM_OK;
+}
+// That the workspace is large enough, aligned, and apart from the arguments.
+inline int check_workspace(const Arg* args, int n, const void* workspace, size_t bytes, size_t need, int align, const char* who) {
+  if (!need) return LSAM_OK;
+  if (!workspace || bytes < need)
+    return refuse(LSAM_ENOMEM, "%s: the workspace has %zu bytes, %zu are needed", who, workspace ? bytes : 0, need);
+  if (misaligned(workspace, align)) return refuse(LSAM_EINVAL, "%s: the workspace must be %d-byte aligned", who, align);
+  for (int i = 0; i < n; ++i)
+    if (args[i].p && overlap(workspace, (int64_t)need, args[i].p, args[i].bytes))
+      return refuse(LSAM_EINVAL, "%s: the workspace lies over %s", who, args[i].name);
+  return LSAM_OK;
+}
+
 #if defined(__HIPCC__)
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));

@@ -1305,32 +1305,6 @@ int check(const lsam_adapter_desc* d, const char* who) {
   return LSAM_OK;
 }
 
-// An argument: `bytes` from the first to behind the last value; where it is blocks of `one` bytes each `step` bytes apart, as the
-// adapters of one vector per replica are, those too.
-struct Arg { const char* name; const void* p; int64_t bytes; int align; bool output; int64_t one, step; };
-bool meet(const Arg& a, const Arg& b) {
-  if (!a.p || !b.p || !overlap(a.p, a.bytes, b.p, b.bytes)) return false;
-  if (a.step > 0 && a.step == b.step) {
-    // blocks of both, in turn
-    const int64_t off = (int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p)) % a.step;
-    const int64_t at = off < 0 ? off + a.step : off;
-    return !(at >= a.one && at + b.one <= a.step);
-  }
-  return true;
-}
-int check_args(const Arg* args, int n, const char* who) {
-  for (int i = 0; i < n; ++i) {
-    if (args[i].bytes < 0) return refuse(LSAM_EINVAL, "%s: a stride of %s is too small, or the array is too large", who, args[i].name);
-    if (args[i].bytes && !args[i].p) return refuse(LSAM_EINVAL, "%s: %s is NULL", who, args[i].name);
-    if (misaligned(args[i].p, args[i].align)) return refuse(LSAM_EINVAL, "%s: %s is not aligned to its values", who, args[i].name);
-  }
-  for (int i = 0; i < n; ++i)
-    for (int j = 0; j < n; ++j)
-      if (i != j && args[i].output && meet(args[i], args[j]))
-        return refuse(LSAM_EINVAL, "%s: %s lies over %s", who, args[i].name, args[j].name);
-  return LSAM_OK;
-}
-
 template <int DTYPE, int ATYPE, bool UNIT, int NR, int RT>
 void launch_shrink_tile(const ShrinkParams& p, dim3 grid, bool staged, hipStream_t s) {
   constexpr int waves = kShrinkWaves<DTYPE, ATYPE, UNIT, NR, RT>;
@@ -1534,13 +1508,6 @@ Segments segments(const lsam_adapter_desc* d, const int32_t* begin, const int32_
   return g;
 }
 
-int check_workspace(size_t need, const void* workspace, size_t bytes, const char* who) {
-  if (need && (!workspace || bytes < need))
-    return refuse(LSAM_ENOMEM, "%s: the workspace has %zu bytes, %zu are needed", who, workspace ? bytes : 0, need);
-  if (need && misaligned(workspace, 256)) return refuse(LSAM_EINVAL, "%s: the workspace must be 256-byte aligned", who);
-  return LSAM_OK;
-}
-
 }  // namespace
 }  // namespace lsam
 
@@ -1567,10 +1534,11 @@ extern "C" int lsam_adapter(const lsam_adapter_desc* d, const void* x, const voi
       {"seg_adapter", seg_adapter, d->segs * 4ll, 4, false, 0, 0},
       {"u", u, d->rows * d->rank * 4, 4, true, 0, 0},
       {"y", y, extent(1, 0, d->rows, d->y_stride, d->out, b), b, true, 0, 0}};
-  rc = check_args(args, sizeof args / sizeof args[0], "adapter");
-  if (rc != LSAM_OK) return rc;
+  constexpr int n = sizeof args / sizeof args[0];
   Layout l = layout(d, false);
-  rc = check_workspace(l.total, workspace, workspace_bytes, "adapter");
+  rc = check_values(args, n, "adapter");
+  if (rc == LSAM_OK) rc = check_apart(args, n, "adapter");
+  if (rc == LSAM_OK) rc = check_workspace(args, n, workspace, workspace_bytes, l.total, 256, "adapter");
   if (rc != LSAM_OK) return rc;
   if (!l.copies && !(straight(x, d->x_stride, d->in, d->dtype) && straight(W, d->w_stride, d->in, d->dtype))) l.tiles = false;
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -1607,10 +1575,11 @@ extern "C" int lsam_adapter_backward(const lsam_adapter_desc* d, const void* x, 
        extent(1, 0, d->rank, d->da_stride, d->in, 4), d->adapters > 1 ? d->da_adapter * 4 : 0},
       {"dB", dB, dB && !apart(d->adapters, d->db_adapter, d->out, d->db_stride, d->rank) ? -1 : nb, 4, true,
        extent(1, 0, d->out, d->db_stride, d->rank, 4), d->adapters > 1 ? d->db_adapter * 4 : 0}};
-  rc = check_args(args, sizeof args / sizeof args[0], "adapter_backward");
-  if (rc != LSAM_OK) return rc;
+  constexpr int n = sizeof args / sizeof args[0];
   const Layout l = layout(d, true);
-  rc = check_workspace(l.total, workspace, workspace_bytes, "adapter_backward");
+  rc = check_values(args, n, "adapter_backward");
+  if (rc == LSAM_OK) rc = check_apart(args, n, "adapter_backward");
+  if (rc == LSAM_OK) rc = check_workspace(args, n, workspace, workspace_bytes, l.total, 256, "adapter_backward");
   if (rc != LSAM_OK) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const Segments g = segments(d, seg_begin, seg_adapter);

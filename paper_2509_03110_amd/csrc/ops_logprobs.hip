@@ -485,19 +485,21 @@ extern "C" size_t lsam_logprobs_workspace_bytes(const lsam_logprobs_desc* d) {
 extern "C" int lsam_logprobs(const lsam_logprobs_desc* d, const void* logits, const int32_t* tokens, float* logp, float* lse,
                              float* entropy, int32_t* top_ids, float* top_logp, void* workspace, size_t workspace_bytes,
                              void* stream) {
-  const int rc = check(d, "logprobs");
+  int rc = check(d, "logprobs");
   if (rc != LSAM_OK) return rc;
   if (d->rows == 0) return LSAM_OK;
-  if (!logits || !lse || !entropy || (tokens && !logp) || (d->top && (!top_ids || !top_logp)))
-    return refuse(LSAM_EINVAL, "logprobs: a NULL pointer");
-  if (misaligned(logits, dtype_bytes(d->dtype)) || misaligned(tokens, 4) || misaligned(logp, 4) || misaligned(lse, 4) ||
-      misaligned(entropy, 4) || misaligned(top_ids, 4) || misaligned(top_logp, 4))
-    return refuse(LSAM_EINVAL, "logprobs: a pointer is not aligned to its values");
+  const int bytes = dtype_bytes(d->dtype);
+  const int64_t column = d->rows * 4;
+  const Arg args[] = {{"logits", logits, extent(1, 0, d->rows, d->stride, d->vocab, bytes), bytes, false, 0, 0},
+                      {"tokens", tokens, tokens ? column : 0, 4, false, 0, 0}, {"logp", logp, tokens ? column : 0, 4, true, 0, 0},
+                      {"lse", lse, 2 * column, 4, true, 0, 0}, {"entropy", entropy, column, 4, true, 0, 0},
+                      {"top_ids", top_ids, column * d->top, 4, true, 0, 0}, {"top_logp", top_logp, column * d->top, 4, true, 0, 0}};
+  constexpr int n = sizeof args / sizeof args[0];
+  rc = check_values(args, n, "logprobs");
+  if (rc == LSAM_OK) rc = check_workspace(args, n, workspace, workspace_bytes, lsam_logprobs_workspace_bytes(d), 16, "logprobs");
+  if (rc == LSAM_OK) rc = check_apart(args, n, "logprobs");
+  if (rc != LSAM_OK) return rc;
   const Cut c = cut_rows(d->rows, d->vocab);
-  const size_t need = lsam_logprobs_workspace_bytes(d);
-  if (need && (!workspace || workspace_bytes < need))
-    return refuse(LSAM_ENOMEM, "logprobs: the workspace has %zu bytes, %zu are needed", workspace ? workspace_bytes : 0, need);
-  if (need && misaligned(workspace, 16)) return refuse(LSAM_EINVAL, "logprobs: the workspace must be 16-byte aligned");
   LogprobParams p;
   p.z = logits; p.stride = d->stride; p.rows = d->rows; p.V = d->vocab;
   p.tokens = tokens; p.logp = logp; p.lse = lse; p.entropy = entropy; p.ids = top_ids; p.best = top_logp;
@@ -518,19 +520,22 @@ extern "C" int lsam_logprobs(const lsam_logprobs_desc* d, const void* logits, co
 extern "C" int lsam_logprobs_backward(const lsam_logprobs_desc* d, const void* logits, const int32_t* tokens, const float* lse,
                                       const float* entropy, const float* g_logp, const float* g_entropy, void* dlogits,
                                       int64_t dlogits_stride, void* stream) {
-  const int rc = check(d, "logprobs_backward");
+  int rc = check(d, "logprobs_backward");
   if (rc != LSAM_OK) return rc;
   if (d->rows == 0) return LSAM_OK;
-  if (!logits || !lse || !entropy || !dlogits) return refuse(LSAM_EINVAL, "logprobs_backward: a NULL pointer");
   if (g_logp && !tokens) return refuse(LSAM_EINVAL, "logprobs_backward: g_logp without tokens");
   const int bytes = dtype_bytes(d->dtype);
-  const int64_t nz = extent(1, 0, d->rows, d->stride, d->vocab, bytes), nd = extent(1, 0, d->rows, dlogits_stride, d->vocab, bytes);
-  if (nd < 0) return refuse(LSAM_EINVAL, "logprobs_backward: the row stride of dlogits is below vocab, or the array is too large");
-  if (overlap(logits, nz, dlogits, nd) && !(logits == dlogits && (d->rows == 1 || d->stride == dlogits_stride)))
-    return refuse(LSAM_EINVAL, "logprobs_backward: dlogits lies over logits without being it");
-  if (misaligned(logits, bytes) || misaligned(dlogits, bytes) || misaligned(tokens, 4) || misaligned(lse, 4) ||
-      misaligned(entropy, 4) || misaligned(g_logp, 4) || misaligned(g_entropy, 4))
-    return refuse(LSAM_EINVAL, "logprobs_backward: a pointer is not aligned to its values");
+  const int64_t column = d->rows * 4, nd = extent(1, 0, d->rows, dlogits_stride, d->vocab, bytes);
+  const bool in_place = logits == dlogits && (d->rows == 1 || d->stride == dlogits_stride);
+  const Arg args[] = {{"dlogits", dlogits, nd, bytes, true, 0, 0},
+                      {"tokens", tokens, tokens ? column : 0, 4, false, 0, 0}, {"lse", lse, 2 * column, 4, false, 0, 0},
+                      {"entropy", entropy, column, 4, false, 0, 0}, {"g_logp", g_logp, g_logp ? column : 0, 4, false, 0, 0},
+                      {"g_entropy", g_entropy, g_entropy ? column : 0, 4, false, 0, 0},
+                      {"logits", logits, extent(1, 0, d->rows, d->stride, d->vocab, bytes), bytes, false, 0, 0}};
+  constexpr int n = sizeof args / sizeof args[0];
+  rc = check_values(args, n, "logprobs_backward");
+  if (rc == LSAM_OK) rc = check_apart(args, in_place ? n - 1 : n, "logprobs_backward");      // dlogits may be the logits themselves
+  if (rc != LSAM_OK) return rc;
   GradParams p;
   p.z = logits; p.stride = d->stride; p.dz = dlogits; p.dstride = dlogits_stride; p.V = d->vocab;
   p.pieces = (unsigned)((d->vocab + kGradStep - 1) / kGradStep);

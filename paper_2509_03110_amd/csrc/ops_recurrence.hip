@@ -440,20 +440,6 @@ int64_t spans(const lsam_recurrence_desc* d, const lsam_rows& t, bool output) {
   return extent(mats, t.seq, d->rows, t.stride, d->dim, dtype_bytes(d->dtype));
 }
 
-struct Arg { const char* name; const void* p; int64_t bytes; int align; bool output; };
-int check_args(const Arg* args, int n, const char* who) {
-  for (int i = 0; i < n; ++i) {
-    if (args[i].bytes < 0) return refuse(LSAM_EINVAL, "%s: a stride of %s is too small, or the array is too large", who, args[i].name);
-    if (args[i].bytes && !args[i].p) return refuse(LSAM_EINVAL, "%s: %s is NULL", who, args[i].name);
-    if (misaligned(args[i].p, args[i].align)) return refuse(LSAM_EINVAL, "%s: %s is not aligned to its values", who, args[i].name);
-  }
-  for (int i = 0; i < n; ++i)
-    for (int j = 0; j < n; ++j)
-      if (i != j && args[i].output && args[i].p && args[j].p && overlap(args[i].p, args[i].bytes, args[j].p, args[j].bytes))
-        return refuse(LSAM_EINVAL, "%s: %s lies over %s", who, args[i].name, args[j].name);
-  return LSAM_OK;
-}
-
 Tensor tensor(const void* p, const lsam_rows& r, bool packed) { return Tensor{p, r.stride, packed ? 0 : r.seq}; }
 
 template <int DTYPE, int NW, bool GRAD>
@@ -493,14 +479,6 @@ void launch_any(const RecurrenceParams& p, const lsam_recurrence_desc* d, int wa
   }
 }
 
-int check_workspace(const lsam_recurrence_desc* d, const void* workspace, size_t bytes, const char* who) {
-  const size_t need = lsam_recurrence_workspace_bytes(d);
-  if (need && (!workspace || bytes < need))
-    return refuse(LSAM_ENOMEM, "%s: the workspace has %zu bytes, %zu are needed", who, workspace ? bytes : 0, need);
-  if (need && misaligned(workspace, 16)) return refuse(LSAM_EINVAL, "%s: the workspace must be 16-byte aligned", who);
-  return LSAM_OK;
-}
-
 RecurrenceParams params(const lsam_recurrence_desc* d, const Plan& c, const int64_t* offsets, void* workspace) {
   RecurrenceParams p{};
   p.offsets = d->packed ? offsets : nullptr;
@@ -536,13 +514,14 @@ extern "C" int lsam_recurrence(const lsam_recurrence_desc* d, const int64_t* off
   const Plan c = plan(d);
   const int b = dtype_bytes(d->dtype);
   const int64_t state = d->seqs * d->dim * 4;
-  const Arg args[] = {{"f", f, spans(d, d->f, false), b, false}, {"x", x, spans(d, d->x, false), b, false},
-                      {"h", h, spans(d, d->h, true), b, true}, {"h0", h0, h0 ? state : 0, 4, false},
-                      {"last", last, last ? state : 0, 4, true}, {"states", states, states ? c.states * d->dim * 4 : 0, 4, true},
-                      {"offsets", d->packed ? offsets : nullptr, d->packed ? (d->seqs + 1) * 8 : 0, 8, false}};
-  rc = check_args(args, sizeof args / sizeof args[0], "recurrence");
-  if (rc != LSAM_OK) return rc;
-  rc = check_workspace(d, workspace, workspace_bytes, "recurrence");
+  const Arg args[] = {{"f", f, spans(d, d->f, false), b, false, 0, 0}, {"x", x, spans(d, d->x, false), b, false, 0, 0},
+                      {"h", h, spans(d, d->h, true), b, true, 0, 0}, {"h0", h0, h0 ? state : 0, 4, false, 0, 0},
+                      {"last", last, last ? state : 0, 4, true, 0, 0}, {"states", states, states ? c.states * d->dim * 4 : 0, 4, true, 0, 0},
+                      {"offsets", d->packed ? offsets : nullptr, d->packed ? (d->seqs + 1) * 8 : 0, 8, false, 0, 0}};
+  constexpr int n = sizeof args / sizeof args[0];
+  rc = check_values(args, n, "recurrence");
+  if (rc == LSAM_OK) rc = check_apart(args, n, "recurrence");
+  if (rc == LSAM_OK) rc = check_workspace(args, n, workspace, workspace_bytes, lsam_recurrence_workspace_bytes(d), 16, "recurrence");
   if (rc != LSAM_OK) return rc;
   RecurrenceParams p = params(d, c, offsets, workspace);
   p.f = tensor(f, d->f, d->packed); p.x = tensor(x, d->x, d->packed); p.h = tensor(h, d->h, d->packed);
@@ -562,15 +541,16 @@ extern "C" int lsam_recurrence_backward(const lsam_recurrence_desc* d, const int
   const Plan c = plan(d);
   const int b = dtype_bytes(d->dtype);
   const int64_t state = d->seqs * d->dim * 4;
-  const Arg args[] = {{"f", f, spans(d, d->f, false), b, false}, {"x", x, spans(d, d->x, false), b, false},
-                      {"dh", dh, spans(d, d->dh, false), b, false}, {"df", df, spans(d, d->df, true), b, true},
-                      {"dx", dx, spans(d, d->dx, true), b, true}, {"h0", h0, h0 ? state : 0, 4, false},
-                      {"dlast", dlast, dlast ? state : 0, 4, false}, {"dh0", dh0, dh0 ? state : 0, 4, true},
-                      {"states", states, c.states * d->dim * 4, 4, false},
-                      {"offsets", d->packed ? offsets : nullptr, d->packed ? (d->seqs + 1) * 8 : 0, 8, false}};
-  rc = check_args(args, sizeof args / sizeof args[0], "recurrence_backward");
-  if (rc != LSAM_OK) return rc;
-  rc = check_workspace(d, workspace, workspace_bytes, "recurrence_backward");
+  const Arg args[] = {{"f", f, spans(d, d->f, false), b, false, 0, 0}, {"x", x, spans(d, d->x, false), b, false, 0, 0},
+                      {"dh", dh, spans(d, d->dh, false), b, false, 0, 0}, {"df", df, spans(d, d->df, true), b, true, 0, 0},
+                      {"dx", dx, spans(d, d->dx, true), b, true, 0, 0}, {"h0", h0, h0 ? state : 0, 4, false, 0, 0},
+                      {"dlast", dlast, dlast ? state : 0, 4, false, 0, 0}, {"dh0", dh0, dh0 ? state : 0, 4, true, 0, 0},
+                      {"states", states, c.states * d->dim * 4, 4, false, 0, 0},
+                      {"offsets", d->packed ? offsets : nullptr, d->packed ? (d->seqs + 1) * 8 : 0, 8, false, 0, 0}};
+  constexpr int n = sizeof args / sizeof args[0];
+  rc = check_values(args, n, "recurrence_backward");
+  if (rc == LSAM_OK) rc = check_apart(args, n, "recurrence_backward");
+  if (rc == LSAM_OK) rc = check_workspace(args, n, workspace, workspace_bytes, lsam_recurrence_workspace_bytes(d), 16, "recurrence_backward");
   if (rc != LSAM_OK) return rc;
   RecurrenceParams p = params(d, c, offsets, workspace);
   p.f = tensor(f, d->f, d->packed); p.x = tensor(x, d->x, d->packed); p.dh = tensor(dh, d->dh, d->packed);
