@@ -51,17 +51,42 @@ inline bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
 }
 inline bool misaligned(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
 
-// An argument: `bytes` from the first to behind the last value; where it is blocks of `one` bytes each `step` bytes apart, as the
-// adapters of one vector per replica are, those too.
-struct Arg { const char* name; const void* p; int64_t bytes; int align; bool output; int64_t one, step; };
+// An argument: `bytes` from the first to behind the last value, in blocks of `one` bytes whose starts are multiples of `step` apart
+// (0: it is one block), the rows of a part of wider rows, say; and, coarser, in blocks of `many` bytes `far` apart, as the
+// factors of one vector per replica are.
+struct Arg {
+  const char* name; const void* p; int64_t bytes; int align; bool output;
+  int64_t one = 0, step = 0, many = 0, far = 0;
+};
+inline int64_t common(int64_t a, int64_t b) {
+  while (b) { const int64_t r = a % b; a = b; b = r; }
+  return a;
+}
+// The same for `mats` matrices of `rows` rows, from their first to behind their last value.
+inline Arg matrices(const char* name, const void* p, int64_t mats, int64_t mat_stride, int64_t rows, int64_t stride, int64_t cols, int bytes,
+                    bool output) {
+  Arg a{name, p, extent(mats, mat_stride, rows, stride, cols, bytes), bytes, output};
+  if (a.bytes <= 0) return a;
+  const int64_t apart = mats > 1 ? mat_stride * bytes : 0;
+  a.one = cols * bytes;
+  a.step = common(apart, rows > 1 ? stride * bytes : 0);
+  a.many = extent(1, 0, rows, stride, cols, bytes);
+  a.far = apart;
+  return a;
+}
+// Whether two arguments have a byte in common; where blocks of different strides go through each other, whether they might.
 inline bool meet(const Arg& a, const Arg& b) {
   if (!a.p || !b.p || !overlap(a.p, a.bytes, b.p, b.bytes)) return false;
-  if (a.step > 0 && a.step == b.step) {
-    // blocks of both, in turn
-    const int64_t off = (int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p)) % a.step;
-    const int64_t at = off < 0 ? off + a.step : off;
-    return !(at >= a.one && at + b.one <= a.step);
-  }
+  // blocks of both in turn: all of a's begin at the same place of every g bytes, all of b's at another, and none reaches the other's
+  const int64_t size[2][2] = {{a.one, a.many}, {b.one, b.many}}, step[2][2] = {{a.step, a.far}, {b.step, b.far}};
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2; ++j) {
+      const int64_t g = common(step[0][i], step[1][j]), m = size[0][i], n = size[1][j];
+      if (!g || !m || !n) continue;
+      const int64_t off = (int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p)) % g;
+      const int64_t at = off < 0 ? off + g : off;
+      if (at >= m && at + n <= g) return false;
+    }
   return true;
 }
 // That arguments are there, aligned and not too large.
@@ -88,7 +113,7 @@ inline int check_workspace(const Arg* args, int n, const void* workspace, size_t
     return refuse(LSAM_ENOMEM, "%s: the workspace has %zu bytes, %zu are needed", who, workspace ? bytes : 0, need);
   if (misaligned(workspace, align)) return refuse(LSAM_EINVAL, "%s: the workspace must be %d-byte aligned", who, align);
   for (int i = 0; i < n; ++i)
-    if (args[i].p && overlap(workspace, (int64_t)need, args[i].p, args[i].bytes))
+    if (meet(Arg{"", workspace, (int64_t)need, align, true}, args[i]))
       return refuse(LSAM_EINVAL, "%s: the workspace lies over %s", who, args[i].name);
   return LSAM_OK;
 }

@@ -1525,15 +1525,15 @@ extern "C" int lsam_adapter(const lsam_adapter_desc* d, const void* x, const voi
   if (d->rows == 0) return LSAM_OK;
   const int b = dtype_bytes(d->dtype), ba = dtype_bytes(d->adapter_dtype);
   const Arg args[] = {
-      {"x", x, extent(1, 0, d->rows, d->x_stride, d->in, b), b, false, 0, 0},
-      {"W", W, extent(1, 0, d->out, d->w_stride, d->in, b), b, false, 0, 0},
-      {"bias", bias, bias ? d->out * 4ll : 0, 4, false, 0, 0},
-      {"A", A, extent(d->adapters, d->a_adapter, d->rank, d->a_stride, d->in, ba), ba, false, 0, 0},
-      {"B", B, extent(d->adapters, d->b_adapter, d->out, d->b_stride, d->rank, ba), ba, false, 0, 0},
-      {"seg_begin", seg_begin, d->segs ? (d->segs + 1) * 4ll : 0, 4, false, 0, 0},
-      {"seg_adapter", seg_adapter, d->segs * 4ll, 4, false, 0, 0},
-      {"u", u, d->rows * d->rank * 4, 4, true, 0, 0},
-      {"y", y, extent(1, 0, d->rows, d->y_stride, d->out, b), b, true, 0, 0}};
+      matrices("x", x, 1, 0, d->rows, d->x_stride, d->in, b, false),
+      matrices("W", W, 1, 0, d->out, d->w_stride, d->in, b, false),
+      {"bias", bias, bias ? d->out * 4ll : 0, 4, false},
+      matrices("A", A, d->adapters, d->a_adapter, d->rank, d->a_stride, d->in, ba, false),
+      matrices("B", B, d->adapters, d->b_adapter, d->out, d->b_stride, d->rank, ba, false),
+      {"seg_begin", seg_begin, d->segs ? (d->segs + 1) * 4ll : 0, 4, false},
+      {"seg_adapter", seg_adapter, d->segs * 4ll, 4, false},
+      {"u", u, d->rows * d->rank * 4, 4, true},
+      matrices("y", y, 1, 0, d->rows, d->y_stride, d->out, b, true)};
   constexpr int n = sizeof args / sizeof args[0];
   Layout l = layout(d, false);
   rc = check_values(args, n, "adapter");
@@ -1559,22 +1559,20 @@ extern "C" int lsam_adapter_backward(const lsam_adapter_desc* d, const void* x, 
   if (rc != LSAM_OK) return rc;
   if ((dA == nullptr) != (dB == nullptr)) return refuse(LSAM_EINVAL, "adapter_backward: dA and dB are wanted together");
   const int b = dtype_bytes(d->dtype), ba = dtype_bytes(d->adapter_dtype);
-  const int64_t na = dA ? extent(d->adapters, d->da_adapter, d->rank, d->da_stride, d->in, 4) : 0;
-  const int64_t nb = dB ? extent(d->adapters, d->db_adapter, d->out, d->db_stride, d->rank, 4) : 0;
-  const Arg args[] = {
-      {"x", x, dA ? extent(1, 0, d->rows, d->x_stride, d->in, b) : 0, b, false, 0, 0},
-      {"W", W, dx && d->rows ? extent(1, 0, d->out, d->w_stride, d->in, b) : 0, b, false, 0, 0},
-      {"A", A, d->rows ? extent(d->adapters, d->a_adapter, d->rank, d->a_stride, d->in, ba) : 0, ba, false, 0, 0},
-      {"B", B, d->rows ? extent(d->adapters, d->b_adapter, d->out, d->b_stride, d->rank, ba) : 0, ba, false, 0, 0},
-      {"seg_begin", seg_begin, d->segs ? (d->segs + 1) * 4ll : 0, 4, false, 0, 0},
-      {"seg_adapter", seg_adapter, d->segs * 4ll, 4, false, 0, 0},
-      {"u", u, dA ? d->rows * d->rank * 4 : 0, 4, false, 0, 0},
-      {"dy", dy, extent(1, 0, d->rows, d->dy_stride, d->out, b), b, false, 0, 0},
-      {"dx", dx, dx ? extent(1, 0, d->rows, d->dx_stride, d->in, b) : 0, b, true, 0, 0},
-      {"dA", dA, dA && !apart(d->adapters, d->da_adapter, d->rank, d->da_stride, d->in) ? -1 : na, 4, true,
-       extent(1, 0, d->rank, d->da_stride, d->in, 4), d->adapters > 1 ? d->da_adapter * 4 : 0},
-      {"dB", dB, dB && !apart(d->adapters, d->db_adapter, d->out, d->db_stride, d->rank) ? -1 : nb, 4, true,
-       extent(1, 0, d->out, d->db_stride, d->rank, 4), d->adapters > 1 ? d->db_adapter * 4 : 0}};
+  Arg args[] = {
+      matrices("x", x, 1, 0, dA ? d->rows : 0, d->x_stride, d->in, b, false),
+      matrices("W", W, 1, 0, dx && d->rows ? d->out : 0, d->w_stride, d->in, b, false),
+      matrices("A", A, d->rows ? d->adapters : 0, d->a_adapter, d->rank, d->a_stride, d->in, ba, false),
+      matrices("B", B, d->rows ? d->adapters : 0, d->b_adapter, d->out, d->b_stride, d->rank, ba, false),
+      {"seg_begin", seg_begin, d->segs ? (d->segs + 1) * 4ll : 0, 4, false},
+      {"seg_adapter", seg_adapter, d->segs * 4ll, 4, false},
+      {"u", u, dA ? d->rows * d->rank * 4 : 0, 4, false},
+      matrices("dy", dy, 1, 0, d->rows, d->dy_stride, d->out, b, false),
+      matrices("dx", dx, 1, 0, dx ? d->rows : 0, d->dx_stride, d->in, b, true),
+      matrices("dA", dA, dA ? d->adapters : 0, d->da_adapter, d->rank, d->da_stride, d->in, 4, true),
+      matrices("dB", dB, dB ? d->adapters : 0, d->db_adapter, d->out, d->db_stride, d->rank, 4, true)};
+  if (dA && !apart(d->adapters, d->da_adapter, d->rank, d->da_stride, d->in)) args[9].bytes = -1;
+  if (dB && !apart(d->adapters, d->db_adapter, d->out, d->db_stride, d->rank)) args[10].bytes = -1;
   constexpr int n = sizeof args / sizeof args[0];
   const Layout l = layout(d, true);
   rc = check_values(args, n, "adapter_backward");

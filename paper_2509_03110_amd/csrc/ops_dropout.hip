@@ -76,22 +76,21 @@ extern "C" int lsam_dropout(const lsam_dropout_desc* d, const void* x, const voi
   if (d->site > 65535 || (uint64_t)d->first_replica + (uint64_t)d->replicas > 65536)
     return refuse(LSAM_EINVAL, "dropout: site and replicas must be below 65536");
   if (d->replicas == 0 || d->rows == 0 || d->cols == 0) return LSAM_OK;
-  if (!x || !y) return refuse(LSAM_EINVAL, "dropout: x or y is NULL");
   const int bytes = dtype_bytes(d->dtype);
-  const int64_t nx = extent(d->replicas, d->x_replica, d->rows, d->x_stride, d->cols, bytes);
-  const int64_t nr = residual ? extent(d->replicas, d->residual_replica, d->rows, d->residual_stride, d->cols, bytes) : 0;
-  const int64_t ny = extent(d->replicas, d->y_replica, d->rows, d->y_stride, d->cols, bytes);
   const bool many = d->replicas > 1, tall = d->rows > 1;
-  if (nx < 0 || nr < 0 || ny < 0) return refuse(LSAM_EINVAL, "dropout: a row stride is below cols, or an array is too large");
+  const Arg args[] = {matrices("x", x, d->replicas, d->x_replica, d->rows, d->x_stride, d->cols, bytes, false),
+                      matrices("y", y, d->replicas, d->y_replica, d->rows, d->y_stride, d->cols, bytes, true),
+                      matrices("the residual", residual, residual ? d->replicas : 0, d->residual_replica, d->rows, d->residual_stride,
+                               d->cols, bytes, false)};
+  const int rc = check_values(args, 3, "dropout");
+  if (rc != LSAM_OK) return rc;
   if (!apart(d->replicas, d->y_replica, d->rows, d->y_stride, d->cols))
     return refuse(LSAM_EINVAL, "dropout: the replicas of y lie over each other");
-  if (overlap(x, nx, y, ny) && !(x == y && (!tall || d->x_stride == d->y_stride) && (!many || d->x_replica == d->y_replica)))
+  if (meet(args[0], args[1]) && !(x == y && (!tall || d->x_stride == d->y_stride) && (!many || d->x_replica == d->y_replica)))
     return refuse(LSAM_EINVAL, "dropout: y lies over x without being x");
-  if (overlap(residual, nr, y, ny) &&
+  if (meet(args[2], args[1]) &&
       !(residual == y && (!tall || d->residual_stride == d->y_stride) && (!many || d->residual_replica == d->y_replica)))
     return refuse(LSAM_EINVAL, "dropout: y lies over the residual without being it");
-  if (misaligned(x, bytes) || misaligned(y, bytes) || misaligned(residual, bytes))
-    return refuse(LSAM_EINVAL, "dropout: a pointer is not aligned to its values");
 
   DropoutParams p;
   p.x = x; p.residual = residual; p.y = y;

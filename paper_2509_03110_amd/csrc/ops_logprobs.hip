@@ -490,10 +490,10 @@ extern "C" int lsam_logprobs(const lsam_logprobs_desc* d, const void* logits, co
   if (d->rows == 0) return LSAM_OK;
   const int bytes = dtype_bytes(d->dtype);
   const int64_t column = d->rows * 4;
-  const Arg args[] = {{"logits", logits, extent(1, 0, d->rows, d->stride, d->vocab, bytes), bytes, false, 0, 0},
-                      {"tokens", tokens, tokens ? column : 0, 4, false, 0, 0}, {"logp", logp, tokens ? column : 0, 4, true, 0, 0},
-                      {"lse", lse, 2 * column, 4, true, 0, 0}, {"entropy", entropy, column, 4, true, 0, 0},
-                      {"top_ids", top_ids, column * d->top, 4, true, 0, 0}, {"top_logp", top_logp, column * d->top, 4, true, 0, 0}};
+  const Arg args[] = {matrices("logits", logits, 1, 0, d->rows, d->stride, d->vocab, bytes, false),
+                      {"tokens", tokens, tokens ? column : 0, 4, false}, {"logp", logp, tokens ? column : 0, 4, true},
+                      {"lse", lse, 2 * column, 4, true}, {"entropy", entropy, column, 4, true},
+                      {"top_ids", top_ids, column * d->top, 4, true}, {"top_logp", top_logp, column * d->top, 4, true}};
   constexpr int n = sizeof args / sizeof args[0];
   rc = check_values(args, n, "logprobs");
   if (rc == LSAM_OK) rc = check_workspace(args, n, workspace, workspace_bytes, lsam_logprobs_workspace_bytes(d), 16, "logprobs");
@@ -525,13 +525,13 @@ extern "C" int lsam_logprobs_backward(const lsam_logprobs_desc* d, const void* l
   if (d->rows == 0) return LSAM_OK;
   if (g_logp && !tokens) return refuse(LSAM_EINVAL, "logprobs_backward: g_logp without tokens");
   const int bytes = dtype_bytes(d->dtype);
-  const int64_t column = d->rows * 4, nd = extent(1, 0, d->rows, dlogits_stride, d->vocab, bytes);
+  const int64_t column = d->rows * 4;
   const bool in_place = logits == dlogits && (d->rows == 1 || d->stride == dlogits_stride);
-  const Arg args[] = {{"dlogits", dlogits, nd, bytes, true, 0, 0},
-                      {"tokens", tokens, tokens ? column : 0, 4, false, 0, 0}, {"lse", lse, 2 * column, 4, false, 0, 0},
-                      {"entropy", entropy, column, 4, false, 0, 0}, {"g_logp", g_logp, g_logp ? column : 0, 4, false, 0, 0},
-                      {"g_entropy", g_entropy, g_entropy ? column : 0, 4, false, 0, 0},
-                      {"logits", logits, extent(1, 0, d->rows, d->stride, d->vocab, bytes), bytes, false, 0, 0}};
+  const Arg args[] = {matrices("dlogits", dlogits, 1, 0, d->rows, dlogits_stride, d->vocab, bytes, true),
+                      {"tokens", tokens, tokens ? column : 0, 4, false}, {"lse", lse, 2 * column, 4, false},
+                      {"entropy", entropy, column, 4, false}, {"g_logp", g_logp, g_logp ? column : 0, 4, false},
+                      {"g_entropy", g_entropy, g_entropy ? column : 0, 4, false},
+                      matrices("logits", logits, 1, 0, d->rows, d->stride, d->vocab, bytes, false)};
   constexpr int n = sizeof args / sizeof args[0];
   rc = check_values(args, n, "logprobs_backward");
   if (rc == LSAM_OK) rc = check_apart(args, in_place ? n - 1 : n, "logprobs_backward");      // dlogits may be the logits themselves

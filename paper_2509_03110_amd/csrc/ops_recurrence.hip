@@ -433,11 +433,12 @@ int check(const lsam_recurrence_desc* d, const char* who) {
   return LSAM_OK;
 }
 
-// The bytes that a tensor spans (-1: refused), sequences of an output apart from each other.
-int64_t spans(const lsam_recurrence_desc* d, const lsam_rows& t, bool output) {
+// A tensor as an argument; sequences of an output have to lie apart from each other.
+Arg arg(const lsam_recurrence_desc* d, const char* name, const void* p, const lsam_rows& t, bool output) {
   const int64_t mats = d->packed ? 1 : d->seqs;
-  if (output && !apart(mats, t.seq, d->rows, t.stride, d->dim)) return -1;
-  return extent(mats, t.seq, d->rows, t.stride, d->dim, dtype_bytes(d->dtype));
+  Arg a = matrices(name, p, mats, t.seq, d->rows, t.stride, d->dim, dtype_bytes(d->dtype), output);
+  if (output && !apart(mats, t.seq, d->rows, t.stride, d->dim)) a.bytes = -1;
+  return a;
 }
 
 Tensor tensor(const void* p, const lsam_rows& r, bool packed) { return Tensor{p, r.stride, packed ? 0 : r.seq}; }
@@ -512,12 +513,11 @@ extern "C" int lsam_recurrence(const lsam_recurrence_desc* d, const int64_t* off
   if (d->seqs == 0) return LSAM_OK;
   if (d->packed && !offsets) return refuse(LSAM_EINVAL, "recurrence: packed sequences need offsets");
   const Plan c = plan(d);
-  const int b = dtype_bytes(d->dtype);
   const int64_t state = d->seqs * d->dim * 4;
-  const Arg args[] = {{"f", f, spans(d, d->f, false), b, false, 0, 0}, {"x", x, spans(d, d->x, false), b, false, 0, 0},
-                      {"h", h, spans(d, d->h, true), b, true, 0, 0}, {"h0", h0, h0 ? state : 0, 4, false, 0, 0},
-                      {"last", last, last ? state : 0, 4, true, 0, 0}, {"states", states, states ? c.states * d->dim * 4 : 0, 4, true, 0, 0},
-                      {"offsets", d->packed ? offsets : nullptr, d->packed ? (d->seqs + 1) * 8 : 0, 8, false, 0, 0}};
+  const Arg args[] = {arg(d, "f", f, d->f, false), arg(d, "x", x, d->x, false),
+                      arg(d, "h", h, d->h, true), {"h0", h0, h0 ? state : 0, 4, false},
+                      {"last", last, last ? state : 0, 4, true}, {"states", states, states ? c.states * d->dim * 4 : 0, 4, true},
+                      {"offsets", d->packed ? offsets : nullptr, d->packed ? (d->seqs + 1) * 8 : 0, 8, false}};
   constexpr int n = sizeof args / sizeof args[0];
   rc = check_values(args, n, "recurrence");
   if (rc == LSAM_OK) rc = check_apart(args, n, "recurrence");
@@ -539,14 +539,13 @@ extern "C" int lsam_recurrence_backward(const lsam_recurrence_desc* d, const int
   if (d->seqs == 0) return LSAM_OK;
   if (d->packed && !offsets) return refuse(LSAM_EINVAL, "recurrence_backward: packed sequences need offsets");
   const Plan c = plan(d);
-  const int b = dtype_bytes(d->dtype);
   const int64_t state = d->seqs * d->dim * 4;
-  const Arg args[] = {{"f", f, spans(d, d->f, false), b, false, 0, 0}, {"x", x, spans(d, d->x, false), b, false, 0, 0},
-                      {"dh", dh, spans(d, d->dh, false), b, false, 0, 0}, {"df", df, spans(d, d->df, true), b, true, 0, 0},
-                      {"dx", dx, spans(d, d->dx, true), b, true, 0, 0}, {"h0", h0, h0 ? state : 0, 4, false, 0, 0},
-                      {"dlast", dlast, dlast ? state : 0, 4, false, 0, 0}, {"dh0", dh0, dh0 ? state : 0, 4, true, 0, 0},
-                      {"states", states, c.states * d->dim * 4, 4, false, 0, 0},
-                      {"offsets", d->packed ? offsets : nullptr, d->packed ? (d->seqs + 1) * 8 : 0, 8, false, 0, 0}};
+  const Arg args[] = {arg(d, "f", f, d->f, false), arg(d, "x", x, d->x, false),
+                      arg(d, "dh", dh, d->dh, false), arg(d, "df", df, d->df, true),
+                      arg(d, "dx", dx, d->dx, true), {"h0", h0, h0 ? state : 0, 4, false},
+                      {"dlast", dlast, dlast ? state : 0, 4, false}, {"dh0", dh0, dh0 ? state : 0, 4, true},
+                      {"states", states, c.states * d->dim * 4, 4, false},
+                      {"offsets", d->packed ? offsets : nullptr, d->packed ? (d->seqs + 1) * 8 : 0, 8, false}};
   constexpr int n = sizeof args / sizeof args[0];
   rc = check_values(args, n, "recurrence_backward");
   if (rc == LSAM_OK) rc = check_apart(args, n, "recurrence_backward");
