@@ -4,7 +4,8 @@ Tensors are checked for what the C boundary cannot see (device, type, shape, con
 as they lie, strides included.  Outputs that are not given are allocated on the stream that the call runs on: the
 current stream of x's device, or `stream` (a torch.cuda.Stream).  As with any torch operation, inputs that were made
 on another stream have to be ready on this one, and tensors that are dropped while another stream still reads them
-need record_stream.  Gradients are entry points of their own; nothing here records for autograd.
+need record_stream.  Gradients are entry points of their own; nothing here records for autograd, and tensors that require
+a gradient are refused while torch records (torch.no_grad(), or detach() them).
 """
 from __future__ import annotations
 
@@ -114,6 +115,8 @@ def _expect(t, what, like=None, shape=None, dtype=None, dense=False):
     """Whether `t` is a tensor of that device, shape and type with a contiguous last index (dense: all of it)."""
     if not t.is_cuda:
         _refuse("%s is not on a GPU" % what)
+    if t.requires_grad and torch.is_grad_enabled():
+        _refuse("%s requires a gradient, which this call does not record: see its backward call, and torch.no_grad()" % what)
     if like is not None and t.device != like.device:
         _refuse("%s is on %s, not on %s" % (what, t.device, like.device))
     if shape is not None and t.shape != shape:
