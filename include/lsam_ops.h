@@ -64,9 +64,10 @@ int lsam_dropout(const lsam_dropout_desc* d, const void* x, const void* residual
  *           tokens [device] [rows] int32, or NULL: logp is not written
  *   top_ids, top_logp [device] [rows, top]: the `top` largest logits' indices and log probabilities, the largest first, the
  *           lowest index first among equals.  May be NULL where top = 0
- * A logit of -inf is barred: probability 0, gradient 0, never an alternative; where fewer than `top` are left the
- * rest is index -1, log probability -inf.  A row with every logit barred has lse (-inf, 0), entropy 0, logp -inf and
- * no gradient.  NaN or +inf in a row makes its lse, entropy and log probabilities NaN.
+ * A logit of -inf is barred: probability 0, never an alternative, gradient 0 unless it is the row's own token (whose logp is
+ * -inf, and whose logit receives g_logp as the formula below has it).  Where fewer than `top` are left the rest is index -1,
+ * log probability -inf.  A row with every logit barred has lse (-inf, 0), entropy 0, logp -inf and no gradient.  NaN or +inf in
+ * a row makes its lse, entropy and log probabilities NaN.
  * workspace [device, 16-byte aligned], lsam_logprobs_workspace_bytes(d) bytes (0 where rows fill the chip; also 0, with a
  * message, for a descriptor that is refused); nothing in it has to survive the call. */
 #define LSAM_TOP_MAX 32

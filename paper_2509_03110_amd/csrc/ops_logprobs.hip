@@ -409,7 +409,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(GradParams p) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float ln = x[j][e] - lo, q = power(ln);
-        x[j][e] = q == 0.f ? 0.f : -q * __builtin_fmaf(h, ln + H, g);      // a barred logit has no gradient, nor has a row of them
+        x[j][e] = q == 0.f ? 0.f : -q * __builtin_fmaf(h, ln + H, g);      // nothing for a barred logit or a row of them
       }
     } else {
 #pragma unroll
