@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from paper_2509_03110_amd import ops
+from test_gpu_dropout import philox
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -73,3 +74,44 @@ def test_copies_of_more_numbers_than_a_launch_has_lanes_for():
     y, u = ops.adapter(x, W, A, B, sb, which, 1.0)
     assert torch.equal(y[marked, 0].float(), torch.tensor([129.0, 129, 129, 129, 258], device=DEV).to(B16).float())
     assert int((y != 0).sum()) == 5 and int((u != 0).sum()) == 1
+
+
+def test_log_probabilities_of_more_rows_than_a_launch_takes():
+    rows, V = (1 << 23) + 37, 3
+    g = torch.Generator(device=DEV).manual_seed(3)
+    z = torch.randn(rows, V, device=DEV, generator=g)
+    tokens = torch.randint(0, V, (rows,), device=DEV, generator=g, dtype=torch.int32)
+    r = ops.logprobs(z, tokens, top=2)
+    gl, ge = torch.randn(rows, device=DEV, generator=g), torch.randn(rows, device=DEV, generator=g)
+    dz = ops.logprobs_backward(z, tokens, r.lse, r.entropy, gl, ge)
+    for rows_of in (slice(0, 50), slice((1 << 23) - 50, rows)):
+        part = ops.logprobs(z[rows_of], tokens[rows_of], top=2)
+        for p, q in zip(r, part):
+            assert torch.equal(p[rows_of], q)
+        assert torch.equal(dz[rows_of], ops.logprobs_backward(z[rows_of], tokens[rows_of], part.lse, part.entropy, gl[rows_of], ge[rows_of]))
+
+
+@pytest.mark.parametrize("length", [1, 2, 20])
+def test_more_sequences_than_a_launch_takes(length):
+    # workgroups of one wavefront: 2^22 - 8 sequences a launch; of eight: 2^19 - 8
+    S = (1 << 22) + 11 if length < 20 else (1 << 19) + 11
+    g = torch.Generator(device=DEV).manual_seed(4)
+    n = lambda *s: torch.randn(*s, device=DEV, generator=g)  # noqa: E731
+    f, x, dh = (n(S, length, 1) for _ in range(3))
+    h0, dlast = n(S, 1), n(S, 1)
+    r = ops.recurrence(f, x, h0=h0, save=True)
+    got = (r.h, r.last) + ops.recurrence_backward(f, x, dh, r.states, h0=h0, dlast=dlast)
+    for part in (slice(0, 300), slice(S - 300, S)):
+        q = ops.recurrence(f[part], x[part], h0=h0[part], save=True)
+        want = (q.h, q.last) + ops.recurrence_backward(f[part], x[part], dh[part], q.states, h0=h0[part], dlast=dlast[part])
+        assert all(torch.equal(p[part], w) for p, w in zip(got, want))
+
+
+def test_dropout_of_more_pieces_than_a_launch_takes():
+    need(14)
+    rows, step, site = (1 << 31) - 1, 4, 2                  # a launch takes 2^31 - 256 pieces, a row of one column each
+    x = torch.ones(rows, 1, device=DEV, dtype=B16)
+    y = ops.dropout(x, 0.5, 3, step, site=site)
+    for lo in (0, (1 << 31) - 456, rows - 200):
+        keep = [philox((0, r, site, step), (3, 0))[0] & 0xFFFF >= 1 << 15 for r in range(lo, lo + 200)]
+        assert y[lo:lo + 200, 0].tolist() == [2.0 if k else 0.0 for k in keep]
