@@ -120,23 +120,17 @@ inline int check_workspace(const Arg* args, int n, const void* workspace, size_t
 
 #if defined(__HIPCC__)
 
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned short u16x4 __attribute__((ext_vector_type(4)));
 typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 // Global memory takes wide accesses at any address that a value may have.
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
-typedef f32x2 f32x2_any __attribute__((aligned(4)));
 typedef u16x8 u16x8_any __attribute__((aligned(2)));
 typedef u16x4 u16x4_any __attribute__((aligned(2)));
-typedef u16x2 u16x2_any __attribute__((aligned(2)));
 
 __device__ __forceinline__ float widen(unsigned short b) { return __builtin_bit_cast(float, (unsigned)b << 16); }
 __device__ __forceinline__ unsigned short narrow(float f) { return __builtin_bit_cast(unsigned short, static_cast<__bf16>(f)); }

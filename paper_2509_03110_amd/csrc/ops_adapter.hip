@@ -53,18 +53,16 @@ __device__ __forceinline__ int seg_copy(const Segments& g, int s) {
   const int a = seg_adapter(g, s);
   return a >= 0 && g.each ? s : a;
 }
-// The adapter of a row, another row in every lane; `begin` may be a copy of the segments'.
-__device__ __forceinline__ int row_adapter(const Segments& g, const int* begin, int64_t row, int64_t rows) {
+// The adapter of a row, another row in every lane.
+__device__ __forceinline__ int row_adapter(const Segments& g, int64_t row, int64_t rows) {
   int lo = 0, hi = g.n;
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;
-    if (begin[mid] <= row) lo = mid + 1; else hi = mid;
+    if (g.begin[mid] <= row) lo = mid + 1; else hi = mid;
   }
-  const int64_t end = lo > 0 ? begin[lo] : 0;
-  return lo > 0 && row < (end > rows ? rows : end) ? seg_adapter(g, lo - 1) : -1;
+  return lo > 0 && row < seg_row(g, lo, rows) ? seg_adapter(g, lo - 1) : -1;
 }
 
-template <int N> struct Count { static constexpr int value = N; };
 // What is written above stays above: a run of loads goes out before the first of them is waited for.
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
 
@@ -210,11 +208,9 @@ struct Lines {
   static constexpr int BYTES = ROWS * 128 * EACH, NLOAD = ROWS / 8 * EACH;
   static constexpr int B = DTYPE == LSAM_DTYPE_BF16 ? 2 : 4;
   unsigned goff[ROWS / 8];
-  int k;
   __device__ __forceinline__ void init(int64_t stride, int lane) {
 #pragma unroll
     for (int j = 0; j < ROWS / 8; ++j) goff[j] = (unsigned)((j * 8 + (lane >> 3)) * stride * B);
-    k = 0;
   }
   // Rows past the resource's end and units past K arrive as zeros.
   __device__ __forceinline__ void issue(__amdgpu_buffer_rsrc_t rsrc, lds_byte* tile, int k0, int K, int lane) const {
@@ -480,7 +476,7 @@ __global__ __launch_bounds__(WAVES * 64) void shrink_kernel(ShrinkParams p) {
     // the last one: adapters of rows, and the rows without one (a search that the others need not wait for)
     for (int i = tid; i < ROWS; i += WAVES * 64) {
       if (row0 + i >= row1) break;
-      const int a = row_adapter(p.g, p.g.begin, row0 + i, p.rows);
+      const int a = row_adapter(p.g, row0 + i, p.rows);
       if (p.adapter) p.adapter[row0 + i] = a;
       if (a < 0)
         for (int r = 0; r < p.rank; ++r) p.u[(row0 + i) * p.rank + r] = 0.f;
