@@ -451,7 +451,7 @@ constexpr int kShrinkWaves = waves_for(kStageBytes<ATYPE, DTYPE, UNIT, NR, RT>);
 
 // Workgroup (tile, j, r): ranks 16 NR r and on of the j-th, j + groups-th, ... segment of the tile's 16 RT rows, the contraction
 // cut over its wavefronts.  Bound by reading x where segments are long (16384 x 4096 bf16, 134 MB, rank 16 with fp32 adapters,
-// whose pieces the vector units cut: 42 us, 3.2 TB/s), by reading A where each row has its own (32 rows of 32 adapters,
+// whose pieces the vector units cut: 43-48 us, 2.8-3.1 TB/s), by reading A where each row has its own (32 rows of 32 adapters,
 // 4096 -> rank 16: 7 us, half of it the wait for the segments and then the first rows).  UNIT: the contraction is contiguous in A.
 template <int DTYPE, int ATYPE, bool UNIT, int NR, int RT, int WAVES, bool STAGED>
 __global__ __launch_bounds__(WAVES * 64) void shrink_kernel(ShrinkParams p) {
@@ -543,7 +543,7 @@ struct CopiesParams {
 };
 // An infinity or NaN in an adapter would reach the rows of other segments in its tile, whose 0 it is multiplied with: it is left
 // out here, and the outputs it belongs to are marked.  There is a copy for each segment or for each adapter, whichever are fewer: what
-// a call costs does not go by adapters that it does not use.  16 adapters of 8192 x 32 in bf16 15 us.
+// a call costs does not go by adapters that it does not use.  16 adapters of 8192 x 32 in bf16 23-25 us.
 template <int QTYPE>
 __global__ __launch_bounds__(256) void copies_kernel(CopiesParams p) {
   typedef typename Value<QTYPE>::T TQ;
@@ -653,9 +653,10 @@ __device__ __forceinline__ void interleave() {
 // LDS: one is multiplied, the others are on their way.  fp32 results: all three pieces of both operands are there together, and
 // their six products are formed from the same fragments (one product after the other, each with tiles of its own, read
 // twice as much: the whole call 777 x 1000 -> 1501 96 us, 71 so).
-// 16384 x 4096 -> 4096 bf16 485-560 us (0.98-1.13 PFLOP/s, from card to card; a library's product of 8192 a side reaches 1.33,
-// the matrix units alone 2.08): bound by the power that products of random numbers draw -- rings of smaller steps, other orders of
-// the loads and of the fragments all measured the same, and zeros run at 1.5.  fp32 4096 x 4096 -> 4096: 0.98 PFLOP/s of its pieces.
+// 16384 x 4096 -> 4096 bf16 without segments 466 us (1.18 PFLOP/s; the library's product of the same numbers 352, 1.56, the matrix
+// units alone 2.09), 500-590 with eight segments of rank 16 and whatever else runs around it.  The matrix units work 59 % of the
+// cycles, memory and LDS are far from theirs; what they wait for is open: rings of smaller steps, other orders of the loads and
+// of the fragments all measured the same, and zeros take 378 us (the library 256).  fp32 4096 x 4096 -> 4096: 0.98 PFLOP/s of its pieces.
 template <int OTYPE, int BM, int BN, int BK, int S>
 __device__ __forceinline__ void product_tile(const ProductParams& p) {
   constexpr int NW = 4, WN = 2;
@@ -1310,8 +1311,8 @@ void launch_shrink_tile(const ShrinkParams& p, dim3 grid, bool staged, hipStream
 template <int DTYPE, int ATYPE, bool UNIT, int NR>
 void launch_shrink_rank(const ShrinkParams& p, hipStream_t s) {
   // Tiles of 64 rows read the adapter least often; of 32 or 16 rows where those leave units idle or segments are short.  Calls
-  // with 8 outputs, 4096 -> rank 16 in fp32 adapters, us in tiles of 64 / 32 / 16 rows: 16384 rows 59 / 72 / 99, 8191 47 / 57 / 73,
-  // 6144 44 / 41 / 55, 4096 44 / 39 / 40, 1024 42 / 36 / 36; 1024 rows of 512 segments 77 / 73 / 70.
+  // with 8 outputs, 4096 -> rank 16 in fp32 adapters, us in tiles of 64 / 32 / 16 rows: 16384 rows 61 / 76 / 104, 8191 47 / 58 / 75,
+  // 6144 45 / 41 / 56, 4096 45 / 40 / 41, 1024 44 / 37 / 37; 1024 rows of 512 segments, bf16, 52 / 48 / 45.
   // A launch has less than 2^32 lanes (more wrap, without an error): from 2^26 rows on tiles have 64 whatever the segments are.
   const bool brief = p.rows <= 16ll * p.g.n && p.rows < 1ll << 26;
   const int64_t rows = !brief && p.rows >= 64 * 112 ? 64 : !brief && p.rows >= 32 * 192 ? 32 : 16;
@@ -1327,8 +1328,8 @@ void launch_shrink_rank(const ShrinkParams& p, hipStream_t s) {
 }
 // A workgroup has at most 32 ranks, which leaves LDS for more wavefronts to cut fp32's pieces; all 64 where there is nothing to
 // cut and many rows would be read twice.  Rank 64, 4096 numbers, calls with 8 outputs, us with 64 / 32 ranks a workgroup: 30 rows
-// fp32 121 / 72, bf16 24 / 22; 1024 rows fp32 154 / 99, bf16 34 / 31; 16384 rows fp32 441 / 499, bf16 with fp32 adapters 122 / 91,
-// bf16 63 / 88.
+// fp32 120 / 71, bf16 24 / 22; 1024 rows fp32 154 / 98, bf16 35 / 31; 16384 rows fp32 440 / 499, bf16 with fp32 adapters 137 / 101,
+// bf16 68 / 93.
 template <int DTYPE, int ATYPE, bool UNIT>
 void launch_shrink_along(const ShrinkParams& p, hipStream_t s) {
   if (p.rank <= 16) return launch_shrink_rank<DTYPE, ATYPE, UNIT, 1>(p, s);
@@ -1384,10 +1385,10 @@ void launch_product_tile(ProductParams p, hipStream_t s) {
   product_kernel<OTYPE, BM, BN, BK, S><<<(unsigned)p.tilesM * (unsigned)p.tilesN, 256, 0, s>>>(p);
 }
 // Large tiles reuse what they read most, and are taken where they still fill the 256 units; the smaller ones where the next
-// larger would leave units idle.  Whole calls, us, in tiles of 256 / 128 / 64 a side, bf16: 16384 x 4096 -> 4096 505 / 647 / 1042,
-// 4096 x 2048 -> 3584 (224 tiles of 256) 81 / 107 / 152, 2048 x 2048 -> 3584 (112 of 256, 448 of 128) 73 / 57 / 83,
-// 1024 x 2048 -> 1024 (64 of 128) 67 / 33 / 23, and 64 x 4096 -> 65536, whose tiles of 256 are mostly empty, 170 in those and
-// 156 in tiles of 64.  fp32: 4096 x 4096 -> 4096 819 in tiles of 256 x 128, 868 of 128 x 128; 2048 x 2048 -> 2048 141 of
+// larger would leave units idle.  Whole calls, us, in tiles of 256 / 128 / 64 a side, bf16: 16384 x 4096 -> 4096 517 / 635 / 1009,
+// 4096 x 2048 -> 3584 (224 tiles of 256) 83 / 105 / 145, 2048 x 2048 -> 3584 (112 of 256, 448 of 128) 73 / 57 / 80,
+// 1024 x 2048 -> 1024 (64 of 128) 66 / 32 / 24, and 64 x 4096 -> 65536, whose tiles of 256 are mostly empty, 167 / 152 / 147.
+// fp32: 4096 x 4096 -> 4096 819 in tiles of 256 x 128, 868 of 128 x 128; 2048 x 2048 -> 2048 141 of
 // 128 x 128, 164 of 128 x 64, 184 of 64 x 64; 777 x 1000 -> 1501 85 of 128 x 128, 71 of 128 x 64, 81 of 64 x 64 (312 tiles: a
 // second round for 56 of them); 1024 x 1024 -> 1024 60 of 128 x 64, 53 of 64 x 64.
 void launch_product(const ProductParams& p, int dtype, hipStream_t s) {

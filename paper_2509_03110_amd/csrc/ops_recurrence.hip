@@ -10,13 +10,13 @@
 //
 // Backward: with e_t = a_t (dh_t + e_{t+1}) -- what step t hands to the one before it, the same kind of recurrence from
 // the other end -- d_t = dh_t + e_{t+1},  dx_t = (1 - a_t) d_t,  df_t = a_t (1 - a_t) d_t (h_{t-1} - x_t).
-// The h_{t-1} are formed again, in fp32, from the state that the forward pass saved at the head of each tile.
+// The h_{t-1} are formed again, in fp32, from the state that the forward pass saved at the head of each tile (128 rows, 16 with one wavefront).
 #include "ops.h"
 
 namespace lsam {
 namespace {
 
-// Rows of a tile that one wavefront takes, and wavefronts of a workgroup (one where sequences are no longer than its rows).
+// Rows of a tile that one wavefront takes, and wavefronts of a workgroup (one where sequences are no longer than its rows, packed ones on the average).
 // 8 x 4096 x 2048 bf16 forward and backward take 252 us with 16 rows and 8 wavefronts, 318 with 8 rows, 289 with 8 rows and 16
 // wavefronts, 456 with 16 and 16 (too few registers); a tile more on its way 250, at twice the registers.
 constexpr int kRows = 16;
@@ -154,9 +154,10 @@ __device__ __forceinline__ Place place(const RecurrenceParams& p) {
 }
 
 // RUNS: only (A, H) of the workgroup's run, for a launch that follows.
-// Bound by memory and, with one workgroup on a unit, by how much of it is on its way: 8 x 4096 x 2048 bf16, 403 MB, 101-105 us
-// (3.9 TB/s, the vector units half busy); 131073 x 1000 fp32 in runs, 1.05 GB read for the runs in 220 us and 1.57 GB in 340 us
-// (4.7 TB/s), rows of 4000 bytes that do not begin on lines.
+// 8 x 4096 x 2048 bf16, 403 MB, 100-105 us: 3.9 TB/s, the vector units half busy.  A lane moves two bytes an instruction, and a tile
+// more on its way brings 1 %: likely bound by the address unit, which takes such narrow accesses no faster than wide ones.  131073 x
+// 1000 fp32 in runs, 1.05 GB read for the runs in 225-230 us and 1.57 GB in 322-349 us (4.5-4.9 TB/s), rows of 4000 bytes that do
+// not begin on lines.
 template <int DTYPE, int NW, bool RUNS>
 __global__ __launch_bounds__(NW * 64) void recurrence_kernel(RecurrenceParams p) {
   typedef typename Value<DTYPE>::T T;
@@ -238,8 +239,8 @@ __global__ __launch_bounds__(NW * 64) void recurrence_kernel(RecurrenceParams p)
 }
 
 // RUNS: only (A, E) of the workgroup's run.
-// 8 x 4096 x 2048 bf16, 671 MB, 153 us (4.4 TB/s); 131073 x 1000 fp32, 1.05 GB for the runs in 230 us and 2.62 GB in 545 us
-// (4.8 TB/s).
+// 8 x 4096 x 2048 bf16, 671 MB, 152-155 us (4.4 TB/s), bound as the forward pass is; 131073 x 1000 fp32, 1.05 GB for the runs in
+// 225-242 us and 2.62 GB in 546-555 us (4.8 TB/s).
 template <int DTYPE, int NW, bool RUNS>
 __global__ __launch_bounds__(NW * 64) void recurrence_grad_kernel(RecurrenceParams p) {
   typedef typename Value<DTYPE>::T T;
@@ -395,10 +396,13 @@ __global__ __launch_bounds__(256) void recurrence_step_kernel(RecurrenceParams p
   }
 }
 
-// How a call is cut.  One wavefront where sequences are no longer than its rows (a step of generation).  Runs where
-// sequences times channels give fewer workgroups than there are units: all of one length, so that sequences of any lengths
-// fill the chip evenly, as many as give it kRunGroups workgroups, of at least four tiles each (131073 x 1000 fp32, both directions:
-// 1340 us with 1024, 1350 with 2048; 1 x 32768 x 4096 bf16 forward 306, 309 with 512).
+// How a call is cut.  One wavefront where sequences are no longer than its rows, packed ones on the average.  Runs where sequences
+// times channels give fewer workgroups than there are units: all of one length, so that below that number sequences of any
+// lengths fill the chip evenly, as many as give it kRunGroups workgroups, of at least four tiles each (131073 x 1000 fp32, both
+// directions: 1330-1360 us with 1024, 1350 with 2048; 1 x 32768 x 4096 bf16 forward 310, 309 with 512).  The lengths of packed
+// sequences are not known here: where there are workgroups enough a long one among many short ones is walked by its own alone (64
+// sequences x 256 channels bf16, one of half the rows, 307 us forward, of equal lengths 27; 255 of one row and one of 4000, 4096 channels,
+// 260, one sequence of as many rows 51).
 constexpr int kRunGroups = 1024;
 struct Plan { int waves, splits, slabs; int64_t run_tiles, tiles_of_each, states; };
 Plan plan(const lsam_recurrence_desc* d) {
