@@ -177,6 +177,81 @@ int lsam_adapter_backward(const lsam_adapter_desc* d, const void* x, const void*
                           const int32_t* seg_begin, const int32_t* seg_adapter, const float* u, const void* dy, void* dx,
                           float* dA, float* dB, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- embedding ---------------------------------------------------------------------------------
+ * y = scale E_k[token] for `rows` tokens of each of `replicas` replicas: rows of the replica's table E_k [vocab, dim], or of one table
+ * that all share (table_replica = 0).  A token outside 0..vocab-1 holds nothing (padding): its row of y is 0.
+ *   tokens [device] replicas times [rows] int32, token_replica apart
+ *   table  [device] of table_dtype;  y [device] of dtype, rounded once */
+#define LSAM_EMBEDDING_MAX_VOCAB (1 << 22)
+typedef struct {
+  int32_t replicas;                          /* 0..65535                                     */
+  int32_t dtype, table_dtype;                /* LSAM_DTYPE_* of y and dy, of the table       */
+  float scale;
+  int64_t rows;                              /* of one replica, below 2^31                   */
+  int64_t vocab;                             /* 1..LSAM_EMBEDDING_MAX_VOCAB                  */
+  int64_t dim;                               /* 1..2^24                                      */
+  int64_t token_replica;                     /* from replica to replica                      */
+  int64_t table_stride, table_replica;       /* from row to row, from replica to replica     */
+  int64_t y_stride, y_replica;
+  int64_t dy_stride, dy_replica;             /* backward pass only, as what follows          */
+  int64_t dtable_stride, dtable_replica;
+} lsam_embedding_desc;
+int lsam_embedding(const lsam_embedding_desc* d, const int32_t* tokens, const void* table, void* y, void* stream);
+
+/* Gradient with respect to the tables:  dE_k[v] = scale sum of the replica's rows of dy whose token is v, in fp32, in the order of the rows.
+ *   dtable [device] replicas times [vocab, dim] floats, apart from each other; written whole (0 where a token does not occur), not
+ *          added to.  They may be parts of one [replicas, d] array.  The gradient of a table that replicas share is that of one
+ *          replica with all their rows
+ * workspace [device, 16-byte aligned], lsam_embedding_workspace_bytes(d) bytes (0, with a message, for a descriptor that is refused);
+ * nothing in it has to survive the call. */
+size_t lsam_embedding_workspace_bytes(const lsam_embedding_desc* d);
+int lsam_embedding_backward(const lsam_embedding_desc* d, const int32_t* tokens, const void* dy, float* dtable, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* ---- between two blocks --------------------------------------------------------------------------
+ * With n(x) = x / sqrt(mean x^2 + eps) over the `dim` numbers of a row, for `rows` rows of each of `replicas` replicas:
+ *   r' = alpha r + beta sigmoid(gate) w_post n(y)     what a block made of the stream joins it
+ *   h  = w_pre n(r')                                  what the next block reads; the norm is that of r' as it is stored
+ *   r, y, gate [device] of dtype; gate NULL: 1
+ *   w_post     [device] replicas times [dim] floats, or NULL: y itself in place of w_post n(y)
+ *   w_pre      [device] replicas times [dim] floats, or NULL: no h
+ *   r_out, h   [device] of dtype.  r_out may be r itself (same pointer and strides)
+ * y NULL (before the first block): r' is r, nothing is joined, and r_out, gate and w_post are not looked at.
+ * Sums are fp32: a row whose squares pass its range has n(x) = 0.  What is not finite in a row reaches no other row. */
+#define LSAM_RESIDUAL_MAX_DIM 16384
+typedef struct {
+  int32_t replicas;                          /* 0..65535                                     */
+  int32_t dtype;                             /* LSAM_DTYPE_*                                 */
+  int64_t rows;                              /* of one replica, below 2^31                   */
+  int64_t dim;                               /* 1..LSAM_RESIDUAL_MAX_DIM                     */
+  float alpha, beta, eps;                    /* eps >= 0                                     */
+  int64_t w_pre_replica, w_post_replica;     /* from replica to replica; 0: all share one    */
+  int64_t r_stride, r_replica;               /* from row to row, from replica to replica     */
+  int64_t y_stride, y_replica, gate_stride, gate_replica;
+  int64_t r_out_stride, r_out_replica, h_stride, h_replica;
+  int64_t dr_stride, dr_replica, dh_stride, dh_replica;              /* backward pass only, as what follows */
+  int64_t dr_out_stride, dr_out_replica, dy_stride, dy_replica, dgate_stride, dgate_replica;
+  int64_t dw_pre_replica, dw_post_replica;
+} lsam_residual_desc;
+int lsam_residual(const lsam_residual_desc* d, const void* r, const void* y, const void* gate, const float* w_pre, const float* w_post,
+                  void* r_out, void* h, void* stream);
+
+/* Gradients of sum dr r' + dh h, where r is r' as the forward call left it (the stream before it where y is NULL):
+ *   D = dr + through(r', w_pre dh),  dr_out = alpha D (D where y is NULL),  o = w_post n(y),  dgate = beta D o s (1 - s),  s = sigmoid(gate),
+ *   dy = through(y, beta D s w_post),  dw_pre = sum dh n(r'),  dw_post = sum beta D s n(y) over the rows of a replica,
+ *   through(x, g) = (g - n(x) mean(g n(x))) / sqrt(mean x^2 + eps), g itself where there is no norm
+ *   dr      [device] of dtype, or NULL: 0.  dr_out may be dr itself (same pointer and strides)
+ *   dh      [device] of dtype; not looked at where w_pre is NULL
+ *   dr_out, dy, dgate [device] of dtype, dw_pre, dw_post [device] replicas times [dim] floats; each may be NULL: not wanted.  Weights
+ *           are written whole, not added to, lie apart from each other, and may be parts of one [replicas, d] array
+ * The gradient of weights that replicas share is that of one replica with all their rows.
+ * workspace [device, 16-byte aligned], lsam_residual_workspace_bytes(d) bytes (0, with a message, for a descriptor that is refused);
+ * needed where a gradient of weights is wanted; nothing in it has to survive the call. */
+size_t lsam_residual_workspace_bytes(const lsam_residual_desc* d);
+int lsam_residual_backward(const lsam_residual_desc* d, const void* r, const void* y, const void* gate, const float* w_pre,
+                           const float* w_post, const void* dr, const void* dh, void* dr_out, void* dy, void* dgate, float* dw_pre,
+                           float* dw_post, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,428 @@
+// lsam_embedding, lsam_embedding_backward: rows of a table for tokens, and the sum of each token's rows of a gradient.
+//
+//   lookup_kernel   y = scale E[token]: eight numbers a lane
+//   order_kernel    the places of a replica's tokens, sorted by token and within a token by place, with no atomics and no exchange between
+//                   workgroups: each owns a range of tokens, walks over all places, and keeps what is in its range
+//   sums_kernel     a wavefront takes 64 sorted places and 256 columns; a token whose places all lie there is finished, of
+//                   others it leaves partial sums; further wavefronts write the zeros of tokens that do not occur
+//   join_kernel     partial sums of tokens that go on past 64 places
+#include "ops.h"
+
+namespace lsam {
+namespace {
+
+constexpr int kOrderWaves = 16;
+constexpr int kMaxRange = 512;         // tokens of a workgroup of order_kernel: [range][wavefronts] counters in LDS, 32 KiB
+constexpr int kAhead = 8;              // loads of 64 tokens on their way
+constexpr int kPlaces = 64;            // sorted places of a wavefront of sums_kernel, one for each lane
+constexpr int kSlab = 256;             // columns of a wavefront, four a lane
+
+struct EmbeddingParams {
+  const int32_t* tokens; const void* table; void* y;
+  const void* dy; float* dtable;
+  int64_t rows, vocab, dim, token_replica;
+  int64_t table_stride, table_replica, y_stride, y_replica, dy_stride, dy_replica, dtable_stride, dtable_replica;
+  float scale;
+  int32_t replica0;                    // first replica of this launch
+  int64_t row0, chunk0;                // first row of the launch (lookup; zeros of sums_kernel), first chunk (sums, join)
+  unsigned units, zeros;               // lanes with work (lookup); wavefronts that sum, or join, and that write zeros
+  unsigned pieces;                     // of eight columns in a row (lookup), of kSlab (sums, join)
+  int64_t chunks;                      // of kPlaces places
+  unsigned range;                      // order_kernel
+  int32_t* order; int32_t* start;      // [replicas][rows], [replicas][vocab + 1]
+  float* partial;                      // [replicas][chunks][2][dim]: of the token that comes from the chunk before, that goes on into the next
+};
+
+// One load of a token before the row's address is known, so bound by latency where rows are few; 4096 x 1024 of four replicas move at the rate of a copy.
+template <int TABLE, int DTYPE>
+__global__ __launch_bounds__(256) void lookup_kernel(EmbeddingParams p) {
+  const unsigned unit = blockIdx.x * 256 + threadIdx.x;
+  if (unit >= p.units) return;
+  const int64_t replica = p.replica0 + blockIdx.y;
+  const unsigned local = unit / p.pieces, col = (unit - local * p.pieces) * 8;
+  const int64_t row = p.row0 + local;
+  const int32_t token = p.tokens[replica * p.token_replica + row];
+  const bool there = token >= 0 && token < p.vocab;
+  const typename Value<TABLE>::T* src = static_cast<const typename Value<TABLE>::T*>(p.table) + replica * p.table_replica + (there ? token : 0) * p.table_stride + col;
+  typename Value<DTYPE>::T* dst = static_cast<typename Value<DTYPE>::T*>(p.y) + replica * p.y_replica + row * p.y_stride + col;
+  const int n = (int)(p.dim - col < 8 ? p.dim - col : 8);
+  float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if (n == 8) {
+    if (there) Value<TABLE>::load8(src, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = there ? v[e] * p.scale : 0.f;
+    Value<DTYPE>::store8(dst, v);
+  } else {
+    for (int e = 0; e < n; ++e) Value<DTYPE>::put(dst + e, there ? Value<TABLE>::get(src + e) * p.scale : 0.f);
+  }
+}
+
+// Calls f(token, lanes that hold it) for every token of the range that the wavefront holds.
+template <typename F>
+__device__ __forceinline__ void each_token(int32_t token, bool mine, F f) {
+  unsigned long long left = __ballot(mine);
+  while (left) {
+    const int32_t t = __builtin_amdgcn_readlane(token, __builtin_ctzll(left));
+    const unsigned long long same = __ballot(mine && token == t);
+    f(t, same);
+    left &= ~same;
+  }
+}
+
+// Each wavefront owns a run of places and a column of counters, so that places keep their order: counted first, then, from the sums of
+// the counters before, put where they belong.  All lanes update a counter alike.  Tokens of other ranges cost a load and two comparisons.
+__global__ __launch_bounds__(kOrderWaves * 64) void order_kernel(EmbeddingParams p) {
+  __shared__ uint32_t counts[kMaxRange * kOrderWaves], sums[kOrderWaves], below[kOrderWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t replica = p.replica0 + blockIdx.y;
+  const int32_t* tokens = p.tokens + replica * p.token_replica;
+  int32_t* order = p.order + replica * p.rows;
+  const int32_t lo = (int32_t)(blockIdx.x * p.range), hi = (int32_t)(lo + p.range < p.vocab ? lo + p.range : p.vocab);
+  const int entries = (hi - lo) * kOrderWaves;
+  for (int i = tid; i < entries; i += kOrderWaves * 64) counts[i] = 0;
+  __syncthreads();
+  const int64_t steps = (p.rows + 63) / 64, each = (steps + kOrderWaves - 1) / kOrderWaves;
+  const int64_t first = wave * each * 64;
+  int64_t end = (wave + 1) * each * 64;
+  end = end < p.rows ? end : p.rows;
+
+  uint32_t fewer = 0;                                      // tokens of lower ranges
+  for (int64_t at = first; at < end; at += 64 * kAhead) {
+    int32_t t[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int64_t row = at + i * 64 + lane;
+      t[i] = row < end ? tokens[row] : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      fewer += (uint32_t)__popcll(__ballot(t[i] >= 0 && t[i] < lo));
+      each_token(t[i], t[i] >= lo && t[i] < hi, [&](int32_t token, unsigned long long same) {
+        counts[(token - lo) * kOrderWaves + wave] += (uint32_t)__popcll(same);
+      });
+    }
+  }
+  if (lane == 0) below[wave] = fewer;
+  __syncthreads();
+
+  // sums of all counters before each: a run of counters a thread, then over the threads
+  const int run = (entries + kOrderWaves * 64 - 1) / (kOrderWaves * 64);
+  const int from = tid * run < entries ? tid * run : entries, to = from + run < entries ? from + run : entries;
+  uint32_t mine = 0;
+  for (int i = from; i < to; ++i) mine += counts[i];
+  uint32_t before = mine;                                  // with those of lower lanes
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t other = __shfl_up(before, d);
+    if (lane >= d) before += other;
+  }
+  if (lane == 63) sums[wave] = before;
+  __syncthreads();
+  before -= mine;
+  for (int w = 0; w < kOrderWaves; ++w) {
+    before += below[w];
+    if (w < wave) before += sums[w];
+  }
+  for (int i = from; i < to; ++i) {
+    const uint32_t c = counts[i];
+    counts[i] = before;
+    before += c;
+  }
+  __syncthreads();
+  int32_t* start = p.start + replica * (p.vocab + 1);
+  for (int i = tid; i < hi - lo; i += kOrderWaves * 64) start[lo + i] = (int32_t)counts[i * kOrderWaves];
+  if (hi == p.vocab && tid == 0) {
+    uint32_t all = 0;
+    for (int w = 0; w < kOrderWaves; ++w) all += below[w] + sums[w];
+    start[p.vocab] = (int32_t)all;
+  }
+  __syncthreads();
+
+  for (int64_t at = first; at < end; at += 64 * kAhead) {
+    int32_t t[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int64_t row = at + i * 64 + lane;
+      t[i] = row < end ? tokens[row] : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      each_token(t[i], t[i] >= lo && t[i] < hi, [&](int32_t token, unsigned long long same) {
+        uint32_t* c = &counts[(token - lo) * kOrderWaves + wave];
+        const uint32_t place = *c;
+        if (same >> lane & 1) order[place + (uint32_t)__popcll(same & ((1ull << lane) - 1))] = (int32_t)(at + i * 64 + lane);
+        *c = place + (uint32_t)__popcll(same);
+      });
+    }
+  }
+}
+
+// Four columns of a row from `col` on, zeros behind the row's end.
+template <int DTYPE>
+__device__ __forceinline__ f32x4 load4(const typename Value<DTYPE>::T* p, int n) {
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (n == 4) {
+    if constexpr (DTYPE == LSAM_DTYPE_FP32) {
+      v = *reinterpret_cast<const f32x4_any*>(p);
+    } else {
+      const u16x4 w = *reinterpret_cast<const u16x4_any*>(p);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = widen(w[e]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < n) v[e] = Value<DTYPE>::get(p + e);
+  }
+  return v;
+}
+__device__ __forceinline__ void store4(float* p, f32x4 v, int n) {
+  if (n == 4) {
+    *reinterpret_cast<f32x4_any*>(p) = v;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < n) p[e] = v[e];
+  }
+}
+
+// The first p.units wavefronts of a replica sum, p.zeros more write zeros.
+template <int DTYPE>
+__global__ __launch_bounds__(256) void sums_kernel(EmbeddingParams p) {
+  typedef typename Value<DTYPE>::T T;
+  const int lane = threadIdx.x & 63;
+  const int64_t replica = p.replica0 + blockIdx.y;
+  unsigned unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int32_t* start = p.start + replica * (p.vocab + 1);
+  float* dtable = p.dtable + replica * p.dtable_replica;
+  if (unit >= p.units) {
+    unit -= p.units;
+    if (unit >= p.zeros) return;
+    const int64_t row = p.row0 + unit / p.pieces;
+    if (start[row] != start[row + 1]) return;
+    const int64_t col = (int64_t)(unit % p.pieces) * kSlab + lane * 4;
+    const int n = (int)(p.dim - col < 4 ? p.dim - col : 4);
+    if (n > 0) store4(dtable + row * p.dtable_stride + col, f32x4{0.f, 0.f, 0.f, 0.f}, n);
+    return;
+  }
+  const int64_t chunk = p.chunk0 + unit / p.pieces, col = (int64_t)(unit % p.pieces) * kSlab + lane * 4;
+  const int64_t at = chunk * kPlaces, all = start[p.vocab];
+  if (at >= all) return;
+  const int n = (int)(p.dim - col < 4 ? p.dim - col : 4);                   // none of a lane behind the row's end
+  const int32_t* order = p.order + replica * p.rows;
+  const int32_t* tokens = p.tokens + replica * p.token_replica;
+  const int places = (int)(all - at < kPlaces ? all - at : kPlaces);
+  const int32_t row = order[at + (lane < places ? lane : places - 1)], token = tokens[row];
+  const int32_t prev = at > 0 ? tokens[order[at - 1]] : -1, next = at + places < all ? tokens[order[at + places]] : -1;
+  const int32_t left = __shfl_up(token, 1);
+  const unsigned long long heads = __ballot(lane > 0 && lane < places && token != left);   // a token begins there
+  const T* dy = static_cast<const T*>(p.dy) + replica * p.dy_replica + (n > 0 ? col : 0);
+  float* partial = p.partial + (replica * p.chunks + chunk) * 2 * p.dim + col;
+  bool open = __builtin_amdgcn_readfirstlane(token) == prev;                // the first token comes from the chunk before
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  auto leave = [&](int place, bool more) {                                  // the token that ends at `place`, or goes on
+    if (n > 0) {
+      if (open) store4(partial, acc, n);
+      else if (more) store4(partial + p.dim, acc, n);
+      else store4(dtable + __builtin_amdgcn_readlane(token, place) * p.dtable_stride + col, acc * p.scale, n);
+    }
+    open = false;
+    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  };
+  for (int i0 = 0; i0 < places; i0 += 8) {
+    f32x4 v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int place = i0 + i < places ? i0 + i : places - 1;
+      v[i] = load4<DTYPE>(dy + __builtin_amdgcn_readlane(row, place) * p.dy_stride, n);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i0 + i >= places) break;
+      if (heads >> (i0 + i) & 1) leave(i0 + i - 1, false);
+      acc += v[i];
+    }
+  }
+  leave(places - 1, __builtin_amdgcn_readlane(token, places - 1) == next);
+}
+
+// A wavefront for each chunk in which a token begins that goes on into the next.
+__global__ __launch_bounds__(256) void join_kernel(EmbeddingParams p) {
+  const int lane = threadIdx.x & 63;
+  const int64_t replica = p.replica0 + blockIdx.y;
+  const unsigned unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (unit >= p.units) return;
+  const int32_t* start = p.start + replica * (p.vocab + 1);
+  const int64_t chunk = p.chunk0 + unit / p.pieces, col = (int64_t)(unit % p.pieces) * kSlab + lane * 4, edge = (chunk + 1) * kPlaces;
+  if (edge >= start[p.vocab]) return;
+  const int32_t* order = p.order + replica * p.rows;
+  const int32_t token = p.tokens[replica * p.token_replica + order[edge]];
+  const int64_t begin = start[token], end = start[token + 1];
+  if (begin >= edge || begin < edge - kPlaces) return;
+  const int n = (int)(p.dim - col < 4 ? p.dim - col : 4);
+  if (n <= 0) return;
+  const int64_t last = (end - 1) / kPlaces, step = 2 * p.dim;
+  const float* partial = p.partial + (replica * p.chunks + chunk) * step + col;
+  f32x4 acc = load4<LSAM_DTYPE_FP32>(partial + p.dim, n);
+  int64_t c = 1;                                                            // the same sums in the same order, whatever is loaded ahead
+  for (; chunk + c + 7 <= last; c += 8) {
+    f32x4 v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = load4<LSAM_DTYPE_FP32>(partial + (c + i) * step, n);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc += v[i];
+  }
+  for (; chunk + c <= last; ++c) acc += load4<LSAM_DTYPE_FP32>(partial + c * step, n);
+  store4(p.dtable + replica * p.dtable_replica + token * p.dtable_stride + col, acc * p.scale, n);
+}
+
+struct Plan { int ranges; unsigned range; int64_t chunks; size_t start_at, partial_at, bytes; };
+// Ranges of tokens: about as many workgroups as there are units, so that each holds few of the tokens that it walks over.
+Plan plan(const lsam_embedding_desc* d) {
+  Plan c;
+  const int64_t replicas = d->replicas > 0 ? d->replicas : 1;
+  int64_t want = (256 + replicas - 1) / replicas;
+  const int64_t least = (d->vocab + kMaxRange - 1) / kMaxRange;
+  want = want < least ? least : want > d->vocab ? d->vocab : want;
+  c.range = (unsigned)((d->vocab + want - 1) / want);
+  c.ranges = (int)((d->vocab + c.range - 1) / c.range);
+  c.chunks = (d->rows + kPlaces - 1) / kPlaces;
+  const auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+  c.start_at = up((size_t)d->replicas * d->rows * 4);
+  c.partial_at = c.start_at + up((size_t)d->replicas * (d->vocab + 1) * 4);
+  c.bytes = c.partial_at + (size_t)d->replicas * c.chunks * 2 * d->dim * 4;
+  return c;
+}
+
+int check(const lsam_embedding_desc* d, const char* who) {
+  if (!d) return refuse(LSAM_EINVAL, "%s: the descriptor is NULL", who);
+  if (!known_dtype(d->dtype) || !known_dtype(d->table_dtype)) return refuse(LSAM_EINVAL, "%s: dtype %d, %d: LSAM_DTYPE_* are wanted", who, d->dtype, d->table_dtype);
+  if (d->replicas < 0 || d->replicas > 65535) return refuse(LSAM_EINVAL, "%s: replicas must be in 0..65535", who);
+  if (d->rows < 0 || d->rows >= 1ll << 31) return refuse(LSAM_EINVAL, "%s: rows must be in 0..2^31-1", who);
+  if (d->vocab < 1 || d->vocab > LSAM_EMBEDDING_MAX_VOCAB) return refuse(LSAM_EINVAL, "%s: vocab must be in 1..%d", who, LSAM_EMBEDDING_MAX_VOCAB);
+  if (d->dim < 1 || d->dim > 1 << 24) return refuse(LSAM_EINVAL, "%s: dim must be in 1..2^24", who);
+  if ((__int128)d->replicas * (d->rows > d->vocab ? d->rows : d->vocab) * d->dim >= (__int128)1 << 44)
+    return refuse(LSAM_EINVAL, "%s: the arrays are too large", who);
+  return LSAM_OK;
+}
+
+EmbeddingParams params(const lsam_embedding_desc* d, const int32_t* tokens) {
+  EmbeddingParams p{};
+  p.tokens = tokens;
+  p.rows = d->rows; p.vocab = d->vocab; p.dim = d->dim; p.token_replica = d->token_replica; p.scale = d->scale;
+  return p;
+}
+
+template <int TABLE>
+void lookup(const EmbeddingParams& p, int dtype, dim3 grid, hipStream_t s) {
+  if (dtype == LSAM_DTYPE_BF16) lookup_kernel<TABLE, LSAM_DTYPE_BF16><<<grid, 256, 0, s>>>(p);
+  else lookup_kernel<TABLE, LSAM_DTYPE_FP32><<<grid, 256, 0, s>>>(p);
+}
+
+}  // namespace
+}  // namespace lsam
+
+using namespace lsam;
+
+extern "C" int lsam_embedding(const lsam_embedding_desc* d, const int32_t* tokens, const void* table, void* y, void* stream) {
+  int rc = check(d, "embedding");
+  if (rc != LSAM_OK) return rc;
+  if (d->replicas == 0 || d->rows == 0) return LSAM_OK;
+  Arg args[] = {matrices("tokens", tokens, 1, 0, d->replicas, d->token_replica, d->rows, 4, false),
+                matrices("table", table, d->replicas, d->table_replica, d->vocab, d->table_stride, d->dim, dtype_bytes(d->table_dtype), false),
+                matrices("y", y, d->replicas, d->y_replica, d->rows, d->y_stride, d->dim, dtype_bytes(d->dtype), true)};
+  constexpr int n = sizeof args / sizeof args[0];
+  if (d->token_replica >= 0 && d->token_replica < d->rows)    // replicas may share tokens, or read parts that overlap
+    args[0] = matrices("tokens", tokens, d->replicas, d->token_replica, 1, 0, d->rows, 4, false);
+  if (!apart(d->replicas, d->y_replica, d->rows, d->y_stride, d->dim)) return refuse(LSAM_EINVAL, "embedding: the replicas of y lie over each other");
+  rc = check_values(args, n, "embedding");
+  if (rc == LSAM_OK) rc = check_apart(args, n, "embedding");
+  if (rc != LSAM_OK) return rc;
+  EmbeddingParams p = params(d, tokens);
+  p.table = table; p.y = y;
+  p.table_stride = d->table_stride; p.table_replica = d->table_replica; p.y_stride = d->y_stride; p.y_replica = d->y_replica;
+  p.pieces = (unsigned)((d->dim + 7) / 8);
+  // launches of less than 2^32 lanes
+  const int64_t most = (1 << 30) / p.pieces;
+  const unsigned K = (unsigned)d->replicas;
+  for (int64_t r0 = 0; r0 < d->rows; r0 += most) {
+    p.row0 = r0;
+    p.units = (unsigned)((d->rows - r0 < most ? d->rows - r0 : most) * p.pieces);
+    const unsigned blocks = (p.units + 255) / 256, together = (1u << 23) / blocks < 65535 ? (1u << 23) / blocks : 65535;
+    for (unsigned k = 0; k < K; k += together) {
+      p.replica0 = (int32_t)k;
+      const dim3 grid(blocks, K - k < together ? K - k : together);
+      if (d->table_dtype == LSAM_DTYPE_BF16) lookup<LSAM_DTYPE_BF16>(p, d->dtype, grid, static_cast<hipStream_t>(stream));
+      else lookup<LSAM_DTYPE_FP32>(p, d->dtype, grid, static_cast<hipStream_t>(stream));
+    }
+  }
+  return launched();
+}
+
+extern "C" size_t lsam_embedding_workspace_bytes(const lsam_embedding_desc* d) {
+  if (check(d, "embedding") != LSAM_OK) return 0;
+  return plan(d).bytes;
+}
+
+extern "C" int lsam_embedding_backward(const lsam_embedding_desc* d, const int32_t* tokens, const void* dy, float* dtable, void* workspace,
+                                       size_t workspace_bytes, void* stream) {
+  const char* who = "embedding_backward";
+  int rc = check(d, who);
+  if (rc != LSAM_OK) return rc;
+  if (d->replicas == 0) return LSAM_OK;
+  const Plan c = plan(d);
+  Arg args[] = {matrices("tokens", tokens, 1, 0, d->replicas, d->token_replica, d->rows, 4, false),
+                matrices("dy", dy, d->replicas, d->dy_replica, d->rows, d->dy_stride, d->dim, dtype_bytes(d->dtype), false),
+                matrices("dtable", dtable, d->replicas, d->dtable_replica, d->vocab, d->dtable_stride, d->dim, 4, true)};
+  constexpr int n = sizeof args / sizeof args[0];
+  if (d->token_replica >= 0 && d->token_replica < d->rows)
+    args[0] = matrices("tokens", tokens, d->replicas, d->token_replica, 1, 0, d->rows, 4, false);
+  if (!apart(d->replicas, d->dtable_replica, d->vocab, d->dtable_stride, d->dim)) return refuse(LSAM_EINVAL, "%s: the replicas of dtable lie over each other", who);
+  rc = check_values(args, n, who);
+  if (rc == LSAM_OK) rc = check_apart(args, n, who);
+  if (rc == LSAM_OK) rc = check_workspace(args, n, workspace, workspace_bytes, c.bytes, 16, who);
+  if (rc != LSAM_OK) return rc;
+  EmbeddingParams p = params(d, tokens);
+  p.dy = dy; p.dtable = dtable;
+  p.dy_stride = d->dy_stride; p.dy_replica = d->dy_replica; p.dtable_stride = d->dtable_stride; p.dtable_replica = d->dtable_replica;
+  p.order = static_cast<int32_t*>(workspace);
+  p.start = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + c.start_at);
+  p.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + c.partial_at);
+  p.range = c.range;
+  p.chunks = c.chunks;
+  p.pieces = (unsigned)((d->dim + kSlab - 1) / kSlab);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const unsigned K = (unsigned)d->replicas;
+  // launches of less than 2^32 lanes
+  const unsigned apiece = (unsigned)((1 << 21) / c.ranges);
+  for (unsigned k = 0; k < K; k += apiece) {
+    p.replica0 = (int32_t)k;
+    order_kernel<<<dim3((unsigned)c.ranges, K - k < apiece ? K - k : apiece), kOrderWaves * 64, 0, s>>>(p);
+  }
+  // lines of columns, a wavefront for each of a line's pieces: chunks to be summed first, then rows of the table
+  const int64_t most = (1 << 24) / p.pieces;
+  for (int64_t c0 = 0, r0 = 0; c0 < c.chunks || r0 < d->vocab;) {
+    const int64_t nc = c.chunks - c0 < most ? c.chunks - c0 : most, nr = d->vocab - r0 < most - nc ? d->vocab - r0 : most - nc;
+    p.chunk0 = c0; p.row0 = r0;
+    p.units = (unsigned)(nc * p.pieces); p.zeros = (unsigned)(nr * p.pieces);
+    const unsigned blocks = (p.units + p.zeros + 3) / 4, together = (1u << 23) / blocks < 65535 ? (1u << 23) / blocks : 65535;
+    for (unsigned k = 0; k < K; k += together) {
+      p.replica0 = (int32_t)k;
+      const dim3 grid(blocks, K - k < together ? K - k : together);
+      if (d->dtype == LSAM_DTYPE_BF16) sums_kernel<LSAM_DTYPE_BF16><<<grid, 256, 0, s>>>(p);
+      else sums_kernel<LSAM_DTYPE_FP32><<<grid, 256, 0, s>>>(p);
+    }
+    c0 += nc;
+    r0 += nr;
+  }
+  for (int64_t c0 = 0; c0 + 1 < c.chunks; c0 += most) {
+    p.chunk0 = c0;
+    p.units = (unsigned)((c.chunks - 1 - c0 < most ? c.chunks - 1 - c0 : most) * p.pieces);
+    const unsigned blocks = (p.units + 3) / 4, together = (1u << 23) / blocks < 65535 ? (1u << 23) / blocks : 65535;
+    for (unsigned k = 0; k < K; k += together) {
+      p.replica0 = (int32_t)k;
+      join_kernel<<<dim3(blocks, K - k < together ? K - k : together), 256, 0, s>>>(p);
+    }
+  }
+  return launched();
+}

@@ -19,10 +19,14 @@ DTYPE_FP32, DTYPE_BF16 = 0, 1
 
 TOP_MAX = 32
 ADAPTER_MAX_RANK = 64
+EMBEDDING_MAX_VOCAB = 1 << 22
+RESIDUAL_MAX_DIM = 16384
 
 EXPORTS = ["lsam_dropout", "lsam_logprobs_workspace_bytes", "lsam_logprobs", "lsam_logprobs_backward",
            "lsam_recurrence_workspace_bytes", "lsam_recurrence_states", "lsam_recurrence", "lsam_recurrence_backward",
-           "lsam_adapter_workspace_bytes", "lsam_adapter", "lsam_adapter_backward"]
+           "lsam_adapter_workspace_bytes", "lsam_adapter", "lsam_adapter_backward",
+           "lsam_embedding", "lsam_embedding_workspace_bytes", "lsam_embedding_backward",
+           "lsam_residual", "lsam_residual_workspace_bytes", "lsam_residual_backward"]
 
 
 class lsam_dropout_desc(C.Structure):
@@ -54,6 +58,22 @@ class lsam_adapter_desc(C.Structure):
                 ("segs", C.c_int32), ("dtype", C.c_int32), ("adapter_dtype", C.c_int32), ("scale", C.c_float)] + [
                     (n, C.c_int64) for n in ("x_stride", "w_stride", "y_stride", "a_adapter", "a_stride", "b_adapter", "b_stride",
                                              "dy_stride", "dx_stride", "da_adapter", "da_stride", "db_adapter", "db_stride")]
+
+
+class lsam_embedding_desc(C.Structure):
+    _fields_ = [("replicas", C.c_int32), ("dtype", C.c_int32), ("table_dtype", C.c_int32), ("scale", C.c_float)] + [
+        (n, C.c_int64) for n in ("rows", "vocab", "dim", "token_replica", "table_stride", "table_replica", "y_stride", "y_replica",
+                                 "dy_stride", "dy_replica", "dtable_stride", "dtable_replica")]
+
+
+class lsam_residual_desc(C.Structure):
+    _fields_ = [("replicas", C.c_int32), ("dtype", C.c_int32), ("rows", C.c_int64), ("dim", C.c_int64), ("alpha", C.c_float),
+                ("beta", C.c_float), ("eps", C.c_float)] + [
+                    (n, C.c_int64) for n in ("w_pre_replica", "w_post_replica", "r_stride", "r_replica", "y_stride", "y_replica",
+                                             "gate_stride", "gate_replica", "r_out_stride", "r_out_replica", "h_stride", "h_replica",
+                                             "dr_stride", "dr_replica", "dh_stride", "dh_replica", "dr_out_stride", "dr_out_replica",
+                                             "dy_stride", "dy_replica", "dgate_stride", "dgate_replica", "dw_pre_replica",
+                                             "dw_post_replica")]
 
 
 _ready = None
@@ -89,6 +109,19 @@ def _lib():
         L.lsam_adapter.argtypes = [C.POINTER(lsam_adapter_desc)] + [vp] * 10 + [C.c_size_t, vp]
         L.lsam_adapter_backward.restype = C.c_int
         L.lsam_adapter_backward.argtypes = [C.POINTER(lsam_adapter_desc)] + [vp] * 12 + [C.c_size_t, vp]
+        emb, res = C.POINTER(lsam_embedding_desc), C.POINTER(lsam_residual_desc)
+        L.lsam_embedding.restype = C.c_int
+        L.lsam_embedding.argtypes = [emb] + [vp] * 4
+        L.lsam_embedding_workspace_bytes.restype = C.c_size_t
+        L.lsam_embedding_workspace_bytes.argtypes = [emb]
+        L.lsam_embedding_backward.restype = C.c_int
+        L.lsam_embedding_backward.argtypes = [emb] + [vp] * 4 + [C.c_size_t, vp]
+        L.lsam_residual.restype = C.c_int
+        L.lsam_residual.argtypes = [res] + [vp] * 8
+        L.lsam_residual_workspace_bytes.restype = C.c_size_t
+        L.lsam_residual_workspace_bytes.argtypes = [res]
+        L.lsam_residual_backward.restype = C.c_int
+        L.lsam_residual_backward.argtypes = [res] + [vp] * 13 + [C.c_size_t, vp]
         _ready = L
     return _ready
 
@@ -395,3 +428,159 @@ def adapter_backward(x, W, A, B, u, dy, seg_begin, seg_adapter, scale, dx=None, 
                                        seg_adapter.data_ptr(), u.data_ptr(), dy.data_ptr(), _ptr(dx), _ptr(dA), _ptr(dB), _ptr(ws),
                                        need, raw))
     return dx, dA, dB
+
+
+def _of_replicas(t):
+    """Strides from row to row and from replica to replica; without the latter index there is one replica."""
+    s = t.stride()
+    return (s[0], 0) if len(s) == 2 else (s[1], s[0])
+
+
+def _embedding_tokens(tokens):
+    if not 1 <= tokens.dim() <= 2:
+        _refuse("the tokens have %d indices: [rows] or [K, rows] is wanted" % tokens.dim())
+    _expect(tokens, "the tokens", None, None, torch.int32)
+    return (1, tokens.shape[0], 0) if tokens.dim() == 1 else (tokens.shape[0], tokens.shape[1], tokens.stride(0))
+
+
+def embedding(tokens, table, scale=1.0, dtype=None, out=None, stream=None):
+    """scale * table[token] in `dtype` (the table's, or out's): tokens [rows] and one table [vocab, dim], or tokens [K, rows] of K replicas and their tables
+    [K, vocab, dim], or one table [vocab, dim] that all read.  A token outside the vocabulary has a row of zeros; see
+    lsam_embedding."""
+    L = _ready or _lib()
+    K, rows, apart = _embedding_tokens(tokens)
+    n = table.dim()
+    if not 2 <= n <= tokens.dim() + 1:
+        _refuse("the table has %d indices: [vocab, dim] is wanted, or [K, vocab, dim] for tokens [K, rows]" % n)
+    _expect(table, "the table", tokens, (K,) + tuple(table.shape[1:]) if n == 3 else None)
+    vocab, dim = table.shape[-2:]
+    shape = tuple(tokens.shape) + (dim,)
+    if out is not None:
+        _expect(out, "out", tokens, shape, dtype)
+    with _On(tokens, stream) as raw:
+        y = torch.empty(shape, dtype=table.dtype if dtype is None else dtype, device=tokens.device) if out is None else out
+        d = lsam_embedding_desc(K, _dtype(y, "the result"), _dtype(table, "the table"), scale, rows, vocab, dim, apart, *_of_replicas(table),
+                                *_of_replicas(y))
+        _check(L.lsam_embedding(C.byref(d), tokens.data_ptr(), table.data_ptr(), y.data_ptr(), raw))
+    return y
+
+
+def embedding_backward(tokens, dy, vocab, scale=1.0, out=None, stream=None):
+    """Gradient of the tables in fp32, [vocab, dim] or [K, vocab, dim], written whole: scale times the sum of each token's rows of dy (tokens'
+    shape + [dim]).  The gradient of a table that K replicas share is that of their tokens and dy as one replica's: tokens.view(-1).  `out` may be
+    part of one [K, d] array; see lsam_embedding_backward."""
+    L = _ready or _lib()
+    K, rows, apart = _embedding_tokens(tokens)
+    if dy.dim() != tokens.dim() + 1:
+        _refuse("dy has %d indices: %d are wanted" % (dy.dim(), tokens.dim() + 1))
+    _expect(dy, "dy", tokens, tuple(tokens.shape) + (dy.shape[-1],))
+    shape = tuple(tokens.shape[:-1]) + (vocab, dy.shape[-1])
+    if out is not None:
+        _expect(out, "out", tokens, shape, torch.float32)
+    d = lsam_embedding_desc(K, _dtype(dy, "dy"), DTYPE_FP32, scale, rows, vocab, dy.shape[-1], apart, 0, 0, 0, 0, *_of_replicas(dy))
+    at = C.byref(d)
+    with _On(tokens, stream) as raw:
+        need = L.lsam_embedding_workspace_bytes(at)
+        if need == 0 and K > 0:
+            _refuse(lsam.last_error())
+        dtable = torch.empty(shape, dtype=torch.float32, device=tokens.device) if out is None else out
+        d.dtable_stride, d.dtable_replica = _of_replicas(dtable)
+        ws = torch.empty(need, dtype=torch.uint8, device=tokens.device) if need else None
+        _check(L.lsam_embedding_backward(at, tokens.data_ptr(), dy.data_ptr(), dtable.data_ptr(), _ptr(ws), need, raw))
+    return dtable
+
+
+ResidualGradients = namedtuple("ResidualGradients", "dr dy dgate dw_pre dw_post")
+
+
+def _residual_desc(r, y, w_pre, w_post, gate, alpha, beta, eps):
+    if not 2 <= r.dim() <= 3:
+        _refuse("r has %d indices: [rows, dim] or [K, rows, dim] is wanted" % r.dim())
+    _expect(r, "r")
+    for t, what in ((y, "y"), (gate, "the gate")):
+        if t is not None:
+            _expect(t, what, r, r.shape, r.dtype)
+    K, rows, dim = (1,) * (3 - r.dim()) + tuple(r.shape)
+    d = lsam_residual_desc(K, _dtype(r, "r"), rows, dim, alpha, beta, eps)
+    for t, what, name in ((w_pre, "w_pre", "w_pre_replica"), (w_post, "w_post", "w_post_replica")):
+        if t is not None:
+            _expect(t, what, r, (K, dim) if t.dim() == 2 else (dim,), torch.float32)
+            if t.dim() == 2:
+                setattr(d, name, t.stride(0))
+    for t, name in ((r, "r"), (y, "y"), (gate, "gate")):
+        if t is not None:
+            _set_rows(d, name, t)
+    return d
+
+
+def _set_rows(d, name, t):
+    row, replica = _of_replicas(t)
+    setattr(d, name + "_stride", row)
+    setattr(d, name + "_replica", replica)
+
+
+def residual(r, y, w_pre, w_post=None, gate=None, alpha=1.0, beta=1.0, eps=1e-6, out=None, h=None, stream=None):
+    """(r', h) with r' = alpha r + beta sigmoid(gate) w_post n(y) and h = w_pre n(r'), n(x) = x / sqrt(mean x^2 + eps): what a block made of the
+    stream r joins it, and the stream as the next block reads it.  r, y, gate: [rows, dim], or [K, rows, dim] of K replicas; weights fp32 [dim],
+    or [K, dim].  No gate, no w_post (y as it is), no w_pre (h is None) and no y (r' is r itself) are possible; `out` for r' may be r; see
+    lsam_residual."""
+    L = _ready or _lib()
+    d = _residual_desc(r, y, w_pre, w_post, gate, alpha, beta, eps)
+    for t, what in ((out, "out"), (h, "h")):
+        if t is not None:
+            _expect(t, what, r, r.shape, r.dtype)
+    with _On(r, stream) as raw:
+        if y is None:
+            new = r
+        else:
+            new = torch.empty(r.shape, dtype=r.dtype, device=r.device) if out is None else out
+            _set_rows(d, "r_out", new)
+        if w_pre is None:
+            h = None
+        else:
+            h = torch.empty(r.shape, dtype=r.dtype, device=r.device) if h is None else h
+            _set_rows(d, "h", h)
+        _check(L.lsam_residual(C.byref(d), r.data_ptr(), _ptr(y), _ptr(gate), _ptr(w_pre), _ptr(w_post),
+                               None if y is None else new.data_ptr(), _ptr(h), raw))
+    return new, h
+
+
+def residual_backward(r, y, w_pre, dr, dh, w_post=None, gate=None, alpha=1.0, beta=1.0, eps=1e-6, dr_out=None, dy=None, dgate=None, dw_pre=None,
+                      dw_post=None, want_weights=True, stream=None):
+    """Gradients (dr, dy, dgate, dw_pre, dw_post) of `residual` for the gradients dr of r' (or None: 0) and dh of h; r is r' as `residual` left it.
+    Those of the weights are fp32, written whole; weights of K replicas are [K, dim], and their gradients may be parts of one [K, d]
+    array.  dr_out may be dr.  What has no gradient is None; see lsam_residual_backward."""
+    L = _ready or _lib()
+    d = _residual_desc(r, y, w_pre, w_post, gate, alpha, beta, eps)
+    if y is None:
+        w_post = gate = None
+    for t, what in ((w_pre, "w_pre"), (w_post, "w_post")):
+        if want_weights and t is not None and t.dim() != r.dim() - 1:
+            _refuse("%s is shared by replicas: pass their rows as one replica's for its gradient" % what)
+    for t, what in ((dr, "dr"), (dh, "dh"), (dr_out, "dr_out"), (dy, "dy"), (dgate, "dgate")):
+        if t is not None:
+            _expect(t, what, r, r.shape, r.dtype)
+    if w_pre is not None and dh is None:
+        _refuse("dh is missing: there is a w_pre")
+    for t, what, w in ((dw_pre, "dw_pre", w_pre), (dw_post, "dw_post", w_post)):
+        if t is not None and w is not None:
+            _expect(t, what, r, w.shape, torch.float32)
+    at, device = C.byref(d), r.device
+    with _On(r, stream) as raw:
+        new = lambda t, like, dtype: torch.empty(like.shape, dtype=dtype, device=device) if t is None else t  # noqa: E731
+        dr_out = new(dr_out, r, r.dtype)
+        dy = new(dy, r, r.dtype) if y is not None else None
+        dgate = new(dgate, r, r.dtype) if gate is not None else None
+        dw_pre = new(dw_pre, w_pre, torch.float32) if want_weights and w_pre is not None else None
+        dw_post = new(dw_post, w_post, torch.float32) if want_weights and w_post is not None else None
+        for t, name in ((dr, "dr"), (dh, "dh"), (dr_out, "dr_out"), (dy, "dy"), (dgate, "dgate")):
+            if t is not None:
+                _set_rows(d, name, t)
+        for t, name in ((dw_pre, "dw_pre_replica"), (dw_post, "dw_post_replica")):
+            if t is not None and t.dim() == 2:
+                setattr(d, name, t.stride(0))
+        need = L.lsam_residual_workspace_bytes(at) if dw_pre is not None or dw_post is not None else 0
+        ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+        _check(L.lsam_residual_backward(at, r.data_ptr(), _ptr(y), _ptr(gate), _ptr(w_pre), _ptr(w_post), _ptr(dr), _ptr(dh), dr_out.data_ptr(),
+                                        _ptr(dy), _ptr(dgate), _ptr(dw_pre), _ptr(dw_post), _ptr(ws), need, raw))
+    return ResidualGradients(dr_out, dy, dgate, dw_pre, dw_post)
