@@ -252,6 +252,44 @@ int lsam_residual_backward(const lsam_residual_desc* d, const void* r, const voi
                            const float* w_post, const void* dr, const void* dh, void* dr_out, void* dy, void* dgate, float* dw_pre,
                            float* dw_post, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- attention -----------------------------------------------------------------------------------
+ * For sequences packed one after the other, causal, with `heads` query heads in kv_heads groups of neighbours that share keys and values:
+ *   o_i = sum_j p_ij v_j,  p_ij = e^{scale q_i k_j - lse_i},  lse_i = ln sum_j e^{scale q_i k_j},  j over the rows of i's sequence up to i itself
+ * Sequence s is rows offsets[s] .. offsets[s + 1] - 1 (offsets [device] [seqs + 1] int64, not decreasing, within 0..rows: values outside are
+ * taken as the nearest inside).  What rows of no sequence hold reaches nothing, and outputs are not written there.
+ *   q, o   [device] [rows, heads, dim], k, v [rows, kv_heads, dim], of dtype; strides from row to row and from head to head are free, so q, k and
+ *          v may be parts of one array
+ *   lse    [device] [heads, rows] floats that receive lse, for the backward pass, or NULL
+ * Scores, sums and lse are fp32, and so are products of fp32 operands; bf16 operands meet probabilities rounded to bf16 (2^-9 of themselves, one rounding before
+ * the sum over j).  What is not finite in a row that i does not see does not reach o_i. */
+#define LSAM_ATTENTION_MAX_DIM 128
+typedef struct {
+  int64_t stride, head;                      /* from row to row, from head to head           */
+} lsam_heads;
+typedef struct {
+  int64_t rows;                              /* rows heads below 2^31                        */
+  int64_t seqs;                              /* below 2^31                                   */
+  int32_t heads, kv_heads;                   /* heads a multiple of kv_heads, at most 65536  */
+  int32_t dim;                               /* 1..LSAM_ATTENTION_MAX_DIM                    */
+  int32_t dtype;                             /* LSAM_DTYPE_*                                 */
+  float scale;                               /* finite, not negative                         */
+  lsam_heads q, k, v, o;
+  lsam_heads d_o, dq, dk, dv;                /* not looked at by the forward pass            */
+} lsam_attention_desc;
+int lsam_attention(const lsam_attention_desc* d, const int64_t* offsets, const void* q, const void* k, const void* v, void* o, float* lse,
+                   void* stream);
+
+/* Gradients of sum d_o o with respect to q, k and v:
+ *   ds_ij = p_ij (d_o_i v_j - d_o_i o_i),  dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij d_o_i,
+ * those of k and v summed over the heads of their group.  o and lse as the forward call left them; d_o, dq, dk, dv [device] of dtype, laid out
+ * as o, q, k and v, strides of their own.  bf16 operands meet p and ds rounded to bf16.
+ * workspace [device, 16-byte aligned], lsam_attention_workspace_bytes(d) bytes (0, with a message, for a descriptor that is refused); nothing in
+ * it has to survive the call. */
+size_t lsam_attention_workspace_bytes(const lsam_attention_desc* d);
+int lsam_attention_backward(const lsam_attention_desc* d, const int64_t* offsets, const void* q, const void* k, const void* v, const void* o,
+                            const float* lse, const void* d_o, void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,293 @@
+// What the attention kernels share: operands of the matrix units, tiles of rows in LDS, and which rows see which.
+//
+// Products are 32 x 32 results over 16 numbers at a time.  A lane's part of a result is one column (lane % 32) and sixteen rows, 8 (r / 4) +
+// 4 (lane / 32) + r % 4.  Its eight numbers of an operand may be any eight of the sixteen as long as both operands agree, so
+// results r = 8 t .. 8 t + 7 are, as they lie, the operand of a next product that sums over rows 16 t .. 16 t + 15: probabilities go from
+// one product into the next without leaving the lane.
+#pragma once
+#include "ops.h"
+
+namespace lsam {
+
+#if defined(__HIPCC__)
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+
+template <int DTYPE> struct Operand;
+template <> struct Operand<LSAM_DTYPE_BF16> {
+  typedef bf16x8 F;
+  static constexpr int B = 2;
+  static __device__ __forceinline__ f32x16 multiply(F a, F b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ F from(const f32x16& s, int t) {
+    F f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = static_cast<__bf16>(s[8 * t + e]);
+    return f;
+  }
+  static __device__ __forceinline__ bool not_finite(F f) {
+    const u32x4 w = __builtin_bit_cast(u32x4, f);
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bad |= (w[i] & 0x7F80u) == 0x7F80u || (w[i] & 0x7F800000u) == 0x7F800000u;
+    return bad;
+  }
+};
+// fp32 products stay in fp32: eight products over two numbers.
+template <> struct Operand<LSAM_DTYPE_FP32> {
+  typedef f32x8 F;
+  static constexpr int B = 4;
+  static __device__ __forceinline__ f32x16 multiply(F a, F b, f32x16 c) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ F from(const f32x16& s, int t) {
+    F f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = s[8 * t + e];
+    return f;
+  }
+  static __device__ __forceinline__ bool not_finite(F f) {
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float x = f[e];                  // (a bit cast of the element itself takes the first one)
+      bad |= (__builtin_bit_cast(unsigned, x) & 0x7F800000u) == 0x7F800000u;
+    }
+    return bad;
+  }
+};
+
+// Rows of DP numbers in LDS, in units of 16 bytes.  A unit's place in its row goes by the row, so that neither sixteen lanes that read
+// the same unit of sixteen rows nor sixteen that read 32 bytes of four rows meet in a bank.
+template <int DTYPE, int DP>
+struct Rows {
+  typedef typename Operand<DTYPE>::F F;
+  static constexpr int B = Operand<DTYPE>::B, U = DP * B / 16, BYTES = DP * B;
+  static __device__ __forceinline__ int turn(int row) {
+    if constexpr (DTYPE == LSAM_DTYPE_FP32) return row & 15 & (U - 1);
+    else if constexpr (U >= 16) return (row & 3) << 2 | (row >> 2 & 3);
+    else return (row >> 1 & 1) << 2 | (row >> 2 & 3);
+  }
+  static __device__ __forceinline__ int place(int row, int unit) { return row * BYTES + ((unit ^ turn(row)) << 4); }
+
+  // Row row0 + lane % 32, numbers 16 step + 8 (lane / 32) .. + 7.
+  static __device__ __forceinline__ F along(const lds_byte* tile, int row0, int step, int lane) {
+    typedef const __attribute__((address_space(3))) u32x4* unit_ptr;
+    const int row = row0 + (lane & 31);
+    if constexpr (DTYPE == LSAM_DTYPE_BF16) {
+      return __builtin_bit_cast(F, *reinterpret_cast<unit_ptr>(tile + place(row, step * 2 + (lane >> 5))));
+    } else {
+      const int u = step * 4 + (lane >> 5) * 2;
+      const f32x4 a = __builtin_bit_cast(f32x4, *reinterpret_cast<unit_ptr>(tile + place(row, u)));
+      const f32x4 b = __builtin_bit_cast(f32x4, *reinterpret_cast<unit_ptr>(tile + place(row, u + 1)));
+      return F{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    }
+  }
+  // Column col0 + lane % 32, rows row0 + 4 (lane / 32) + 0 .. 3 and 8 further: the rows of a lane's results.
+  static __device__ __forceinline__ F across(const lds_byte* tile, int row0, int col0, int lane) {
+    if constexpr (DTYPE == LSAM_DTYPE_BF16) {
+      // sixteen lanes read four rows of sixteen columns, four columns a lane, and each gets a column
+      typedef __attribute__((address_space(3))) s16x4* quad_ptr;
+      const int row = row0 + (lane >> 5) * 4 + (lane >> 2 & 3), col = col0 + (lane & 16) + (lane & 3) * 4;
+      lds_byte* p = const_cast<lds_byte*>(tile) + (col & 7) * 2;
+      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((quad_ptr)(p + place(row, col >> 3)));
+      const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((quad_ptr)(p + place(row + 8, col >> 3)));
+      return __builtin_bit_cast(F, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+      const int col = col0 + (lane & 31);
+      F f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int row = row0 + (lane >> 5) * 4 + (e & 3) + (e >> 2) * 8;
+        f[e] = *reinterpret_cast<const __attribute__((address_space(3))) float*>(tile + place(row, col >> 2) + (col & 3) * 4);
+      }
+      return f;
+    }
+  }
+};
+
+// Rows of a tensor for one head.
+struct HeadRows { const void* p; int64_t stride; };
+
+// 16 bytes of a row from unit u on; numbers behind `dim` count as 0.
+template <int DTYPE>
+__device__ __forceinline__ u32x4 load_unit(const typename Value<DTYPE>::T* row, int u, int dim) {
+  constexpr int N = 16 / Operand<DTYPE>::B;
+  const int n = dim - u * N;
+  u32x4 w = {0, 0, 0, 0};
+  if constexpr (DTYPE == LSAM_DTYPE_BF16) {
+    if (n >= N) {
+      w = __builtin_bit_cast(u32x4, *reinterpret_cast<const u16x8_any*>(row + u * N));
+    } else if (n > 0) {
+      u16x8 v;
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = e < n ? row[u * N + e] : (unsigned short)0;
+      w = __builtin_bit_cast(u32x4, v);
+    }
+  } else {
+    if (n >= N) {
+      w = __builtin_bit_cast(u32x4, *reinterpret_cast<const f32x4_any*>(row + u * N));
+    } else if (n > 0) {
+      f32x4 v;
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = e < n ? row[u * N + e] : 0.f;
+      w = __builtin_bit_cast(u32x4, v);
+    }
+  }
+  return w;
+}
+
+// A lane's operand straight from a row in memory: numbers 16 step + 8 (lane / 32) .. + 7.
+template <int DTYPE>
+__device__ __forceinline__ typename Operand<DTYPE>::F load_operand(const typename Value<DTYPE>::T* row, int step, int lane, int dim) {
+  if constexpr (DTYPE == LSAM_DTYPE_BF16) {
+    return __builtin_bit_cast(bf16x8, load_unit<DTYPE>(row, step * 2 + (lane >> 5), dim));
+  } else {
+    const int u = step * 4 + (lane >> 5) * 2;
+    const f32x4 a = __builtin_bit_cast(f32x4, load_unit<DTYPE>(row, u, dim)), b = __builtin_bit_cast(f32x4, load_unit<DTYPE>(row, u + 1, dim));
+    return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  }
+}
+
+// A workgroup's way of bringing ROWS rows into LDS: asked for, then put there; rows from `limit` on count as 0.
+template <int DTYPE, int DP, int ROWS, int THREADS>
+struct Stage {
+  typedef typename Value<DTYPE>::T T;
+  typedef Rows<DTYPE, DP> R;
+  static constexpr int N = ROWS * R::U / THREADS;
+  u32x4 w[N];
+  __device__ __forceinline__ void ask(const HeadRows& t, int64_t row0, int64_t limit, int dim) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int n = threadIdx.x + i * THREADS, row = n / R::U;
+      w[i] = u32x4{0, 0, 0, 0};
+      if (row0 + row < limit) w[i] = load_unit<DTYPE>(static_cast<const T*>(t.p) + (row0 + row) * t.stride, n % R::U, dim);
+    }
+  }
+  __device__ __forceinline__ void put(lds_byte* tile) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int n = threadIdx.x + i * THREADS;
+      *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(tile + R::place(n / R::U, n % R::U)) = w[i];
+    }
+  }
+};
+
+// acc += tile^T p over the 16 rows from row0 on, p a lane's column; where `masked`, a row that a lane's column does not see (outside first ..
+// last) adds nothing even if it is not finite: p is 0 there, but 0 times infinity is not.  So numbers that are not finite are left
+// out of the product, and added row by row to the columns that see them.
+template <int DTYPE, int DP>
+__device__ __forceinline__ void multiply_across(f32x16 (&acc)[DP / 32], const lds_byte* tile, int row0, typename Operand<DTYPE>::F p, int lane, bool masked,
+                                                int first, int last) {
+  typedef Operand<DTYPE> O;
+  typedef Rows<DTYPE, DP> R;
+  if (masked) {
+    bool bad = false;
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t) bad |= O::not_finite(R::across(tile, row0, t * 32, lane));
+    if (__any(bad)) {
+#pragma unroll 1
+      for (int k = -1; k < 16; ++k) {                       // -1: what is finite, of all rows; then what is not, of row k
+        const bool mine = (lane >> 5) == (k >> 2 & 1), seen = k < 0 || (row0 + k >= first && row0 + k <= last);
+        const int at = (k & 3) | (k >> 3) << 2;
+        typename O::F b;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) b[e] = k < 0 || (mine && e == at) ? p[e] : 0;
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t) {
+          typename O::F a = R::across(tile, row0, t * 32, lane);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) a[e] = (k < 0 ? __builtin_isfinite((float)a[e]) : mine && e == at && !__builtin_isfinite((float)a[e])) ? a[e] : 0;
+          if (k < 0) {
+            acc[t] = O::multiply(a, b, acc[t]);
+          } else {
+            f32x16 d;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) d[r] = 0.f;
+            d = O::multiply(a, b, d);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[t][r] = seen ? acc[t][r] + d[r] : acc[t][r];
+          }
+        }
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < DP / 32; ++t) acc[t] = O::multiply(R::across(tile, row0, t * 32, lane), p, acc[t]);
+}
+
+// factor times a lane's column of results to a row in memory.
+template <int DTYPE, int DP>
+__device__ __forceinline__ void store_column(const f32x16 (&acc)[DP / 32], float factor, typename Value<DTYPE>::T* row, int lane, int dim) {
+#pragma unroll
+  for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int d = t * 32 + g * 8 + (lane >> 5) * 4;
+      if (d + 4 <= dim) {
+        if constexpr (DTYPE == LSAM_DTYPE_BF16) {
+          u16x4 w;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = narrow(acc[t][4 * g + e] * factor);
+          *reinterpret_cast<u16x4_any*>(row + d) = w;
+        } else {
+          f32x4 w;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = acc[t][4 * g + e] * factor;
+          *reinterpret_cast<f32x4_any*>(row + d) = w;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (d + e < dim) Value<DTYPE>::put(row + d + e, acc[t][4 * g + e] * factor);
+      }
+    }
+}
+
+// What the other half of a wavefront holds in the same column.
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+
+// ---- sequences --------------------------------------------------------------------------------------
+// Sequence s is rows offsets[s] .. offsets[s + 1] - 1.  Whatever the offsets hold, no row outside 0..rows is touched.
+struct Sequences { const int64_t* offsets; int n; int rows; };
+
+// The last of `n` sequences that begins at or before `row`, or -1; the same row in all lanes, the last 64 candidates together.
+__device__ __forceinline__ int last_before(const Sequences& q, int64_t row) {
+  int lo = 0, hi = q.n;
+  while (hi - lo > 64) {
+    const int mid = (lo + hi) >> 1;
+    if (q.offsets[mid] <= row) lo = mid + 1; else hi = mid;
+  }
+  const int i = lo + (int)(threadIdx.x & 63);
+  return lo + __popcll(__ballot(i < hi && q.offsets[i < hi ? i : 0] <= row)) - 1;
+}
+// Begin and end of the sequence of a lane's row row0 + 0 .. 31; both 0 where it has none.
+__device__ __forceinline__ void span_of(const Sequences& q, int row0, int row, int& begin, int& end) {
+  const int top = row0 + 31 < q.rows ? row0 + 31 : q.rows - 1;
+  begin = end = 0;
+  if (row0 >= q.rows) return;
+  int lo = last_before(q, row0) + 1, hi = last_before(q, top) + 1;
+  while (lo < hi) {                                         // sequences of a lane: up to lo - 1 begin at or before its row
+    const int mid = (lo + hi) >> 1;
+    if (q.offsets[mid] <= row) lo = mid + 1; else hi = mid;
+  }
+  if (lo == 0 || row >= q.rows) return;
+  int64_t b = q.offsets[lo - 1], e = q.offsets[lo];
+  b = b < 0 ? 0 : b;
+  e = e < q.rows ? e : q.rows;
+  if (b <= row && row < e) { begin = (int)b; end = (int)e; }
+}
+__device__ __forceinline__ int smallest(int v) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) { const int o = __shfl_xor(v, d); v = o < v ? o : v; }
+  return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int largest(int v) { return -smallest(-v); }
+
+#endif
+
+}  // namespace lsam

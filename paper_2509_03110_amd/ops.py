@@ -21,12 +21,14 @@ TOP_MAX = 32
 ADAPTER_MAX_RANK = 64
 EMBEDDING_MAX_VOCAB = 1 << 22
 RESIDUAL_MAX_DIM = 16384
+ATTENTION_MAX_DIM = 128
 
 EXPORTS = ["lsam_dropout", "lsam_logprobs_workspace_bytes", "lsam_logprobs", "lsam_logprobs_backward",
            "lsam_recurrence_workspace_bytes", "lsam_recurrence_states", "lsam_recurrence", "lsam_recurrence_backward",
            "lsam_adapter_workspace_bytes", "lsam_adapter", "lsam_adapter_backward",
            "lsam_embedding", "lsam_embedding_workspace_bytes", "lsam_embedding_backward",
-           "lsam_residual", "lsam_residual_workspace_bytes", "lsam_residual_backward"]
+           "lsam_residual", "lsam_residual_workspace_bytes", "lsam_residual_backward",
+           "lsam_attention", "lsam_attention_workspace_bytes", "lsam_attention_backward"]
 
 
 class lsam_dropout_desc(C.Structure):
@@ -76,6 +78,15 @@ class lsam_residual_desc(C.Structure):
                                              "dw_post_replica")]
 
 
+class lsam_heads(C.Structure):
+    _fields_ = [("stride", C.c_int64), ("head", C.c_int64)]
+
+
+class lsam_attention_desc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("seqs", C.c_int64), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("dim", C.c_int32), ("dtype", C.c_int32),
+                ("scale", C.c_float)] + [(n, lsam_heads) for n in ("q", "k", "v", "o", "d_o", "dq", "dk", "dv")]
+
+
 _ready = None
 torch = None              # imported with the library's first use, as in lsam.py
 
@@ -122,6 +133,13 @@ def _lib():
         L.lsam_residual_workspace_bytes.argtypes = [res]
         L.lsam_residual_backward.restype = C.c_int
         L.lsam_residual_backward.argtypes = [res] + [vp] * 13 + [C.c_size_t, vp]
+        att = C.POINTER(lsam_attention_desc)
+        L.lsam_attention.restype = C.c_int
+        L.lsam_attention.argtypes = [att] + [vp] * 7
+        L.lsam_attention_workspace_bytes.restype = C.c_size_t
+        L.lsam_attention_workspace_bytes.argtypes = [att]
+        L.lsam_attention_backward.restype = C.c_int
+        L.lsam_attention_backward.argtypes = [att] + [vp] * 11 + [C.c_size_t, vp]
         _ready = L
     return _ready
 
@@ -584,3 +602,64 @@ def residual_backward(r, y, w_pre, dr, dh, w_post=None, gate=None, alpha=1.0, be
         _check(L.lsam_residual_backward(at, r.data_ptr(), _ptr(y), _ptr(gate), _ptr(w_pre), _ptr(w_post), _ptr(dr), _ptr(dh), dr_out.data_ptr(),
                                         _ptr(dy), _ptr(dgate), _ptr(dw_pre), _ptr(dw_post), _ptr(ws), need, raw))
     return ResidualGradients(dr_out, dy, dgate, dw_pre, dw_post)
+
+
+Attention = namedtuple("Attention", "o lse")
+
+
+def _attention_desc(q, k, v, offsets, scale):
+    for t, what in ((q, "q"), (k, "k"), (v, "v")):
+        if t.dim() != 3:
+            _refuse("%s has %d indices: [rows, heads, dim] is wanted" % (what, t.dim()))
+    if offsets.dim() != 1 or offsets.shape[0] < 1:
+        _refuse("the offsets must be [seqs + 1]")
+    _expect(q, "q")
+    rows, heads, dim = q.shape
+    kv_heads = k.shape[1]
+    _expect(k, "k", q, (rows, kv_heads, dim), q.dtype)
+    _expect(v, "v", q, (rows, kv_heads, dim), q.dtype)
+    _expect(offsets, "the offsets", q, None, torch.int64, True)
+    return lsam_attention_desc(rows, offsets.shape[0] - 1, heads, kv_heads, dim, _dtype(q, "q"), dim ** -0.5 if scale is None else scale,
+                               q.stride()[:2], k.stride()[:2], v.stride()[:2])
+
+
+def attention(q, k, v, offsets, scale=None, save=False, out=None, stream=None):
+    """Causal attention of packed sequences: o [rows, heads, dim] = softmax(scale q k) v for q [rows, heads, dim] and k, v [rows, kv_heads, dim],
+    heads a multiple of kv_heads, sequence s the rows offsets[s] .. offsets[s + 1] - 1 (int64 [seqs + 1]); scale is dim^-0.5 where none is
+    given.  Returns (o, lse), lse [heads, rows] in fp32 with `save`, for `attention_backward`, else None.  Rows of no sequence are not written;
+    see lsam_attention."""
+    L = _ready or _lib()
+    d = _attention_desc(q, k, v, offsets, scale)
+    if out is not None:
+        _expect(out, "out", q, q.shape, q.dtype)
+    with _On(q, stream) as raw:
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+        d.o = o.stride()[:2]
+        lse = torch.empty((d.heads, d.rows), dtype=torch.float32, device=q.device) if save else None
+        _check(L.lsam_attention(C.byref(d), offsets.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _ptr(lse), raw))
+    return Attention(o, lse)
+
+
+def attention_backward(q, k, v, offsets, o, lse, do, scale=None, dq=None, dk=None, dv=None, stream=None):
+    """Gradients (dq, dk, dv) of `attention` for the gradient do of o, in their types; o and lse are those it returned.  Rows of no sequence are not
+    written; see lsam_attention_backward."""
+    L = _ready or _lib()
+    d = _attention_desc(q, k, v, offsets, scale)
+    for t, what in ((o, "o"), (do, "do"), (dq, "dq")):
+        if t is not None:
+            _expect(t, what, q, q.shape, q.dtype)
+    for t, what in ((dk, "dk"), (dv, "dv")):
+        if t is not None:
+            _expect(t, what, q, k.shape, q.dtype)
+    _expect(lse, "lse", q, (d.heads, d.rows), torch.float32, True)
+    at, device = C.byref(d), q.device
+    with _On(q, stream) as raw:
+        dq = torch.empty(q.shape, dtype=q.dtype, device=device) if dq is None else dq
+        dk = torch.empty(k.shape, dtype=q.dtype, device=device) if dk is None else dk
+        dv = torch.empty(k.shape, dtype=q.dtype, device=device) if dv is None else dv
+        d.o, d.d_o, d.dq, d.dk, d.dv = (t.stride()[:2] for t in (o, do, dq, dk, dv))
+        need = L.lsam_attention_workspace_bytes(at)
+        ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+        _check(L.lsam_attention_backward(at, offsets.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), do.data_ptr(),
+                                         dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _ptr(ws), need, raw))
+    return dq, dk, dv
