@@ -290,6 +290,33 @@ int lsam_attention_backward(const lsam_attention_desc* d, const int64_t* offsets
                             const float* lse, const void* d_o, void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes,
                             void* stream);
 
+/* ---- attention of one token -----------------------------------------------------------------------
+ * The step of generation: one query of each of `seqs` sequences attends to `prefix` keys and values that all sequences share (an instruction, or one
+ * prompt of many answers), and then to the first lengths[s] of its own:  o = softmax(scale q k) v over both.  The prefix is read once for
+ * all sequences.  With nothing to attend to o is 0.
+ *   q, o               [device] [seqs, heads, dim] of dtype
+ *   k, v               [device] caches [seqs, capacity, kv_heads, dim] of dtype; places from lengths[s] on reach nothing
+ *   lengths            [device] [seqs] int32; values outside 0..capacity are taken as the nearest inside
+ *   prefix_k, prefix_v [device] [prefix, kv_heads, dim] of dtype; may be NULL where prefix is 0
+ * Numerics are those of lsam_attention.  All strides of k, v and the prefix may be anything not negative.
+ * workspace [device, 16-byte aligned], lsam_attention_step_workspace_bytes(d) bytes (0 where sequences and heads fill the chip; also 0, with a
+ * message, for a descriptor that is refused); nothing in it has to survive the call. */
+typedef struct {
+  int64_t seqs;                              /* seqs heads below 2^23                        */
+  int64_t capacity, prefix;                  /* below 2^31                                   */
+  int32_t heads, kv_heads;                   /* heads a multiple of kv_heads, at most 65536  */
+  int32_t dim;                               /* 1..LSAM_ATTENTION_MAX_DIM                    */
+  int32_t dtype;                             /* LSAM_DTYPE_*                                 */
+  float scale;                               /* finite, not negative                         */
+  lsam_heads q, o;                           /* stride: from sequence to sequence            */
+  lsam_heads k, v;                           /* stride: from place to place                  */
+  int64_t k_seq, v_seq;                      /* from sequence to sequence                    */
+  lsam_heads prefix_k, prefix_v;
+} lsam_attention_step_desc;
+size_t lsam_attention_step_workspace_bytes(const lsam_attention_step_desc* d);
+int lsam_attention_step(const lsam_attention_step_desc* d, const int32_t* lengths, const void* q, const void* k, const void* v,
+                        const void* prefix_k, const void* prefix_v, void* o, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

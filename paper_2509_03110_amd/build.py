@@ -8,7 +8,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblsam.so")
 SOURCES = ["lsam_api.hip", "kernels_stream.hip", "kernels_gemm.hip", "kernels_gemm_bf16.hip", "kernels_ce.hip", "kernels_conv.hip", "kernels_conv_gemm.hip",
            "kernels_probe.hip", "lsam_static.hip", "ops_dropout.hip",
-           "ops_logprobs.hip", "ops_recurrence.hip", "ops_adapter.hip", "ops_embedding.hip", "ops_residual.hip", "ops_attention.hip"]
+           "ops_logprobs.hip", "ops_recurrence.hip", "ops_adapter.hip", "ops_embedding.hip", "ops_residual.hip", "ops_attention.hip", "ops_attention_step.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-command-line-argument"]

@@ -248,6 +248,19 @@ __device__ __forceinline__ void store_column(const f32x16 (&acc)[DP / 32], float
     }
 }
 
+constexpr float kLog2e = 1.4426950408889634f;
+// Scores as powers of 2; above 0, since 0 times the -inf of a masked score is not -inf.
+__device__ __forceinline__ float exponent(float scale) { return __builtin_fmaxf(scale * kLog2e, 0x1p-126f); }
+
+__device__ __forceinline__ f32x16 zero16() {
+  f32x16 z;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) z[r] = 0.f;
+  return z;
+}
+// The row of a lane's result r.
+__device__ __forceinline__ int result_row(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
+
 // What the other half of a wavefront holds in the same column.
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
 

@@ -15,7 +15,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kRowsOf = 128;               // rows of a workgroup
-constexpr float kLog2e = 1.4426950408889634f;
 
 struct Tensor { void* p; int64_t stride, head; };
 
@@ -81,18 +80,6 @@ __device__ __forceinline__ void join_ranges(const Range& r, int& lo, int& hi) {
 
 template <int DTYPE>
 __device__ __forceinline__ typename Value<DTYPE>::T* head_of(const Tensor& t, int head) { return static_cast<typename Value<DTYPE>::T*>(t.p) + head * t.head; }
-
-__device__ __forceinline__ f32x16 zero16() {
-  f32x16 z;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) z[r] = 0.f;
-  return z;
-}
-// The row of a lane's result r.
-__device__ __forceinline__ int result_row(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
-
-// Scores as powers of 2; above 0, since 0 times the -inf of a masked score is not -inf.
-__device__ __forceinline__ float exponent(float scale) { return __builtin_fmaxf(scale * kLog2e, 0x1p-126f); }
 
 template <int DTYPE, int DP>
 __global__ __launch_bounds__(kThreads) void attention_kernel(AttentionParams p) {

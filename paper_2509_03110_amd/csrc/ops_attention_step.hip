@@ -1,0 +1,322 @@
+// lsam_attention_step: one token of each sequence attends to a prefix that all share and to its own cache.
+//
+//   step_kernel  keys are cut into parts.  Queries are columns, 32 a wavefront: of the prefix those of all sequences and of a group's heads,
+//                of a cache those of its sequence's group alone.  Where there are more than 32 a workgroup's wavefronts take columns of
+//                their own and share the keys; where there are not they share the columns, and take 32 keys of a tile each.  A
+//                part leaves the maximum, the sum and the weighted values of each column
+//   join_kernel  weighs the parts against each other
+#include "attention.h"
+
+namespace lsam {
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kKeys = 32 * kWaves;         // of a tile
+constexpr int kMaxParts = 64;              // of the prefix, and of a cache
+
+struct Cache { const void* k; const void* v; int64_t k_stride, k_head, k_seq, v_stride, v_head, v_seq; };
+
+struct StepParams {
+  Cache prefix, own;
+  const void* q; void* o;
+  int64_t q_stride, q_head, o_stride, o_head;
+  const int32_t* lengths;
+  int seqs, heads, group, kv_heads, dim, capacity, prefix_keys;
+  float scale;
+  int parts[2];                            // of the prefix, of a cache
+  int columns[2];                          // workgroups that the columns of a part take
+  unsigned prefix_blocks;                  // workgroups of the prefix come first
+  bool spread;                             // of the prefix: a wavefront has columns of its own
+  bool whole;                              // there is one part: o is written at once
+  float* sums; float* values;              // [parts][seqs heads][2], [parts][seqs heads][dim]
+};
+
+template <int DTYPE, int DP>
+__global__ __launch_bounds__(kThreads) void step_kernel(StepParams p) {
+  typedef typename Value<DTYPE>::T T;
+  typedef Operand<DTYPE> O;
+  typedef Rows<DTYPE, DP> R;
+  constexpr int STEPS = DP / 16;
+  __shared__ __attribute__((aligned(16))) unsigned char memory[2 * kKeys * R::BYTES];
+  __shared__ float of_waves[2][kWaves][32];
+  lds_byte* const tk = (lds_byte*)memory;
+  lds_byte* const tv = tk + kKeys * R::BYTES;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+  // what this workgroup does: a part of the prefix for some columns, or a part of a cache
+  const bool shared = blockIdx.x < p.prefix_blocks;
+  unsigned unit;
+  int seq = 0, kv, part, first_column;
+  int64_t keys;
+  if (shared) {
+    // those that read the same keys meet in an XCD
+    const unsigned i = blockIdx.x / 8;
+    unit = i / p.columns[0] * 8 + blockIdx.x % 8;
+    if (unit >= (unsigned)(p.kv_heads * p.parts[0])) return;
+    part = unit / p.kv_heads;
+    kv = unit % p.kv_heads;
+    first_column = (int)(i % p.columns[0]) * (p.spread ? kThreads / 2 : 32) + (p.spread ? wave * 32 : 0);
+    keys = p.prefix_keys;
+  } else {
+    unit = blockIdx.x - p.prefix_blocks;
+    first_column = (int)(unit % p.columns[1]) * 32;
+    unit /= p.columns[1];
+    kv = unit % p.kv_heads;
+    unit /= p.kv_heads;
+    seq = unit % p.seqs;
+    part = unit / p.seqs;
+    keys = p.lengths[seq];
+    keys = keys < 0 ? 0 : keys > p.capacity ? p.capacity : keys;
+  }
+  const bool spread = shared && p.spread;
+  const int all = shared ? p.seqs * p.group : p.group, column = first_column + (lane & 31);
+  const bool valid = column < all;
+  if (shared && valid) seq = column / p.group;
+  const int head = kv * p.group + (shared ? column % p.group : column);
+  const int64_t place = ((int64_t)(shared ? part : p.parts[0] + part) * p.seqs + seq) * p.heads + head;
+
+  const int64_t tiles = (keys + kKeys - 1) / kKeys, run = (tiles + p.parts[!shared] - 1) / p.parts[!shared] * kKeys;
+  const int64_t from = part * run, to = from + run < keys ? from + run : keys;
+  const Cache& c = shared ? p.prefix : p.own;
+  const int64_t of = shared ? 0 : seq;
+  const HeadRows k{static_cast<const T*>(c.k) + of * c.k_seq + kv * c.k_head, c.k_stride};
+  const HeadRows v{static_cast<const T*>(c.v) + of * c.v_seq + kv * c.v_head, c.v_stride};
+  Stage<DTYPE, DP, kKeys, kThreads> sk, sv;
+  sk.ask(k, from, to, p.dim);
+  sv.ask(v, from, to, p.dim);
+  typename O::F q[STEPS];
+  const T* q_row = static_cast<const T*>(p.q) + (valid ? seq * p.q_stride + head * p.q_head : 0);
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) q[s] = load_operand<DTYPE>(q_row, s, lane, valid ? p.dim : 0);
+  const float scale = exponent(p.scale);
+  float m = -__builtin_inff(), l = 0.f;
+  f32x16 acc[DP / 32];
+#pragma unroll
+  for (int t = 0; t < DP / 32; ++t) acc[t] = zero16();
+  for (int64_t j0 = from; j0 < to; j0 += kKeys) {
+    if (j0 > from) __syncthreads();
+    sk.put(tk);
+    sv.put(tv);
+    __syncthreads();
+    if (j0 + kKeys < to) {
+      sk.ask(k, j0 + kKeys, to, p.dim);
+      sv.ask(v, j0 + kKeys, to, p.dim);
+    }
+#pragma unroll 1
+    for (int i = spread ? 0 : wave; i < (spread ? kWaves : wave + 1); ++i) {
+      const int left = (int)(to - j0 - i * 32 < 32 ? to - j0 - i * 32 : 32);      // keys that are there; the others are zeros
+      if (left <= 0) break;
+      f32x16 s = zero16();
+#pragma unroll
+      for (int d = 0; d < STEPS; ++d) s = O::multiply(R::along(tk, i * 32, d, lane), q[d], s);
+      if (left < 32) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (result_row(e, lane) >= left) s[e] = -__builtin_inff();
+      }
+      float most = m;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) most = __builtin_fmaxf(most, s[e]);
+      most = __builtin_fmaxf(most, other_half(most));
+      const float base = most == -__builtin_inff() ? 0.f : most * scale;
+      if (__any(most > m)) {
+        const float less = __builtin_amdgcn_exp2f(m * scale - base);
+        l *= less;
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t) acc[t] *= less;
+      }
+      m = most;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[e] = __builtin_amdgcn_exp2f(s[e] * scale - base);
+        l += s[e];
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) multiply_across<DTYPE, DP>(acc, tv, i * 32 + t * 16, O::from(s, t), lane, false, 0, 0);
+    }
+  }
+  l += other_half(l);
+  m = m == -__builtin_inff() ? m : m * scale;
+  if (!spread) {
+    // the wavefronts' keys together: each column's maximum, then wavefront by wavefront
+    if (lane < 32) of_waves[0][wave][lane] = m;
+    __syncthreads();
+    float most = of_waves[0][0][lane & 31];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) most = __builtin_fmaxf(most, of_waves[0][w][lane & 31]);
+    const float less = __builtin_amdgcn_exp2f(m - (most == -__builtin_inff() ? 0.f : most));
+    if (lane < 32) of_waves[1][wave][lane] = l * less;
+    m = most;
+    float* const values = reinterpret_cast<float*>(memory);          // [wavefront - 1][number][lane]
+    if (wave > 0) {
+#pragma unroll
+      for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) values[(((wave - 1) * DP / 32 + t) * 16 + r) * 64 + lane] = acc[t][r] * less;
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    l = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) l += of_waves[1][w][lane & 31];
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        acc[t][r] *= less;
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) acc[t][r] += values[(((w - 1) * DP / 32 + t) * 16 + r) * 64 + lane];
+      }
+  }
+  if (!valid) return;
+  if (p.whole) {
+    store_column<DTYPE, DP>(acc, l == 0.f ? 0.f : 1.f / l, static_cast<T*>(p.o) + seq * p.o_stride + head * p.o_head, lane, p.dim);
+  } else {
+    if (lane < 32) { p.sums[place * 2] = m; p.sums[place * 2 + 1] = l; }
+    if (l != 0.f) store_column<LSAM_DTYPE_FP32, DP>(acc, 1.f, p.values + place * p.dim, lane, p.dim);
+  }
+}
+
+// A wavefront for each sequence and head: four columns a lane, lanes in groups of 32 take parts in turn.
+template <int DTYPE>
+__global__ __launch_bounds__(64) void join_kernel(StepParams p) {
+  const int lane = threadIdx.x, parts = p.parts[0] + p.parts[1];
+  const int64_t at = blockIdx.x, all = (int64_t)p.seqs * p.heads;
+  const int col = (lane & 31) * 4, n = p.dim - col < 4 ? p.dim - col : 4;
+  float most = -__builtin_inff();
+  for (int i = 0; i < parts; ++i) most = __builtin_fmaxf(most, p.sums[(i * all + at) * 2]);
+  const float base = most == -__builtin_inff() ? 0.f : most;
+  float l = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int i = lane >> 5; i < parts; i += 2) {
+    const float mine = p.sums[(i * all + at) * 2], sum = p.sums[(i * all + at) * 2 + 1];
+    if (sum == 0.f) continue;                                         // no keys: its values were not written
+    const float weight = __builtin_amdgcn_exp2f(mine - base);
+    l += sum * weight;
+    const float* from = p.values + (i * all + at) * p.dim + col;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < n) v[e] += from[e] * weight;
+  }
+  l += other_half(l);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] += other_half(v[e]);
+  if (lane >= 32) return;
+  typename Value<DTYPE>::T* o = static_cast<typename Value<DTYPE>::T*>(p.o) + at / p.heads * p.o_stride + at % p.heads * p.o_head + col;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (e < n) Value<DTYPE>::put(o + e, l == 0.f ? 0.f : v[e] / l);
+}
+
+// How keys are cut: about as many workgroups as two for each unit, of a tile of keys at least.
+constexpr int kGroups = 512;
+struct Plan { int parts[2], columns[2]; bool spread; unsigned prefix_blocks, blocks; size_t values_at, bytes; };
+Plan plan(const lsam_attention_step_desc* d) {
+  Plan c{};
+  const int group = d->heads / d->kv_heads;
+  const int64_t together = d->seqs * group;
+  c.spread = together > 32;
+  c.columns[0] = (int)(c.spread ? (together + kThreads / 2 - 1) / (kThreads / 2) : 1);
+  c.columns[1] = (group + 31) / 32;
+  const int64_t keys[2] = {d->prefix, d->capacity}, base[2] = {(int64_t)d->kv_heads * c.columns[0], d->seqs * d->kv_heads * c.columns[1]};
+  for (int i = 0; i < 2; ++i) {
+    int64_t parts = (kGroups + base[i] - 1) / base[i];
+    const int64_t tiles = (keys[i] + kKeys - 1) / kKeys;
+    parts = parts < tiles ? parts : tiles;
+    c.parts[i] = (int)(parts < kMaxParts ? parts : kMaxParts);
+  }
+  c.prefix_blocks = (unsigned)(((int64_t)d->kv_heads * c.parts[0] + 7) / 8 * 8 * c.columns[0]);
+  c.blocks = c.prefix_blocks + (unsigned)(base[1] * c.parts[1]);
+  const int parts = c.parts[0] + c.parts[1];
+  const size_t places = (size_t)parts * d->seqs * d->heads;
+  if (parts > 1) {
+    c.values_at = (places * 8 + 255) / 256 * 256;
+    c.bytes = c.values_at + places * d->dim * 4;
+  }
+  return c;
+}
+
+int check(const lsam_attention_step_desc* d, const char* who) {
+  if (!d) return refuse(LSAM_EINVAL, "%s: the descriptor is NULL", who);
+  if (!known_dtype(d->dtype)) return refuse(LSAM_EINVAL, "%s: dtype %d is none of LSAM_DTYPE_*", who, d->dtype);
+  if (d->kv_heads < 1 || d->heads < 1 || d->heads > 65536 || d->heads % d->kv_heads)
+    return refuse(LSAM_EINVAL, "%s: heads must be a multiple of kv_heads, in 1..65536", who);
+  if (d->dim < 1 || d->dim > LSAM_ATTENTION_MAX_DIM) return refuse(LSAM_EINVAL, "%s: dim must be in 1..%d", who, LSAM_ATTENTION_MAX_DIM);
+  if (d->seqs < 0 || d->seqs >= 1 << 23 || d->seqs * d->heads >= 1 << 23) return refuse(LSAM_EINVAL, "%s: seqs times heads must be below 2^23", who);
+  if (d->capacity < 0 || d->capacity >= 1ll << 31 || d->prefix < 0 || d->prefix >= 1ll << 31)
+    return refuse(LSAM_EINVAL, "%s: capacity and prefix must be in 0..2^31-1", who);
+  if (!(d->scale >= 0.f) || d->scale > 3e38f) return refuse(LSAM_EINVAL, "%s: the scale must be finite and not negative", who);
+  return LSAM_OK;
+}
+
+// Rows that are only read, of any strides that are not negative.
+Arg read_only(const lsam_attention_step_desc* d, const char* name, const void* p, int64_t seqs, int64_t seq, int64_t rows, const lsam_heads& t, int heads) {
+  const int b = dtype_bytes(d->dtype);
+  if (seqs == 0 || rows == 0) return Arg{name, p, 0, b, false};
+  if (t.stride < 0 || t.head < 0 || (seqs > 1 && seq < 0)) return Arg{name, p, -1, b, false};
+  const __int128 n = ((__int128)(seqs - 1) * (seqs > 1 ? seq : 0) + (__int128)(rows - 1) * t.stride + (__int128)(heads - 1) * t.head + d->dim) * b;
+  return Arg{name, p, n < ((__int128)1 << 46) ? (int64_t)n : -1, b, false};
+}
+
+template <int DTYPE, int DP>
+void launch(const StepParams& p, unsigned blocks, hipStream_t s) {
+  if (blocks) step_kernel<DTYPE, DP><<<blocks, kThreads, 0, s>>>(p);
+  if (!p.whole) join_kernel<DTYPE><<<(unsigned)(p.seqs * p.heads), 64, 0, s>>>(p);
+}
+
+}  // namespace
+}  // namespace lsam
+
+using namespace lsam;
+
+extern "C" size_t lsam_attention_step_workspace_bytes(const lsam_attention_step_desc* d) {
+  if (check(d, "attention_step") != LSAM_OK) return 0;
+  return d->seqs ? plan(d).bytes : 0;
+}
+
+extern "C" int lsam_attention_step(const lsam_attention_step_desc* d, const int32_t* lengths, const void* q, const void* k, const void* v,
+                                   const void* prefix_k, const void* prefix_v, void* o, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "attention_step";
+  int rc = check(d, who);
+  if (rc != LSAM_OK) return rc;
+  if (d->seqs == 0) return LSAM_OK;
+  const Plan c = plan(d);
+  const int b = dtype_bytes(d->dtype);
+  const Arg args[] = {read_only(d, "q", q, 1, 0, d->seqs, d->q, d->heads), read_only(d, "k", k, d->seqs, d->k_seq, d->capacity, d->k, d->kv_heads),
+                      read_only(d, "v", v, d->seqs, d->v_seq, d->capacity, d->v, d->kv_heads),
+                      read_only(d, "prefix_k", prefix_k, 1, 0, d->prefix, d->prefix_k, d->kv_heads),
+                      read_only(d, "prefix_v", prefix_v, 1, 0, d->prefix, d->prefix_v, d->kv_heads),
+                      {"lengths", lengths, d->seqs * 4, 4, false},
+                      [&] {
+                        if (d->heads > 1 && d->o.head >= d->dim && d->seqs > 1 && (__int128)d->o.stride >= (__int128)(d->heads - 1) * d->o.head + d->dim)
+                          return matrices("o", o, 1, 0, d->seqs, d->o.stride, (d->heads - 1) * d->o.head + d->dim, b, true);
+                        Arg a = matrices("o", o, d->heads, d->o.head, d->seqs, d->o.stride, d->dim, b, true);
+                        if (!apart(d->heads, d->o.head, d->seqs, d->o.stride, d->dim)) a.bytes = -1;
+                        return a;
+                      }()};
+  constexpr int n = sizeof args / sizeof args[0];
+  rc = check_values(args, n, who);
+  if (rc == LSAM_OK) rc = check_apart(args, n, who);
+  if (rc == LSAM_OK) rc = check_workspace(args, n, workspace, workspace_bytes, c.bytes, 16, who);
+  if (rc != LSAM_OK) return rc;
+  StepParams p{};
+  p.prefix = Cache{prefix_k, prefix_v, d->prefix_k.stride, d->prefix_k.head, 0, d->prefix_v.stride, d->prefix_v.head, 0};
+  p.own = Cache{k, v, d->k.stride, d->k.head, d->k_seq, d->v.stride, d->v.head, d->v_seq};
+  p.q = q; p.o = o;
+  p.q_stride = d->q.stride; p.q_head = d->q.head; p.o_stride = d->o.stride; p.o_head = d->o.head;
+  p.lengths = lengths;
+  p.seqs = (int)d->seqs; p.heads = d->heads; p.kv_heads = d->kv_heads; p.group = d->heads / d->kv_heads; p.dim = d->dim;
+  p.capacity = (int)d->capacity; p.prefix_keys = (int)d->prefix; p.scale = d->scale;
+  for (int i = 0; i < 2; ++i) { p.parts[i] = c.parts[i]; p.columns[i] = c.columns[i]; }
+  p.prefix_blocks = c.prefix_blocks; p.spread = c.spread;
+  p.whole = c.parts[0] + c.parts[1] == 1;
+  p.sums = static_cast<float*>(workspace);
+  p.values = reinterpret_cast<float*>(static_cast<char*>(workspace) + c.values_at);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (d->dtype == LSAM_DTYPE_BF16) {
+    if (p.dim <= 64) launch<LSAM_DTYPE_BF16, 64>(p, c.blocks, s); else launch<LSAM_DTYPE_BF16, 128>(p, c.blocks, s);
+  } else {
+    if (p.dim <= 64) launch<LSAM_DTYPE_FP32, 64>(p, c.blocks, s); else launch<LSAM_DTYPE_FP32, 128>(p, c.blocks, s);
+  }
+  return launched();
+}

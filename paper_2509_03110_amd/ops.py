@@ -28,7 +28,8 @@ EXPORTS = ["lsam_dropout", "lsam_logprobs_workspace_bytes", "lsam_logprobs", "ls
            "lsam_adapter_workspace_bytes", "lsam_adapter", "lsam_adapter_backward",
            "lsam_embedding", "lsam_embedding_workspace_bytes", "lsam_embedding_backward",
            "lsam_residual", "lsam_residual_workspace_bytes", "lsam_residual_backward",
-           "lsam_attention", "lsam_attention_workspace_bytes", "lsam_attention_backward"]
+           "lsam_attention", "lsam_attention_workspace_bytes", "lsam_attention_backward",
+           "lsam_attention_step_workspace_bytes", "lsam_attention_step"]
 
 
 class lsam_dropout_desc(C.Structure):
@@ -87,6 +88,12 @@ class lsam_attention_desc(C.Structure):
                 ("scale", C.c_float)] + [(n, lsam_heads) for n in ("q", "k", "v", "o", "d_o", "dq", "dk", "dv")]
 
 
+class lsam_attention_step_desc(C.Structure):
+    _fields_ = [("seqs", C.c_int64), ("capacity", C.c_int64), ("prefix", C.c_int64), ("heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("dim", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float), ("q", lsam_heads), ("o", lsam_heads), ("k", lsam_heads),
+                ("v", lsam_heads), ("k_seq", C.c_int64), ("v_seq", C.c_int64), ("prefix_k", lsam_heads), ("prefix_v", lsam_heads)]
+
+
 _ready = None
 torch = None              # imported with the library's first use, as in lsam.py
 
@@ -140,6 +147,11 @@ def _lib():
         L.lsam_attention_workspace_bytes.argtypes = [att]
         L.lsam_attention_backward.restype = C.c_int
         L.lsam_attention_backward.argtypes = [att] + [vp] * 11 + [C.c_size_t, vp]
+        step = C.POINTER(lsam_attention_step_desc)
+        L.lsam_attention_step_workspace_bytes.restype = C.c_size_t
+        L.lsam_attention_step_workspace_bytes.argtypes = [step]
+        L.lsam_attention_step.restype = C.c_int
+        L.lsam_attention_step.argtypes = [step] + [vp] * 8 + [C.c_size_t, vp]
         _ready = L
     return _ready
 
@@ -663,3 +675,38 @@ def attention_backward(q, k, v, offsets, o, lse, do, scale=None, dq=None, dk=Non
         _check(L.lsam_attention_backward(at, offsets.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), do.data_ptr(),
                                          dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _ptr(ws), need, raw))
     return dq, dk, dv
+
+
+def attention_step(q, k, v, lengths, prefix_k=None, prefix_v=None, scale=None, out=None, stream=None):
+    """One token of each sequence: softmax(scale q k) v [seqs, heads, dim] over the prefix [prefix, kv_heads, dim], which all sequences share, and
+    the first lengths[s] (int32 [seqs]) places of the caches k, v [seqs, capacity, kv_heads, dim]; 0 where both are empty.  scale is dim^-0.5 where
+    none is given; see lsam_attention_step."""
+    L = _ready or _lib()
+    for t, what, n in ((q, "q", 3), (k, "k", 4), (v, "v", 4), (prefix_k, "prefix_k", 3), (prefix_v, "prefix_v", 3)):
+        if t is not None and t.dim() != n:
+            _refuse("%s has %d indices: %d are wanted" % (what, t.dim(), n))
+    if (prefix_k is None) != (prefix_v is None):
+        _refuse("of prefix_k and prefix_v one is missing")
+    _expect(q, "q")
+    (seqs, heads, dim), (_, capacity, kv_heads, _) = q.shape, k.shape
+    _expect(k, "k", q, (seqs, capacity, kv_heads, dim), q.dtype)
+    _expect(v, "v", q, (seqs, capacity, kv_heads, dim), q.dtype)
+    _expect(lengths, "the lengths", q, (seqs,), torch.int32, True)
+    prefix, pk, pv = 0, (0, 0), (0, 0)
+    if prefix_k is not None:
+        prefix = prefix_k.shape[0]
+        _expect(prefix_k, "prefix_k", q, (prefix, kv_heads, dim), q.dtype)
+        _expect(prefix_v, "prefix_v", q, (prefix, kv_heads, dim), q.dtype)
+        pk, pv = prefix_k.stride()[:2], prefix_v.stride()[:2]
+    if out is not None:
+        _expect(out, "out", q, q.shape, q.dtype)
+    ks, vs = k.stride(), v.stride()
+    with _On(q, stream) as raw:
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+        d = lsam_attention_step_desc(seqs, capacity, prefix, heads, kv_heads, dim, _dtype(q, "q"), dim ** -0.5 if scale is None else scale,
+                                     q.stride()[:2], o.stride()[:2], ks[1:3], vs[1:3], ks[0], vs[0], pk, pv)
+        need = L.lsam_attention_step_workspace_bytes(C.byref(d))
+        ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+        _check(L.lsam_attention_step(C.byref(d), lengths.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(prefix_k), _ptr(prefix_v),
+                                     o.data_ptr(), _ptr(ws), need, raw))
+    return o
