@@ -26,12 +26,16 @@ template <> struct Operand<LSAM_DTYPE_BF16> {
     for (int e = 0; e < 8; ++e) f[e] = static_cast<__bf16>(s[8 * t + e]);
     return f;
   }
-  static __device__ __forceinline__ bool not_finite(F f) {
-    const u32x4 w = __builtin_bit_cast(u32x4, f);
-    bool bad = false;
+  // 0 in place of what is not finite, whose sign bits come into `found`.
+  static __device__ __forceinline__ F clean(F f, unsigned& found) {
+    u32x4 w = __builtin_bit_cast(u32x4, f);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) bad |= (w[i] & 0x7F80u) == 0x7F80u || (w[i] & 0x7F800000u) == 0x7F800000u;
-    return bad;
+    for (int i = 0; i < 4; ++i) {
+      const unsigned top = ((w[i] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;      // an exponent of ones carries into the sign's place
+      found |= top;
+      w[i] &= ~(top | (top - (top >> 15)));
+    }
+    return __builtin_bit_cast(F, w);
   }
 };
 // fp32 products stay in fp32: eight products over two numbers.
@@ -49,14 +53,14 @@ template <> struct Operand<LSAM_DTYPE_FP32> {
     for (int e = 0; e < 8; ++e) f[e] = s[8 * t + e];
     return f;
   }
-  static __device__ __forceinline__ bool not_finite(F f) {
-    bool bad = false;
+  static __device__ __forceinline__ F clean(F f, unsigned& found) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float x = f[e];                  // (a bit cast of the element itself takes the first one)
-      bad |= (__builtin_bit_cast(unsigned, x) & 0x7F800000u) == 0x7F800000u;
+      const bool fine = __builtin_isfinite(f[e]);
+      found |= fine ? 0u : 1u;
+      f[e] = fine ? f[e] : 0.f;
     }
-    return bad;
+    return f;
   }
 };
 
@@ -65,47 +69,68 @@ template <> struct Operand<LSAM_DTYPE_FP32> {
 template <int DTYPE, int DP>
 struct Rows {
   typedef typename Operand<DTYPE>::F F;
-  static constexpr int B = Operand<DTYPE>::B, U = DP * B / 16, BYTES = DP * B;
+  static constexpr int B = Operand<DTYPE>::B, WIDE = DP > 64 ? 128 : DP > 32 ? 64 : 32, U = WIDE * B / 16, BYTES = WIDE * B;
   static __device__ __forceinline__ int turn(int row) {
     if constexpr (DTYPE == LSAM_DTYPE_FP32) return row & 15 & (U - 1);
-    else if constexpr (U >= 16) return (row & 3) << 2 | (row >> 2 & 3);
-    else return (row >> 1 & 1) << 2 | (row >> 2 & 3);
+    else if constexpr (U == 16) return (row & 3) << 2 | (row >> 2 & 3);
+    else if constexpr (U == 8) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
+    else return row >> 2 & 3;
   }
   static __device__ __forceinline__ int place(int row, int unit) { return row * BYTES + ((unit ^ turn(row)) << 4); }
 
-  // Row row0 + lane % 32, numbers 16 step + 8 (lane / 32) .. + 7.
-  static __device__ __forceinline__ F along(const lds_byte* tile, int row0, int step, int lane) {
-    typedef const __attribute__((address_space(3))) u32x4* unit_ptr;
-    const int row = row0 + (lane & 31);
-    if constexpr (DTYPE == LSAM_DTYPE_BF16) {
-      return __builtin_bit_cast(F, *reinterpret_cast<unit_ptr>(tile + place(row, step * 2 + (lane >> 5))));
-    } else {
-      const int u = step * 4 + (lane >> 5) * 2;
-      const f32x4 a = __builtin_bit_cast(f32x4, *reinterpret_cast<unit_ptr>(tile + place(row, u)));
-      const f32x4 b = __builtin_bit_cast(f32x4, *reinterpret_cast<unit_ptr>(tile + place(row, u + 1)));
-      return F{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-    }
-  }
-  // Column col0 + lane % 32, rows row0 + 4 (lane / 32) + 0 .. 3 and 8 further: the rows of a lane's results.
-  static __device__ __forceinline__ F across(const lds_byte* tile, int row0, int col0, int lane) {
-    if constexpr (DTYPE == LSAM_DTYPE_BF16) {
-      // sixteen lanes read four rows of sixteen columns, four columns a lane, and each gets a column
-      typedef __attribute__((address_space(3))) s16x4* quad_ptr;
-      const int row = row0 + (lane >> 5) * 4 + (lane >> 2 & 3), col = col0 + (lane & 16) + (lane & 3) * 4;
-      lds_byte* p = const_cast<lds_byte*>(tile) + (col & 7) * 2;
-      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((quad_ptr)(p + place(row, col >> 3)));
-      const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((quad_ptr)(p + place(row + 8, col >> 3)));
-      return __builtin_bit_cast(F, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
-    } else {
-      const int col = col0 + (lane & 31);
-      F f;
+};
+
+// A lane's places in a tile of rows, found once: what is read from a tile whose address is known when this is compiled takes an
+// offset beside them and no arithmetic.
+template <int DTYPE, int DP> struct Reader;
+template <int DP> struct Reader<LSAM_DTYPE_BF16, DP> {
+  typedef Rows<LSAM_DTYPE_BF16, DP> R;
+  typedef bf16x8 F;
+  unsigned row[DP / 16], column[DP / 32][2];
+  __device__ __forceinline__ Reader(int lane) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int row = row0 + (lane >> 5) * 4 + (e & 3) + (e >> 2) * 8;
-        f[e] = *reinterpret_cast<const __attribute__((address_space(3))) float*>(tile + place(row, col >> 2) + (col & 3) * 4);
-      }
-      return f;
+    for (int s = 0; s < DP / 16; ++s) row[s] = R::place(lane & 31, s * 2 + (lane >> 5));
+    // sixteen lanes read four rows of sixteen columns, four columns a lane, and each gets a column
+    const int r = (lane >> 5) * 4 + (lane >> 2 & 3), col = (lane & 16) + (lane & 3) * 4;
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) column[t][i] = R::place(r + 8 * i, t * 4 + (col >> 3)) + (col & 7) * 2;
+  }
+  // Row row0 + lane % 32, numbers 16 step + 8 (lane / 32) .. + 7.
+  __device__ __forceinline__ F along(const lds_byte* tile, int row0, int step) const {
+    return __builtin_bit_cast(F, *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(tile + row0 * R::BYTES + row[step]));
+  }
+  // Column 32 t + lane % 32, rows row0 + 4 (lane / 32) + 0 .. 3 and 8 further: the rows of a lane's results.
+  __device__ __forceinline__ F across(const lds_byte* tile, int row0, int t) const {
+    typedef __attribute__((address_space(3))) s16x4* quad_ptr;
+    lds_byte* const p = const_cast<lds_byte*>(tile) + row0 * R::BYTES;
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((quad_ptr)(p + column[t][0]));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((quad_ptr)(p + column[t][1]));
+    return __builtin_bit_cast(F, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+template <int DP> struct Reader<LSAM_DTYPE_FP32, DP> {
+  typedef Rows<LSAM_DTYPE_FP32, DP> R;
+  typedef f32x8 F;
+  int lane;
+  __device__ __forceinline__ Reader(int l) : lane(l) {}
+  __device__ __forceinline__ F along(const lds_byte* tile, int row0, int step) const {
+    typedef const __attribute__((address_space(3))) u32x4* unit_ptr;
+    const int r = row0 + (lane & 31), u = step * 4 + (lane >> 5) * 2;
+    const f32x4 a = __builtin_bit_cast(f32x4, *reinterpret_cast<unit_ptr>(tile + R::place(r, u)));
+    const f32x4 b = __builtin_bit_cast(f32x4, *reinterpret_cast<unit_ptr>(tile + R::place(r, u + 1)));
+    return F{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  }
+  __device__ __forceinline__ F across(const lds_byte* tile, int row0, int t) const {
+    const int col = t * 32 + (lane & 31);
+    F f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int r = row0 + (lane >> 5) * 4 + (e & 3) + (e >> 2) * 8;
+      f[e] = *reinterpret_cast<const __attribute__((address_space(3))) float*>(tile + R::place(r, col >> 2) + (col & 3) * 4);
     }
+    return f;
   }
 };
 
@@ -152,72 +177,138 @@ __device__ __forceinline__ typename Operand<DTYPE>::F load_operand(const typenam
   }
 }
 
-// A workgroup's way of bringing ROWS rows into LDS: asked for, then put there; rows from `limit` on count as 0.
-template <int DTYPE, int DP, int ROWS, int THREADS>
+// A workgroup's way of bringing ROWS rows into LDS; rows from `limit` on count as 0.  Rows that are aligned to 16 bytes (DIRECT) go there
+// without passing through registers: asked for a tile ahead, there when the wavefront has waited for its loads.  Others
+// are asked for a tile ahead as well, and put there when they are needed.
+template <int DTYPE, int DP, int ROWS, int THREADS, bool DIRECT>
 struct Stage {
   typedef typename Value<DTYPE>::T T;
   typedef Rows<DTYPE, DP> R;
   static constexpr int N = ROWS * R::U / THREADS;
-  u32x4 w[N];
-  __device__ __forceinline__ void ask(const HeadRows& t, int64_t row0, int64_t limit, int dim) {
+  static_assert(N * THREADS == ROWS * R::U, "whole rounds of loads");
+  const T* p;
+  int64_t stride;
+  int dim;
+  u32x4 w[DIRECT ? 1 : N];
+  unsigned at[DIRECT ? N : 1];
+  __device__ __forceinline__ void init(const HeadRows& t, int d) {
+    p = static_cast<const T*>(t.p);
+    stride = t.stride;
+    dim = d;
+    if constexpr (DIRECT) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int n = threadIdx.x + i * THREADS, row = n / R::U;
-      w[i] = u32x4{0, 0, 0, 0};
-      if (row0 + row < limit) w[i] = load_unit<DTYPE>(static_cast<const T*>(t.p) + (row0 + row) * t.stride, n % R::U, dim);
+      for (int i = 0; i < N; ++i) {
+        const int n = threadIdx.x + i * THREADS, row = n / R::U, unit = (n % R::U) ^ R::turn(row);
+        at[i] = unit * 16 < dim * R::B ? (unsigned)(row * stride * R::B) + unit * 16 : 0x7FFFFFF0u;
+      }
+    }
+  }
+  __device__ __forceinline__ void ask(lds_byte* tile, int64_t row0, int64_t limit) {
+    if constexpr (DIRECT) {
+      const int64_t rows = limit - row0 < ROWS ? limit - row0 : ROWS;
+      const unsigned bytes = rows > 0 ? (unsigned)(((rows - 1) * stride + dim) * R::B) : 0;
+      const unsigned long long a = reinterpret_cast<unsigned long long>(p + row0 * stride);
+      const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)a), hi = __builtin_amdgcn_readfirstlane((unsigned)(a >> 32));
+      const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((unsigned long long)hi << 32 | lo), 0,
+                                                                            __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+      const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(tile + (wave * 64 + i * THREADS) * 16), 16, at[i], 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int n = threadIdx.x + i * THREADS, row = n / R::U;
+        w[i] = u32x4{0, 0, 0, 0};
+        if (row0 + row < limit) w[i] = load_unit<DTYPE>(p + (row0 + row) * stride, n % R::U, dim);
+      }
     }
   }
   __device__ __forceinline__ void put(lds_byte* tile) const {
+    if constexpr (!DIRECT) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int n = threadIdx.x + i * THREADS;
-      *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(tile + R::place(n / R::U, n % R::U)) = w[i];
+      for (int i = 0; i < N; ++i) {
+        const int n = threadIdx.x + i * THREADS;
+        *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(tile + R::place(n / R::U, n % R::U)) = w[i];
+      }
     }
   }
 };
+// Waits for the wavefront's own loads, and for the other wavefronts.
+__device__ __forceinline__ void arrived() {
+  __builtin_amdgcn_s_waitcnt(0x0070);                      // no load on its way, no LDS access
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+// Whether rows can go to LDS directly: 16-byte units all the way, and a tile within 32-bit offsets.
+inline bool direct(const void* p, int64_t stride, int64_t head, int64_t seq, int dim, int dtype) {
+  const int b = dtype_bytes(dtype);
+  return !misaligned(p, 16) && stride * b % 16 == 0 && head * b % 16 == 0 && seq * b % 16 == 0 && dim * b % 16 == 0 && stride < 1 << 20;
+}
 
-// acc += tile^T p over the 16 rows from row0 on, p a lane's column; where `masked`, a row that a lane's column does not see (outside first ..
-// last) adds nothing even if it is not finite: p is 0 there, but 0 times infinity is not.  So numbers that are not finite are left
-// out of the product, and added row by row to the columns that see them.
-template <int DTYPE, int DP>
-__device__ __forceinline__ void multiply_across(f32x16 (&acc)[DP / 32], const lds_byte* tile, int row0, typename Operand<DTYPE>::F p, int lane, bool masked,
-                                                int first, int last) {
-  typedef Operand<DTYPE> O;
-  typedef Rows<DTYPE, DP> R;
-  if (masked) {
-    bool bad = false;
+constexpr float kLog2e = 1.4426950408889634f;
+// Scores as powers of 2; above 0, since 0 times the -inf of a masked score is not -inf.
+__device__ __forceinline__ float exponent(float scale) { return __builtin_fmaxf(scale * kLog2e, 0x1p-126f); }
+
+__device__ __forceinline__ f32x16 zero16() {
+  f32x16 z;
 #pragma unroll
-    for (int t = 0; t < DP / 32; ++t) bad |= O::not_finite(R::across(tile, row0, t * 32, lane));
-    if (__any(bad)) {
-#pragma unroll 1
-      for (int k = -1; k < 16; ++k) {                       // -1: what is finite, of all rows; then what is not, of row k
-        const bool mine = (lane >> 5) == (k >> 2 & 1), seen = k < 0 || (row0 + k >= first && row0 + k <= last);
-        const int at = (k & 3) | (k >> 3) << 2;
-        typename O::F b;
+  for (int r = 0; r < 16; ++r) z[r] = 0.f;
+  return z;
+}
+// The row of a lane's result r.
+__device__ __forceinline__ int result_row(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
+
+// N products whose operand from LDS is asked for AHEAD products before: a wavefront's registers do not hold more than that of
+// them, and vector arithmetic may move in between.
+template <int N, int AHEAD, typename Load, typename Use>
+__device__ __forceinline__ void products(Load load, Use use) {
+  decltype(load(0)) ring[AHEAD];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) b[e] = k < 0 || (mine && e == at) ? p[e] : 0;
+  for (int n = 0; n < AHEAD && n < N; ++n) ring[n] = load(n);
 #pragma unroll
-        for (int t = 0; t < DP / 32; ++t) {
-          typename O::F a = R::across(tile, row0, t * 32, lane);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) a[e] = (k < 0 ? __builtin_isfinite((float)a[e]) : mine && e == at && !__builtin_isfinite((float)a[e])) ? a[e] : 0;
-          if (k < 0) {
-            acc[t] = O::multiply(a, b, acc[t]);
-          } else {
-            f32x16 d;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) d[r] = 0.f;
-            d = O::multiply(a, b, d);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[t][r] = seen ? acc[t][r] + d[r] : acc[t][r];
-          }
-        }
-      }
-      return;
-    }
+  for (int n = 0; n < N; ++n) {
+    use(n, ring[n % AHEAD]);
+    if (n + AHEAD < N) ring[n % AHEAD] = load(n + AHEAD);
+    __builtin_amdgcn_sched_barrier(0x0406);
   }
+}
+constexpr int kAhead = 3;
+
+// acc += tile^T p over the 16 rows from row0 on, p a lane's column.
+template <int DTYPE, int DP>
+__device__ __forceinline__ void multiply_across(f32x16 (&acc)[DP / 32], const Reader<DTYPE, DP>& read, const lds_byte* tile, int row0,
+                                                typename Operand<DTYPE>::F p) {
+  typedef Operand<DTYPE> O;
+  products<DP / 32, kAhead>([&](int t) { return read.across(tile, row0, t); },
+                            [&](int t, const typename O::F& a) { acc[t] = O::multiply(a, p, acc[t]); });
+}
+// The same where a lane's column does not see all rows: p is 0 there, but 0 times infinity is not.  What is not finite counts as 0 and
+// is `found`; add_what_is_seen() brings it to the columns that see it.
+template <int DTYPE, int DP>
+__device__ __forceinline__ void multiply_finite(f32x16 (&acc)[DP / 32], const Reader<DTYPE, DP>& read, const lds_byte* tile, int row0,
+                                                typename Operand<DTYPE>::F p, unsigned& found) {
+  typedef Operand<DTYPE> O;
+  products<DP / 32, kAhead>([&](int t) { return read.across(tile, row0, t); },
+                            [&](int t, const typename O::F& a) { acc[t] = O::multiply(O::clean(a, found), p, acc[t]); });
+}
+// Adds what is not finite in rows from .. to - 1 to the lanes' columns that see the row, first .. last.
+template <int DTYPE, int DP>
+__device__ __forceinline__ void add_what_is_seen(f32x16 (&acc)[DP / 32], const HeadRows& rows, int from, int to, int first, int last, int lane, int dim) {
+#pragma unroll 1
+  for (int j = from; j < to; ++j) {
+    const typename Value<DTYPE>::T* row = static_cast<const typename Value<DTYPE>::T*>(rows.p) + j * rows.stride;
+    const bool seen = j >= first && j <= last;
 #pragma unroll
-  for (int t = 0; t < DP / 32; ++t) acc[t] = O::multiply(R::across(tile, row0, t * 32, lane), p, acc[t]);
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int d = t * 32 + result_row(r, lane);
+        const float v = d < dim ? Value<DTYPE>::get(row + d) : 0.f;
+        if (seen && !__builtin_isfinite(v)) acc[t][r] += v;
+      }
+  }
 }
 
 // factor times a lane's column of results to a row in memory.
@@ -247,19 +338,6 @@ __device__ __forceinline__ void store_column(const f32x16 (&acc)[DP / 32], float
       }
     }
 }
-
-constexpr float kLog2e = 1.4426950408889634f;
-// Scores as powers of 2; above 0, since 0 times the -inf of a masked score is not -inf.
-__device__ __forceinline__ float exponent(float scale) { return __builtin_fmaxf(scale * kLog2e, 0x1p-126f); }
-
-__device__ __forceinline__ f32x16 zero16() {
-  f32x16 z;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) z[r] = 0.f;
-  return z;
-}
-// The row of a lane's result r.
-__device__ __forceinline__ int result_row(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
 
 // What the other half of a wavefront holds in the same column.
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }

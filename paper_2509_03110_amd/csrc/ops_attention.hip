@@ -29,7 +29,7 @@ struct AttentionParams {
 };
 
 template <int DTYPE> constexpr int kTile = DTYPE == LSAM_DTYPE_BF16 ? 64 : 32;      // rows of a tile in LDS
-template <int DTYPE, int DP> constexpr int kLds = 4 * kTile<DTYPE> * DP * Operand<DTYPE>::B;   // two tensors, two tiles of each
+template <int DTYPE, int DP> constexpr int kLds = 2 * kTile<DTYPE> * Rows<DTYPE, DP>::BYTES;   // a tile of two tensors
 
 // Which tile of rows and which head a workgroup has.  Workgroups go round the eight XCDs in turn: those that read the same keys
 // meet in as few XCDs as that many heads allow.  `of`: heads of a group that are workgroups of their own.
@@ -81,14 +81,116 @@ __device__ __forceinline__ void join_ranges(const Range& r, int& lo, int& hi) {
 template <int DTYPE>
 __device__ __forceinline__ typename Value<DTYPE>::T* head_of(const Tensor& t, int head) { return static_cast<typename Value<DTYPE>::T*>(t.p) + head * t.head; }
 
-template <int DTYPE, int DP>
-__global__ __launch_bounds__(kThreads) void attention_kernel(AttentionParams p) {
+// Keys lo .. hi in tiles, `f(tile of k, tile of v, first key)` for each.  Two tiles a turn in arrays of their own: so the compiler sees that what is
+// read is not what is on its way, and their places are constants.
+template <int DTYPE, int DP, bool DIRECT, typename F>
+__device__ __forceinline__ void walk(lds_byte* even, lds_byte* odd, const HeadRows& k, const HeadRows& v, int lo, int hi, int dim, F f) {
+  constexpr int BN = kTile<DTYPE>, BYTES = BN * Rows<DTYPE, DP>::BYTES;
+  Stage<DTYPE, DP, BN, kThreads, DIRECT> sk, sv;
+  sk.init(k, dim);
+  sv.init(v, dim);
+  sk.ask(even, lo, hi + 1);
+  sv.ask(even + BYTES, lo, hi + 1);
+  for (int j0 = lo; j0 <= hi;) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      lds_byte* const tk = b ? odd : even;
+      lds_byte* const next = b ? even : odd;
+      sk.put(tk);
+      sv.put(tk + BYTES);
+      arrived();
+      if (j0 + BN <= hi) {
+        sk.ask(next, j0 + BN, hi + 1);
+        sv.ask(next + BYTES, j0 + BN, hi + 1);
+      }
+      f(tk, tk + BYTES, j0);
+      j0 += BN;
+      if (j0 > hi) return;
+    }
+  }
+}
+
+// A column's running sums.
+template <int DP> struct Running {
+  float m = -__builtin_inff(), base = 0.f, l = 0.f;          // the largest score, or one not far below; the same as a power of 2
+  unsigned found = 0;                                        // whether a tile that is not seen whole held what is not finite
+  f32x16 acc[DP / 32];
+};
+// How far scores may be above the running maximum, as a power of 2, before sums are scaled to a new one.
+constexpr float kSlack = 8.f;
+
+// The first of a lane's result rows that lie in first .. last, and the last: rows of results 0 .. 15 are compared with them without the lane's part.
+struct Seen {
+  int first, last;
+  __device__ __forceinline__ Seen(int f, int l, int lane) : first(f - 4 * (lane >> 5)), last(l - 4 * (lane >> 5)) {}
+  __device__ __forceinline__ bool operator()(int tile, int r) const {
+    const int row = tile * 32 + 8 * (r >> 2) + (r & 3);
+    return row >= first && row <= last;
+  }
+};
+
+// What is not finite in the tiles, of BN rows from lo on, that a wavefront's columns do not all see.
+template <int DTYPE, int DP, int BN>
+__device__ __forceinline__ void add_masked(f32x16 (&acc)[DP / 32], const HeadRows& rows, int lo, const Range& r, int first, int last, int lane, int dim) {
+  for (int j0 = lo; j0 <= r.hi; j0 += BN)
+    if (j0 + BN > r.lo && (j0 < r.all_lo || j0 + BN - 1 > r.all_hi))
+      add_what_is_seen<DTYPE, DP>(acc, rows, j0, j0 + BN <= r.hi ? j0 + BN : r.hi + 1, first, last, lane, dim);
+}
+
+template <int DTYPE, int DP, int TILES>
+__device__ __forceinline__ void attend(Running<DP>& a, const Reader<DTYPE, DP>& read, const typename Operand<DTYPE>::F (&q)[DP / 16], const lds_byte* tk,
+                                       const lds_byte* tv, float c, int lane, bool masked, int first, int last) {
+  typedef Operand<DTYPE> O;
+  constexpr int STEPS = DP / 16;
+  f32x16 s[TILES];
+#pragma unroll
+  for (int i = 0; i < TILES; ++i) s[i] = zero16();
+  products<TILES * STEPS, kAhead>([&](int n) { return read.along(tk, n / STEPS * 32, n % STEPS); },
+                                  [&](int n, const typename O::F& k) { s[n / STEPS] = O::multiply(k, q[n % STEPS], s[n / STEPS]); });
+  if (masked) {
+    const Seen seen(first, last, lane);
+#pragma unroll
+    for (int i = 0; i < TILES; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[i][e] = seen(i, e) ? s[i][e] : -__builtin_inff();
+  }
+  float most = a.m;
+#pragma unroll
+  for (int i = 0; i < TILES; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) most = __builtin_fmaxf(most, s[i][e]);
+  most = __builtin_fmaxf(most, other_half(most));
+  const bool grown = (most - a.m) * c > kSlack;              // of this lane's column alone: no other column's scores change its bits
+  if (__any(grown)) {
+    const float base = grown ? most * c : a.base, less = !grown ? 1.f : a.m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(a.base - base);
+    a.m = grown ? most : a.m;
+    a.base = base;
+    a.l *= less;
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t) a.acc[t] *= less;
+  }
+#pragma unroll
+  for (int i = 0; i < TILES; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[i][e] = __builtin_amdgcn_exp2f(s[i][e] * c - a.base);
+      a.l += s[i][e];
+    }
+  if (masked) {
+#pragma unroll
+    for (int n = 0; n < TILES * 2; ++n) multiply_finite<DTYPE, DP>(a.acc, read, tv, n * 16, O::from(s[n / 2], n & 1), a.found);
+  } else {
+#pragma unroll
+    for (int n = 0; n < TILES * 2; ++n) multiply_across<DTYPE, DP>(a.acc, read, tv, n * 16, O::from(s[n / 2], n & 1));
+  }
+}
+
+template <int DTYPE, int DP, bool DIRECT>
+__global__ __launch_bounds__(kThreads, 2) void attention_kernel(AttentionParams p) {
   typedef typename Value<DTYPE>::T T;
   typedef Operand<DTYPE> O;
-  typedef Rows<DTYPE, DP> R;
   constexpr int BN = kTile<DTYPE>, STEPS = DP / 16;
-  __shared__ __attribute__((aligned(16))) unsigned char memory[kLds<DTYPE, DP>];
-  lds_byte* const lds = (lds_byte*)memory;
+  __shared__ __attribute__((aligned(1024))) unsigned char even[kLds<DTYPE, DP>], odd[kLds<DTYPE, DP>];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Work w = work(p.tiles, p.heads / p.group, p.group, true);
   if (!w.here) return;
@@ -102,89 +204,63 @@ __global__ __launch_bounds__(kThreads) void attention_kernel(AttentionParams p) 
   join_ranges(r, lo, hi);
   if (hi < 0) return;
 
-  const HeadRows k{head_of<DTYPE>(p.k, w.kv), p.k.stride}, v{head_of<DTYPE>(p.v, w.kv), p.v.stride};
-  Stage<DTYPE, DP, BN, kThreads> sk, sv;
-  sk.ask(k, lo, hi + 1, p.dim);
-  sv.ask(v, lo, hi + 1, p.dim);
   typename O::F q[STEPS];
   const T* q_row = head_of<DTYPE>(p.q, head) + (valid ? row : 0) * p.q.stride;
 #pragma unroll
   for (int s = 0; s < STEPS; ++s) q[s] = load_operand<DTYPE>(q_row, s, lane, valid ? p.dim : 0);
-
+  const Reader<DTYPE, DP> read(lane);
   const float c = exponent(p.scale);
-  float m = -__builtin_inff(), l = 0.f;
-  f32x16 acc[DP / 32];
+  Running<DP> a;
 #pragma unroll
-  for (int t = 0; t < DP / 32; ++t) acc[t] = zero16();
-  int b = 0;
-  for (int j0 = lo; j0 <= hi; j0 += BN, b ^= 1) {
-    lds_byte* const tk = lds + b * 2 * BN * R::BYTES;
-    lds_byte* const tv = tk + BN * R::BYTES;
-    sk.put(tk);
-    sv.put(tv);
-    __syncthreads();
-    if (j0 + BN <= hi) {
-      sk.ask(k, j0 + BN, hi + 1, p.dim);
-      sv.ask(v, j0 + BN, hi + 1, p.dim);
-    }
-    if (j0 > r.hi || j0 + BN <= r.lo) continue;
-    f32x16 s[BN / 32];
-#pragma unroll
-    for (int i = 0; i < BN / 32; ++i) s[i] = zero16();
-#pragma unroll
-    for (int d = 0; d < STEPS; ++d)
-#pragma unroll
-      for (int i = 0; i < BN / 32; ++i) s[i] = O::multiply(R::along(tk, i * 32, d, lane), q[d], s[i]);
-    const bool masked = j0 < r.all_lo || j0 + BN - 1 > r.all_hi;
-    if (masked) {
-#pragma unroll
-      for (int i = 0; i < BN / 32; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int j = j0 + i * 32 + result_row(e, lane);
-          if (j < first || j > last) s[i][e] = -__builtin_inff();
-        }
-    }
-    float most = m;
-#pragma unroll
-    for (int i = 0; i < BN / 32; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) most = __builtin_fmaxf(most, s[i][e]);
-    most = __builtin_fmaxf(most, other_half(most));
-    const float base = most == -__builtin_inff() ? 0.f : most * c;
-    if (__any(most > m)) {
-      const float less = __builtin_amdgcn_exp2f(m * c - base);
-      l *= less;
-#pragma unroll
-      for (int t = 0; t < DP / 32; ++t) acc[t] *= less;
-    }
-    m = most;
-#pragma unroll
-    for (int i = 0; i < BN / 32; ++i) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        s[i][e] = __builtin_amdgcn_exp2f(s[i][e] * c - base);
-        l += s[i][e];
-      }
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-        multiply_across<DTYPE, DP>(acc, tv, i * 32 + t * 16, O::from(s[i], t), lane, masked, first - j0, last - j0);
-    }
-  }
+  for (int t = 0; t < DP / 32; ++t) a.acc[t] = zero16();
+  const HeadRows k{head_of<DTYPE>(p.k, w.kv), p.k.stride}, v{head_of<DTYPE>(p.v, w.kv), p.v.stride};
+  walk<DTYPE, DP, DIRECT>((lds_byte*)even, (lds_byte*)odd, k, v, lo, hi, p.dim,
+                          [&](const lds_byte* tk, const lds_byte* tv, int j0) {
+                            if (j0 > r.hi || j0 + BN <= r.lo) return;
+                            attend<DTYPE, DP, BN / 32>(a, read, q, tk, tv, c, lane, j0 < r.all_lo || j0 + BN - 1 > r.all_hi, first - j0, last - j0);
+                          });
+  if (__any(a.found != 0)) add_masked<DTYPE, DP, BN>(a.acc, v, lo, r, first, last, lane, p.dim);
   if (!valid) return;
-  l += other_half(l);
-  store_column<DTYPE, DP>(acc, 1.f / l, head_of<DTYPE>(p.o, head) + row * p.o.stride, lane, p.dim);
-  if (p.lse && lane < 32) p.lse[(int64_t)head * p.seq.rows + row] = m * p.scale + __logf(l);
+  const float l = a.l + other_half(a.l);
+  store_column<DTYPE, DP>(a.acc, 1.f / l, head_of<DTYPE>(p.o, head) + row * p.o.stride, lane, p.dim);
+  if (p.lse && lane < 32) p.lse[(int64_t)head * p.seq.rows + row] = a.m * p.scale + __logf(l);
 }
 
-template <int DTYPE, int DP>
-__global__ __launch_bounds__(kThreads) void dq_kernel(AttentionParams p) {
+template <int DTYPE, int DP, int TILES>
+__device__ __forceinline__ void dq_tile(f32x16 (&acc)[DP / 32], const Reader<DTYPE, DP>& read, const typename Operand<DTYPE>::F (&q)[DP / 16],
+                                        const typename Operand<DTYPE>::F (&g)[DP / 16], const lds_byte* tk, const lds_byte* tv, float c, float base,
+                                        float dot, int lane, bool masked, int first, int last, unsigned& found) {
+  typedef Operand<DTYPE> O;
+#pragma unroll
+  for (int i = 0; i < TILES; ++i) {
+    f32x16 s = zero16(), d = zero16();
+    products<DP / 8, kAhead>([&](int n) { return read.along(n & 1 ? tv : tk, i * 32, n / 2); },
+                             [&](int n, const typename O::F& a) {
+                               if (n & 1) d = O::multiply(a, g[n / 2], d); else s = O::multiply(a, q[n / 2], s);
+                             });
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(s[e] * c - base) * (d[e] - dot);
+    if (masked) {
+      const Seen seen(first, last, lane);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = seen(i, e) ? s[e] : 0.f;
+    }
+    if (masked) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) multiply_finite<DTYPE, DP>(acc, read, tk, i * 32 + t * 16, O::from(s, t), found);
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) multiply_across<DTYPE, DP>(acc, read, tk, i * 32 + t * 16, O::from(s, t));
+    }
+  }
+}
+
+template <int DTYPE, int DP, bool DIRECT>
+__global__ __launch_bounds__(kThreads, 2) void dq_kernel(AttentionParams p) {
   typedef typename Value<DTYPE>::T T;
   typedef Operand<DTYPE> O;
-  typedef Rows<DTYPE, DP> R;
   constexpr int BN = kTile<DTYPE>, STEPS = DP / 16;
-  __shared__ __attribute__((aligned(16))) unsigned char memory[kLds<DTYPE, DP>];
-  lds_byte* const lds = (lds_byte*)memory;
+  __shared__ __attribute__((aligned(1024))) unsigned char even[kLds<DTYPE, DP>], odd[kLds<DTYPE, DP>];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Work w = work(p.tiles, p.heads / p.group, p.group, true);
   if (!w.here) return;
@@ -198,10 +274,6 @@ __global__ __launch_bounds__(kThreads) void dq_kernel(AttentionParams p) {
   join_ranges(r, lo, hi);
   if (hi < 0) return;
 
-  const HeadRows k{head_of<DTYPE>(p.k, w.kv), p.k.stride}, v{head_of<DTYPE>(p.v, w.kv), p.v.stride};
-  Stage<DTYPE, DP, BN, kThreads> sk, sv;
-  sk.ask(k, lo, hi + 1, p.dim);
-  sv.ask(v, lo, hi + 1, p.dim);
   typename O::F q[STEPS], g[STEPS];
   const int at = valid ? row : 0, dim = valid ? p.dim : 0;
   const T* q_row = head_of<DTYPE>(p.q, head) + at * p.q.stride;
@@ -217,57 +289,78 @@ __global__ __launch_bounds__(kThreads) void dq_kernel(AttentionParams p) {
     for (int e = 0; e < 8; ++e) dot += (float)o[e] * (float)g[s][e];
   }
   dot += other_half(dot);
+  const Reader<DTYPE, DP> read(lane);
   const float c = exponent(p.scale), base = valid ? p.lse[(int64_t)head * p.seq.rows + row] * kLog2e : 0.f;
   if (valid && lane < 32) {
     p.stats[head * p.padded + row] = base;
     p.stats[(p.heads + head) * p.padded + row] = dot;
   }
+  unsigned found = 0;
   f32x16 acc[DP / 32];
 #pragma unroll
   for (int t = 0; t < DP / 32; ++t) acc[t] = zero16();
-  int b = 0;
-  for (int j0 = lo; j0 <= hi; j0 += BN, b ^= 1) {
-    lds_byte* const tk = lds + b * 2 * BN * R::BYTES;
-    lds_byte* const tv = tk + BN * R::BYTES;
-    sk.put(tk);
-    sv.put(tv);
-    __syncthreads();
-    if (j0 + BN <= hi) {
-      sk.ask(k, j0 + BN, hi + 1, p.dim);
-      sv.ask(v, j0 + BN, hi + 1, p.dim);
-    }
-    if (j0 > r.hi || j0 + BN <= r.lo) continue;
-    const bool masked = j0 < r.all_lo || j0 + BN - 1 > r.all_hi;
-#pragma unroll
-    for (int i = 0; i < BN / 32; ++i) {
-      f32x16 s = zero16(), d = zero16();
-#pragma unroll
-      for (int n = 0; n < STEPS; ++n) {
-        s = O::multiply(R::along(tk, i * 32, n, lane), q[n], s);
-        d = O::multiply(R::along(tv, i * 32, n, lane), g[n], d);
-      }
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int j = j0 + i * 32 + result_row(e, lane);
-        s[e] = __builtin_amdgcn_exp2f(s[e] * c - base) * (d[e] - dot);
-        if (masked && (j < first || j > last)) s[e] = 0.f;
-      }
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-        multiply_across<DTYPE, DP>(acc, tk, i * 32 + t * 16, O::from(s, t), lane, masked, first - j0, last - j0);
-    }
-  }
+  const HeadRows k{head_of<DTYPE>(p.k, w.kv), p.k.stride}, v{head_of<DTYPE>(p.v, w.kv), p.v.stride};
+  walk<DTYPE, DP, DIRECT>((lds_byte*)even, (lds_byte*)odd, k, v, lo, hi, p.dim,
+                          [&](const lds_byte* tk, const lds_byte* tv, int j0) {
+                            if (j0 > r.hi || j0 + BN <= r.lo) return;
+                            dq_tile<DTYPE, DP, BN / 32>(acc, read, q, g, tk, tv, c, base, dot, lane, j0 < r.all_lo || j0 + BN - 1 > r.all_hi, first - j0,
+                                                        last - j0, found);
+                          });
+  if (__any(found != 0)) add_masked<DTYPE, DP, BN>(acc, k, lo, r, first, last, lane, p.dim);
   if (valid) store_column<DTYPE, DP>(acc, p.scale, head_of<DTYPE>(p.dq, head) + row * p.dq.stride, lane, p.dim);
 }
 
+// 32 rows from row0 of the tiles on; first .. last and the rows of base and dots count from there too.
 template <int DTYPE, int DP>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 2))) void dkv_kernel(AttentionParams p) {
+__device__ __forceinline__ void dkv_tile(f32x16 (&dk)[DP / 32], f32x16 (&dv)[DP / 32], const Reader<DTYPE, DP>& read,
+                                         const typename Operand<DTYPE>::F (&k)[DP / 16], const typename Operand<DTYPE>::F (&v)[DP / 16], const lds_byte* tq,
+                                         const lds_byte* tg, int row0, const float* base, const float* dots, float c, int lane, bool masked, int first,
+                                         int last, unsigned& found) {
+  typedef Operand<DTYPE> O;
+  f32x16 s = zero16(), d = zero16();
+  products<DP / 8, kAhead>([&](int n) { return read.along(n & 1 ? tg : tq, row0, n / 2); },
+                           [&](int n, const typename O::F& a) {
+                             if (n & 1) d = O::multiply(a, v[n / 2], d); else s = O::multiply(a, k[n / 2], s);
+                           });
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const int of = 8 * g + 4 * (lane >> 5);
+    const f32x4 bs = *reinterpret_cast<const f32x4_any*>(base + of), ds = *reinterpret_cast<const f32x4_any*>(dots + of);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      s[4 * g + e] = __builtin_amdgcn_exp2f(s[4 * g + e] * c - bs[e]);
+      d[4 * g + e] = s[4 * g + e] * (d[4 * g + e] - ds[e]);
+    }
+  }
+  if (masked) {
+    const Seen seen(first, last, lane);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[e] = seen(0, e) ? s[e] : 0.f;
+      d[e] = seen(0, e) ? d[e] : 0.f;
+    }
+  }
+  if (masked) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      multiply_finite<DTYPE, DP>(dv, read, tg, row0 + t * 16, O::from(s, t), found);
+      multiply_finite<DTYPE, DP>(dk, read, tq, row0 + t * 16, O::from(d, t), found);
+    }
+  } else {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      multiply_across<DTYPE, DP>(dv, read, tg, row0 + t * 16, O::from(s, t));
+      multiply_across<DTYPE, DP>(dk, read, tq, row0 + t * 16, O::from(d, t));
+    }
+  }
+}
+
+template <int DTYPE, int DP, bool DIRECT>
+__device__ __forceinline__ void dkv(const AttentionParams& p) {
   typedef typename Value<DTYPE>::T T;
   typedef Operand<DTYPE> O;
-  typedef Rows<DTYPE, DP> R;
-  constexpr int BN = kTile<DTYPE>, STEPS = DP / 16;
-  __shared__ __attribute__((aligned(16))) unsigned char memory[kLds<DTYPE, DP>];
-  lds_byte* const lds = (lds_byte*)memory;
+  constexpr int BN = kTile<DTYPE>, STEPS = DP / 16, BYTES = BN * Rows<DTYPE, DP>::BYTES;
+  __shared__ __attribute__((aligned(1024))) unsigned char even[kLds<DTYPE, DP>], odd[kLds<DTYPE, DP>];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Work w = work(p.tiles, p.heads / p.group, 1, false);
   if (!w.here) return;
@@ -290,64 +383,62 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 2))
     k[s] = load_operand<DTYPE>(k_row, s, lane, dim);
     v[s] = load_operand<DTYPE>(v_row, s, lane, dim);
   }
+  const Reader<DTYPE, DP> read(lane);
   const float c = exponent(p.scale);
+  unsigned found = 0;
   f32x16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
   for (int t = 0; t < DP / 32; ++t) dk[t] = dv[t] = zero16();
-  Stage<DTYPE, DP, BN, kThreads> sq, sg;
-  auto ask = [&](int head, int i0) {
-    sq.ask(HeadRows{head_of<DTYPE>(p.q, head), p.q.stride}, i0, hi + 1, p.dim);
-    sg.ask(HeadRows{head_of<DTYPE>(p.d_o, head), p.d_o.stride}, i0, hi + 1, p.dim);
-  };
-  int head = w.kv * p.group, b = 0;
+  Stage<DTYPE, DP, BN, kThreads, DIRECT> sq, sg;
+  int head = w.kv * p.group;
   const int behind = head + p.group;
-  ask(head, lo);
-  for (int i0 = lo; head < behind; b ^= 1) {
-    lds_byte* const tq = lds + b * 2 * BN * R::BYTES;
-    lds_byte* const tg = tq + BN * R::BYTES;
-    sq.put(tq);
-    sg.put(tg);
-    __syncthreads();
-    const int now = i0, with = head;
-    i0 += BN;
-    if (i0 > hi) { i0 = lo; ++head; }
-    if (head < behind) ask(head, i0);
-    const float* base = p.stats + with * p.padded;
-    const float* dots = base + p.heads * p.padded;
+  sq.init(HeadRows{head_of<DTYPE>(p.q, head), p.q.stride}, p.dim);
+  sg.init(HeadRows{head_of<DTYPE>(p.d_o, head), p.d_o.stride}, p.dim);
+  sq.ask((lds_byte*)even, lo, hi + 1);
+  sg.ask((lds_byte*)even + BYTES, lo, hi + 1);
+  for (int i0 = lo; head < behind;) {
 #pragma unroll
-    for (int i = 0; i < BN / 32; ++i) {
-      const int top = now + i * 32;
-      if (top > r.hi || top + 32 <= r.lo) continue;
-      const bool masked = top < r.all_lo || top + 31 > r.all_hi;
-      f32x16 s = zero16(), d = zero16();
-#pragma unroll
-      for (int n = 0; n < STEPS; ++n) {
-        s = O::multiply(R::along(tq, i * 32, n, lane), k[n], s);
-        d = O::multiply(R::along(tg, i * 32, n, lane), v[n], d);
+    for (int b = 0; b < 2; ++b) {
+      lds_byte* const tq = (lds_byte*)(b ? odd : even);
+      lds_byte* const tg = tq + BYTES;
+      sq.put(tq);
+      sg.put(tg);
+      arrived();
+      const int now = i0;
+      const float* base = p.stats + head * p.padded + now;
+      i0 += BN;
+      if (i0 > hi) { i0 = lo; ++head; }
+      if (head < behind) {
+        lds_byte* const next = (lds_byte*)(b ? even : odd);
+        sq.p = head_of<DTYPE>(p.q, head);
+        sg.p = head_of<DTYPE>(p.d_o, head);
+        sq.ask(next, i0, hi + 1);
+        sg.ask(next + BYTES, i0, hi + 1);
       }
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int of = top + 8 * g + 4 * (lane >> 5);
-        const f32x4 bs = *reinterpret_cast<const f32x4_any*>(base + of), ds = *reinterpret_cast<const f32x4_any*>(dots + of);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float pr = __builtin_amdgcn_exp2f(s[4 * g + e] * c - bs[e]);
-          s[4 * g + e] = pr;
-          d[4 * g + e] = pr * (d[4 * g + e] - ds[e]);
-          if (masked && (of + e < first || of + e > last)) s[4 * g + e] = d[4 * g + e] = 0.f;
-        }
+      for (int i = 0; i < BN; i += 32) {
+        const int top = now + i;
+        if (top > r.hi || top + 32 <= r.lo) continue;
+        const float* const bases = base + i;
+        const float* const dots = bases + p.heads * p.padded;
+        dkv_tile<DTYPE, DP>(dk, dv, read, k, v, tq, tg, i, bases, dots, c, lane, top < r.all_lo || top + 31 > r.all_hi, first - top, last - top, found);
       }
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        multiply_across<DTYPE, DP>(dv, tg, i * 32 + t * 16, O::from(s, t), lane, masked, first - now, last - now);
-        multiply_across<DTYPE, DP>(dk, tq, i * 32 + t * 16, O::from(d, t), lane, masked, first - now, last - now);
-      }
+      if (head == behind) break;
+    }
+  }
+  if (__any(found != 0)) {
+    for (head = behind - p.group; head < behind; ++head) {
+      add_masked<DTYPE, DP, 32>(dk, HeadRows{head_of<DTYPE>(p.q, head), p.q.stride}, lo, r, first, last, lane, p.dim);
+      add_masked<DTYPE, DP, 32>(dv, HeadRows{head_of<DTYPE>(p.d_o, head), p.d_o.stride}, lo, r, first, last, lane, p.dim);
     }
   }
   if (!valid) return;
   store_column<DTYPE, DP>(dk, p.scale, head_of<DTYPE>(p.dk, w.kv) + row * p.dk.stride, lane, p.dim);
   store_column<DTYPE, DP>(dv, 1.f, head_of<DTYPE>(p.dv, w.kv) + row * p.dv.stride, lane, p.dim);
 }
+
+template <int DTYPE, int DP, bool DIRECT>
+__global__ __launch_bounds__(kThreads) void dkv_kernel(AttentionParams p) { dkv<DTYPE, DP, DIRECT>(p); }
 
 int check(const lsam_attention_desc* d, const char* who) {
   if (!d) return refuse(LSAM_EINVAL, "%s: the descriptor is NULL", who);
@@ -381,21 +472,29 @@ AttentionParams params(const lsam_attention_desc* d, const int64_t* offsets) {
   return p;
 }
 
-template <int DTYPE, int DP>
+template <int DTYPE, int DP, bool DIRECT>
 int launch(const AttentionParams& p, bool backward, hipStream_t s) {
   const unsigned all = workgroups(p.tiles, p.heads / p.group, p.group), of_keys = workgroups(p.tiles, p.heads / p.group, 1);
   if (backward) {
-    dq_kernel<DTYPE, DP><<<all, kThreads, 0, s>>>(p);
-    dkv_kernel<DTYPE, DP><<<of_keys, kThreads, 0, s>>>(p);
+    dq_kernel<DTYPE, DP, DIRECT><<<all, kThreads, 0, s>>>(p);
+    dkv_kernel<DTYPE, DP, DIRECT><<<of_keys, kThreads, 0, s>>>(p);
   } else {
-    attention_kernel<DTYPE, DP><<<all, kThreads, 0, s>>>(p);
+    attention_kernel<DTYPE, DP, DIRECT><<<all, kThreads, 0, s>>>(p);
   }
   return launched();
 }
+template <int DTYPE, bool DIRECT>
+int launch_wide(const AttentionParams& p, bool backward, hipStream_t s) {
+  if (p.dim <= 32) return launch<DTYPE, 32, DIRECT>(p, backward, s);
+  if (p.dim <= 64) return launch<DTYPE, 64, DIRECT>(p, backward, s);
+  if (p.dim <= 96) return launch<DTYPE, 96, DIRECT>(p, backward, s);
+  return launch<DTYPE, 128, DIRECT>(p, backward, s);
+}
 int launch_any(const AttentionParams& p, int dtype, bool backward, hipStream_t s) {
-  if (dtype == LSAM_DTYPE_BF16)
-    return p.dim <= 64 ? launch<LSAM_DTYPE_BF16, 64>(p, backward, s) : launch<LSAM_DTYPE_BF16, 128>(p, backward, s);
-  return p.dim <= 64 ? launch<LSAM_DTYPE_FP32, 64>(p, backward, s) : launch<LSAM_DTYPE_FP32, 128>(p, backward, s);
+  const auto fits = [&](const Tensor& t) { return direct(t.p, t.stride, t.head, 0, p.dim, dtype); };
+  const bool fast = fits(p.k) && fits(p.v) && (!backward || (fits(p.q) && fits(p.d_o)));
+  if (dtype == LSAM_DTYPE_BF16) return fast ? launch_wide<LSAM_DTYPE_BF16, true>(p, backward, s) : launch_wide<LSAM_DTYPE_BF16, false>(p, backward, s);
+  return fast ? launch_wide<LSAM_DTYPE_FP32, true>(p, backward, s) : launch_wide<LSAM_DTYPE_FP32, false>(p, backward, s);
 }
 
 }  // namespace

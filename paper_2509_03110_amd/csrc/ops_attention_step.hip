@@ -81,13 +81,16 @@ __global__ __launch_bounds__(kThreads) void step_kernel(StepParams p) {
   const int64_t of = shared ? 0 : seq;
   const HeadRows k{static_cast<const T*>(c.k) + of * c.k_seq + kv * c.k_head, c.k_stride};
   const HeadRows v{static_cast<const T*>(c.v) + of * c.v_seq + kv * c.v_head, c.v_stride};
-  Stage<DTYPE, DP, kKeys, kThreads> sk, sv;
-  sk.ask(k, from, to, p.dim);
-  sv.ask(v, from, to, p.dim);
+  Stage<DTYPE, DP, kKeys, kThreads, false> sk, sv;
+  sk.init(k, p.dim);
+  sv.init(v, p.dim);
+  sk.ask(tk, from, to);
+  sv.ask(tv, from, to);
   typename O::F q[STEPS];
   const T* q_row = static_cast<const T*>(p.q) + (valid ? seq * p.q_stride + head * p.q_head : 0);
 #pragma unroll
   for (int s = 0; s < STEPS; ++s) q[s] = load_operand<DTYPE>(q_row, s, lane, valid ? p.dim : 0);
+  const Reader<DTYPE, DP> read(lane);
   const float scale = exponent(p.scale);
   float m = -__builtin_inff(), l = 0.f;
   f32x16 acc[DP / 32];
@@ -99,8 +102,8 @@ __global__ __launch_bounds__(kThreads) void step_kernel(StepParams p) {
     sv.put(tv);
     __syncthreads();
     if (j0 + kKeys < to) {
-      sk.ask(k, j0 + kKeys, to, p.dim);
-      sv.ask(v, j0 + kKeys, to, p.dim);
+      sk.ask(tk, j0 + kKeys, to);
+      sv.ask(tv, j0 + kKeys, to);
     }
 #pragma unroll 1
     for (int i = spread ? 0 : wave; i < (spread ? kWaves : wave + 1); ++i) {
@@ -108,7 +111,7 @@ __global__ __launch_bounds__(kThreads) void step_kernel(StepParams p) {
       if (left <= 0) break;
       f32x16 s = zero16();
 #pragma unroll
-      for (int d = 0; d < STEPS; ++d) s = O::multiply(R::along(tk, i * 32, d, lane), q[d], s);
+      for (int d = 0; d < STEPS; ++d) s = O::multiply(read.along(tk, i * 32, d), q[d], s);
       if (left < 32) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
@@ -132,7 +135,7 @@ __global__ __launch_bounds__(kThreads) void step_kernel(StepParams p) {
         l += s[e];
       }
 #pragma unroll
-      for (int t = 0; t < 2; ++t) multiply_across<DTYPE, DP>(acc, tv, i * 32 + t * 16, O::from(s, t), lane, false, 0, 0);
+      for (int t = 0; t < 2; ++t) multiply_across<DTYPE, DP>(acc, read, tv, i * 32 + t * 16, O::from(s, t));
     }
   }
   l += other_half(l);
