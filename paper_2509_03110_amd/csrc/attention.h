@@ -261,9 +261,9 @@ __device__ __forceinline__ f32x16 zero16() {
 __device__ __forceinline__ int result_row(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
 
 // N products whose operand from LDS is asked for AHEAD products before: a wavefront's registers do not hold more than that of
-// them, and vector arithmetic may move in between.
-template <int N, int AHEAD, typename Load, typename Use>
-__device__ __forceinline__ void products(Load load, Use use) {
+// them, and vector arithmetic may move in between.  `beside(n)` is work of the vector units for the time that product n takes.
+template <int N, int AHEAD, typename Load, typename Use, typename Beside>
+__device__ __forceinline__ void products(Load load, Use use, Beside beside) {
   decltype(load(0)) ring[AHEAD];
 #pragma unroll
   for (int n = 0; n < AHEAD && n < N; ++n) ring[n] = load(n);
@@ -271,9 +271,12 @@ __device__ __forceinline__ void products(Load load, Use use) {
   for (int n = 0; n < N; ++n) {
     use(n, ring[n % AHEAD]);
     if (n + AHEAD < N) ring[n % AHEAD] = load(n + AHEAD);
+    beside(n);
     __builtin_amdgcn_sched_barrier(0x0406);
   }
 }
+template <int N, int AHEAD, typename Load, typename Use>
+__device__ __forceinline__ void products(Load load, Use use) { products<N, AHEAD>(load, use, [](int) {}); }
 constexpr int kAhead = 3;
 
 // acc += tile^T p over the 16 rows from row0 on, p a lane's column.
@@ -293,7 +296,8 @@ __device__ __forceinline__ void multiply_finite(f32x16 (&acc)[DP / 32], const Re
   products<DP / 32, kAhead>([&](int t) { return read.across(tile, row0, t); },
                             [&](int t, const typename O::F& a) { acc[t] = O::multiply(O::clean(a, found), p, acc[t]); });
 }
-// Adds what is not finite in rows from .. to - 1 to the lanes' columns that see the row, first .. last.
+// Adds what is not finite in rows from .. to - 1 to the lanes' columns that see the row, first .. last.  Where it was multiplied
+// already, the sum is not finite either way.
 template <int DTYPE, int DP>
 __device__ __forceinline__ void add_what_is_seen(f32x16 (&acc)[DP / 32], const HeadRows& rows, int from, int to, int first, int last, int lane, int dim) {
 #pragma unroll 1

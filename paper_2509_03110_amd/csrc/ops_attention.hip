@@ -129,14 +129,6 @@ struct Seen {
   }
 };
 
-// What is not finite in the tiles, of BN rows from lo on, that a wavefront's columns do not all see.
-template <int DTYPE, int DP, int BN>
-__device__ __forceinline__ void add_masked(f32x16 (&acc)[DP / 32], const HeadRows& rows, int lo, const Range& r, int first, int last, int lane, int dim) {
-  for (int j0 = lo; j0 <= r.hi; j0 += BN)
-    if (j0 + BN > r.lo && (j0 < r.all_lo || j0 + BN - 1 > r.all_hi))
-      add_what_is_seen<DTYPE, DP>(acc, rows, j0, j0 + BN <= r.hi ? j0 + BN : r.hi + 1, first, last, lane, dim);
-}
-
 template <int DTYPE, int DP, int TILES>
 __device__ __forceinline__ void attend(Running<DP>& a, const Reader<DTYPE, DP>& read, const typename Operand<DTYPE>::F (&q)[DP / 16], const lds_byte* tk,
                                        const lds_byte* tv, float c, int lane, bool masked, int first, int last) {
@@ -219,7 +211,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(AttentionParams 
                             if (j0 > r.hi || j0 + BN <= r.lo) return;
                             attend<DTYPE, DP, BN / 32>(a, read, q, tk, tv, c, lane, j0 < r.all_lo || j0 + BN - 1 > r.all_hi, first - j0, last - j0);
                           });
-  if (__any(a.found != 0)) add_masked<DTYPE, DP, BN>(a.acc, v, lo, r, first, last, lane, p.dim);
+  if (__any(a.found != 0)) add_what_is_seen<DTYPE, DP>(a.acc, v, r.lo, r.hi + 1, first, last, lane, p.dim);
   if (!valid) return;
   const float l = a.l + other_half(a.l);
   store_column<DTYPE, DP>(a.acc, 1.f / l, head_of<DTYPE>(p.o, head) + row * p.o.stride, lane, p.dim);
@@ -306,33 +298,54 @@ __global__ __launch_bounds__(kThreads, 2) void dq_kernel(AttentionParams p) {
                             dq_tile<DTYPE, DP, BN / 32>(acc, read, q, g, tk, tv, c, base, dot, lane, j0 < r.all_lo || j0 + BN - 1 > r.all_hi, first - j0,
                                                         last - j0, found);
                           });
-  if (__any(found != 0)) add_masked<DTYPE, DP, BN>(acc, k, lo, r, first, last, lane, p.dim);
+  if (__any(found != 0)) add_what_is_seen<DTYPE, DP>(acc, k, r.lo, r.hi + 1, first, last, lane, p.dim);
   if (valid) store_column<DTYPE, DP>(acc, p.scale, head_of<DTYPE>(p.dq, head) + row * p.dq.stride, lane, p.dim);
 }
 
-// 32 rows from row0 of the tiles on; first .. last and the rows of base and dots count from there too.
-template <int DTYPE, int DP>
-__device__ __forceinline__ void dkv_tile(f32x16 (&dk)[DP / 32], f32x16 (&dv)[DP / 32], const Reader<DTYPE, DP>& read,
-                                         const typename Operand<DTYPE>::F (&k)[DP / 16], const typename Operand<DTYPE>::F (&v)[DP / 16], const lds_byte* tq,
-                                         const lds_byte* tg, int row0, const float* base, const float* dots, float c, int lane, bool masked, int first,
-                                         int last, unsigned& found) {
+// What a wavefront of dkv_kernel has: its keys and values, and the sums for them.
+template <int DTYPE, int DP> struct Keys {
+  typename Operand<DTYPE>::F k[DP / 16], v[DP / 16];
+  f32x16 dk[DP / 32], dv[DP / 32];
+  unsigned found = 0;
+};
+
+// The steps for 32 rows from row0 of the tiles on: scores and d_o v; p and ds of them; dv and dk.  stats: lse and d_o o of the
+// tile's rows, 64 each.
+template <int DTYPE, int DP> struct KeySteps {
   typedef Operand<DTYPE> O;
+  typedef typename O::F F;
+  static constexpr int N = DP / 8, T = DP / 32;             // products of the first step, and of the last
+  const Reader<DTYPE, DP>& read;
+  const lds_byte* tq;
+  const lds_byte* tg;
+  const lds_byte* stats;
+  int row0, lane;
+  float c;
   f32x16 s = zero16(), d = zero16();
-  products<DP / 8, kAhead>([&](int n) { return read.along(n & 1 ? tg : tq, row0, n / 2); },
-                           [&](int n, const typename O::F& a) {
-                             if (n & 1) d = O::multiply(a, v[n / 2], d); else s = O::multiply(a, k[n / 2], s);
-                           });
-#pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    const int of = 8 * g + 4 * (lane >> 5);
-    const f32x4 bs = *reinterpret_cast<const f32x4_any*>(base + of), ds = *reinterpret_cast<const f32x4_any*>(dots + of);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      s[4 * g + e] = __builtin_amdgcn_exp2f(s[4 * g + e] * c - bs[e]);
-      d[4 * g + e] = s[4 * g + e] * (d[4 * g + e] - ds[e]);
-    }
+  f32x4 base, dot;
+  F weight[4];
+
+  __device__ __forceinline__ F load(int n) const { return read.along(n & 1 ? tg : tq, row0, n / 2); }
+  __device__ __forceinline__ void score(const Keys<DTYPE, DP>& w, int n, const F& a) {
+    if (n & 1) d = O::multiply(a, w.v[n / 2], d); else s = O::multiply(a, w.k[n / 2], s);
   }
-  if (masked) {
+  __device__ __forceinline__ void weigh(int e) {
+    typedef const __attribute__((address_space(3))) f32x4* quad_ptr;
+    if (e % 4 == 0) {
+      const lds_byte* at = stats + (row0 + 2 * e + 4 * (lane >> 5)) * 4;
+      base = *reinterpret_cast<quad_ptr>(at);
+      dot = *reinterpret_cast<quad_ptr>(at + 256);
+    }
+    s[e] = __builtin_amdgcn_exp2f(s[e] * c - base[e % 4]);
+    d[e] = s[e] * (d[e] - dot[e % 4]);
+  }
+  // The share of weigh(0 .. 15) beside product n of `all`.
+  __device__ __forceinline__ void weigh_beside(int n, int all) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (e >= n * 16 / all && e < (n + 1) * 16 / all) weigh(e);
+  }
+  __device__ __forceinline__ void mask(int first, int last) {
     const Seen seen(first, last, lane);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -340,27 +353,58 @@ __device__ __forceinline__ void dkv_tile(f32x16 (&dk)[DP / 32], f32x16 (&dv)[DP 
       d[e] = seen(0, e) ? d[e] : 0.f;
     }
   }
-  if (masked) {
+  __device__ __forceinline__ void pack() {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      multiply_finite<DTYPE, DP>(dv, read, tg, row0 + t * 16, O::from(s, t), found);
-      multiply_finite<DTYPE, DP>(dk, read, tq, row0 + t * 16, O::from(d, t), found);
-    }
-  } else {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      multiply_across<DTYPE, DP>(dv, read, tg, row0 + t * 16, O::from(s, t));
-      multiply_across<DTYPE, DP>(dk, read, tq, row0 + t * 16, O::from(d, t));
-    }
+    for (int i = 0; i < 4; ++i) weight[i] = O::from(i & 1 ? d : s, i / 2);
   }
+  // Product n of 4 T: dv then dk of rows 0 .. 15, dv then dk of rows 16 .. 31.
+  __device__ __forceinline__ F load_sum(int n) const { return read.across(n / T & 1 ? tq : tg, row0 + n / (2 * T) * 16, n % T); }
+  __device__ __forceinline__ void sum(Keys<DTYPE, DP>& w, int n, const F& a) const {
+    f32x16& to = n / T & 1 ? w.dk[n % T] : w.dv[n % T];
+    to = O::multiply(a, weight[n / T], to);
+  }
+};
+
+// Rows from `row0` on that some keys do not see, 32 of them.
+template <int DTYPE, int DP>
+__device__ __forceinline__ void dkv_masked(Keys<DTYPE, DP>& w, KeySteps<DTYPE, DP> a, int first, int last) {
+  typedef KeySteps<DTYPE, DP> K;
+  products<K::N, kAhead>([&](int n) { return a.load(n); }, [&](int n, const typename K::F& f) { a.score(w, n, f); });
+#pragma unroll
+  for (int e = 0; e < 16; ++e) a.weigh(e);
+  a.mask(first, last);
+  a.pack();
+  products<4 * K::T, kAhead>([&](int n) { return a.load_sum(n); }, [&](int n, const typename K::F& f) { a.sum(w, n, K::O::clean(f, w.found)); });
+}
+// 64 rows that all keys see.  There is one wavefront a SIMD, so the powers of the first 32 rows go beside the products of the others' scores, and those
+// of the others beside the first sums.
+template <int DTYPE, int DP>
+__device__ __forceinline__ void dkv_pair(Keys<DTYPE, DP>& w, KeySteps<DTYPE, DP> a, KeySteps<DTYPE, DP> b) {
+  typedef KeySteps<DTYPE, DP> K;
+  products<K::N, kAhead>([&](int n) { return a.load(n); }, [&](int n, const typename K::F& f) { a.score(w, n, f); });
+  products<K::N, kAhead>([&](int n) { return b.load(n); }, [&](int n, const typename K::F& f) { b.score(w, n, f); },
+                         [&](int n) { a.weigh_beside(n, K::N); });
+  a.pack();
+  products<4 * K::T, kAhead>([&](int n) { return a.load_sum(n); }, [&](int n, const typename K::F& f) { a.sum(w, n, f); },
+                             [&](int n) { b.weigh_beside(n, 4 * K::T); });
+  b.pack();
+  products<4 * K::T, kAhead>([&](int n) { return b.load_sum(n); }, [&](int n, const typename K::F& f) { b.sum(w, n, f); });
+}
+
+// 64 rows' lse and d_o o to LDS: a wavefront each.
+__device__ __forceinline__ void ask_stats(lds_byte* to, const AttentionParams& p, int head, int row0, int wave) {
+  if (wave >= 2) return;
+  const unsigned long long a = reinterpret_cast<unsigned long long>(p.stats + (wave * p.heads + head) * p.padded + row0);
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)a), hi = __builtin_amdgcn_readfirstlane((unsigned)(a >> 32));
+  const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((unsigned long long)hi << 32 | lo), 0, 256, 0x00020000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(to + wave * 256), 4, (threadIdx.x & 63) * 4, 0, 0, 0);
 }
 
 template <int DTYPE, int DP, bool DIRECT>
 __device__ __forceinline__ void dkv(const AttentionParams& p) {
   typedef typename Value<DTYPE>::T T;
-  typedef Operand<DTYPE> O;
   constexpr int BN = kTile<DTYPE>, STEPS = DP / 16, BYTES = BN * Rows<DTYPE, DP>::BYTES;
-  __shared__ __attribute__((aligned(1024))) unsigned char even[kLds<DTYPE, DP>], odd[kLds<DTYPE, DP>];
+  __shared__ __attribute__((aligned(1024))) unsigned char even[kLds<DTYPE, DP> + 512], odd[kLds<DTYPE, DP> + 512];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Work w = work(p.tiles, p.heads / p.group, 1, false);
   if (!w.here) return;
@@ -374,21 +418,19 @@ __device__ __forceinline__ void dkv(const AttentionParams& p) {
   join_ranges(r, lo, hi);
   if (hi < 0) return;
 
-  typename O::F k[STEPS], v[STEPS];
+  Keys<DTYPE, DP> keys;
   const int at = valid ? row : 0, dim = valid ? p.dim : 0;
   const T* k_row = head_of<DTYPE>(p.k, w.kv) + at * p.k.stride;
   const T* v_row = head_of<DTYPE>(p.v, w.kv) + at * p.v.stride;
 #pragma unroll
   for (int s = 0; s < STEPS; ++s) {
-    k[s] = load_operand<DTYPE>(k_row, s, lane, dim);
-    v[s] = load_operand<DTYPE>(v_row, s, lane, dim);
+    keys.k[s] = load_operand<DTYPE>(k_row, s, lane, dim);
+    keys.v[s] = load_operand<DTYPE>(v_row, s, lane, dim);
   }
   const Reader<DTYPE, DP> read(lane);
   const float c = exponent(p.scale);
-  unsigned found = 0;
-  f32x16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
-  for (int t = 0; t < DP / 32; ++t) dk[t] = dv[t] = zero16();
+  for (int t = 0; t < DP / 32; ++t) keys.dk[t] = keys.dv[t] = zero16();
   Stage<DTYPE, DP, BN, kThreads, DIRECT> sq, sg;
   int head = w.kv * p.group;
   const int behind = head + p.group;
@@ -396,6 +438,7 @@ __device__ __forceinline__ void dkv(const AttentionParams& p) {
   sg.init(HeadRows{head_of<DTYPE>(p.d_o, head), p.d_o.stride}, p.dim);
   sq.ask((lds_byte*)even, lo, hi + 1);
   sg.ask((lds_byte*)even + BYTES, lo, hi + 1);
+  ask_stats((lds_byte*)even + 2 * BYTES, p, head, lo, wave);
   for (int i0 = lo; head < behind;) {
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
@@ -405,7 +448,6 @@ __device__ __forceinline__ void dkv(const AttentionParams& p) {
       sg.put(tg);
       arrived();
       const int now = i0;
-      const float* base = p.stats + head * p.padded + now;
       i0 += BN;
       if (i0 > hi) { i0 = lo; ++head; }
       if (head < behind) {
@@ -414,27 +456,30 @@ __device__ __forceinline__ void dkv(const AttentionParams& p) {
         sg.p = head_of<DTYPE>(p.d_o, head);
         sq.ask(next, i0, hi + 1);
         sg.ask(next + BYTES, i0, hi + 1);
+        ask_stats(next + 2 * BYTES, p, head, i0, wave);
       }
+      const auto steps = [&](int from) { return KeySteps<DTYPE, DP>{read, tq, tg, tg + BYTES, from, lane, c}; };
+      if (BN == 64 && now >= r.all_lo && now + 63 <= r.all_hi) {
+        dkv_pair<DTYPE, DP>(keys, steps(0), steps(32));
+      } else {
 #pragma unroll
-      for (int i = 0; i < BN; i += 32) {
-        const int top = now + i;
-        if (top > r.hi || top + 32 <= r.lo) continue;
-        const float* const bases = base + i;
-        const float* const dots = bases + p.heads * p.padded;
-        dkv_tile<DTYPE, DP>(dk, dv, read, k, v, tq, tg, i, bases, dots, c, lane, top < r.all_lo || top + 31 > r.all_hi, first - top, last - top, found);
+        for (int i = 0; i < BN; i += 32) {
+          const int top = now + i;
+          if (top <= r.hi && top + 32 > r.lo) dkv_masked<DTYPE, DP>(keys, steps(i), first - top, last - top);
+        }
       }
       if (head == behind) break;
     }
   }
-  if (__any(found != 0)) {
+  if (__any(keys.found != 0)) {
     for (head = behind - p.group; head < behind; ++head) {
-      add_masked<DTYPE, DP, 32>(dk, HeadRows{head_of<DTYPE>(p.q, head), p.q.stride}, lo, r, first, last, lane, p.dim);
-      add_masked<DTYPE, DP, 32>(dv, HeadRows{head_of<DTYPE>(p.d_o, head), p.d_o.stride}, lo, r, first, last, lane, p.dim);
+      add_what_is_seen<DTYPE, DP>(keys.dk, HeadRows{head_of<DTYPE>(p.q, head), p.q.stride}, r.lo, r.hi + 1, first, last, lane, p.dim);
+      add_what_is_seen<DTYPE, DP>(keys.dv, HeadRows{head_of<DTYPE>(p.d_o, head), p.d_o.stride}, r.lo, r.hi + 1, first, last, lane, p.dim);
     }
   }
   if (!valid) return;
-  store_column<DTYPE, DP>(dk, p.scale, head_of<DTYPE>(p.dk, w.kv) + row * p.dk.stride, lane, p.dim);
-  store_column<DTYPE, DP>(dv, 1.f, head_of<DTYPE>(p.dv, w.kv) + row * p.dv.stride, lane, p.dim);
+  store_column<DTYPE, DP>(keys.dk, p.scale, head_of<DTYPE>(p.dk, w.kv) + row * p.dk.stride, lane, p.dim);
+  store_column<DTYPE, DP>(keys.dv, 1.f, head_of<DTYPE>(p.dv, w.kv) + row * p.dv.stride, lane, p.dim);
 }
 
 template <int DTYPE, int DP, bool DIRECT>
