@@ -12,6 +12,7 @@ namespace lsam {
 #if defined(__HIPCC__)
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) unsigned char lds_byte;
 
@@ -69,12 +70,11 @@ template <> struct Operand<LSAM_DTYPE_FP32> {
 template <int DTYPE, int DP>
 struct Rows {
   typedef typename Operand<DTYPE>::F F;
-  static constexpr int B = Operand<DTYPE>::B, WIDE = DP > 64 ? 128 : DP > 32 ? 64 : 32, U = WIDE * B / 16, BYTES = WIDE * B;
+  static constexpr int B = Operand<DTYPE>::B, WIDE = DP > 64 ? 128 : 64, U = WIDE * B / 16, BYTES = WIDE * B;
   static __device__ __forceinline__ int turn(int row) {
     if constexpr (DTYPE == LSAM_DTYPE_FP32) return row & 15 & (U - 1);
     else if constexpr (U == 16) return (row & 3) << 2 | (row >> 2 & 3);
-    else if constexpr (U == 8) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
-    else return row >> 2 & 3;
+    else return (row >> 1 & 1) << 2 | (row >> 2 & 3);
   }
   static __device__ __forceinline__ int place(int row, int unit) { return row * BYTES + ((unit ^ turn(row)) << 4); }
 
@@ -279,22 +279,24 @@ template <int N, int AHEAD, typename Load, typename Use>
 __device__ __forceinline__ void products(Load load, Use use) { products<N, AHEAD>(load, use, [](int) {}); }
 constexpr int kAhead = 3;
 
-// acc += tile^T p over the 16 rows from row0 on, p a lane's column.
-template <int DTYPE, int DP>
+// acc += tile^T p over the 16 rows from row0 on, p a lane's column.  A column that does not see a row has p = 0 there, but 0 times infinity is not 0:
+// with CLEAN what is not finite counts as 0 and is `found`, and add_what_is_seen() brings it to the columns that see it.
+template <int DTYPE, int DP, bool CLEAN>
 __device__ __forceinline__ void multiply_across(f32x16 (&acc)[DP / 32], const Reader<DTYPE, DP>& read, const lds_byte* tile, int row0,
-                                                typename Operand<DTYPE>::F p) {
-  typedef Operand<DTYPE> O;
-  products<DP / 32, kAhead>([&](int t) { return read.across(tile, row0, t); },
-                            [&](int t, const typename O::F& a) { acc[t] = O::multiply(a, p, acc[t]); });
-}
-// The same where a lane's column does not see all rows: p is 0 there, but 0 times infinity is not.  What is not finite counts as 0 and
-// is `found`; add_what_is_seen() brings it to the columns that see it.
-template <int DTYPE, int DP>
-__device__ __forceinline__ void multiply_finite(f32x16 (&acc)[DP / 32], const Reader<DTYPE, DP>& read, const lds_byte* tile, int row0,
                                                 typename Operand<DTYPE>::F p, unsigned& found) {
   typedef Operand<DTYPE> O;
   products<DP / 32, kAhead>([&](int t) { return read.across(tile, row0, t); },
-                            [&](int t, const typename O::F& a) { acc[t] = O::multiply(O::clean(a, found), p, acc[t]); });
+                            [&](int t, const typename O::F& a) { acc[t] = O::multiply(CLEAN ? O::clean(a, found) : a, p, acc[t]); });
+}
+// Whether a lane's sums hold what is not finite.
+template <int N>
+__device__ __forceinline__ bool not_finite(const f32x16 (&acc)[N]) {
+  bool bad = false;
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) bad |= !__builtin_isfinite(acc[t][r]);
+  return bad;
 }
 // Adds what is not finite in rows from .. to - 1 to the lanes' columns that see the row, first .. last.  Where it was multiplied
 // already, the sum is not finite either way.

@@ -22,7 +22,7 @@ struct AttentionParams {
   Tensor q, k, v, o, d_o, dq, dk, dv;
   Sequences seq;
   float* lse;
-  float* stats;                            // backward: [2][heads][padded]: lse in powers of 2, d_o o
+  f32x2* stats;                            // backward: [heads][padded]: lse as a power of 2, d_o o
   int64_t padded;                          // rows, and what a tile may reach past them
   int heads, group, dim, tiles;
   float scale;
@@ -78,8 +78,23 @@ __device__ __forceinline__ void join_ranges(const Range& r, int& lo, int& hi) {
   hi = __builtin_amdgcn_readfirstlane(hi);
 }
 
+// Whether a lane of the workgroup says so.
+__device__ __forceinline__ bool any_of_workgroup(bool v) {
+  __shared__ int shared[kThreads / 64];
+  const bool mine = __any(v);
+  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = mine;
+  __syncthreads();
+  bool all = false;
+#pragma unroll
+  for (int i = 0; i < kThreads / 64; ++i) all |= shared[i] != 0;
+  return all;
+}
+
 template <int DTYPE>
 __device__ __forceinline__ typename Value<DTYPE>::T* head_of(const Tensor& t, int head) { return static_cast<typename Value<DTYPE>::T*>(t.p) + head * t.head; }
+
+struct No { static constexpr bool value = false; };
+struct Yes { static constexpr bool value = true; };
 
 // Keys lo .. hi in tiles, `f(tile of k, tile of v, first key)` for each.  Two tiles a turn in arrays of their own: so the compiler sees that what is
 // read is not what is on its way, and their places are constants.
@@ -113,7 +128,6 @@ __device__ __forceinline__ void walk(lds_byte* even, lds_byte* odd, const HeadRo
 // A column's running sums.
 template <int DP> struct Running {
   float m = -__builtin_inff(), base = 0.f, l = 0.f;          // the largest score, or one not far below; the same as a power of 2
-  unsigned found = 0;                                        // whether a tile that is not seen whole held what is not finite
   f32x16 acc[DP / 32];
 };
 // How far scores may be above the running maximum, as a power of 2, before sums are scaled to a new one.
@@ -129,9 +143,9 @@ struct Seen {
   }
 };
 
-template <int DTYPE, int DP, int TILES>
+template <int DTYPE, int DP, int TILES, bool CLEAN>
 __device__ __forceinline__ void attend(Running<DP>& a, const Reader<DTYPE, DP>& read, const typename Operand<DTYPE>::F (&q)[DP / 16], const lds_byte* tk,
-                                       const lds_byte* tv, float c, int lane, bool masked, int first, int last) {
+                                       const lds_byte* tv, float c, int lane, bool masked, int first, int last, unsigned& found) {
   typedef Operand<DTYPE> O;
   constexpr int STEPS = DP / 16;
   f32x16 s[TILES];
@@ -168,13 +182,8 @@ __device__ __forceinline__ void attend(Running<DP>& a, const Reader<DTYPE, DP>& 
       s[i][e] = __builtin_amdgcn_exp2f(s[i][e] * c - a.base);
       a.l += s[i][e];
     }
-  if (masked) {
 #pragma unroll
-    for (int n = 0; n < TILES * 2; ++n) multiply_finite<DTYPE, DP>(a.acc, read, tv, n * 16, O::from(s[n / 2], n & 1), a.found);
-  } else {
-#pragma unroll
-    for (int n = 0; n < TILES * 2; ++n) multiply_across<DTYPE, DP>(a.acc, read, tv, n * 16, O::from(s[n / 2], n & 1));
-  }
+  for (int n = 0; n < TILES * 2; ++n) multiply_across<DTYPE, DP, CLEAN>(a.acc, read, tv, n * 16, O::from(s[n / 2], n & 1), found);
 }
 
 template <int DTYPE, int DP, bool DIRECT>
@@ -202,23 +211,30 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(AttentionParams 
   for (int s = 0; s < STEPS; ++s) q[s] = load_operand<DTYPE>(q_row, s, lane, valid ? p.dim : 0);
   const Reader<DTYPE, DP> read(lane);
   const float c = exponent(p.scale);
-  Running<DP> a;
-#pragma unroll
-  for (int t = 0; t < DP / 32; ++t) a.acc[t] = zero16();
   const HeadRows k{head_of<DTYPE>(p.k, w.kv), p.k.stride}, v{head_of<DTYPE>(p.v, w.kv), p.v.stride};
-  walk<DTYPE, DP, DIRECT>((lds_byte*)even, (lds_byte*)odd, k, v, lo, hi, p.dim,
-                          [&](const lds_byte* tk, const lds_byte* tv, int j0) {
-                            if (j0 > r.hi || j0 + BN <= r.lo) return;
-                            attend<DTYPE, DP, BN / 32>(a, read, q, tk, tv, c, lane, j0 < r.all_lo || j0 + BN - 1 > r.all_hi, first - j0, last - j0);
-                          });
-  if (__any(a.found != 0)) add_what_is_seen<DTYPE, DP>(a.acc, v, r.lo, r.hi + 1, first, last, lane, p.dim);
+  Running<DP> a;
+  unsigned found = 0;
+  const auto pass = [&](auto clean) {
+    a = Running<DP>();
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t) a.acc[t] = zero16();
+    walk<DTYPE, DP, DIRECT>((lds_byte*)even, (lds_byte*)odd, k, v, lo, hi, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0) {
+      if (j0 > r.hi || j0 + BN <= r.lo) return;
+      attend<DTYPE, DP, BN / 32, decltype(clean)::value>(a, read, q, tk, tv, c, lane, j0 < r.all_lo || j0 + BN - 1 > r.all_hi, first - j0, last - j0, found);
+    });
+  };
+  pass(No());
+  if (any_of_workgroup(valid && not_finite(a.acc))) {        // by a value that is seen, or by one that is not: again, telling them apart
+    pass(Yes());
+    if (__any(found != 0)) add_what_is_seen<DTYPE, DP>(a.acc, v, r.lo, r.hi + 1, first, last, lane, p.dim);
+  }
   if (!valid) return;
   const float l = a.l + other_half(a.l);
   store_column<DTYPE, DP>(a.acc, 1.f / l, head_of<DTYPE>(p.o, head) + row * p.o.stride, lane, p.dim);
   if (p.lse && lane < 32) p.lse[(int64_t)head * p.seq.rows + row] = a.m * p.scale + __logf(l);
 }
 
-template <int DTYPE, int DP, int TILES>
+template <int DTYPE, int DP, int TILES, bool CLEAN>
 __device__ __forceinline__ void dq_tile(f32x16 (&acc)[DP / 32], const Reader<DTYPE, DP>& read, const typename Operand<DTYPE>::F (&q)[DP / 16],
                                         const typename Operand<DTYPE>::F (&g)[DP / 16], const lds_byte* tk, const lds_byte* tv, float c, float base,
                                         float dot, int lane, bool masked, int first, int last, unsigned& found) {
@@ -237,13 +253,8 @@ __device__ __forceinline__ void dq_tile(f32x16 (&acc)[DP / 32], const Reader<DTY
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = seen(i, e) ? s[e] : 0.f;
     }
-    if (masked) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) multiply_finite<DTYPE, DP>(acc, read, tk, i * 32 + t * 16, O::from(s, t), found);
-    } else {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) multiply_across<DTYPE, DP>(acc, read, tk, i * 32 + t * 16, O::from(s, t));
-    }
+    for (int t = 0; t < 2; ++t) multiply_across<DTYPE, DP, CLEAN>(acc, read, tk, i * 32 + t * 16, O::from(s, t), found);
   }
 }
 
@@ -283,69 +294,63 @@ __global__ __launch_bounds__(kThreads, 2) void dq_kernel(AttentionParams p) {
   dot += other_half(dot);
   const Reader<DTYPE, DP> read(lane);
   const float c = exponent(p.scale), base = valid ? p.lse[(int64_t)head * p.seq.rows + row] * kLog2e : 0.f;
-  if (valid && lane < 32) {
-    p.stats[head * p.padded + row] = base;
-    p.stats[(p.heads + head) * p.padded + row] = dot;
-  }
+  if (valid && lane < 32) p.stats[head * p.padded + row] = f32x2{base, dot};
+  const HeadRows k{head_of<DTYPE>(p.k, w.kv), p.k.stride}, v{head_of<DTYPE>(p.v, w.kv), p.v.stride};
   unsigned found = 0;
   f32x16 acc[DP / 32];
+  const auto pass = [&](auto clean) {
 #pragma unroll
-  for (int t = 0; t < DP / 32; ++t) acc[t] = zero16();
-  const HeadRows k{head_of<DTYPE>(p.k, w.kv), p.k.stride}, v{head_of<DTYPE>(p.v, w.kv), p.v.stride};
-  walk<DTYPE, DP, DIRECT>((lds_byte*)even, (lds_byte*)odd, k, v, lo, hi, p.dim,
-                          [&](const lds_byte* tk, const lds_byte* tv, int j0) {
-                            if (j0 > r.hi || j0 + BN <= r.lo) return;
-                            dq_tile<DTYPE, DP, BN / 32>(acc, read, q, g, tk, tv, c, base, dot, lane, j0 < r.all_lo || j0 + BN - 1 > r.all_hi, first - j0,
-                                                        last - j0, found);
-                          });
-  if (__any(found != 0)) add_what_is_seen<DTYPE, DP>(acc, k, r.lo, r.hi + 1, first, last, lane, p.dim);
+    for (int t = 0; t < DP / 32; ++t) acc[t] = zero16();
+    walk<DTYPE, DP, DIRECT>((lds_byte*)even, (lds_byte*)odd, k, v, lo, hi, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0) {
+      if (j0 > r.hi || j0 + BN <= r.lo) return;
+      dq_tile<DTYPE, DP, BN / 32, decltype(clean)::value>(acc, read, q, g, tk, tv, c, base, dot, lane, j0 < r.all_lo || j0 + BN - 1 > r.all_hi, first - j0,
+                                                          last - j0, found);
+    });
+  };
+  pass(No());
+  if (any_of_workgroup(valid && not_finite(acc))) {
+    pass(Yes());
+    if (__any(found != 0)) add_what_is_seen<DTYPE, DP>(acc, k, r.lo, r.hi + 1, first, last, lane, p.dim);
+  }
   if (valid) store_column<DTYPE, DP>(acc, p.scale, head_of<DTYPE>(p.dq, head) + row * p.dq.stride, lane, p.dim);
 }
 
-// What a wavefront of dkv_kernel has: its keys and values, and the sums for them.
+// Rows of a tile of dkv_kernel, and its LDS: such tiles of q and d_o with lse and d_o o of their rows.
+constexpr int kSeenRows = 32;
+template <int DTYPE, int DP> constexpr int kSeenLds = 2 * kSeenRows * Rows<DTYPE, DP>::BYTES + 8 * kSeenRows;
+
+// What a wavefront of dkv_kernel has: its values, where its keys are, and the sums for them.
 template <int DTYPE, int DP> struct Keys {
-  typename Operand<DTYPE>::F k[DP / 16], v[DP / 16];
+  const lds_byte* k;
+  typename Operand<DTYPE>::F v[DP / 16];
   f32x16 dk[DP / 32], dv[DP / 32];
-  unsigned found = 0;
 };
 
-// The steps for 32 rows from row0 of the tiles on: scores and d_o v; p and ds of them; dv and dk.  stats: lse and d_o o of the
-// tile's rows, 64 each.
-template <int DTYPE, int DP> struct KeySteps {
+// A tile of rows: scores and d_o v; p and ds of them; dv and dk.
+template <int DTYPE, int DP, bool CLEAN>
+__device__ __forceinline__ void dkv_tile(Keys<DTYPE, DP>& w, const Reader<DTYPE, DP>& read, const lds_byte* tq, float c, int lane, bool masked, int first,
+                                         int last, unsigned& found) {
   typedef Operand<DTYPE> O;
   typedef typename O::F F;
-  static constexpr int N = DP / 8, T = DP / 32;             // products of the first step, and of the last
-  const Reader<DTYPE, DP>& read;
-  const lds_byte* tq;
-  const lds_byte* tg;
-  const lds_byte* stats;
-  int row0, lane;
-  float c;
+  typedef const __attribute__((address_space(3))) f32x4* quad_ptr;
+  constexpr int T = DP / 32, BYTES = kSeenRows * Rows<DTYPE, DP>::BYTES;
+  const lds_byte* const tg = tq + BYTES;
+  const lds_byte* const stats = tg + BYTES;
+  struct Both { F a, b; };
   f32x16 s = zero16(), d = zero16();
-  f32x4 base, dot;
-  F weight[4];
-
-  __device__ __forceinline__ F load(int n) const { return read.along(n & 1 ? tg : tq, row0, n / 2); }
-  __device__ __forceinline__ void score(const Keys<DTYPE, DP>& w, int n, const F& a) {
-    if (n & 1) d = O::multiply(a, w.v[n / 2], d); else s = O::multiply(a, w.k[n / 2], s);
-  }
-  __device__ __forceinline__ void weigh(int e) {
-    typedef const __attribute__((address_space(3))) f32x4* quad_ptr;
-    if (e % 4 == 0) {
-      const lds_byte* at = stats + (row0 + 2 * e + 4 * (lane >> 5)) * 4;
-      base = *reinterpret_cast<quad_ptr>(at);
-      dot = *reinterpret_cast<quad_ptr>(at + 256);
-    }
-    s[e] = __builtin_amdgcn_exp2f(s[e] * c - base[e % 4]);
-    d[e] = s[e] * (d[e] - dot[e % 4]);
-  }
-  // The share of weigh(0 .. 15) beside product n of `all`.
-  __device__ __forceinline__ void weigh_beside(int n, int all) {
+  products<DP / 16, 2>([&](int n) { return Both{read.along(tq, 0, n), read.along(w.k, 0, n)}; }, [&](int n, const Both& f) { s = O::multiply(f.a, f.b, s); });
+  products<DP / 16, kAhead>([&](int n) { return read.along(tg, 0, n); }, [&](int n, const F& f) { d = O::multiply(f, w.v[n], d); });
 #pragma unroll
-    for (int e = 0; e < 16; ++e)
-      if (e >= n * 16 / all && e < (n + 1) * 16 / all) weigh(e);
+  for (int g = 0; g < 4; ++g) {
+    const lds_byte* const at = stats + (8 * g + 4 * (lane >> 5)) * 8;
+    const f32x4 two[2] = {*reinterpret_cast<quad_ptr>(at), *reinterpret_cast<quad_ptr>(at + 16)};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      s[4 * g + e] = __builtin_amdgcn_exp2f(s[4 * g + e] * c - two[e / 2][e % 2 * 2]);
+      d[4 * g + e] = s[4 * g + e] * (d[4 * g + e] - two[e / 2][e % 2 * 2 + 1]);
+    }
   }
-  __device__ __forceinline__ void mask(int first, int last) {
+  if (masked) {
     const Seen seen(first, last, lane);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -353,58 +358,49 @@ template <int DTYPE, int DP> struct KeySteps {
       d[e] = seen(0, e) ? d[e] : 0.f;
     }
   }
-  __device__ __forceinline__ void pack() {
+  F weight[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) weight[i] = O::from(i & 1 ? d : s, i / 2);
+  for (int i = 0; i < 4; ++i) weight[i] = O::from(i & 1 ? d : s, i / 2);
+  // dv then dk of rows 0 .. 15, dv then dk of rows 16 .. 31
+  products<4 * T, kAhead>([&](int n) { return read.across(n / T & 1 ? tq : tg, n / (2 * T) * 16, n % T); },
+                          [&](int n, const F& f) {
+                            f32x16& to = n / T & 1 ? w.dk[n % T] : w.dv[n % T];
+                            to = O::multiply(CLEAN ? O::clean(f, found) : f, weight[n / T], to);
+                          });
+}
+
+// A tile's lse and d_o o to LDS.
+__device__ __forceinline__ void ask_stats(lds_byte* to, const AttentionParams& p, int head, int row0, int wave) {
+  static_assert(kSeenRows * 8 == 64 * 4, "four bytes a lane");
+  if (wave != 0) return;
+  const unsigned long long a = reinterpret_cast<unsigned long long>(p.stats + head * p.padded + row0);
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)a), hi = __builtin_amdgcn_readfirstlane((unsigned)(a >> 32));
+  const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((unsigned long long)hi << 32 | lo), 0, 8 * kSeenRows, 0x00020000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 4, (threadIdx.x & 63) * 4, 0, 0, 0);
+}
+
+// A tile of q, d_o and what goes with their rows.
+template <int DTYPE, int DP, bool DIRECT> struct SeenStage {
+  static constexpr int BYTES = kSeenRows * Rows<DTYPE, DP>::BYTES;
+  Stage<DTYPE, DP, kSeenRows, kThreads, DIRECT> q, g;
+  __device__ __forceinline__ void ask(lds_byte* to, const AttentionParams& p, int head, int row0, int limit, int wave) {
+    q.p = head_of<DTYPE>(p.q, head);
+    g.p = head_of<DTYPE>(p.d_o, head);
+    q.ask(to, row0, limit);
+    g.ask(to + BYTES, row0, limit);
+    ask_stats(to + 2 * BYTES, p, head, row0, wave);
   }
-  // Product n of 4 T: dv then dk of rows 0 .. 15, dv then dk of rows 16 .. 31.
-  __device__ __forceinline__ F load_sum(int n) const { return read.across(n / T & 1 ? tq : tg, row0 + n / (2 * T) * 16, n % T); }
-  __device__ __forceinline__ void sum(Keys<DTYPE, DP>& w, int n, const F& a) const {
-    f32x16& to = n / T & 1 ? w.dk[n % T] : w.dv[n % T];
-    to = O::multiply(a, weight[n / T], to);
+  __device__ __forceinline__ void put(lds_byte* to) const {
+    q.put(to);
+    g.put(to + BYTES);
   }
 };
-
-// Rows from `row0` on that some keys do not see, 32 of them.
-template <int DTYPE, int DP>
-__device__ __forceinline__ void dkv_masked(Keys<DTYPE, DP>& w, KeySteps<DTYPE, DP> a, int first, int last) {
-  typedef KeySteps<DTYPE, DP> K;
-  products<K::N, kAhead>([&](int n) { return a.load(n); }, [&](int n, const typename K::F& f) { a.score(w, n, f); });
-#pragma unroll
-  for (int e = 0; e < 16; ++e) a.weigh(e);
-  a.mask(first, last);
-  a.pack();
-  products<4 * K::T, kAhead>([&](int n) { return a.load_sum(n); }, [&](int n, const typename K::F& f) { a.sum(w, n, K::O::clean(f, w.found)); });
-}
-// 64 rows that all keys see.  There is one wavefront a SIMD, so the powers of the first 32 rows go beside the products of the others' scores, and those
-// of the others beside the first sums.
-template <int DTYPE, int DP>
-__device__ __forceinline__ void dkv_pair(Keys<DTYPE, DP>& w, KeySteps<DTYPE, DP> a, KeySteps<DTYPE, DP> b) {
-  typedef KeySteps<DTYPE, DP> K;
-  products<K::N, kAhead>([&](int n) { return a.load(n); }, [&](int n, const typename K::F& f) { a.score(w, n, f); });
-  products<K::N, kAhead>([&](int n) { return b.load(n); }, [&](int n, const typename K::F& f) { b.score(w, n, f); },
-                         [&](int n) { a.weigh_beside(n, K::N); });
-  a.pack();
-  products<4 * K::T, kAhead>([&](int n) { return a.load_sum(n); }, [&](int n, const typename K::F& f) { a.sum(w, n, f); },
-                             [&](int n) { b.weigh_beside(n, 4 * K::T); });
-  b.pack();
-  products<4 * K::T, kAhead>([&](int n) { return b.load_sum(n); }, [&](int n, const typename K::F& f) { b.sum(w, n, f); });
-}
-
-// 64 rows' lse and d_o o to LDS: a wavefront each.
-__device__ __forceinline__ void ask_stats(lds_byte* to, const AttentionParams& p, int head, int row0, int wave) {
-  if (wave >= 2) return;
-  const unsigned long long a = reinterpret_cast<unsigned long long>(p.stats + (wave * p.heads + head) * p.padded + row0);
-  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)a), hi = __builtin_amdgcn_readfirstlane((unsigned)(a >> 32));
-  const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((unsigned long long)hi << 32 | lo), 0, 256, 0x00020000);
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(to + wave * 256), 4, (threadIdx.x & 63) * 4, 0, 0, 0);
-}
 
 template <int DTYPE, int DP, bool DIRECT>
 __device__ __forceinline__ void dkv(const AttentionParams& p) {
   typedef typename Value<DTYPE>::T T;
-  constexpr int BN = kTile<DTYPE>, STEPS = DP / 16, BYTES = BN * Rows<DTYPE, DP>::BYTES;
-  __shared__ __attribute__((aligned(1024))) unsigned char even[kLds<DTYPE, DP> + 512], odd[kLds<DTYPE, DP> + 512];
+  constexpr int BN = kSeenRows, STEPS = DP / 16;
+  __shared__ __attribute__((aligned(1024))) unsigned char even[kSeenLds<DTYPE, DP>], odd[kSeenLds<DTYPE, DP>], own[kRowsOf * Rows<DTYPE, DP>::BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Work w = work(p.tiles, p.heads / p.group, 1, false);
   if (!w.here) return;
@@ -418,63 +414,51 @@ __device__ __forceinline__ void dkv(const AttentionParams& p) {
   join_ranges(r, lo, hi);
   if (hi < 0) return;
 
+  Stage<DTYPE, DP, kRowsOf, kThreads, DIRECT> sk;
+  sk.init(HeadRows{head_of<DTYPE>(p.k, w.kv), p.k.stride}, p.dim);
+  sk.ask((lds_byte*)own, w.tile * kRowsOf, p.seq.rows);
+  sk.put((lds_byte*)own);
   Keys<DTYPE, DP> keys;
-  const int at = valid ? row : 0, dim = valid ? p.dim : 0;
-  const T* k_row = head_of<DTYPE>(p.k, w.kv) + at * p.k.stride;
-  const T* v_row = head_of<DTYPE>(p.v, w.kv) + at * p.v.stride;
+  keys.k = (lds_byte*)own + wave * 32 * Rows<DTYPE, DP>::BYTES;
+  const T* v_row = head_of<DTYPE>(p.v, w.kv) + (valid ? row : 0) * p.v.stride;
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) {
-    keys.k[s] = load_operand<DTYPE>(k_row, s, lane, dim);
-    keys.v[s] = load_operand<DTYPE>(v_row, s, lane, dim);
-  }
+  for (int s = 0; s < STEPS; ++s) keys.v[s] = load_operand<DTYPE>(v_row, s, lane, valid ? p.dim : 0);
   const Reader<DTYPE, DP> read(lane);
   const float c = exponent(p.scale);
+  SeenStage<DTYPE, DP, DIRECT> stage;
+  const int head0 = w.kv * p.group, behind = head0 + p.group;
+  stage.q.init(HeadRows{head_of<DTYPE>(p.q, head0), p.q.stride}, p.dim);
+  stage.g.init(HeadRows{head_of<DTYPE>(p.d_o, head0), p.d_o.stride}, p.dim);
+  unsigned found = 0;
+  const auto pass = [&](auto clean) {
 #pragma unroll
-  for (int t = 0; t < DP / 32; ++t) keys.dk[t] = keys.dv[t] = zero16();
-  Stage<DTYPE, DP, BN, kThreads, DIRECT> sq, sg;
-  int head = w.kv * p.group;
-  const int behind = head + p.group;
-  sq.init(HeadRows{head_of<DTYPE>(p.q, head), p.q.stride}, p.dim);
-  sg.init(HeadRows{head_of<DTYPE>(p.d_o, head), p.d_o.stride}, p.dim);
-  sq.ask((lds_byte*)even, lo, hi + 1);
-  sg.ask((lds_byte*)even + BYTES, lo, hi + 1);
-  ask_stats((lds_byte*)even + 2 * BYTES, p, head, lo, wave);
-  for (int i0 = lo; head < behind;) {
+    for (int t = 0; t < DP / 32; ++t) keys.dk[t] = keys.dv[t] = zero16();
+    int head = head0;
+    stage.ask((lds_byte*)even, p, head, lo, hi + 1, wave);
+    for (int i0 = lo; head < behind;) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      lds_byte* const tq = (lds_byte*)(b ? odd : even);
-      lds_byte* const tg = tq + BYTES;
-      sq.put(tq);
-      sg.put(tg);
-      arrived();
-      const int now = i0;
-      i0 += BN;
-      if (i0 > hi) { i0 = lo; ++head; }
-      if (head < behind) {
-        lds_byte* const next = (lds_byte*)(b ? even : odd);
-        sq.p = head_of<DTYPE>(p.q, head);
-        sg.p = head_of<DTYPE>(p.d_o, head);
-        sq.ask(next, i0, hi + 1);
-        sg.ask(next + BYTES, i0, hi + 1);
-        ask_stats(next + 2 * BYTES, p, head, i0, wave);
+      for (int b = 0; b < 2; ++b) {
+        lds_byte* const tq = (lds_byte*)(b ? odd : even);
+        stage.put(tq);
+        arrived();
+        const int now = i0;
+        i0 += BN;
+        if (i0 > hi) { i0 = lo; ++head; }
+        if (head < behind) stage.ask((lds_byte*)(b ? even : odd), p, head, i0, hi + 1, wave);
+        if (now <= r.hi && now + BN > r.lo)
+          dkv_tile<DTYPE, DP, decltype(clean)::value>(keys, read, tq, c, lane, now < r.all_lo || now + BN - 1 > r.all_hi, first - now, last - now, found);
+        if (head == behind) break;
       }
-      const auto steps = [&](int from) { return KeySteps<DTYPE, DP>{read, tq, tg, tg + BYTES, from, lane, c}; };
-      if (BN == 64 && now >= r.all_lo && now + 63 <= r.all_hi) {
-        dkv_pair<DTYPE, DP>(keys, steps(0), steps(32));
-      } else {
-#pragma unroll
-        for (int i = 0; i < BN; i += 32) {
-          const int top = now + i;
-          if (top <= r.hi && top + 32 > r.lo) dkv_masked<DTYPE, DP>(keys, steps(i), first - top, last - top);
-        }
-      }
-      if (head == behind) break;
     }
-  }
-  if (__any(keys.found != 0)) {
-    for (head = behind - p.group; head < behind; ++head) {
-      add_what_is_seen<DTYPE, DP>(keys.dk, HeadRows{head_of<DTYPE>(p.q, head), p.q.stride}, r.lo, r.hi + 1, first, last, lane, p.dim);
-      add_what_is_seen<DTYPE, DP>(keys.dv, HeadRows{head_of<DTYPE>(p.d_o, head), p.d_o.stride}, r.lo, r.hi + 1, first, last, lane, p.dim);
+  };
+  pass(No());
+  if (any_of_workgroup(valid && (not_finite(keys.dk) || not_finite(keys.dv)))) {
+    pass(Yes());
+    if (__any(found != 0)) {
+      for (int head = head0; head < behind; ++head) {
+        add_what_is_seen<DTYPE, DP>(keys.dk, HeadRows{head_of<DTYPE>(p.q, head), p.q.stride}, r.lo, r.hi + 1, first, last, lane, p.dim);
+        add_what_is_seen<DTYPE, DP>(keys.dv, HeadRows{head_of<DTYPE>(p.d_o, head), p.d_o.stride}, r.lo, r.hi + 1, first, last, lane, p.dim);
+      }
     }
   }
   if (!valid) return;
@@ -483,7 +467,7 @@ __device__ __forceinline__ void dkv(const AttentionParams& p) {
 }
 
 template <int DTYPE, int DP, bool DIRECT>
-__global__ __launch_bounds__(kThreads) void dkv_kernel(AttentionParams p) { dkv<DTYPE, DP, DIRECT>(p); }
+__global__ __launch_bounds__(kThreads, 2) void dkv_kernel(AttentionParams p) { dkv<DTYPE, DP, DIRECT>(p); }
 
 int check(const lsam_attention_desc* d, const char* who) {
   if (!d) return refuse(LSAM_EINVAL, "%s: the descriptor is NULL", who);
@@ -592,6 +576,6 @@ extern "C" int lsam_attention_backward(const lsam_attention_desc* d, const int64
   AttentionParams p = params(d, offsets);
   p.q = tensor(q, d->q); p.k = tensor(k, d->k); p.v = tensor(v, d->v); p.o = tensor(o, d->o);
   p.d_o = tensor(d_o, d->d_o); p.dq = tensor(dq, d->dq); p.dk = tensor(dk, d->dk); p.dv = tensor(dv, d->dv);
-  p.lse = const_cast<float*>(lse); p.stats = static_cast<float*>(workspace);
+  p.lse = const_cast<float*>(lse); p.stats = static_cast<f32x2*>(workspace);
   return launch_any(p, d->dtype, true, static_cast<hipStream_t>(stream));
 }

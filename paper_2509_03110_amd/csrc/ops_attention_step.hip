@@ -93,6 +93,7 @@ __global__ __launch_bounds__(kThreads) void step_kernel(StepParams p) {
   const Reader<DTYPE, DP> read(lane);
   const float scale = exponent(p.scale);
   float m = -__builtin_inff(), l = 0.f;
+  unsigned found = 0;
   f32x16 acc[DP / 32];
 #pragma unroll
   for (int t = 0; t < DP / 32; ++t) acc[t] = zero16();
@@ -135,7 +136,7 @@ __global__ __launch_bounds__(kThreads) void step_kernel(StepParams p) {
         l += s[e];
       }
 #pragma unroll
-      for (int t = 0; t < 2; ++t) multiply_across<DTYPE, DP>(acc, read, tv, i * 32 + t * 16, O::from(s, t));
+      for (int t = 0; t < 2; ++t) multiply_across<DTYPE, DP, false>(acc, read, tv, i * 32 + t * 16, O::from(s, t), found);
     }
   }
   l += other_half(l);
