@@ -362,28 +362,53 @@ __device__ __forceinline__ int last_before(const Sequences& q, int64_t row) {
   const int i = lo + (int)(threadIdx.x & 63);
   return lo + __popcll(__ballot(i < hi && q.offsets[i < hi ? i : 0] <= row)) - 1;
 }
-// Begin and end of the sequence of a lane's row row0 + 0 .. 31; both 0 where it has none.
-__device__ __forceinline__ void span_of(const Sequences& q, int row0, int row, int& begin, int& end) {
-  const int top = row0 + 31 < q.rows ? row0 + 31 : q.rows - 1;
-  begin = end = 0;
-  if (row0 >= q.rows) return;
-  int lo = last_before(q, row0) + 1, hi = last_before(q, top) + 1;
-  while (lo < hi) {                                         // sequences of a lane: up to lo - 1 begin at or before its row
-    const int mid = (lo + hi) >> 1;
-    if (q.offsets[mid] <= row) lo = mid + 1; else hi = mid;
-  }
-  if (lo == 0 || row >= q.rows) return;
-  int64_t b = q.offsets[lo - 1], e = q.offsets[lo];
-  b = b < 0 ? 0 : b;
-  e = e < q.rows ? e : q.rows;
-  if (b <= row && row < e) { begin = (int)b; end = (int)e; }
-}
-__device__ __forceinline__ int smallest(int v) {
+__device__ __forceinline__ int from_lane(int v, int lane) { return __builtin_amdgcn_ds_bpermute(lane << 2, v); }
+
+// Begin and end of the sequence of a lane's row; both 0 where it has none.  And, the same in all lanes, the begin of the sequence of row
+// `top` (top itself where it has none) and the end of that of row `bottom` (behind bottom where it has none): all rows between are in
+// sequences that begin and end within.  64 offsets lie side by side in the lanes and are searched there: one load for up to 63 sequences.
+struct Span { int begin, end, top_begin, bottom_end; };
+__device__ __forceinline__ Span span_of(const Sequences& q, int row, int top, int bottom) {
+  constexpr int kNone = 0x7FFFFFFF;
+  const int lane = threadIdx.x & 63;
+  int s0 = q.n > 63 ? last_before(q, top) : 0;
+  s0 = s0 < 0 ? 0 : s0;
+  const int64_t offset = q.offsets[s0 + lane <= q.n ? s0 + lane : q.n];
+  const int w = s0 + lane > q.n ? kNone : offset < 0 ? 0 : offset < q.rows ? (int)offset : q.rows;
+  Span r{0, 0, top, bottom + 1};
+  if (__builtin_amdgcn_readlane(w, 63) > bottom) {
+    int n = 0;                                              // offsets at or before the lane's row
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) { const int o = __shfl_xor(v, d); v = o < v ? o : v; }
-  return __builtin_amdgcn_readfirstlane(v);
+    for (int step = 32; step; step >>= 1)
+      if (from_lane(w, n + step - 1) <= row) n += step;
+    const int b = from_lane(w, n > 0 ? n - 1 : 0), e = from_lane(w, n);
+    if (n > 0 && e != kNone) { r.begin = b; r.end = e; }
+    const int above = __popcll(__ballot(w <= top)), below = __popcll(__ballot(w <= bottom));
+    if (above > 0 && above < 64 && __builtin_amdgcn_readlane(w, above < 64 ? above : 63) != kNone) r.top_begin = __builtin_amdgcn_readlane(w, above - 1);
+    const int behind = below > 0 && below < 64 ? __builtin_amdgcn_readlane(w, below) : kNone;
+    if (behind != kNone) r.bottom_end = behind;
+  } else {                                                  // more than 62 sequences in the tile: each lane searches for itself
+    const auto find = [&](int of, int& begin, int& end) {
+      int lo = 0, hi = q.n;
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (q.offsets[mid] <= of) lo = mid + 1; else hi = mid;
+      }
+      if (lo == 0 || of >= q.rows) return;
+      const int64_t b = q.offsets[lo - 1], e = q.offsets[lo];
+      if (of < e) { begin = b < 0 ? 0 : (int)b; end = e < q.rows ? (int)e : q.rows; }
+    };
+    find(row, r.begin, r.end);
+    int first = top, last = 0, none = 0;
+    find(top, first, none);
+    find(bottom, none, last);
+    r.top_begin = first;
+    if (last > 0) r.bottom_end = last;
+  }
+  r.top_begin = __builtin_amdgcn_readfirstlane(r.top_begin < top ? r.top_begin : top);
+  r.bottom_end = __builtin_amdgcn_readfirstlane(r.bottom_end > bottom ? r.bottom_end : bottom + 1);
+  return r;
 }
-__device__ __forceinline__ int largest(int v) { return -smallest(-v); }
 
 #endif
 

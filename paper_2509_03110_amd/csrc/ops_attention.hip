@@ -32,7 +32,9 @@ template <int DTYPE> constexpr int kTile = DTYPE == LSAM_DTYPE_BF16 ? 64 : 32;  
 template <int DTYPE, int DP> constexpr int kLds = 2 * kTile<DTYPE> * Rows<DTYPE, DP>::BYTES;   // a tile of two tensors
 
 // Which tile of rows and which head a workgroup has.  Workgroups go round the eight XCDs in turn: those that read the same keys
-// meet in as few XCDs as that many heads allow.  `of`: heads of a group that are workgroups of their own.
+// meet in as few XCDs as that many heads allow.  `of`: heads of a group that are workgroups of their own.  The last tiles of a sequence see most
+// keys and come first (last_first); the first keys are seen by most rows and come first, but every second round of an XCD's 32 units
+// goes backwards: all workgroups are there at once, two to a unit, and a unit with a long one gets a short one.
 struct Work { int tile, kv, g; bool here; };
 __device__ __forceinline__ Work work(int tiles, int kv_heads, int of, bool last_first) {
   const unsigned common = kv_heads % 8 == 0 ? 8 : kv_heads % 4 == 0 ? 4 : kv_heads % 2 == 0 ? 2 : 1;
@@ -40,8 +42,13 @@ __device__ __forceinline__ Work work(int tiles, int kv_heads, int of, bool last_
   Work w;
   w.g = i % of;
   const unsigned rest = i / of;
+  unsigned at = rest / mine;
+  if (!last_first) {
+    const unsigned all = (tiles + parts - 1) / parts, round = mine < 32 ? 32 / mine : 1, from = at / round * round;
+    if (at / round % 2) at = from + (from + round <= all ? round : all - from) - 1 - (at - from);
+  }
   w.kv = (int)(rest % mine * common + xcd % common);
-  w.tile = (int)(rest / mine * parts + xcd / common);
+  w.tile = (int)(at * parts + xcd / common);
   w.here = w.tile < tiles;
   if (last_first) w.tile = tiles - 1 - w.tile;
   return w;
@@ -52,30 +59,16 @@ unsigned workgroups(int tiles, int kv_heads, int of) {
   return 8 * (((unsigned)tiles + parts - 1) / parts) * mine * of;
 }
 
-// What a wavefront's rows see (or are seen by): numbers lo .. hi altogether, all of them from `all_lo` to `all_hi`.
+// What a wavefront's rows see (or are seen by): numbers lo .. hi altogether, all of them from all_lo to all_hi.  Both ends grow with the
+// row, so the first and the last row that has a sequence tell.  Without any: lo behind everything, hi before it.
 struct Range { int lo, hi, all_lo, all_hi; };
 __device__ __forceinline__ Range range_of(bool valid, int first, int last) {
-  Range r;
-  r.lo = smallest(valid ? first : 0x7FFFFFFF);
-  r.hi = largest(valid ? last : -1);
-  r.all_lo = largest(valid ? first : -1);
-  r.all_hi = smallest(valid ? last : 0x7FFFFFFF);
-  return r;
-}
-// The same for the workgroup.
-__device__ __forceinline__ void join_ranges(const Range& r, int& lo, int& hi) {
-  __shared__ int shared[2][kThreads / 64];
-  if ((threadIdx.x & 63) == 0) { shared[0][threadIdx.x >> 6] = r.lo; shared[1][threadIdx.x >> 6] = r.hi; }
-  __syncthreads();
-  lo = shared[0][0];
-  hi = shared[1][0];
-#pragma unroll
-  for (int i = 1; i < kThreads / 64; ++i) {
-    lo = shared[0][i] < lo ? shared[0][i] : lo;
-    hi = shared[1][i] > hi ? shared[1][i] : hi;
-  }
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  hi = __builtin_amdgcn_readfirstlane(hi);
+  const unsigned long long rows = __ballot(valid);
+  if (!rows) return Range{0x7FFFFFFF, -1, 0x7FFFFFFF, -1};
+  const int a = __builtin_ctzll(rows), b = 63 - __builtin_clzll(rows);      // (the upper half of the lanes has the same rows)
+  const int low = a < 32 ? a : a - 32, high = b >= 32 ? b - 32 : b;
+  return Range{__builtin_amdgcn_readlane(first, low), __builtin_amdgcn_readlane(last, high), __builtin_amdgcn_readlane(first, high),
+               __builtin_amdgcn_readlane(last, low)};
 }
 
 // Whether a lane of the workgroup says so.
@@ -196,19 +189,16 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(AttentionParams 
   const Work w = work(p.tiles, p.heads / p.group, p.group, true);
   if (!w.here) return;
   const int head = w.kv * p.group + w.g, row0 = w.tile * kRowsOf + wave * 32, row = row0 + (lane & 31);
-  int begin, end;
-  span_of(p.seq, row0, row, begin, end);
-  const bool valid = end > 0;
-  const int first = valid ? begin : 0x7FFFFFFF, last = valid ? row : -1;
-  const Range r = range_of(valid, first, last);
-  int lo, hi;
-  join_ranges(r, lo, hi);
-  if (hi < 0) return;
-
-  typename O::F q[STEPS];
-  const T* q_row = head_of<DTYPE>(p.q, head) + (valid ? row : 0) * p.q.stride;
+  const int top = w.tile * kRowsOf, bottom = top + kRowsOf <= p.seq.rows ? top + kRowsOf - 1 : p.seq.rows - 1;
+  typename O::F q[STEPS];                                    // on its way while sequences are looked for
+  const T* q_row = head_of<DTYPE>(p.q, head) + (row <= bottom ? row : bottom) * p.q.stride;
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) q[s] = load_operand<DTYPE>(q_row, s, lane, valid ? p.dim : 0);
+  for (int s = 0; s < STEPS; ++s) q[s] = load_operand<DTYPE>(q_row, s, lane, p.dim);
+  const Span span = span_of(p.seq, row, top, bottom);
+  const bool valid = span.end > 0;
+  const int first = valid ? span.begin : 0x7FFFFFFF, last = valid ? row : -1;
+  const Range r = range_of(valid, first, last);
+  const int lo = span.top_begin, hi = bottom;
   const Reader<DTYPE, DP> read(lane);
   const float c = exponent(p.scale);
   const HeadRows k{head_of<DTYPE>(p.k, w.kv), p.k.stride}, v{head_of<DTYPE>(p.v, w.kv), p.v.stride};
@@ -268,32 +258,30 @@ __global__ __launch_bounds__(kThreads, 2) void dq_kernel(AttentionParams p) {
   const Work w = work(p.tiles, p.heads / p.group, p.group, true);
   if (!w.here) return;
   const int head = w.kv * p.group + w.g, row0 = w.tile * kRowsOf + wave * 32, row = row0 + (lane & 31);
-  int begin, end;
-  span_of(p.seq, row0, row, begin, end);
-  const bool valid = end > 0;
-  const int first = valid ? begin : 0x7FFFFFFF, last = valid ? row : -1;
-  const Range r = range_of(valid, first, last);
-  int lo, hi;
-  join_ranges(r, lo, hi);
-  if (hi < 0) return;
-
-  typename O::F q[STEPS], g[STEPS];
-  const int at = valid ? row : 0, dim = valid ? p.dim : 0;
+  const int top = w.tile * kRowsOf, bottom = top + kRowsOf <= p.seq.rows ? top + kRowsOf - 1 : p.seq.rows - 1;
+  typename O::F q[STEPS], g[STEPS];                          // on their way while sequences are looked for
+  const int at = row <= bottom ? row : bottom;
   const T* q_row = head_of<DTYPE>(p.q, head) + at * p.q.stride;
   const T* g_row = head_of<DTYPE>(p.d_o, head) + at * p.d_o.stride;
   const T* o_row = head_of<DTYPE>(p.o, head) + at * p.o.stride;
   float dot = 0.f;
 #pragma unroll
   for (int s = 0; s < STEPS; ++s) {
-    q[s] = load_operand<DTYPE>(q_row, s, lane, dim);
-    g[s] = load_operand<DTYPE>(g_row, s, lane, dim);
-    const typename O::F o = load_operand<DTYPE>(o_row, s, lane, dim);
+    q[s] = load_operand<DTYPE>(q_row, s, lane, p.dim);
+    g[s] = load_operand<DTYPE>(g_row, s, lane, p.dim);
+    const typename O::F o = load_operand<DTYPE>(o_row, s, lane, p.dim);
 #pragma unroll
     for (int e = 0; e < 8; ++e) dot += (float)o[e] * (float)g[s][e];
   }
   dot += other_half(dot);
+  const float base = p.lse[(int64_t)head * p.seq.rows + at] * kLog2e;
+  const Span span = span_of(p.seq, row, top, bottom);
+  const bool valid = span.end > 0;
+  const int first = valid ? span.begin : 0x7FFFFFFF, last = valid ? row : -1;
+  const Range r = range_of(valid, first, last);
+  const int lo = span.top_begin, hi = bottom;
   const Reader<DTYPE, DP> read(lane);
-  const float c = exponent(p.scale), base = valid ? p.lse[(int64_t)head * p.seq.rows + row] * kLog2e : 0.f;
+  const float c = exponent(p.scale);
   if (valid && lane < 32) p.stats[head * p.padded + row] = f32x2{base, dot};
   const HeadRows k{head_of<DTYPE>(p.k, w.kv), p.k.stride}, v{head_of<DTYPE>(p.v, w.kv), p.v.stride};
   unsigned found = 0;
@@ -405,24 +393,21 @@ __device__ __forceinline__ void dkv(const AttentionParams& p) {
   const Work w = work(p.tiles, p.heads / p.group, 1, false);
   if (!w.here) return;
   const int row0 = w.tile * kRowsOf + wave * 32, row = row0 + (lane & 31);
-  int begin, end;
-  span_of(p.seq, row0, row, begin, end);
-  const bool valid = end > 0;
-  const int first = valid ? row : 0x7FFFFFFF, last = valid ? end - 1 : -1;          // rows that see this key
-  const Range r = range_of(valid, first, last);
-  int lo, hi;
-  join_ranges(r, lo, hi);
-  if (hi < 0) return;
-
+  const int top = w.tile * kRowsOf, bottom = top + kRowsOf <= p.seq.rows ? top + kRowsOf - 1 : p.seq.rows - 1;
   Stage<DTYPE, DP, kRowsOf, kThreads, DIRECT> sk;
   sk.init(HeadRows{head_of<DTYPE>(p.k, w.kv), p.k.stride}, p.dim);
-  sk.ask((lds_byte*)own, w.tile * kRowsOf, p.seq.rows);
+  sk.ask((lds_byte*)own, top, p.seq.rows);
   sk.put((lds_byte*)own);
   Keys<DTYPE, DP> keys;
   keys.k = (lds_byte*)own + wave * 32 * Rows<DTYPE, DP>::BYTES;
-  const T* v_row = head_of<DTYPE>(p.v, w.kv) + (valid ? row : 0) * p.v.stride;
+  const T* v_row = head_of<DTYPE>(p.v, w.kv) + (row <= bottom ? row : bottom) * p.v.stride;
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) keys.v[s] = load_operand<DTYPE>(v_row, s, lane, valid ? p.dim : 0);
+  for (int s = 0; s < STEPS; ++s) keys.v[s] = load_operand<DTYPE>(v_row, s, lane, p.dim);
+  const Span span = span_of(p.seq, row, top, bottom);
+  const bool valid = span.end > 0;
+  const int first = valid ? row : 0x7FFFFFFF, last = valid ? span.end - 1 : -1;     // rows that see this key
+  const Range r = range_of(valid, first, last);
+  const int lo = top, hi = span.bottom_end - 1;
   const Reader<DTYPE, DP> read(lane);
   const float c = exponent(p.scale);
   SeenStage<DTYPE, DP, DIRECT> stage;
@@ -467,7 +452,7 @@ __device__ __forceinline__ void dkv(const AttentionParams& p) {
 }
 
 template <int DTYPE, int DP, bool DIRECT>
-__global__ __launch_bounds__(kThreads, 2) void dkv_kernel(AttentionParams p) { dkv<DTYPE, DP, DIRECT>(p); }
+__global__ __launch_bounds__(kThreads, DTYPE == LSAM_DTYPE_BF16 ? 2 : 1) void dkv_kernel(AttentionParams p) { dkv<DTYPE, DP, DIRECT>(p); }
 
 int check(const lsam_attention_desc* d, const char* who) {
   if (!d) return refuse(LSAM_EINVAL, "%s: the descriptor is NULL", who);
