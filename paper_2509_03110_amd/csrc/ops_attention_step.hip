@@ -181,35 +181,63 @@ __global__ __launch_bounds__(kThreads) void step_kernel(StepParams p) {
   }
 }
 
-// A wavefront for each sequence and head: four columns a lane, lanes in groups of 32 take parts in turn.
+// A workgroup for each sequence and head: a part's maximum and sum in each lane, found once; then its eight groups of 32 lanes, four columns a lane,
+// weigh every eighth part.
 template <int DTYPE>
-__global__ __launch_bounds__(64) void join_kernel(StepParams p) {
-  const int lane = threadIdx.x, parts = p.parts[0] + p.parts[1];
+__global__ __launch_bounds__(256) void join_kernel(StepParams p) {
+  static_assert(2 * kMaxParts <= 128, "two parts a lane");
+  __shared__ float weights[2 * kMaxParts], values[8][32][4];
+  const int lane = threadIdx.x & 63, group = threadIdx.x >> 5, parts = p.parts[0] + p.parts[1];
   const int64_t at = blockIdx.x, all = (int64_t)p.seqs * p.heads;
-  const int col = (lane & 31) * 4, n = p.dim - col < 4 ? p.dim - col : 4;
-  float most = -__builtin_inff();
-  for (int i = 0; i < parts; ++i) most = __builtin_fmaxf(most, p.sums[(i * all + at) * 2]);
-  const float base = most == -__builtin_inff() ? 0.f : most;
-  float l = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int i = lane >> 5; i < parts; i += 2) {
-    const float mine = p.sums[(i * all + at) * 2], sum = p.sums[(i * all + at) * 2 + 1];
-    if (sum == 0.f) continue;                                         // no keys: its values were not written
-    const float weight = __builtin_amdgcn_exp2f(mine - base);
-    l += sum * weight;
-    const float* from = p.values + (i * all + at) * p.dim + col;
+  float m[2], sum[2];
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (e < n) v[e] += from[e] * weight;
+  for (int i = 0; i < 2; ++i) {
+    const int part = i * 64 + lane;
+    const f32x2 v = part < parts ? *reinterpret_cast<const f32x2*>(p.sums + (part * all + at) * 2) : f32x2{-__builtin_inff(), 0.f};
+    m[i] = v[0];
+    sum[i] = v[1];
   }
-  l += other_half(l);
+  float most = __builtin_fmaxf(m[0], m[1]);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] += other_half(v[e]);
-  if (lane >= 32) return;
+  for (int d = 1; d < 64; d <<= 1) most = __builtin_fmaxf(most, __shfl_xor(most, d));
+  const float base = most == -__builtin_inff() ? 0.f : most;
+  float l = 0.f;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float weight = sum[i] == 0.f ? 0.f : __builtin_amdgcn_exp2f(m[i] - base);      // no keys: its values were not written
+    l += sum[i] * weight;
+    if (threadIdx.x < 64) weights[i * 64 + lane] = sum[i] == 0.f ? -1.f : weight;
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
+  __syncthreads();
+  const int col = (threadIdx.x & 31) * 4, n = p.dim - col < 4 ? p.dim - col : 4;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  if (n > 0) {
+#pragma unroll 4
+    for (int i = group; i < parts; i += 8) {
+      const float weight = weights[i];
+      const float* from = p.values + (i * all + at) * p.dim + col;
+      if (weight == -1.f) continue;
+      if (n == 4) {
+        const f32x4 w = *reinterpret_cast<const f32x4_any*>(from);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += w[e] * weight;
+      } else {
+        for (int e = 0; e < n; ++e) v[e] += from[e] * weight;
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) values[group][threadIdx.x & 31][e] = v[e];
+  __syncthreads();
+  if (threadIdx.x >= 32 || n <= 0) return;
+#pragma unroll
+  for (int g = 1; g < 8; ++g)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += values[g][threadIdx.x][e];
   typename Value<DTYPE>::T* o = static_cast<typename Value<DTYPE>::T*>(p.o) + at / p.heads * p.o_stride + at % p.heads * p.o_head + col;
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (e < n) Value<DTYPE>::put(o + e, l == 0.f ? 0.f : v[e] / l);
+  for (int e = 0; e < n; ++e) Value<DTYPE>::put(o + e, l == 0.f ? 0.f : v[e] / l);
 }
 
 // How keys are cut: about as many workgroups as two for each unit, of a tile of keys at least.
@@ -265,7 +293,7 @@ Arg read_only(const lsam_attention_step_desc* d, const char* name, const void* p
 template <int DTYPE, int DP>
 void launch(const StepParams& p, unsigned blocks, hipStream_t s) {
   if (blocks) step_kernel<DTYPE, DP><<<blocks, kThreads, 0, s>>>(p);
-  if (!p.whole) join_kernel<DTYPE><<<(unsigned)(p.seqs * p.heads), 64, 0, s>>>(p);
+  if (!p.whole) join_kernel<DTYPE><<<(unsigned)(p.seqs * p.heads), 256, 0, s>>>(p);
 }
 
 }  // namespace

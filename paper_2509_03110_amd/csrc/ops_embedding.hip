@@ -5,7 +5,7 @@
 //                   workgroups: each owns a range of tokens, walks over all places, and keeps what is in its range
 //   sums_kernel     a wavefront takes 64 sorted places and 256 columns; a token whose places all lie there is finished, of
 //                   others it leaves partial sums; further wavefronts write the zeros of tokens that do not occur
-//   join_kernel     partial sums of tokens that go on past 64 places
+//   join_kernel     partial sums of tokens that go on past an edge of 64 places
 #include "ops.h"
 
 namespace lsam {
@@ -16,6 +16,8 @@ constexpr int kMaxRange = 512;         // tokens of a workgroup of order_kernel:
 constexpr int kAhead = 8;              // loads of 64 tokens on their way
 constexpr int kPlaces = 64;            // sorted places of a wavefront of sums_kernel, one for each lane
 constexpr int kSlab = 256;             // columns of a wavefront, four a lane
+constexpr int kZeroRows = 16;          // rows of the table that a wavefront looks at for tokens that do not occur
+constexpr int kJoinWaves = 8;
 
 struct EmbeddingParams {
   const int32_t* tokens; const void* table; void* y;
@@ -69,8 +71,12 @@ __device__ __forceinline__ void each_token(int32_t token, bool mine, F f) {
   }
 }
 
+// The same for a range of few tokens: all counters of a wavefront are scalars, and nothing waits for LDS.
+constexpr int kFew = 8;
+
 // Each wavefront owns a run of places and a column of counters, so that places keep their order: counted first, then, from the sums of
 // the counters before, put where they belong.  All lanes update a counter alike.  Tokens of other ranges cost a load and two comparisons.
+template <bool FEW>
 __global__ __launch_bounds__(kOrderWaves * 64) void order_kernel(EmbeddingParams p) {
   __shared__ uint32_t counts[kMaxRange * kOrderWaves], sums[kOrderWaves], below[kOrderWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -87,6 +93,7 @@ __global__ __launch_bounds__(kOrderWaves * 64) void order_kernel(EmbeddingParams
   end = end < p.rows ? end : p.rows;
 
   uint32_t fewer = 0;                                      // tokens of lower ranges
+  uint32_t few[kFew] = {};
   for (int64_t at = first; at < end; at += 64 * kAhead) {
     int32_t t[kAhead];
 #pragma unroll
@@ -97,12 +104,22 @@ __global__ __launch_bounds__(kOrderWaves * 64) void order_kernel(EmbeddingParams
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       fewer += (uint32_t)__popcll(__ballot(t[i] >= 0 && t[i] < lo));
+      if constexpr (FEW) {
+#pragma unroll
+        for (int k = 0; k < kFew; ++k) few[k] += (uint32_t)__popcll(__ballot(t[i] == lo + k));
+        continue;
+      }
       each_token(t[i], t[i] >= lo && t[i] < hi, [&](int32_t token, unsigned long long same) {
         counts[(token - lo) * kOrderWaves + wave] += (uint32_t)__popcll(same);
       });
     }
   }
   if (lane == 0) below[wave] = fewer;
+  if constexpr (FEW) {
+#pragma unroll
+    for (int k = 0; k < kFew; ++k)
+      if (k < hi - lo) counts[k * kOrderWaves + wave] = few[k];
+  }
   __syncthreads();
 
   // sums of all counters before each: a run of counters a thread, then over the threads
@@ -138,6 +155,10 @@ __global__ __launch_bounds__(kOrderWaves * 64) void order_kernel(EmbeddingParams
   }
   __syncthreads();
 
+  if constexpr (FEW) {
+#pragma unroll
+    for (int k = 0; k < kFew; ++k) few[k] = k < hi - lo ? __builtin_amdgcn_readfirstlane(counts[k * kOrderWaves + wave]) : 0;
+  }
   for (int64_t at = first; at < end; at += 64 * kAhead) {
     int32_t t[kAhead];
 #pragma unroll
@@ -147,6 +168,15 @@ __global__ __launch_bounds__(kOrderWaves * 64) void order_kernel(EmbeddingParams
     }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
+      if constexpr (FEW) {
+#pragma unroll
+        for (int k = 0; k < kFew; ++k) {
+          const unsigned long long same = __ballot(k < hi - lo && t[i] == lo + k);
+          if (same >> lane & 1) order[few[k] + (uint32_t)__popcll(same & ((1ull << lane) - 1))] = (int32_t)(at + i * 64 + lane);
+          few[k] += (uint32_t)__popcll(same);
+        }
+        continue;
+      }
       each_token(t[i], t[i] >= lo && t[i] < hi, [&](int32_t token, unsigned long long same) {
         uint32_t* c = &counts[(token - lo) * kOrderWaves + wave];
         const uint32_t place = *c;
@@ -198,11 +228,12 @@ __global__ __launch_bounds__(256) void sums_kernel(EmbeddingParams p) {
   if (unit >= p.units) {
     unit -= p.units;
     if (unit >= p.zeros) return;
-    const int64_t row = p.row0 + unit / p.pieces;
-    if (start[row] != start[row + 1]) return;
-    const int64_t col = (int64_t)(unit % p.pieces) * kSlab + lane * 4;
-    const int n = (int)(p.dim - col < 4 ? p.dim - col : 4);
-    if (n > 0) store4(dtable + row * p.dtable_stride + col, f32x4{0.f, 0.f, 0.f, 0.f}, n);
+    const int64_t row0 = p.row0 + (int64_t)unit * kZeroRows, at = row0 + lane;
+    unsigned long long left = __ballot(lane < kZeroRows && at < p.vocab && start[at < p.vocab ? at : 0] == start[at < p.vocab ? at + 1 : 0]);
+    for (; left; left &= left - 1) {
+      float* row = dtable + (row0 + __builtin_ctzll(left)) * p.dtable_stride;
+      for (int64_t col = lane * 4; col < p.dim; col += kSlab) store4(row + col, f32x4{0.f, 0.f, 0.f, 0.f}, (int)(p.dim - col < 4 ? p.dim - col : 4));
+    }
     return;
   }
   const int64_t chunk = p.chunk0 + unit / p.pieces, col = (int64_t)(unit % p.pieces) * kSlab + lane * 4;
@@ -246,33 +277,37 @@ __global__ __launch_bounds__(256) void sums_kernel(EmbeddingParams p) {
   leave(places - 1, __builtin_amdgcn_readlane(token, places - 1) == next);
 }
 
-// A wavefront for each chunk in which a token begins that goes on into the next.
-__global__ __launch_bounds__(256) void join_kernel(EmbeddingParams p) {
-  const int lane = threadIdx.x & 63;
+// A workgroup for each chunk in which a token begins that goes on into the next: its wavefronts add runs of the token's partial sums, which
+// are added in their order.
+__global__ __launch_bounds__(kJoinWaves * 64) void join_kernel(EmbeddingParams p) {
+  __shared__ f32x4 part[kJoinWaves][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t replica = p.replica0 + blockIdx.y;
-  const unsigned unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (unit >= p.units) return;
   const int32_t* start = p.start + replica * (p.vocab + 1);
-  const int64_t chunk = p.chunk0 + unit / p.pieces, col = (int64_t)(unit % p.pieces) * kSlab + lane * 4, edge = (chunk + 1) * kPlaces;
+  const int64_t chunk = p.chunk0 + blockIdx.x / p.pieces, col = (int64_t)(blockIdx.x % p.pieces) * kSlab + lane * 4, edge = (chunk + 1) * kPlaces;
   if (edge >= start[p.vocab]) return;
   const int32_t* order = p.order + replica * p.rows;
   const int32_t token = p.tokens[replica * p.token_replica + order[edge]];
   const int64_t begin = start[token], end = start[token + 1];
   if (begin >= edge || begin < edge - kPlaces) return;
   const int n = (int)(p.dim - col < 4 ? p.dim - col : 4);
-  if (n <= 0) return;
-  const int64_t last = (end - 1) / kPlaces, step = 2 * p.dim;
-  const float* partial = p.partial + (replica * p.chunks + chunk) * step + col;
-  f32x4 acc = load4<LSAM_DTYPE_FP32>(partial + p.dim, n);
-  int64_t c = 1;                                                            // the same sums in the same order, whatever is loaded ahead
-  for (; chunk + c + 7 <= last; c += 8) {
+  const int64_t all = (end - 1) / kPlaces - chunk, step = 2 * p.dim;         // of the chunks behind this one
+  const int64_t each = (all + kJoinWaves - 1) / kJoinWaves, from = wave * each, to = from + each < all ? from + each : all;
+  const float* partial = p.partial + (replica * p.chunks + chunk) * step + (n > 0 ? col : 0);
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  if (wave == 0) acc = load4<LSAM_DTYPE_FP32>(partial + p.dim, n);
+  for (int64_t c = from; c < to; c += 8) {
     f32x4 v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = load4<LSAM_DTYPE_FP32>(partial + (c + i) * step, n);
+    for (int i = 0; i < 8; ++i) v[i] = load4<LSAM_DTYPE_FP32>(partial + ((c + i < to ? c + i : to - 1) + 1) * step, n);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) acc += v[i];
+    for (int i = 0; i < 8; ++i)
+      if (c + i < to) acc += v[i];
   }
-  for (; chunk + c <= last; ++c) acc += load4<LSAM_DTYPE_FP32>(partial + c * step, n);
+  part[wave][lane] = acc;
+  __syncthreads();
+  if (wave != 0 || n <= 0) return;
+  for (int w = 1; w < kJoinWaves; ++w) acc += part[w][lane];
   store4(p.dtable + replica * p.dtable_replica + token * p.dtable_stride + col, acc * p.scale, n);
 }
 
@@ -397,14 +432,16 @@ extern "C" int lsam_embedding_backward(const lsam_embedding_desc* d, const int32
   const unsigned apiece = (unsigned)((1 << 21) / c.ranges);
   for (unsigned k = 0; k < K; k += apiece) {
     p.replica0 = (int32_t)k;
-    order_kernel<<<dim3((unsigned)c.ranges, K - k < apiece ? K - k : apiece), kOrderWaves * 64, 0, s>>>(p);
+    const dim3 grid((unsigned)c.ranges, K - k < apiece ? K - k : apiece);
+    if (c.range <= kFew) order_kernel<true><<<grid, kOrderWaves * 64, 0, s>>>(p);
+    else order_kernel<false><<<grid, kOrderWaves * 64, 0, s>>>(p);
   }
-  // lines of columns, a wavefront for each of a line's pieces: chunks to be summed first, then rows of the table
-  const int64_t most = (1 << 24) / p.pieces;
+  // a wavefront for each chunk and piece of columns to be summed, then for each kZeroRows rows of the table
+  const int64_t most = (1 << 24) / p.pieces, most_rows = (int64_t)kZeroRows << 24;
   for (int64_t c0 = 0, r0 = 0; c0 < c.chunks || r0 < d->vocab;) {
-    const int64_t nc = c.chunks - c0 < most ? c.chunks - c0 : most, nr = d->vocab - r0 < most - nc ? d->vocab - r0 : most - nc;
+    const int64_t nc = c.chunks - c0 < most ? c.chunks - c0 : most, nr = d->vocab - r0 < most_rows ? d->vocab - r0 : most_rows;
     p.chunk0 = c0; p.row0 = r0;
-    p.units = (unsigned)(nc * p.pieces); p.zeros = (unsigned)(nr * p.pieces);
+    p.units = (unsigned)(nc * p.pieces); p.zeros = (unsigned)((nr + kZeroRows - 1) / kZeroRows);
     const unsigned blocks = (p.units + p.zeros + 3) / 4, together = (1u << 23) / blocks < 65535 ? (1u << 23) / blocks : 65535;
     for (unsigned k = 0; k < K; k += together) {
       p.replica0 = (int32_t)k;
@@ -415,13 +452,14 @@ extern "C" int lsam_embedding_backward(const lsam_embedding_desc* d, const int32
     c0 += nc;
     r0 += nr;
   }
-  for (int64_t c0 = 0; c0 + 1 < c.chunks; c0 += most) {
+  const int64_t joined = (1 << 22) / p.pieces;
+  for (int64_t c0 = 0; c0 + 1 < c.chunks; c0 += joined) {
     p.chunk0 = c0;
-    p.units = (unsigned)((c.chunks - 1 - c0 < most ? c.chunks - 1 - c0 : most) * p.pieces);
-    const unsigned blocks = (p.units + 3) / 4, together = (1u << 23) / blocks < 65535 ? (1u << 23) / blocks : 65535;
+    const unsigned blocks = (unsigned)((c.chunks - 1 - c0 < joined ? c.chunks - 1 - c0 : joined) * p.pieces);
+    const unsigned together = (1u << 22) / blocks < 65535 ? (1u << 22) / blocks : 65535;
     for (unsigned k = 0; k < K; k += together) {
       p.replica0 = (int32_t)k;
-      join_kernel<<<dim3(blocks, K - k < together ? K - k : together), 256, 0, s>>>(p);
+      join_kernel<<<dim3(blocks, K - k < together ? K - k : together), kJoinWaves * 64, 0, s>>>(p);
     }
   }
   return launched();

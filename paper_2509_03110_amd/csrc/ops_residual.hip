@@ -24,6 +24,23 @@ struct ResidualParams {
 };
 struct SumsParams { const float* sums; float* out[2]; int64_t stride[2], dim; int groups; int32_t replica0; };
 
+// Eight numbers as they are stored.
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+template <int DTYPE> struct Raw;
+template <> struct Raw<LSAM_DTYPE_BF16> {
+  typedef u16x8 T;
+  static __device__ __forceinline__ T load(const unsigned short* p) { return *reinterpret_cast<const u16x8_any*>(p); }
+  static __device__ __forceinline__ float wide(unsigned short v) { return widen(v); }
+};
+template <> struct Raw<LSAM_DTYPE_FP32> {
+  typedef f32x8 T;
+  static __device__ __forceinline__ T load(const float* p) {
+    const f32x4 a = *reinterpret_cast<const f32x4_any*>(p), b = *reinterpret_cast<const f32x4_any*>(p + 4);
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  static __device__ __forceinline__ float wide(float v) { return v; }
+};
+
 // Sum over all lanes of the workgroup, the same in each; `shared`: a number for each wavefront, not in use.
 template <int WAVES>
 __device__ __forceinline__ float sum_over_row(float v, float* shared) {
@@ -37,6 +54,28 @@ __device__ __forceinline__ float sum_over_row(float v, float* shared) {
     for (int w = 0; w < WAVES; ++w) v += shared[w];
   }
   return v;
+}
+
+// The same for N sums at once.
+template <int WAVES, int N>
+__device__ __forceinline__ void sums_over_row(float (&v)[N], float (*shared)[WAVES]) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], d);
+  if constexpr (WAVES > 1) {
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) shared[i][threadIdx.x >> 6] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[i] = 0.f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) v[i] += shared[i][w];
+    }
+  }
 }
 
 // A lane's numbers of a row: CH runs of eight, neighbouring lanes side by side.
@@ -61,6 +100,23 @@ struct Columns {
       }
     }
   }
+  // As they are stored, for a row ahead; zeros behind the row's end.
+  template <int DTYPE>
+  __device__ __forceinline__ void ask(const typename Value<DTYPE>::T* p, typename Raw<DTYPE>::T (&v)[CH]) const {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int n = count(c);
+      if (n == 8) {
+        v[c] = Raw<DTYPE>::load(p + col(c));
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          v[c][e] = 0;
+          if (e < n) v[c][e] = p[col(c) + e];
+        }
+      }
+    }
+  }
   template <int DTYPE>
   __device__ __forceinline__ void store(typename Value<DTYPE>::T* p, const float (&v)[CH][8]) const {
 #pragma unroll
@@ -76,6 +132,14 @@ struct Columns {
     }
   }
 };
+
+template <int DTYPE, int CH>
+__device__ __forceinline__ void widen_row(const typename Raw<DTYPE>::T (&r)[CH], float (&v)[CH][8]) {
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[c][e] = Raw<DTYPE>::wide(r[c][e]);
+}
 
 template <int DTYPE>
 __device__ __forceinline__ typename Value<DTYPE>::T* row_of(const Tensor& t, int64_t replica, int64_t row) {
@@ -144,86 +208,96 @@ __global__ __launch_bounds__(WAVES * 64) void residual_kernel(ResidualParams p) 
   }
 }
 
+// A row's sums are two rounds: the squares of r' and y; then, of m = n(r'), g = w_pre dh, and what is multiplied by c = beta s w_post n(y),
+//   sum g m,  sum c (dr + i g),  sum c m    (i = 1 / sqrt(mean r'^2 + eps)),
+// of which sum c D = sum c (dr + i g) - i mean(g m) sum c m needs no third.  The next row is on its way meanwhile.
 template <int DTYPE, int WAVES, int CH>
 __global__ __launch_bounds__(WAVES * 64) void residual_grad_kernel(ResidualParams p) {
-  __shared__ float shared[2][4][WAVES];
+  typedef typename Raw<DTYPE>::T Eight;
+  __shared__ float shared[2][5][WAVES];
   const Columns<WAVES, CH> at{p.dim};
   const int64_t replica = p.replica0 + blockIdx.y;
   const bool join = p.y.p != nullptr, post = p.w_post != nullptr, gated = p.gate.p != nullptr, pre = p.w_pre != nullptr;
   const float per = 1.f / (float)p.dim;
   float w_pre[CH][8], w_post[CH][8], sum_pre[CH][8], sum_post[CH][8];
+  Eight next_r[CH], next_h[CH], next_d[CH], next_y[CH], next_g[CH];
 #pragma unroll
-  for (int c = 0; c < CH; ++c)
+  for (int c = 0; c < CH; ++c) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) { w_pre[c][e] = w_post[c][e] = 1.f; sum_pre[c][e] = sum_post[c][e] = 0.f; }
+    for (int e = 0; e < 8; ++e) {
+      w_pre[c][e] = w_post[c][e] = 1.f;
+      sum_pre[c][e] = sum_post[c][e] = 0.f;
+      next_r[c][e] = next_h[c][e] = next_d[c][e] = next_y[c][e] = next_g[c][e] = 0;
+    }
+  }
   if (pre) at.template load<LSAM_DTYPE_FP32>(p.w_pre + replica * p.w_pre_replica, w_pre);
   if (post) at.template load<LSAM_DTYPE_FP32>(p.w_post + replica * p.w_post_replica, w_post);
+  const auto ask = [&](int64_t row) {
+    if (row >= p.rows) return;
+    if (pre) {
+      at.template ask<DTYPE>(row_of<DTYPE>(p.r, replica, row), next_r);
+      at.template ask<DTYPE>(row_of<DTYPE>(p.dh, replica, row), next_h);
+    }
+    if (p.dr.p) at.template ask<DTYPE>(row_of<DTYPE>(p.dr, replica, row), next_d);
+    if (join) at.template ask<DTYPE>(row_of<DTYPE>(p.y, replica, row), next_y);
+    if (join && gated) at.template ask<DTYPE>(row_of<DTYPE>(p.gate, replica, row), next_g);
+  };
+  ask(blockIdx.x);
   int b = 0;
   for (int64_t row = blockIdx.x; row < p.rows; row += p.groups, b ^= 1) {
-    float d[CH][8], y[CH][8], g[CH][8];
-#pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) d[c][e] = g[c][e] = 0.f;
-    if (p.dr.p) at.template load<DTYPE>(row_of<DTYPE>(p.dr, replica, row), d);
-    if (join) at.template load<DTYPE>(row_of<DTYPE>(p.y, replica, row), y);
-    if (join && gated) at.template load<DTYPE>(row_of<DTYPE>(p.gate, replica, row), g);
-    if (pre) {
-      float r[CH][8], dh[CH][8];
-      at.template load<DTYPE>(row_of<DTYPE>(p.r, replica, row), r);
-      at.template load<DTYPE>(row_of<DTYPE>(p.dh, replica, row), dh);
-      const float inv = inverse(sum_over_row<WAVES>(squares(r), shared[b][0]), p);
-      float dot = 0.f;
-#pragma unroll
-      for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          r[c][e] *= inv;
-          sum_pre[c][e] += dh[c][e] * r[c][e];
-          dh[c][e] *= w_pre[c][e];
-          dot += dh[c][e] * r[c][e];
-        }
-      dot = sum_over_row<WAVES>(dot, shared[b][1]) * per;
-#pragma unroll
-      for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) d[c][e] += inv * (dh[c][e] - r[c][e] * dot);
-    }
-    if (p.dr_out.p) {
-      float out[CH][8];
-#pragma unroll
-      for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) out[c][e] = join ? p.alpha * d[c][e] : d[c][e];
-      at.template store<DTYPE>(row_of<DTYPE>(p.dr_out, replica, row), out);
-    }
-    if (!join) continue;
-    float inv = 1.f, dot = 0.f;
-    if (post) inv = inverse(sum_over_row<WAVES>(squares(y), shared[b][2]), p);
+    float r[CH][8], h[CH][8], d[CH][8], y[CH][8], g[CH][8];
+    widen_row<DTYPE>(next_r, r);
+    widen_row<DTYPE>(next_h, h);
+    widen_row<DTYPE>(next_d, d);
+    widen_row<DTYPE>(next_y, y);
+    widen_row<DTYPE>(next_g, g);
+    ask(row + p.groups);
+    float two[2] = {squares(r), squares(y)};
+    sums_over_row<WAVES>(two, &shared[b][0]);
+    const float ir = pre ? inverse(two[0], p) : 0.f, iy = post ? inverse(two[1], p) : 1.f;
+    float three[3] = {0.f, 0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         float s = 1.f, rest = 0.f;
         if (gated) sigmoid(g[c][e], s, rest);
-        const float n = y[c][e] * inv, whole = p.beta * d[c][e], part = whole * s;
-        g[c][e] = whole * (n * w_post[c][e]) * (s * rest);
-        sum_post[c][e] += part * n;
-        d[c][e] = part * w_post[c][e];
-        y[c][e] = n;
-        dot += d[c][e] * n;
+        r[c][e] *= ir;
+        sum_pre[c][e] += h[c][e] * r[c][e];
+        h[c][e] *= w_pre[c][e];
+        d[c][e] += ir * h[c][e];
+        y[c][e] *= iy;
+        const float by = p.beta * s * w_post[c][e] * y[c][e];
+        three[0] += h[c][e] * r[c][e];
+        three[1] += by * d[c][e];
+        three[2] += by * r[c][e];
+      }
+    sums_over_row<WAVES>(three, &shared[b][2]);
+    const float dot = ir * three[0] * per, post_dot = (three[1] - dot * three[2]) * per;
+    float out[CH][8];
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        d[c][e] -= dot * r[c][e];
+        out[c][e] = join ? p.alpha * d[c][e] : d[c][e];
+      }
+    if (p.dr_out.p) at.template store<DTYPE>(row_of<DTYPE>(p.dr_out, replica, row), out);
+    if (!join) continue;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float s = 1.f, rest = 0.f;
+        if (gated) sigmoid(g[c][e], s, rest);
+        const float whole = p.beta * d[c][e], part = whole * s;
+        g[c][e] = whole * (y[c][e] * w_post[c][e]) * (s * rest);
+        sum_post[c][e] += part * y[c][e];
+        out[c][e] = part * w_post[c][e];
+        if (post) out[c][e] = iy * (out[c][e] - y[c][e] * post_dot);
       }
     if (gated && p.dgate.p) at.template store<DTYPE>(row_of<DTYPE>(p.dgate, replica, row), g);
-    if (p.dy.p) {
-      if (post) {
-        dot = sum_over_row<WAVES>(dot, shared[b][3]) * per;
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) d[c][e] = inv * (d[c][e] - y[c][e] * dot);
-      }
-      at.template store<DTYPE>(row_of<DTYPE>(p.dy, replica, row), d);
-    }
+    if (p.dy.p) at.template store<DTYPE>(row_of<DTYPE>(p.dy, replica, row), out);
   }
   float* sums = p.sums + (replica * p.groups + blockIdx.x) * 2 * p.dim;
   if (p.want_pre) at.template store<LSAM_DTYPE_FP32>(sums, sum_pre);
