@@ -1,8 +1,10 @@
 // lsam_embedding, lsam_embedding_backward: rows of a table for tokens, and the sum of each token's rows of a gradient.
 //
-//   lookup_kernel   y = scale E[token]: eight numbers a lane
-//   order_kernel    the places of a replica's tokens, sorted by token and within a token by place, with no atomics and no exchange between
-//                   workgroups: each owns a range of tokens, walks over all places, and keeps what is in its range
+//   lookup_kernel   y = scale E[token]: sixteen bytes of y a lane
+//   order_kernel    the places of a replica's tokens, sorted by token and within a token by place, with no atomics: a workgroup owns
+//                   a range of tokens, walks over the places and keeps what is in its range.  Where places are many they are cut
+//                   into parts for several workgroups, and
+//   count_kernel    says before how often each token occurs in each part
 //   sums_kernel     a wavefront takes 64 sorted places and 256 columns; a token whose places all lie there is finished, of
 //                   others it leaves partial sums; further wavefronts write the zeros of tokens that do not occur
 //   join_kernel     partial sums of tokens that go on past an edge of 64 places
@@ -28,164 +30,17 @@ struct EmbeddingParams {
   int32_t replica0;                    // first replica of this launch
   int64_t row0, chunk0;                // first row of the launch (lookup; zeros of sums_kernel), first chunk (sums, join)
   unsigned units, zeros;               // lanes with work (lookup); wavefronts that sum, or join, and that write zeros
-  unsigned pieces;                     // of eight columns in a row (lookup), of kSlab (sums, join)
+  unsigned pieces;                     // of a lane's columns in a row (lookup), of kSlab (sums, join)
   int64_t chunks;                      // of kPlaces places
-  unsigned range;                      // order_kernel
+  unsigned range, ranges, parts;       // order_kernel: tokens of a workgroup, workgroups for all tokens, parts of the places
+  int64_t part;                        // places of a part
+  uint32_t* count; uint32_t* total;    // [replicas][vocab][parts], [replicas][ranges][parts]
   int32_t* order; int32_t* start;      // [replicas][rows], [replicas][vocab + 1]
   float* partial;                      // [replicas][chunks][2][dim]: of the token that comes from the chunk before, that goes on into the next
 };
 
-// One load of a token before the row's address is known, so bound by latency where rows are few; 4096 x 1024 of four replicas move at the rate of a copy.
-template <int TABLE, int DTYPE>
-__global__ __launch_bounds__(256) void lookup_kernel(EmbeddingParams p) {
-  const unsigned unit = blockIdx.x * 256 + threadIdx.x;
-  if (unit >= p.units) return;
-  const int64_t replica = p.replica0 + blockIdx.y;
-  const unsigned local = unit / p.pieces, col = (unit - local * p.pieces) * 8;
-  const int64_t row = p.row0 + local;
-  const int32_t token = p.tokens[replica * p.token_replica + row];
-  const bool there = token >= 0 && token < p.vocab;
-  const typename Value<TABLE>::T* src = static_cast<const typename Value<TABLE>::T*>(p.table) + replica * p.table_replica + (there ? token : 0) * p.table_stride + col;
-  typename Value<DTYPE>::T* dst = static_cast<typename Value<DTYPE>::T*>(p.y) + replica * p.y_replica + row * p.y_stride + col;
-  const int n = (int)(p.dim - col < 8 ? p.dim - col : 8);
-  float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (n == 8) {
-    if (there) Value<TABLE>::load8(src, v);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = there ? v[e] * p.scale : 0.f;
-    Value<DTYPE>::store8(dst, v);
-  } else {
-    for (int e = 0; e < n; ++e) Value<DTYPE>::put(dst + e, there ? Value<TABLE>::get(src + e) * p.scale : 0.f);
-  }
-}
-
-// Calls f(token, lanes that hold it) for every token of the range that the wavefront holds.
-template <typename F>
-__device__ __forceinline__ void each_token(int32_t token, bool mine, F f) {
-  unsigned long long left = __ballot(mine);
-  while (left) {
-    const int32_t t = __builtin_amdgcn_readlane(token, __builtin_ctzll(left));
-    const unsigned long long same = __ballot(mine && token == t);
-    f(t, same);
-    left &= ~same;
-  }
-}
-
-// The same for a range of few tokens: all counters of a wavefront are scalars, and nothing waits for LDS.
-constexpr int kFew = 8;
-
-// Each wavefront owns a run of places and a column of counters, so that places keep their order: counted first, then, from the sums of
-// the counters before, put where they belong.  All lanes update a counter alike.  Tokens of other ranges cost a load and two comparisons.
-template <bool FEW>
-__global__ __launch_bounds__(kOrderWaves * 64) void order_kernel(EmbeddingParams p) {
-  __shared__ uint32_t counts[kMaxRange * kOrderWaves], sums[kOrderWaves], below[kOrderWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int64_t replica = p.replica0 + blockIdx.y;
-  const int32_t* tokens = p.tokens + replica * p.token_replica;
-  int32_t* order = p.order + replica * p.rows;
-  const int32_t lo = (int32_t)(blockIdx.x * p.range), hi = (int32_t)(lo + p.range < p.vocab ? lo + p.range : p.vocab);
-  const int entries = (hi - lo) * kOrderWaves;
-  for (int i = tid; i < entries; i += kOrderWaves * 64) counts[i] = 0;
-  __syncthreads();
-  const int64_t steps = (p.rows + 63) / 64, each = (steps + kOrderWaves - 1) / kOrderWaves;
-  const int64_t first = wave * each * 64;
-  int64_t end = (wave + 1) * each * 64;
-  end = end < p.rows ? end : p.rows;
-
-  uint32_t fewer = 0;                                      // tokens of lower ranges
-  uint32_t few[kFew] = {};
-  for (int64_t at = first; at < end; at += 64 * kAhead) {
-    int32_t t[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const int64_t row = at + i * 64 + lane;
-      t[i] = row < end ? tokens[row] : -1;
-    }
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      fewer += (uint32_t)__popcll(__ballot(t[i] >= 0 && t[i] < lo));
-      if constexpr (FEW) {
-#pragma unroll
-        for (int k = 0; k < kFew; ++k) few[k] += (uint32_t)__popcll(__ballot(t[i] == lo + k));
-        continue;
-      }
-      each_token(t[i], t[i] >= lo && t[i] < hi, [&](int32_t token, unsigned long long same) {
-        counts[(token - lo) * kOrderWaves + wave] += (uint32_t)__popcll(same);
-      });
-    }
-  }
-  if (lane == 0) below[wave] = fewer;
-  if constexpr (FEW) {
-#pragma unroll
-    for (int k = 0; k < kFew; ++k)
-      if (k < hi - lo) counts[k * kOrderWaves + wave] = few[k];
-  }
-  __syncthreads();
-
-  // sums of all counters before each: a run of counters a thread, then over the threads
-  const int run = (entries + kOrderWaves * 64 - 1) / (kOrderWaves * 64);
-  const int from = tid * run < entries ? tid * run : entries, to = from + run < entries ? from + run : entries;
-  uint32_t mine = 0;
-  for (int i = from; i < to; ++i) mine += counts[i];
-  uint32_t before = mine;                                  // with those of lower lanes
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t other = __shfl_up(before, d);
-    if (lane >= d) before += other;
-  }
-  if (lane == 63) sums[wave] = before;
-  __syncthreads();
-  before -= mine;
-  for (int w = 0; w < kOrderWaves; ++w) {
-    before += below[w];
-    if (w < wave) before += sums[w];
-  }
-  for (int i = from; i < to; ++i) {
-    const uint32_t c = counts[i];
-    counts[i] = before;
-    before += c;
-  }
-  __syncthreads();
-  int32_t* start = p.start + replica * (p.vocab + 1);
-  for (int i = tid; i < hi - lo; i += kOrderWaves * 64) start[lo + i] = (int32_t)counts[i * kOrderWaves];
-  if (hi == p.vocab && tid == 0) {
-    uint32_t all = 0;
-    for (int w = 0; w < kOrderWaves; ++w) all += below[w] + sums[w];
-    start[p.vocab] = (int32_t)all;
-  }
-  __syncthreads();
-
-  if constexpr (FEW) {
-#pragma unroll
-    for (int k = 0; k < kFew; ++k) few[k] = k < hi - lo ? __builtin_amdgcn_readfirstlane(counts[k * kOrderWaves + wave]) : 0;
-  }
-  for (int64_t at = first; at < end; at += 64 * kAhead) {
-    int32_t t[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const int64_t row = at + i * 64 + lane;
-      t[i] = row < end ? tokens[row] : -1;
-    }
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      if constexpr (FEW) {
-#pragma unroll
-        for (int k = 0; k < kFew; ++k) {
-          const unsigned long long same = __ballot(k < hi - lo && t[i] == lo + k);
-          if (same >> lane & 1) order[few[k] + (uint32_t)__popcll(same & ((1ull << lane) - 1))] = (int32_t)(at + i * 64 + lane);
-          few[k] += (uint32_t)__popcll(same);
-        }
-        continue;
-      }
-      each_token(t[i], t[i] >= lo && t[i] < hi, [&](int32_t token, unsigned long long same) {
-        uint32_t* c = &counts[(token - lo) * kOrderWaves + wave];
-        const uint32_t place = *c;
-        if (same >> lane & 1) order[place + (uint32_t)__popcll(same & ((1ull << lane) - 1))] = (int32_t)(at + i * 64 + lane);
-        *c = place + (uint32_t)__popcll(same);
-      });
-    }
-  }
-}
+// Numbers of y that a lane writes.
+template <int DTYPE> constexpr int kLookup = DTYPE == LSAM_DTYPE_BF16 ? 8 : 4;
 
 // Four columns of a row from `col` on, zeros behind the row's end.
 template <int DTYPE>
@@ -216,6 +71,189 @@ __device__ __forceinline__ void store4(float* p, f32x4 v, int n) {
   }
 }
 
+// One load of a token before the row's address is known, so bound by latency where rows are few; 4096 x 1024 of four replicas move at the rate of a copy.
+template <int TABLE, int DTYPE>
+__global__ __launch_bounds__(256) void lookup_kernel(EmbeddingParams p) {
+  const unsigned unit = blockIdx.x * 256 + threadIdx.x;
+  if (unit >= p.units) return;
+  const int64_t replica = p.replica0 + blockIdx.y;
+  constexpr int N = kLookup<DTYPE>;
+  const unsigned local = unit / p.pieces, col = (unit - local * p.pieces) * N;
+  const int64_t row = p.row0 + local;
+  const int32_t token = p.tokens[replica * p.token_replica + row];
+  const bool there = token >= 0 && token < p.vocab;
+  const typename Value<TABLE>::T* src = static_cast<const typename Value<TABLE>::T*>(p.table) + replica * p.table_replica + (there ? token : 0) * p.table_stride + col;
+  typename Value<DTYPE>::T* dst = static_cast<typename Value<DTYPE>::T*>(p.y) + replica * p.y_replica + row * p.y_stride + col;
+  const int n = (int)(p.dim - col < N ? p.dim - col : N);
+  if (n == N) {
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if constexpr (N == 8) {
+      if (there) Value<TABLE>::load8(src, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = there ? v[e] * p.scale : 0.f;
+      Value<DTYPE>::store8(dst, v);
+    } else {
+      const f32x4 w = there ? load4<TABLE>(src, 4) * p.scale : f32x4{0.f, 0.f, 0.f, 0.f};
+      *reinterpret_cast<f32x4_any*>(dst) = w;
+    }
+  } else {
+    for (int e = 0; e < n; ++e) Value<DTYPE>::put(dst + e, there ? Value<TABLE>::get(src + e) * p.scale : 0.f);
+  }
+}
+
+// Calls f(token, lanes that hold it) for every token of the range that the wavefront holds.
+template <typename F>
+__device__ __forceinline__ void each_token(int32_t token, bool mine, F f) {
+  unsigned long long left = __ballot(mine);
+  while (left) {
+    const int32_t t = __builtin_amdgcn_readlane(token, __builtin_ctzll(left));
+    const unsigned long long same = __ballot(mine && token == t);
+    f(t, same);
+    left &= ~same;
+  }
+}
+
+// A wavefront's run of the places of a workgroup's part: f(tokens, first place of them), 64 tokens in the lanes, kAhead times at once.
+template <typename F>
+__device__ __forceinline__ void each_run(const EmbeddingParams& p, const int32_t* tokens, int part, int wave, F f) {
+  const int lane = threadIdx.x & 63;
+  const int64_t begin = part * p.part, end = begin + p.part < p.rows ? begin + p.part : p.rows;
+  const int64_t steps = (end - begin + 63) / 64, each = (steps + kOrderWaves - 1) / kOrderWaves;
+  const int64_t first = begin + wave * each * 64, last = first + each * 64 < end ? first + each * 64 : end;
+  for (int64_t at = first; at < last; at += 64 * kAhead) {
+    int32_t t[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int64_t row = at + i * 64 + lane;
+      t[i] = row < last ? tokens[row] : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (at + i * 64 < last) f(t[i], at + i * 64);
+  }
+}
+// A range of tokens, and the counters [range][wavefronts] of a workgroup's part, one column for each wavefront; all its lanes update one alike.
+struct Range { int32_t lo, hi; };
+__device__ __forceinline__ Range range_of(const EmbeddingParams& p) {
+  const int32_t lo = (int32_t)(blockIdx.x * p.range);
+  return Range{lo, (int32_t)(lo + p.range < p.vocab ? lo + p.range : p.vocab)};
+}
+__device__ __forceinline__ uint32_t count_tokens(const EmbeddingParams& p, const int32_t* tokens, const Range& r, int part, int wave, uint32_t* counts) {
+  for (int i = threadIdx.x; i < (r.hi - r.lo) * kOrderWaves; i += kOrderWaves * 64) counts[i] = 0;
+  __syncthreads();
+  uint32_t fewer = 0;                                      // tokens of lower ranges
+  each_run(p, tokens, part, wave, [&](int32_t t, int64_t) {
+    fewer += (uint32_t)__popcll(__ballot(t >= 0 && t < r.lo));
+    each_token(t, t >= r.lo && t < r.hi, [&](int32_t token, unsigned long long same) { counts[(token - r.lo) * kOrderWaves + wave] += (uint32_t)__popcll(same); });
+  });
+  __syncthreads();
+  return fewer;
+}
+__device__ __forceinline__ uint32_t of_token(const uint32_t* counts, int token) {
+  uint32_t n = 0;
+#pragma unroll
+  for (int w = 0; w < kOrderWaves; ++w) n += counts[token * kOrderWaves + w];
+  return n;
+}
+// Sum over the workgroup's threads before this one, and of all.
+__device__ __forceinline__ uint32_t before_thread(uint32_t mine, uint32_t& all) {
+  __shared__ uint32_t sums[kOrderWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t before = mine;                                  // with those of lower lanes
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t other = __shfl_up(before, d);
+    if (lane >= d) before += other;
+  }
+  if (lane == 63) sums[wave] = before;
+  __syncthreads();
+  before -= mine;
+  all = 0;
+  for (int w = 0; w < kOrderWaves; ++w) {
+    if (w < wave) before += sums[w];
+    all += sums[w];
+  }
+  __syncthreads();
+  return before;
+}
+
+__global__ __launch_bounds__(kOrderWaves * 64) void count_kernel(EmbeddingParams p) {
+  __shared__ uint32_t counts[kMaxRange * kOrderWaves];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = blockIdx.y;
+  const int64_t replica = p.replica0 + blockIdx.z;
+  const Range r = range_of(p);
+  count_tokens(p, p.tokens + replica * p.token_replica, r, part, wave, counts);
+  const uint32_t n = tid < r.hi - r.lo ? of_token(counts, tid) : 0;
+  if (tid < r.hi - r.lo) p.count[(replica * p.vocab + r.lo + tid) * p.parts + part] = n;
+  uint32_t all;
+  before_thread(n, all);
+  if (tid == 0) p.total[(replica * p.ranges + blockIdx.x) * p.parts + part] = all;
+}
+
+// Each wavefront owns a run of places and a column of counters, so that places keep their order: counted first, then, from where each token's
+// places of the wavefront begin, put there.  Tokens of other ranges cost a load and two comparisons.  131072 places of 1000 tokens: 64 us with all places for each
+// of 250 workgroups.
+__global__ __launch_bounds__(kOrderWaves * 64) void order_kernel(EmbeddingParams p) {
+  __shared__ uint32_t counts[kMaxRange * kOrderWaves], below[kOrderWaves];
+  static_assert(kMaxRange <= kOrderWaves * 64, "a token a thread");
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = blockIdx.y;
+  const int64_t replica = p.replica0 + blockIdx.z;
+  const int32_t* tokens = p.tokens + replica * p.token_replica;
+  int32_t* order = p.order + replica * p.rows;
+  const Range r = range_of(p);
+  uint32_t fewer = count_tokens(p, tokens, r, part, wave, counts);
+  uint32_t base = 0, mine = 0, earlier = 0;                // places of lower ranges; a token's, one a thread, and those of them in earlier parts
+  if (p.parts > 1) {
+    uint32_t lower = 0;
+    for (int64_t i = tid; i < (int64_t)blockIdx.x * p.parts; i += kOrderWaves * 64) lower += p.total[replica * p.ranges * p.parts + i];
+    before_thread(lower, base);
+    if (tid < r.hi - r.lo) {
+      const uint32_t* of = p.count + (replica * p.vocab + r.lo + tid) * p.parts;
+      for (unsigned i = 0; i < p.parts; ++i) {
+        if ((int)i < part) earlier += of[i];
+        mine += of[i];
+      }
+    }
+  } else {
+    if (lane == 0) below[wave] = fewer;
+    __syncthreads();
+    for (int w = 0; w < kOrderWaves; ++w) base += below[w];
+    if (tid < r.hi - r.lo) mine = of_token(counts, tid);
+  }
+  uint32_t all;
+  uint32_t at = base + before_thread(mine, all);
+  int32_t* start = p.start + replica * (p.vocab + 1);
+  if (tid < r.hi - r.lo) {
+    if (part == 0) start[r.lo + tid] = (int32_t)at;
+    at += earlier;
+#pragma unroll
+    for (int w = 0; w < kOrderWaves; ++w) {
+      const uint32_t c = counts[tid * kOrderWaves + w];
+      counts[tid * kOrderWaves + w] = at;
+      at += c;
+    }
+  }
+  if (part == 0 && r.hi == p.vocab && tid == 0) start[p.vocab] = (int32_t)(base + all);
+  __syncthreads();
+  each_run(p, tokens, part, wave, [&](int32_t t, int64_t row0) {
+    each_token(t, t >= r.lo && t < r.hi, [&](int32_t token, unsigned long long same) {
+      uint32_t* c = &counts[(token - r.lo) * kOrderWaves + wave];
+      const uint32_t place = *c;
+      if (same >> lane & 1) order[place + (uint32_t)__popcll(same & ((1ull << lane) - 1))] = (int32_t)(row0 + lane);
+      *c = place + (uint32_t)__popcll(same);
+    });
+  });
+}
+
+// The same for what is not read again soon: it does not take the place of other lines in the caches.
+__device__ __forceinline__ void store4_past(float* p, f32x4 v, int n) {
+  if (n == 4) {
+    __builtin_nontemporal_store(v, reinterpret_cast<f32x4_any*>(p));
+  } else {
+    store4(p, v, n);
+  }
+}
+
 // The first p.units wavefronts of a replica sum, p.zeros more write zeros.
 template <int DTYPE>
 __global__ __launch_bounds__(256) void sums_kernel(EmbeddingParams p) {
@@ -232,7 +270,7 @@ __global__ __launch_bounds__(256) void sums_kernel(EmbeddingParams p) {
     unsigned long long left = __ballot(lane < kZeroRows && at < p.vocab && start[at < p.vocab ? at : 0] == start[at < p.vocab ? at + 1 : 0]);
     for (; left; left &= left - 1) {
       float* row = dtable + (row0 + __builtin_ctzll(left)) * p.dtable_stride;
-      for (int64_t col = lane * 4; col < p.dim; col += kSlab) store4(row + col, f32x4{0.f, 0.f, 0.f, 0.f}, (int)(p.dim - col < 4 ? p.dim - col : 4));
+      for (int64_t col = lane * 4; col < p.dim; col += kSlab) store4_past(row + col, f32x4{0.f, 0.f, 0.f, 0.f}, (int)(p.dim - col < 4 ? p.dim - col : 4));
     }
     return;
   }
@@ -311,12 +349,20 @@ __global__ __launch_bounds__(kJoinWaves * 64) void join_kernel(EmbeddingParams p
   store4(p.dtable + replica * p.dtable_replica + token * p.dtable_stride + col, acc * p.scale, n);
 }
 
-struct Plan { int ranges; unsigned range; int64_t chunks; size_t start_at, partial_at, bytes; };
-// Ranges of tokens: about as many workgroups as there are units, so that each holds few of the tokens that it walks over.
+struct Plan { int ranges, parts; unsigned range; int64_t part, chunks; size_t start_at, count_at, total_at, partial_at, bytes; };
+// Ranges of tokens and parts of the places: about as many workgroups as there are units, each of kPart places where the counts of all
+// parts are not much to read.
+constexpr int kPart = 8192;
+constexpr int64_t kMaxCounts = 1 << 22;
 Plan plan(const lsam_embedding_desc* d) {
   Plan c;
   const int64_t replicas = d->replicas > 0 ? d->replicas : 1;
-  int64_t want = (256 + replicas - 1) / replicas;
+  int64_t parts = (d->rows + kPart - 1) / kPart;
+  parts = parts < kMaxCounts / d->vocab ? parts : kMaxCounts / d->vocab;
+  parts = parts < 1 ? 1 : parts > 64 ? 64 : parts;
+  c.part = (d->rows + parts - 1) / parts;
+  c.parts = (int)(c.part > 0 ? (d->rows + c.part - 1) / c.part : 1);
+  int64_t want = (256 + replicas * c.parts - 1) / (replicas * c.parts);
   const int64_t least = (d->vocab + kMaxRange - 1) / kMaxRange;
   want = want < least ? least : want > d->vocab ? d->vocab : want;
   c.range = (unsigned)((d->vocab + want - 1) / want);
@@ -324,7 +370,9 @@ Plan plan(const lsam_embedding_desc* d) {
   c.chunks = (d->rows + kPlaces - 1) / kPlaces;
   const auto up = [](size_t n) { return (n + 255) / 256 * 256; };
   c.start_at = up((size_t)d->replicas * d->rows * 4);
-  c.partial_at = c.start_at + up((size_t)d->replicas * (d->vocab + 1) * 4);
+  c.count_at = c.start_at + up((size_t)d->replicas * (d->vocab + 1) * 4);
+  c.total_at = c.count_at + (c.parts > 1 ? up((size_t)d->replicas * d->vocab * c.parts * 4) : 0);
+  c.partial_at = c.total_at + (c.parts > 1 ? up((size_t)d->replicas * c.ranges * c.parts * 4) : 0);
   c.bytes = c.partial_at + (size_t)d->replicas * c.chunks * 2 * d->dim * 4;
   return c;
 }
@@ -376,7 +424,8 @@ extern "C" int lsam_embedding(const lsam_embedding_desc* d, const int32_t* token
   EmbeddingParams p = params(d, tokens);
   p.table = table; p.y = y;
   p.table_stride = d->table_stride; p.table_replica = d->table_replica; p.y_stride = d->y_stride; p.y_replica = d->y_replica;
-  p.pieces = (unsigned)((d->dim + 7) / 8);
+  const int each = d->dtype == LSAM_DTYPE_BF16 ? kLookup<LSAM_DTYPE_BF16> : kLookup<LSAM_DTYPE_FP32>;
+  p.pieces = (unsigned)((d->dim + each - 1) / each);
   // launches of less than 2^32 lanes
   const int64_t most = (1 << 30) / p.pieces;
   const unsigned K = (unsigned)d->replicas;
@@ -423,18 +472,21 @@ extern "C" int lsam_embedding_backward(const lsam_embedding_desc* d, const int32
   p.order = static_cast<int32_t*>(workspace);
   p.start = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + c.start_at);
   p.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + c.partial_at);
-  p.range = c.range;
+  p.count = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + c.count_at);
+  p.total = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + c.total_at);
+  p.range = c.range; p.ranges = (unsigned)c.ranges; p.parts = (unsigned)c.parts; p.part = c.part;
   p.chunks = c.chunks;
   p.pieces = (unsigned)((d->dim + kSlab - 1) / kSlab);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const unsigned K = (unsigned)d->replicas;
   // launches of less than 2^32 lanes
-  const unsigned apiece = (unsigned)((1 << 21) / c.ranges);
+  const int64_t fit = (1 << 21) / ((int64_t)c.ranges * c.parts);
+  const unsigned apiece = (unsigned)(fit < 1 ? 1 : fit < 65535 ? fit : 65535);
   for (unsigned k = 0; k < K; k += apiece) {
     p.replica0 = (int32_t)k;
-    const dim3 grid((unsigned)c.ranges, K - k < apiece ? K - k : apiece);
-    if (c.range <= kFew) order_kernel<true><<<grid, kOrderWaves * 64, 0, s>>>(p);
-    else order_kernel<false><<<grid, kOrderWaves * 64, 0, s>>>(p);
+    const dim3 grid((unsigned)c.ranges, (unsigned)c.parts, K - k < apiece ? K - k : apiece);
+    if (c.parts > 1) count_kernel<<<grid, kOrderWaves * 64, 0, s>>>(p);
+    order_kernel<<<grid, kOrderWaves * 64, 0, s>>>(p);
   }
   // a wavefront for each chunk and piece of columns to be summed, then for each kZeroRows rows of the table
   const int64_t most = (1 << 24) / p.pieces, most_rows = (int64_t)kZeroRows << 24;
