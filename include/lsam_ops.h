@@ -267,7 +267,7 @@ typedef struct {
   int64_t stride, head;                      /* from row to row, from head to head           */
 } lsam_heads;
 typedef struct {
-  int64_t rows;                              /* rows heads below 2^31                        */
+  int64_t rows;                              /* below 2^30; rows heads below 2^31            */
   int64_t seqs;                              /* below 2^31                                   */
   int32_t heads, kv_heads;                   /* heads a multiple of kv_heads, at most 65536  */
   int32_t dim;                               /* 1..LSAM_ATTENTION_MAX_DIM                    */
@@ -303,7 +303,7 @@ int lsam_attention_backward(const lsam_attention_desc* d, const int64_t* offsets
  * message, for a descriptor that is refused); nothing in it has to survive the call. */
 typedef struct {
   int64_t seqs;                              /* seqs heads below 2^23                        */
-  int64_t capacity, prefix;                  /* below 2^31                                   */
+  int64_t capacity, prefix;                  /* below 2^30                                   */
   int32_t heads, kv_heads;                   /* heads a multiple of kv_heads, at most 65536  */
   int32_t dim;                               /* 1..LSAM_ATTENTION_MAX_DIM                    */
   int32_t dtype;                             /* LSAM_DTYPE_*                                 */

@@ -6,6 +6,7 @@
 // one product into the next without leaving the lane.
 #pragma once
 #include "ops.h"
+#include "planes.h"
 
 namespace lsam {
 
@@ -19,7 +20,7 @@ typedef __attribute__((address_space(3))) unsigned char lds_byte;
 template <int DTYPE> struct Operand;
 template <> struct Operand<LSAM_DTYPE_BF16> {
   typedef bf16x8 F;
-  static constexpr int B = 2;
+  static constexpr int PLANES = 1;
   static __device__ __forceinline__ f32x16 multiply(F a, F b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ F from(const f32x16& s, int t) {
     F f;
@@ -38,54 +39,65 @@ template <> struct Operand<LSAM_DTYPE_BF16> {
     }
     return __builtin_bit_cast(F, w);
   }
+  static __device__ __forceinline__ F set(const u32x4 (&w)[1]) { return __builtin_bit_cast(F, w[0]); }
 };
-// fp32 products stay in fp32: eight products over two numbers.
+// An fp32 number is three bfloat16 pieces, h + m + l, which hold all its digits; of their nine products the six that fp32 can tell
+// from 0 are formed, the smallest first: l h, m m, h l, m h, h m, h h.  Six products of 32 cycles against eight of 64 of the fp32 unit over the same
+// sixteen numbers.
 template <> struct Operand<LSAM_DTYPE_FP32> {
-  typedef f32x8 F;
-  static constexpr int B = 4;
-  static __device__ __forceinline__ f32x16 multiply(F a, F b, f32x16 c) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
-    return c;
+  typedef Operand<LSAM_DTYPE_BF16> One;
+  struct F { bf16x8 p[3]; };
+  static constexpr int PLANES = 3;
+  static __device__ __forceinline__ f32x16 multiply(const F& a, const F& b, f32x16 c) {
+    c = One::multiply(a.p[2], b.p[0], c);
+    c = One::multiply(a.p[1], b.p[1], c);
+    c = One::multiply(a.p[0], b.p[2], c);
+    c = One::multiply(a.p[1], b.p[0], c);
+    c = One::multiply(a.p[0], b.p[1], c);
+    return One::multiply(a.p[0], b.p[0], c);
   }
-  static __device__ __forceinline__ F from(const f32x16& s, int t) {
+  static __device__ __forceinline__ F split(const float (&v)[8]) {
+    unsigned w[3][4];
+    float most = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = largest_of(most, v[e]);
+    if (past_rounding(most)) split_words_any<3, 8>(v, w);
+    else split_words<3, 8>(v, w);
     F f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = s[8 * t + e];
+    for (int q = 0; q < 3; ++q) f.p[q] = __builtin_bit_cast(bf16x8, u32x4{w[q][0], w[q][1], w[q][2], w[q][3]});
     return f;
   }
-  static __device__ __forceinline__ F clean(F f, unsigned& found) {
+  static __device__ __forceinline__ F from(const f32x16& s, int t) {
+    float v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const bool fine = __builtin_isfinite(f[e]);
-      found |= fine ? 0u : 1u;
-      f[e] = fine ? f[e] : 0.f;
-    }
-    return f;
+    for (int e = 0; e < 8; ++e) v[e] = s[8 * t + e];
+    return split(v);
+  }
+  static __device__ __forceinline__ F clean(const F& f, unsigned& found) { return F{One::clean(f.p[0], found), One::clean(f.p[1], found), One::clean(f.p[2], found)}; }
+  static __device__ __forceinline__ F set(const u32x4 (&w)[3]) {
+    return F{__builtin_bit_cast(bf16x8, w[0]), __builtin_bit_cast(bf16x8, w[1]), __builtin_bit_cast(bf16x8, w[2])};
   }
 };
 
-// Rows of DP numbers in LDS, in units of 16 bytes.  A unit's place in its row goes by the row, so that neither sixteen lanes that read
-// the same unit of sixteen rows nor sixteen that read 32 bytes of four rows meet in a bank.
+// Rows of DP numbers in LDS, in units of eight bfloat16 numbers, of fp32 numbers the pieces one behind the other.  A unit's place in its row goes
+// by the row, so that neither sixteen lanes that read the same unit of sixteen rows nor sixteen that read 32 bytes of four rows meet in a bank.
 template <int DTYPE, int DP>
 struct Rows {
-  typedef typename Operand<DTYPE>::F F;
-  static constexpr int B = Operand<DTYPE>::B, WIDE = DP > 64 ? 128 : 64, U = WIDE * B / 16, BYTES = WIDE * B;
+  static constexpr int WIDE = DP > 64 ? 128 : 64, U = WIDE / 8, PLANE = WIDE * 2, BYTES = PLANE * Operand<DTYPE>::PLANES;
   static __device__ __forceinline__ int turn(int row) {
-    if constexpr (DTYPE == LSAM_DTYPE_FP32) return row & 15 & (U - 1);
-    else if constexpr (U == 16) return (row & 3) << 2 | (row >> 2 & 3);
+    if constexpr (U == 16) return (row & 3) << 2 | (row >> 2 & 3);
     else return (row >> 1 & 1) << 2 | (row >> 2 & 3);
   }
   static __device__ __forceinline__ int place(int row, int unit) { return row * BYTES + ((unit ^ turn(row)) << 4); }
-
 };
 
 // A lane's places in a tile of rows, found once: what is read from a tile whose address is known when this is compiled takes an
 // offset beside them and no arithmetic.
-template <int DTYPE, int DP> struct Reader;
-template <int DP> struct Reader<LSAM_DTYPE_BF16, DP> {
-  typedef Rows<LSAM_DTYPE_BF16, DP> R;
-  typedef bf16x8 F;
+template <int DTYPE, int DP> struct Reader {
+  typedef Rows<DTYPE, DP> R;
+  typedef Operand<DTYPE> O;
+  typedef typename O::F F;
   unsigned row[DP / 16], column[DP / 32][2];
   __device__ __forceinline__ Reader(int lane) {
 #pragma unroll
@@ -99,97 +111,76 @@ template <int DP> struct Reader<LSAM_DTYPE_BF16, DP> {
   }
   // Row row0 + lane % 32, numbers 16 step + 8 (lane / 32) .. + 7.
   __device__ __forceinline__ F along(const lds_byte* tile, int row0, int step) const {
-    return __builtin_bit_cast(F, *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(tile + row0 * R::BYTES + row[step]));
+    u32x4 w[O::PLANES];
+#pragma unroll
+    for (int q = 0; q < O::PLANES; ++q)
+      w[q] = *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(tile + row0 * R::BYTES + row[step] + q * R::PLANE);
+    return O::set(w);
   }
   // Column 32 t + lane % 32, rows row0 + 4 (lane / 32) + 0 .. 3 and 8 further: the rows of a lane's results.
   __device__ __forceinline__ F across(const lds_byte* tile, int row0, int t) const {
     typedef __attribute__((address_space(3))) s16x4* quad_ptr;
-    lds_byte* const p = const_cast<lds_byte*>(tile) + row0 * R::BYTES;
-    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((quad_ptr)(p + column[t][0]));
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((quad_ptr)(p + column[t][1]));
-    return __builtin_bit_cast(F, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
-  }
-};
-template <int DP> struct Reader<LSAM_DTYPE_FP32, DP> {
-  typedef Rows<LSAM_DTYPE_FP32, DP> R;
-  typedef f32x8 F;
-  int lane;
-  __device__ __forceinline__ Reader(int l) : lane(l) {}
-  __device__ __forceinline__ F along(const lds_byte* tile, int row0, int step) const {
-    typedef const __attribute__((address_space(3))) u32x4* unit_ptr;
-    const int r = row0 + (lane & 31), u = step * 4 + (lane >> 5) * 2;
-    const f32x4 a = __builtin_bit_cast(f32x4, *reinterpret_cast<unit_ptr>(tile + R::place(r, u)));
-    const f32x4 b = __builtin_bit_cast(f32x4, *reinterpret_cast<unit_ptr>(tile + R::place(r, u + 1)));
-    return F{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-  }
-  __device__ __forceinline__ F across(const lds_byte* tile, int row0, int t) const {
-    const int col = t * 32 + (lane & 31);
-    F f;
+    u32x4 w[O::PLANES];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int r = row0 + (lane >> 5) * 4 + (e & 3) + (e >> 2) * 8;
-      f[e] = *reinterpret_cast<const __attribute__((address_space(3))) float*>(tile + R::place(r, col >> 2) + (col & 3) * 4);
+    for (int q = 0; q < O::PLANES; ++q) {
+      lds_byte* const p = const_cast<lds_byte*>(tile) + row0 * R::BYTES + q * R::PLANE;
+      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((quad_ptr)(p + column[t][0]));
+      const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((quad_ptr)(p + column[t][1]));
+      w[q] = __builtin_bit_cast(u32x4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
     }
-    return f;
+    return O::set(w);
   }
 };
 
 // Rows of a tensor for one head.
 struct HeadRows { const void* p; int64_t stride; };
 
-// 16 bytes of a row from unit u on; numbers behind `dim` count as 0.
+// Eight numbers of a row from unit u on, as they are stored; numbers behind `dim` count as 0.
+template <int DTYPE> struct Unit;
+template <> struct Unit<LSAM_DTYPE_BF16> { typedef u16x8 T; typedef u16x8_any Any; };
+typedef f32x8 f32x8_any __attribute__((aligned(4)));
+template <> struct Unit<LSAM_DTYPE_FP32> { typedef f32x8 T; typedef f32x8_any Any; };
 template <int DTYPE>
-__device__ __forceinline__ u32x4 load_unit(const typename Value<DTYPE>::T* row, int u, int dim) {
-  constexpr int N = 16 / Operand<DTYPE>::B;
-  const int n = dim - u * N;
-  u32x4 w = {0, 0, 0, 0};
-  if constexpr (DTYPE == LSAM_DTYPE_BF16) {
-    if (n >= N) {
-      w = __builtin_bit_cast(u32x4, *reinterpret_cast<const u16x8_any*>(row + u * N));
-    } else if (n > 0) {
-      u16x8 v;
-#pragma unroll
-      for (int e = 0; e < N; ++e) v[e] = e < n ? row[u * N + e] : (unsigned short)0;
-      w = __builtin_bit_cast(u32x4, v);
-    }
+__device__ __forceinline__ typename Unit<DTYPE>::T load_unit(const typename Value<DTYPE>::T* row, int u, int dim) {
+  const int n = dim - u * 8;
+  typename Unit<DTYPE>::T v;
+  if (n >= 8) {
+    v = *reinterpret_cast<const typename Unit<DTYPE>::Any*>(row + u * 8);
   } else {
-    if (n >= N) {
-      w = __builtin_bit_cast(u32x4, *reinterpret_cast<const f32x4_any*>(row + u * N));
-    } else if (n > 0) {
-      f32x4 v;
 #pragma unroll
-      for (int e = 0; e < N; ++e) v[e] = e < n ? row[u * N + e] : 0.f;
-      w = __builtin_bit_cast(u32x4, v);
+    for (int e = 0; e < 8; ++e) {
+      v[e] = 0;
+      if (e < n) v[e] = row[u * 8 + e];
     }
   }
-  return w;
+  return v;
 }
-
-// A lane's operand straight from a row in memory: numbers 16 step + 8 (lane / 32) .. + 7.
+__device__ __forceinline__ Operand<LSAM_DTYPE_BF16>::F operand(u16x8 v) { return __builtin_bit_cast(bf16x8, v); }
+__device__ __forceinline__ Operand<LSAM_DTYPE_FP32>::F operand(f32x8 v) {
+  const float x[8] = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+  return Operand<LSAM_DTYPE_FP32>::split(x);
+}
+__device__ __forceinline__ float number(unsigned short v) { return widen(v); }
+__device__ __forceinline__ float number(float v) { return v; }
+// A lane's part of a row in memory: numbers 16 step + 8 (lane / 32) .. + 7.
 template <int DTYPE>
-__device__ __forceinline__ typename Operand<DTYPE>::F load_operand(const typename Value<DTYPE>::T* row, int step, int lane, int dim) {
-  if constexpr (DTYPE == LSAM_DTYPE_BF16) {
-    return __builtin_bit_cast(bf16x8, load_unit<DTYPE>(row, step * 2 + (lane >> 5), dim));
-  } else {
-    const int u = step * 4 + (lane >> 5) * 2;
-    const f32x4 a = __builtin_bit_cast(f32x4, load_unit<DTYPE>(row, u, dim)), b = __builtin_bit_cast(f32x4, load_unit<DTYPE>(row, u + 1, dim));
-    return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-  }
+__device__ __forceinline__ typename Unit<DTYPE>::T load_part(const typename Value<DTYPE>::T* row, int step, int lane, int dim) {
+  return load_unit<DTYPE>(row, step * 2 + (lane >> 5), dim);
 }
 
-// A workgroup's way of bringing ROWS rows into LDS; rows from `limit` on count as 0.  Rows that are aligned to 16 bytes (DIRECT) go there
+// A workgroup's way of bringing ROWS rows into LDS; rows from `limit` on count as 0.  bf16 rows that are aligned to 16 bytes (DIRECT) go there
 // without passing through registers: asked for a tile ahead, there when the wavefront has waited for its loads.  Others
 // are asked for a tile ahead as well, and put there when they are needed.
 template <int DTYPE, int DP, int ROWS, int THREADS, bool DIRECT>
 struct Stage {
   typedef typename Value<DTYPE>::T T;
   typedef Rows<DTYPE, DP> R;
-  static constexpr int N = ROWS * R::U / THREADS;
-  static_assert(N * THREADS == ROWS * R::U, "whole rounds of loads");
+  static constexpr int N = ROWS * R::U / THREADS, PLANES = Operand<DTYPE>::PLANES;
+  static_assert(N * THREADS == ROWS * R::U && !(DIRECT && PLANES > 1), "whole rounds of loads; pieces pass through registers");
   const T* p;
   int64_t stride;
   int dim;
-  u32x4 w[DIRECT ? 1 : N];
+  typename Unit<DTYPE>::T w[DIRECT ? 1 : N];
   unsigned at[DIRECT ? N : 1];
   __device__ __forceinline__ void init(const HeadRows& t, int d) {
     p = static_cast<const T*>(t.p);
@@ -199,14 +190,14 @@ struct Stage {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int n = threadIdx.x + i * THREADS, row = n / R::U, unit = (n % R::U) ^ R::turn(row);
-        at[i] = unit * 16 < dim * R::B ? (unsigned)(row * stride * R::B) + unit * 16 : 0x7FFFFFF0u;
+        at[i] = unit * 8 < dim ? (unsigned)(row * stride * 2) + unit * 16 : 0x7FFFFFF0u;
       }
     }
   }
   __device__ __forceinline__ void ask(lds_byte* tile, int64_t row0, int64_t limit) {
     if constexpr (DIRECT) {
       const int64_t rows = limit - row0 < ROWS ? limit - row0 : ROWS;
-      const unsigned bytes = rows > 0 ? (unsigned)(((rows - 1) * stride + dim) * R::B) : 0;
+      const unsigned bytes = rows > 0 ? (unsigned)(((rows - 1) * stride + dim) * 2) : 0;
       const unsigned long long a = reinterpret_cast<unsigned long long>(p + row0 * stride);
       const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)a), hi = __builtin_amdgcn_readfirstlane((unsigned)(a >> 32));
       const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((unsigned long long)hi << 32 | lo), 0,
@@ -219,7 +210,8 @@ struct Stage {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int n = threadIdx.x + i * THREADS, row = n / R::U;
-        w[i] = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[i][e] = 0;
         if (row0 + row < limit) w[i] = load_unit<DTYPE>(p + (row0 + row) * stride, n % R::U, dim);
       }
     }
@@ -229,7 +221,11 @@ struct Stage {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int n = threadIdx.x + i * THREADS;
-        *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(tile + R::place(n / R::U, n % R::U)) = w[i];
+        const typename Operand<DTYPE>::F f = operand(w[i]);
+        const bf16x8* pieces = reinterpret_cast<const bf16x8*>(&f);
+#pragma unroll
+        for (int q = 0; q < PLANES; ++q)
+          *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(tile + R::place(n / R::U, n % R::U) + q * R::PLANE) = __builtin_bit_cast(u32x4, pieces[q]);
       }
     }
   }
@@ -243,8 +239,7 @@ __device__ __forceinline__ void arrived() {
 }
 // Whether rows can go to LDS directly: 16-byte units all the way, and a tile within 32-bit offsets.
 inline bool direct(const void* p, int64_t stride, int64_t head, int64_t seq, int dim, int dtype) {
-  const int b = dtype_bytes(dtype);
-  return !misaligned(p, 16) && stride * b % 16 == 0 && head * b % 16 == 0 && seq * b % 16 == 0 && dim * b % 16 == 0 && stride < 1 << 20;
+  return dtype == LSAM_DTYPE_BF16 && !misaligned(p, 16) && stride % 8 == 0 && head % 8 == 0 && seq % 8 == 0 && dim % 8 == 0 && stride < 1 << 20;
 }
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -347,6 +342,106 @@ __device__ __forceinline__ void store_column(const f32x16 (&acc)[DP / 32], float
 
 // What the other half of a wavefront holds in the same column.
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+
+// ---- a walk over keys -----------------------------------------------------------------------------------
+constexpr int kThreads = 256;              // of a workgroup
+template <int DTYPE> constexpr int kWavesOf = DTYPE == LSAM_DTYPE_BF16 ? 2 : 1;    // of a SIMD
+template <int DTYPE> constexpr int kTile = DTYPE == LSAM_DTYPE_BF16 ? 64 : 32;      // rows of a tile in LDS
+template <int DTYPE, int DP> constexpr int kLds = 2 * kTile<DTYPE> * Rows<DTYPE, DP>::BYTES;   // a tile of two tensors
+
+struct No { static constexpr bool value = false; };
+struct Yes { static constexpr bool value = true; };
+
+// Keys lo .. hi in tiles, `f(tile of k, tile of v, first key)` for each.  Two tiles a turn in arrays of their own: so the compiler sees that what is
+// read is not what is on its way, and their places are constants.
+template <int DTYPE, int DP, bool DIRECT, typename F>
+__device__ __forceinline__ void walk(lds_byte* even, lds_byte* odd, const HeadRows& k, const HeadRows& v, int lo, int hi, int dim, F f) {
+  constexpr int BN = kTile<DTYPE>, BYTES = BN * Rows<DTYPE, DP>::BYTES;
+  if (lo > hi) return;                                      // nothing is asked for that nothing waits for
+  Stage<DTYPE, DP, BN, kThreads, DIRECT> sk, sv;
+  sk.init(k, dim);
+  sv.init(v, dim);
+  sk.ask(even, lo, hi + 1);
+  sv.ask(even + BYTES, lo, hi + 1);
+  for (int j0 = lo; j0 <= hi;) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      lds_byte* const tk = b ? odd : even;
+      lds_byte* const next = b ? even : odd;
+      sk.put(tk);
+      sv.put(tk + BYTES);
+      arrived();
+      if (j0 + BN <= hi) {
+        sk.ask(next, j0 + BN, hi + 1);
+        sv.ask(next + BYTES, j0 + BN, hi + 1);
+      }
+      f(tk, tk + BYTES, j0);
+      j0 += BN;
+      if (j0 > hi) return;
+    }
+  }
+}
+
+// A column's running sums.
+template <int DP> struct Running {
+  float m = -__builtin_inff(), base = 0.f, l = 0.f;          // the largest score, or one not far below; the same as a power of 2
+  f32x16 acc[DP / 32];
+};
+// How far scores may be above the running maximum, as a power of 2, before sums are scaled to a new one.
+constexpr float kSlack = 8.f;
+
+// The first of a lane's result rows that lie in first .. last, and the last: rows of results 0 .. 15 are compared with them without the lane's part.
+struct Seen {
+  int first, last;
+  __device__ __forceinline__ Seen(int f, int l, int lane) : first(f - 4 * (lane >> 5)), last(l - 4 * (lane >> 5)) {}
+  __device__ __forceinline__ bool operator()(int tile, int r) const {
+    const int row = tile * 32 + 8 * (r >> 2) + (r & 3);
+    return row >= first && row <= last;
+  }
+};
+
+template <int DTYPE, int DP, int TILES, bool CLEAN>
+__device__ __forceinline__ void attend(Running<DP>& a, const Reader<DTYPE, DP>& read, const typename Operand<DTYPE>::F (&q)[DP / 16], const lds_byte* tk,
+                                       const lds_byte* tv, float c, int lane, bool masked, int first, int last, unsigned& found) {
+  typedef Operand<DTYPE> O;
+  constexpr int STEPS = DP / 16;
+  f32x16 s[TILES];
+#pragma unroll
+  for (int i = 0; i < TILES; ++i) s[i] = zero16();
+  products<TILES * STEPS, kAhead>([&](int n) { return read.along(tk, n / STEPS * 32, n % STEPS); },
+                                  [&](int n, const typename O::F& k) { s[n / STEPS] = O::multiply(k, q[n % STEPS], s[n / STEPS]); });
+  if (masked) {
+    const Seen seen(first, last, lane);
+#pragma unroll
+    for (int i = 0; i < TILES; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[i][e] = seen(i, e) ? s[i][e] : -__builtin_inff();
+  }
+  float most = a.m;
+#pragma unroll
+  for (int i = 0; i < TILES; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) most = __builtin_fmaxf(most, s[i][e]);
+  most = __builtin_fmaxf(most, other_half(most));
+  const bool grown = (most - a.m) * c > kSlack;              // of this lane's column alone: no other column's scores change its bits
+  if (__any(grown)) {
+    const float base = grown ? most * c : a.base, less = !grown ? 1.f : a.m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(a.base - base);
+    a.m = grown ? most : a.m;
+    a.base = base;
+    a.l *= less;
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t) a.acc[t] *= less;
+  }
+#pragma unroll
+  for (int i = 0; i < TILES; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[i][e] = __builtin_amdgcn_exp2f(s[i][e] * c - a.base);
+      a.l += s[i][e];
+    }
+#pragma unroll
+  for (int n = 0; n < TILES * 2; ++n) multiply_across<DTYPE, DP, CLEAN>(a.acc, read, tv, n * 16, O::from(s[n / 2], n & 1), found);
+}
 
 // ---- sequences --------------------------------------------------------------------------------------
 // Sequence s is rows offsets[s] .. offsets[s + 1] - 1.  Whatever the offsets hold, no row outside 0..rows is touched.

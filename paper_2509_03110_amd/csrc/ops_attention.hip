@@ -13,7 +13,6 @@
 namespace lsam {
 namespace {
 
-constexpr int kThreads = 256;
 constexpr int kRowsOf = 128;               // rows of a workgroup
 
 struct Tensor { void* p; int64_t stride, head; };
@@ -27,9 +26,6 @@ struct AttentionParams {
   int heads, group, dim, tiles;
   float scale;
 };
-
-template <int DTYPE> constexpr int kTile = DTYPE == LSAM_DTYPE_BF16 ? 64 : 32;      // rows of a tile in LDS
-template <int DTYPE, int DP> constexpr int kLds = 2 * kTile<DTYPE> * Rows<DTYPE, DP>::BYTES;   // a tile of two tensors
 
 // Which tile of rows and which head a workgroup has.  Workgroups go round the eight XCDs in turn: those that read the same keys
 // meet in as few XCDs as that many heads allow.  `of`: heads of a group that are workgroups of their own.  The last tiles of a sequence see most
@@ -86,101 +82,8 @@ __device__ __forceinline__ bool any_of_workgroup(bool v) {
 template <int DTYPE>
 __device__ __forceinline__ typename Value<DTYPE>::T* head_of(const Tensor& t, int head) { return static_cast<typename Value<DTYPE>::T*>(t.p) + head * t.head; }
 
-struct No { static constexpr bool value = false; };
-struct Yes { static constexpr bool value = true; };
-
-// Keys lo .. hi in tiles, `f(tile of k, tile of v, first key)` for each.  Two tiles a turn in arrays of their own: so the compiler sees that what is
-// read is not what is on its way, and their places are constants.
-template <int DTYPE, int DP, bool DIRECT, typename F>
-__device__ __forceinline__ void walk(lds_byte* even, lds_byte* odd, const HeadRows& k, const HeadRows& v, int lo, int hi, int dim, F f) {
-  constexpr int BN = kTile<DTYPE>, BYTES = BN * Rows<DTYPE, DP>::BYTES;
-  Stage<DTYPE, DP, BN, kThreads, DIRECT> sk, sv;
-  sk.init(k, dim);
-  sv.init(v, dim);
-  sk.ask(even, lo, hi + 1);
-  sv.ask(even + BYTES, lo, hi + 1);
-  for (int j0 = lo; j0 <= hi;) {
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      lds_byte* const tk = b ? odd : even;
-      lds_byte* const next = b ? even : odd;
-      sk.put(tk);
-      sv.put(tk + BYTES);
-      arrived();
-      if (j0 + BN <= hi) {
-        sk.ask(next, j0 + BN, hi + 1);
-        sv.ask(next + BYTES, j0 + BN, hi + 1);
-      }
-      f(tk, tk + BYTES, j0);
-      j0 += BN;
-      if (j0 > hi) return;
-    }
-  }
-}
-
-// A column's running sums.
-template <int DP> struct Running {
-  float m = -__builtin_inff(), base = 0.f, l = 0.f;          // the largest score, or one not far below; the same as a power of 2
-  f32x16 acc[DP / 32];
-};
-// How far scores may be above the running maximum, as a power of 2, before sums are scaled to a new one.
-constexpr float kSlack = 8.f;
-
-// The first of a lane's result rows that lie in first .. last, and the last: rows of results 0 .. 15 are compared with them without the lane's part.
-struct Seen {
-  int first, last;
-  __device__ __forceinline__ Seen(int f, int l, int lane) : first(f - 4 * (lane >> 5)), last(l - 4 * (lane >> 5)) {}
-  __device__ __forceinline__ bool operator()(int tile, int r) const {
-    const int row = tile * 32 + 8 * (r >> 2) + (r & 3);
-    return row >= first && row <= last;
-  }
-};
-
-template <int DTYPE, int DP, int TILES, bool CLEAN>
-__device__ __forceinline__ void attend(Running<DP>& a, const Reader<DTYPE, DP>& read, const typename Operand<DTYPE>::F (&q)[DP / 16], const lds_byte* tk,
-                                       const lds_byte* tv, float c, int lane, bool masked, int first, int last, unsigned& found) {
-  typedef Operand<DTYPE> O;
-  constexpr int STEPS = DP / 16;
-  f32x16 s[TILES];
-#pragma unroll
-  for (int i = 0; i < TILES; ++i) s[i] = zero16();
-  products<TILES * STEPS, kAhead>([&](int n) { return read.along(tk, n / STEPS * 32, n % STEPS); },
-                                  [&](int n, const typename O::F& k) { s[n / STEPS] = O::multiply(k, q[n % STEPS], s[n / STEPS]); });
-  if (masked) {
-    const Seen seen(first, last, lane);
-#pragma unroll
-    for (int i = 0; i < TILES; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[i][e] = seen(i, e) ? s[i][e] : -__builtin_inff();
-  }
-  float most = a.m;
-#pragma unroll
-  for (int i = 0; i < TILES; ++i)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) most = __builtin_fmaxf(most, s[i][e]);
-  most = __builtin_fmaxf(most, other_half(most));
-  const bool grown = (most - a.m) * c > kSlack;              // of this lane's column alone: no other column's scores change its bits
-  if (__any(grown)) {
-    const float base = grown ? most * c : a.base, less = !grown ? 1.f : a.m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(a.base - base);
-    a.m = grown ? most : a.m;
-    a.base = base;
-    a.l *= less;
-#pragma unroll
-    for (int t = 0; t < DP / 32; ++t) a.acc[t] *= less;
-  }
-#pragma unroll
-  for (int i = 0; i < TILES; ++i)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      s[i][e] = __builtin_amdgcn_exp2f(s[i][e] * c - a.base);
-      a.l += s[i][e];
-    }
-#pragma unroll
-  for (int n = 0; n < TILES * 2; ++n) multiply_across<DTYPE, DP, CLEAN>(a.acc, read, tv, n * 16, O::from(s[n / 2], n & 1), found);
-}
-
 template <int DTYPE, int DP, bool DIRECT>
-__global__ __launch_bounds__(kThreads, 2) void attention_kernel(AttentionParams p) {
+__global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void attention_kernel(AttentionParams p) {
   typedef typename Value<DTYPE>::T T;
   typedef Operand<DTYPE> O;
   constexpr int BN = kTile<DTYPE>, STEPS = DP / 16;
@@ -193,7 +96,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(AttentionParams 
   typename O::F q[STEPS];                                    // on its way while sequences are looked for
   const T* q_row = head_of<DTYPE>(p.q, head) + (row <= bottom ? row : bottom) * p.q.stride;
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) q[s] = load_operand<DTYPE>(q_row, s, lane, p.dim);
+  for (int s = 0; s < STEPS; ++s) q[s] = operand(load_part<DTYPE>(q_row, s, lane, p.dim));
   const Span span = span_of(p.seq, row, top, bottom);
   const bool valid = span.end > 0;
   const int first = valid ? span.begin : 0x7FFFFFFF, last = valid ? row : -1;
@@ -249,7 +152,7 @@ __device__ __forceinline__ void dq_tile(f32x16 (&acc)[DP / 32], const Reader<DTY
 }
 
 template <int DTYPE, int DP, bool DIRECT>
-__global__ __launch_bounds__(kThreads, 2) void dq_kernel(AttentionParams p) {
+__global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void dq_kernel(AttentionParams p) {
   typedef typename Value<DTYPE>::T T;
   typedef Operand<DTYPE> O;
   constexpr int BN = kTile<DTYPE>, STEPS = DP / 16;
@@ -267,11 +170,11 @@ __global__ __launch_bounds__(kThreads, 2) void dq_kernel(AttentionParams p) {
   float dot = 0.f;
 #pragma unroll
   for (int s = 0; s < STEPS; ++s) {
-    q[s] = load_operand<DTYPE>(q_row, s, lane, p.dim);
-    g[s] = load_operand<DTYPE>(g_row, s, lane, p.dim);
-    const typename O::F o = load_operand<DTYPE>(o_row, s, lane, p.dim);
+    q[s] = operand(load_part<DTYPE>(q_row, s, lane, p.dim));
+    const typename Unit<DTYPE>::T d_o = load_part<DTYPE>(g_row, s, lane, p.dim), o = load_part<DTYPE>(o_row, s, lane, p.dim);
+    g[s] = operand(d_o);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) dot += (float)o[e] * (float)g[s][e];
+    for (int e = 0; e < 8; ++e) dot += number(o[e]) * number(d_o[e]);
   }
   dot += other_half(dot);
   const float base = p.lse[(int64_t)head * p.seq.rows + at] * kLog2e;
@@ -307,9 +210,11 @@ __global__ __launch_bounds__(kThreads, 2) void dq_kernel(AttentionParams p) {
 constexpr int kSeenRows = 32;
 template <int DTYPE, int DP> constexpr int kSeenLds = 2 * kSeenRows * Rows<DTYPE, DP>::BYTES + 8 * kSeenRows;
 
-// What a wavefront of dkv_kernel has: its values, where its keys are, and the sums for them.
+// What a wavefront of dkv_kernel has: its keys or where they are, its values, and the sums for them.
 template <int DTYPE, int DP> struct Keys {
-  const lds_byte* k;
+  static constexpr bool LDS = DTYPE == LSAM_DTYPE_BF16;      // three pieces of 128 keys have no room there, but one wavefront a SIMD has registers
+  const lds_byte* at;
+  typename Operand<DTYPE>::F k[LDS ? 1 : DP / 16];
   typename Operand<DTYPE>::F v[DP / 16];
   f32x16 dk[DP / 32], dv[DP / 32];
 };
@@ -326,7 +231,10 @@ __device__ __forceinline__ void dkv_tile(Keys<DTYPE, DP>& w, const Reader<DTYPE,
   const lds_byte* const stats = tg + BYTES;
   struct Both { F a, b; };
   f32x16 s = zero16(), d = zero16();
-  products<DP / 16, 2>([&](int n) { return Both{read.along(tq, 0, n), read.along(w.k, 0, n)}; }, [&](int n, const Both& f) { s = O::multiply(f.a, f.b, s); });
+  if constexpr (Keys<DTYPE, DP>::LDS)
+    products<DP / 16, 2>([&](int n) { return Both{read.along(tq, 0, n), read.along(w.at, 0, n)}; }, [&](int n, const Both& f) { s = O::multiply(f.a, f.b, s); });
+  else
+    products<DP / 16, kAhead>([&](int n) { return read.along(tq, 0, n); }, [&](int n, const F& f) { s = O::multiply(f, w.k[n], s); });
   products<DP / 16, kAhead>([&](int n) { return read.along(tg, 0, n); }, [&](int n, const F& f) { d = O::multiply(f, w.v[n], d); });
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
@@ -388,21 +296,27 @@ template <int DTYPE, int DP, bool DIRECT>
 __device__ __forceinline__ void dkv(const AttentionParams& p) {
   typedef typename Value<DTYPE>::T T;
   constexpr int BN = kSeenRows, STEPS = DP / 16;
-  __shared__ __attribute__((aligned(1024))) unsigned char even[kSeenLds<DTYPE, DP>], odd[kSeenLds<DTYPE, DP>], own[kRowsOf * Rows<DTYPE, DP>::BYTES];
+  __shared__ __attribute__((aligned(1024))) unsigned char even[kSeenLds<DTYPE, DP>], odd[kSeenLds<DTYPE, DP>], own[Keys<DTYPE, DP>::LDS ? kRowsOf * Rows<DTYPE, DP>::BYTES : 16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Work w = work(p.tiles, p.heads / p.group, 1, false);
   if (!w.here) return;
   const int row0 = w.tile * kRowsOf + wave * 32, row = row0 + (lane & 31);
   const int top = w.tile * kRowsOf, bottom = top + kRowsOf <= p.seq.rows ? top + kRowsOf - 1 : p.seq.rows - 1;
-  Stage<DTYPE, DP, kRowsOf, kThreads, DIRECT> sk;
-  sk.init(HeadRows{head_of<DTYPE>(p.k, w.kv), p.k.stride}, p.dim);
-  sk.ask((lds_byte*)own, top, p.seq.rows);
-  sk.put((lds_byte*)own);
   Keys<DTYPE, DP> keys;
-  keys.k = (lds_byte*)own + wave * 32 * Rows<DTYPE, DP>::BYTES;
+  if constexpr (Keys<DTYPE, DP>::LDS) {
+    Stage<DTYPE, DP, kRowsOf, kThreads, DIRECT> sk;
+    sk.init(HeadRows{head_of<DTYPE>(p.k, w.kv), p.k.stride}, p.dim);
+    sk.ask((lds_byte*)own, top, p.seq.rows);
+    sk.put((lds_byte*)own);
+    keys.at = (lds_byte*)own + wave * 32 * Rows<DTYPE, DP>::BYTES;
+  } else {
+    const T* k_row = head_of<DTYPE>(p.k, w.kv) + (row <= bottom ? row : bottom) * p.k.stride;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) keys.k[s] = operand(load_part<DTYPE>(k_row, s, lane, p.dim));
+  }
   const T* v_row = head_of<DTYPE>(p.v, w.kv) + (row <= bottom ? row : bottom) * p.v.stride;
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) keys.v[s] = load_operand<DTYPE>(v_row, s, lane, p.dim);
+  for (int s = 0; s < STEPS; ++s) keys.v[s] = operand(load_part<DTYPE>(v_row, s, lane, p.dim));
   const Span span = span_of(p.seq, row, top, bottom);
   const bool valid = span.end > 0;
   const int first = valid ? row : 0x7FFFFFFF, last = valid ? span.end - 1 : -1;     // rows that see this key
@@ -452,7 +366,7 @@ __device__ __forceinline__ void dkv(const AttentionParams& p) {
 }
 
 template <int DTYPE, int DP, bool DIRECT>
-__global__ __launch_bounds__(kThreads, DTYPE == LSAM_DTYPE_BF16 ? 2 : 1) void dkv_kernel(AttentionParams p) { dkv<DTYPE, DP, DIRECT>(p); }
+__global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void dkv_kernel(AttentionParams p) { dkv<DTYPE, DP, DIRECT>(p); }
 
 int check(const lsam_attention_desc* d, const char* who) {
   if (!d) return refuse(LSAM_EINVAL, "%s: the descriptor is NULL", who);
@@ -461,7 +375,8 @@ int check(const lsam_attention_desc* d, const char* who) {
     return refuse(LSAM_EINVAL, "%s: heads must be a multiple of kv_heads, in 1..65536", who);
   if (d->dim < 1 || d->dim > LSAM_ATTENTION_MAX_DIM) return refuse(LSAM_EINVAL, "%s: dim must be in 1..%d", who, LSAM_ATTENTION_MAX_DIM);
   if (d->seqs < 0 || d->seqs >= 1ll << 31) return refuse(LSAM_EINVAL, "%s: seqs must be in 0..2^31-1", who);
-  if (d->rows < 0 || d->rows >= 1ll << 31 || d->rows * d->heads >= 1ll << 31) return refuse(LSAM_EINVAL, "%s: rows times heads must be below 2^31", who);
+  if (d->rows < 0 || d->rows >= 1 << 30 || d->rows * d->heads >= 1ll << 31)
+    return refuse(LSAM_EINVAL, "%s: rows must be below 2^30, and times heads below 2^31", who);
   if (!(d->scale >= 0.f) || d->scale > 3e38f) return refuse(LSAM_EINVAL, "%s: the scale must be finite and not negative", who);
   return LSAM_OK;
 }
@@ -508,7 +423,7 @@ int launch_any(const AttentionParams& p, int dtype, bool backward, hipStream_t s
   const auto fits = [&](const Tensor& t) { return direct(t.p, t.stride, t.head, 0, p.dim, dtype); };
   const bool fast = fits(p.k) && fits(p.v) && (!backward || (fits(p.q) && fits(p.d_o)));
   if (dtype == LSAM_DTYPE_BF16) return fast ? launch_wide<LSAM_DTYPE_BF16, true>(p, backward, s) : launch_wide<LSAM_DTYPE_BF16, false>(p, backward, s);
-  return fast ? launch_wide<LSAM_DTYPE_FP32, true>(p, backward, s) : launch_wide<LSAM_DTYPE_FP32, false>(p, backward, s);
+  return launch_wide<LSAM_DTYPE_FP32, false>(p, backward, s);
 }
 
 }  // namespace

@@ -2,16 +2,15 @@
 //
 //   step_kernel  keys are cut into parts.  Queries are columns, 32 a wavefront: of the prefix those of all sequences and of a group's heads,
 //                of a cache those of its sequence's group alone.  Where there are more than 32 a workgroup's wavefronts take columns of
-//                their own and share the keys; where there are not they share the columns, and take 32 keys of a tile each.  A
-//                part leaves the maximum, the sum and the weighted values of each column
+//                their own and share the keys, tile by tile; where there are not they share the columns, and take 32 keys of a tile
+//                each.  A part leaves the maximum, the sum and the weighted values of each column
 //   join_kernel  weighs the parts against each other
 #include "attention.h"
 
 namespace lsam {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kKeys = 32 * kWaves;         // of a tile
+constexpr int kKeys = 128;                 // parts are cut between so many
 constexpr int kMaxParts = 64;              // of the prefix, and of a cache
 
 struct Cache { const void* k; const void* v; int64_t k_stride, k_head, k_seq, v_stride, v_head, v_seq; };
@@ -31,23 +30,20 @@ struct StepParams {
   float* sums; float* values;              // [parts][seqs heads][2], [parts][seqs heads][dim]
 };
 
-template <int DTYPE, int DP>
-__global__ __launch_bounds__(kThreads) void step_kernel(StepParams p) {
+template <int DTYPE, int DP, bool DIRECT>
+__global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void step_kernel(StepParams p) {
   typedef typename Value<DTYPE>::T T;
   typedef Operand<DTYPE> O;
-  typedef Rows<DTYPE, DP> R;
-  constexpr int STEPS = DP / 16;
-  __shared__ __attribute__((aligned(16))) unsigned char memory[2 * kKeys * R::BYTES];
-  __shared__ float of_waves[2][kWaves][32];
-  lds_byte* const tk = (lds_byte*)memory;
-  lds_byte* const tv = tk + kKeys * R::BYTES;
+  constexpr int STEPS = DP / 16, BN = kTile<DTYPE>, WAVES = 2 * BN / 32, BLOCK = DP * 32 * 4;
+  static_assert(kKeys % (2 * BN) == 0 && 2 * BLOCK <= kLds<DTYPE, DP>, "whole tiles; the sums of two wavefronts have room");
+  __shared__ __attribute__((aligned(1024))) unsigned char even[kLds<DTYPE, DP>], odd[kLds<DTYPE, DP>];
+  __shared__ float of_waves[2][WAVES][32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
   // what this workgroup does: a part of the prefix for some columns, or a part of a cache
   const bool shared = blockIdx.x < p.prefix_blocks;
   unsigned unit;
-  int seq = 0, kv, part, first_column;
-  int64_t keys;
+  int seq = 0, kv, part, first_column, keys;
   if (shared) {
     // those that read the same keys meet in an XCD
     const unsigned i = blockIdx.x / 8;
@@ -75,109 +71,85 @@ __global__ __launch_bounds__(kThreads) void step_kernel(StepParams p) {
   const int head = kv * p.group + (shared ? column % p.group : column);
   const int64_t place = ((int64_t)(shared ? part : p.parts[0] + part) * p.seqs + seq) * p.heads + head;
 
-  const int64_t tiles = (keys + kKeys - 1) / kKeys, run = (tiles + p.parts[!shared] - 1) / p.parts[!shared] * kKeys;
-  const int64_t from = part * run, to = from + run < keys ? from + run : keys;
+  const int64_t tiles = ((int64_t)keys + kKeys - 1) / kKeys, run = (tiles + p.parts[!shared] - 1) / p.parts[!shared] * kKeys;
+  const int from = (int)(part * run < keys ? part * run : keys), to = (int)(from + run < keys ? from + run : keys);
   const Cache& c = shared ? p.prefix : p.own;
   const int64_t of = shared ? 0 : seq;
   const HeadRows k{static_cast<const T*>(c.k) + of * c.k_seq + kv * c.k_head, c.k_stride};
   const HeadRows v{static_cast<const T*>(c.v) + of * c.v_seq + kv * c.v_head, c.v_stride};
-  Stage<DTYPE, DP, kKeys, kThreads, false> sk, sv;
-  sk.init(k, p.dim);
-  sv.init(v, p.dim);
-  sk.ask(tk, from, to);
-  sv.ask(tv, from, to);
   typename O::F q[STEPS];
   const T* q_row = static_cast<const T*>(p.q) + (valid ? seq * p.q_stride + head * p.q_head : 0);
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) q[s] = load_operand<DTYPE>(q_row, s, lane, valid ? p.dim : 0);
+  for (int s = 0; s < STEPS; ++s) q[s] = operand(load_part<DTYPE>(q_row, s, lane, valid ? p.dim : 0));
   const Reader<DTYPE, DP> read(lane);
   const float scale = exponent(p.scale);
-  float m = -__builtin_inff(), l = 0.f;
-  unsigned found = 0;
-  f32x16 acc[DP / 32];
+  unsigned found = 0;                                        // keys that are not there are zeros: nothing has to be told apart
+  Running<DP> a;
 #pragma unroll
-  for (int t = 0; t < DP / 32; ++t) acc[t] = zero16();
-  for (int64_t j0 = from; j0 < to; j0 += kKeys) {
-    if (j0 > from) __syncthreads();
-    sk.put(tk);
-    sv.put(tv);
-    __syncthreads();
-    if (j0 + kKeys < to) {
-      sk.ask(tk, j0 + kKeys, to);
-      sv.ask(tv, j0 + kKeys, to);
+  for (int t = 0; t < DP / 32; ++t) a.acc[t] = zero16();
+  float l;
+  if (spread) {
+    walk<DTYPE, DP, DIRECT>((lds_byte*)even, (lds_byte*)odd, k, v, from, to - 1, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0) {
+      attend<DTYPE, DP, BN / 32, false>(a, read, q, tk, tv, scale, lane, j0 + BN > to, 0, to - 1 - j0, found);
+    });
+    l = a.l + other_half(a.l);
+  } else {
+    // one tile of keys and one of values; two workgroups of a unit take turns
+    lds_byte* const tk = (lds_byte*)even;
+    lds_byte* const tv = (lds_byte*)odd;
+    Stage<DTYPE, DP, 2 * BN, kThreads, DIRECT> sk, sv;
+    sk.init(k, p.dim);
+    sv.init(v, p.dim);
+    for (int j0 = from; j0 < to; j0 += 2 * BN) {
+      if (j0 > from) __syncthreads();
+      sk.ask(tk, j0, to);
+      sv.ask(tv, j0, to);
+      sk.put(tk);
+      sv.put(tv);
+      arrived();
+      const int left = to - j0 - wave * 32;                  // keys of this wavefront
+      if (wave < WAVES && left > 0)
+        attend<DTYPE, DP, 1, false>(a, read, q, tk + wave * 32 * Rows<DTYPE, DP>::BYTES, tv + wave * 32 * Rows<DTYPE, DP>::BYTES, scale, lane, left < 32, 0,
+                                    left - 1, found);
     }
-#pragma unroll 1
-    for (int i = spread ? 0 : wave; i < (spread ? kWaves : wave + 1); ++i) {
-      const int left = (int)(to - j0 - i * 32 < 32 ? to - j0 - i * 32 : 32);      // keys that are there; the others are zeros
-      if (left <= 0) break;
-      f32x16 s = zero16();
-#pragma unroll
-      for (int d = 0; d < STEPS; ++d) s = O::multiply(read.along(tk, i * 32, d), q[d], s);
-      if (left < 32) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (result_row(e, lane) >= left) s[e] = -__builtin_inff();
-      }
-      float most = m;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) most = __builtin_fmaxf(most, s[e]);
-      most = __builtin_fmaxf(most, other_half(most));
-      const float base = most == -__builtin_inff() ? 0.f : most * scale;
-      if (__any(most > m)) {
-        const float less = __builtin_amdgcn_exp2f(m * scale - base);
-        l *= less;
-#pragma unroll
-        for (int t = 0; t < DP / 32; ++t) acc[t] *= less;
-      }
-      m = most;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        s[e] = __builtin_amdgcn_exp2f(s[e] * scale - base);
-        l += s[e];
-      }
-#pragma unroll
-      for (int t = 0; t < 2; ++t) multiply_across<DTYPE, DP, false>(acc, read, tv, i * 32 + t * 16, O::from(s, t), found);
-    }
-  }
-  l += other_half(l);
-  m = m == -__builtin_inff() ? m : m * scale;
-  if (!spread) {
     // the wavefronts' keys together: each column's maximum, then wavefront by wavefront
-    if (lane < 32) of_waves[0][wave][lane] = m;
+    l = a.l + other_half(a.l);
+    if (lane < 32 && wave < WAVES) of_waves[0][wave][lane] = a.m;
     __syncthreads();
     float most = of_waves[0][0][lane & 31];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) most = __builtin_fmaxf(most, of_waves[0][w][lane & 31]);
-    const float less = __builtin_amdgcn_exp2f(m - (most == -__builtin_inff() ? 0.f : most));
-    if (lane < 32) of_waves[1][wave][lane] = l * less;
-    m = most;
-    float* const values = reinterpret_cast<float*>(memory);          // [wavefront - 1][number][lane]
-    if (wave > 0) {
+    for (int w = 1; w < WAVES; ++w) most = __builtin_fmaxf(most, of_waves[0][w][lane & 31]);
+    const float base = most == -__builtin_inff() ? 0.f : most * scale, less = a.m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(a.base - base);
+    if (lane < 32 && wave < WAVES) of_waves[1][wave][lane] = l * less;
+    a.m = most;
+    const auto block = [&](int w) { return reinterpret_cast<float*>(w <= 2 ? even + (w - 1) * BLOCK : odd); };
+    if (wave > 0 && wave < WAVES) {
 #pragma unroll
       for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) values[(((wave - 1) * DP / 32 + t) * 16 + r) * 64 + lane] = acc[t][r] * less;
+        for (int r = 0; r < 16; ++r) block(wave)[(t * 16 + r) * 64 + lane] = a.acc[t][r] * less;
     }
     __syncthreads();
     if (wave > 0) return;
     l = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) l += of_waves[1][w][lane & 31];
+    for (int w = 0; w < WAVES; ++w) l += of_waves[1][w][lane & 31];
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        acc[t][r] *= less;
+        a.acc[t][r] *= less;
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) acc[t][r] += values[(((w - 1) * DP / 32 + t) * 16 + r) * 64 + lane];
+        for (int w = 1; w < WAVES; ++w) a.acc[t][r] += block(w)[(t * 16 + r) * 64 + lane];
       }
+    a.base = base;
   }
   if (!valid) return;
   if (p.whole) {
-    store_column<DTYPE, DP>(acc, l == 0.f ? 0.f : 1.f / l, static_cast<T*>(p.o) + seq * p.o_stride + head * p.o_head, lane, p.dim);
+    store_column<DTYPE, DP>(a.acc, l == 0.f ? 0.f : 1.f / l, static_cast<T*>(p.o) + seq * p.o_stride + head * p.o_head, lane, p.dim);
   } else {
-    if (lane < 32) { p.sums[place * 2] = m; p.sums[place * 2 + 1] = l; }
-    if (l != 0.f) store_column<LSAM_DTYPE_FP32, DP>(acc, 1.f, p.values + place * p.dim, lane, p.dim);
+    if (lane < 32) *reinterpret_cast<f32x2*>(p.sums + place * 2) = f32x2{l == 0.f ? -__builtin_inff() : a.base, l};
+    if (l != 0.f) store_column<LSAM_DTYPE_FP32, DP>(a.acc, 1.f, p.values + place * p.dim, lane, p.dim);
   }
 }
 
@@ -275,8 +247,8 @@ int check(const lsam_attention_step_desc* d, const char* who) {
     return refuse(LSAM_EINVAL, "%s: heads must be a multiple of kv_heads, in 1..65536", who);
   if (d->dim < 1 || d->dim > LSAM_ATTENTION_MAX_DIM) return refuse(LSAM_EINVAL, "%s: dim must be in 1..%d", who, LSAM_ATTENTION_MAX_DIM);
   if (d->seqs < 0 || d->seqs >= 1 << 23 || d->seqs * d->heads >= 1 << 23) return refuse(LSAM_EINVAL, "%s: seqs times heads must be below 2^23", who);
-  if (d->capacity < 0 || d->capacity >= 1ll << 31 || d->prefix < 0 || d->prefix >= 1ll << 31)
-    return refuse(LSAM_EINVAL, "%s: capacity and prefix must be in 0..2^31-1", who);
+  if (d->capacity < 0 || d->capacity >= 1 << 30 || d->prefix < 0 || d->prefix >= 1 << 30)
+    return refuse(LSAM_EINVAL, "%s: capacity and prefix must be in 0..2^30-1", who);
   if (!(d->scale >= 0.f) || d->scale > 3e38f) return refuse(LSAM_EINVAL, "%s: the scale must be finite and not negative", who);
   return LSAM_OK;
 }
@@ -290,10 +262,15 @@ Arg read_only(const lsam_attention_step_desc* d, const char* name, const void* p
   return Arg{name, p, n < ((__int128)1 << 46) ? (int64_t)n : -1, b, false};
 }
 
-template <int DTYPE, int DP>
+template <int DTYPE, int DP, bool DIRECT>
 void launch(const StepParams& p, unsigned blocks, hipStream_t s) {
-  if (blocks) step_kernel<DTYPE, DP><<<blocks, kThreads, 0, s>>>(p);
+  if (blocks) step_kernel<DTYPE, DP, DIRECT><<<blocks, kThreads, 0, s>>>(p);
   if (!p.whole) join_kernel<DTYPE><<<(unsigned)(p.seqs * p.heads), 256, 0, s>>>(p);
+}
+template <int DTYPE, bool DIRECT>
+void launch_wide(const StepParams& p, unsigned blocks, hipStream_t s) {
+  if (p.dim <= 64) launch<DTYPE, 64, DIRECT>(p, blocks, s);
+  else launch<DTYPE, 128, DIRECT>(p, blocks, s);
 }
 
 }  // namespace
@@ -345,10 +322,11 @@ extern "C" int lsam_attention_step(const lsam_attention_step_desc* d, const int3
   p.sums = static_cast<float*>(workspace);
   p.values = reinterpret_cast<float*>(static_cast<char*>(workspace) + c.values_at);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (d->dtype == LSAM_DTYPE_BF16) {
-    if (p.dim <= 64) launch<LSAM_DTYPE_BF16, 64>(p, c.blocks, s); else launch<LSAM_DTYPE_BF16, 128>(p, c.blocks, s);
-  } else {
-    if (p.dim <= 64) launch<LSAM_DTYPE_FP32, 64>(p, c.blocks, s); else launch<LSAM_DTYPE_FP32, 128>(p, c.blocks, s);
-  }
+  const auto fits = [&](const void* t, const lsam_heads& h, int64_t seq) { return direct(t, h.stride, h.head, seq, d->dim, d->dtype); };
+  const bool fast = (c.parts[0] == 0 || (fits(prefix_k, d->prefix_k, 0) && fits(prefix_v, d->prefix_v, 0))) &&
+                    (c.parts[1] == 0 || (fits(k, d->k, d->k_seq) && fits(v, d->v, d->v_seq)));
+  if (d->dtype == LSAM_DTYPE_FP32) launch_wide<LSAM_DTYPE_FP32, false>(p, c.blocks, s);
+  else if (fast) launch_wide<LSAM_DTYPE_BF16, true>(p, c.blocks, s);
+  else launch_wide<LSAM_DTYPE_BF16, false>(p, c.blocks, s);
   return launched();
 }
