@@ -22,7 +22,8 @@ template <> struct Operand<LSAM_DTYPE_BF16> {
   typedef bf16x8 F;
   static constexpr int PLANES = 1;
   static __device__ __forceinline__ f32x16 multiply(F a, F b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-  static __device__ __forceinline__ F from(const f32x16& s, int t) {
+  // Results 8 t .. of a product as an operand of the next; `weights`: none is above 2^9.
+  static __device__ __forceinline__ F from(const f32x16& s, int t, bool weights) {
     F f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] = static_cast<__bf16>(s[8 * t + e]);
@@ -56,23 +57,25 @@ template <> struct Operand<LSAM_DTYPE_FP32> {
     c = One::multiply(a.p[0], b.p[1], c);
     return One::multiply(a.p[0], b.p[0], c);
   }
-  static __device__ __forceinline__ F split(const float (&v)[8]) {
+  static __device__ __forceinline__ F split(const float (&v)[8], bool weights) {
     unsigned w[3][4];
     float most = 0.f;
+    if (!weights) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) most = largest_of(most, v[e]);
-    if (past_rounding(most)) split_words_any<3, 8>(v, w);
+      for (int e = 0; e < 8; ++e) most = largest_of(most, v[e]);
+    }
+    if (__any(past_rounding(most))) split_words_any<3, 8>(v, w);
     else split_words<3, 8>(v, w);
     F f;
 #pragma unroll
     for (int q = 0; q < 3; ++q) f.p[q] = __builtin_bit_cast(bf16x8, u32x4{w[q][0], w[q][1], w[q][2], w[q][3]});
     return f;
   }
-  static __device__ __forceinline__ F from(const f32x16& s, int t) {
+  static __device__ __forceinline__ F from(const f32x16& s, int t, bool weights) {
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = s[8 * t + e];
-    return split(v);
+    return split(v, weights);
   }
   static __device__ __forceinline__ F clean(const F& f, unsigned& found) { return F{One::clean(f.p[0], found), One::clean(f.p[1], found), One::clean(f.p[2], found)}; }
   static __device__ __forceinline__ F set(const u32x4 (&w)[3]) {
@@ -148,9 +151,11 @@ __device__ __forceinline__ typename Unit<DTYPE>::T load_unit(const typename Valu
     v = *reinterpret_cast<const typename Unit<DTYPE>::Any*>(row + u * 8);
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      v[e] = 0;
-      if (e < n) v[e] = row[u * 8 + e];
+    for (int e = 0; e < 8; ++e) v[e] = 0;
+    if (n > 0) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < n) v[e] = row[u * 8 + e];
     }
   }
   return v;
@@ -158,7 +163,7 @@ __device__ __forceinline__ typename Unit<DTYPE>::T load_unit(const typename Valu
 __device__ __forceinline__ Operand<LSAM_DTYPE_BF16>::F operand(u16x8 v) { return __builtin_bit_cast(bf16x8, v); }
 __device__ __forceinline__ Operand<LSAM_DTYPE_FP32>::F operand(f32x8 v) {
   const float x[8] = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
-  return Operand<LSAM_DTYPE_FP32>::split(x);
+  return Operand<LSAM_DTYPE_FP32>::split(x, false);
 }
 __device__ __forceinline__ float number(unsigned short v) { return widen(v); }
 __device__ __forceinline__ float number(float v) { return v; }
@@ -440,7 +445,91 @@ __device__ __forceinline__ void attend(Running<DP>& a, const Reader<DTYPE, DP>& 
       a.l += s[i][e];
     }
 #pragma unroll
-  for (int n = 0; n < TILES * 2; ++n) multiply_across<DTYPE, DP, CLEAN>(a.acc, read, tv, n * 16, O::from(s[n / 2], n & 1), found);
+  for (int n = 0; n < TILES * 2; ++n) multiply_across<DTYPE, DP, CLEAN>(a.acc, read, tv, n * 16, O::from(s[n / 2], n & 1, true), found);
+}
+
+// ---- wavefronts that share columns ------------------------------------------------------------------------
+// Where there are few columns for the chip a workgroup's wavefronts share 32, and take 32 keys each of a tile of as many as have room in LDS.
+template <int DTYPE> constexpr int kSharing = 2 * kTile<DTYPE> / 32;
+
+// The sums of a workgroup's wavefronts in its first one; `even` and `odd` are free.
+template <int DTYPE, int DP>
+__device__ __forceinline__ void join_sums(f32x16 (&acc)[DP / 32], int wave, int lane, unsigned char* even, unsigned char* odd) {
+  constexpr int BLOCK = DP * 32 * 4;
+  static_assert(2 * BLOCK <= kLds<DTYPE, DP> && kSharing<DTYPE> <= 4, "two wavefronts' sums in an array");
+  const auto block = [&](int w) { return reinterpret_cast<float*>(w <= 2 ? even + (w - 1) * BLOCK : odd); };
+  if (wave > 0 && wave < kSharing<DTYPE>) {
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) block(wave)[(t * 16 + r) * 64 + lane] = acc[t][r];
+  }
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int w = 1; w < kSharing<DTYPE>; ++w) acc[t][r] += block(w)[(t * 16 + r) * 64 + lane];
+}
+// The same for running sums: each column's maximum first.  l comes whole, of both halves.
+template <int DTYPE, int DP>
+__device__ __forceinline__ void join_running(Running<DP>& a, float c, int wave, int lane, unsigned char* even, unsigned char* odd) {
+  constexpr int N = kSharing<DTYPE>;
+  __shared__ float of_waves[2][N][32];
+  a.l += other_half(a.l);
+  if (lane < 32 && wave < N) of_waves[0][wave][lane] = a.m;
+  __syncthreads();
+  float most = of_waves[0][0][lane & 31];
+#pragma unroll
+  for (int w = 1; w < N; ++w) most = __builtin_fmaxf(most, of_waves[0][w][lane & 31]);
+  const float base = most == -__builtin_inff() ? 0.f : most * c, less = a.m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(a.base - base);
+  if (lane < 32 && wave < N) of_waves[1][wave][lane] = a.l * less;
+  if (wave < N) {
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t) a.acc[t] *= less;
+  }
+  join_sums<DTYPE, DP>(a.acc, wave, lane, even, odd);
+  a.m = most;
+  a.base = base;
+  a.l = 0.f;
+#pragma unroll
+  for (int w = 0; w < N; ++w) a.l += of_waves[1][w][lane & 31];
+}
+// Keys lo .. hi in tiles of kSharing x 32, `f(its keys, their values, the first of them)` for each wavefront that has some.  One tile at a time; two
+// workgroups of a unit take turns.
+template <int DTYPE, int DP, bool DIRECT, typename F>
+__device__ __forceinline__ void walk_shared(unsigned char* even, unsigned char* odd, const HeadRows& k, const HeadRows& v, int lo, int hi, int dim, F f) {
+  constexpr int ROWS = kSharing<DTYPE> * 32, EACH = 32 * Rows<DTYPE, DP>::BYTES;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Stage<DTYPE, DP, ROWS, kThreads, DIRECT> sk, sv;
+  sk.init(k, dim);
+  sv.init(v, dim);
+  if constexpr (!DIRECT) {
+    if (lo <= hi) {
+      sk.ask((lds_byte*)even, lo, hi + 1);
+      sv.ask((lds_byte*)odd, lo, hi + 1);
+    }
+  }
+  for (int j0 = lo; j0 <= hi; j0 += ROWS) {
+    if (j0 > lo) __syncthreads();
+    if constexpr (DIRECT) {
+      sk.ask((lds_byte*)even, j0, hi + 1);
+      sv.ask((lds_byte*)odd, j0, hi + 1);
+    }
+    sk.put((lds_byte*)even);
+    sv.put((lds_byte*)odd);
+    arrived();
+    if constexpr (!DIRECT) {
+      if (j0 + ROWS <= hi) {
+        sk.ask((lds_byte*)even, j0 + ROWS, hi + 1);
+        sv.ask((lds_byte*)odd, j0 + ROWS, hi + 1);
+      }
+    }
+    if (wave < kSharing<DTYPE> && j0 + wave * 32 <= hi) f((lds_byte*)even + wave * EACH, (lds_byte*)odd + wave * EACH, j0 + wave * 32);
+  }
+  __syncthreads();                                           // the arrays are free
 }
 
 // ---- sequences --------------------------------------------------------------------------------------

@@ -13,7 +13,8 @@
 namespace lsam {
 namespace {
 
-constexpr int kRowsOf = 128;               // rows of a workgroup
+// Rows of a workgroup: 32 a wavefront, or 32 that its wavefronts share.
+template <bool SHARED> constexpr int kRowsOf = SHARED ? 32 : 32 * kThreads / 64;
 
 struct Tensor { void* p; int64_t stride, head; };
 
@@ -71,6 +72,7 @@ __device__ __forceinline__ Range range_of(bool valid, int first, int last) {
 __device__ __forceinline__ bool any_of_workgroup(bool v) {
   __shared__ int shared[kThreads / 64];
   const bool mine = __any(v);
+  __syncthreads();                                           // an answer before has been read
   if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = mine;
   __syncthreads();
   bool all = false;
@@ -82,7 +84,7 @@ __device__ __forceinline__ bool any_of_workgroup(bool v) {
 template <int DTYPE>
 __device__ __forceinline__ typename Value<DTYPE>::T* head_of(const Tensor& t, int head) { return static_cast<typename Value<DTYPE>::T*>(t.p) + head * t.head; }
 
-template <int DTYPE, int DP, bool DIRECT>
+template <int DTYPE, int DP, bool DIRECT, bool SHARED>
 __global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void attention_kernel(AttentionParams p) {
   typedef typename Value<DTYPE>::T T;
   typedef Operand<DTYPE> O;
@@ -91,8 +93,8 @@ __global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void attention_kernel(At
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Work w = work(p.tiles, p.heads / p.group, p.group, true);
   if (!w.here) return;
-  const int head = w.kv * p.group + w.g, row0 = w.tile * kRowsOf + wave * 32, row = row0 + (lane & 31);
-  const int top = w.tile * kRowsOf, bottom = top + kRowsOf <= p.seq.rows ? top + kRowsOf - 1 : p.seq.rows - 1;
+  const int head = w.kv * p.group + w.g, row = w.tile * kRowsOf<SHARED> + (SHARED ? 0 : wave * 32) + (lane & 31);
+  const int top = w.tile * kRowsOf<SHARED>, bottom = top + kRowsOf<SHARED> <= p.seq.rows ? top + kRowsOf<SHARED> - 1 : p.seq.rows - 1;
   typename O::F q[STEPS];                                    // on its way while sequences are looked for
   const T* q_row = head_of<DTYPE>(p.q, head) + (row <= bottom ? row : bottom) * p.q.stride;
 #pragma unroll
@@ -111,20 +113,29 @@ __global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void attention_kernel(At
     a = Running<DP>();
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t) a.acc[t] = zero16();
-    walk<DTYPE, DP, DIRECT>((lds_byte*)even, (lds_byte*)odd, k, v, lo, hi, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0) {
-      if (j0 > r.hi || j0 + BN <= r.lo) return;
-      attend<DTYPE, DP, BN / 32, decltype(clean)::value>(a, read, q, tk, tv, c, lane, j0 < r.all_lo || j0 + BN - 1 > r.all_hi, first - j0, last - j0, found);
-    });
+    if constexpr (SHARED) {
+      walk_shared<DTYPE, DP, DIRECT>(even, odd, k, v, lo, hi, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0) {
+        if (j0 > r.hi || j0 + 32 <= r.lo) return;
+        attend<DTYPE, DP, 1, decltype(clean)::value>(a, read, q, tk, tv, c, lane, j0 < r.all_lo || j0 + 31 > r.all_hi, first - j0, last - j0, found);
+      });
+      join_running<DTYPE, DP>(a, c, wave, lane, even, odd);
+    } else {
+      walk<DTYPE, DP, DIRECT>((lds_byte*)even, (lds_byte*)odd, k, v, lo, hi, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0) {
+        if (j0 > r.hi || j0 + BN <= r.lo) return;
+        attend<DTYPE, DP, BN / 32, decltype(clean)::value>(a, read, q, tk, tv, c, lane, j0 < r.all_lo || j0 + BN - 1 > r.all_hi, first - j0, last - j0, found);
+      });
+      a.l += other_half(a.l);
+    }
   };
   pass(No());
-  if (any_of_workgroup(valid && not_finite(a.acc))) {        // by a value that is seen, or by one that is not: again, telling them apart
+  const bool mine = valid && (!SHARED || wave == 0);         // this wavefront has results
+  if (any_of_workgroup(mine && not_finite(a.acc))) {         // by a value that is seen, or by one that is not: again, telling them apart
     pass(Yes());
-    if (__any(found != 0)) add_what_is_seen<DTYPE, DP>(a.acc, v, r.lo, r.hi + 1, first, last, lane, p.dim);
+    if (any_of_workgroup(found != 0)) add_what_is_seen<DTYPE, DP>(a.acc, v, r.lo, r.hi + 1, first, last, lane, p.dim);
   }
-  if (!valid) return;
-  const float l = a.l + other_half(a.l);
-  store_column<DTYPE, DP>(a.acc, 1.f / l, head_of<DTYPE>(p.o, head) + row * p.o.stride, lane, p.dim);
-  if (p.lse && lane < 32) p.lse[(int64_t)head * p.seq.rows + row] = a.m * p.scale + __logf(l);
+  if (!mine) return;
+  store_column<DTYPE, DP>(a.acc, 1.f / a.l, head_of<DTYPE>(p.o, head) + row * p.o.stride, lane, p.dim);
+  if (p.lse && lane < 32) p.lse[(int64_t)head * p.seq.rows + row] = a.m * p.scale + __logf(a.l);
 }
 
 template <int DTYPE, int DP, int TILES, bool CLEAN>
@@ -147,11 +158,11 @@ __device__ __forceinline__ void dq_tile(f32x16 (&acc)[DP / 32], const Reader<DTY
       for (int e = 0; e < 16; ++e) s[e] = seen(i, e) ? s[e] : 0.f;
     }
 #pragma unroll
-    for (int t = 0; t < 2; ++t) multiply_across<DTYPE, DP, CLEAN>(acc, read, tk, i * 32 + t * 16, O::from(s, t), found);
+    for (int t = 0; t < 2; ++t) multiply_across<DTYPE, DP, CLEAN>(acc, read, tk, i * 32 + t * 16, O::from(s, t, false), found);
   }
 }
 
-template <int DTYPE, int DP, bool DIRECT>
+template <int DTYPE, int DP, bool DIRECT, bool SHARED>
 __global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void dq_kernel(AttentionParams p) {
   typedef typename Value<DTYPE>::T T;
   typedef Operand<DTYPE> O;
@@ -160,8 +171,8 @@ __global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void dq_kernel(Attention
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Work w = work(p.tiles, p.heads / p.group, p.group, true);
   if (!w.here) return;
-  const int head = w.kv * p.group + w.g, row0 = w.tile * kRowsOf + wave * 32, row = row0 + (lane & 31);
-  const int top = w.tile * kRowsOf, bottom = top + kRowsOf <= p.seq.rows ? top + kRowsOf - 1 : p.seq.rows - 1;
+  const int head = w.kv * p.group + w.g, row = w.tile * kRowsOf<SHARED> + (SHARED ? 0 : wave * 32) + (lane & 31);
+  const int top = w.tile * kRowsOf<SHARED>, bottom = top + kRowsOf<SHARED> <= p.seq.rows ? top + kRowsOf<SHARED> - 1 : p.seq.rows - 1;
   typename O::F q[STEPS], g[STEPS];                          // on their way while sequences are looked for
   const int at = row <= bottom ? row : bottom;
   const T* q_row = head_of<DTYPE>(p.q, head) + at * p.q.stride;
@@ -185,34 +196,44 @@ __global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void dq_kernel(Attention
   const int lo = span.top_begin, hi = bottom;
   const Reader<DTYPE, DP> read(lane);
   const float c = exponent(p.scale);
-  if (valid && lane < 32) p.stats[head * p.padded + row] = f32x2{base, dot};
+  if (valid && lane < 32 && (!SHARED || wave == 0)) p.stats[head * p.padded + row] = f32x2{base, dot};
   const HeadRows k{head_of<DTYPE>(p.k, w.kv), p.k.stride}, v{head_of<DTYPE>(p.v, w.kv), p.v.stride};
   unsigned found = 0;
   f32x16 acc[DP / 32];
   const auto pass = [&](auto clean) {
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t) acc[t] = zero16();
-    walk<DTYPE, DP, DIRECT>((lds_byte*)even, (lds_byte*)odd, k, v, lo, hi, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0) {
-      if (j0 > r.hi || j0 + BN <= r.lo) return;
-      dq_tile<DTYPE, DP, BN / 32, decltype(clean)::value>(acc, read, q, g, tk, tv, c, base, dot, lane, j0 < r.all_lo || j0 + BN - 1 > r.all_hi, first - j0,
-                                                          last - j0, found);
-    });
+    if constexpr (SHARED) {
+      walk_shared<DTYPE, DP, DIRECT>(even, odd, k, v, lo, hi, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0) {
+        if (j0 > r.hi || j0 + 32 <= r.lo) return;
+        dq_tile<DTYPE, DP, 1, decltype(clean)::value>(acc, read, q, g, tk, tv, c, base, dot, lane, j0 < r.all_lo || j0 + 31 > r.all_hi, first - j0, last - j0,
+                                                      found);
+      });
+      join_sums<DTYPE, DP>(acc, wave, lane, even, odd);
+    } else {
+      walk<DTYPE, DP, DIRECT>((lds_byte*)even, (lds_byte*)odd, k, v, lo, hi, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0) {
+        if (j0 > r.hi || j0 + BN <= r.lo) return;
+        dq_tile<DTYPE, DP, BN / 32, decltype(clean)::value>(acc, read, q, g, tk, tv, c, base, dot, lane, j0 < r.all_lo || j0 + BN - 1 > r.all_hi, first - j0,
+                                                            last - j0, found);
+      });
+    }
   };
   pass(No());
-  if (any_of_workgroup(valid && not_finite(acc))) {
+  const bool mine = valid && (!SHARED || wave == 0);
+  if (any_of_workgroup(mine && not_finite(acc))) {
     pass(Yes());
-    if (__any(found != 0)) add_what_is_seen<DTYPE, DP>(acc, k, r.lo, r.hi + 1, first, last, lane, p.dim);
+    if (any_of_workgroup(found != 0)) add_what_is_seen<DTYPE, DP>(acc, k, r.lo, r.hi + 1, first, last, lane, p.dim);
   }
-  if (valid) store_column<DTYPE, DP>(acc, p.scale, head_of<DTYPE>(p.dq, head) + row * p.dq.stride, lane, p.dim);
+  if (mine) store_column<DTYPE, DP>(acc, p.scale, head_of<DTYPE>(p.dq, head) + row * p.dq.stride, lane, p.dim);
 }
 
 // Rows of a tile of dkv_kernel, and its LDS: such tiles of q and d_o with lse and d_o o of their rows.
-constexpr int kSeenRows = 32;
-template <int DTYPE, int DP> constexpr int kSeenLds = 2 * kSeenRows * Rows<DTYPE, DP>::BYTES + 8 * kSeenRows;
+template <int DTYPE, bool SHARED> constexpr int kSeenRows = SHARED ? 32 * kSharing<DTYPE> : 32;
+template <int DTYPE, int DP, bool SHARED> constexpr int kSeenLds = kSeenRows<DTYPE, SHARED> * (2 * Rows<DTYPE, DP>::BYTES + 8);
 
 // What a wavefront of dkv_kernel has: its keys or where they are, its values, and the sums for them.
-template <int DTYPE, int DP> struct Keys {
-  static constexpr bool LDS = DTYPE == LSAM_DTYPE_BF16;      // three pieces of 128 keys have no room there, but one wavefront a SIMD has registers
+template <int DTYPE, int DP, bool IN_LDS> struct Keys {
+  static constexpr bool LDS = IN_LDS;
   const lds_byte* at;
   typename Operand<DTYPE>::F k[LDS ? 1 : DP / 16];
   typename Operand<DTYPE>::F v[DP / 16];
@@ -220,18 +241,16 @@ template <int DTYPE, int DP> struct Keys {
 };
 
 // A tile of rows: scores and d_o v; p and ds of them; dv and dk.
-template <int DTYPE, int DP, bool CLEAN>
-__device__ __forceinline__ void dkv_tile(Keys<DTYPE, DP>& w, const Reader<DTYPE, DP>& read, const lds_byte* tq, float c, int lane, bool masked, int first,
-                                         int last, unsigned& found) {
+template <int DTYPE, int DP, bool CLEAN, bool IN_LDS>
+__device__ __forceinline__ void dkv_tile(Keys<DTYPE, DP, IN_LDS>& w, const Reader<DTYPE, DP>& read, const lds_byte* tq, const lds_byte* tg,
+                                         const lds_byte* stats, float c, int lane, bool masked, int first, int last, unsigned& found) {
   typedef Operand<DTYPE> O;
   typedef typename O::F F;
   typedef const __attribute__((address_space(3))) f32x4* quad_ptr;
-  constexpr int T = DP / 32, BYTES = kSeenRows * Rows<DTYPE, DP>::BYTES;
-  const lds_byte* const tg = tq + BYTES;
-  const lds_byte* const stats = tg + BYTES;
+  constexpr int T = DP / 32;
   struct Both { F a, b; };
   f32x16 s = zero16(), d = zero16();
-  if constexpr (Keys<DTYPE, DP>::LDS)
+  if constexpr (IN_LDS)
     products<DP / 16, 2>([&](int n) { return Both{read.along(tq, 0, n), read.along(w.at, 0, n)}; }, [&](int n, const Both& f) { s = O::multiply(f.a, f.b, s); });
   else
     products<DP / 16, kAhead>([&](int n) { return read.along(tq, 0, n); }, [&](int n, const F& f) { s = O::multiply(f, w.k[n], s); });
@@ -256,7 +275,7 @@ __device__ __forceinline__ void dkv_tile(Keys<DTYPE, DP>& w, const Reader<DTYPE,
   }
   F weight[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) weight[i] = O::from(i & 1 ? d : s, i / 2);
+  for (int i = 0; i < 4; ++i) weight[i] = O::from(i & 1 ? d : s, i / 2, !(i & 1));
   // dv then dk of rows 0 .. 15, dv then dk of rows 16 .. 31
   products<4 * T, kAhead>([&](int n) { return read.across(n / T & 1 ? tq : tg, n / (2 * T) * 16, n % T); },
                           [&](int n, const F& f) {
@@ -265,26 +284,26 @@ __device__ __forceinline__ void dkv_tile(Keys<DTYPE, DP>& w, const Reader<DTYPE,
                           });
 }
 
-// A tile's lse and d_o o to LDS.
+// ROWS rows' lse and d_o o to LDS, 32 rows a wavefront.
+template <int ROWS>
 __device__ __forceinline__ void ask_stats(lds_byte* to, const AttentionParams& p, int head, int row0, int wave) {
-  static_assert(kSeenRows * 8 == 64 * 4, "four bytes a lane");
-  if (wave != 0) return;
-  const unsigned long long a = reinterpret_cast<unsigned long long>(p.stats + head * p.padded + row0);
+  if (wave >= ROWS / 32) return;
+  const unsigned long long a = reinterpret_cast<unsigned long long>(p.stats + head * p.padded + row0 + wave * 32);
   const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)a), hi = __builtin_amdgcn_readfirstlane((unsigned)(a >> 32));
-  const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((unsigned long long)hi << 32 | lo), 0, 8 * kSeenRows, 0x00020000);
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 4, (threadIdx.x & 63) * 4, 0, 0, 0);
+  const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((unsigned long long)hi << 32 | lo), 0, 256, 0x00020000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(to + wave * 256), 4, (threadIdx.x & 63) * 4, 0, 0, 0);
 }
 
 // A tile of q, d_o and what goes with their rows.
-template <int DTYPE, int DP, bool DIRECT> struct SeenStage {
-  static constexpr int BYTES = kSeenRows * Rows<DTYPE, DP>::BYTES;
-  Stage<DTYPE, DP, kSeenRows, kThreads, DIRECT> q, g;
+template <int DTYPE, int DP, bool DIRECT, int ROWS> struct SeenStage {
+  static constexpr int BYTES = ROWS * Rows<DTYPE, DP>::BYTES;
+  Stage<DTYPE, DP, ROWS, kThreads, DIRECT> q, g;
   __device__ __forceinline__ void ask(lds_byte* to, const AttentionParams& p, int head, int row0, int limit, int wave) {
     q.p = head_of<DTYPE>(p.q, head);
     g.p = head_of<DTYPE>(p.d_o, head);
     q.ask(to, row0, limit);
     g.ask(to + BYTES, row0, limit);
-    ask_stats(to + 2 * BYTES, p, head, row0, wave);
+    ask_stats<ROWS>(to + 2 * BYTES, p, head, row0, wave);
   }
   __device__ __forceinline__ void put(lds_byte* to) const {
     q.put(to);
@@ -292,23 +311,26 @@ template <int DTYPE, int DP, bool DIRECT> struct SeenStage {
   }
 };
 
-template <int DTYPE, int DP, bool DIRECT>
+template <int DTYPE, int DP, bool DIRECT, bool SHARED>
 __device__ __forceinline__ void dkv(const AttentionParams& p) {
   typedef typename Value<DTYPE>::T T;
-  constexpr int BN = kSeenRows, STEPS = DP / 16;
-  __shared__ __attribute__((aligned(1024))) unsigned char even[kSeenLds<DTYPE, DP>], odd[kSeenLds<DTYPE, DP>], own[Keys<DTYPE, DP>::LDS ? kRowsOf * Rows<DTYPE, DP>::BYTES : 16];
+  // keys in LDS where registers are short; three pieces of 128 have no room there, but one wavefront a SIMD has registers
+  constexpr bool IN_LDS = DTYPE == LSAM_DTYPE_BF16 && !SHARED;
+  constexpr int BN = kSeenRows<DTYPE, SHARED>, STEPS = DP / 16, BYTES = BN * Rows<DTYPE, DP>::BYTES, EACH = 32 * Rows<DTYPE, DP>::BYTES;
+  constexpr int LDS = kSeenLds<DTYPE, DP, SHARED>;
+  __shared__ __attribute__((aligned(1024))) unsigned char even[LDS], odd[SHARED ? 16 : LDS], own[IN_LDS ? kRowsOf<SHARED> * Rows<DTYPE, DP>::BYTES : 16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Work w = work(p.tiles, p.heads / p.group, 1, false);
   if (!w.here) return;
-  const int row0 = w.tile * kRowsOf + wave * 32, row = row0 + (lane & 31);
-  const int top = w.tile * kRowsOf, bottom = top + kRowsOf <= p.seq.rows ? top + kRowsOf - 1 : p.seq.rows - 1;
-  Keys<DTYPE, DP> keys;
-  if constexpr (Keys<DTYPE, DP>::LDS) {
-    Stage<DTYPE, DP, kRowsOf, kThreads, DIRECT> sk;
+  const int row = w.tile * kRowsOf<SHARED> + (SHARED ? 0 : wave * 32) + (lane & 31);
+  const int top = w.tile * kRowsOf<SHARED>, bottom = top + kRowsOf<SHARED> <= p.seq.rows ? top + kRowsOf<SHARED> - 1 : p.seq.rows - 1;
+  Keys<DTYPE, DP, IN_LDS> keys;
+  if constexpr (IN_LDS) {
+    Stage<DTYPE, DP, kRowsOf<SHARED>, kThreads, DIRECT> sk;
     sk.init(HeadRows{head_of<DTYPE>(p.k, w.kv), p.k.stride}, p.dim);
     sk.ask((lds_byte*)own, top, p.seq.rows);
     sk.put((lds_byte*)own);
-    keys.at = (lds_byte*)own + wave * 32 * Rows<DTYPE, DP>::BYTES;
+    keys.at = (lds_byte*)own + wave * EACH;
   } else {
     const T* k_row = head_of<DTYPE>(p.k, w.kv) + (row <= bottom ? row : bottom) * p.k.stride;
 #pragma unroll
@@ -324,7 +346,7 @@ __device__ __forceinline__ void dkv(const AttentionParams& p) {
   const int lo = top, hi = span.bottom_end - 1;
   const Reader<DTYPE, DP> read(lane);
   const float c = exponent(p.scale);
-  SeenStage<DTYPE, DP, DIRECT> stage;
+  SeenStage<DTYPE, DP, DIRECT, BN> stage;
   const int head0 = w.kv * p.group, behind = head0 + p.group;
   stage.q.init(HeadRows{head_of<DTYPE>(p.q, head0), p.q.stride}, p.dim);
   stage.g.init(HeadRows{head_of<DTYPE>(p.d_o, head0), p.d_o.stride}, p.dim);
@@ -336,37 +358,50 @@ __device__ __forceinline__ void dkv(const AttentionParams& p) {
     stage.ask((lds_byte*)even, p, head, lo, hi + 1, wave);
     for (int i0 = lo; head < behind;) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+      for (int b = 0; b < (SHARED ? 1 : 2); ++b) {
         lds_byte* const tq = (lds_byte*)(b ? odd : even);
         stage.put(tq);
         arrived();
-        const int now = i0;
+        const int mine = SHARED ? wave : 0, now = i0 + mine * 32;
         i0 += BN;
         if (i0 > hi) { i0 = lo; ++head; }
-        if (head < behind) stage.ask((lds_byte*)(b ? even : odd), p, head, i0, hi + 1, wave);
-        if (now <= r.hi && now + BN > r.lo)
-          dkv_tile<DTYPE, DP, decltype(clean)::value>(keys, read, tq, c, lane, now < r.all_lo || now + BN - 1 > r.all_hi, first - now, last - now, found);
+        if (!SHARED && head < behind) stage.ask((lds_byte*)(b ? even : odd), p, head, i0, hi + 1, wave);
+        if (mine < BN / 32 && now <= r.hi && now + 32 > r.lo)
+          dkv_tile<DTYPE, DP, decltype(clean)::value, IN_LDS>(keys, read, tq + mine * EACH, tq + BYTES + mine * EACH, tq + 2 * BYTES + mine * 256, c, lane,
+                                                              now < r.all_lo || now + 31 > r.all_hi, first - now, last - now, found);
+        if constexpr (SHARED) {                              // one tile at a time
+          __syncthreads();
+          if (head < behind) stage.ask(tq, p, head, i0, hi + 1, wave);
+        }
         if (head == behind) break;
       }
     }
+    if constexpr (SHARED) {
+      static_assert(LDS >= 3 * DP * 32 * 4 || kSharing<DTYPE> == 2, "sums of three wavefronts");
+      join_sums<DTYPE, DP>(keys.dv, wave, lane, even, even + 2 * DP * 32 * 4);
+      __syncthreads();
+      join_sums<DTYPE, DP>(keys.dk, wave, lane, even, even + 2 * DP * 32 * 4);
+      __syncthreads();
+    }
   };
   pass(No());
-  if (any_of_workgroup(valid && (not_finite(keys.dk) || not_finite(keys.dv)))) {
+  const bool mine = valid && (!SHARED || wave == 0);
+  if (any_of_workgroup(mine && (not_finite(keys.dk) || not_finite(keys.dv)))) {
     pass(Yes());
-    if (__any(found != 0)) {
+    if (any_of_workgroup(found != 0)) {
       for (int head = head0; head < behind; ++head) {
         add_what_is_seen<DTYPE, DP>(keys.dk, HeadRows{head_of<DTYPE>(p.q, head), p.q.stride}, r.lo, r.hi + 1, first, last, lane, p.dim);
         add_what_is_seen<DTYPE, DP>(keys.dv, HeadRows{head_of<DTYPE>(p.d_o, head), p.d_o.stride}, r.lo, r.hi + 1, first, last, lane, p.dim);
       }
     }
   }
-  if (!valid) return;
+  if (!mine) return;
   store_column<DTYPE, DP>(keys.dk, p.scale, head_of<DTYPE>(p.dk, w.kv) + row * p.dk.stride, lane, p.dim);
   store_column<DTYPE, DP>(keys.dv, 1.f, head_of<DTYPE>(p.dv, w.kv) + row * p.dv.stride, lane, p.dim);
 }
 
-template <int DTYPE, int DP, bool DIRECT>
-__global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void dkv_kernel(AttentionParams p) { dkv<DTYPE, DP, DIRECT>(p); }
+template <int DTYPE, int DP, bool DIRECT, bool SHARED>
+__global__ __launch_bounds__(kThreads, SHARED ? 1 : kWavesOf<DTYPE>) void dkv_kernel(AttentionParams p) { dkv<DTYPE, DP, DIRECT, SHARED>(p); }
 
 int check(const lsam_attention_desc* d, const char* who) {
   if (!d) return refuse(LSAM_EINVAL, "%s: the descriptor is NULL", who);
@@ -396,20 +431,29 @@ AttentionParams params(const lsam_attention_desc* d, const int64_t* offsets) {
   AttentionParams p{};
   p.seq = Sequences{offsets, (int)d->seqs, (int)d->rows};
   p.heads = d->heads; p.group = d->heads / d->kv_heads; p.dim = d->dim; p.scale = d->scale;
-  p.tiles = (int)((d->rows + kRowsOf - 1) / kRowsOf);
-  p.padded = (d->rows + 127) / 64 * 64;
+  p.padded = (d->rows + 191) / 64 * 64;
   return p;
 }
 
+// Wavefronts share rows where workgroups of 128 rows would leave units without work.
+constexpr int kUnits = 256;
 template <int DTYPE, int DP, bool DIRECT>
-int launch(const AttentionParams& p, bool backward, hipStream_t s) {
-  const unsigned all = workgroups(p.tiles, p.heads / p.group, p.group), of_keys = workgroups(p.tiles, p.heads / p.group, 1);
-  if (backward) {
-    dq_kernel<DTYPE, DP, DIRECT><<<all, kThreads, 0, s>>>(p);
-    dkv_kernel<DTYPE, DP, DIRECT><<<of_keys, kThreads, 0, s>>>(p);
-  } else {
-    attention_kernel<DTYPE, DP, DIRECT><<<all, kThreads, 0, s>>>(p);
+int launch(AttentionParams p, bool backward, hipStream_t s) {
+  const int rows = p.seq.rows, kv = p.heads / p.group, wide = (rows + kRowsOf<false> - 1) / kRowsOf<false>, narrow = (rows + kRowsOf<true> - 1) / kRowsOf<true>;
+  const bool share = (int64_t)wide * p.heads < kUnits, share_keys = (int64_t)wide * kv < kUnits;
+  p.tiles = share ? narrow : wide;
+  const unsigned all = workgroups(p.tiles, kv, p.group);
+  if (!backward) {
+    if (share) attention_kernel<DTYPE, DP, DIRECT, true><<<all, kThreads, 0, s>>>(p);
+    else attention_kernel<DTYPE, DP, DIRECT, false><<<all, kThreads, 0, s>>>(p);
+    return launched();
   }
+  if (share) dq_kernel<DTYPE, DP, DIRECT, true><<<all, kThreads, 0, s>>>(p);
+  else dq_kernel<DTYPE, DP, DIRECT, false><<<all, kThreads, 0, s>>>(p);
+  p.tiles = share_keys ? narrow : wide;
+  const unsigned of_keys = workgroups(p.tiles, kv, 1);
+  if (share_keys) dkv_kernel<DTYPE, DP, DIRECT, true><<<of_keys, kThreads, 0, s>>>(p);
+  else dkv_kernel<DTYPE, DP, DIRECT, false><<<of_keys, kThreads, 0, s>>>(p);
   return launched();
 }
 template <int DTYPE, bool DIRECT>

@@ -34,10 +34,9 @@ template <int DTYPE, int DP, bool DIRECT>
 __global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void step_kernel(StepParams p) {
   typedef typename Value<DTYPE>::T T;
   typedef Operand<DTYPE> O;
-  constexpr int STEPS = DP / 16, BN = kTile<DTYPE>, WAVES = 2 * BN / 32, BLOCK = DP * 32 * 4;
-  static_assert(kKeys % (2 * BN) == 0 && 2 * BLOCK <= kLds<DTYPE, DP>, "whole tiles; the sums of two wavefronts have room");
+  constexpr int STEPS = DP / 16, BN = kTile<DTYPE>;
+  static_assert(kKeys % (2 * BN) == 0, "whole tiles");
   __shared__ __attribute__((aligned(1024))) unsigned char even[kLds<DTYPE, DP>], odd[kLds<DTYPE, DP>];
-  __shared__ float of_waves[2][WAVES][32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
   // what this workgroup does: a part of the prefix for some columns, or a part of a cache
@@ -94,55 +93,12 @@ __global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void step_kernel(StepPar
     });
     l = a.l + other_half(a.l);
   } else {
-    // one tile of keys and one of values; two workgroups of a unit take turns
-    lds_byte* const tk = (lds_byte*)even;
-    lds_byte* const tv = (lds_byte*)odd;
-    Stage<DTYPE, DP, 2 * BN, kThreads, DIRECT> sk, sv;
-    sk.init(k, p.dim);
-    sv.init(v, p.dim);
-    for (int j0 = from; j0 < to; j0 += 2 * BN) {
-      if (j0 > from) __syncthreads();
-      sk.ask(tk, j0, to);
-      sv.ask(tv, j0, to);
-      sk.put(tk);
-      sv.put(tv);
-      arrived();
-      const int left = to - j0 - wave * 32;                  // keys of this wavefront
-      if (wave < WAVES && left > 0)
-        attend<DTYPE, DP, 1, false>(a, read, q, tk + wave * 32 * Rows<DTYPE, DP>::BYTES, tv + wave * 32 * Rows<DTYPE, DP>::BYTES, scale, lane, left < 32, 0,
-                                    left - 1, found);
-    }
-    // the wavefronts' keys together: each column's maximum, then wavefront by wavefront
-    l = a.l + other_half(a.l);
-    if (lane < 32 && wave < WAVES) of_waves[0][wave][lane] = a.m;
-    __syncthreads();
-    float most = of_waves[0][0][lane & 31];
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) most = __builtin_fmaxf(most, of_waves[0][w][lane & 31]);
-    const float base = most == -__builtin_inff() ? 0.f : most * scale, less = a.m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(a.base - base);
-    if (lane < 32 && wave < WAVES) of_waves[1][wave][lane] = l * less;
-    a.m = most;
-    const auto block = [&](int w) { return reinterpret_cast<float*>(w <= 2 ? even + (w - 1) * BLOCK : odd); };
-    if (wave > 0 && wave < WAVES) {
-#pragma unroll
-      for (int t = 0; t < DP / 32; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) block(wave)[(t * 16 + r) * 64 + lane] = a.acc[t][r] * less;
-    }
-    __syncthreads();
+    walk_shared<DTYPE, DP, DIRECT>(even, odd, k, v, from, to - 1, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0) {
+      attend<DTYPE, DP, 1, false>(a, read, q, tk, tv, scale, lane, j0 + 32 > to, 0, to - 1 - j0, found);
+    });
+    join_running<DTYPE, DP>(a, scale, wave, lane, even, odd);
     if (wave > 0) return;
-    l = 0.f;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) l += of_waves[1][w][lane & 31];
-#pragma unroll
-    for (int t = 0; t < DP / 32; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        a.acc[t][r] *= less;
-#pragma unroll
-        for (int w = 1; w < WAVES; ++w) a.acc[t][r] += block(w)[(t * 16 + r) * 64 + lane];
-      }
-    a.base = base;
+    l = a.l;
   }
   if (!valid) return;
   if (p.whole) {

@@ -53,7 +53,7 @@ def check_gradient(d, tokens, dy, scale):
 
 
 SIZES = [(1, 1, 1, 1), (1, 63, 5, 3), (2, 64, 7, 4), (1, 65, 1000, 257), (3, 1000, 13, 33), (1, 5000, 2, 8), (2, 3000, 3000, 256),
-         (1, 700, 200001, 5), (2, 129, 600, 260), (5, 200, 1, 1030)]
+         (1, 700, 200001, 5), (2, 129, 600, 260), (5, 200, 1, 1030), (1, 20001, 300, 3), (2, 33000, 1500, 6)]   # the last two: places in parts
 
 
 @pytest.mark.parametrize("K,rows,V,D", SIZES)
