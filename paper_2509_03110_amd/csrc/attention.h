@@ -21,7 +21,9 @@ template <int DTYPE> struct Operand;
 template <> struct Operand<LSAM_DTYPE_BF16> {
   typedef bf16x8 F;
   static constexpr int PLANES = 1;
-  static __device__ __forceinline__ f32x16 multiply(F a, F b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  static constexpr int PRODUCTS = 1;
+  // Product i of PRODUCTS that make a b.
+  static __device__ __forceinline__ f32x16 multiply(int, const F& a, const F& b, const f32x16& c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
   // Results 8 t .. of a product as an operand of the next; `weights`: none is above 2^9.
   static __device__ __forceinline__ F from(const f32x16& s, int t, bool weights) {
     F f;
@@ -49,13 +51,10 @@ template <> struct Operand<LSAM_DTYPE_FP32> {
   typedef Operand<LSAM_DTYPE_BF16> One;
   struct F { bf16x8 p[3]; };
   static constexpr int PLANES = 3;
-  static __device__ __forceinline__ f32x16 multiply(const F& a, const F& b, f32x16 c) {
-    c = One::multiply(a.p[2], b.p[0], c);
-    c = One::multiply(a.p[1], b.p[1], c);
-    c = One::multiply(a.p[0], b.p[2], c);
-    c = One::multiply(a.p[1], b.p[0], c);
-    c = One::multiply(a.p[0], b.p[1], c);
-    return One::multiply(a.p[0], b.p[0], c);
+  static constexpr int PRODUCTS = 6;
+  static __device__ __forceinline__ f32x16 multiply(int i, const F& a, const F& b, const f32x16& c) {
+    constexpr int left[6] = {2, 1, 0, 1, 0, 0}, right[6] = {0, 1, 2, 0, 1, 0};
+    return One::multiply(0, a.p[left[i]], b.p[right[i]], c);
   }
   static __device__ __forceinline__ F split(const float (&v)[8], bool weights) {
     unsigned w[3][4];
@@ -173,19 +172,27 @@ __device__ __forceinline__ typename Unit<DTYPE>::T load_part(const typename Valu
   return load_unit<DTYPE>(row, step * 2 + (lane >> 5), dim);
 }
 
-// A workgroup's way of bringing ROWS rows into LDS; rows from `limit` on count as 0.  bf16 rows that are aligned to 16 bytes (DIRECT) go there
-// without passing through registers: asked for a tile ahead, there when the wavefront has waited for its loads.  Others
-// are asked for a tile ahead as well, and put there when they are needed.
+// The bytes behind p, the same in all lanes.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const void* p, unsigned bytes) {
+  const unsigned long long a = reinterpret_cast<unsigned long long>(p);
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)a), hi = __builtin_amdgcn_readfirstlane((unsigned)(a >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((unsigned long long)hi << 32 | lo), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+}
+
+// A workgroup's way of bringing ROWS rows into LDS; rows from `limit` on count as 0.  Whole units of eight numbers (DIRECT): bf16 rows go there
+// without passing through registers, asked for a tile ahead, there when the wavefront has waited for its loads; fp32 rows pass through them, where
+// they are cut into pieces, but no load waits for another and none is in a branch.  Other rows are looked at number by number.
 template <int DTYPE, int DP, int ROWS, int THREADS, bool DIRECT>
 struct Stage {
   typedef typename Value<DTYPE>::T T;
   typedef Rows<DTYPE, DP> R;
-  static constexpr int N = ROWS * R::U / THREADS, PLANES = Operand<DTYPE>::PLANES;
-  static_assert(N * THREADS == ROWS * R::U && !(DIRECT && PLANES > 1), "whole rounds of loads; pieces pass through registers");
+  static constexpr int N = ROWS * R::U / THREADS, PLANES = Operand<DTYPE>::PLANES, B = sizeof(T);
+  static constexpr bool THROUGH = !DIRECT || PLANES > 1;     // registers
+  static_assert(N * THREADS == ROWS * R::U, "whole rounds of loads");
   const T* p;
   int64_t stride;
   int dim;
-  typename Unit<DTYPE>::T w[DIRECT ? 1 : N];
+  typename Unit<DTYPE>::T w[THROUGH ? N : 1];
   unsigned at[DIRECT ? N : 1];
   __device__ __forceinline__ void init(const HeadRows& t, int d) {
     p = static_cast<const T*>(t.p);
@@ -194,23 +201,25 @@ struct Stage {
     if constexpr (DIRECT) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int n = threadIdx.x + i * THREADS, row = n / R::U, unit = (n % R::U) ^ R::turn(row);
-        at[i] = unit * 8 < dim ? (unsigned)(row * stride * 2) + unit * 16 : 0x7FFFFFF0u;
+        const int n = threadIdx.x + i * THREADS, row = n / R::U, unit = THROUGH ? n % R::U : (n % R::U) ^ R::turn(row);
+        at[i] = unit * 8 < dim ? (unsigned)(row * stride * B) + unit * 8 * B : 0x7FFFFFC0u;
       }
     }
   }
   __device__ __forceinline__ void ask(lds_byte* tile, int64_t row0, int64_t limit) {
     if constexpr (DIRECT) {
       const int64_t rows = limit - row0 < ROWS ? limit - row0 : ROWS;
-      const unsigned bytes = rows > 0 ? (unsigned)(((rows - 1) * stride + dim) * 2) : 0;
-      const unsigned long long a = reinterpret_cast<unsigned long long>(p + row0 * stride);
-      const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)a), hi = __builtin_amdgcn_readfirstlane((unsigned)(a >> 32));
-      const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((unsigned long long)hi << 32 | lo), 0,
-                                                                            __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+      const __amdgpu_buffer_rsrc_t from = resource(p + row0 * stride, rows > 0 ? (unsigned)(((rows - 1) * stride + dim) * B) : 0);
       const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(tile + (wave * 64 + i * THREADS) * 16), 16, at[i], 0, 0, 0);
+      for (int i = 0; i < N; ++i) {
+        if constexpr (THROUGH) {
+          const u32x4 a = __builtin_amdgcn_raw_buffer_load_b128(from, at[i], 0, 0), b = __builtin_amdgcn_raw_buffer_load_b128(from, at[i] + 16, 0, 0);
+          w[i] = __builtin_bit_cast(typename Unit<DTYPE>::T, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(tile + (wave * 64 + i * THREADS) * 16), 16, at[i], 0, 0, 0);
+        }
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
@@ -222,7 +231,7 @@ struct Stage {
     }
   }
   __device__ __forceinline__ void put(lds_byte* tile) const {
-    if constexpr (!DIRECT) {
+    if constexpr (THROUGH) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int n = threadIdx.x + i * THREADS;
@@ -242,9 +251,10 @@ __device__ __forceinline__ void arrived() {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
-// Whether rows can go to LDS directly: 16-byte units all the way, and a tile within 32-bit offsets.
+// Whether rows are whole units, and a tile within 32-bit offsets; bf16 ones have to be aligned to go to LDS directly.
 inline bool direct(const void* p, int64_t stride, int64_t head, int64_t seq, int dim, int dtype) {
-  return dtype == LSAM_DTYPE_BF16 && !misaligned(p, 16) && stride % 8 == 0 && head % 8 == 0 && seq % 8 == 0 && dim % 8 == 0 && stride < 1 << 20;
+  if (dim % 8 || stride >= 1 << 20) return false;
+  return dtype == LSAM_DTYPE_FP32 || (!misaligned(p, 16) && stride % 8 == 0 && head % 8 == 0 && seq % 8 == 0);
 }
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -259,6 +269,16 @@ __device__ __forceinline__ f32x16 zero16() {
 }
 // The row of a lane's result r.
 __device__ __forceinline__ int result_row(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
+
+// Several products at once: none waits for the one before it.
+template <int DTYPE, int N> struct Few { typename Operand<DTYPE>::F f[N]; };
+template <int DTYPE, int N, typename To, typename With>
+__device__ __forceinline__ void multiply_few(const Few<DTYPE, N>& a, With with, To to) {
+#pragma unroll
+  for (int i = 0; i < Operand<DTYPE>::PRODUCTS; ++i)
+#pragma unroll
+    for (int n = 0; n < N; ++n) to(n) = Operand<DTYPE>::multiply(i, a.f[n], with(n), to(n));
+}
 
 // N products whose operand from LDS is asked for AHEAD products before: a wavefront's registers do not hold more than that of
 // them, and vector arithmetic may move in between.  `beside(n)` is work of the vector units for the time that product n takes.
@@ -285,8 +305,18 @@ template <int DTYPE, int DP, bool CLEAN>
 __device__ __forceinline__ void multiply_across(f32x16 (&acc)[DP / 32], const Reader<DTYPE, DP>& read, const lds_byte* tile, int row0,
                                                 typename Operand<DTYPE>::F p, unsigned& found) {
   typedef Operand<DTYPE> O;
-  products<DP / 32, kAhead>([&](int t) { return read.across(tile, row0, t); },
-                            [&](int t, const typename O::F& a) { acc[t] = O::multiply(CLEAN ? O::clean(a, found) : a, p, acc[t]); });
+  if constexpr (O::PRODUCTS == 1) {
+    products<DP / 32, kAhead>([&](int t) { return read.across(tile, row0, t); },
+                              [&](int t, const typename O::F& a) { acc[t] = O::multiply(0, CLEAN ? O::clean(a, found) : a, p, acc[t]); });
+  } else {
+    Few<DTYPE, DP / 32> a;
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t) {
+      a.f[t] = read.across(tile, row0, t);
+      if constexpr (CLEAN) a.f[t] = O::clean(a.f[t], found);
+    }
+    multiply_few<DTYPE, DP / 32>(a, [&](int) -> const typename O::F& { return p; }, [&](int t) -> f32x16& { return acc[t]; });
+  }
 }
 // Whether a lane's sums hold what is not finite.
 template <int N>
@@ -411,10 +441,18 @@ __device__ __forceinline__ void attend(Running<DP>& a, const Reader<DTYPE, DP>& 
   typedef Operand<DTYPE> O;
   constexpr int STEPS = DP / 16;
   f32x16 s[TILES];
-#pragma unroll
-  for (int i = 0; i < TILES; ++i) s[i] = zero16();
-  products<TILES * STEPS, kAhead>([&](int n) { return read.along(tk, n / STEPS * 32, n % STEPS); },
-                                  [&](int n, const typename O::F& k) { s[n / STEPS] = O::multiply(k, q[n % STEPS], s[n / STEPS]); });
+  {
+    // two sums in turn: of two tiles, or of every other step of one
+    f32x16 two[2] = {zero16(), zero16()};
+    products<TILES * STEPS / 2, 2>([&](int n) { return Few<DTYPE, 2>{TILES == 2 ? read.along(tk, 0, n) : read.along(tk, 0, 2 * n), TILES == 2 ? read.along(tk, 32, n) : read.along(tk, 0, 2 * n + 1)}; },
+                                   [&](int n, const Few<DTYPE, 2>& k) {
+                                     multiply_few<DTYPE, 2>(k, [&](int i) -> const typename O::F& { return q[TILES == 2 ? n : 2 * n + i]; },
+                                                            [&](int i) -> f32x16& { return two[i]; });
+                                   });
+    static_assert(TILES == 1 || TILES == 2, "");
+    s[0] = TILES == 2 ? two[0] : two[0] + two[1];
+    if constexpr (TILES == 2) s[1] = two[1];
+  }
   if (masked) {
     const Seen seen(first, last, lane);
 #pragma unroll
@@ -506,27 +544,13 @@ __device__ __forceinline__ void walk_shared(unsigned char* even, unsigned char* 
   Stage<DTYPE, DP, ROWS, kThreads, DIRECT> sk, sv;
   sk.init(k, dim);
   sv.init(v, dim);
-  if constexpr (!DIRECT) {
-    if (lo <= hi) {
-      sk.ask((lds_byte*)even, lo, hi + 1);
-      sv.ask((lds_byte*)odd, lo, hi + 1);
-    }
-  }
   for (int j0 = lo; j0 <= hi; j0 += ROWS) {
     if (j0 > lo) __syncthreads();
-    if constexpr (DIRECT) {
-      sk.ask((lds_byte*)even, j0, hi + 1);
-      sv.ask((lds_byte*)odd, j0, hi + 1);
-    }
+    sk.ask((lds_byte*)even, j0, hi + 1);
+    sv.ask((lds_byte*)odd, j0, hi + 1);
     sk.put((lds_byte*)even);
     sv.put((lds_byte*)odd);
     arrived();
-    if constexpr (!DIRECT) {
-      if (j0 + ROWS <= hi) {
-        sk.ask((lds_byte*)even, j0 + ROWS, hi + 1);
-        sv.ask((lds_byte*)odd, j0 + ROWS, hi + 1);
-      }
-    }
     if (wave < kSharing<DTYPE> && j0 + wave * 32 <= hi) f((lds_byte*)even + wave * EACH, (lds_byte*)odd + wave * EACH, j0 + wave * 32);
   }
   __syncthreads();                                           // the arrays are free

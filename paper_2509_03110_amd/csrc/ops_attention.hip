@@ -146,10 +146,10 @@ __device__ __forceinline__ void dq_tile(f32x16 (&acc)[DP / 32], const Reader<DTY
 #pragma unroll
   for (int i = 0; i < TILES; ++i) {
     f32x16 s = zero16(), d = zero16();
-    products<DP / 8, kAhead>([&](int n) { return read.along(n & 1 ? tv : tk, i * 32, n / 2); },
-                             [&](int n, const typename O::F& a) {
-                               if (n & 1) d = O::multiply(a, g[n / 2], d); else s = O::multiply(a, q[n / 2], s);
-                             });
+    products<DP / 16, 2>([&](int n) { return Few<DTYPE, 2>{read.along(tk, i * 32, n), read.along(tv, i * 32, n)}; },
+                         [&](int n, const Few<DTYPE, 2>& a) {
+                           multiply_few<DTYPE, 2>(a, [&](int j) -> const typename O::F& { return j ? g[n] : q[n]; }, [&](int j) -> f32x16& { return j ? d : s; });
+                         });
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(s[e] * c - base) * (d[e] - dot);
     if (masked) {
@@ -248,13 +248,18 @@ __device__ __forceinline__ void dkv_tile(Keys<DTYPE, DP, IN_LDS>& w, const Reade
   typedef typename O::F F;
   typedef const __attribute__((address_space(3))) f32x4* quad_ptr;
   constexpr int T = DP / 32;
-  struct Both { F a, b; };
   f32x16 s = zero16(), d = zero16();
   if constexpr (IN_LDS)
-    products<DP / 16, 2>([&](int n) { return Both{read.along(tq, 0, n), read.along(w.at, 0, n)}; }, [&](int n, const Both& f) { s = O::multiply(f.a, f.b, s); });
+    products<DP / 16, 2>([&](int n) { return Few<DTYPE, 3>{read.along(tq, 0, n), read.along(tg, 0, n), read.along(w.at, 0, n)}; },
+                         [&](int n, const Few<DTYPE, 3>& a) {
+                           s = O::multiply(0, a.f[0], a.f[2], s);
+                           d = O::multiply(0, a.f[1], w.v[n], d);
+                         });
   else
-    products<DP / 16, kAhead>([&](int n) { return read.along(tq, 0, n); }, [&](int n, const F& f) { s = O::multiply(f, w.k[n], s); });
-  products<DP / 16, kAhead>([&](int n) { return read.along(tg, 0, n); }, [&](int n, const F& f) { d = O::multiply(f, w.v[n], d); });
+    products<DP / 16, 2>([&](int n) { return Few<DTYPE, 2>{read.along(tq, 0, n), read.along(tg, 0, n)}; },
+                         [&](int n, const Few<DTYPE, 2>& a) {
+                           multiply_few<DTYPE, 2>(a, [&](int j) -> const F& { return j ? w.v[n] : w.k[n]; }, [&](int j) -> f32x16& { return j ? d : s; });
+                         });
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
     const lds_byte* const at = stats + (8 * g + 4 * (lane >> 5)) * 8;
@@ -277,20 +282,23 @@ __device__ __forceinline__ void dkv_tile(Keys<DTYPE, DP, IN_LDS>& w, const Reade
 #pragma unroll
   for (int i = 0; i < 4; ++i) weight[i] = O::from(i & 1 ? d : s, i / 2, !(i & 1));
   // dv then dk of rows 0 .. 15, dv then dk of rows 16 .. 31
-  products<4 * T, kAhead>([&](int n) { return read.across(n / T & 1 ? tq : tg, n / (2 * T) * 16, n % T); },
-                          [&](int n, const F& f) {
-                            f32x16& to = n / T & 1 ? w.dk[n % T] : w.dv[n % T];
-                            to = O::multiply(CLEAN ? O::clean(f, found) : f, weight[n / T], to);
-                          });
+  if constexpr (O::PRODUCTS == 1) {
+    products<4 * T, kAhead>([&](int n) { return read.across(n / T & 1 ? tq : tg, n / (2 * T) * 16, n % T); },
+                            [&](int n, const F& f) {
+                              f32x16& to = n / T & 1 ? w.dk[n % T] : w.dv[n % T];
+                              to = O::multiply(0, CLEAN ? O::clean(f, found) : f, weight[n / T], to);
+                            });
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) multiply_across<DTYPE, DP, CLEAN>(i & 1 ? w.dk : w.dv, read, i & 1 ? tq : tg, i / 2 * 16, weight[i], found);
+  }
 }
 
 // ROWS rows' lse and d_o o to LDS, 32 rows a wavefront.
 template <int ROWS>
 __device__ __forceinline__ void ask_stats(lds_byte* to, const AttentionParams& p, int head, int row0, int wave) {
   if (wave >= ROWS / 32) return;
-  const unsigned long long a = reinterpret_cast<unsigned long long>(p.stats + head * p.padded + row0 + wave * 32);
-  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)a), hi = __builtin_amdgcn_readfirstlane((unsigned)(a >> 32));
-  const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((unsigned long long)hi << 32 | lo), 0, 256, 0x00020000);
+  const __amdgpu_buffer_rsrc_t from = resource(p.stats + head * p.padded + row0 + wave * 32, 256);
   __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(to + wave * 256), 4, (threadIdx.x & 63) * 4, 0, 0, 0);
 }
 
@@ -355,11 +363,12 @@ __device__ __forceinline__ void dkv(const AttentionParams& p) {
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t) keys.dk[t] = keys.dv[t] = zero16();
     int head = head0;
-    stage.ask((lds_byte*)even, p, head, lo, hi + 1, wave);
+    if constexpr (!SHARED) stage.ask((lds_byte*)even, p, head, lo, hi + 1, wave);
     for (int i0 = lo; head < behind;) {
 #pragma unroll
       for (int b = 0; b < (SHARED ? 1 : 2); ++b) {
         lds_byte* const tq = (lds_byte*)(b ? odd : even);
+        if constexpr (SHARED) stage.ask(tq, p, head, i0, hi + 1, wave);
         stage.put(tq);
         arrived();
         const int mine = SHARED ? wave : 0, now = i0 + mine * 32;
@@ -369,10 +378,7 @@ __device__ __forceinline__ void dkv(const AttentionParams& p) {
         if (mine < BN / 32 && now <= r.hi && now + 32 > r.lo)
           dkv_tile<DTYPE, DP, decltype(clean)::value, IN_LDS>(keys, read, tq + mine * EACH, tq + BYTES + mine * EACH, tq + 2 * BYTES + mine * 256, c, lane,
                                                               now < r.all_lo || now + 31 > r.all_hi, first - now, last - now, found);
-        if constexpr (SHARED) {                              // one tile at a time
-          __syncthreads();
-          if (head < behind) stage.ask(tq, p, head, i0, hi + 1, wave);
-        }
+        if constexpr (SHARED) __syncthreads();               // one tile at a time
         if (head == behind) break;
       }
     }
@@ -467,7 +473,7 @@ int launch_any(const AttentionParams& p, int dtype, bool backward, hipStream_t s
   const auto fits = [&](const Tensor& t) { return direct(t.p, t.stride, t.head, 0, p.dim, dtype); };
   const bool fast = fits(p.k) && fits(p.v) && (!backward || (fits(p.q) && fits(p.d_o)));
   if (dtype == LSAM_DTYPE_BF16) return fast ? launch_wide<LSAM_DTYPE_BF16, true>(p, backward, s) : launch_wide<LSAM_DTYPE_BF16, false>(p, backward, s);
-  return launch_wide<LSAM_DTYPE_FP32, false>(p, backward, s);
+  return fast ? launch_wide<LSAM_DTYPE_FP32, true>(p, backward, s) : launch_wide<LSAM_DTYPE_FP32, false>(p, backward, s);
 }
 
 }  // namespace

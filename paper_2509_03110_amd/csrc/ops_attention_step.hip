@@ -281,7 +281,8 @@ extern "C" int lsam_attention_step(const lsam_attention_step_desc* d, const int3
   const auto fits = [&](const void* t, const lsam_heads& h, int64_t seq) { return direct(t, h.stride, h.head, seq, d->dim, d->dtype); };
   const bool fast = (c.parts[0] == 0 || (fits(prefix_k, d->prefix_k, 0) && fits(prefix_v, d->prefix_v, 0))) &&
                     (c.parts[1] == 0 || (fits(k, d->k, d->k_seq) && fits(v, d->v, d->v_seq)));
-  if (d->dtype == LSAM_DTYPE_FP32) launch_wide<LSAM_DTYPE_FP32, false>(p, c.blocks, s);
+  if (d->dtype == LSAM_DTYPE_FP32 && fast) launch_wide<LSAM_DTYPE_FP32, true>(p, c.blocks, s);
+  else if (d->dtype == LSAM_DTYPE_FP32) launch_wide<LSAM_DTYPE_FP32, false>(p, c.blocks, s);
   else if (fast) launch_wide<LSAM_DTYPE_BF16, true>(p, c.blocks, s);
   else launch_wide<LSAM_DTYPE_BF16, false>(p, c.blocks, s);
   return launched();
