@@ -24,7 +24,7 @@ struct StepParams {
   float scale;
   int parts[2];                            // of the prefix, of a cache
   int columns[2];                          // workgroups that the columns of a part take
-  unsigned prefix_blocks;                  // workgroups of the prefix come first
+  unsigned prefix_blocks;                  // workgroups of the prefix, a multiple of eight
   bool spread;                             // of the prefix: a wavefront has columns of its own
   bool whole;                              // there is one part: o is written at once
   float* sums; float* values;              // [parts][seqs heads][2], [parts][seqs heads][dim]
@@ -40,20 +40,32 @@ __global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void step_kernel(StepPar
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
   // what this workgroup does: a part of the prefix for some columns, or a part of a cache
-  const bool shared = blockIdx.x < p.prefix_blocks;
+  // (products and memory side by side: groups of eight workgroups of the one and of the other in turn, while there are both)
+  const unsigned own_blocks = gridDim.x - p.prefix_blocks, pairs = (p.prefix_blocks < own_blocks ? p.prefix_blocks : own_blocks) / 8;
+  const unsigned eight = blockIdx.x / 8;
+  unsigned block = blockIdx.x;
+  bool shared;
+  if (eight < 2 * pairs) {
+    shared = eight % 2 == 0;
+    block = eight / 2 * 8 + blockIdx.x % 8;
+  } else {
+    block -= pairs * 8;                                      // behind the pairs: what is left of the one, then of the other
+    shared = block < p.prefix_blocks;
+    if (!shared) block = blockIdx.x - p.prefix_blocks;
+  }
   unsigned unit;
   int seq = 0, kv, part, first_column, keys;
   if (shared) {
     // those that read the same keys meet in an XCD
-    const unsigned i = blockIdx.x / 8;
-    unit = i / p.columns[0] * 8 + blockIdx.x % 8;
+    const unsigned i = block / 8;
+    unit = i / p.columns[0] * 8 + block % 8;
     if (unit >= (unsigned)(p.kv_heads * p.parts[0])) return;
     part = unit / p.kv_heads;
     kv = unit % p.kv_heads;
     first_column = (int)(i % p.columns[0]) * (p.spread ? kThreads / 2 : 32) + (p.spread ? wave * 32 : 0);
     keys = p.prefix_keys;
   } else {
-    unit = blockIdx.x - p.prefix_blocks;
+    unit = block;
     first_column = (int)(unit % p.columns[1]) * 32;
     unit /= p.columns[1];
     kv = unit % p.kv_heads;

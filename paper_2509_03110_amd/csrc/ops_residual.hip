@@ -82,7 +82,7 @@ __device__ __forceinline__ void sums_over_row(float (&v)[N], float (*shared)[WAV
 template <int WAVES, int CH>
 struct Columns {
   int64_t dim;
-  __device__ __forceinline__ int64_t col(int c) const { return (int64_t)(c * WAVES * 64 + threadIdx.x) * 8; }
+  __device__ __forceinline__ int64_t col(int c) const { return (int64_t)(c * WAVES * 64 + threadIdx.x % (WAVES * 64)) * 8; }
   __device__ __forceinline__ int count(int c) const {
     const int64_t n = dim - col(c);
     return n < 0 ? 0 : n < 8 ? (int)n : 8;
@@ -164,11 +164,15 @@ __device__ __forceinline__ float squares(const float (&v)[CH][8]) {
 // 1 / sqrt(mean x^2 + eps)
 __device__ __forceinline__ float inverse(float squares, const ResidualParams& p) { return 1.f / __builtin_sqrtf(squares / (float)p.dim + p.eps); }
 
+// Rows of a workgroup of the forward pass: where a wavefront holds one, four.
+template <int WAVES> constexpr int kRowsOf = WAVES == 1 ? 4 : 1;
+
 template <int DTYPE, int WAVES, int CH>
-__global__ __launch_bounds__(WAVES * 64) void residual_kernel(ResidualParams p) {
+__global__ __launch_bounds__(WAVES * 64 * kRowsOf<WAVES>) void residual_kernel(ResidualParams p) {
   __shared__ float shared[2][WAVES];
   const Columns<WAVES, CH> at{p.dim};
-  const int64_t replica = p.replica0 + blockIdx.y, row = p.row0 + blockIdx.x;
+  const int64_t replica = p.replica0 + blockIdx.y, row = p.row0 + (int64_t)blockIdx.x * kRowsOf<WAVES> + (kRowsOf<WAVES> > 1 ? threadIdx.x >> 6 : 0);
+  if (row >= p.rows) return;
   float r[CH][8];
   at.template load<DTYPE>(row_of<DTYPE>(p.r, replica, row), r);
   if (p.y.p) {
@@ -365,8 +369,12 @@ int check_apart_but(const Arg* args, int n, int in, bool same, const char* who) 
 
 template <int DTYPE, int WAVES, int CH>
 void launch(const ResidualParams& p, bool grad, dim3 grid, hipStream_t s) {
-  if (grad) residual_grad_kernel<DTYPE, WAVES, CH><<<grid, WAVES * 64, 0, s>>>(p);
-  else residual_kernel<DTYPE, WAVES, CH><<<grid, WAVES * 64, 0, s>>>(p);
+  if (grad) {
+    residual_grad_kernel<DTYPE, WAVES, CH><<<grid, WAVES * 64, 0, s>>>(p);
+  } else {
+    grid.x = (grid.x + kRowsOf<WAVES> - 1) / kRowsOf<WAVES>;
+    residual_kernel<DTYPE, WAVES, CH><<<grid, WAVES * 64 * kRowsOf<WAVES>, 0, s>>>(p);
+  }
 }
 template <int DTYPE>
 void launch_wide(const ResidualParams& p, bool grad, dim3 grid, hipStream_t s) {

@@ -523,30 +523,34 @@ def embedding_backward(tokens, dy, vocab, scale=1.0, out=None, stream=None):
 ResidualGradients = namedtuple("ResidualGradients", "dr dy dgate dw_pre dw_post")
 
 
-def _residual_desc(r, y, w_pre, w_post, gate, alpha, beta, eps):
-    if not 2 <= r.dim() <= 3:
-        _refuse("r has %d indices: [rows, dim] or [K, rows, dim] is wanted" % r.dim())
+_NO_ROWS = (0, 0)
+
+
+def _residual_desc(r, y, w_pre, w_post, gate, alpha, beta, eps, outs):
+    """`outs`: strides from row to row and from replica to replica of what comes behind the gate in the descriptor."""
+    n, shape = r.dim(), r.shape
     _expect(r, "r")
-    for t, what in ((y, "y"), (gate, "the gate")):
+    if y is not None:
+        _expect(y, "y", r, shape, r.dtype)
+    if gate is not None:
+        _expect(gate, "the gate", r, shape, r.dtype)
+    K, rows, dim = shape if n == 3 else (1,) + shape
+    apart = [0, 0]
+    for i, (t, what) in enumerate(((w_pre, "w_pre"), (w_post, "w_post"))):
         if t is not None:
-            _expect(t, what, r, r.shape, r.dtype)
-    K, rows, dim = (1,) * (3 - r.dim()) + tuple(r.shape)
-    d = lsam_residual_desc(K, _dtype(r, "r"), rows, dim, alpha, beta, eps)
-    for t, what, name in ((w_pre, "w_pre", "w_pre_replica"), (w_post, "w_post", "w_post_replica")):
-        if t is not None:
-            _expect(t, what, r, (K, dim) if t.dim() == 2 else (dim,), torch.float32)
-            if t.dim() == 2:
-                setattr(d, name, t.stride(0))
-    for t, name in ((r, "r"), (y, "y"), (gate, "gate")):
-        if t is not None:
-            _set_rows(d, name, t)
-    return d
+            one = t.dim() == 1
+            _expect(t, what, r, (dim,) if one else (K, dim), torch.float32)
+            if not one:
+                apart[i] = t.stride(0)
+    return lsam_residual_desc(K, _dtype(r, "r"), rows, dim, alpha, beta, eps, *apart, *_of_replicas(r), *(_NO_ROWS if y is None else _of_replicas(y)),
+                              *(_NO_ROWS if gate is None else _of_replicas(gate)), *outs)
 
 
-def _set_rows(d, name, t):
-    row, replica = _of_replicas(t)
-    setattr(d, name + "_stride", row)
-    setattr(d, name + "_replica", replica)
+def _strides(*tensors):
+    s = []
+    for t in tensors:
+        s += _NO_ROWS if t is None else _of_replicas(t)
+    return s
 
 
 def residual(r, y, w_pre, w_post=None, gate=None, alpha=1.0, beta=1.0, eps=1e-6, out=None, h=None, stream=None):
@@ -555,24 +559,17 @@ def residual(r, y, w_pre, w_post=None, gate=None, alpha=1.0, beta=1.0, eps=1e-6,
     or [K, dim].  No gate, no w_post (y as it is), no w_pre (h is None) and no y (r' is r itself) are possible; `out` for r' may be r; see
     lsam_residual."""
     L = _ready or _lib()
-    d = _residual_desc(r, y, w_pre, w_post, gate, alpha, beta, eps)
+    if not 2 <= r.dim() <= 3:
+        _refuse("r has %d indices: [rows, dim] or [K, rows, dim] is wanted" % r.dim())
     for t, what in ((out, "out"), (h, "h")):
         if t is not None:
             _expect(t, what, r, r.shape, r.dtype)
     with _On(r, stream) as raw:
-        if y is None:
-            new = r
-        else:
-            new = torch.empty(r.shape, dtype=r.dtype, device=r.device) if out is None else out
-            _set_rows(d, "r_out", new)
-        if w_pre is None:
-            h = None
-        else:
-            h = torch.empty(r.shape, dtype=r.dtype, device=r.device) if h is None else h
-            _set_rows(d, "h", h)
-        _check(L.lsam_residual(C.byref(d), r.data_ptr(), _ptr(y), _ptr(gate), _ptr(w_pre), _ptr(w_post),
-                               None if y is None else new.data_ptr(), _ptr(h), raw))
-    return new, h
+        new = None if y is None else torch.empty(r.shape, dtype=r.dtype, device=r.device) if out is None else out
+        h = None if w_pre is None else torch.empty(r.shape, dtype=r.dtype, device=r.device) if h is None else h
+        d = _residual_desc(r, y, w_pre, w_post, gate, alpha, beta, eps, _strides(new, h))
+        _check(L.lsam_residual(C.byref(d), r.data_ptr(), _ptr(y), _ptr(gate), _ptr(w_pre), _ptr(w_post), _ptr(new), _ptr(h), raw))
+    return r if y is None else new, h
 
 
 def residual_backward(r, y, w_pre, dr, dh, w_post=None, gate=None, alpha=1.0, beta=1.0, eps=1e-6, dr_out=None, dy=None, dgate=None, dw_pre=None,
@@ -581,7 +578,8 @@ def residual_backward(r, y, w_pre, dr, dh, w_post=None, gate=None, alpha=1.0, be
     Those of the weights are fp32, written whole; weights of K replicas are [K, dim], and their gradients may be parts of one [K, d]
     array.  dr_out may be dr.  What has no gradient is None; see lsam_residual_backward."""
     L = _ready or _lib()
-    d = _residual_desc(r, y, w_pre, w_post, gate, alpha, beta, eps)
+    if not 2 <= r.dim() <= 3:
+        _refuse("r has %d indices: [rows, dim] or [K, rows, dim] is wanted" % r.dim())
     if y is None:
         w_post = gate = None
     for t, what in ((w_pre, "w_pre"), (w_post, "w_post")):
@@ -595,7 +593,7 @@ def residual_backward(r, y, w_pre, dr, dh, w_post=None, gate=None, alpha=1.0, be
     for t, what, w in ((dw_pre, "dw_pre", w_pre), (dw_post, "dw_post", w_post)):
         if t is not None and w is not None:
             _expect(t, what, r, w.shape, torch.float32)
-    at, device = C.byref(d), r.device
+    device = r.device
     with _On(r, stream) as raw:
         new = lambda t, like, dtype: torch.empty(like.shape, dtype=dtype, device=device) if t is None else t  # noqa: E731
         dr_out = new(dr_out, r, r.dtype)
@@ -603,12 +601,9 @@ def residual_backward(r, y, w_pre, dr, dh, w_post=None, gate=None, alpha=1.0, be
         dgate = new(dgate, r, r.dtype) if gate is not None else None
         dw_pre = new(dw_pre, w_pre, torch.float32) if want_weights and w_pre is not None else None
         dw_post = new(dw_post, w_post, torch.float32) if want_weights and w_post is not None else None
-        for t, name in ((dr, "dr"), (dh, "dh"), (dr_out, "dr_out"), (dy, "dy"), (dgate, "dgate")):
-            if t is not None:
-                _set_rows(d, name, t)
-        for t, name in ((dw_pre, "dw_pre_replica"), (dw_post, "dw_post_replica")):
-            if t is not None and t.dim() == 2:
-                setattr(d, name, t.stride(0))
+        apart = [0 if t is None or t.dim() == 1 else t.stride(0) for t in (dw_pre, dw_post)]
+        d = _residual_desc(r, y, w_pre, w_post, gate, alpha, beta, eps, _strides(None, None, dr, dh, dr_out, dy, dgate) + apart)
+        at = C.byref(d)
         need = L.lsam_residual_workspace_bytes(at) if dw_pre is not None or dw_post is not None else 0
         ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
         _check(L.lsam_residual_backward(at, r.data_ptr(), _ptr(y), _ptr(gate), _ptr(w_pre), _ptr(w_post), _ptr(dr), _ptr(dh), dr_out.data_ptr(),
