@@ -201,7 +201,7 @@ struct Stage {
     if constexpr (DIRECT) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int n = threadIdx.x + i * THREADS, row = n / R::U, unit = THROUGH ? n % R::U : (n % R::U) ^ R::turn(row);
+        const int n = threadIdx.x % THREADS + i * THREADS, row = n / R::U, unit = THROUGH ? n % R::U : (n % R::U) ^ R::turn(row);
         at[i] = unit * 8 < dim ? (unsigned)(row * stride * B) + unit * 8 * B : 0x7FFFFFC0u;
       }
     }
@@ -210,7 +210,7 @@ struct Stage {
     if constexpr (DIRECT) {
       const int64_t rows = limit - row0 < ROWS ? limit - row0 : ROWS;
       const __amdgpu_buffer_rsrc_t from = resource(p + row0 * stride, rows > 0 ? (unsigned)(((rows - 1) * stride + dim) * B) : 0);
-      const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+      const int wave = THREADS > 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         if constexpr (THROUGH) {
@@ -244,6 +244,18 @@ struct Stage {
     }
   }
 };
+// Waits for all but the last N of the wavefront's own loads.
+template <int N> __device__ __forceinline__ void all_but() {
+  static_assert(N < 16, "");
+  __builtin_amdgcn_s_waitcnt(0x0F70 + N);
+  asm volatile("" ::: "memory");
+}
+// Waits for the wavefront's own reads of LDS.
+__device__ __forceinline__ void lds_read() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);
+  asm volatile("" ::: "memory");
+}
 // Waits for the wavefront's own loads, and for the other wavefronts.
 __device__ __forceinline__ void arrived() {
   __builtin_amdgcn_s_waitcnt(0x0070);                      // no load on its way, no LDS access
@@ -435,9 +447,17 @@ struct Seen {
   }
 };
 
-template <int DTYPE, int DP, int TILES, bool CLEAN>
+// What a tile's products say to those who bring tiles: that its keys have been read, that its values are read next.
+struct Quiet {
+  __device__ __forceinline__ void keys_read() const {}
+  __device__ __forceinline__ void values_next() const {}
+  __device__ __forceinline__ void both_next() const {}
+  __device__ __forceinline__ void neither() const {}
+};
+
+template <int DTYPE, int DP, int TILES, bool CLEAN, typename B = Quiet>
 __device__ __forceinline__ void attend(Running<DP>& a, const Reader<DTYPE, DP>& read, const typename Operand<DTYPE>::F (&q)[DP / 16], const lds_byte* tk,
-                                       const lds_byte* tv, float c, int lane, bool masked, int first, int last, unsigned& found) {
+                                       const lds_byte* tv, float c, int lane, bool masked, int first, int last, unsigned& found, const B& bring = B()) {
   typedef Operand<DTYPE> O;
   constexpr int STEPS = DP / 16;
   f32x16 s[TILES];
@@ -453,6 +473,7 @@ __device__ __forceinline__ void attend(Running<DP>& a, const Reader<DTYPE, DP>& 
     s[0] = TILES == 2 ? two[0] : two[0] + two[1];
     if constexpr (TILES == 2) s[1] = two[1];
   }
+  bring.keys_read();
   if (masked) {
     const Seen seen(first, last, lane);
 #pragma unroll
@@ -482,6 +503,7 @@ __device__ __forceinline__ void attend(Running<DP>& a, const Reader<DTYPE, DP>& 
       s[i][e] = __builtin_amdgcn_exp2f(s[i][e] * c - a.base);
       a.l += s[i][e];
     }
+  bring.values_next();
 #pragma unroll
   for (int n = 0; n < TILES * 2; ++n) multiply_across<DTYPE, DP, CLEAN>(a.acc, read, tv, n * 16, O::from(s[n / 2], n & 1, true), found);
 }
@@ -535,23 +557,68 @@ __device__ __forceinline__ void join_running(Running<DP>& a, float c, int wave, 
 #pragma unroll
   for (int w = 0; w < N; ++w) a.l += of_waves[1][w][lane & 31];
 }
-// Keys lo .. hi in tiles of kSharing x 32, `f(its keys, their values, the first of them)` for each wavefront that has some.  One tile at a time; two
-// workgroups of a unit take turns.
+// Rows of bf16 that go to LDS directly are each wavefront's own business: it asks for its next keys when those it has are read, for its next
+// values when those are, and waits for neither longer than it has to.
+template <int DTYPE, int DP>
+struct Ahead {
+  typedef Stage<DTYPE, DP, 32, 64, true> S;
+  S k, v;
+  lds_byte *tk, *tv;
+  int next, end;
+  __device__ __forceinline__ void keys_read() const {
+    lds_read();
+    const_cast<S&>(k).ask(tk, next, end);
+  }
+  __device__ __forceinline__ void values_next() const { all_but<S::N>(); }      // the next keys are behind them
+  __device__ __forceinline__ void both_next() const { all_but<0>(); }
+  __device__ __forceinline__ void neither() const {
+    all_but<0>();
+    keys_read();
+  }
+  __device__ __forceinline__ void values_read() const {
+    lds_read();
+    const_cast<S&>(v).ask(tv, next, end);
+  }
+};
+// Keys lo .. hi in tiles of kSharing x 32, `f(its keys, their values, the first of them, who brings them)` for each wavefront that has some.  Other rows
+// come one tile at a time; two workgroups of a unit take turns.
 template <int DTYPE, int DP, bool DIRECT, typename F>
 __device__ __forceinline__ void walk_shared(unsigned char* even, unsigned char* odd, const HeadRows& k, const HeadRows& v, int lo, int hi, int dim, F f) {
   constexpr int ROWS = kSharing<DTYPE> * 32, EACH = 32 * Rows<DTYPE, DP>::BYTES;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  Stage<DTYPE, DP, ROWS, kThreads, DIRECT> sk, sv;
-  sk.init(k, dim);
-  sv.init(v, dim);
-  for (int j0 = lo; j0 <= hi; j0 += ROWS) {
-    if (j0 > lo) __syncthreads();
-    sk.ask((lds_byte*)even, j0, hi + 1);
-    sv.ask((lds_byte*)odd, j0, hi + 1);
-    sk.put((lds_byte*)even);
-    sv.put((lds_byte*)odd);
-    arrived();
-    if (wave < kSharing<DTYPE> && j0 + wave * 32 <= hi) f((lds_byte*)even + wave * EACH, (lds_byte*)odd + wave * EACH, j0 + wave * 32);
+  if constexpr (DIRECT && Operand<DTYPE>::PLANES == 1) {
+    static_assert(ROWS == kThreads / 64 * 32, "every wavefront takes part");
+    Ahead<DTYPE, DP> a;
+    a.k.init(k, dim);
+    a.v.init(v, dim);
+    a.tk = (lds_byte*)even + wave * EACH;
+    a.tv = (lds_byte*)odd + wave * EACH;
+    a.end = hi + 1;
+    a.next = lo + wave * 32;
+    if (a.next <= hi) {
+      a.keys_read();
+      a.values_read();
+      for (int j0 = a.next; j0 <= hi; j0 = a.next) {
+        a.next = j0 + ROWS;
+        all_but<Ahead<DTYPE, DP>::S::N>();
+        f(a.tk, a.tv, j0, a);
+        a.values_read();
+      }
+    }
+    all_but<0>();                                            // what was asked for behind the last
+  } else {
+    Stage<DTYPE, DP, ROWS, kThreads, DIRECT> sk, sv;
+    sk.init(k, dim);
+    sv.init(v, dim);
+    for (int j0 = lo; j0 <= hi; j0 += ROWS) {
+      if (j0 > lo) __syncthreads();
+      sk.ask((lds_byte*)even, j0, hi + 1);
+      sv.ask((lds_byte*)odd, j0, hi + 1);
+      sk.put((lds_byte*)even);
+      sv.put((lds_byte*)odd);
+      arrived();
+      if (wave < kSharing<DTYPE> && j0 + wave * 32 <= hi) f((lds_byte*)even + wave * EACH, (lds_byte*)odd + wave * EACH, j0 + wave * 32, Quiet());
+    }
   }
   __syncthreads();                                           // the arrays are free
 }

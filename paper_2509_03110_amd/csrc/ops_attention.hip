@@ -114,9 +114,9 @@ __global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void attention_kernel(At
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t) a.acc[t] = zero16();
     if constexpr (SHARED) {
-      walk_shared<DTYPE, DP, DIRECT>(even, odd, k, v, lo, hi, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0) {
-        if (j0 > r.hi || j0 + 32 <= r.lo) return;
-        attend<DTYPE, DP, 1, decltype(clean)::value>(a, read, q, tk, tv, c, lane, j0 < r.all_lo || j0 + 31 > r.all_hi, first - j0, last - j0, found);
+      walk_shared<DTYPE, DP, DIRECT>(even, odd, k, v, lo, hi, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0, const auto& bring) {
+        if (j0 > r.hi || j0 + 32 <= r.lo) return bring.neither();
+        attend<DTYPE, DP, 1, decltype(clean)::value>(a, read, q, tk, tv, c, lane, j0 < r.all_lo || j0 + 31 > r.all_hi, first - j0, last - j0, found, bring);
       });
       join_running<DTYPE, DP>(a, c, wave, lane, even, odd);
     } else {
@@ -204,10 +204,12 @@ __global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void dq_kernel(Attention
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t) acc[t] = zero16();
     if constexpr (SHARED) {
-      walk_shared<DTYPE, DP, DIRECT>(even, odd, k, v, lo, hi, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0) {
-        if (j0 > r.hi || j0 + 32 <= r.lo) return;
+      walk_shared<DTYPE, DP, DIRECT>(even, odd, k, v, lo, hi, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0, const auto& bring) {
+        if (j0 > r.hi || j0 + 32 <= r.lo) return bring.neither();
+        bring.both_next();
         dq_tile<DTYPE, DP, 1, decltype(clean)::value>(acc, read, q, g, tk, tv, c, base, dot, lane, j0 < r.all_lo || j0 + 31 > r.all_hi, first - j0, last - j0,
                                                       found);
+        bring.keys_read();
       });
       join_sums<DTYPE, DP>(acc, wave, lane, even, odd);
     } else {

@@ -105,8 +105,8 @@ __global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void step_kernel(StepPar
     });
     l = a.l + other_half(a.l);
   } else {
-    walk_shared<DTYPE, DP, DIRECT>(even, odd, k, v, from, to - 1, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0) {
-      attend<DTYPE, DP, 1, false>(a, read, q, tk, tv, scale, lane, j0 + 32 > to, 0, to - 1 - j0, found);
+    walk_shared<DTYPE, DP, DIRECT>(even, odd, k, v, from, to - 1, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0, const auto& bring) {
+      attend<DTYPE, DP, 1, false>(a, read, q, tk, tv, scale, lane, j0 + 32 > to, 0, to - 1 - j0, found, bring);
     });
     join_running<DTYPE, DP>(a, scale, wave, lane, even, odd);
     if (wave > 0) return;
