@@ -260,19 +260,21 @@ int lsam_residual_backward(const lsam_residual_desc* d, const void* r, const voi
  *   q, o   [device] [rows, heads, dim], k, v [rows, kv_heads, dim], of dtype; strides from row to row and from head to head are free, so q, k and
  *          v may be parts of one array
  *   lse    [device] [heads, rows] floats that receive lse, for the backward pass, or NULL
- * Scores, sums and lse are fp32, and so are products of fp32 operands; bf16 operands meet probabilities rounded to bf16 (2^-9 of themselves, one rounding before
- * the sum over j).  What is not finite in a row that i does not see does not reach o_i. */
+ * Scores, sums and lse are fp32.  Products of fp32 operands are those of three bf16 pieces of each, six products in fp32: 2^-22 of |a| |b| at most is
+ * left out.  bf16 operands meet probabilities rounded to bf16 (2^-8 of themselves, once, before the sum over j).  What is not finite in a row that i
+ * does not see does not reach o_i. */
 #define LSAM_ATTENTION_MAX_DIM 128
+#define LSAM_ATTENTION_MAX_SCALE 0x1p100f
 typedef struct {
   int64_t stride, head;                      /* from row to row, from head to head           */
 } lsam_heads;
 typedef struct {
-  int64_t rows;                              /* below 2^30; rows heads below 2^31            */
+  int64_t rows;                              /* rows heads below 2^30                        */
   int64_t seqs;                              /* below 2^31                                   */
   int32_t heads, kv_heads;                   /* heads a multiple of kv_heads, at most 65536  */
   int32_t dim;                               /* 1..LSAM_ATTENTION_MAX_DIM                    */
   int32_t dtype;                             /* LSAM_DTYPE_*                                 */
-  float scale;                               /* finite, not negative                         */
+  float scale;                               /* 0..LSAM_ATTENTION_MAX_SCALE                  */
   lsam_heads q, k, v, o;
   lsam_heads d_o, dq, dk, dv;                /* not looked at by the forward pass            */
 } lsam_attention_desc;
@@ -307,7 +309,7 @@ typedef struct {
   int32_t heads, kv_heads;                   /* heads a multiple of kv_heads, at most 65536  */
   int32_t dim;                               /* 1..LSAM_ATTENTION_MAX_DIM                    */
   int32_t dtype;                             /* LSAM_DTYPE_*                                 */
-  float scale;                               /* finite, not negative                         */
+  float scale;                               /* 0..LSAM_ATTENTION_MAX_SCALE                  */
   lsam_heads q, o;                           /* stride: from sequence to sequence            */
   lsam_heads k, v;                           /* stride: from place to place                  */
   int64_t k_seq, v_seq;                      /* from sequence to sequence                    */

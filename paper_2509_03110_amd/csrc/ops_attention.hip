@@ -418,9 +418,9 @@ int check(const lsam_attention_desc* d, const char* who) {
     return refuse(LSAM_EINVAL, "%s: heads must be a multiple of kv_heads, in 1..65536", who);
   if (d->dim < 1 || d->dim > LSAM_ATTENTION_MAX_DIM) return refuse(LSAM_EINVAL, "%s: dim must be in 1..%d", who, LSAM_ATTENTION_MAX_DIM);
   if (d->seqs < 0 || d->seqs >= 1ll << 31) return refuse(LSAM_EINVAL, "%s: seqs must be in 0..2^31-1", who);
-  if (d->rows < 0 || d->rows >= 1 << 30 || d->rows * d->heads >= 1ll << 31)
-    return refuse(LSAM_EINVAL, "%s: rows must be below 2^30, and times heads below 2^31", who);
-  if (!(d->scale >= 0.f) || d->scale > 3e38f) return refuse(LSAM_EINVAL, "%s: the scale must be finite and not negative", who);
+  if (d->rows < 0 || d->rows >= 1 << 30 || d->rows * d->heads >= 1 << 30)
+    return refuse(LSAM_EINVAL, "%s: rows times heads must be below 2^30", who);      // launches of less than 2^32 lanes
+  if (!(d->scale >= 0.f) || d->scale > LSAM_ATTENTION_MAX_SCALE) return refuse(LSAM_EINVAL, "%s: the scale must be in 0..2^100", who);
   return LSAM_OK;
 }
 

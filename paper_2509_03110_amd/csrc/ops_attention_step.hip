@@ -217,7 +217,7 @@ int check(const lsam_attention_step_desc* d, const char* who) {
   if (d->seqs < 0 || d->seqs >= 1 << 23 || d->seqs * d->heads >= 1 << 23) return refuse(LSAM_EINVAL, "%s: seqs times heads must be below 2^23", who);
   if (d->capacity < 0 || d->capacity >= 1 << 30 || d->prefix < 0 || d->prefix >= 1 << 30)
     return refuse(LSAM_EINVAL, "%s: capacity and prefix must be in 0..2^30-1", who);
-  if (!(d->scale >= 0.f) || d->scale > 3e38f) return refuse(LSAM_EINVAL, "%s: the scale must be finite and not negative", who);
+  if (!(d->scale >= 0.f) || d->scale > LSAM_ATTENTION_MAX_SCALE) return refuse(LSAM_EINVAL, "%s: the scale must be in 0..2^100", who);
   return LSAM_OK;
 }
 
