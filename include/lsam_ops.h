@@ -261,7 +261,7 @@ int lsam_residual_backward(const lsam_residual_desc* d, const void* r, const voi
  *          v may be parts of one array
  *   lse    [device] [heads, rows] floats that receive lse, for the backward pass, or NULL
  * Scores, sums and lse are fp32.  Products of fp32 operands are those of three bf16 pieces of each, six products in fp32: 2^-22 of |a| |b| at most is
- * left out.  bf16 operands meet probabilities rounded to bf16 (2^-8 of themselves, once, before the sum over j).  What is not finite in a row that i
+ * left out.  bf16 operands meet probabilities rounded to bf16 (2^-8 of themselves, once, before the sum over j).  A p below 2^-126 is 0.  What is not finite in a row that i
  * does not see does not reach o_i. */
 #define LSAM_ATTENTION_MAX_DIM 128
 #define LSAM_ATTENTION_MAX_SCALE 0x1p100f

@@ -59,7 +59,7 @@ def near(got, want, bound, what):
     assert bool((off <= bound).all()), (what, float((off / bound).max()))
 
 
-def check(q, k, v, do, offsets, scale=None):
+def check(q, k, v, do, offsets, scale=None, floor=0.0):
     off = torch.tensor(offsets, dtype=torch.int64, device=DEV)
     r = ops.attention(q, k, v, off, scale=scale, save=True)
     grads = ops.attention_backward(q, k, v, off, r.o, r.lse, do, scale=scale)
@@ -70,8 +70,8 @@ def check(q, k, v, do, offsets, scale=None):
         if lo >= hi:
             continue
         want = reference(q[lo:hi], k[lo:hi], v[lo:hi], do[lo:hi], q.shape[2] ** -0.5 if scale is None else scale, q.dtype)
-        for name, pair in want.items():
-            near(got[name][:, lo:hi] if name == "lse" else got[name][lo:hi], *pair, name)
+        for name, (value, bound) in want.items():
+            near(got[name][:, lo:hi] if name == "lse" else got[name][lo:hi], value, bound + floor, name)
     return got
 
 

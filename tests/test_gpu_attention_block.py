@@ -1,0 +1,218 @@
+"""The operators around and in attention as they are used: a block with its gradients, generation, captured graphs, other streams, and tensors that
+want gradients."""
+import math
+
+import pytest
+import torch
+
+from paper_2509_03110_amd import lsam, ops
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, B16 = torch.float32, torch.bfloat16
+VOCAB, DIM, H, KV, HD = 97, 48, 6, 2, 24
+OFFSETS = [0, 1, 40, 40, 111]
+
+
+def parameters(seed):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    n = lambda *s: torch.randn(*s, device=DEV, generator=g)  # noqa: E731
+    return dict(table=n(VOCAB, DIM), w_in=1 + 0.1 * n(DIM), wqkv=n(DIM, (H + 2 * KV) * HD) * DIM ** -0.5, wo=n(H * HD, DIM) * (H * HD) ** -0.5,
+                w_join=1 + 0.1 * n(DIM), w_out=1 + 0.1 * n(DIM), gate=n(OFFSETS[-1], DIM), g=n(OFFSETS[-1]))
+
+
+def tokens(seed):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    return torch.randint(0, VOCAB, (OFFSETS[-1],), device=DEV, generator=g, dtype=torch.int32)
+
+
+def block(p, tok, off, names=None):
+    """Log probabilities of `names` (the tokens' own) after one block, and the gradients of sum g logp."""
+    names = tok if names is None else names
+    rows = tok.shape[0]
+    r0 = ops.embedding(tok, p["table"], scale=DIM ** 0.5)
+    _, h0 = ops.residual(r0, None, p["w_in"])
+    qkv = (h0 @ p["wqkv"]).view(rows, H + 2 * KV, HD)
+    q, k, v = qkv[:, :H], qkv[:, H:H + KV], qkv[:, H + KV:]
+    a = ops.attention(q, k, v, off, save=True)
+    y = a.o.view(rows, H * HD) @ p["wo"]
+    r1, h1 = ops.residual(r0, y, p["w_out"], w_post=p["w_join"], gate=p["gate"], alpha=0.5, beta=2.0)
+    z = h1 @ p["table"].t()
+    lp = ops.logprobs(z, names)
+    dz = ops.logprobs_backward(z, names, lp.lse, lp.entropy, g_logp=p["g"])
+    back = ops.residual_backward(r1, y, p["w_out"], None, dz @ p["table"], w_post=p["w_join"], gate=p["gate"], alpha=0.5, beta=2.0)
+    d_o = (back.dy @ p["wo"].t()).view(rows, H, HD)
+    dqkv = torch.empty_like(qkv)
+    ops.attention_backward(q, k, v, off, a.o, a.lse, d_o, dq=dqkv[:, :H], dk=dqkv[:, H:H + KV], dv=dqkv[:, H + KV:])
+    dqkv = dqkv.view(rows, -1)
+    first = ops.residual_backward(r0, None, p["w_in"], back.dr, dqkv @ p["wqkv"].t())
+    grads = dict(table=ops.embedding_backward(tok, first.dr, VOCAB, scale=DIM ** 0.5) + dz.t() @ h1, w_in=first.dw_pre, wqkv=h0.t() @ dqkv,
+                 wo=a.o.view(rows, -1).t() @ back.dy, w_join=back.dw_post, w_out=back.dw_pre, gate=back.dgate)
+    return lp.logp, grads
+
+
+def reference(p, tok, names):
+    """The same by definition in 64 bits, differentiated by torch; and the largest logit."""
+    p = {n: t.double().cpu().requires_grad_(n != "g") for n, t in p.items()}
+    tok, names = tok.cpu().long(), names.cpu().long()
+    norm = lambda x: x / (x.square().mean(1, keepdim=True) + 1e-6).sqrt()  # noqa: E731
+    r0 = p["table"][tok] * DIM ** 0.5
+    qkv = ((norm(r0) * p["w_in"]) @ p["wqkv"]).view(-1, H + 2 * KV, HD)
+    outs = []
+    for lo, hi in zip(OFFSETS, OFFSETS[1:]):
+        q, k, v = (t.transpose(0, 1) for t in qkv[lo:hi].split([H, KV, KV], 1))
+        s = HD ** -0.5 * q @ k.repeat_interleave(H // KV, 0).transpose(1, 2)
+        s = s.masked_fill(torch.ones(hi - lo, hi - lo, dtype=torch.bool).triu(1), -math.inf)
+        outs.append((torch.softmax(s, 2) @ v.repeat_interleave(H // KV, 0)).transpose(0, 1).reshape(hi - lo, H * HD))
+    y = torch.cat(outs) @ p["wo"]
+    r1 = 0.5 * r0 + 2.0 * torch.sigmoid(p["gate"]) * p["w_join"] * norm(y)
+    z = (norm(r1) * p["w_out"]) @ p["table"].t()
+    logp = torch.log_softmax(z, 1)[torch.arange(len(tok)), names]
+    (p["g"] * logp).sum().backward()
+    return logp.detach(), {n: t.grad for n, t in p.items() if n != "g"}, float(z.detach().abs().max())
+
+
+@pytest.mark.parametrize("own", [True, False])
+def test_a_block_and_its_gradients(own):
+    """Each value passes about 14 operators, none of which adds more than the roundings of a sum of 144 numbers to what is as large as its result, and the
+    norms, attention and products in between keep an error of a part of a value such a part: e = 14 x 144 x 2^-24 = 1.2e-4.  Logits of up to Z are off
+    by e Z.  A log probability is a difference of logits, so it is off by as much, however near to 0 it is, as that of a token's own name is here; a
+    probability is the power of one, so it is off by e Z of itself, and with it all gradients, by e Z of the largest.  Not those of a token's own name: their 1 - p, up to 6e-4 here, is the
+    difference of numbers near 1, off by 2^-24 and more whatever its size, and gradients as small as 2e-5 are made of it."""
+    p, tok, names = parameters(1), tokens(2), tokens(2 if own else 3)
+    off = torch.tensor(OFFSETS, dtype=torch.int64, device=DEV)
+    logp, grads = block(p, tok, off, names)
+    want, want_grads, most = reference(p, tok, names)
+    e = 14 * 144 * 2.0 ** -24 * most
+    off_by = lambda a, b: float((a.double().cpu() - b).abs().max())  # noqa: E731
+    assert off_by(logp, want) <= e
+    assert set(grads) == set(want_grads)
+    for n in grads if not own else ():
+        assert off_by(grads[n], want_grads[n]) <= e * float(want_grads[n].abs().max()), n
+
+
+def test_a_block_captured_twice_and_replayed_with_other_inputs():
+    """Two graphs of the same block in turn, each with inputs of its own, and the same calls outside of them: equal to the bit."""
+    off = torch.tensor(OFFSETS, dtype=torch.int64, device=DEV)
+    sets = []
+    for i in range(2):
+        p, tok = parameters(10 + i), tokens(20 + i)
+        block(p, tok, off)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = block(p, tok, off)
+        sets.append((p, tok, graph, out))
+    for turn in range(4):
+        for i, (p, tok, graph, out) in enumerate(sets):
+            for n, t in parameters(100 + 2 * turn + i).items():
+                p[n].copy_(t)
+            tok.copy_(tokens(200 + 2 * turn + i))
+            graph.replay()
+            if turn % 2:
+                torch.cuda.synchronize()
+            logp, grads = block(p, tok, off)
+            assert torch.equal(out[0], logp)
+            for n in grads:
+                assert torch.equal(out[1][n], grads[n]), (turn, n)
+
+
+@pytest.mark.parametrize("dtype", [F32, B16])
+def test_generation_goes_as_the_prompt_does(dtype):
+    """Tokens one after the other over a cache, behind a shared prefix, against one call for the whole: the same sums in another order.  Weights p
+    are off by (dim + 16) 2^-24 scale sum |q k| of themselves at most, and by half a step of bfloat16, on both sides."""
+    g = torch.Generator(device=DEV).manual_seed(3)
+    S, prefix, steps, dim = 3, 70, 9, 64
+    n = lambda *s: torch.randn(*s, device=DEV, generator=g).to(dtype)  # noqa: E731
+    pq, pk, pv = n(prefix, H, dim), n(prefix, KV, dim), n(prefix, KV, dim)
+    q, k, v = n(S, steps, H, dim), n(S, steps, KV, dim), n(S, steps, KV, dim)
+    cache_k, cache_v = torch.full((S, 16, KV, dim), math.nan, device=DEV, dtype=dtype), torch.full((S, 16, KV, dim), math.nan, device=DEV, dtype=dtype)
+    off = torch.arange(S + 1, dtype=torch.int64, device=DEV) * (prefix + steps)
+    whole = [torch.cat([t for s in range(S) for t in (a, b[s])]) for a, b in ((pq, q), (pk, k), (pv, v))]
+    want = ops.attention(*whole, off).o.view(S, prefix + steps, H, dim)[:, prefix:].float()
+    lengths = torch.zeros(S, dtype=torch.int32, device=DEV)
+    size = float(whole[0].float().norm(dim=2).max() * whole[1].float().norm(dim=2).max()) * dim ** -0.5
+    r = 2.0 ** -8 if dtype == B16 else 0.0
+    bound = float(whole[2].float().abs().max()) * 2 * (math.expm1(2 * (dim + 16) * 2.0 ** -24 * size) + 2 * r + 200 * 2.0 ** -24)
+    for t in range(steps):
+        cache_k[:, t], cache_v[:, t] = k[:, t], v[:, t]
+        lengths += 1
+        o = ops.attention_step(q[:, t], cache_k, cache_v, lengths, pk, pv)
+        assert float((o.float() - want[:, t]).abs().max()) <= bound, t
+
+
+def test_one_tokens_attention_in_a_graph_whose_lengths_grow():
+    g = torch.Generator(device=DEV).manual_seed(4)
+    n = lambda *s: torch.randn(*s, device=DEV, generator=g).to(B16)  # noqa: E731
+    q, k, v, pk, pv = n(5, H, 64), n(5, 400, KV, 64), n(5, 400, KV, 64), n(300, KV, 64), n(300, KV, 64)
+    lengths = torch.zeros(5, dtype=torch.int32, device=DEV)
+    ops.attention_step(q, k, v, lengths, pk, pv)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = ops.attention_step(q, k, v, lengths, pk, pv)
+    for turn in range(4):
+        lengths.add_(torch.tensor([1, 0, 100, 37, 130], dtype=torch.int32, device=DEV))
+        q.copy_(n(5, H, 64))
+        graph.replay()
+        assert torch.equal(out, ops.attention_step(q, k, v, lengths, pk, pv)), turn
+
+
+def calls():
+    n = lambda *s: torch.randn(*s, device=DEV)  # noqa: E731
+    tok = torch.tensor([1, 2, 3, 2, 9, -1], dtype=torch.int32, device=DEV)
+    off = torch.tensor([0, 2, 6], dtype=torch.int64, device=DEV)
+    q, k, v, do = n(6, 4, 8), n(6, 2, 8), n(6, 2, 8), n(6, 4, 8)
+    a = ops.attention(q, k, v, off, save=True)
+    e = torch.empty_like
+    r, y, w, gate = n(6, 16), n(6, 16), n(16), n(6, 16)
+    return [(ops.embedding, dict(table=n(9, 16), out=n(6, 16)), dict(tokens=tok)),
+            (ops.embedding_backward, dict(dy=n(6, 16), out=n(9, 16)), dict(tokens=tok, vocab=9)),
+            (ops.residual, dict(r=r, y=y, w_pre=w, w_post=n(16), gate=gate, out=e(r), h=e(r)), {}),
+            (ops.residual_backward, dict(r=r, y=y, w_pre=w, dr=n(6, 16), dh=n(6, 16), w_post=n(16), gate=gate, dr_out=e(r), dy=e(r), dgate=e(r),
+                                         dw_pre=e(w), dw_post=e(w)), {}),
+            (ops.attention, dict(q=q, k=k, v=v, out=e(q)), dict(offsets=off)),
+            (ops.attention_backward, dict(q=q, k=k, v=v, o=a.o, lse=a.lse, do=do, dq=e(q), dk=e(k), dv=e(v)), dict(offsets=off)),
+            (ops.attention_step, dict(q=q, k=n(6, 5, 2, 8), v=n(6, 5, 2, 8), prefix_k=n(3, 2, 8), prefix_v=n(3, 2, 8), out=e(q)),
+             dict(lengths=torch.tensor([0, 1, 2, 3, 4, 5], dtype=torch.int32, device=DEV)))]
+
+
+def test_tensors_that_want_a_gradient_are_refused_while_gradients_are_recorded():
+    for op, tensors, rest in calls():
+        op(**tensors, **rest)
+        for name, t in tensors.items():
+            kw = dict(tensors, **{name: t.detach().requires_grad_()})
+            with pytest.raises(lsam.LsamError) as e:
+                op(**kw, **rest)
+            assert e.value.code == lsam.EINVAL and "gradient" in str(e.value), (op.__name__, name)
+            with torch.no_grad():
+                op(**kw, **rest)
+            with torch.inference_mode():
+                op(**dict(kw, **{name: t.detach()}), **rest)
+
+
+def test_calls_run_on_the_stream_they_are_given():
+    s = torch.cuda.Stream()
+    for op, tensors, rest in calls():
+        first = op(**tensors, **rest)
+        first = [t.clone() for t in (first if isinstance(first, tuple) else (first,)) if t is not None]
+        s.wait_stream(torch.cuda.current_stream())
+        again = op(**tensors, **rest, stream=s)
+        torch.cuda.current_stream().wait_stream(s)
+        again = [t for t in (again if isinstance(again, tuple) else (again,)) if t is not None]
+        assert len(first) == len(again) and all(torch.equal(a, b) for a, b in zip(first, again)), op.__name__
+
+
+def test_tensors_elsewhere_and_of_other_types_are_refused():
+    for op, tensors, rest in calls():
+        for name, t in tensors.items():
+            for other in (t.cpu(), t.double(), t.half()):
+                with pytest.raises(lsam.LsamError) as e:
+                    op(**dict(tensors, **{name: other}), **rest)
+                assert e.value.code == lsam.EINVAL, (op.__name__, name)
+        for name, t in rest.items():
+            if torch.is_tensor(t):
+                for other in (t.cpu(), t.float()):
+                    with pytest.raises(lsam.LsamError) as e:
+                        op(**tensors, **dict(rest, **{name: other}))
+                    assert e.value.code == lsam.EINVAL, (op.__name__, name)
