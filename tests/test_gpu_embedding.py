@@ -86,6 +86,29 @@ def test_tokens_that_end_at_and_beside_the_edges_of_64_places(tokens):
     assert torch.equal(got[0], torch.zeros(5, 6, device=DEV).index_add_(0, t[0][keep].long(), dy[0][keep]))
 
 
+@pytest.mark.parametrize("before", [0, 1, 63])
+@pytest.mark.parametrize("n", [64 * 8, 64 * 9, 64 * 9 + 1, 64 * 10 - 1, 64 * 70 + 5])
+def test_runs_over_few_and_many_chunks_of_64_places(n, before):
+    """One token's run, and a shorter one behind it, with columns for three wavefronts; small whole numbers, so exact."""
+    t = torch.tensor([[0] * before + [1] * n + [2] * 200], dtype=torch.int32, device=DEV)
+    t = t[:, torch.randperm(t.shape[1], device=DEV, generator=gen(n))].contiguous()
+    dy = torch.randint(-8, 9, (1, t.shape[1], 520), device=DEV, generator=gen(1)).float()
+    assert torch.equal(ops.embedding_backward(t, dy, 4)[0], torch.zeros(4, 520, device=DEV).index_add_(0, t[0].long(), dy[0]))
+
+
+@pytest.mark.parametrize("table_type,dtype,rows,D", [(F32, F32, 22000, 777), (B16, F32, 33000, 513), (F32, B16, 33000, 1031), (B16, B16, 60000, 600)])
+def test_many_rows_of_which_a_lane_has_several(table_type, dtype, rows, D):
+    tokens = some_tokens(2, rows, 50, seed=rows)
+    wide = torch.full((2, rows, D + 5), 7.0, dtype=dtype, device=DEV)
+    table = torch.randn(2, 50, D, device=DEV, generator=gen(5)).to(table_type)
+    y = ops.embedding(tokens, table, scale=0.75, out=wide[:, :, 3:3 + D])
+    there = (tokens >= 0) & (tokens < 50)
+    for k in range(2):
+        want = (table[k].float() * 0.75).to(dtype)[tokens[k].long().clamp(0, 49)]          # one product, one rounding: exact
+        assert torch.equal(y[k], torch.where(there[k][:, None], want, torch.zeros_like(want)))
+    assert bool((wide[:, :, :3] == 7).all()) and bool((wide[:, :, 3 + D:] == 7).all())
+
+
 def test_one_replica_without_its_index_and_a_table_that_all_read():
     tokens = some_tokens(3, 50, 20, seed=2)
     table = torch.randn(20, 12, device=DEV, generator=gen(3))
