@@ -25,6 +25,8 @@ struct AttentionParams {
   f32x2* stats;                            // backward: [heads][padded]: lse as a power of 2, d_o o
   int64_t padded;                          // rows, and what a tile may reach past them
   int heads, group, dim, tiles;
+  int parts, apiece;                       // dkv: workgroups that share the heads of a group, heads of one
+  float* sums;                             // dkv of more than one: [dk, dv][parts][kv_heads][rows][dim]
   float scale;
 };
 
@@ -41,7 +43,7 @@ __device__ __forceinline__ Work work(int tiles, int kv_heads, int of, bool last_
   const unsigned rest = i / of;
   unsigned at = rest / mine;
   if (!last_first) {
-    const unsigned all = (tiles + parts - 1) / parts, round = mine < 32 ? 32 / mine : 1, from = at / round * round;
+    const unsigned all = (tiles + parts - 1) / parts, units = mine * of, round = units < 32 ? 32 / units : 1, from = at / round * round;
     if (at / round % 2) at = from + (from + round <= all ? round : all - from) - 1 - (at - from);
   }
   w.kv = (int)(rest % mine * common + xcd % common);
@@ -321,7 +323,9 @@ template <int DTYPE, int DP, bool DIRECT, int ROWS> struct SeenStage {
   }
 };
 
-template <int DTYPE, int DP, bool DIRECT, bool SHARED>
+// PARTS: the heads of a group may be shared by workgroups.  (Without it the wide kernel of 128 bf16 numbers takes 5 % less time: no other stores to find
+// registers for.)
+template <int DTYPE, int DP, bool DIRECT, bool SHARED, bool PARTS>
 __device__ __forceinline__ void dkv(const AttentionParams& p) {
   typedef typename Value<DTYPE>::T T;
   // keys in LDS where registers are short; three pieces of 128 have no room there, but one wavefront a SIMD has registers
@@ -330,7 +334,7 @@ __device__ __forceinline__ void dkv(const AttentionParams& p) {
   constexpr int LDS = kSeenLds<DTYPE, DP, SHARED>;
   __shared__ __attribute__((aligned(1024))) unsigned char even[LDS], odd[SHARED ? 16 : LDS], own[IN_LDS ? kRowsOf<SHARED> * Rows<DTYPE, DP>::BYTES : 16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Work w = work(p.tiles, p.heads / p.group, 1, false);
+  const Work w = work(p.tiles, p.heads / p.group, PARTS ? p.parts : 1, false);
   if (!w.here) return;
   const int row = w.tile * kRowsOf<SHARED> + (SHARED ? 0 : wave * 32) + (lane & 31);
   const int top = w.tile * kRowsOf<SHARED>, bottom = top + kRowsOf<SHARED> <= p.seq.rows ? top + kRowsOf<SHARED> - 1 : p.seq.rows - 1;
@@ -357,7 +361,7 @@ __device__ __forceinline__ void dkv(const AttentionParams& p) {
   const Reader<DTYPE, DP> read(lane);
   const float c = exponent(p.scale);
   SeenStage<DTYPE, DP, DIRECT, BN> stage;
-  const int head0 = w.kv * p.group, behind = head0 + p.group;
+  const int head0 = w.kv * p.group + (PARTS ? w.g * p.apiece : 0), behind = PARTS && (w.g + 1) * p.apiece < p.group ? head0 + p.apiece : (w.kv + 1) * p.group;
   stage.q.init(HeadRows{head_of<DTYPE>(p.q, head0), p.q.stride}, p.dim);
   stage.g.init(HeadRows{head_of<DTYPE>(p.d_o, head0), p.d_o.stride}, p.dim);
   unsigned found = 0;
@@ -404,12 +408,54 @@ __device__ __forceinline__ void dkv(const AttentionParams& p) {
     }
   }
   if (!mine) return;
-  store_column<DTYPE, DP>(keys.dk, p.scale, head_of<DTYPE>(p.dk, w.kv) + row * p.dk.stride, lane, p.dim);
-  store_column<DTYPE, DP>(keys.dv, 1.f, head_of<DTYPE>(p.dv, w.kv) + row * p.dv.stride, lane, p.dim);
+  if (PARTS && p.parts > 1) {
+    const int64_t kv_heads = p.heads / p.group, all = kv_heads * p.seq.rows, at = w.g * all + (int64_t)w.kv * p.seq.rows + row;
+    store_column<LSAM_DTYPE_FP32, DP>(keys.dk, p.scale, p.sums + at * p.dim, lane, p.dim);
+    store_column<LSAM_DTYPE_FP32, DP>(keys.dv, 1.f, p.sums + (p.parts * all + at) * p.dim, lane, p.dim);
+  } else {
+    store_column<DTYPE, DP>(keys.dk, p.scale, head_of<DTYPE>(p.dk, w.kv) + row * p.dk.stride, lane, p.dim);
+    store_column<DTYPE, DP>(keys.dv, 1.f, head_of<DTYPE>(p.dv, w.kv) + row * p.dv.stride, lane, p.dim);
+  }
 }
 
-template <int DTYPE, int DP, bool DIRECT, bool SHARED>
-__global__ __launch_bounds__(kThreads, SHARED ? 1 : kWavesOf<DTYPE>) void dkv_kernel(AttentionParams p) { dkv<DTYPE, DP, DIRECT, SHARED>(p); }
+template <int DTYPE, int DP, bool DIRECT, bool SHARED, bool PARTS>
+__global__ __launch_bounds__(kThreads, SHARED ? 1 : kWavesOf<DTYPE>) void dkv_kernel(AttentionParams p) { dkv<DTYPE, DP, DIRECT, SHARED, PARTS>(p); }
+
+// The sums of the workgroups that share a group's heads, in their order: a few rows of a head of keys a workgroup, four columns a lane.
+constexpr int kJoinRows = 8;
+template <int DTYPE>
+__global__ __launch_bounds__(256) void join_kernel(AttentionParams p) {
+  typedef typename Value<DTYPE>::T T;
+  const unsigned kv_heads = p.heads / p.group;
+  const int kv = blockIdx.x % kv_heads, top = blockIdx.x / kv_heads * kJoinRows, lane = threadIdx.x & 63;
+  const int bottom = top + kJoinRows <= p.seq.rows ? top + kJoinRows - 1 : p.seq.rows - 1;
+  const int row = top + lane % kJoinRows;
+  const Span span = span_of(p.seq, row, top, bottom);        // by all lanes
+  const unsigned long long valid = __ballot(row <= bottom && span.end > 0);
+  const unsigned pieces = (p.dim + 3) / 4;
+  const int64_t all = (int64_t)kv_heads * p.seq.rows * p.dim;
+  for (unsigned i = threadIdx.x; i < 2 * kJoinRows * pieces; i += 256) {
+    const unsigned line = i / pieces, local = line % kJoinRows;
+    const int col = (int)(i - line * pieces) * 4, n = p.dim - col < 4 ? p.dim - col : 4;
+    if (!(valid >> local & 1)) continue;
+    const bool of_v = line >= kJoinRows;
+    const float* from = p.sums + (of_v ? p.parts * all : 0) + ((int64_t)kv * p.seq.rows + top + local) * p.dim + col;
+    const Tensor& t = of_v ? p.dv : p.dk;
+    T* to = head_of<DTYPE>(t, kv) + (top + local) * t.stride + col;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    if (n == 4) {
+      for (int part = 0; part < p.parts; ++part) sum += *reinterpret_cast<const f32x4_any*>(from + part * all);
+    } else {
+      for (int part = 0; part < p.parts; ++part)
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+          if (e < n) sum[e] += from[part * all + e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < n) Value<DTYPE>::put(to + e, sum[e]);
+  }
+}
 
 int check(const lsam_attention_desc* d, const char* who) {
   if (!d) return refuse(LSAM_EINVAL, "%s: the descriptor is NULL", who);
@@ -444,11 +490,25 @@ AttentionParams params(const lsam_attention_desc* d, const int64_t* offsets) {
 }
 
 // Wavefronts share rows where workgroups of 128 rows would leave units without work.
-constexpr int kUnits = 256;
+constexpr int kUnits = 256, kPerUnit = 2;
+// Workgroups for keys: of 128 or of 32 keys, and how many share the heads of a group.
+struct OfKeys { bool share; int tiles, parts, apiece; };
+OfKeys of_keys(int64_t rows, int kv_heads, int group) {
+  const int64_t wide = (rows + kRowsOf<false> - 1) / kRowsOf<false>, narrow = (rows + kRowsOf<true> - 1) / kRowsOf<true>;
+  OfKeys c;
+  c.share = wide * kv_heads < kUnits;
+  c.tiles = (int)(c.share ? narrow : wide);
+  const int64_t all = (int64_t)c.tiles * kv_heads, want = all > 0 ? (kPerUnit * kUnits + all - 1) / all : 1;
+  c.apiece = want < group ? (int)((group + want - 1) / want) : 1;
+  c.parts = (group + c.apiece - 1) / c.apiece;
+  return c;
+}
+size_t stats_bytes(const AttentionParams& p) { return ((size_t)p.heads * p.padded * 8 + 255) / 256 * 256; }
+
 template <int DTYPE, int DP, bool DIRECT>
 int launch(AttentionParams p, bool backward, hipStream_t s) {
   const int rows = p.seq.rows, kv = p.heads / p.group, wide = (rows + kRowsOf<false> - 1) / kRowsOf<false>, narrow = (rows + kRowsOf<true> - 1) / kRowsOf<true>;
-  const bool share = (int64_t)wide * p.heads < kUnits, share_keys = (int64_t)wide * kv < kUnits;
+  const bool share = (int64_t)wide * p.heads < kUnits;
   p.tiles = share ? narrow : wide;
   const unsigned all = workgroups(p.tiles, kv, p.group);
   if (!backward) {
@@ -458,10 +518,15 @@ int launch(AttentionParams p, bool backward, hipStream_t s) {
   }
   if (share) dq_kernel<DTYPE, DP, DIRECT, true><<<all, kThreads, 0, s>>>(p);
   else dq_kernel<DTYPE, DP, DIRECT, false><<<all, kThreads, 0, s>>>(p);
-  p.tiles = share_keys ? narrow : wide;
-  const unsigned of_keys = workgroups(p.tiles, kv, 1);
-  if (share_keys) dkv_kernel<DTYPE, DP, DIRECT, true><<<of_keys, kThreads, 0, s>>>(p);
-  else dkv_kernel<DTYPE, DP, DIRECT, false><<<of_keys, kThreads, 0, s>>>(p);
+  const OfKeys c = of_keys(rows, kv, p.group);
+  p.tiles = c.tiles;
+  p.parts = c.parts;
+  p.apiece = c.apiece;
+  const unsigned groups = workgroups(c.tiles, kv, c.parts);
+  if (c.share) dkv_kernel<DTYPE, DP, DIRECT, true, true><<<groups, kThreads, 0, s>>>(p);
+  else if (c.parts > 1) dkv_kernel<DTYPE, DP, DIRECT, false, true><<<groups, kThreads, 0, s>>>(p);
+  else dkv_kernel<DTYPE, DP, DIRECT, false, false><<<groups, kThreads, 0, s>>>(p);
+  if (c.parts > 1) join_kernel<DTYPE><<<(unsigned)((rows + kJoinRows - 1) / kJoinRows * kv), 256, 0, s>>>(p);
   return launched();
 }
 template <int DTYPE, bool DIRECT>
@@ -505,7 +570,8 @@ extern "C" int lsam_attention(const lsam_attention_desc* d, const int64_t* offse
 extern "C" size_t lsam_attention_workspace_bytes(const lsam_attention_desc* d) {
   if (check(d, "attention") != LSAM_OK) return 0;
   const AttentionParams p = params(d, nullptr);
-  return (size_t)p.heads * p.padded * 2 * 4;
+  const OfKeys c = of_keys(d->rows, d->kv_heads, p.group);
+  return stats_bytes(p) + (c.parts > 1 ? (size_t)2 * c.parts * d->kv_heads * d->rows * d->dim * 4 : 0);
 }
 
 extern "C" int lsam_attention_backward(const lsam_attention_desc* d, const int64_t* offsets, const void* q, const void* k, const void* v, const void* o,
@@ -529,5 +595,6 @@ extern "C" int lsam_attention_backward(const lsam_attention_desc* d, const int64
   p.q = tensor(q, d->q); p.k = tensor(k, d->k); p.v = tensor(v, d->v); p.o = tensor(o, d->o);
   p.d_o = tensor(d_o, d->d_o); p.dq = tensor(dq, d->dq); p.dk = tensor(dk, d->dk); p.dv = tensor(dv, d->dv);
   p.lse = const_cast<float*>(lse); p.stats = static_cast<f32x2*>(workspace);
+  p.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + stats_bytes(p));
   return launch_any(p, d->dtype, true, static_cast<hipStream_t>(stream));
 }
