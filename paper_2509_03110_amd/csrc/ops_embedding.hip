@@ -215,8 +215,8 @@ __global__ __launch_bounds__(kOrderWaves * 64) void count_kernel(EmbeddingParams
 }
 
 // Each wavefront owns a run of places and a column of counters, so that places keep their order: counted first, then, from where each token's
-// places of the wavefront begin, put there.  Tokens of other ranges cost a load and two comparisons.  131072 places of 1000 tokens: 64 us with all places for each
-// of 250 workgroups.
+// places of the wavefront begin, put there.  Tokens of other ranges cost a load and two comparisons.  131072 places of 1000 tokens: 64 us
+// with all places for each of 250 workgroups, 18 and 8 for the counts with 16 parts of them; 4 x 4096 places of 32003 tokens 9 us, most of it latency.
 __global__ __launch_bounds__(kOrderWaves * 64) void order_kernel(EmbeddingParams p) {
   __shared__ uint32_t counts[kMaxRange * kOrderWaves], below[kOrderWaves];
   static_assert(kMaxRange <= kOrderWaves * 64, "a token a thread");
@@ -278,7 +278,8 @@ __device__ __forceinline__ void store4_past(float* p, f32x4 v, int n) {
   }
 }
 
-// The first p.units wavefronts of a replica sum, p.zeros more write zeros.
+// The first p.units wavefronts of a replica sum, p.zeros more write zeros.  Bound by memory: 131072 rows of 777 numbers of fp32, read in the order of their
+// tokens, take 123 us (3.3 TB/s); 4 x 4096 rows of 1024 with tables of 32003 rows, which are written whole, 105 us (5.3 TB/s).
 template <int DTYPE>
 __global__ __launch_bounds__(256) void sums_kernel(EmbeddingParams p) {
   typedef typename Value<DTYPE>::T T;
@@ -341,7 +342,7 @@ __global__ __launch_bounds__(256) void sums_kernel(EmbeddingParams p) {
 
 // A wavefront for each chunk, and kSlab columns, in which a token begins that goes on into the next: it adds the token's partial sums, or, where
 // they are more than kAlone, the workgroup's wavefronts add runs of them, which are added in their order.  A workgroup's units lie far apart, since
-// many partial sums of a token are those of neighbours.
+// many partial sums of a token are those of neighbours: 131072 places of 1000 tokens take 13 us, 28 with neighbours and 19 with a workgroup for each unit.
 constexpr int kAlone = 8;
 struct Joined { int64_t chunk, col, all; int32_t token; int n; };            // all: chunks behind this one; 0: nothing to join
 __device__ __forceinline__ Joined joined(const EmbeddingParams& p, unsigned unit, int64_t replica, int lane) {
