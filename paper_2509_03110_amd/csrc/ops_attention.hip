@@ -5,7 +5,8 @@
 //                     maximum and sum of each column, and adds the tile's part of o^T
 //   dq_kernel         the same walk: scores and d_o v again, ds, dq^T; leaves d_o o and lse of each row for
 //   dkv_kernel        a wavefront owns 32 keys, and walks over the rows that see them, head by head of the group: scores with queries as
-//                     rows, dv^T and dk^T.  No sum goes over workgroups, so no atomics
+//                     rows, dv^T and dk^T.  Where keys are few workgroups share a group's heads, and
+//   join_kernel       adds their sums in their order: no atomics
 //
 // Both gradients form the scores again: 7 products in place of 5, for results that do not depend on timing.
 //

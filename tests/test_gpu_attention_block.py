@@ -216,3 +216,42 @@ def test_tensors_elsewhere_and_of_other_types_are_refused():
                     with pytest.raises(lsam.LsamError) as e:
                         op(**tensors, **dict(rest, **{name: other}))
                     assert e.value.code == lsam.EINVAL, (op.__name__, name)
+
+
+def test_rows_and_places_whose_offsets_pass_32_bits():
+    """Rows 2^16 numbers apart, of which 70000 lie over 9 GB; sequences of a cache 2^32 numbers apart; a cache of 2^24 places: as in arrays of their own."""
+    g = torch.Generator(device=DEV).manual_seed(5)
+    n = lambda *s: torch.randn(*s, device=DEV, generator=g).to(B16)  # noqa: E731
+    rows = 70000
+    off = torch.cat([torch.arange(0, rows, 1000, device=DEV), torch.tensor([rows], device=DEV)])
+    wide = torch.empty(rows, 1 << 16, device=DEV, dtype=B16)
+    apart = [wide[:, 64 * i:64 * i + 64].unsqueeze(1) for i in range(8)]
+    compact = [n(rows, 1, 64) for _ in range(4)]
+    for a, c in zip(apart, compact):
+        a.copy_(c)
+    q, k, v, do = compact
+    r = ops.attention(q, k, v, off, save=True)
+    s = ops.attention(*apart[:3], off, save=True, out=apart[4])
+    assert torch.equal(r.o, s.o) and torch.equal(r.lse, s.lse)
+    want = ops.attention_backward(q, k, v, off, r.o, r.lse, do)
+    got = ops.attention_backward(*apart[:3], off, s.o, s.lse, apart[3], dq=apart[5], dk=apart[6], dv=apart[7])
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+    flat = wide.view(-1)                                       # 4.6e9 numbers
+    cache = [flat[i * 100000:].as_strided((2, 200, 2, 64), (1 << 32, 128, 64, 1)) for i in range(2)]
+    ck, cv, q = n(2, 200, 2, 64), n(2, 200, 2, 64), n(2, 4, 64)
+    cache[0].copy_(ck)
+    cache[1].copy_(cv)
+    lengths = torch.tensor([200, 133], dtype=torch.int32, device=DEV)
+    assert torch.equal(ops.attention_step(q, ck, cv, lengths), ops.attention_step(q, *cache, lengths))
+    del wide, apart, flat, cache
+
+    places = (1 << 24) + 5
+    k, v = torch.zeros(1, places, 1, 128, device=DEV, dtype=B16), torch.zeros(1, places, 1, 128, device=DEV, dtype=B16)
+    last = n(128)
+    k[0, -1], v[0, -1] = 4.0, last
+    q = torch.ones(1, 1, 128, device=DEV, dtype=B16)
+    # the last place weighs e^45 against 2^24: all but 6e-13
+    o = ops.attention_step(q, k, v, torch.tensor([places], dtype=torch.int32, device=DEV))
+    assert float((o.float() - last.float()).abs().max()) <= 2.0 ** -7 * float(last.float().abs().max())
+    assert not bool(ops.attention_step(q, k, v, torch.tensor([places - 1], dtype=torch.int32, device=DEV)).any())
