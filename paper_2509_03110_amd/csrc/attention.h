@@ -657,7 +657,7 @@ __device__ __forceinline__ Span span_of(const Sequences& q, int row, int top, in
     for (int step = 32; step; step >>= 1)
       if (from_lane(w, n + step - 1) <= row) n += step;
     const int b = from_lane(w, n > 0 ? n - 1 : 0), e = from_lane(w, n);
-    if (n > 0 && e != kNone) { r.begin = b; r.end = e; }
+    if (n > 0 && row < e && e != kNone) { r.begin = b; r.end = e; }       // (the search says 63 at most: for a row behind the last that may be its end)
     const int above = __popcll(__ballot(w <= top)), below = __popcll(__ballot(w <= bottom));
     if (above > 0 && above < 64 && __builtin_amdgcn_readlane(w, above < 64 ? above : 63) != kNone) r.top_begin = __builtin_amdgcn_readlane(w, above - 1);
     const int behind = below > 0 && below < 64 ? __builtin_amdgcn_readlane(w, below) : kNone;
