@@ -631,11 +631,11 @@ struct Sequences { const int64_t* offsets; int n; int rows; };
 __device__ __forceinline__ int last_before(const Sequences& q, int64_t row) {
   int lo = 0, hi = q.n;
   while (hi - lo > 64) {
-    const int mid = (lo + hi) >> 1;
+    const int mid = lo + ((hi - lo) >> 1);
     if (q.offsets[mid] <= row) lo = mid + 1; else hi = mid;
   }
-  const int i = lo + (int)(threadIdx.x & 63);
-  return lo + __popcll(__ballot(i < hi && q.offsets[i < hi ? i : 0] <= row)) - 1;
+  const int i = (int)(threadIdx.x & 63) < hi - lo ? lo + (int)(threadIdx.x & 63) : -1;
+  return lo + __popcll(__ballot(i >= 0 && q.offsets[i < 0 ? 0 : i] <= row)) - 1;
 }
 __device__ __forceinline__ int from_lane(int v, int lane) { return __builtin_amdgcn_ds_bpermute(lane << 2, v); }
 
@@ -648,8 +648,9 @@ __device__ __forceinline__ Span span_of(const Sequences& q, int row, int top, in
   const int lane = threadIdx.x & 63;
   int s0 = q.n > 63 ? last_before(q, top) : 0;
   s0 = s0 < 0 ? 0 : s0;
-  const int64_t offset = q.offsets[s0 + lane <= q.n ? s0 + lane : q.n];
-  const int w = s0 + lane > q.n ? kNone : offset < 0 ? 0 : offset < q.rows ? (int)offset : q.rows;
+  const bool there = lane <= q.n - s0;
+  const int64_t offset = q.offsets[there ? s0 + lane : q.n];
+  const int w = !there ? kNone : offset < 0 ? 0 : offset < q.rows ? (int)offset : q.rows;
   Span r{0, 0, top, bottom + 1};
   if (__builtin_amdgcn_readlane(w, 63) > bottom) {
     int n = 0;                                              // offsets at or before the lane's row
@@ -666,7 +667,7 @@ __device__ __forceinline__ Span span_of(const Sequences& q, int row, int top, in
     const auto find = [&](int of, int& begin, int& end) {
       int lo = 0, hi = q.n;
       while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
+        const int mid = lo + ((hi - lo) >> 1);
         if (q.offsets[mid] <= of) lo = mid + 1; else hi = mid;
       }
       if (lo == 0 || of >= q.rows) return;

@@ -56,3 +56,8 @@ def test_any_offsets(driver):
         values = [rng.randint(min(lo, hi), max(lo, hi)) for _ in range(rng.choice([n + 1, 3, 12]))]
         cases.append(case(rows, sorted(rng.choice(values) for _ in range(n + 1))))
     run(driver, "list", cases)
+
+
+def test_more_sequences_than_half_of_32_bits_count(driver):
+    """Numbers of sequences near the limits of int: nearly all are empty, of offsets that are not in memory."""
+    run(driver, "many", [[100, n, tail] for n in (2 ** 30 - 1, 2 ** 30 + 70, 2 ** 31 - 1) for tail in (1, 5, 100)])
