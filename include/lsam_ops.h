@@ -261,8 +261,8 @@ int lsam_residual_backward(const lsam_residual_desc* d, const void* r, const voi
  *          v may be parts of one array
  *   lse    [device] [heads, rows] floats that receive lse, for the backward pass, or NULL
  * Scores, sums and lse are fp32.  Products of fp32 operands are those of three bf16 pieces of each, six products in fp32: 2^-22 of |a| |b| at most is
- * left out.  bf16 operands meet probabilities rounded to bf16 (2^-8 of themselves, once, before the sum over j).  A p below 2^-126 is 0.  What is not finite in a row that i
- * does not see does not reach o_i. */
+ * left out.  bf16 operands meet probabilities rounded to bf16 (2^-8 of themselves, once, before the sum over j).  A p below 2^-126 is 0, and
+ * that of a score of -inf.  What is not finite in a row that i does not see does not reach o_i. */
 #define LSAM_ATTENTION_MAX_DIM 128
 #define LSAM_ATTENTION_MAX_SCALE 0x1p100f
 typedef struct {
@@ -296,7 +296,7 @@ int lsam_attention_backward(const lsam_attention_desc* d, const int64_t* offsets
 /* ---- attention of one token -----------------------------------------------------------------------
  * The step of generation: one query of each of `seqs` sequences attends to `prefix` keys and values that all sequences share (an instruction, or one
  * prompt of many answers), and then to the first lengths[s] of its own:  o = softmax(scale q k) v over both.  The prefix is read once for
- * all sequences.  With nothing to attend to o is 0.
+ * all sequences.  With nothing to attend to, or with scores that are all -inf, o is 0.
  *   q, o               [device] [seqs, heads, dim] of dtype
  *   k, v               [device] caches [seqs, capacity, kv_heads, dim] of dtype; places from lengths[s] on reach nothing
  *   lengths            [device] [seqs] int32; values outside 0..capacity are taken as the nearest inside

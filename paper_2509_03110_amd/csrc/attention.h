@@ -399,6 +399,19 @@ template <int DTYPE, int DP> constexpr int kLds = 2 * kTile<DTYPE> * Rows<DTYPE,
 struct No { static constexpr bool value = false; };
 struct Yes { static constexpr bool value = true; };
 
+// Whether a lane of the workgroup says so.
+__device__ __forceinline__ bool any_of_workgroup(bool v) {
+  __shared__ int shared[kThreads / 64];
+  const bool mine = __any(v);
+  __syncthreads();                                           // an answer before has been read
+  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = mine;
+  __syncthreads();
+  bool all = false;
+#pragma unroll
+  for (int i = 0; i < kThreads / 64; ++i) all |= shared[i] != 0;
+  return all;
+}
+
 // Keys lo .. hi in tiles, `f(tile of k, tile of v, first key)` for each.  Two tiles a turn in arrays of their own: so the compiler sees that what is
 // read is not what is on its way, and their places are constants.
 template <int DTYPE, int DP, bool DIRECT, typename F>
@@ -447,6 +460,41 @@ struct Seen {
   }
 };
 
+// The pieces of an infinity are itself, 0 and 0, and those of a finite number have any signs: their products, or such that pass the range of fp32, make a
+// NaN of a score that is -inf and weighs nothing.  So where sums are formed AGAIN because one is not finite, the scores of tile i, of rows
+// row0 + 32 i .., that are not are formed from the numbers as they are: row `column` of `own`, a lane's, with the rows first .. last.  A column that has met a NaN
+// or inf is `lost` either way.
+template <int DTYPE, bool AGAIN>
+struct Scores {
+  typedef typename Value<DTYPE>::T T;
+  HeadRows rows;
+  int row0;
+  HeadRows own;
+  int column, first, last, lane, dim;
+  bool& lost;
+  __device__ __forceinline__ void operator()(f32x16& s, int i) const {
+    if constexpr (AGAIN && Operand<DTYPE>::PLANES > 1) {
+      const int top = row0 + i * 32;
+      const Seen seen(first - top, last - top, lane);
+      unsigned bad = 0;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) bad |= seen(0, e) && !__builtin_isfinite(s[e]) ? 1u << e : 0u;
+      while (bad && !lost) {
+        const int r = __builtin_ctz(bad);
+        bad &= bad - 1;
+        const T* a = static_cast<const T*>(rows.p) + (top + result_row(r, lane)) * rows.stride;
+        const T* b = static_cast<const T*>(own.p) + column * own.stride;
+        float sum = 0.f;
+#pragma unroll 1
+        for (int d = 0; d < dim; ++d) sum += a[d] * b[d];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = e == r ? sum : s[e];
+        lost = !(sum < __builtin_inff());
+      }
+    }
+  }
+};
+
 // What a tile's products say to those who bring tiles: that its keys have been read, that its values are read next.
 struct Quiet {
   __device__ __forceinline__ void keys_read() const {}
@@ -455,9 +503,10 @@ struct Quiet {
   __device__ __forceinline__ void neither() const {}
 };
 
-template <int DTYPE, int DP, int TILES, bool CLEAN, typename B = Quiet>
+template <int DTYPE, int DP, int TILES, bool CLEAN, typename B>
 __device__ __forceinline__ void attend(Running<DP>& a, const Reader<DTYPE, DP>& read, const typename Operand<DTYPE>::F (&q)[DP / 16], const lds_byte* tk,
-                                       const lds_byte* tv, float c, int lane, bool masked, int first, int last, unsigned& found, const B& bring = B()) {
+                                       const lds_byte* tv, float c, int lane, bool masked, int first, int last, unsigned& found,
+                                       const Scores<DTYPE, CLEAN>& again, const B& bring) {
   typedef Operand<DTYPE> O;
   constexpr int STEPS = DP / 16;
   f32x16 s[TILES];
@@ -474,6 +523,8 @@ __device__ __forceinline__ void attend(Running<DP>& a, const Reader<DTYPE, DP>& 
     if constexpr (TILES == 2) s[1] = two[1];
   }
   bring.keys_read();
+#pragma unroll
+  for (int i = 0; i < TILES; ++i) again(s[i], i);
   if (masked) {
     const Seen seen(first, last, lane);
 #pragma unroll

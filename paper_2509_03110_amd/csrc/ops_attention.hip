@@ -78,24 +78,12 @@ __device__ __forceinline__ Range range_of(bool valid, int first, int last) {
                __builtin_amdgcn_readlane(last, low)};
 }
 
-// Whether a lane of the workgroup says so.
-__device__ __forceinline__ bool any_of_workgroup(bool v) {
-  __shared__ int shared[kThreads / 64];
-  const bool mine = __any(v);
-  __syncthreads();                                           // an answer before has been read
-  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = mine;
-  __syncthreads();
-  bool all = false;
-#pragma unroll
-  for (int i = 0; i < kThreads / 64; ++i) all |= shared[i] != 0;
-  return all;
-}
-
 template <int DTYPE>
 __device__ __forceinline__ typename Value<DTYPE>::T* head_of(const Tensor& t, int head) { return static_cast<typename Value<DTYPE>::T*>(t.p) + head * t.head; }
 
+// (64 numbers of fp32: two wavefronts a SIMD where rows are shared; the second pass would take that room, which the first does not need.)
 template <int DTYPE, int DP, bool DIRECT, bool SHARED>
-__global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void attention_kernel(AttentionParams p) {
+__global__ __launch_bounds__(kThreads, SHARED && DP == 64 ? 2 : kWavesOf<DTYPE>) void attention_kernel(AttentionParams p) {
   typedef typename Value<DTYPE>::T T;
   typedef Operand<DTYPE> O;
   constexpr int BN = kTile<DTYPE>, STEPS = DP / 16;
@@ -119,20 +107,23 @@ __global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void attention_kernel(At
   const HeadRows k{head_of<DTYPE>(p.k, w.kv), p.k.stride}, v{head_of<DTYPE>(p.v, w.kv), p.v.stride};
   Running<DP> a;
   unsigned found = 0;
+  bool lost = false;
   const auto pass = [&](auto clean) {
+    constexpr bool CLEAN = decltype(clean)::value;
+    const auto again = [&](int j0) { return Scores<DTYPE, CLEAN>{k, j0, HeadRows{head_of<DTYPE>(p.q, head), p.q.stride}, row, first, last, lane, p.dim, lost}; };
     a = Running<DP>();
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t) a.acc[t] = zero16();
     if constexpr (SHARED) {
       walk_shared<DTYPE, DP, DIRECT>(even, odd, k, v, lo, hi, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0, const auto& bring) {
         if (j0 > r.hi || j0 + 32 <= r.lo) return bring.neither();
-        attend<DTYPE, DP, 1, decltype(clean)::value>(a, read, q, tk, tv, c, lane, j0 < r.all_lo || j0 + 31 > r.all_hi, first - j0, last - j0, found, bring);
+        attend<DTYPE, DP, 1, CLEAN>(a, read, q, tk, tv, c, lane, j0 < r.all_lo || j0 + 31 > r.all_hi, first - j0, last - j0, found, again(j0), bring);
       });
       join_running<DTYPE, DP>(a, c, wave, lane, even, odd);
     } else {
       walk<DTYPE, DP, DIRECT>((lds_byte*)even, (lds_byte*)odd, k, v, lo, hi, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0) {
         if (j0 > r.hi || j0 + BN <= r.lo) return;
-        attend<DTYPE, DP, BN / 32, decltype(clean)::value>(a, read, q, tk, tv, c, lane, j0 < r.all_lo || j0 + BN - 1 > r.all_hi, first - j0, last - j0, found);
+        attend<DTYPE, DP, BN / 32, CLEAN>(a, read, q, tk, tv, c, lane, j0 < r.all_lo || j0 + BN - 1 > r.all_hi, first - j0, last - j0, found, again(j0), Quiet());
       });
       a.l += other_half(a.l);
     }
@@ -151,7 +142,8 @@ __global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void attention_kernel(At
 template <int DTYPE, int DP, int TILES, bool CLEAN>
 __device__ __forceinline__ void dq_tile(f32x16 (&acc)[DP / 32], const Reader<DTYPE, DP>& read, const typename Operand<DTYPE>::F (&q)[DP / 16],
                                         const typename Operand<DTYPE>::F (&g)[DP / 16], const lds_byte* tk, const lds_byte* tv, float c, float base,
-                                        float dot, int lane, bool masked, int first, int last, unsigned& found) {
+                                        float dot, int lane, bool masked, int first, int last, unsigned& found,
+                                        const Scores<DTYPE, CLEAN>& again) {
   typedef Operand<DTYPE> O;
 #pragma unroll
   for (int i = 0; i < TILES; ++i) {
@@ -160,6 +152,7 @@ __device__ __forceinline__ void dq_tile(f32x16 (&acc)[DP / 32], const Reader<DTY
                          [&](int n, const Few<DTYPE, 2>& a) {
                            multiply_few<DTYPE, 2>(a, [&](int j) -> const typename O::F& { return j ? g[n] : q[n]; }, [&](int j) -> f32x16& { return j ? d : s; });
                          });
+    again(s, i);
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(s[e] * c - base) * (d[e] - dot);
     if (masked) {
@@ -209,24 +202,27 @@ __global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void dq_kernel(Attention
   if (valid && lane < 32 && (!SHARED || wave == 0)) p.stats[head * p.padded + row] = f32x2{base, dot};
   const HeadRows k{head_of<DTYPE>(p.k, w.kv), p.k.stride}, v{head_of<DTYPE>(p.v, w.kv), p.v.stride};
   unsigned found = 0;
+  bool lost = false;
   f32x16 acc[DP / 32];
   const auto pass = [&](auto clean) {
+    constexpr bool CLEAN = decltype(clean)::value;
+    const auto again = [&](int j0) { return Scores<DTYPE, CLEAN>{k, j0, HeadRows{head_of<DTYPE>(p.q, head), p.q.stride}, row, first, last, lane, p.dim, lost}; };
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t) acc[t] = zero16();
     if constexpr (SHARED) {
       walk_shared<DTYPE, DP, DIRECT>(even, odd, k, v, lo, hi, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0, const auto& bring) {
         if (j0 > r.hi || j0 + 32 <= r.lo) return bring.neither();
         bring.both_next();
-        dq_tile<DTYPE, DP, 1, decltype(clean)::value>(acc, read, q, g, tk, tv, c, base, dot, lane, j0 < r.all_lo || j0 + 31 > r.all_hi, first - j0, last - j0,
-                                                      found);
+        dq_tile<DTYPE, DP, 1, CLEAN>(acc, read, q, g, tk, tv, c, base, dot, lane, j0 < r.all_lo || j0 + 31 > r.all_hi, first - j0, last - j0,
+                                                      found, again(j0));
         bring.keys_read();
       });
       join_sums<DTYPE, DP>(acc, wave, lane, even, odd);
     } else {
       walk<DTYPE, DP, DIRECT>((lds_byte*)even, (lds_byte*)odd, k, v, lo, hi, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0) {
         if (j0 > r.hi || j0 + BN <= r.lo) return;
-        dq_tile<DTYPE, DP, BN / 32, decltype(clean)::value>(acc, read, q, g, tk, tv, c, base, dot, lane, j0 < r.all_lo || j0 + BN - 1 > r.all_hi, first - j0,
-                                                            last - j0, found);
+        dq_tile<DTYPE, DP, BN / 32, CLEAN>(acc, read, q, g, tk, tv, c, base, dot, lane, j0 < r.all_lo || j0 + BN - 1 > r.all_hi, first - j0,
+                                                            last - j0, found, again(j0));
       });
     }
   };
@@ -255,7 +251,8 @@ template <int DTYPE, int DP, bool IN_LDS> struct Keys {
 // A tile of rows: scores and d_o v; p and ds of them; dv and dk.
 template <int DTYPE, int DP, bool CLEAN, bool IN_LDS>
 __device__ __forceinline__ void dkv_tile(Keys<DTYPE, DP, IN_LDS>& w, const Reader<DTYPE, DP>& read, const lds_byte* tq, const lds_byte* tg,
-                                         const lds_byte* stats, float c, int lane, bool masked, int first, int last, unsigned& found) {
+                                         const lds_byte* stats, float c, int lane, bool masked, int first, int last, unsigned& found,
+                                        const Scores<DTYPE, CLEAN>& again) {
   typedef Operand<DTYPE> O;
   typedef typename O::F F;
   typedef const __attribute__((address_space(3))) f32x4* quad_ptr;
@@ -272,6 +269,7 @@ __device__ __forceinline__ void dkv_tile(Keys<DTYPE, DP, IN_LDS>& w, const Reade
                          [&](int n, const Few<DTYPE, 2>& a) {
                            multiply_few<DTYPE, 2>(a, [&](int j) -> const F& { return j ? w.v[n] : w.k[n]; }, [&](int j) -> f32x16& { return j ? d : s; });
                          });
+  again(s, 0);
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
     const lds_byte* const at = stats + (8 * g + 4 * (lane >> 5)) * 8;
@@ -373,7 +371,9 @@ __device__ __forceinline__ void dkv(const AttentionParams& p) {
   stage.q.init(HeadRows{head_of<DTYPE>(p.q, head0), p.q.stride}, p.dim);
   stage.g.init(HeadRows{head_of<DTYPE>(p.d_o, head0), p.d_o.stride}, p.dim);
   unsigned found = 0;
+  bool lost = false;
   const auto pass = [&](auto clean) {
+    constexpr bool CLEAN = decltype(clean)::value;
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t) keys.dk[t] = keys.dv[t] = zero16();
     int head = head0;
@@ -385,13 +385,15 @@ __device__ __forceinline__ void dkv(const AttentionParams& p) {
         if constexpr (SHARED) stage.ask(tq, p, head, i0, hi + 1, wave);
         stage.put(tq);
         arrived();
-        const int mine = SHARED ? wave : 0, now = i0 + mine * 32;
+        const int mine = SHARED ? wave : 0, now = i0 + mine * 32, of = head;
         i0 += BN;
         if (i0 > hi) { i0 = lo; ++head; }
         if (!SHARED && head < behind) stage.ask((lds_byte*)(b ? even : odd), p, head, i0, hi + 1, wave);
         if (mine < BN / 32 && now <= r.hi && now + 32 > r.lo)
-          dkv_tile<DTYPE, DP, decltype(clean)::value, IN_LDS>(keys, read, tq + mine * EACH, tq + BYTES + mine * EACH, tq + 2 * BYTES + mine * 256, c, lane,
-                                                              now < r.all_lo || now + 31 > r.all_hi, first - now, last - now, found);
+          dkv_tile<DTYPE, DP, CLEAN, IN_LDS>(keys, read, tq + mine * EACH, tq + BYTES + mine * EACH, tq + 2 * BYTES + mine * 256, c, lane,
+                                             now < r.all_lo || now + 31 > r.all_hi, first - now, last - now, found,
+                                             Scores<DTYPE, CLEAN>{HeadRows{head_of<DTYPE>(p.q, of), p.q.stride}, now,
+                                                                  HeadRows{head_of<DTYPE>(p.k, w.kv), p.k.stride}, row, first, last, lane, p.dim, lost});
         if constexpr (SHARED) __syncthreads();               // one tile at a time
         if (head == behind) break;
       }

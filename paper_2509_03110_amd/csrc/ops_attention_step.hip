@@ -34,8 +34,9 @@ struct StepParams {
   float* sums; float* values;              // [parts][seqs heads][2], [parts][seqs heads][dim]
 };
 
+// (64 numbers of fp32: two wavefronts a SIMD, 43 us in place of 64 for eight sequences of 20000, 2 heads; the second pass would take that room.)
 template <int DTYPE, int DP, bool DIRECT>
-__global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void step_kernel(StepParams p) {
+__global__ __launch_bounds__(kThreads, DP == 64 ? 2 : kWavesOf<DTYPE>) void step_kernel(StepParams p) {
   typedef typename Value<DTYPE>::T T;
   typedef Operand<DTYPE> O;
   constexpr int STEPS = DP / 16, BN = kTile<DTYPE>;
@@ -98,25 +99,37 @@ __global__ __launch_bounds__(kThreads, kWavesOf<DTYPE>) void step_kernel(StepPar
   for (int s = 0; s < STEPS; ++s) q[s] = operand(load_part<DTYPE>(q_row, s, lane, valid ? p.dim : 0));
   const Reader<DTYPE, DP> read(lane);
   const float scale = exponent(p.scale);
-  unsigned found = 0;                                        // keys that are not there are zeros: nothing has to be told apart
+  unsigned found = 0;                                        // keys that are not there are zeros: nothing has to be told apart in a first pass
+  bool lost = false;
   Running<DP> a;
+  const auto pass = [&](auto clean) {
+    constexpr bool CLEAN = decltype(clean)::value;
+    const auto again = [&](int j0) { return Scores<DTYPE, CLEAN>{k, j0, HeadRows{q_row, 0}, 0, 0, to - 1, lane, p.dim, lost}; };
+    a = Running<DP>();
 #pragma unroll
-  for (int t = 0; t < DP / 32; ++t) a.acc[t] = zero16();
-  float l;
-  if (spread) {
-    walk<DTYPE, DP, DIRECT>((lds_byte*)even, (lds_byte*)odd, k, v, from, to - 1, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0) {
-      attend<DTYPE, DP, BN / 32, false>(a, read, q, tk, tv, scale, lane, j0 + BN > to, 0, to - 1 - j0, found);
-    });
-    l = a.l + other_half(a.l);
-  } else {
-    walk_shared<DTYPE, DP, DIRECT>(even, odd, k, v, from, to - 1, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0, const auto& bring) {
-      attend<DTYPE, DP, 1, false>(a, read, q, tk, tv, scale, lane, j0 + 32 > to, 0, to - 1 - j0, found, bring);
-    });
-    join_running<DTYPE, DP>(a, scale, wave, lane, even, odd);
-    if (wave > 0) return;
-    l = a.l;
+    for (int t = 0; t < DP / 32; ++t) a.acc[t] = zero16();
+    if (spread) {
+      walk<DTYPE, DP, DIRECT>((lds_byte*)even, (lds_byte*)odd, k, v, from, to - 1, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0) {
+        attend<DTYPE, DP, BN / 32, CLEAN>(a, read, q, tk, tv, scale, lane, j0 + BN > to, 0, to - 1 - j0, found, again(j0), Quiet());
+      });
+      a.l += other_half(a.l);
+    } else {
+      walk_shared<DTYPE, DP, DIRECT>(even, odd, k, v, from, to - 1, p.dim, [&](const lds_byte* tk, const lds_byte* tv, int j0, const auto& bring) {
+        attend<DTYPE, DP, 1, CLEAN>(a, read, q, tk, tv, scale, lane, j0 + 32 > to, 0, to - 1 - j0, found, again(j0), bring);
+      });
+      join_running<DTYPE, DP>(a, scale, wave, lane, even, odd);
+    }
+  };
+  pass(No());
+  const bool mine = valid && (spread || wave == 0);          // this wavefront has results
+  if constexpr (O::PLANES > 1) {                             // pieces of what is not finite: again, with such numbers told apart
+    if (any_of_workgroup(mine && not_finite(a.acc))) {
+      pass(Yes());
+      if (any_of_workgroup(found != 0)) add_what_is_seen<DTYPE, DP>(a.acc, v, from, to, 0, to - 1, lane, p.dim);
+    }
   }
-  if (!valid) return;
+  if (!mine) return;
+  const float l = a.l;
   if (p.whole) {
     store_column<DTYPE, DP>(a.acc, l == 0.f ? 0.f : 1.f / l, static_cast<T*>(p.o) + seq * p.o_stride + head * p.o_head, lane, p.dim);
   } else {
