@@ -263,9 +263,10 @@ __device__ __forceinline__ void arrived() {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
-// Whether rows are whole units, and a tile within 32-bit offsets; bf16 ones have to be aligned to go to LDS directly.
+// Whether rows are whole units, a tile within 32-bit offsets, and rows behind the last one behind its bytes too, where loads give 0; bf16 ones have to be
+// aligned to go to LDS directly.
 inline bool direct(const void* p, int64_t stride, int64_t head, int64_t seq, int dim, int dtype) {
-  if (dim % 8 || stride >= 1 << 20) return false;
+  if (dim % 8 || stride < dim || stride >= 1 << 20) return false;
   return dtype == LSAM_DTYPE_FP32 || (!misaligned(p, 16) && stride % 8 == 0 && head % 8 == 0 && seq % 8 == 0);
 }
 

@@ -137,3 +137,21 @@ def test_one_token_that_meets_only_scores_of_minus_infinity(dtype):
     c = caches(3, 4, 2, 64, 90, 0, dtype)
     c["k"][..., 3] = -math.inf
     assert bool((ops.attention_step(**c) == 0).all())
+
+
+@TYPES
+def test_places_behind_the_length_that_share_memory_with_those_before(dtype):
+    """Strides below the width: what lies behind a sequence's last place is part of places that it has, infinite ones among them, and still weighs nothing."""
+    S, H, KV, dim, cap, n = 3, 4, 2, 64, 60, 37
+    g = torch.Generator(device=DEV).manual_seed(11)
+    q = torch.randn(S, H, dim, device=DEV, generator=g).to(dtype)
+    lengths = torch.full((S,), n, dtype=torch.int32, device=DEV)
+    for step in (0, 8, 32):
+        base = torch.randn(2, S, KV, 2048 + dim, device=DEV, generator=g).to(dtype)
+        base[1, :, :, (n - 1) * step + dim - 1] = math.inf                      # the last number of the last place
+        k, v = (t.as_strided((S, cap, KV, dim), (KV * (2048 + dim), step, 2048 + dim, 1), t.storage_offset()) for t in base)
+        got = ops.attention_step(q, k, v, lengths)
+        same(got, ops.attention_step(q, k.contiguous(), v.contiguous(), lengths), step)
+        assert bool((got[..., -1] == math.inf).all()) and bool(got[..., :dim - max(step, 1)].isfinite().all())
+        prefix = ops.attention_step(q, k[:, :0], v[:, :0], lengths, prefix_k=k[0, :n], prefix_v=v[0, :n])
+        same(prefix, ops.attention_step(q, k[:, :0], v[:, :0], lengths, prefix_k=k[0, :n].contiguous(), prefix_v=v[0, :n].contiguous()), step)
