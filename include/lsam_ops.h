@@ -217,7 +217,8 @@ int lsam_embedding_backward(const lsam_embedding_desc* d, const int32_t* tokens,
  *   w_pre      [device] replicas times [dim] floats, or NULL: no h
  *   r_out, h   [device] of dtype.  r_out may be r itself (same pointer and strides)
  * y NULL (before the first block): r' is r, nothing is joined, and r_out, gate and w_post are not looked at.
- * Sums are fp32: a row whose squares pass its range has n(x) = 0.  What is not finite in a row reaches no other row. */
+ * Sums are fp32: a row whose squares pass its range, or whose mean x^2 + eps is below its normal numbers (2^-126), has n(x) = 0, and no gradient through
+ * it.  What is not finite in a row reaches no other row. */
 #define LSAM_RESIDUAL_MAX_DIM 16384
 typedef struct {
   int32_t replicas;                          /* 0..65535                                     */

@@ -163,8 +163,12 @@ __device__ __forceinline__ float squares(const float (&v)[CH][8]) {
     for (int e = 0; e < 8; ++e) s += v[c][e] * v[c][e];
   return s;
 }
-// 1 / sqrt(mean x^2 + eps)
-__device__ __forceinline__ float inverse(float squares, const ResidualParams& p) { return 1.f / __builtin_sqrtf(squares / (float)p.dim + p.eps); }
+// 1 / sqrt(mean x^2 + eps); 0 where that mean is below the normal numbers, as 1 / inf is where it is above: squares lose digits there, down to 1 / 0.  (From
+// 2^-126 on what underflow takes from dim squares, half a step of 2^-149 each, is at most 2^-24 of their sum.)
+__device__ __forceinline__ float inverse(float squares, const ResidualParams& p) {
+  const float mean = squares / (float)p.dim + p.eps;
+  return mean < 0x1p-126f ? 0.f : 1.f / __builtin_sqrtf(mean);
+}
 
 // Rows of a workgroup of the forward pass: where a wavefront holds one, four.
 template <int WAVES> constexpr int kRowsOf = WAVES == 1 ? 4 : 1;
