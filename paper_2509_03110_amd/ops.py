@@ -614,6 +614,10 @@ def residual_backward(r, y, w_pre, dr, dh, w_post=None, gate=None, alpha=1.0, be
 Attention = namedtuple("Attention", "o lse")
 
 
+def _scale(dim, scale):
+    return max(dim, 1) ** -0.5 if scale is None else scale
+
+
 def _attention_desc(q, k, v, offsets, scale):
     for t, what in ((q, "q"), (k, "k"), (v, "v")):
         if t.dim() != 3:
@@ -626,7 +630,7 @@ def _attention_desc(q, k, v, offsets, scale):
     _expect(k, "k", q, (rows, kv_heads, dim), q.dtype)
     _expect(v, "v", q, (rows, kv_heads, dim), q.dtype)
     _expect(offsets, "the offsets", q, None, torch.int64, True)
-    return lsam_attention_desc(rows, offsets.shape[0] - 1, heads, kv_heads, dim, _dtype(q, "q"), dim ** -0.5 if scale is None else scale,
+    return lsam_attention_desc(rows, offsets.shape[0] - 1, heads, kv_heads, dim, _dtype(q, "q"), _scale(dim, scale),
                                q.stride()[:2], k.stride()[:2], v.stride()[:2])
 
 
@@ -698,7 +702,7 @@ def attention_step(q, k, v, lengths, prefix_k=None, prefix_v=None, scale=None, o
     ks, vs = k.stride(), v.stride()
     with _On(q, stream) as raw:
         o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
-        d = lsam_attention_step_desc(seqs, capacity, prefix, heads, kv_heads, dim, _dtype(q, "q"), dim ** -0.5 if scale is None else scale,
+        d = lsam_attention_step_desc(seqs, capacity, prefix, heads, kv_heads, dim, _dtype(q, "q"), _scale(dim, scale),
                                      q.stride()[:2], o.stride()[:2], ks[1:3], vs[1:3], ks[0], vs[0], pk, pv)
         need = L.lsam_attention_step_workspace_bytes(C.byref(d))
         ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
