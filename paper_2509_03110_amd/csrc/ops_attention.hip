@@ -11,11 +11,13 @@
 // Both gradients form the scores again: 7 products in place of 5, for results that do not depend on timing.
 //
 // Rounded to bf16, for products of bf16 operands: p (o, dv) and ds (dq, dk), each by half a step at most and once.  Held in two pieces they would cost
-// half the products again; gradients are off by 2.5e-3 of their norm with it, 1.7e-3 of which is the rounding of what is stored.
+// half the products again.  d_o o is that of o as it was stored: exact ones, sums of p d_o v, would cost dq_kernel a second walk.  Off from the definition in 64 bits,
+// of the norm, at 2048, 256, 16 and 2 rows a sequence: o 2.1e-3, 1.9e-3, 1.7e-3, 1.1e-3; dq and dk 2.5e-3, 2.6e-3, 3.1e-3, 4.4e-3; dv 2.3e-3, 2.3e-3, 2.2e-3, 1.9e-3.  The
+// rounding of what is stored is 1.7e-3 by itself.
 //
 // Bound by the vector unit beside the matrix unit, which is busy for 43 to 49 % of the time: exponentials, maxima and roundings of a tile take as long as
-// its products, and the two of a wavefront do not overlap.  Four sequences of 4096, 16 heads of 128 over 4: 300 us forward (0.92 PFLOP/s), dq 440 us
-// (0.94), dk and dv 690 us (0.80).
+// its products, and the two of a wavefront do not overlap.  Four sequences of 4096, 16 heads of 128 over 4: 302 us forward (0.91 PFLOP/s), dq 428 us
+// (0.96), dk and dv 648 us (0.85); together 1378 with a profiler attached, 1348 without.
 #include "attention.h"
 
 namespace lsam {

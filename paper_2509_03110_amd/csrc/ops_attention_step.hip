@@ -6,9 +6,9 @@
 //                each.  A part leaves the maximum, the sum and the weighted values of each column
 //   join_kernel  weighs the parts against each other
 //
-// Bound by memory once keys are many: eight sequences of up to 100000, 2 heads of 64 bf16 numbers: 54 us, 5.6 TB/s.  64 sequences, 32 heads of 128 over 8: a prefix
-// of 16001 alone 48 us (each of its keys meets 256 queries: 2.9 times as long as its products take at the rate of large ones), caches of 768 alone 40 (5.0 TB/s), both 60
-// in one launch.  One sequence: 8 us and 4 for joining, two launches that follow each other.
+// Bound by memory once keys are many: eight sequences of up to 100000, 2 heads of 64 bf16 numbers: 53 us, 5.6 TB/s.  64 sequences, 32 heads of 128 over 8: a prefix
+// of 16001 alone 48 us (each of its keys meets 256 queries: 2.9 times as long as its products take at the rate of large ones), caches of 768 alone 40 (5.0 TB/s), both 64
+// in one launch.  One sequence: 8 us and 5 for joining, two launches that follow each other.
 #include "attention.h"
 
 namespace lsam {

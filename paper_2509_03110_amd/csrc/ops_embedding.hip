@@ -279,7 +279,7 @@ __device__ __forceinline__ void store4_past(float* p, f32x4 v, int n) {
 }
 
 // The first p.units wavefronts of a replica sum, p.zeros more write zeros.  Bound by memory: 131072 rows of 777 numbers of fp32, read in the order of their
-// tokens, take 123 us (3.3 TB/s); 4 x 4096 rows of 1024 with tables of 32003 rows, which are written whole, 105 us (5.3 TB/s).
+// tokens, take 126 us (3.3 TB/s); 4 x 4096 rows of 1024 with tables of 32003 rows, which are written whole, 105 us (5.3 TB/s).
 template <int DTYPE>
 __global__ __launch_bounds__(256) void sums_kernel(EmbeddingParams p) {
   typedef typename Value<DTYPE>::T T;

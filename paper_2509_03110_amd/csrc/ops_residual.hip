@@ -4,8 +4,9 @@
 // lane, or sixteen, and as many wavefronts as that takes.  The sums over a row go through a wavefront's lanes and LDS.  The
 // backward pass forms both norms again from r' and y, of which it needs every number anyway; its sums over rows stay in
 // registers while a workgroup walks over some of a replica's rows, and a second launch adds those of the workgroups.
-// Bound by memory.  3 x 5001 x 1001 fp32 (240 MB, which the last-level cache holds in part): 38 us, 6.3 TB/s; the gradient of 8 x 2048 x 4096 bf16 with gate and
-// both weights (1.07 GB): 227 us, 4.7 TB/s, and 8 for the workgroups' sums.
+// Bound by memory.  3 x 5001 x 1001 fp32 (240 MB, which the last-level cache holds in part): 39 us, 6.2 TB/s; the gradient of 8 x 2048 x 4096 bf16 with gate and
+// both weights (1.07 GB): 228 us, 4.7 TB/s, 8 of them for the workgroups' sums.  Registers do not hold what the gradient keeps of rows of more than 8192 numbers, nor of more
+// than 4096 of fp32: 540 MB of 8192 numbers a row take 149 us in bf16 and 182 in fp32, of 16384 639 and 604 (540 and 768 bytes a lane in memory).
 #include "ops.h"
 
 namespace lsam {
